@@ -46,29 +46,29 @@ def _q4_case(N, d, group, B):
 def listed():
     cases = {
         # the smallest catalogue, one position: launches and what the host does around them
-        "codes, tiny, 1 position": _codes_case(10_000, 4, 256, 1, "step"),
+        "codes tiny 1 position": _codes_case(10_000, 4, 256, 1, "step"),
         # a Gowalla-sized catalogue, the last positions of 64 users
-        "codes, gowalla, 64 positions": _codes_case(1_280_000, 8, 256, 64, "step"),
+        "codes gowalla 64 positions": _codes_case(1_280_000, 8, 256, 64, "step"),
         # the data set's own odd number of items, popular sub-ids, a full training batch
-        "codes, gowalla, 1024 positions": _codes_case(1_271_638, 8, 256, 1024, "step", "zipf", 3.5),
+        "codes gowalla 1024 positions": _codes_case(1_271_638, 8, 256, 1024, "step", "zipf", 3.5),
         # validation loss over a larger catalogue with finer codes
-        "codes, finer, loss of 16": _codes_case(5_000_000, 16, 256, 16, "loss"),
+        "codes finer loss of 16": _codes_case(5_000_000, 16, 256, 16, "loss"),
         # dense head of a small catalogue, an odd batch of short sequences: latency
-        "dense, tiny, 50 positions": _dense_case(10_000, 64, 50, "float32"),
+        "dense tiny 50 positions": _dense_case(10_000, 64, 50, "float32"),
         # dense head of a hotel catalogue (Booking.com's 34,742 items), 32-bit training
-        "dense, booking, 2048 positions": _dense_case(34_742, 512, 2048, "float32"),
+        "dense booking 2048 positions": _dense_case(34_742, 512, 2048, "float32"),
         # dense head of the large catalogue in bfloat16: few positions, bound by W
-        "dense, gowalla, 64 positions": _dense_case(1_271_638, 512, 64, "bfloat16"),
+        "dense gowalla 64 positions": _dense_case(1_271_638, 512, 64, "bfloat16"),
         # ... and a training batch, bound by the matrix cores
-        "dense, gowalla, 1024 positions": _dense_case(1_280_000, 512, 1024, "bfloat16"),
+        "dense gowalla 1024 positions": _dense_case(1_280_000, 512, 1024, "bfloat16"),
         # tables of one query back to its embedding
-        "eq4, tiny, 1 query": _eq4_case(64, 4, 256, 1),
+        "eq4 tiny 1 query": _eq4_case(64, 4, 256, 1),
         # ... of a training batch
-        "eq4, 1024 queries": _eq4_case(512, 8, 256, 1024),
+        "eq4 1024 queries": _eq4_case(512, 8, 256, 1024),
         # one user of the large catalogue, dense scores from four bits
-        "q4, gowalla, one user": _q4_case(1_280_000, 512, 64, 1),
+        "q4 gowalla one user": _q4_case(1_280_000, 512, 64, 1),
         # a batch of users collected over a few milliseconds
-        "q4, gowalla, 16 users": _q4_case(1_271_638, 512, 128, 16),
+        "q4 gowalla 16 users": _q4_case(1_271_638, 512, 128, 16),
     }
     return [dict(case, name=name) for name, case in cases.items()]
 
