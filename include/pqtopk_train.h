@@ -1,0 +1,87 @@
+/*
+ * pqtopk_train.h -- training the scoring head: the catalogue's softmax cross entropy and its gradients.
+ *
+ * The items of the catalogue are the model's vocabulary.  For the sequence embedding phi_q of a position with the
+ * target item t_q, and the scores r_qi of all N items,
+ *
+ *     lse_q  = log sum_i exp r_qi            loss_q = lse_q - r_{q,t_q}
+ *     d loss_q / d r_qi = exp(r_qi - lse_q) - [i = t_q]
+ *
+ * Scores are either Eq. 5's sums of m sub-item scores (pq_cross_entropy: the codebook stands for the items, the gradient
+ * is the score tables' and pq_subitem_scores_backward() takes it on to phi and Psi) or the default scorer's W phi
+ * (pq_default_cross_entropy: gradients of phi and W).  No score and no probability of the N items is kept: the backward
+ * calls compute them again, piece by piece.
+ *
+ * Conventions are those of pqtopk.h (device pointers, row-major, caller's stream, no allocation, no synchronisation,
+ * arguments checked before anything is enqueued), and besides:
+ *   - targets are int32 item ids.  A position whose target lies outside [0, N) has none (padding): its lse is computed,
+ *     its loss is 0 and it adds nothing to any gradient.
+ *   - grad_loss is float [B], the gradient of the final objective with respect to loss_q (1 / count for a mean).
+ *   - Softmax statistics and all sums are held in 32 bits or more.  Every result is the same from run to run: no sum
+ *     depends on the order in which workgroups or waves finish.
+ *   - workspace: at least the bytes that the call's _workspace_bytes function names, 16-byte aligned; contents on entry
+ *     are irrelevant; calls that share one must not overlap in time.  Those functions are host arithmetic and return 0
+ *     for arguments that the call would reject.
+ */
+#ifndef PQTOPK_TRAIN_H
+#define PQTOPK_TRAIN_H
+
+#include "pqtopk.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * Loss and log-sum of B positions by sub-ids: r_qi = sum_k S[q][k][codes[i][k]].
+ *   codes    in   uint8 [N][m]     codebook G (Eq. 1), sub-ids < b (16-byte aligned);  uint16 [N][m] for the _u16 call
+ *   S        in   float [B][m][b]  from pq_subitem_scores().  Entries may be -inf (a sub-id out of play: its items have
+ *                                  probability 0); a position for which nothing is left has lse = -inf, loss 0, no gradient
+ *   targets  in   int32 [B]
+ *   loss     out  float [B];  lse  out  float [B]
+ * b <= 256 for one-byte sub-ids, <= 65536 for two bytes.  A sub-id >= b makes the result unspecified; nothing outside the
+ * arguments is touched.
+ * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, B, m, b < 1; b too large; N >= 2^31), PQ_ERR_UNSUPPORTED (m > PQ_MAX_M,
+ *         B > PQ_MAX_B, or one query's table too large for LDS: m * max(b, 256) <= 36864 for one-byte sub-ids, m * b <=
+ *         36864 for two), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
+ */
+size_t pq_cross_entropy_workspace_bytes(long long N, int B, int m, int b);
+int pq_cross_entropy(const uint8_t* codes, const float* S, const int* targets, long long N, int B, int m, int b,
+                     float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t pq_cross_entropy_u16_workspace_bytes(long long N, int B, int m, int b);
+int pq_cross_entropy_u16(const uint16_t* codes, const float* S, const int* targets, long long N, int B, int m, int b,
+                         float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradient of sum_q grad_loss[q] * loss[q] with respect to the score tables:
+ *     dS[q][k][j] = grad_loss[q] * ( sum_{i: codes[i][k] = j} exp(r_qi - lse_q) - [codes[t_q][k] = j] )
+ *   lse  in  float [B]  as returned by pq_cross_entropy() for the same codes and S
+ *   dS   out float [B][m][b]
+ * Probabilities are summed as whole multiples of 2^-62 in 64 bits, so the order of the additions does not matter.
+ * Errors: as pq_cross_entropy().
+ */
+size_t pq_cross_entropy_backward_workspace_bytes(long long N, int B, int m, int b);
+int pq_cross_entropy_backward(const uint8_t* codes, const float* S, const int* targets, const float* lse,
+                              const float* grad_loss, long long N, int B, int m, int b, float* dS, void* workspace,
+                              size_t workspace_bytes, void* stream);
+size_t pq_cross_entropy_u16_backward_workspace_bytes(long long N, int B, int m, int b);
+int pq_cross_entropy_u16_backward(const uint16_t* codes, const float* S, const int* targets, const float* lse,
+                                  const float* grad_loss, long long N, int B, int m, int b, float* dS, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/*
+ * Eq. 4's gradients: for S[q][k][j] = psi_{k,j} . phi_{q,k} and a gradient dS of the tables,
+ *     dqueries[q][k s + e] = sum_j dS[q][k][j] * psi[k][j][e]      dcentroids[k][j][e] = sum_q dS[q][k][j] * phi[q][k s + e]
+ * with s = d / m.  Either output may be NULL (not both): it is not computed.
+ *   dS float [B][m][b];  queries float [B][d];  centroids float [m][b][s];  dqueries float [B][d];  dcentroids float [m][b][s]
+ * Sums in float32 by fused multiply-adds, in an order that depends on the shape alone.
+ * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (B, d, m, b < 1; d % m; b > 65536), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B, m > PQ_MAX_M),
+ *         PQ_ERR_ALIGN, PQ_ERR_HIP.
+ */
+int pq_subitem_scores_backward(const float* dS, const float* queries, const float* centroids, float* dqueries,
+                               float* dcentroids, int B, int d, int m, int b, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* PQTOPK_TRAIN_H */

@@ -8,7 +8,10 @@ from __future__ import annotations
 __all__ = ["workloads", "pq_subitem_scores", "pq_score_topk", "pq_score_topk_workspace_bytes", "pq_score_topk_u16",
            "pq_score_topk_u16_workspace_bytes", "pq_score_topk_subset",
            "pq_score_topk_subset_workspace_bytes", "pq_topk_scores", "pq_topk_scores_workspace_bytes", "pq_recjpq_scores",
-           "pq_reconstruct_items", "pq_default_scores", "pq_strerror"]
+           "pq_reconstruct_items", "pq_default_scores", "pq_strerror", "pq_cross_entropy", "pq_cross_entropy_workspace_bytes",
+           "pq_cross_entropy_backward", "pq_cross_entropy_backward_workspace_bytes", "pq_cross_entropy_u16",
+           "pq_cross_entropy_u16_workspace_bytes", "pq_cross_entropy_u16_backward", "pq_cross_entropy_u16_backward_workspace_bytes",
+           "pq_subitem_scores_backward"]
 
 
 def __getattr__(name):

@@ -87,6 +87,14 @@ def lib() -> ctypes.CDLL:
         L.pq_measure_plan.restype = I
         L.pq_measure_step_stamps.argtypes = [P, P, P, LL, I, I, I, I, I, P, P, P, P, SZ, P, SZ, ctypes.POINTER(I * 2), P]
         L.pq_measure_step_stamps.restype = I
+        for width in ("", "_u16"):
+            for call, pointers, outputs in (("pq_cross_entropy" + width, 3, 2), ("pq_cross_entropy" + width + "_backward", 5, 1)):
+                size = getattr(L, call + "_workspace_bytes")
+                size.argtypes, size.restype = [LL, I, I, I], SZ
+                getattr(L, call).argtypes = [P] * pointers + [LL, I, I, I] + [P] * outputs + [P, SZ, P]
+                getattr(L, call).restype = I
+        L.pq_subitem_scores_backward.argtypes = [P, P, P, P, P, I, I, I, I, P]
+        L.pq_subitem_scores_backward.restype = I
         L.pq_strerror.argtypes = [I]
         L.pq_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -385,6 +393,137 @@ def pq_default_scores(W: torch.Tensor, queries: torch.Tensor, out: Optional[torc
     if rc != PQ_OK:
         raise PQError(rc, "pq_default_scores")
     return out
+
+
+def _per_position(t: Optional[torch.Tensor], B: int, like: torch.Tensor, what: str) -> torch.Tensor:
+    """A float32 vector of one value per position: the caller's, checked, or a new one."""
+    if t is None:
+        return torch.empty(B, dtype=torch.float32, device=like.device)
+    _dev(t, torch.float32, what)
+    if tuple(t.shape) != (B,):
+        raise ValueError(f"{what} must have one value per position")
+    return t
+
+
+def _targets(targets: torch.Tensor, B: int) -> torch.Tensor:
+    _dev(targets, torch.int32, "targets")
+    if tuple(targets.shape) != (B,):
+        raise ValueError("targets must have one item id per position")
+    return targets
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor) -> torch.Tensor:
+    """The caller's workspace, or one of `need` bytes (the call reports one that is too small)."""
+    if workspace is None:
+        return torch.empty(max(need, 16), dtype=torch.uint8, device=like.device)
+    return _dev(workspace, torch.uint8, "workspace")
+
+
+def _same_device(first: torch.Tensor, *others: torch.Tensor) -> None:
+    if any(t.device != first.device for t in others):
+        raise ValueError("all tensors of a call must live on one device")
+
+
+def _cross_entropy(entry: str, code_type, codes, S, targets, workspace, loss, lse):
+    _dev(codes, code_type, "codes")
+    _dev(S, torch.float32, "S")
+    if codes.dim() != 2 or S.dim() != 3 or S.shape[1] != codes.shape[1]:
+        raise PQError(PQ_ERR_SHAPE, entry)
+    (N, m), (B, _, b) = codes.shape, S.shape
+    _targets(targets, B)
+    loss, lse = _per_position(loss, B, S, "loss"), _per_position(lse, B, S, "lse")
+    workspace = _scratch(workspace, int(getattr(lib(), entry + "_workspace_bytes")(N, B, m, b)), S)
+    _same_device(codes, S, targets, loss, lse, workspace)
+    rc = getattr(lib(), entry)(codes.data_ptr(), S.data_ptr(), targets.data_ptr(), N, B, m, b, loss.data_ptr(), lse.data_ptr(),
+                               workspace.data_ptr(), workspace.numel(), _stream())
+    if rc != PQ_OK:
+        raise PQError(rc, entry)
+    return loss, lse
+
+
+def _cross_entropy_backward(entry: str, code_type, codes, S, targets, lse, grad_loss, workspace, out):
+    _dev(codes, code_type, "codes")
+    _dev(S, torch.float32, "S")
+    if codes.dim() != 2 or S.dim() != 3 or S.shape[1] != codes.shape[1]:
+        raise PQError(PQ_ERR_SHAPE, entry)
+    (N, m), (B, _, b) = codes.shape, S.shape
+    _targets(targets, B)
+    _per_position(lse, B, S, "lse"), _per_position(grad_loss, B, S, "grad_loss")
+    if out is None:
+        out = torch.empty_like(S)
+    _dev(out, torch.float32, "dS")
+    if out.shape != S.shape:
+        raise ValueError("dS must have the shape of S")
+    workspace = _scratch(workspace, int(getattr(lib(), entry + "_workspace_bytes")(N, B, m, b)), S)
+    _same_device(codes, S, targets, lse, grad_loss, out, workspace)
+    rc = getattr(lib(), entry)(codes.data_ptr(), S.data_ptr(), targets.data_ptr(), lse.data_ptr(), grad_loss.data_ptr(), N, B, m, b,
+                               out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream())
+    if rc != PQ_OK:
+        raise PQError(rc, entry)
+    return out
+
+
+def pq_cross_entropy_workspace_bytes(N: int, B: int, m: int, b: int) -> int:
+    return int(lib().pq_cross_entropy_workspace_bytes(N, B, m, b))
+
+
+def pq_cross_entropy(codes: torch.Tensor, S: torch.Tensor, targets: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                     loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Softmax cross entropy of the whole catalogue by sub-ids: codes uint8 [N][m], S fp32 [B][m][b], targets int32 [B] (an id
+    outside [0, N): no target) -> (loss fp32 [B], lse fp32 [B])."""
+    return _cross_entropy("pq_cross_entropy", torch.uint8, codes, S, targets, workspace, loss, lse)
+
+
+def pq_cross_entropy_backward_workspace_bytes(N: int, B: int, m: int, b: int) -> int:
+    return int(lib().pq_cross_entropy_backward_workspace_bytes(N, B, m, b))
+
+
+def pq_cross_entropy_backward(codes: torch.Tensor, S: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor,
+                              workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of sum(grad_loss * loss) with respect to S: lse as pq_cross_entropy returned it -> dS fp32 [B][m][b]."""
+    return _cross_entropy_backward("pq_cross_entropy_backward", torch.uint8, codes, S, targets, lse, grad_loss, workspace, out)
+
+
+def pq_cross_entropy_u16_workspace_bytes(N: int, B: int, m: int, b: int) -> int:
+    return int(lib().pq_cross_entropy_u16_workspace_bytes(N, B, m, b))
+
+
+def pq_cross_entropy_u16(codes: torch.Tensor, S: torch.Tensor, targets: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                         loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """pq_cross_entropy over 16-bit sub-ids: codes uint16 [N][m]."""
+    return _cross_entropy("pq_cross_entropy_u16", torch.uint16, codes, S, targets, workspace, loss, lse)
+
+
+def pq_cross_entropy_u16_backward_workspace_bytes(N: int, B: int, m: int, b: int) -> int:
+    return int(lib().pq_cross_entropy_u16_backward_workspace_bytes(N, B, m, b))
+
+
+def pq_cross_entropy_u16_backward(codes: torch.Tensor, S: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor,
+                                  workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """pq_cross_entropy_backward over 16-bit sub-ids: codes uint16 [N][m]."""
+    return _cross_entropy_backward("pq_cross_entropy_u16_backward", torch.uint16, codes, S, targets, lse, grad_loss, workspace, out)
+
+
+def pq_subitem_scores_backward(dS: torch.Tensor, queries: torch.Tensor, centroids: torch.Tensor, dqueries: Optional[torch.Tensor] = None,
+                               dcentroids: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Eq. 4's gradients: dS fp32 [B][m][b], queries [B][d], centroids [m][b][d/m] -> (dqueries [B][d], dcentroids [m][b][d/m])."""
+    for t, what in ((dS, "dS"), (queries, "queries"), (centroids, "centroids")):
+        _dev(t, torch.float32, what)
+    if dS.dim() != 3 or queries.dim() != 2 or centroids.dim() != 3:
+        raise PQError(PQ_ERR_SHAPE, "pq_subitem_scores_backward")
+    (B, d), (m, b, s) = queries.shape, centroids.shape
+    if tuple(dS.shape) != (B, m, b) or m * s != d:
+        raise PQError(PQ_ERR_SHAPE, "pq_subitem_scores_backward")
+    dqueries = torch.empty_like(queries) if dqueries is None else _dev(dqueries, torch.float32, "dqueries")
+    dcentroids = torch.empty_like(centroids) if dcentroids is None else _dev(dcentroids, torch.float32, "dcentroids")
+    if dqueries.shape != queries.shape or dcentroids.shape != centroids.shape:
+        raise ValueError("gradients must have the shapes of queries and centroids")
+    _same_device(dS, queries, centroids, dqueries, dcentroids)
+    rc = lib().pq_subitem_scores_backward(dS.data_ptr(), queries.data_ptr(), centroids.data_ptr(), dqueries.data_ptr(),
+                                          dcentroids.data_ptr(), B, d, m, b, _stream())
+    if rc != PQ_OK:
+        raise PQError(rc, "pq_subitem_scores_backward")
+    return dqueries, dcentroids
 
 
 def pq_score_topk_profile(codes: torch.Tensor, S: torch.Tensor, K: int, iters: int,

@@ -1,0 +1,39 @@
+// What the kernels that train the scoring head share: constants, cross-lane steps, the host's checks.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace pqk {
+
+// pqtopk.hip: keeps HIP's text for pq_strerror() and returns PQ_ERR_HIP, or PQ_OK for hipSuccess.
+__attribute__((visibility("hidden"))) int record_hip_error(hipError_t e);
+
+namespace head {
+
+constexpr int kWave = 64;
+constexpr int kCUs = 256;                            // MI355X; only sizes grids and workspaces
+constexpr size_t kMaxLds = 160 * 1024;               // LDS per workgroup on gfx950
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp, results below 2^-126 become 0
+
+// A sum of exponentials held as scale and mantissa: total = s * 2^c.  c = -inf: nothing yet (s = 0).
+__device__ __forceinline__ void join_sums(float& c, float& s, float c2, float s2) {
+    const float top = fmaxf(c, c2);
+    const float at = top == -__builtin_inff() ? 0.0f : top;
+    s = s * exp2_fast(c - at) + s2 * exp2_fast(c2 - at);
+    c = top;
+}
+
+template <typename F>
+inline hipError_t allow_lds(F* kernel, size_t bytes) {
+    if (bytes <= 64 * 1024) return hipSuccess;
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+inline size_t round_up(size_t a, size_t to) { return (a + to - 1) / to * to; }
+
+}  // namespace head
+}  // namespace pqk

@@ -40,6 +40,7 @@
 #include "pqtopk.h"
 #include "pqtopk_measure.h"
 #include "kernels.hpp"
+#include "head_common.hpp"
 
 // Built-in scratch of pq_score_topk_static(): device memory, one copy per GPU, held until the process ends.  Host code
 // never uses this name as an address (it is a handle for hipGetSymbolAddress(), see static_scratch() below).
@@ -1594,6 +1595,8 @@ int static_scratch(void** out) {
 }
 
 }  // namespace
+
+int pqk::record_hip_error(hipError_t e) { return record_hip(e); }
 
 extern "C" {
 
