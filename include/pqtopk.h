@@ -208,6 +208,32 @@ int pq_reconstruct_items(const uint8_t* codes, const float* centroids, long long
 int pq_default_scores(const float* W, const float* queries, long long N, int B, int d, float* scores, long long ld,
                       void* stream);
 
+/*
+ * The default scorer's item embeddings in four bits: a group of `group` neighbouring elements of a row shares a scale,
+ * element e of item i stands for scales[i][e / group] * (n - 8) with n in 0..15.
+ *   W       in   float [N][d]             (16-byte aligned)
+ *   packed  out  uint8 [N][d / 2]         (16-byte aligned) element 2j in the low half of byte j, 2j + 1 in the high half
+ *   scales  out  bfloat16 [N][d / group]  the group's largest absolute value / 7, rounded to bfloat16 (nearest even); weights
+ *                                         are then rounded to the nearest multiple of the rounded scale (ties to even) and
+ *                                         held within -8 .. 7 times it
+ * group is 32, 64 or 128 and divides d.
+ * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, d < 1, another group, d % group, N >= 2^31), PQ_ERR_UNSUPPORTED (d > 16384),
+ *         PQ_ERR_ALIGN, PQ_ERR_HIP.
+ */
+int pq_quantise_items(const float* W, long long N, int d, int group, uint8_t* packed, uint16_t* scales, void* stream);
+
+/*
+ * Eq. 3's scores from such embeddings: scores[q][i] = sum_e scales[i][e / group] * (n[i][e] - 8) * phi_q[e], for
+ * pq_topk_scores() to rank.  One pass over the embeddings serves up to 32 queries.
+ *   queries in float [B][d];  scores out float [B][ld], ld >= N
+ * A query's elements are taken as whole multiples of 2^-30 of a power of two above its largest one; sums within a group are
+ * exact integers, the sum over groups is float32.  A query that holds an infinity or a NaN has NaN scores.
+ * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (as above; B < 1, ld < N), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B; d > 9600, 4800 for groups
+ *         of 32: a query's digits would not fit LDS), PQ_ERR_ALIGN, PQ_ERR_HIP.
+ */
+int pq_default_scores_q4(const uint8_t* packed, const uint16_t* scales, const float* queries, long long N, int B, int d,
+                         int group, float* scores, long long ld, void* stream);
+
 /* Text for a PQ_* code; for PQ_ERR_HIP the text of the most recent HIP error seen by this thread. */
 const char* pq_strerror(int code);
 

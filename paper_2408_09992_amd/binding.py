@@ -95,6 +95,10 @@ def lib() -> ctypes.CDLL:
                 getattr(L, call).restype = I
         L.pq_subitem_scores_backward.argtypes = [P, P, P, P, P, I, I, I, I, P]
         L.pq_subitem_scores_backward.restype = I
+        L.pq_quantise_items.argtypes = [P, LL, I, I, P, P, P]
+        L.pq_quantise_items.restype = I
+        L.pq_default_scores_q4.argtypes = [P, P, P, LL, I, I, I, P, LL, P]
+        L.pq_default_scores_q4.restype = I
         L.pq_strerror.argtypes = [I]
         L.pq_strerror.restype = ctypes.c_char_p
         _lib = L
@@ -392,6 +396,53 @@ def pq_default_scores(W: torch.Tensor, queries: torch.Tensor, out: Optional[torc
     rc = lib().pq_default_scores(W.data_ptr(), queries.data_ptr(), N, B, d, out.data_ptr(), out.shape[1], _stream())
     if rc != PQ_OK:
         raise PQError(rc, "pq_default_scores")
+    return out
+
+
+def pq_quantise_items(W: torch.Tensor, group: int = 64, packed: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None
+                      ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Item embeddings in four bits: W fp32 [N][d] -> (packed uint8 [N][d/2], scales bf16 [N][d/group]); group 32, 64 or 128."""
+    _dev(W, torch.float32, "W")
+    if W.dim() != 2 or group < 1 or W.shape[1] % group:
+        raise PQError(PQ_ERR_SHAPE, "pq_quantise_items")
+    N, d = W.shape
+    if packed is None:
+        packed = torch.empty((N, d // 2), dtype=torch.uint8, device=W.device)
+    if scales is None:
+        scales = torch.empty((N, d // group), dtype=torch.bfloat16, device=W.device)
+    _dev(packed, torch.uint8, "packed")
+    _dev(scales, torch.bfloat16, "scales")
+    if tuple(packed.shape) != (N, d // 2) or tuple(scales.shape) != (N, d // group):
+        raise ValueError("packed must be [N][d/2] and scales [N][d/group]")
+    _same_device(W, packed, scales)
+    rc = lib().pq_quantise_items(W.data_ptr(), N, d, group, packed.data_ptr(), scales.data_ptr(), _stream())
+    if rc != PQ_OK:
+        raise PQError(rc, "pq_quantise_items")
+    return packed, scales
+
+
+def pq_default_scores_q4(packed: torch.Tensor, scales: torch.Tensor, queries: torch.Tensor, out: Optional[torch.Tensor] = None
+                         ) -> torch.Tensor:
+    """Eq. 3 from four-bit item embeddings: packed uint8 [N][d/2], scales bf16 [N][d/group], queries fp32 [B][d] -> scores
+    fp32 [B][ld] (ld = N rounded up to a multiple of 4 when allocated here)."""
+    _dev(packed, torch.uint8, "packed")
+    _dev(scales, torch.bfloat16, "scales")
+    _dev(queries, torch.float32, "queries")
+    if packed.dim() != 2 or scales.dim() != 2 or queries.dim() != 2:
+        raise PQError(PQ_ERR_SHAPE, "pq_default_scores_q4")
+    (N, half), (B, d) = packed.shape, queries.shape
+    if scales.shape[0] != N or half * 2 != d or scales.shape[1] < 1 or d % scales.shape[1]:
+        raise PQError(PQ_ERR_SHAPE, "pq_default_scores_q4")
+    if out is None:
+        out = torch.empty((B, (N + 3) // 4 * 4), dtype=torch.float32, device=packed.device)
+    _dev(out, torch.float32, "scores")
+    if out.dim() != 2 or out.shape[0] != B:
+        raise ValueError("scores must be [B][ld]")
+    _same_device(packed, scales, queries, out)
+    rc = lib().pq_default_scores_q4(packed.data_ptr(), scales.data_ptr(), queries.data_ptr(), N, B, d, d // scales.shape[1],
+                                    out.data_ptr(), out.shape[1], _stream())
+    if rc != PQ_OK:
+        raise PQError(rc, "pq_default_scores_q4")
     return out
 
 
