@@ -81,6 +81,37 @@ int pq_cross_entropy_u16_backward(const uint16_t* codes, const float* S, const i
 int pq_subitem_scores_backward(const float* dS, const float* queries, const float* centroids, float* dqueries,
                                float* dcentroids, int B, int d, int m, int b, void* stream);
 
+#define PQ_FLOAT32  0        /* `type` of the calls below: what W, queries and their gradients hold */
+#define PQ_BFLOAT16 1
+#define PQ_FLOAT16  2
+
+/*
+ * Loss and log-sum of B positions by the default scorer: r_qi = W[i] . phi_q.
+ *   W        in   type [N][d]   (16-byte aligned);   queries  in  type [B][d]  (16-byte aligned)
+ *   targets  in   int32 [B];    loss, lse  out  float [B]
+ * Scores are float32 sums of the products on the matrix cores (16-bit inputs: exact products); they are never stored.
+ * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, B, d < 1; an unknown type; N >= 2^31), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B, d > 16384,
+ *         d no multiple of 16 bytes of elements: 4 of float32, 8 of 16-bit types), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
+ */
+size_t pq_default_cross_entropy_workspace_bytes(long long N, int B, int d, int type);
+int pq_default_cross_entropy(const void* W, const void* queries, const int* targets, long long N, int B, int d, int type,
+                             float* loss, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of sum_q grad_loss[q] * loss[q] with respect to queries and W:
+ *     dz_qi = grad_loss[q] * (exp(r_qi - lse_q) - [i = t_q])     dqueries = dz W     dW = dz^T queries
+ *   lse  in  float [B]  as returned by pq_default_cross_entropy() for the same W and queries
+ *   dqueries  out  type [B][d];  dW  out  type [N][d]  (both 16-byte aligned, every element written)
+ * The items are taken in pieces whose dz fits the workspace (2^26 elements, more for more than 32768 positions).  dz is
+ * held in the inputs' type, scaled so that float16 keeps probabilities down to 2^-39; the products' sums are float32,
+ * rounded to the type once.
+ * Errors: as pq_default_cross_entropy().
+ */
+size_t pq_default_cross_entropy_backward_workspace_bytes(long long N, int B, int d, int type);
+int pq_default_cross_entropy_backward(const void* W, const void* queries, const int* targets, const float* lse,
+                                      const float* grad_loss, long long N, int B, int d, int type, void* dqueries, void* dW,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -95,6 +95,11 @@ def lib() -> ctypes.CDLL:
                 getattr(L, call).restype = I
         L.pq_subitem_scores_backward.argtypes = [P, P, P, P, P, I, I, I, I, P]
         L.pq_subitem_scores_backward.restype = I
+        for call in ("pq_default_cross_entropy", "pq_default_cross_entropy_backward"):
+            size = getattr(L, call + "_workspace_bytes")
+            size.argtypes, size.restype = [LL, I, I, I], SZ
+            getattr(L, call).argtypes = [P] * (3 if call.endswith("entropy") else 5) + [LL, I, I, I, P, P, P, SZ, P]
+            getattr(L, call).restype = I
         L.pq_quantise_items.argtypes = [P, LL, I, I, P, P, P]
         L.pq_quantise_items.restype = I
         L.pq_default_scores_q4.argtypes = [P, P, P, LL, I, I, I, P, LL, P]
@@ -553,6 +558,66 @@ def pq_cross_entropy_u16_backward(codes: torch.Tensor, S: torch.Tensor, targets:
                                   workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """pq_cross_entropy_backward over 16-bit sub-ids: codes uint16 [N][m]."""
     return _cross_entropy_backward("pq_cross_entropy_u16_backward", torch.uint16, codes, S, targets, lse, grad_loss, workspace, out)
+
+
+PQ_FLOAT32, PQ_BFLOAT16, PQ_FLOAT16 = 0, 1, 2
+_TYPES = {torch.float32: PQ_FLOAT32, torch.bfloat16: PQ_BFLOAT16, torch.float16: PQ_FLOAT16}
+
+
+def _dense_args(entry, W, queries, targets):
+    if W.dtype not in _TYPES:
+        raise ValueError("W must be float32, bfloat16 or float16")
+    _dev(W, W.dtype, "W")
+    _dev(queries, W.dtype, "queries")
+    if W.dim() != 2 or queries.dim() != 2 or W.shape[1] != queries.shape[1]:
+        raise PQError(PQ_ERR_SHAPE, entry)
+    (N, d), B = W.shape, queries.shape[0]
+    _targets(targets, B)
+    return N, B, d, _TYPES[W.dtype]
+
+
+def pq_default_cross_entropy_workspace_bytes(N: int, B: int, d: int, type: int) -> int:
+    return int(lib().pq_default_cross_entropy_workspace_bytes(N, B, d, type))
+
+
+def pq_default_cross_entropy(W: torch.Tensor, queries: torch.Tensor, targets: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                             loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Softmax cross entropy of the whole catalogue by W phi: W [N][d], queries [B][d] (both fp32, bf16 or fp16), targets int32 [B]
+    (an id outside [0, N): no target) -> (loss fp32 [B], lse fp32 [B])."""
+    N, B, d, type = _dense_args("pq_default_cross_entropy", W, queries, targets)
+    loss, lse = _per_position(loss, B, W, "loss"), _per_position(lse, B, W, "lse")
+    workspace = _scratch(workspace, pq_default_cross_entropy_workspace_bytes(N, B, d, type), W)
+    _same_device(W, queries, targets, loss, lse, workspace)
+    rc = lib().pq_default_cross_entropy(W.data_ptr(), queries.data_ptr(), targets.data_ptr(), N, B, d, type, loss.data_ptr(),
+                                        lse.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream())
+    if rc != PQ_OK:
+        raise PQError(rc, "pq_default_cross_entropy")
+    return loss, lse
+
+
+def pq_default_cross_entropy_backward_workspace_bytes(N: int, B: int, d: int, type: int) -> int:
+    return int(lib().pq_default_cross_entropy_backward_workspace_bytes(N, B, d, type))
+
+
+def pq_default_cross_entropy_backward(W: torch.Tensor, queries: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
+                                      grad_loss: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                                      dqueries: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None
+                                      ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Gradients of sum(grad_loss * loss) with respect to queries and W, in their type: lse as pq_default_cross_entropy returned it."""
+    N, B, d, type = _dense_args("pq_default_cross_entropy_backward", W, queries, targets)
+    _per_position(lse, B, W, "lse"), _per_position(grad_loss, B, W, "grad_loss")
+    dqueries = torch.empty_like(queries) if dqueries is None else _dev(dqueries, W.dtype, "dqueries")
+    dW = torch.empty_like(W) if dW is None else _dev(dW, W.dtype, "dW")
+    if dqueries.shape != queries.shape or dW.shape != W.shape:
+        raise ValueError("gradients must have the shapes of queries and W")
+    workspace = _scratch(workspace, pq_default_cross_entropy_backward_workspace_bytes(N, B, d, type), W)
+    _same_device(W, queries, targets, lse, grad_loss, dqueries, dW, workspace)
+    rc = lib().pq_default_cross_entropy_backward(W.data_ptr(), queries.data_ptr(), targets.data_ptr(), lse.data_ptr(),
+                                                 grad_loss.data_ptr(), N, B, d, type, dqueries.data_ptr(), dW.data_ptr(),
+                                                 workspace.data_ptr(), workspace.numel(), _stream())
+    if rc != PQ_OK:
+        raise PQError(rc, "pq_default_cross_entropy_backward")
+    return dqueries, dW
 
 
 def pq_subitem_scores_backward(dS: torch.Tensor, queries: torch.Tensor, centroids: torch.Tensor, dqueries: Optional[torch.Tensor] = None,

@@ -1,0 +1,214 @@
+// A tile of a matrix product C[r][c] = sum_k A(r, k) B(c, k) on the matrix cores, for 16-bit and float32 operands, each of
+// them stored either with k running along its rows ("along": element (r, k) at base + r ld + k) or across them ("across":
+// element (r, k) at base + k ld + r).
+//
+// Both operands come to LDS by asynchronous 16-byte loads, three stages of 64 bytes of k (32 16-bit elements, 16 floats), so
+// two stages are in flight while one is multiplied.  A stage's chunks of 16 bytes are swapped within their row so that the
+// reads of a matrix operand meet every bank: the load picks its source accordingly, as it writes LDS in lane order.
+//   along:  [row][4 chunks], chunk c of row r lies at c ^ (r / 4 % 4); an operand is one 16-byte read
+//   across: [k][chunks of the rows], 16-bit: chunk c of row k lies at c ^ 4 (k % 4); an operand is two transposing reads
+// A lane's operand is 16 bytes in either case: row lane % 32, and of k eight (16-bit: one 32x32x16 instruction) or four
+// (float32: four 32x32x2 instructions, whose order of k is the same for A and B).
+#pragma once
+#include <type_traits>
+#include "head_common.hpp"
+
+namespace pqk {
+namespace head {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+static __device__ const uint4 kZeros = {0u, 0u, 0u, 0u};
+
+constexpr int kStageBytes = 64, kStages = 3;
+
+struct Operand {
+    const void* base;
+    size_t ld;             // bytes from one stored row to the next
+    long long row0;        // first row (r) of the tile
+    long long rows;        // rows there are: past the last one the last is read again
+    long long k0, k1;      // range of k: past k1 zeros are read
+};
+
+template <typename T> struct Mfma;
+template <> struct Mfma<__bf16> {
+    static __device__ __forceinline__ f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mfma<_Float16> {
+    static __device__ __forceinline__ f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Mfma<float> {
+    static __device__ __forceinline__ f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// ROWS rows of an operand, as a workgroup of THREADS brings them to LDS and its waves read them.
+template <typename T, int ROWS, bool ALONG, int THREADS>
+struct Side {
+    static constexpr int kBytes = ROWS * kStageBytes;                      // of a stage
+    static constexpr int kK = kStageBytes / (int)sizeof(T);                // k of a stage
+    static constexpr int kRowChunks = ROWS * (int)sizeof(T) / 16;          // across: chunks of a stored row
+    static constexpr int kLoads = kBytes / 16 / THREADS;                   // asynchronous loads of a thread and stage
+    static_assert(kBytes % (16 * THREADS) == 0, "every wave loads as much");
+
+    const char* base;                                                      // moves on stage by stage
+    size_t ld;
+    uint32_t offset[kLoads];
+    long long k, k1;
+
+    int tid;
+
+    __device__ __forceinline__ void start(const Operand& o) {
+        tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));                                      // (so that a loop over tiles does not keep all this in registers meanwhile)
+        k = o.k0; k1 = o.k1; ld = o.ld;
+        if constexpr (ALONG) base = static_cast<const char*>(o.base) + (size_t)o.row0 * ld + (size_t)o.k0 * sizeof(T);
+        else base = static_cast<const char*>(o.base) + (size_t)o.k0 * ld + (size_t)o.row0 * sizeof(T);
+        const int last = (int)min((long long)ROWS, o.rows - o.row0) - 1;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int at = (tid / kWave * kLoads + i) * kWave + tid % kWave;
+            if constexpr (ALONG) {
+                const int row = at / 4, chunk = (at % 4) ^ (row / 4 % 4);
+                offset[i] = (uint32_t)min(row, last) * (uint32_t)ld + (uint32_t)chunk * 16u;
+            } else {
+                const int kk = at / kRowChunks, chunk = swap(at % kRowChunks, kk), most = last * (int)sizeof(T) / 16;
+                offset[i] = (uint32_t)kk * (uint32_t)ld + (uint32_t)min(chunk, most) * 16u;
+            }
+        }
+    }
+    static __device__ __forceinline__ int swap(int chunk, int kk) { return sizeof(T) == 2 ? chunk ^ (4 * (kk % 4)) : chunk; }
+
+    __device__ __forceinline__ void load(unsigned char* stage) {
+        unsigned char* to = stage + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (kLoads * kWave * 16);
+        const bool whole = k + kK <= k1;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const char* from = base + offset[i];
+            if (!whole) {                                                  // (the same for all lanes)
+                const int at = (tid / kWave * kLoads + i) * kWave + tid % kWave;
+                const int kk = ALONG ? ((at % 4) ^ (at / 4 / 4 % 4)) * (16 / (int)sizeof(T)) : at / kRowChunks;
+                if (k + kk >= k1) from = reinterpret_cast<const char*>(&kZeros);
+            }
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                             (__attribute__((address_space(3))) void*)(to + i * kWave * 16), 16, 0, 0);
+        }
+        k += kK;
+        base += ALONG ? (size_t)kStageBytes : (size_t)kK * ld;
+    }
+
+    // the operand of rows row0 .. + 31 and the u-th half of the stage
+    static __device__ __forceinline__ s16x8 read(const unsigned char* stage, int row0, int u) {
+        const int lane = threadIdx.x % kWave;
+        if constexpr (ALONG) {
+            const int row = row0 + lane % 32;
+            return *reinterpret_cast<const s16x8*>(stage + row * kStageBytes + (((2 * u + lane / 32) ^ (row / 4 % 4)) * 16));
+        } else if constexpr (sizeof(T) == 2) {
+            // sixteen lanes read four stored rows of sixteen elements and get a column each
+            const int kk = 16 * u + 8 * (lane / 32) + lane % 16 / 4, row = row0 + 16 * (lane / 16 % 2) + 4 * (lane % 4);
+            const unsigned char* p = stage + kk * (ROWS * 2) + (swap(row / 8, kk) * 16) + row % 8 * 2;
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 4 * (ROWS * 2)));
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            const unsigned char* p = stage + (8 * u + 4 * (lane / 32)) * (ROWS * 4) + (row0 + lane % 32) * 4;
+            f32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float*>(p + i * (ROWS * 4));
+            return __builtin_bit_cast(s16x8, v);
+        }
+    }
+};
+
+// BM x BN tile by waves in a grid of (BM / WM) x (BN / WN).  acc[mi][ni][i] is row 32 mi + 8 (i / 4) + 4 (lane / 32) + i % 4,
+// column 32 ni + lane % 32 of the wave's part.
+template <typename T, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG>
+struct MatrixTile {
+    static constexpr int kThreads = BM / WM * (BN / WN) * kWave;
+    static constexpr int MI = WM / 32, NI = WN / 32;
+    using A = Side<T, BM, A_ALONG, kThreads>;
+    using B = Side<T, BN, B_ALONG, kThreads>;
+
+    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
+    static __device__ __forceinline__ int wave_row() { return wave() / (BN / WN) * WM; }
+    static __device__ __forceinline__ int wave_col() { return wave() % (BN / WN) * WN; }
+
+    static __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, f32x16 (&acc)[MI][NI]) {
+        // (an array per stage and side: the compiler tells loads into one from reads of another, and waits for no more than it must)
+        __shared__ __align__(16) unsigned char a0[A::kBytes], a1[A::kBytes], a2[A::kBytes], b0[B::kBytes], b1[B::kBytes], b2[B::kBytes];
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = f32x16{};
+        A a;
+        B b;
+        a.start(oa);
+        b.start(ob);
+        const int steps = (int)((oa.k1 - oa.k0 + A::kK - 1) / A::kK);
+        const int row0 = wave_row(), col0 = wave_col();
+
+        auto load = [&](int stage) {
+            a.load(stage == 0 ? a0 : stage == 1 ? a1 : a2);
+            b.load(stage == 0 ? b0 : stage == 1 ? b1 : b2);
+        };
+        auto step = [&](auto stage_c) {
+            constexpr int stage = decltype(stage_c)::value;
+            const unsigned char* sa = stage == 0 ? a0 : stage == 1 ? a1 : a2;
+            const unsigned char* sb = stage == 0 ? b0 : stage == 1 ? b1 : b2;
+            // this stage's loads are done when only the next one's are in flight; past the barrier that holds for every
+            // wave, and every wave is done with the stage that is loaded next
+            wait_loads<A::kLoads + B::kLoads>();
+            s16x8 x[2][MI], y[2][NI];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi) x[u][mi] = A::read(sa, row0 + 32 * mi, u);
+#pragma unroll
+                for (int ni = 0; ni < NI; ++ni) y[u][ni] = B::read(sb, col0 + 32 * ni, u);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load((stage + 2) % 3);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = Mfma<T>::multiply(x[u][mi], y[u][ni], acc[mi][ni]);
+        };
+        // Two stages more than there are get loaded (zeros): the count of loads in flight is the same in every step, and the
+        // compiler, which counts them too, finds nothing else to wait for.
+        load(0);
+        load(1);
+        for (int s = 0;;) {
+            step(std::integral_constant<int, 0>{});
+            if (++s >= steps) break;
+            step(std::integral_constant<int, 1>{});
+            if (++s >= steps) break;
+            step(std::integral_constant<int, 2>{});
+            if (++s >= steps) break;
+        }
+        wait_loads<0>();                                       // nothing is on its way to LDS, or being read there, any more
+    }
+
+    // All but the wave's last LEFT loads have arrived and its LDS reads are done; then the workgroup's barrier.
+    template <int LEFT>
+    static __device__ __forceinline__ void wait_loads() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+    }
+};
+
+}  // namespace head
+}  // namespace pqk

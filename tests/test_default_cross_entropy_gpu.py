@@ -1,0 +1,218 @@
+"""Softmax cross entropy of the catalogue by W phi and its gradients, against the definitions in 64 bits on the same inputs.
+
+u = 2^-24 is float32's unit, U_T the type's (2^-8 bfloat16, 2^-11 float16, u float32).  A score is a float32 sum of d
+products: off by at most (d + 2) u times the sum of their absolute values; log-sum and probability as for the sub-ids.  dz is
+rounded to the type (relative U_T; float16 besides 2^-40 of the largest |g|), the products sum n terms (n + 8 u of the sum of
+absolute values) and are rounded to the type once more."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": (torch.float32, U), "bf16": (torch.bfloat16, 2.0 ** -8), "f16": (torch.float16, 2.0 ** -11)}
+
+
+def draw(N, d, B, type, seed, spread=2.5):
+    rng = np.random.default_rng(seed)
+    dtype = TYPES[type][0]
+    W = torch.from_numpy((rng.standard_normal((N, d)) * d ** -0.5).astype(np.float32)).to(dtype).cuda()
+    H = torch.from_numpy((rng.standard_normal((B, d)) * spread).astype(np.float32)).to(dtype).cuda()
+    targets = torch.from_numpy(rng.integers(0, N, B).astype(np.int32)).cuda()
+    grad = torch.from_numpy(rng.standard_normal(B).astype(np.float32)).cuda()
+    return W, H, targets, grad
+
+
+def check(pq, W, H, targets, grad, type):
+    (N, d), B = W.shape, H.shape[0]
+    unit = TYPES[type][1]
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+    w, h, g = W.double(), H.double(), grad.double()
+    z = (h @ w.t().contiguous())
+    size = (h.abs() @ w.abs().t().contiguous()).max().item()
+    want_lse = torch.logsumexp(z, 1)
+    t = targets.long()
+    there = (t >= 0) & (t < N)
+    rows = torch.arange(B, device="cuda")
+    at = torch.where(there, t, 0)
+    want_loss = torch.where(there, want_lse - z[rows, at], torch.zeros_like(want_lse))
+    score = (d + 2) * U * size
+    tol_lse = score + U * (N / 512 + 64 + 4 * size + 4 * np.log(max(N, 2)))
+    assert ((lse.double() - want_lse).abs() <= tol_lse).all()
+    assert ((loss.double() - want_loss).abs() <= tol_lse + score + U * (size + 4)).all()
+    p = torch.exp(z - want_lse[:, None])
+    dz = p.clone()
+    dz[rows[there], at[there]] -= 1.0
+    g = torch.where(there, g, torch.zeros_like(g))
+    dz *= g[:, None]
+    rel = score + tol_lse + U * (4 * size + 64)                  # of a probability
+    off = g.abs()[:, None] * p * rel + dz.abs() * (unit + 4 * U) + (2.0 ** -40 * g.abs().max() if type == "f16" else 0.0) + 1e-40
+    for got, other, n, by_rows in ((dH, w, N, True), (dW, h, B, False)):
+        a, o = (dz, off) if by_rows else (dz.t().contiguous(), off.t().contiguous())
+        want = a @ other
+        tol = o @ other.abs() + (n + 8) * U * ((a.abs() + o) @ other.abs()) + unit * want.abs() + (2.0 ** -24 if type == "f16" else 1e-40)
+        assert got.dtype == W.dtype and ((got.double() - want).abs() <= tol).all()
+    return loss, lse, dH, dW
+
+
+SHAPES = [(1, 8, 1), (2, 16, 3), (255, 64, 64), (256, 64, 65), (257, 72, 128), (1000, 512, 1), (1003, 512, 50), (5000, 256, 129), (3001, 136, 300), (10_007, 64, 7), (700, 1032, 33), (4096, 128, 257),
+          (70_001, 64, 1030)]
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,d,B", SHAPES)
+def test_loss_and_gradients(pq, N, d, B, type):
+    check(pq, *draw(N, d, B, type, seed=N + d + B), type)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+def test_pieces_of_the_catalogue(pq, type):
+    # more items than a piece holds, an odd number of them
+    N, d, B = 50_003, 32, 4100
+    assert (N * 4224 > 2 ** 26)
+    check(pq, *draw(N, d, B, type, seed=2), type)
+
+
+@pytest.mark.parametrize("d", [4, 12, 20, 36, 100])
+def test_float32_widths(pq, d):
+    check(pq, *draw(900, d, 70, "f32", seed=d), "f32")
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+def test_positions_without_a_target(pq, type):
+    W, H, targets, grad = draw(3000, 64, 70, type, seed=3)
+    targets[::3] = -1
+    targets[1], targets[69] = 3000, -2147483648
+    loss, lse, dH, dW = check(pq, W, H, targets, grad, type)
+    assert not loss[::3].any() and not dH[::3].any() and not dH[1].any() and torch.isfinite(lse).all()
+    targets[:] = -1
+    loss, lse, dH, dW = check(pq, W, H, targets, grad, type)
+    assert not loss.any() and not dH.any() and not dW.any()
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("spread", [0.0, 30.0, 300.0])
+def test_scores_far_apart(pq, type, spread):
+    check(pq, *draw(2000, 64, 20, type, seed=4, spread=spread), type)
+
+
+def test_gradients_of_very_different_size(pq):
+    W, H, targets, grad = draw(2000, 64, 80, "f16", seed=5)
+    grad *= torch.logspace(-6, 6, 80, device="cuda")
+    grad[7] = 0.0
+    W, H = W.float(), H.float()
+    check(pq, W, H, targets, grad, "f32")
+    check(pq, W.bfloat16(), H.bfloat16(), targets, grad, "bf16")
+
+
+def test_gradients_against_differences(pq):
+    # float32; see the sub-ids' test: directions that move no score by more than 1
+    N, d, B = 3000, 64, 9
+    W, H, targets, grad = draw(N, d, B, "f32", seed=6, spread=1.0)
+    D = torch.randn_like(H)
+    D /= (D.double() @ W.double().t().contiguous()).abs().max().float() * 1.01
+    E = torch.randn_like(W)
+    E /= (H.double() @ E.double().t().contiguous()).abs().max().float() * 1.01
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, torch.ones_like(grad))
+    h = 2.0 ** -6
+    size = (H.double().abs() @ W.double().abs().t().contiguous()).max().item() + 1
+    noise = (3 * (d + 2) * size + N / 512 + 64 + 8 * size + 4 * np.log(N)) * U / h
+    up, down = pq.pq_default_cross_entropy(W, H + h * D, targets)[0], pq.pq_default_cross_entropy(W, H - h * D, targets)[0]
+    slope = (up.double() - down.double()) / (2 * h)
+    assert ((slope - (dH.double() * D).sum(1)).abs() <= h * h / 6 + 2 * noise).all()
+    up, down = pq.pq_default_cross_entropy(W + h * E, H, targets)[0], pq.pq_default_cross_entropy(W - h * E, H, targets)[0]
+    slope = ((up.double() - down.double()) / (2 * h)).sum()
+    assert abs(slope - (dW.double() * E).sum()) <= B * (h * h / 6 + 2 * noise)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16"])
+def test_same_bits_every_time_and_on_any_stream(pq, type):
+    W, H, targets, grad = draw(20_000, 128, 200, type, seed=7)
+
+    def run():
+        loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+        return (loss, lse) + pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+
+    first, second = run(), run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        third = run()
+    torch.cuda.synchronize()
+    for a, b, c in zip(first, second, third):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_in_a_graph(pq):
+    N, d, B = 5000, 64, 90
+    W, H, targets, grad = draw(N, d, B, "bf16", seed=8)
+    ws = torch.empty(max(pq.pq_default_cross_entropy_workspace_bytes(N, B, d, pq.PQ_BFLOAT16), pq.pq_default_cross_entropy_backward_workspace_bytes(N, B, d, pq.PQ_BFLOAT16)), dtype=torch.uint8, device="cuda")
+    loss, lse, dH, dW = torch.empty(B, device="cuda"), torch.empty(B, device="cuda"), torch.empty_like(H), torch.empty_like(W)
+
+    def step():
+        pq.pq_default_cross_entropy(W, H, targets, ws, loss, lse)
+        pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad, ws, dH, dW)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        H.add_(0.125 * i)
+        step()
+        want = [x.clone() for x in (loss, lse, dH, dW)]
+        for x in (loss, lse, dH, dW):
+            x.fill_(7.0)
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, (loss, lse, dH, dW)):
+            assert torch.equal(a, b)
+
+
+def test_embeddings_beyond_32_bits_of_offset(pq):
+    # 9 GB of W: every item scores 0 but the last one
+    N, d = 70_000_001, 64
+    W = torch.zeros((N, d), dtype=torch.bfloat16, device="cuda")
+    W[N - 1] = 1.0
+    H = torch.full((2, d), 0.3125, dtype=torch.bfloat16, device="cuda")
+    targets = torch.tensor([N - 1, 3], dtype=torch.int32, device="cuda")
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    want = np.log(np.exp(20.0) + N - 1)
+    tol = U * (64 * 20 + N / 512 + 200)
+    assert abs(lse[0].item() - want) <= tol and abs(loss[0].item() - (want - 20.0)) <= tol and abs(loss[1].item() - want) <= tol
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, torch.ones(2, device="cuda"))
+    p = np.exp(20.0 - want)
+    assert abs(dW[N - 1, 5].item() - (2 * p - 1) * 0.3125) <= 2.0 ** -7 and abs(dW[3, 5].item() + 0.3125) <= 2.0 ** -7
+    assert abs(dH[0, 0].item() - (p - 1)) <= 2.0 ** -7 and abs(dH[1, 0].item() - p) <= 2.0 ** -7
+
+
+def test_refusals(pq):
+    W, H, targets, grad = draw(100, 64, 3, "bf16", seed=1)
+    lse = torch.zeros(3, device="cuda")
+    with pytest.raises(ValueError):
+        pq.pq_default_cross_entropy(W.cpu(), H, targets)
+    with pytest.raises(ValueError):
+        pq.pq_default_cross_entropy(W, H.float(), targets)
+    with pytest.raises(ValueError):
+        pq.pq_default_cross_entropy(W.double(), H.double(), targets)
+    with pytest.raises(ValueError):
+        pq.pq_default_cross_entropy(W, H, targets.long())
+    with pytest.raises(ValueError):
+        pq.pq_default_cross_entropy(W.t().contiguous().t(), H, targets)
+    with pytest.raises(ValueError):
+        pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad[:2])
+    with pytest.raises(ValueError):
+        pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad, dW=W[:50])
+    for w, h, code in ((W, H[:, :32].contiguous(), pq.PQ_ERR_SHAPE), (W[:, :12].contiguous(), H[:, :12].contiguous(), pq.PQ_ERR_UNSUPPORTED)):
+        with pytest.raises(pq.PQError) as e:
+            pq.pq_default_cross_entropy(w, h, targets)
+        assert e.value.code == code
+    with pytest.raises(pq.PQError) as e:
+        pq.pq_default_cross_entropy(W, H, targets, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == pq.PQ_ERR_WORKSPACE
