@@ -47,6 +47,16 @@ __device__ __forceinline__ void chiplet_order(int id, int inner_tiles, int& oute
     outer = local / inner_tiles * 8 + chiplet;
 }
 
+// Orders a wave's LDS accesses (LDS serves a wave's requests in the order in which they were made).
+__device__ __forceinline__ void wave_reads_after_writes() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// How many of a wave's `rows` rows there are, given how many follow its first one.
+__device__ __forceinline__ int left_of(long long rest, int rows) { return (int)max(0LL, min(rest, (long long)rows)); }
+
 struct DenseArgs {
     const void *W, *H;
     const int* targets;
@@ -98,7 +108,7 @@ __global__ __launch_bounds__(kThreads, 2) void default_cross_entropy_kernel(Dens
         if (tile >= a.item_tiles) break;
         f32x16 acc[MI][NI];
         Tile::run(items_of<T>(a, tile * kItems), positions_of<T>(a, pt * BN), acc);
-        const long long left = a.N - tile * kItems - Tile::wave_row();             // items of this wave's rows
+        const int left = left_of(a.N - tile * kItems - Tile::wave_row(), 32 * MI);
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) {
             __builtin_amdgcn_sched_barrier(0);                 // (one column after the other: the registers hold no two of them)
@@ -108,7 +118,7 @@ __global__ __launch_bounds__(kThreads, 2) void default_cross_entropy_kernel(Dens
                 for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        if (32 * mi + 8 * (e / 4) + 4 * (lane / 32) + e % 4 >= left) acc[mi][ni][e] = -__builtin_inff();
+                        if (32 * mi + 8 * (e / 4) + e % 4 >= left - 4 * (lane / 32)) acc[mi][ni][e] = -__builtin_inff();
             }
 #pragma unroll
             for (int mi = 0; mi < MI; ++mi)
@@ -209,38 +219,53 @@ __global__ __launch_bounds__(kThreads, 2) void default_dz_kernel(DenseArgs a) {
     const long long item0 = a.first_item + (long long)tile * kItems;
     f32x16 acc[MI][NI];
     Tile::run(items_of<T>(a, item0), positions_of<T>(a, pt * BN), acc);
-    const long long left = a.N - item0 - Tile::wave_row();
+    const int left = left_of(a.N - item0 - Tile::wave_row(), 32 * MI) - 4 * (lane / 32);
+    unsigned char* own = Tile::own_memory();
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) {
-        const int q = pt * BN + Tile::wave_col() + 32 * ni + lane % 32;
+        const int q0 = pt * BN + Tile::wave_col() + 32 * ni, q = q0 + lane % 32;
         const RowInfo info = a.info[q];
-        const long long hit = (q < a.B ? (long long)a.targets[q] : -1) - item0 - Tile::wave_row();
-        const bool mine = __any(hit >= 0 && hit < 32 * MI), tail = left < 32 * MI;
+        const long long from_first = (q < a.B ? (long long)a.targets[q] : -1) - item0 - Tile::wave_row();
+        const int hit = from_first >= 0 && from_first < 32 * MI ? (int)from_first - 4 * (lane / 32) : -64;
+        const bool special = __any(hit > -64) || left < 32 * MI - 4;           // (rare: a target among these items, the catalogue's end)
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[mi][ni][e] = exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -info.at));
-        if (mine || tail) {
+        if (special) {
 #pragma unroll
             for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int at = 32 * mi + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
+                    const int at = 32 * mi + 8 * (e / 4) + e % 4;
                     if (at == hit) acc[mi][ni][e] -= kDzScale;
                     if (at >= left) acc[mi][ni][e] = 0.0f;
                 }
         }
-        T* row = static_cast<T*>(a.dz) + (size_t)q * a.piece + (size_t)tile * kItems + Tile::wave_row() + 4 * (lane / 32);
+        // 32 positions x 32 items at a time through the wave's LDS: positions leave in rows of 16-byte pieces.  The pieces of
+        // a row are swapped by its number, so that writes and reads spread over the banks.
+        constexpr int kPieces = 32 * (int)sizeof(T) / 16;
+        T* out = static_cast<T*>(a.dz) + (size_t)q0 * a.piece + (size_t)tile * kItems + Tile::wave_row();
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi)
+        for (int mi = 0; mi < MI; ++mi) {
+            typedef T T4 __attribute__((ext_vector_type(4)));
 #pragma unroll
             for (int four = 0; four < 4; ++four) {
-                typedef T T4 __attribute__((ext_vector_type(4)));
                 T4 v;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = (T)(acc[mi][ni][4 * four + e] * info.scale);
-                *reinterpret_cast<T4*>(row + 32 * mi + 8 * four) = v;
+                const int byte = (8 * four + 4 * (lane / 32)) * (int)sizeof(T), piece = (byte / 16) ^ (lane % 32 / (8 / kPieces) % kPieces);
+                *reinterpret_cast<T4*>(own + (lane % 32 * kPieces + piece) * 16 + byte % 16) = v;
             }
+            wave_reads_after_writes();
+#pragma unroll
+            for (int i = 0; i < kPieces / 2; ++i) {
+                const int at = i * kWave + lane, row = at / kPieces, piece = at % kPieces;
+                const uint4 v = *reinterpret_cast<const uint4*>(own + (row * kPieces + (piece ^ (row / (8 / kPieces) % kPieces))) * 16);
+                *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(out + (size_t)row * a.piece + 32 * mi) + piece * 16) = v;
+            }
+            wave_reads_after_writes();
+        }
     }
 }
 
@@ -258,21 +283,31 @@ __global__ __launch_bounds__(kThreads, 2) void default_dw_kernel(DenseArgs a) {
     Tile::run(dz, h, acc);
     const float factor = *a.factor;
     const long long item0 = a.first_item + (long long)tile * kItems + Tile::wave_row();
-    const bool whole = a.N - item0 >= 32 * Tile::MI;           // (nearly always: no check of every row)
+    const int left = left_of(a.N - item0, 32 * Tile::MI), col0 = ct * kColsW + Tile::wave_col();
+    // 32 items x 32 elements at a time through the wave's LDS, as in default_dz_kernel
+    constexpr int kPieces = 32 * (int)sizeof(T) / 16;
+    unsigned char* own = Tile::own_memory();
 #pragma unroll
-    for (int ni = 0; ni < Tile::NI; ++ni) {
-        const int col = ct * kColsW + Tile::wave_col() + 32 * ni + lane % 32;
-        if (col >= a.d) continue;
-        T* out = static_cast<T*>(a.dW) + (size_t)(item0 + 4 * (lane / 32)) * a.d + col;
-        const int left = (int)min(a.N - item0 - 4 * (lane / 32), 32LL * Tile::MI);
+    for (int mi = 0; mi < Tile::MI; ++mi)
 #pragma unroll
-        for (int mi = 0; mi < Tile::MI; ++mi)
+        for (int ni = 0; ni < Tile::NI; ++ni) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int row = 32 * mi + 8 * (e / 4) + e % 4;
-                if (whole || row < left) out[(size_t)row * a.d] = (T)(acc[mi][ni][e] * factor);
+                const int row = 8 * (e / 4) + 4 * (lane / 32) + e % 4, byte = lane % 32 * (int)sizeof(T);
+                const int piece = (byte / 16) ^ (row / (8 / kPieces) % kPieces);
+                *reinterpret_cast<T*>(own + (row * kPieces + piece) * 16 + byte % 16) = (T)(acc[mi][ni][e] * factor);
             }
-    }
+            wave_reads_after_writes();
+#pragma unroll
+            for (int i = 0; i < kPieces / 2; ++i) {
+                const int at = i * kWave + lane, row = at / kPieces, piece = at % kPieces;
+                const uint4 v = *reinterpret_cast<const uint4*>(own + (row * kPieces + (piece ^ (row / (8 / kPieces) % kPieces))) * 16);
+                const int col = col0 + 32 * ni + piece * (16 / (int)sizeof(T));
+                if (32 * mi + row < left && col < a.d)
+                    *reinterpret_cast<uint4*>(static_cast<T*>(a.dW) + (size_t)(item0 + 32 * mi + row) * a.d + col) = v;
+            }
+            wave_reads_after_writes();
+        }
 }
 
 // A slice's share of dH: [positions][d] summed over its items of the piece, added to what earlier pieces left there.
@@ -298,20 +333,28 @@ __global__ __launch_bounds__(kThreads, 2) void default_dh_kernel(DenseArgs a) {
 #pragma unroll
             for (int ni = 0; ni < Tile::NI; ++ni) acc[mi][ni] = f32x16{};
     }
-#pragma unroll
-    for (int ni = 0; ni < Tile::NI; ++ni) {
-        const int col = ct * BN + Tile::wave_col() + 32 * ni + lane % 32;
-        if (col >= a.d) continue;
+    const int q0 = rt * BM + Tile::wave_row(), left = left_of(a.B - q0, 32 * Tile::MI) - 4 * (lane / 32);
+    float* out = a.partial_h + ((size_t)slice * a.B + q0 + 4 * (lane / 32)) * a.d + ct * BN + Tile::wave_col() + lane % 32;
+    auto put = [&](auto whole) {
 #pragma unroll
         for (int mi = 0; mi < Tile::MI; ++mi)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int q = rt * BM + Tile::wave_row() + 32 * mi + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
-                if (q >= a.B) continue;
-                float* p = a.partial_h + ((size_t)slice * a.B + q) * a.d + col;
-                *p = a.more ? *p + acc[mi][ni][e] : acc[mi][ni][e];
+            for (int ni = 0; ni < Tile::NI; ++ni) {
+                const bool there = ct * BN + Tile::wave_col() + 32 * ni + lane % 32 < a.d;
+                float* p = out + (size_t)(32 * mi) * a.d + 32 * ni;
+                float old[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    old[e] = 0.0f;
+                    if (a.more && there && (decltype(whole)::value || 32 * mi + 8 * (e / 4) + e % 4 < left)) old[e] = p[(size_t)(8 * (e / 4) + e % 4) * a.d];
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (there && (decltype(whole)::value || 32 * mi + 8 * (e / 4) + e % 4 < left)) p[(size_t)(8 * (e / 4) + e % 4) * a.d] = old[e] + acc[mi][ni][e];
             }
-    }
+    };
+    if (a.B - q0 >= 32 * Tile::MI) put(std::true_type{});
+    else put(std::false_type{});
 }
 
 // The slices' shares of dH, added in their order.
@@ -335,7 +378,7 @@ struct DensePlan {
     size_t info_at, dz_at, partial_at, bytes;          // its workspace
 };
 
-constexpr long long kDzElements = 1LL << 26;           // of the buffer: 128 MB of 16-bit dz, within the last-level cache
+constexpr long long kDzElements = 1LL << 27;           // of the buffer: 256 MB of 16-bit dz, the size of the last-level cache
 constexpr long long kMaxPiece = 1LL << 22;
 
 DensePlan plan_dense(long long N, int B, int d, int size) {

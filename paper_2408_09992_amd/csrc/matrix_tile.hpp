@@ -146,9 +146,19 @@ struct MatrixTile {
     static __device__ __forceinline__ int wave_row() { return wave() / (BN / WN) * WM; }
     static __device__ __forceinline__ int wave_col() { return wave() % (BN / WN) * WN; }
 
+    // An array per stage and side: the compiler tells loads into one from reads of another, and waits for no more than it must.
+    template <int WHICH, int BYTES>
+    static __device__ __forceinline__ unsigned char* stage_memory() {
+        __shared__ __align__(16) unsigned char memory[BYTES];
+        return memory;
+    }
+    // Between products: LDS of a wave's own, to lay a 32-row block of its part out in rows.
+    static constexpr int kOwnBytes = A::kBytes / (kThreads / kWave);
+    static __device__ __forceinline__ unsigned char* own_memory() { return stage_memory<0, A::kBytes>() + wave() * kOwnBytes; }
+
     static __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, f32x16 (&acc)[MI][NI]) {
-        // (an array per stage and side: the compiler tells loads into one from reads of another, and waits for no more than it must)
-        __shared__ __align__(16) unsigned char a0[A::kBytes], a1[A::kBytes], a2[A::kBytes], b0[B::kBytes], b1[B::kBytes], b2[B::kBytes];
+        unsigned char *a0 = stage_memory<0, A::kBytes>(), *a1 = stage_memory<1, A::kBytes>(), *a2 = stage_memory<2, A::kBytes>();
+        unsigned char *b0 = stage_memory<3, B::kBytes>(), *b1 = stage_memory<4, B::kBytes>(), *b2 = stage_memory<5, B::kBytes>();
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
