@@ -71,11 +71,11 @@ struct DenseArgs {
     const float *lse_in, *grad;
     RowInfo* info;                                     // [positions, padded]
     float* factor;                                     // what the products are multiplied with
-    void* dz;                                          // [positions, padded][piece]
+    void* dz;                                          // [tiles of a piece][positions, padded][kItems]
     float* partial_h;                                  // [slices][B][d]
     void *dH, *dW;
     long long first_item;                              // of the piece
-    int piece, items;                                  // padded and actual items of it (piece: the buffer's row length)
+    int piece, items;                                  // padded and actual items of it
     int padded, slices, slice_items, more;             // positions padded; shares of a piece's items; partial_h holds earlier pieces
     int tiles_m, tiles_n;                              // of the launch
 };
@@ -114,6 +114,7 @@ __global__ __launch_bounds__(kThreads, 2) void default_cross_entropy_kernel(Dens
             __builtin_amdgcn_sched_barrier(0);                 // (one column after the other: the registers hold no two of them)
             float top = -__builtin_inff();
             if (left < 32 * MI) {
+                stay_a_branch();
 #pragma unroll
                 for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
@@ -233,6 +234,7 @@ __global__ __launch_bounds__(kThreads, 2) void default_dz_kernel(DenseArgs a) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[mi][ni][e] = exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -info.at));
         if (special) {
+            stay_a_branch();
 #pragma unroll
             for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(kThreads, 2) void default_dz_kernel(DenseArgs a) {
         // 32 positions x 32 items at a time through the wave's LDS: positions leave in rows of 16-byte pieces.  The pieces of
         // a row are swapped by its number, so that writes and reads spread over the banks.
         constexpr int kPieces = 32 * (int)sizeof(T) / 16;
-        T* out = static_cast<T*>(a.dz) + (size_t)q0 * a.piece + (size_t)tile * kItems + Tile::wave_row();
+        T* out = static_cast<T*>(a.dz) + ((size_t)tile * a.padded + q0) * kItems + Tile::wave_row();
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
             typedef T T4 __attribute__((ext_vector_type(4)));
@@ -262,7 +264,7 @@ __global__ __launch_bounds__(kThreads, 2) void default_dz_kernel(DenseArgs a) {
             for (int i = 0; i < kPieces / 2; ++i) {
                 const int at = i * kWave + lane, row = at / kPieces, piece = at % kPieces;
                 const uint4 v = *reinterpret_cast<const uint4*>(own + (row * kPieces + (piece ^ (row / (8 / kPieces) % kPieces))) * 16);
-                *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(out + (size_t)row * a.piece + 32 * mi) + piece * 16) = v;
+                *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(out + (size_t)row * kItems + 32 * mi) + piece * 16) = v;
             }
             wave_reads_after_writes();
         }
@@ -278,7 +280,7 @@ __global__ __launch_bounds__(kThreads, 2) void default_dw_kernel(DenseArgs a) {
     if (tile >= a.tiles_m) return;
     const int lane = threadIdx.x % kWave;
     f32x16 acc[Tile::MI][Tile::NI];
-    const Operand dz{a.dz, (size_t)a.piece * sizeof(T), (long long)tile * kItems, a.piece, 0, a.padded};
+    const Operand dz{static_cast<const T*>(a.dz) + (size_t)tile * a.padded * kItems, kItems * sizeof(T), 0, kItems, 0, a.padded};
     const Operand h{a.H, (size_t)a.d * sizeof(T), (long long)ct * kColsW, a.d, 0, a.B};
     Tile::run(dz, h, acc);
     const float factor = *a.factor;
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(kThreads, 2) void default_dh_kernel(DenseArgs a) {
     const long long k0 = min((long long)slice * a.slice_items, (long long)a.items), k1 = min(k0 + a.slice_items, (long long)a.items);
     if (a.more && k0 == k1) return;
     f32x16 acc[Tile::MI][Tile::NI];
-    const Operand dz{a.dz, (size_t)a.piece * sizeof(T), (long long)rt * BM, a.padded, k0, k1};
+    const Operand dz{a.dz, kItems * sizeof(T), (long long)rt * BM, a.padded, k0, k1, kItems, (size_t)a.padded * kItems * sizeof(T)};
     const Operand w{static_cast<const T*>(a.W) + (size_t)a.first_item * a.d, (size_t)a.d * sizeof(T), (long long)ct * BN, a.d, k0,
                     min(k1, a.N - a.first_item)};
     if (k0 < k1) Tile::run(dz, w, acc);
@@ -334,23 +336,26 @@ __global__ __launch_bounds__(kThreads, 2) void default_dh_kernel(DenseArgs a) {
             for (int ni = 0; ni < Tile::NI; ++ni) acc[mi][ni] = f32x16{};
     }
     const int q0 = rt * BM + Tile::wave_row(), left = left_of(a.B - q0, 32 * Tile::MI) - 4 * (lane / 32);
-    float* out = a.partial_h + ((size_t)slice * a.B + q0 + 4 * (lane / 32)) * a.d + ct * BN + Tile::wave_col() + lane % 32;
-    auto put = [&](auto whole) {
+    float* out = a.partial_h + ((size_t)slice * a.B + q0 + 4 * (lane / 32)) * a.d;
+    auto put = [&](auto whole_c) {
+        constexpr bool whole = decltype(whole_c)::value;
 #pragma unroll
         for (int mi = 0; mi < Tile::MI; ++mi)
 #pragma unroll
             for (int ni = 0; ni < Tile::NI; ++ni) {
-                const bool there = ct * BN + Tile::wave_col() + 32 * ni + lane % 32 < a.d;
-                float* p = out + (size_t)(32 * mi) * a.d + 32 * ni;
+                const int col = ct * BN + Tile::wave_col() + 32 * ni + lane % 32;
+                float* p = out + (size_t)(32 * mi) * a.d + min(col, a.d - 1);
+                auto row = [&](int e) { return 32 * mi + 8 * (e / 4) + e % 4; };
                 float old[16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    old[e] = 0.0f;
-                    if (a.more && there && (decltype(whole)::value || 32 * mi + 8 * (e / 4) + e % 4 < left)) old[e] = p[(size_t)(8 * (e / 4) + e % 4) * a.d];
+                for (int e = 0; e < 16; ++e) old[e] = 0.0f;
+                if (a.more && (whole || left > 32 * mi)) {         // (all of them asked for at once; past the end the first row's)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) old[e] = p[(size_t)(whole || row(e) < left ? row(e) - 32 * mi : 0) * a.d];
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (there && (decltype(whole)::value || 32 * mi + 8 * (e / 4) + e % 4 < left)) p[(size_t)(8 * (e / 4) + e % 4) * a.d] = old[e] + acc[mi][ni][e];
+                    if (col < a.d && (whole || row(e) < left)) p[(size_t)(row(e) - 32 * mi) * a.d] = old[e] + acc[mi][ni][e];
             }
     };
     if (a.B - q0 >= 32 * Tile::MI) put(std::true_type{});

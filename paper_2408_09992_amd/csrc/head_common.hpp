@@ -18,6 +18,9 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp, results below 2^-126 become 0
 
+// Keeps a branch that is rarely taken a branch: the compiler otherwise runs both sides and selects.
+__device__ __forceinline__ void stay_a_branch() { asm volatile("; rare" ::: "memory"); }
+
 // A sum of exponentials held as scale and mantissa: total = s * 2^c.  c = -inf: nothing yet (s = 0).
 __device__ __forceinline__ void join_sums(float& c, float& s, float c2, float s2) {
     const float top = fmaxf(c, c2);

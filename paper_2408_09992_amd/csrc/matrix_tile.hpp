@@ -33,6 +33,8 @@ struct Operand {
     long long row0;        // first row (r) of the tile
     long long rows;        // rows there are: past the last one the last is read again
     long long k0, k1;      // range of k: past k1 zeros are read
+    int block = 0;         // along: a stored row holds this many k (a power of two, k0 a multiple of it), the next ones lie
+    size_t to_next = 0;    //   to_next bytes on; 0: all of them
 };
 
 template <typename T> struct Mfma;
@@ -68,14 +70,16 @@ struct Side {
     size_t ld;
     uint32_t offset[kLoads];
     long long k, k1;
+    int block;
+    size_t to_next;
 
     int tid;
 
     __device__ __forceinline__ void start(const Operand& o) {
         tid = threadIdx.x;
         asm volatile("" : "+v"(tid));                                      // (so that a loop over tiles does not keep all this in registers meanwhile)
-        k = o.k0; k1 = o.k1; ld = o.ld;
-        if constexpr (ALONG) base = static_cast<const char*>(o.base) + (size_t)o.row0 * ld + (size_t)o.k0 * sizeof(T);
+        k = o.k0; k1 = o.k1; ld = o.ld; block = o.block; to_next = o.to_next;
+        if constexpr (ALONG) base = static_cast<const char*>(o.base) + (size_t)o.row0 * ld + (block ? (size_t)(o.k0 / block) * to_next : (size_t)o.k0 * sizeof(T));
         else base = static_cast<const char*>(o.base) + (size_t)o.k0 * ld + (size_t)o.row0 * sizeof(T);
         const int last = (int)min((long long)ROWS, o.rows - o.row0) - 1;
 #pragma unroll
@@ -94,20 +98,25 @@ struct Side {
 
     __device__ __forceinline__ void load(unsigned char* stage) {
         unsigned char* to = stage + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (kLoads * kWave * 16);
-        const bool whole = k + kK <= k1;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const char* from = base + offset[i];
-            if (!whole) {                                                  // (the same for all lanes)
-                const int at = (tid / kWave * kLoads + i) * kWave + tid % kWave;
-                const int kk = ALONG ? ((at % 4) ^ (at / 4 / 4 % 4)) * (16 / (int)sizeof(T)) : at / kRowChunks;
-                if (k + kk >= k1) from = reinterpret_cast<const char*>(&kZeros);
-            }
+        auto bring = [&](int i, const char* from) {
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                              (__attribute__((address_space(3))) void*)(to + i * kWave * 16), 16, 0, 0);
+        };
+        if (__builtin_expect(k + kK <= k1, 1)) {                           // (the same for all lanes)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) bring(i, base + offset[i]);
+        } else {
+            stay_a_branch();
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int at = (tid / kWave * kLoads + i) * kWave + tid % kWave;
+                const int kk = ALONG ? ((at % 4) ^ (at / 4 / 4 % 4)) * (16 / (int)sizeof(T)) : at / kRowChunks;
+                bring(i, k + kk >= k1 ? reinterpret_cast<const char*>(&kZeros) : base + offset[i]);
+            }
         }
         k += kK;
         base += ALONG ? (size_t)kStageBytes : (size_t)kK * ld;
+        if (ALONG && block && k % block == 0) base += to_next - (size_t)block * sizeof(T);
     }
 
     // the operand of rows row0 .. + 31 and the u-th half of the stage
