@@ -11,8 +11,8 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
-constexpr int kStep = 64;                            // elements of an embedding per matrix instruction
-constexpr int kTileItems = 16;
+constexpr int kStep = 128;                           // elements of an embedding per step: 64 bytes of a row, 16 for a lane
+constexpr int kTileItems = 16, kTiles = 2;           // items of a matrix instruction; instructions side by side
 
 struct Q4Args {
     const uint8_t* packed;      // [N][d / 2]
@@ -20,15 +20,7 @@ struct Q4Args {
     const float* queries;       // [B][d]
     float* scores;              // [B][ld]
     long long N, ld, item_tiles;
-    int B, d, steps;            // steps = d / 64, rounded up
-};
-
-// What LDS holds, for SETS sets of four queries: the queries' digits as the matrix instruction takes them, what the
-// nibbles' offset of 8 adds to each group, and a factor per query.
-struct Q4Lds {
-    i32x4* digits;              // [step][part][set][lane]
-    i32x4* offsets;             // [group][set][query of the set]
-    float* factor;              // [set * 4 + query]
+    int B, d, steps;            // steps = d / 128, rounded up
 };
 
 // A query element as a whole number of 31 bits, in four signed bytes: v = d0 + 2^8 d1 + 2^16 d2 + 2^24 d3.
@@ -42,24 +34,24 @@ __device__ __forceinline__ uint32_t four_digits(float x, int shift) {
 // is the query (to 2^-31 of its largest element, less than its float32 rounding there) and the float32 sum over groups.
 // The instruction's 16 rows are four queries' four digits, its 16 columns items: a lane finishes one score, all its digits
 // at hand, with its item's scale.
-// Bound by the stream of nibbles: per 16 weights a lane spends six instructions on unpacking, one matrix instruction for
-// four queries and eight more a group, which the memory hides up to some 32 queries.  PARTS = 2 (groups of 32): two groups
-// share a step; each gets the step's digits with the other's zeroed.
-template <int SETS, int GROUP, int TILES>
+// Bound by the stream of nibbles, which comes in 16 bytes a lane, 64 neighbouring bytes of sixteen rows an instruction (with
+// 8 bytes a lane the same stream reached 4.4 TB/s instead of 5.9).  Those 64 bytes are 128 elements: two groups of 64, four of
+// 32.  Each group's sums are taken from all lanes' weights with the other groups' digits zeroed: the matrix cores have the
+// time, as four queries ask for 2 PARTS instructions of 16 cycles per 1 KB of weights.
+// GROUP: weights that share a scale; SETS: sets of four queries a pass over the weights serves; WHOLE: d is a multiple of 128.
+template <int SETS, int GROUP, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void default_scores_q4_kernel(Q4Args a) {
-    constexpr int PARTS = GROUP == 32 ? 2 : 1, PER_GROUP = GROUP > kStep ? GROUP / kStep : 1;   // groups a step, steps a group
-    constexpr int kAhead = 8;                                  // steps whose weights a lane has asked for
+    constexpr int PARTS = kStep / GROUP;                       // groups a step
+    constexpr int kAhead = 4;                                  // steps whose weights a lane has asked for
     extern __shared__ __align__(16) unsigned char smem[];
+    i32x4* digits = reinterpret_cast<i32x4*>(smem);            // [step][half][set][lane]: as the matrix instruction takes them
+    float* factor = reinterpret_cast<float*>(digits + (size_t)a.steps * 2 * SETS * kWave);       // [query]
+    int* shift = reinterpret_cast<int*>(factor + SETS * 4);
     const int groups = a.d / GROUP;
-    Q4Lds L;
-    L.digits = reinterpret_cast<i32x4*>(smem);
-    L.offsets = L.digits + (size_t)a.steps * PARTS * SETS * kWave;
-    L.factor = reinterpret_cast<float*>(L.offsets + (size_t)groups * SETS * 4);
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int q0 = blockIdx.y * SETS * 4;
 
     // factors: one wave per query in turn
-    int* shift = reinterpret_cast<int*>(L.factor + SETS * 4);
     for (int s = wave; s < SETS * 4; s += kWaves) {
         float top = 0.0f;
         bool odd = false;
@@ -75,132 +67,114 @@ __global__ __launch_bounds__(kThreads) void default_scores_q4_kernel(Q4Args a) {
         if (lane == 0) {
             int e = 0;
             if (top > 0.0f && !any_odd) (void)frexpf(top, &e);           // top < 2^e
-            shift[s] = any_odd ? 0 : 30 - e;
-            L.factor[s] = any_odd ? __builtin_nanf("") : ldexpf(1.0f, e > -96 ? e - 30 : -126);
-            if (e <= -96) shift[s] = 126;                                // (a query of tiny numbers: as far as float32 goes)
+            // digits are of x 2^(30 - e); a nibble stands for 16 (n - 8) below.  A query of tiny numbers goes as far as float32 does.
+            shift[s] = any_odd ? 0 : e > -92 ? 30 - e : 122;
+            factor[s] = any_odd ? __builtin_nanf("") : ldexpf(1.0f, e > -92 ? e - 34 : -126);
         }
     }
     __syncthreads();
-    // digits: row r of the instruction is digit r % 4 of query r / 4; a lane's 16 bytes are elements 16 (lane / 16) .. + 15
-    // of the step, the even and odd ones of each eight apart, as the nibbles of a word come out
-    for (int i = threadIdx.x; i < a.steps * SETS * kWave; i += kThreads) {
-        const int l = i % kWave, set = i / kWave % SETS, step = i / kWave / SETS;
-        const int row = l % 16, q = set * 4 + row / 4, first = step * kStep + 16 * (l / 16);
-        const bool live = q0 + q < a.B && first < a.d;                   // (d is a multiple of 32: sixteen elements are there or not)
-        i32x4 v = {0, 0, 0, 0};
-        if (live && L.factor[q] == L.factor[q]) {
+    // row r of the instruction is digit r % 4 of query r / 4; a lane's 16 bytes are elements 32 (lane / 16) + 16 half .. + 15 of
+    // the step, the even and odd ones of each eight apart, as the nibbles of a word come out
+    for (int i = threadIdx.x; i < a.steps * 2 * SETS * kWave; i += kThreads) {
+        const int l = i % kWave, set = i / kWave % SETS, half = i / kWave / SETS % 2, step = i / kWave / SETS / 2;
+        const int row = l % 16, q = set * 4 + row / 4, first = step * kStep + 32 * (l / 16) + 16 * half;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (q0 + q < a.B && first < a.d && factor[q] == factor[q]) {     // (d is a multiple of 32: sixteen elements are there or not)
             const float* phi = a.queries + (size_t)(q0 + q) * a.d + first;
-            uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const uint32_t byte = (four_digits(phi[e], shift[q]) >> (8 * (row % 4))) & 255u;
                 w[e / 8 * 2 + e % 2] |= byte << (8 * (e % 8 / 2));
             }
-            v = i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
         }
-        const i32x4 none = {0, 0, 0, 0};
-        if (PARTS == 1) L.digits[((size_t)step * SETS + set) * kWave + l] = v;
-        else {
-            L.digits[((size_t)(step * 2) * SETS + set) * kWave + l] = l < 32 ? v : none;
-            L.digits[((size_t)(step * 2 + 1) * SETS + set) * kWave + l] = l < 32 ? none : v;
-        }
-    }
-    // what the offset of 8 makes of a group: -8 times its digits' sums
-    for (int i = threadIdx.x; i < groups * SETS * 4; i += kThreads) {
-        const int q = i % (SETS * 4), g = i / (SETS * 4);
-        int sum[4] = {0, 0, 0, 0};
-        if (q0 + q < a.B && L.factor[q] == L.factor[q]) {
-            const float* phi = a.queries + (size_t)(q0 + q) * a.d + (size_t)g * GROUP;
-            for (int e = 0; e < GROUP; ++e) {
-                const uint32_t four = four_digits(phi[e], shift[q]);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) sum[r] += (int)(int8_t)(four >> (8 * r));
-            }
-        }
-        L.offsets[i] = i32x4{-8 * sum[0], -8 * sum[1], -8 * sum[2], -8 * sum[3]};
+        digits[i] = i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
     }
     __syncthreads();
 
     const int col = lane % 16, h = lane / 16;
+    int mine[PARTS];                                           // all ones where the lane's elements belong to the step's group p
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) mine[p] = h * PARTS / 4 == p ? -1 : 0;
     const size_t row_bytes = (size_t)a.d / 2;
     const long long last_item = a.N - 1, waves = (long long)gridDim.x * kWaves;
-    for (long long t = (long long)blockIdx.x * kWaves + wave; t * TILES < a.item_tiles; t += waves) {
-        const uint8_t* row[TILES];
-        const uint16_t* scale[TILES];
+    for (long long t = (long long)blockIdx.x * kWaves + wave; t * kTiles < a.item_tiles; t += waves) {
+        const uint8_t* row[kTiles];
+        const uint16_t* scale[kTiles];
 #pragma unroll
-        for (int u = 0; u < TILES; ++u) {
-            const long long item = min((t * TILES + u) * kTileItems + col, last_item);
+        for (int u = 0; u < kTiles; ++u) {
+            const long long item = min((t * kTiles + u) * kTileItems + col, last_item);
             row[u] = a.packed + (size_t)item * row_bytes;
             scale[u] = a.scales + (size_t)item * groups;
         }
-        float sum[TILES][SETS];
+        float sum[kTiles][SETS];
 #pragma unroll
-        for (int u = 0; u < TILES; ++u)
+        for (int u = 0; u < kTiles; ++u)
 #pragma unroll
             for (int s = 0; s < SETS; ++s) sum[u][s] = 0.0f;
         for (int step0 = 0; step0 < a.steps; step0 += kAhead) {
-            uint2 w[kAhead][TILES];
-            uint16_t sc[kAhead / PER_GROUP * PARTS][TILES];
+            uint4 w[kAhead][kTiles];
+            uint16_t sc[kAhead][kTiles][PARTS];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 // past the row's end the digits are zero: any weights will do
-                const int at = min((step0 + i) * (kStep / 2) + 8 * h, (int)row_bytes - 8);
+                const int at = min((step0 + i) * (kStep / 2) + 16 * h, (int)row_bytes - 16);
 #pragma unroll
-                for (int u = 0; u < TILES; ++u) w[i][u] = *reinterpret_cast<const uint2*>(row[u] + at);
+                for (int u = 0; u < kTiles; ++u) w[i][u] = *reinterpret_cast<const uint4*>(row[u] + at);
+#pragma unroll
+                for (int u = 0; u < kTiles; ++u) {
+                    if constexpr (WHOLE) {
+                        typedef uint16_t Scales __attribute__((ext_vector_type(PARTS)));
+                        const Scales v = *reinterpret_cast<const Scales*>(scale[u] + min(step0 + i, a.steps - 1) * PARTS);
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) sc[i][u][p] = v[p];
+                    } else {
+#pragma unroll
+                        for (int p = 0; p < PARTS; ++p) sc[i][u][p] = scale[u][min((step0 + i) * PARTS + p, groups - 1)];
+                    }
+                }
             }
-#pragma unroll
-            for (int i = 0; i < kAhead / PER_GROUP * PARTS; ++i) {
-                const int g = min(step0 / PER_GROUP * PARTS + i, groups - 1);
-#pragma unroll
-                for (int u = 0; u < TILES; ++u) sc[i][u] = scale[u][g];
-            }
-            i32x4 acc[TILES][SETS];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                if (step0 + i < a.steps) {
-                    i32x4 n[TILES];
+                if (step0 + i >= a.steps) break;
+                i32x4 n[2][kTiles];
 #pragma unroll
-                    for (int u = 0; u < TILES; ++u) {
-                        const uint2 v = w[i][u];
-                        n[u] = i32x4{(int)(v.x & 0x0F0F0F0Fu), (int)(v.x >> 4 & 0x0F0F0F0Fu), (int)(v.y & 0x0F0F0F0Fu), (int)(v.y >> 4 & 0x0F0F0F0Fu)};
-                    }
+                for (int u = 0; u < kTiles; ++u) {
+                    // a nibble's two's complement of n - 8 in the high half of a byte: 16 (n - 8)
+                    const uint32_t v[4] = {w[i][u].x ^ 0x88888888u, w[i][u].y ^ 0x88888888u, w[i][u].z ^ 0x88888888u, w[i][u].w ^ 0x88888888u};
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        n[half][u] = i32x4{(int)(v[2 * half] << 4 & 0xF0F0F0F0u), (int)(v[2 * half] & 0xF0F0F0F0u),
+                                           (int)(v[2 * half + 1] << 4 & 0xF0F0F0F0u), (int)(v[2 * half + 1] & 0xF0F0F0F0u)};
+                }
+#pragma unroll
+                for (int s = 0; s < SETS; ++s) {
+                    const i32x4 x = digits[((size_t)(step0 + i) * 2 * SETS + s) * kWave + lane], y = digits[((size_t)((step0 + i) * 2 + 1) * SETS + s) * kWave + lane];
 #pragma unroll
                     for (int p = 0; p < PARTS; ++p) {
-                        const int g = (step0 + i) / PER_GROUP * PARTS + p;
-                        if (PARTS == 2 && g >= groups) continue;         // (d = 32 mod 64: the last step holds one group)
+                        const i32x4 xp = PARTS == 1 ? x : x & mine[p], yp = PARTS == 1 ? y : y & mine[p];
+                        i32x4 acc[kTiles];
 #pragma unroll
-                        for (int s = 0; s < SETS; ++s) {
-                            const i32x4 q = L.digits[((size_t)((step0 + i) * PARTS + p) * SETS + s) * kWave + lane];
-                            if (i % PER_GROUP == 0) {
-                                const i32x4 c = L.offsets[((size_t)g * SETS + s) * 4 + h];
+                        for (int u = 0; u < kTiles; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xp, n[0][u], i32x4{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
-                                for (int u = 0; u < TILES; ++u) acc[u][s] = c;
-                            }
+                        for (int u = 0; u < kTiles; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(yp, n[1][u], acc[u], 0, 0, 0);
 #pragma unroll
-                            for (int u = 0; u < TILES; ++u) acc[u][s] = __builtin_amdgcn_mfma_i32_16x16x64_i8(q, n[u], acc[u][s], 0, 0, 0);
-                            if (i % PER_GROUP == PER_GROUP - 1) {
-#pragma unroll
-                                for (int u = 0; u < TILES; ++u) {
-                                    const i32x4 v = acc[u][s];
-                                    float x = fmaf((float)v[3], 256.0f, (float)v[2]);
-                                    x = fmaf(x, 256.0f, (float)v[1]);
-                                    x = fmaf(x, 256.0f, (float)v[0]);
-                                    const float by = __uint_as_float((uint32_t)sc[(i / PER_GROUP) * PARTS + p][u] << 16);
-                                    sum[u][s] = fmaf(x, by, sum[u][s]);
-                                }
-                            }
+                        for (int u = 0; u < kTiles; ++u) {
+                            float z = fmaf((float)acc[u][3], 256.0f, (float)acc[u][2]);
+                            z = fmaf(z, 256.0f, (float)acc[u][1]);
+                            z = fmaf(z, 256.0f, (float)acc[u][0]);
+                            sum[u][s] = fmaf(z, __uint_as_float((uint32_t)sc[i][u][p] << 16), sum[u][s]);
                         }
                     }
                 }
             }
         }
 #pragma unroll
-        for (int u = 0; u < TILES; ++u) {
-            const long long item = (t * TILES + u) * kTileItems + col;
+        for (int u = 0; u < kTiles; ++u) {
+            const long long item = (t * kTiles + u) * kTileItems + col;
 #pragma unroll
             for (int s = 0; s < SETS; ++s) {
                 const int q = s * 4 + h;
-                if (item < a.N && q0 + q < a.B) a.scores[(size_t)(q0 + q) * a.ld + item] = sum[u][s] * L.factor[q];
+                if (item < a.N && q0 + q < a.B) a.scores[(size_t)(q0 + q) * a.ld + item] = sum[u][s] * factor[q];
             }
         }
     }
@@ -237,32 +211,33 @@ int check_q4(long long N, int B, int d, int group) {
     return PQ_OK;
 }
 
-size_t q4_lds(int sets, int d, int group) {
-    const size_t steps = (size_t)ceil_div(d, kStep);
-    return steps * (group == 32 ? 2 : 1) * sets * kWave * 16 + (size_t)(d / group) * sets * 64 + (size_t)sets * 4 * 8;
-}
+size_t q4_lds(int sets, int d) { return (size_t)ceil_div(d, kStep) * 2 * sets * kWave * 16 + (size_t)sets * 4 * 8; }
 
-template <int SETS, int GROUP>
+template <int SETS, int GROUP, bool WHOLE>
 hipError_t go_q4(Q4Args a, hipStream_t st) {
-    constexpr int TILES = 2;
-    const size_t lds = q4_lds(SETS, a.d, GROUP);
-    const long long tiles = ceil_div(a.N, kTileItems);
-    a.item_tiles = tiles;
+    const size_t lds = q4_lds(SETS, a.d);
+    a.item_tiles = ceil_div(a.N, kTileItems);
     const int query_groups = (int)ceil_div(a.B, SETS * 4), per_cu = lds > kMaxLds / 2 ? 1 : 2;
-    long long blocks = ceil_div(tiles, (long long)TILES * kWaves);
+    long long blocks = ceil_div(a.item_tiles, (long long)kTiles * kWaves);
     if (blocks > (long long)per_cu * kCUs) blocks = (long long)per_cu * kCUs;
-    hipError_t e = allow_lds(default_scores_q4_kernel<SETS, GROUP, TILES>, lds);
+    hipError_t e = allow_lds(default_scores_q4_kernel<SETS, GROUP, WHOLE>, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((default_scores_q4_kernel<SETS, GROUP, TILES>), dim3((unsigned)blocks, query_groups), dim3(kThreads), lds, st, a);
+    hipLaunchKernelGGL((default_scores_q4_kernel<SETS, GROUP, WHOLE>), dim3((unsigned)blocks, query_groups), dim3(kThreads), lds, st, a);
     return hipGetLastError();
 }
 
-template <int GROUP>
+template <int GROUP, bool WHOLE>
 hipError_t go_q4_sets(const Q4Args& a, hipStream_t st) {
     // as many queries a pass over the weights as there are, up to 32 and what LDS holds of their digits
     int sets = a.B <= 4 ? 1 : a.B <= 8 ? 2 : a.B <= 16 ? 4 : 8;
-    while (sets > 1 && q4_lds(sets, a.d, GROUP) > kMaxLds) sets /= 2;
-    return sets == 8 ? go_q4<8, GROUP>(a, st) : sets == 4 ? go_q4<4, GROUP>(a, st) : sets == 2 ? go_q4<2, GROUP>(a, st) : go_q4<1, GROUP>(a, st);
+    while (sets > 1 && q4_lds(sets, a.d) > kMaxLds) sets /= 2;
+    return sets == 8 ? go_q4<8, GROUP, WHOLE>(a, st) : sets == 4 ? go_q4<4, GROUP, WHOLE>(a, st) : sets == 2 ? go_q4<2, GROUP, WHOLE>(a, st) : go_q4<1, GROUP, WHOLE>(a, st);
+}
+
+template <int GROUP>
+hipError_t go_q4_group(const Q4Args& a, hipStream_t st) {
+    if (GROUP == kStep || (a.d % kStep == 0 && ((uintptr_t)a.scales & 7) == 0)) return go_q4_sets<GROUP, true>(a, st);
+    return go_q4_sets<GROUP, GROUP == kStep>(a, st);
 }
 
 }  // namespace
@@ -292,11 +267,11 @@ int pq_default_scores_q4(const uint8_t* packed, const uint16_t* scales, const fl
     const int rc = check_q4(N, B, d, group);
     if (rc != PQ_OK) return rc;
     if (ld < N) return PQ_ERR_SHAPE;
-    if (q4_lds(1, d, group) > kMaxLds) return PQ_ERR_UNSUPPORTED;
+    if (q4_lds(1, d) > kMaxLds) return PQ_ERR_UNSUPPORTED;
     if (((uintptr_t)packed & 15) || ((uintptr_t)scales & 1) || (((uintptr_t)queries | (uintptr_t)scores) & 3)) return PQ_ERR_ALIGN;
     const Q4Args a{packed, scales, queries, scores, N, ld, 0, B, d, (int)ceil_div(d, kStep)};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return pqk::record_hip_error(group == 32 ? go_q4_sets<32>(a, st) : group == 64 ? go_q4_sets<64>(a, st) : go_q4_sets<128>(a, st));
+    return pqk::record_hip_error(group == 32 ? go_q4_group<32>(a, st) : group == 64 ? go_q4_group<64>(a, st) : go_q4_group<128>(a, st));
 }
 
 }  // extern "C"
