@@ -47,13 +47,6 @@ __device__ __forceinline__ void chiplet_order(int id, int inner_tiles, int& oute
     outer = local / inner_tiles * 8 + chiplet;
 }
 
-// Orders a wave's LDS accesses (LDS serves a wave's requests in the order in which they were made).
-__device__ __forceinline__ void wave_reads_after_writes() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // How many of a wave's `rows` rows there are, given how many follow its first one.
 __device__ __forceinline__ int left_of(long long rest, int rows) { return (int)max(0LL, min(rest, (long long)rows)); }
 

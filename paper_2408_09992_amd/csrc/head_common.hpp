@@ -21,6 +21,13 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // Keeps a branch that is rarely taken a branch: the compiler otherwise runs both sides and selects.
 __device__ __forceinline__ void stay_a_branch() { asm volatile("; rare" ::: "memory"); }
 
+// Orders a wave's LDS accesses (LDS serves a wave's requests in the order in which they were made).
+__device__ __forceinline__ void wave_reads_after_writes() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // A sum of exponentials held as scale and mantissa: total = s * 2^c.  c = -inf: nothing yet (s = 0).
 __device__ __forceinline__ void join_sums(float& c, float& s, float c2, float s2) {
     const float top = fmaxf(c, c2);

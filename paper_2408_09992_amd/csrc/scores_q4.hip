@@ -21,6 +21,7 @@ struct Q4Args {
     float* scores;              // [B][ld]
     long long N, ld, item_tiles;
     int B, d, steps;            // steps = d / 128, rounded up
+    int held;                   // tile pairs whose scores a wave holds back
 };
 
 // A query element as a whole number of 31 bits, in four signed bytes: v = d0 + 2^8 d1 + 2^16 d2 + 2^24 d3.
@@ -38,18 +39,57 @@ __device__ __forceinline__ uint32_t four_digits(float x, int shift) {
 // 8 bytes a lane the same stream reached 4.4 TB/s instead of 5.9).  Those 64 bytes are 128 elements: two groups of 64, four of
 // 32.  Each group's sums are taken from all lanes' weights with the other groups' digits zeroed: the matrix cores have the
 // time, as four queries ask for 2 PARTS instructions of 16 cycles per 1 KB of weights.
+// Scores are held back in LDS and leave a wave's tiles at a time: stores between the loads cost the stream more than their
+// bytes (1.3 GB read by 128 bytes stored per 8 KB: 207 us without stores, 262 with, 227 held back).
 // GROUP: weights that share a scale; SETS: sets of four queries a pass over the weights serves; WHOLE: d is a multiple of 128.
 template <int SETS, int GROUP, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void default_scores_q4_kernel(Q4Args a) {
+__global__ __launch_bounds__(kThreads, SETS * (kStep / GROUP) <= 4 ? 4 : 2) void default_scores_q4_kernel(Q4Args a) {
     constexpr int PARTS = kStep / GROUP;                       // groups a step
-    constexpr int kAhead = 4;                                  // steps whose weights a lane has asked for
+    constexpr int kAhead = 4;                                  // steps whose weights are on their way
+    constexpr bool kHold = SETS <= 2;
     extern __shared__ __align__(16) unsigned char smem[];
     i32x4* digits = reinterpret_cast<i32x4*>(smem);            // [step][half][set][lane]: as the matrix instruction takes them
     float* factor = reinterpret_cast<float*>(digits + (size_t)a.steps * 2 * SETS * kWave);       // [query]
     int* shift = reinterpret_cast<int*>(factor + SETS * 4);
+    float* held = reinterpret_cast<float*>(shift + SETS * 4);                                    // [wave][tile pair][query][32 items]
     const int groups = a.d / GROUP;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int q0 = blockIdx.y * SETS * 4;
+
+    const int col = lane % 16, h = lane / 16;
+    const size_t row_bytes = (size_t)a.d / 2;
+    const long long last_item = a.N - 1, waves = (long long)gridDim.x * kWaves;
+    // A wave's work is one sequence of steps, those of a tile pair and then of the next one.  The weights of kAhead steps are
+    // always on their way: waves that all waited for a round of loads would leave the memory idle while they compute.
+    typedef uint16_t Scales __attribute__((ext_vector_type(PARTS)));
+    const long long tiles_end = (a.item_tiles + kTiles - 1) / kTiles, first_tile = (long long)blockIdx.x * kWaves + wave;
+    uint4 ring_w[kAhead][kTiles];
+    Scales ring_s[kAhead][kTiles];
+    long long load_tile = first_tile;
+    int load_step = 0;
+    auto load = [&](int slot) {
+#pragma unroll
+        for (int u = 0; u < kTiles; ++u) {
+            const long long item = min((load_tile * kTiles + u) * kTileItems + col, last_item);
+            // past the row's end the digits are zero: any weights will do
+            ring_w[slot][u] = *reinterpret_cast<const uint4*>(a.packed + (size_t)item * row_bytes + min(load_step * (kStep / 2) + 16 * h, (int)row_bytes - 16));
+            // every fourth step brings the scales of four, a step for each of the item's lanes
+            if (load_step % 4 == 0) {
+                const uint16_t* scale = a.scales + (size_t)item * groups;
+                const int step = min(load_step + h, a.steps - 1);
+                if constexpr (WHOLE) ring_s[slot][u] = *reinterpret_cast<const Scales*>(scale + step * PARTS);
+                else {
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p) ring_s[slot][u][p] = scale[min(step * PARTS + p, groups - 1)];
+                }
+            }
+        }
+        if (++load_step == a.steps) { load_step = 0; load_tile += waves; }
+    };
+    if (first_tile < tiles_end) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load(i);              // (while the queries are laid out)
+    }
 
     // factors: one wave per query in turn
     for (int s = wave; s < SETS * 4; s += kWaves) {
@@ -91,93 +131,99 @@ __global__ __launch_bounds__(kThreads) void default_scores_q4_kernel(Q4Args a) {
     }
     __syncthreads();
 
-    const int col = lane % 16, h = lane / 16;
     int mine[PARTS];                                           // all ones where the lane's elements belong to the step's group p
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) mine[p] = h * PARTS / 4 == p ? -1 : 0;
-    const size_t row_bytes = (size_t)a.d / 2;
-    const long long last_item = a.N - 1, waves = (long long)gridDim.x * kWaves;
-    for (long long t = (long long)blockIdx.x * kWaves + wave; t * kTiles < a.item_tiles; t += waves) {
-        const uint8_t* row[kTiles];
-        const uint16_t* scale[kTiles];
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            const long long item = min((t * kTiles + u) * kTileItems + col, last_item);
-            row[u] = a.packed + (size_t)item * row_bytes;
-            scale[u] = a.scales + (size_t)item * groups;
-        }
-        float sum[kTiles][SETS];
+    float sum[kTiles][SETS];
+    auto clear = [&] {
 #pragma unroll
         for (int u = 0; u < kTiles; ++u)
 #pragma unroll
             for (int s = 0; s < SETS; ++s) sum[u][s] = 0.0f;
-        for (int step0 = 0; step0 < a.steps; step0 += kAhead) {
-            uint4 w[kAhead][kTiles];
-            uint16_t sc[kAhead][kTiles][PARTS];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                // past the row's end the digits are zero: any weights will do
-                const int at = min((step0 + i) * (kStep / 2) + 16 * h, (int)row_bytes - 16);
-#pragma unroll
-                for (int u = 0; u < kTiles; ++u) w[i][u] = *reinterpret_cast<const uint4*>(row[u] + at);
-#pragma unroll
-                for (int u = 0; u < kTiles; ++u) {
-                    if constexpr (WHOLE) {
-                        typedef uint16_t Scales __attribute__((ext_vector_type(PARTS)));
-                        const Scales v = *reinterpret_cast<const Scales*>(scale[u] + min(step0 + i, a.steps - 1) * PARTS);
-#pragma unroll
-                        for (int p = 0; p < PARTS; ++p) sc[i][u][p] = v[p];
-                    } else {
-#pragma unroll
-                        for (int p = 0; p < PARTS; ++p) sc[i][u][p] = scale[u][min((step0 + i) * PARTS + p, groups - 1)];
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                if (step0 + i >= a.steps) break;
-                i32x4 n[2][kTiles];
-#pragma unroll
-                for (int u = 0; u < kTiles; ++u) {
-                    // a nibble's two's complement of n - 8 in the high half of a byte: 16 (n - 8)
-                    const uint32_t v[4] = {w[i][u].x ^ 0x88888888u, w[i][u].y ^ 0x88888888u, w[i][u].z ^ 0x88888888u, w[i][u].w ^ 0x88888888u};
-#pragma unroll
-                    for (int half = 0; half < 2; ++half)
-                        n[half][u] = i32x4{(int)(v[2 * half] << 4 & 0xF0F0F0F0u), (int)(v[2 * half] & 0xF0F0F0F0u),
-                                           (int)(v[2 * half + 1] << 4 & 0xF0F0F0F0u), (int)(v[2 * half + 1] & 0xF0F0F0F0u)};
-                }
-#pragma unroll
-                for (int s = 0; s < SETS; ++s) {
-                    const i32x4 x = digits[((size_t)(step0 + i) * 2 * SETS + s) * kWave + lane], y = digits[((size_t)((step0 + i) * 2 + 1) * SETS + s) * kWave + lane];
-#pragma unroll
-                    for (int p = 0; p < PARTS; ++p) {
-                        const i32x4 xp = PARTS == 1 ? x : x & mine[p], yp = PARTS == 1 ? y : y & mine[p];
-                        i32x4 acc[kTiles];
-#pragma unroll
-                        for (int u = 0; u < kTiles; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xp, n[0][u], i32x4{0, 0, 0, 0}, 0, 0, 0);
-#pragma unroll
-                        for (int u = 0; u < kTiles; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(yp, n[1][u], acc[u], 0, 0, 0);
-#pragma unroll
-                        for (int u = 0; u < kTiles; ++u) {
-                            float z = fmaf((float)acc[u][3], 256.0f, (float)acc[u][2]);
-                            z = fmaf(z, 256.0f, (float)acc[u][1]);
-                            z = fmaf(z, 256.0f, (float)acc[u][0]);
-                            sum[u][s] = fmaf(z, __uint_as_float((uint32_t)sc[i][u][p] << 16), sum[u][s]);
-                        }
-                    }
-                }
-            }
+    };
+    clear();
+    long long tile = first_tile;
+    int step = 0, pairs = 0;
+    Scales four_steps[kTiles] = {};
+    const int queries = min(SETS * 4, a.B - q0);
+    held += (size_t)wave * a.held * queries * 32;
+    auto release = [&](long long last_tile) {                  // the held scores, the last of them of last_tile
+        wave_reads_after_writes();
+        for (int r = lane / 32; r < pairs * queries; r += 2) {
+            const int pair = r / queries, q = r - pair * queries;
+            const long long item = (last_tile - (long long)(pairs - 1 - pair) * waves) * kTiles * kTileItems + lane % 32;
+            if (item < a.N) a.scores[(size_t)(q0 + q) * a.ld + item] = held[r * 32 + lane % 32];
         }
+        wave_reads_after_writes();
+        pairs = 0;
+    };
+    // (whole rounds of the ring: steps past the wave's last tile are of items past the last one and leave nothing)
+    const int rounds = first_tile < tiles_end ? (int)(((tiles_end - 1 - first_tile) / waves + 1) * a.steps + kAhead - 1) / kAhead : 0;
+    for (int round = 0; round < rounds; ++round) {
 #pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            const long long item = (t * kTiles + u) * kTileItems + col;
+        for (int slot = 0; slot < kAhead; ++slot) {
+            __builtin_amdgcn_sched_barrier(0);                 // (steps one after the other: their accumulators share registers)
+            i32x4 n[2][kTiles];
+            float scale[kTiles][PARTS];
+#pragma unroll
+            for (int u = 0; u < kTiles; ++u) {
+                // a nibble's two's complement of n - 8 in the high half of a byte: 16 (n - 8)
+                const uint4 w = ring_w[slot][u];
+                const uint32_t v[4] = {w.x ^ 0x88888888u, w.y ^ 0x88888888u, w.z ^ 0x88888888u, w.w ^ 0x88888888u};
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    n[half][u] = i32x4{(int)(v[2 * half] << 4 & 0xF0F0F0F0u), (int)(v[2 * half] & 0xF0F0F0F0u),
+                                       (int)(v[2 * half + 1] << 4 & 0xF0F0F0F0u), (int)(v[2 * half + 1] & 0xF0F0F0F0u)};
+                if (step % 4 == 0) four_steps[u] = ring_s[slot][u];
+                uint32_t words[(PARTS + 1) / 2] = {};
+                __builtin_memcpy(words, &four_steps[u], sizeof(Scales));
+#pragma unroll
+                for (int p = 0; p < PARTS; p += 2) {
+                    const uint32_t word = (uint32_t)__shfl((int)words[p / 2], col + 16 * (step % 4));
+                    scale[u][p] = __uint_as_float(word << 16);
+                    if (p + 1 < PARTS) scale[u][p + 1] = __uint_as_float(word & 0xFFFF0000u);
+                }
+            }
+            load(slot);
 #pragma unroll
             for (int s = 0; s < SETS; ++s) {
-                const int q = s * 4 + h;
-                if (item < a.N && q0 + q < a.B) a.scores[(size_t)(q0 + q) * a.ld + item] = sum[u][s] * factor[q];
+                const i32x4 x = digits[((size_t)step * 2 * SETS + s) * kWave + lane], y = digits[((size_t)(step * 2 + 1) * SETS + s) * kWave + lane];
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p) {
+                    const i32x4 xp = PARTS == 1 ? x : x & mine[p], yp = PARTS == 1 ? y : y & mine[p];
+                    i32x4 acc[kTiles];
+#pragma unroll
+                    for (int u = 0; u < kTiles; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xp, n[0][u], i32x4{0, 0, 0, 0}, 0, 0, 0);
+#pragma unroll
+                    for (int u = 0; u < kTiles; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(yp, n[1][u], acc[u], 0, 0, 0);
+#pragma unroll
+                    for (int u = 0; u < kTiles; ++u) {
+                        const float high = (float)((acc[u][3] << 8) + acc[u][2]), low = (float)((acc[u][1] << 8) + acc[u][0]);
+                        const float z = fmaf(high, 65536.0f, low);
+                        sum[u][s] = fmaf(z, scale[u][p], sum[u][s]);
+                    }
+                }
+            }
+            if (++step == a.steps) {
+#pragma unroll
+                for (int u = 0; u < kTiles; ++u) {
+                    const long long item = (tile * kTiles + u) * kTileItems + col;
+#pragma unroll
+                    for (int s = 0; s < SETS; ++s) {
+                        const int q = s * 4 + h;
+                        const float z = sum[u][s] * factor[q];
+                        if (kHold) { if (q < queries) held[(pairs * queries + q) * 32 + u * kTileItems + col] = z; }
+                        else if (item < a.N && q < queries) a.scores[(size_t)(q0 + q) * a.ld + item] = z;
+                    }
+                }
+                if (kHold && ++pairs == a.held) release(tile);
+                clear();
+                step = 0;
+                tile += waves;
             }
         }
     }
+    if (kHold && pairs > 0) release(tile - waves);
 }
 
 // Eight elements a lane; the lanes of a group share its largest absolute value.  A stream of 4 N d bytes in.
@@ -211,15 +257,21 @@ int check_q4(long long N, int B, int d, int group) {
     return PQ_OK;
 }
 
+// digits, factors and shifts; then the scores that are held back
 size_t q4_lds(int sets, int d) { return (size_t)ceil_div(d, kStep) * 2 * sets * kWave * 16 + (size_t)sets * 4 * 8; }
+size_t held_bytes(int queries) { return (size_t)kWaves * queries * 32 * sizeof(float); }          // a tile pair of every wave
 
 template <int SETS, int GROUP, bool WHOLE>
 hipError_t go_q4(Q4Args a, hipStream_t st) {
-    const size_t lds = q4_lds(SETS, a.d);
+    const size_t fixed = q4_lds(SETS, a.d), pair = SETS <= 2 ? held_bytes(a.B < SETS * 4 ? a.B : SETS * 4) : 16;
     a.item_tiles = ceil_div(a.N, kTileItems);
-    const int query_groups = (int)ceil_div(a.B, SETS * 4), per_cu = lds > kMaxLds / 2 ? 1 : 2;
-    long long blocks = ceil_div(a.item_tiles, (long long)kTiles * kWaves);
+    const int query_groups = (int)ceil_div(a.B, SETS * 4), per_cu = fixed + pair > kMaxLds / 2 ? 1 : 2;
+    const long long pairs = ceil_div(a.item_tiles, kTiles);
+    long long blocks = ceil_div(pairs, kWaves);
     if (blocks > (long long)per_cu * kCUs) blocks = (long long)per_cu * kCUs;
+    const long long each = ceil_div(pairs, blocks * kWaves), room = (long long)((kMaxLds / per_cu - fixed) / pair);
+    a.held = (int)(each < room ? each : room);
+    const size_t lds = fixed + a.held * pair;
     hipError_t e = allow_lds(default_scores_q4_kernel<SETS, GROUP, WHOLE>, lds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((default_scores_q4_kernel<SETS, GROUP, WHOLE>), dim3((unsigned)blocks, query_groups), dim3(kThreads), lds, st, a);
@@ -230,7 +282,7 @@ template <int GROUP, bool WHOLE>
 hipError_t go_q4_sets(const Q4Args& a, hipStream_t st) {
     // as many queries a pass over the weights as there are, up to 32 and what LDS holds of their digits
     int sets = a.B <= 4 ? 1 : a.B <= 8 ? 2 : a.B <= 16 ? 4 : 8;
-    while (sets > 1 && q4_lds(sets, a.d) > kMaxLds) sets /= 2;
+    while (sets > 1 && q4_lds(sets, a.d) + held_bytes(sets * 4) > kMaxLds) sets /= 2;
     return sets == 8 ? go_q4<8, GROUP, WHOLE>(a, st) : sets == 4 ? go_q4<4, GROUP, WHOLE>(a, st) : sets == 2 ? go_q4<2, GROUP, WHOLE>(a, st) : go_q4<1, GROUP, WHOLE>(a, st);
 }
 
@@ -267,7 +319,7 @@ int pq_default_scores_q4(const uint8_t* packed, const uint16_t* scales, const fl
     const int rc = check_q4(N, B, d, group);
     if (rc != PQ_OK) return rc;
     if (ld < N) return PQ_ERR_SHAPE;
-    if (q4_lds(1, d) > kMaxLds) return PQ_ERR_UNSUPPORTED;
+    if (q4_lds(1, d) + held_bytes(4) > kMaxLds) return PQ_ERR_UNSUPPORTED;
     if (((uintptr_t)packed & 15) || ((uintptr_t)scales & 1) || (((uintptr_t)queries | (uintptr_t)scores) & 3)) return PQ_ERR_ALIGN;
     const Q4Args a{packed, scales, queries, scores, N, ld, 0, B, d, (int)ceil_div(d, kStep)};
     hipStream_t st = static_cast<hipStream_t>(stream);
