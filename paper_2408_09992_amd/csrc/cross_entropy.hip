@@ -47,6 +47,23 @@ struct Row {
         else return min((w[k / 2] >> (16 * (k % 2))) & 65535u, last);
     }
 };
+// A row of one-byte sub-ids turned by `by` places: what was sub-id (k + by) % M is sub-id k.
+template <int M>
+__device__ __forceinline__ Row<M, uint8_t> turned(Row<M, uint8_t> r, uint32_t by) {
+    constexpr int W = Row<M, uint8_t>::kWords;
+#pragma unroll
+    for (int x = 1; x < W; x *= 2) {
+        const uint32_t move = 0u - (by / (4u * x) & 1u);       // (all ones or none: a select would become an array in scratch memory)
+        Row<M, uint8_t> s;
+#pragma unroll
+        for (int i = 0; i < W; ++i) s.w[i] = r.w[i] ^ ((r.w[i] ^ r.w[(i + x) % W]) & move);
+        r = s;
+    }
+    Row<M, uint8_t> s;
+#pragma unroll
+    for (int i = 0; i < W; ++i) s.w[i] = __builtin_amdgcn_alignbyte(r.w[(i + 1) % W], r.w[i], by % 4);
+    return s;
+}
 // Any m: sub-ids are read one by one where they are used.
 template <typename CT>
 struct Row<0, CT> {
@@ -285,6 +302,8 @@ __device__ __forceinline__ float gradient_of(const BackArgs& a, uint64_t sum, in
 // Each sum lies in Q * C places side by side, P = Q C of them a row: at step s of an item, lane l adds the query of place
 // s ^ (l % P).  So the lanes of one instruction spread over all banks whatever the sub-ids are, and a popular sub-id is
 // met by a P-th of the lanes at a time.  With fewer than four queries the C places of a query are summed at the end.
+// For the same reason neighbouring lanes start at different splits (one-byte sub-ids): a sub-id that a fifth of the items
+// share is met by a lane or two of an instruction instead of a fifth of them.
 template <int M, typename CT, int Q, int C>
 __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackArgs a) {
     constexpr int P = Q * C, kUnitsBack = units_back_of<M>();
@@ -311,7 +330,65 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackAr
 
     const uint32_t lo = blockIdx.x * a.share, hi = (uint32_t)min((long long)lo + a.share, a.N);
     const uint32_t last = (uint32_t)(a.N - 1), stride = kThreads * kUnitsBack, last_code = (uint32_t)E - 1u;
-    const uint32_t turn = threadIdx.x % P;
+    constexpr bool kTurned = sizeof(CT) == 1 && M >= 4 && M <= 32;
+    const uint32_t turn = threadIdx.x % P, split_turn = kTurned ? threadIdx.x / P % (M > 0 ? M : 1) : 0u;
+    // LDS address of the lane's first place of split k's sums, sub-id 0
+    const uint32_t sums_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sums + turn * 8u;
+    auto split_at = [&](int k) {
+        const uint32_t split = kTurned ? ((uint32_t)k + split_turn) % (uint32_t)(M > 0 ? M : 1) : (uint32_t)k;
+        return sums_at + split * (uint32_t)E * (P * 8u);
+    };
+    auto step = [&](const Row<M, CT>& row, bool there, auto whole) {
+        float z[Q], p[Q];
+        item_scores<M, CT, Q>(row, table, a.m, a.b, z);
+#pragma unroll
+        for (int r = 0; r < Q; ++r) {
+            p[r] = exp2_fast(fmaf(z[r], kLog2e, -at[r]));
+            if (!decltype(whole)::value) p[r] = there ? p[r] : 0.0f;
+        }
+        // place s ^ turn holds query (s ^ turn) % Q: with C copies a lane adds each query once, in the copy turn / Q
+#pragma unroll
+        for (int x = 1; x < Q; x *= 2) {
+            const bool swap = (turn & (uint32_t)x) != 0;
+#pragma unroll
+            for (int r = 0; r < Q; ++r) {
+                if ((r & x) == 0) {
+                    const float lo_v = p[r], hi_v = p[r | x];
+                    p[r] = swap ? hi_v : lo_v;
+                    p[r | x] = swap ? lo_v : hi_v;
+                }
+            }
+        }
+        unsigned long long fixed[Q];
+#pragma unroll
+        for (int r = 0; r < Q; ++r) {
+            const uint32_t upper = (uint32_t)p[r];
+            const uint32_t lower = (uint32_t)(__builtin_amdgcn_fractf(p[r]) * 0x1p32f);
+            fixed[r] = ((unsigned long long)upper << 32) | lower;
+        }
+        Row<M, CT> mine = row;
+        if constexpr (kTurned) mine = turned<M>(row, split_turn);
+        auto add = [&](int k, uint32_t first) {
+            const uint32_t code = mine.code(k, last_code);
+            uint32_t place = first + code * (P * 8u);
+            if constexpr (kRanges) {
+                const uint32_t entry = (uint32_t)k * (uint32_t)E + code - e0;
+                if (!kTurned && entry >= e1 - e0) return;
+                if (kTurned && place - sums_at >= (e1 - e0) * 8u) return;
+            }
+#pragma unroll
+            for (int r = 0; r < Q; ++r) {
+                auto* to = (unsigned long long*)(__attribute__((address_space(3))) unsigned long long*)(uintptr_t)(place ^ (r * 8u));
+                __hip_atomic_fetch_add(to, fixed[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            }
+        };
+        if constexpr (M > 0) {
+#pragma unroll
+            for (int k = 0; k < M; ++k) add(k, split_at(k) - (kRanges ? e0 * 8u : 0u));
+        } else {
+            for (int k = 0; k < a.m; ++k) add(k, split_at(k) - (kRanges ? e0 * 8u : 0u));
+        }
+    };
     if (any) {
         Row<M, CT> row[kUnitsBack];
         auto load = [&](uint32_t first) {
@@ -325,47 +402,12 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackAr
 #pragma unroll
             for (int u = 0; u < kUnitsBack; ++u) now[u] = row[u];
             load(min(first + stride, last));
+            if (hi - base >= stride) {
 #pragma unroll
-            for (int u = 0; u < kUnitsBack; ++u) {
-                float z[Q];
-                item_scores<M, CT, Q>(now[u], table, a.m, a.b, z);
-                const bool there = first + u * kThreads < hi;
-                float p[Q];
+                for (int u = 0; u < kUnitsBack; ++u) step(now[u], true, std::true_type{});
+            } else {
 #pragma unroll
-                for (int r = 0; r < Q; ++r) p[r] = there ? exp2_fast(fmaf(z[r], kLog2e, -at[r])) : 0.0f;
-                // place s ^ turn holds query (s ^ turn) % Q: with C copies a lane adds each query once, in the copy turn / Q
-#pragma unroll
-                for (int x = 1; x < Q; x *= 2) {
-                    const bool swap = (turn & (uint32_t)x) != 0;
-#pragma unroll
-                    for (int r = 0; r < Q; ++r) {
-                        if ((r & x) == 0) {
-                            const float lo_v = p[r], hi_v = p[r | x];
-                            p[r] = swap ? hi_v : lo_v;
-                            p[r | x] = swap ? lo_v : hi_v;
-                        }
-                    }
-                }
-                unsigned long long fixed[Q];
-#pragma unroll
-                for (int r = 0; r < Q; ++r) {
-                    const uint32_t whole = (uint32_t)p[r];
-                    const uint32_t below = (uint32_t)(__builtin_amdgcn_fractf(p[r]) * 0x1p32f);
-                    fixed[r] = ((unsigned long long)whole << 32) | below;
-                }
-                auto add = [&](int k) {
-                    const uint32_t entry = (uint32_t)k * (uint32_t)E + now[u].code(k, last_code) - e0, place = entry * P | turn;
-                    if (kRanges && entry >= e1 - e0) return;
-#pragma unroll
-                    for (int r = 0; r < Q; ++r)
-                        __hip_atomic_fetch_add(&sums[place ^ (uint32_t)r], fixed[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                };
-                if constexpr (M > 0) {
-#pragma unroll
-                    for (int k = 0; k < M; ++k) add(k);
-                } else {
-                    for (int k = 0; k < a.m; ++k) add(k);
-                }
+                for (int u = 0; u < kUnitsBack; ++u) step(now[u], first + u * kThreads < hi, std::false_type{});
             }
         }
     }
