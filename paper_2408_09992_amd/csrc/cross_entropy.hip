@@ -17,7 +17,7 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 // Items a lane holds at once (loss, gradient): as many as leave the registers of four waves a SIMD room.
 template <int M> constexpr int units_of() { return M >= 64 ? 1 : M >= 32 ? 2 : 4; }
-template <int M> constexpr int units_back_of() { return M >= 32 ? 1 : 2; }
+template <int M, typename CT> constexpr int units_back_of() { return M * (int)sizeof(CT) >= 32 ? 1 : 2; }
 constexpr float kHeadroom = 40.0f;                   // (log2) how far a score may rise over a lane's reference before that moves
 constexpr float kFixedBits = 30.0f;                  // probabilities are whole multiples of 2^-62: 30 bits and 32 more below them
 
@@ -306,7 +306,7 @@ __device__ __forceinline__ float gradient_of(const BackArgs& a, uint64_t sum, in
 // share is met by a lane or two of an instruction instead of a fifth of them.
 template <int M, typename CT, int Q, int C>
 __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackArgs a) {
-    constexpr int P = Q * C, kUnitsBack = units_back_of<M>();
+    constexpr int P = Q * C, kUnitsBack = units_back_of<M, CT>();
     extern __shared__ __align__(16) unsigned char smem[];
     const int E = entries<CT>(a.b);
     unsigned long long* sums = reinterpret_cast<unsigned long long*>(smem);
@@ -402,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackAr
 #pragma unroll
             for (int u = 0; u < kUnitsBack; ++u) now[u] = row[u];
             load(min(first + stride, last));
-            if (hi - base >= stride) {
+            if (M < 64 && hi - base >= stride) {
 #pragma unroll
                 for (int u = 0; u < kUnitsBack; ++u) step(now[u], true, std::true_type{});
             } else {
@@ -490,7 +490,7 @@ bool plan_backward(Plan& p, long long N, int B, int m, int b, int code_bytes) {
     const size_t sums = (size_t)m * E * 8;
     p.Q = B >= 3 ? 4 : B;
     while (p.Q > 1 && (tables + sums) * p.Q > kMaxLds) p.Q /= 2;
-    p.C = 4 / p.Q;
+    p.C = 8 / p.Q;
     while (p.C > 1 && (tables + sums * p.C) * p.Q > kMaxLds) p.C /= 2;
     p.ranges = 1;
     p.kept = (int)(m * E);
@@ -543,6 +543,9 @@ hipError_t go_backward(const Plan& p, const BackArgs& a, hipStream_t st) {
 }
 template <int M, typename CT>
 hipError_t go_backward_q(const Plan& p, const BackArgs& a, hipStream_t st) {
+    if constexpr (fits<M, CT>(4, 8)) { if (p.Q == 4 && p.C == 2) return go_backward<M, CT, 4, 2>(p, a, st); }
+    if constexpr (fits<M, CT>(2, 8)) { if (p.Q == 2 && p.C == 4) return go_backward<M, CT, 2, 4>(p, a, st); }
+    if constexpr (fits<M, CT>(1, 8)) { if (p.C == 8) return go_backward<M, CT, 1, 8>(p, a, st); }
     if constexpr (fits<M, CT>(4, 4)) { if (p.Q == 4) return go_backward<M, CT, 4, 1>(p, a, st); }
     if constexpr (fits<M, CT>(2, 4)) { if (p.Q == 2 && p.C == 2) return go_backward<M, CT, 2, 2>(p, a, st); }
     if constexpr (fits<M, CT>(2, 2)) { if (p.Q == 2) return go_backward<M, CT, 2, 1>(p, a, st); }
