@@ -128,25 +128,27 @@ __device__ __forceinline__ void fill_tables(float* table, const float* S, int q0
     }
 }
 
-// What one position's statistics make of it: lse, and the loss with the target's score summed as its items' scores are.
+// What one position's statistics make of it, by one wave: lse, and the loss with the target's score (its m sub-item scores are
+// fetched by as many lanes at once).
 __device__ __forceinline__ void finish_position(float c, float s, const void* codes, int code_bytes, const float* S, const int* targets,
                                                 long long N, int m, int b, int q, float* loss, float* lse) {
+    const int lane = threadIdx.x % kWave, t = targets[q];
     const float l = (c == -__builtin_inff() && s == 0.0f) ? c : (c + __log2f(s)) * kLn2;
-    const int t = targets[q];
-    float out = 0.0f;
-    if (t >= 0 && t < N && l != -__builtin_inff()) {
-        const float* table = S + (size_t)q * m * b;
-        float z = 0.0f;
-        for (int k = 0; k < m; ++k) {
+    const bool has = t >= 0 && t < N && l != -__builtin_inff();
+    float z = 0.0f;
+    if (has) {
+        for (int k = lane; k < m; k += kWave) {
             const size_t at = (size_t)t * m + k;
             const uint32_t g = code_bytes == 1 ? (uint32_t)static_cast<const uint8_t*>(codes)[at] : (uint32_t)static_cast<const uint16_t*>(codes)[at];
-            const float v = table[(size_t)k * b + min(g, (uint32_t)b - 1u)];
-            z = k == 0 ? v : z + v;
+            z += S[((size_t)q * m + k) * b + min(g, (uint32_t)b - 1u)];
         }
-        out = l - z;
+#pragma unroll
+        for (int x = 1; x < kWave; x *= 2) z += __shfl_xor(z, x);
     }
-    lse[q] = l;
-    loss[q] = out;
+    if (lane == 0) {
+        lse[q] = l;
+        loss[q] = has ? l - z : 0.0f;
+    }
 }
 
 struct LossArgs {
@@ -243,12 +245,12 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_kernel(LossArgs a) {
         if (lane == 0) stat[wave * Q + r] = make_float2(c[r], s[r]);
     }
     __syncthreads();
-    if (threadIdx.x < Q && q0 + (int)threadIdx.x < a.B) {
-        float2 t = stat[threadIdx.x];
-        for (int w = 1; w < kWaves; ++w) join_sums(t.x, t.y, stat[w * Q + threadIdx.x].x, stat[w * Q + threadIdx.x].y);
-        const int q = q0 + threadIdx.x;
-        if (gridDim.x > 1) a.partial[(size_t)blockIdx.x * a.B + q] = t;
-        else finish_position(t.x, t.y, a.codes, sizeof(CT), a.S, a.targets, a.N, a.m, a.b, q, a.loss, a.lse);
+    if (wave < Q && q0 + wave < a.B) {
+        float2 t = stat[wave];
+        for (int w = 1; w < kWaves; ++w) join_sums(t.x, t.y, stat[w * Q + wave].x, stat[w * Q + wave].y);
+        const int q = q0 + wave;
+        if (gridDim.x == 1) finish_position(t.x, t.y, a.codes, sizeof(CT), a.S, a.targets, a.N, a.m, a.b, q, a.loss, a.lse);
+        else if (lane == 0) a.partial[(size_t)blockIdx.x * a.B + q] = t;
     }
 }
 
@@ -265,7 +267,7 @@ __global__ __launch_bounds__(kWave) void cross_entropy_join_kernel(LossArgs a, i
         const float c2 = __shfl_xor(c, x), s2 = __shfl_xor(s, x);
         join_sums(c, s, c2, s2);
     }
-    if (lane == 0) finish_position(c, s, a.codes, code_bytes, a.S, a.targets, a.N, a.m, a.b, q, a.loss, a.lse);
+    finish_position(c, s, a.codes, code_bytes, a.S, a.targets, a.N, a.m, a.b, q, a.loss, a.lse);
 }
 
 struct BackArgs {
@@ -452,15 +454,16 @@ struct Plan {
 
 int entries_of(int b, int code_bytes) { return code_bytes == 1 ? 256 : b; }
 
-// How many shares the items are cut into: the fewest rounds of workgroups over the chip, each of `share` items and a fixed
-// part (tables in, sums out) worth `fixed` items.
-void cut_items(Plan& p, long long N, long long workgroups, long long slots, long long fixed, long long least) {
+// How many shares the items are cut into: the least time by the cycles that an item takes a workgroup (`item`), that a
+// workgroup takes besides (`fixed`: tables in, sums out), and that the launch takes which joins more than one share.
+constexpr double kJoinCycles = 8000;                            // 3.5 us, as measured
+void cut_items(Plan& p, long long N, long long workgroups, long long slots, double item, double fixed) {
     double best = 1e300;
     p.shares = 1;
-    const long long most = N / least > 0 ? N / least : 1;
+    const long long least = 2 * kThreads, most = N / least > 0 ? N / least : 1;
     for (long long s = 1; s <= most && s <= 4 * kCUs; ++s) {
         if (workgroups * s > 4 * slots && s > 1) break;
-        const double cost = (double)ceil_div(workgroups * s, slots) * ((double)ceil_div(N, s) + (double)fixed);
+        const double cost = (double)ceil_div(workgroups * s, slots) * ((double)ceil_div(N, s) * item + fixed) + (s > 1 ? kJoinCycles : 0);
         if (cost < best * 0.98) { best = cost; p.shares = (int)s; }
     }
     p.share = (uint32_t)ceil_div(N, p.shares);
@@ -479,7 +482,8 @@ bool plan_loss(Plan& p, long long N, int B, int m, int b, int code_bytes) {
     p.lds = entry_floats * 4 * p.Q + kStatBytes;
     if (p.lds > kMaxLds) return false;
     p.groups = (int)ceil_div(B, p.Q);
-    cut_items(p, N, p.groups, (p.lds <= kMaxLds / 2 ? 2 : 1) * kCUs, 2048, 2 * kThreads);
+    // a lookup takes a compute unit 0.04 cycles a query (0.08 for one query alone); tables come in at some 20 bytes a cycle
+    cut_items(p, N, p.groups, (p.lds <= kMaxLds / 2 ? 2 : 1) * kCUs, m * (p.Q == 1 ? 0.08 : 0.045 * p.Q), 2000 + p.lds / 20.0);
     return true;
 }
 
@@ -501,7 +505,8 @@ bool plan_backward(Plan& p, long long N, int B, int m, int b, int code_bytes) {
     }
     p.lds = tables * p.Q + (size_t)p.kept * 8 * p.Q * p.C;
     p.groups = (int)ceil_div(B, p.Q);
-    cut_items(p, N, (long long)p.groups * p.ranges, kCUs, 2048, 2 * kThreads);
+    // an addition to a sum takes 0.13 cycles a query
+    cut_items(p, N, (long long)p.groups * p.ranges, kCUs, m * (p.Q == 1 ? 0.25 : 0.17 * p.Q), 2000 + p.lds / 20.0);
     return true;
 }
 
