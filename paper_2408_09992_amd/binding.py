@@ -120,6 +120,8 @@ class _Marshalling:
         return None
 
     score_topk = score_topk_u16 = score_topk_subset = subitem_scores
+    cross_entropy = cross_entropy_u16 = cross_entropy_backward = cross_entropy_u16_backward = subitem_scores
+    subitem_scores_backward = default_cross_entropy = default_cross_entropy_backward = default_scores_q4 = subitem_scores
 
     class Enqueue:
         def _bind(self, which, in0, in1, in2, n, N, B, d, m, b, K, out0, out1, ws, ws_bytes, stream, result, failed):
@@ -430,6 +432,11 @@ def pq_default_scores_q4(packed: torch.Tensor, scales: torch.Tensor, queries: to
                          ) -> torch.Tensor:
     """Eq. 3 from four-bit item embeddings: packed uint8 [N][d/2], scales bf16 [N][d/group], queries fp32 [B][d] -> scores
     fp32 [B][ld] (ld = N rounded up to a multiple of 4 when allocated here)."""
+    r = (_native_module or _native()).default_scores_q4(packed, scales, queries, out)
+    if r.__class__ is int:
+        raise PQError(r, "pq_default_scores_q4")
+    if r is not None:
+        return r
     _dev(packed, torch.uint8, "packed")
     _dev(scales, torch.bfloat16, "scales")
     _dev(queries, torch.float32, "queries")
@@ -527,6 +534,11 @@ def pq_cross_entropy(codes: torch.Tensor, S: torch.Tensor, targets: torch.Tensor
                      loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Softmax cross entropy of the whole catalogue by sub-ids: codes uint8 [N][m], S fp32 [B][m][b], targets int32 [B] (an id
     outside [0, N): no target) -> (loss fp32 [B], lse fp32 [B])."""
+    r = (_native_module or _native()).cross_entropy(codes, S, targets, workspace, loss, lse)
+    if r.__class__ is int:
+        raise PQError(r, "pq_cross_entropy")
+    if r is not None:
+        return r
     return _cross_entropy("pq_cross_entropy", torch.uint8, codes, S, targets, workspace, loss, lse)
 
 
@@ -537,6 +549,11 @@ def pq_cross_entropy_backward_workspace_bytes(N: int, B: int, m: int, b: int) ->
 def pq_cross_entropy_backward(codes: torch.Tensor, S: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor,
                               workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of sum(grad_loss * loss) with respect to S: lse as pq_cross_entropy returned it -> dS fp32 [B][m][b]."""
+    r = (_native_module or _native()).cross_entropy_backward(codes, S, targets, lse, grad_loss, workspace, out)
+    if r.__class__ is int:
+        raise PQError(r, "pq_cross_entropy_backward")
+    if r is not None:
+        return r
     return _cross_entropy_backward("pq_cross_entropy_backward", torch.uint8, codes, S, targets, lse, grad_loss, workspace, out)
 
 
@@ -547,6 +564,11 @@ def pq_cross_entropy_u16_workspace_bytes(N: int, B: int, m: int, b: int) -> int:
 def pq_cross_entropy_u16(codes: torch.Tensor, S: torch.Tensor, targets: torch.Tensor, workspace: Optional[torch.Tensor] = None,
                          loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """pq_cross_entropy over 16-bit sub-ids: codes uint16 [N][m]."""
+    r = (_native_module or _native()).cross_entropy_u16(codes, S, targets, workspace, loss, lse)
+    if r.__class__ is int:
+        raise PQError(r, "pq_cross_entropy_u16")
+    if r is not None:
+        return r
     return _cross_entropy("pq_cross_entropy_u16", torch.uint16, codes, S, targets, workspace, loss, lse)
 
 
@@ -557,6 +579,11 @@ def pq_cross_entropy_u16_backward_workspace_bytes(N: int, B: int, m: int, b: int
 def pq_cross_entropy_u16_backward(codes: torch.Tensor, S: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, grad_loss: torch.Tensor,
                                   workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """pq_cross_entropy_backward over 16-bit sub-ids: codes uint16 [N][m]."""
+    r = (_native_module or _native()).cross_entropy_u16_backward(codes, S, targets, lse, grad_loss, workspace, out)
+    if r.__class__ is int:
+        raise PQError(r, "pq_cross_entropy_u16_backward")
+    if r is not None:
+        return r
     return _cross_entropy_backward("pq_cross_entropy_u16_backward", torch.uint16, codes, S, targets, lse, grad_loss, workspace, out)
 
 
@@ -584,6 +611,11 @@ def pq_default_cross_entropy(W: torch.Tensor, queries: torch.Tensor, targets: to
                              loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Softmax cross entropy of the whole catalogue by W phi: W [N][d], queries [B][d] (both fp32, bf16 or fp16), targets int32 [B]
     (an id outside [0, N): no target) -> (loss fp32 [B], lse fp32 [B])."""
+    r = (_native_module or _native()).default_cross_entropy(W, queries, targets, workspace, loss, lse)
+    if r.__class__ is int:
+        raise PQError(r, "pq_default_cross_entropy")
+    if r is not None:
+        return r
     N, B, d, type = _dense_args("pq_default_cross_entropy", W, queries, targets)
     loss, lse = _per_position(loss, B, W, "loss"), _per_position(lse, B, W, "lse")
     workspace = _scratch(workspace, pq_default_cross_entropy_workspace_bytes(N, B, d, type), W)
@@ -604,6 +636,11 @@ def pq_default_cross_entropy_backward(W: torch.Tensor, queries: torch.Tensor, ta
                                       dqueries: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None
                                       ) -> Tuple[torch.Tensor, torch.Tensor]:
     """Gradients of sum(grad_loss * loss) with respect to queries and W, in their type: lse as pq_default_cross_entropy returned it."""
+    r = (_native_module or _native()).default_cross_entropy_backward(W, queries, targets, lse, grad_loss, workspace, dqueries, dW)
+    if r.__class__ is int:
+        raise PQError(r, "pq_default_cross_entropy_backward")
+    if r is not None:
+        return r
     N, B, d, type = _dense_args("pq_default_cross_entropy_backward", W, queries, targets)
     _per_position(lse, B, W, "lse"), _per_position(grad_loss, B, W, "grad_loss")
     dqueries = torch.empty_like(queries) if dqueries is None else _dev(dqueries, W.dtype, "dqueries")
@@ -623,6 +660,11 @@ def pq_default_cross_entropy_backward(W: torch.Tensor, queries: torch.Tensor, ta
 def pq_subitem_scores_backward(dS: torch.Tensor, queries: torch.Tensor, centroids: torch.Tensor, dqueries: Optional[torch.Tensor] = None,
                                dcentroids: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Eq. 4's gradients: dS fp32 [B][m][b], queries [B][d], centroids [m][b][d/m] -> (dqueries [B][d], dcentroids [m][b][d/m])."""
+    r = (_native_module or _native()).subitem_scores_backward(dS, queries, centroids, dqueries, dcentroids)
+    if r.__class__ is int:
+        raise PQError(r, "pq_subitem_scores_backward")
+    if r is not None:
+        return r
     for t, what in ((dS, "dS"), (queries, "queries"), (centroids, "centroids")):
         _dev(t, torch.float32, what)
     if dS.dim() != 3 or queries.dim() != 2 or centroids.dim() != 3:

@@ -15,6 +15,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "pqtopk.h"
+#include "pqtopk_train.h"
 
 namespace {
 
@@ -187,6 +188,218 @@ PyObject* score_topk_subset(PyObject*, PyObject* const* args, Py_ssize_t n) {
     });
 }
 
+// ---- the scoring head's training and its four-bit form
+
+// An output of a call: the caller's tensor, checked, or one made here; bad: there is one and it does not fit.
+struct Output {
+    PyObject* given = nullptr;
+    at::Tensor made;
+    const at::Tensor* t = nullptr;
+    bool bad = false;
+
+    Output(PyObject* o, at::IntArrayRef size, at::ScalarType type, int device) {
+        if (o == Py_None) {
+            made = empty(size, type, device);
+            t = &made;
+        } else {
+            t = plain(o, type, device);
+            given = o;
+            bad = !t || t->sizes() != size;
+        }
+    }
+    float* floats() { return t->mutable_data_ptr<float>(); }
+    PyObject* object() {
+        if (!given) return THPVariable_Wrap(std::move(made));
+        Py_INCREF(given);
+        return given;
+    }
+};
+
+PyObject* pair(Output& a, Output& b) {
+    PyObject* r = PyTuple_New(2);
+    if (!r) return nullptr;
+    PyTuple_SET_ITEM(r, 0, a.object());
+    PyTuple_SET_ITEM(r, 1, b.object());
+    return r;
+}
+
+// A call's scratch: the caller's uint8 tensor, or memory given back to torch's allocator when the call has been enqueued.
+struct Scratch {
+    c10::DataPtr made;
+    void* p = nullptr;
+    size_t bytes = 0;
+    bool bad = false;
+
+    Scratch(PyObject* o, size_t need, int device) {
+        if (o == Py_None) {
+            bytes = need < 16 ? 16 : need;
+            made = c10::GetAllocator(c10::DeviceType::CUDA)->allocate(bytes);
+            p = made.get();
+        } else {
+            const at::Tensor* t = plain(o, at::kByte, device);
+            bad = !t;
+            if (t) { p = t->mutable_data_ptr(); bytes = (size_t)t->numel(); }
+        }
+    }
+};
+
+bool vector_of(const at::Tensor* t, int64_t n) { return t && t->dim() == 1 && t->size(0) == n; }
+
+// cross_entropy(codes, S, targets, workspace | None, loss | None, lse | None) -> (loss, lse), an error code, or None
+template <bool WIDE>
+PyObject* cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 6) return none();
+        const int device = c10::hip::current_device();
+        const at::Tensor *g = plain(args[0], WIDE ? at::kUInt16 : at::kByte, device), *S = plain(args[1], at::kFloat, device), *t = plain(args[2], at::kInt, device);
+        if (!g || !S || g->dim() != 2 || S->dim() != 3 || S->size(1) != g->size(1) || !vector_of(t, S->size(0))) return none();
+        const int64_t N = g->size(0), m = g->size(1), B = S->size(0), b = S->size(2);
+        Output loss(args[4], {B}, at::kFloat, device), lse(args[5], {B}, at::kFloat, device);
+        Scratch ws(args[3], WIDE ? pq_cross_entropy_u16_workspace_bytes(N, (int)B, (int)m, (int)b) : pq_cross_entropy_workspace_bytes(N, (int)B, (int)m, (int)b), device);
+        if (loss.bad || lse.bad || ws.bad) return none();
+        const void* codes = g->const_data_ptr();
+        const float* s = S->const_data_ptr<float>();
+        const int* targets = t->const_data_ptr<int>();
+        float *l = loss.floats(), *e = lse.floats();
+        void* st = current_stream();
+        const int rc = without_gil([&]() {
+            return WIDE ? pq_cross_entropy_u16(static_cast<const uint16_t*>(codes), s, targets, N, (int)B, (int)m, (int)b, l, e, ws.p, ws.bytes, st)
+                        : pq_cross_entropy(static_cast<const uint8_t*>(codes), s, targets, N, (int)B, (int)m, (int)b, l, e, ws.p, ws.bytes, st);
+        });
+        return rc != PQ_OK ? PyLong_FromLong(rc) : pair(loss, lse);
+    });
+}
+
+// cross_entropy_backward(codes, S, targets, lse, grad_loss, workspace | None, out | None) -> dS, an error code, or None
+template <bool WIDE>
+PyObject* cross_entropy_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 7) return none();
+        const int device = c10::hip::current_device();
+        const at::Tensor *g = plain(args[0], WIDE ? at::kUInt16 : at::kByte, device), *S = plain(args[1], at::kFloat, device), *t = plain(args[2], at::kInt, device);
+        const at::Tensor *e = plain(args[3], at::kFloat, device), *w = plain(args[4], at::kFloat, device);
+        if (!g || !S || g->dim() != 2 || S->dim() != 3 || S->size(1) != g->size(1)) return none();
+        const int64_t N = g->size(0), m = g->size(1), B = S->size(0), b = S->size(2);
+        if (!vector_of(t, B) || !vector_of(e, B) || !vector_of(w, B)) return none();
+        Output dS(args[6], S->sizes(), at::kFloat, device);
+        Scratch ws(args[5], WIDE ? pq_cross_entropy_u16_backward_workspace_bytes(N, (int)B, (int)m, (int)b) : pq_cross_entropy_backward_workspace_bytes(N, (int)B, (int)m, (int)b), device);
+        if (dS.bad || ws.bad) return none();
+        const void* codes = g->const_data_ptr();
+        const float *s = S->const_data_ptr<float>(), *lse = e->const_data_ptr<float>(), *grad = w->const_data_ptr<float>();
+        const int* targets = t->const_data_ptr<int>();
+        float* out = dS.floats();
+        void* st = current_stream();
+        const int rc = without_gil([&]() {
+            return WIDE ? pq_cross_entropy_u16_backward(static_cast<const uint16_t*>(codes), s, targets, lse, grad, N, (int)B, (int)m, (int)b, out, ws.p, ws.bytes, st)
+                        : pq_cross_entropy_backward(static_cast<const uint8_t*>(codes), s, targets, lse, grad, N, (int)B, (int)m, (int)b, out, ws.p, ws.bytes, st);
+        });
+        return rc != PQ_OK ? PyLong_FromLong(rc) : dS.object();
+    });
+}
+
+// subitem_scores_backward(dS, queries, centroids, dqueries | None, dcentroids | None) -> (dqueries, dcentroids), an error code, or None
+PyObject* subitem_scores_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 5) return none();
+        const int device = c10::hip::current_device();
+        const at::Tensor *g = plain(args[0], at::kFloat, device), *q = plain(args[1], at::kFloat, device), *c = plain(args[2], at::kFloat, device);
+        if (!g || !q || !c || g->dim() != 3 || q->dim() != 2 || c->dim() != 3) return none();
+        const int64_t B = q->size(0), d = q->size(1), m = c->size(0), b = c->size(1);
+        if (m * c->size(2) != d || g->size(0) != B || g->size(1) != m || g->size(2) != b) return none();
+        Output dq(args[3], q->sizes(), at::kFloat, device), dc(args[4], c->sizes(), at::kFloat, device);
+        if (dq.bad || dc.bad) return none();
+        const float *dS = g->const_data_ptr<float>(), *phi = q->const_data_ptr<float>(), *psi = c->const_data_ptr<float>();
+        float *dphi = dq.floats(), *dpsi = dc.floats();
+        void* st = current_stream();
+        const int rc = without_gil([&]() { return pq_subitem_scores_backward(dS, phi, psi, dphi, dpsi, (int)B, (int)d, (int)m, (int)b, st); });
+        return rc != PQ_OK ? PyLong_FromLong(rc) : pair(dq, dc);
+    });
+}
+
+// W and queries of one type; its number in the C ABI, or -1
+int dense_type(const at::Tensor& W) {
+    return W.scalar_type() == at::kFloat ? PQ_FLOAT32 : W.scalar_type() == at::kBFloat16 ? PQ_BFLOAT16 : W.scalar_type() == at::kHalf ? PQ_FLOAT16 : -1;
+}
+
+// default_cross_entropy(W, queries, targets, workspace | None, loss | None, lse | None) -> (loss, lse), an error code, or None
+PyObject* default_cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 6 || !THPVariable_Check(args[0])) return none();
+        const int device = c10::hip::current_device();
+        const int type = dense_type(THPVariable_Unpack(args[0]));
+        if (type < 0) return none();
+        const at::ScalarType scalar = THPVariable_Unpack(args[0]).scalar_type();
+        const at::Tensor *W = plain(args[0], scalar, device), *q = plain(args[1], scalar, device), *t = plain(args[2], at::kInt, device);
+        if (!W || !q || W->dim() != 2 || q->dim() != 2 || W->size(1) != q->size(1) || !vector_of(t, q->size(0))) return none();
+        const int64_t N = W->size(0), d = W->size(1), B = q->size(0);
+        Output loss(args[4], {B}, at::kFloat, device), lse(args[5], {B}, at::kFloat, device);
+        Scratch ws(args[3], pq_default_cross_entropy_workspace_bytes(N, (int)B, (int)d, type), device);
+        if (loss.bad || lse.bad || ws.bad) return none();
+        const void *w = W->const_data_ptr(), *h = q->const_data_ptr();
+        const int* targets = t->const_data_ptr<int>();
+        float *l = loss.floats(), *e = lse.floats();
+        void* st = current_stream();
+        const int rc = without_gil([&]() { return pq_default_cross_entropy(w, h, targets, N, (int)B, (int)d, type, l, e, ws.p, ws.bytes, st); });
+        return rc != PQ_OK ? PyLong_FromLong(rc) : pair(loss, lse);
+    });
+}
+
+// default_cross_entropy_backward(W, queries, targets, lse, grad_loss, workspace | None, dqueries | None, dW | None)
+// -> (dqueries, dW), an error code, or None
+PyObject* default_cross_entropy_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 8 || !THPVariable_Check(args[0])) return none();
+        const int device = c10::hip::current_device();
+        const int type = dense_type(THPVariable_Unpack(args[0]));
+        if (type < 0) return none();
+        const at::ScalarType scalar = THPVariable_Unpack(args[0]).scalar_type();
+        const at::Tensor *W = plain(args[0], scalar, device), *q = plain(args[1], scalar, device), *t = plain(args[2], at::kInt, device);
+        const at::Tensor *e = plain(args[3], at::kFloat, device), *g = plain(args[4], at::kFloat, device);
+        if (!W || !q || W->dim() != 2 || q->dim() != 2 || W->size(1) != q->size(1)) return none();
+        const int64_t N = W->size(0), d = W->size(1), B = q->size(0);
+        if (!vector_of(t, B) || !vector_of(e, B) || !vector_of(g, B)) return none();
+        Output dq(args[6], q->sizes(), scalar, device), dW(args[7], W->sizes(), scalar, device);
+        Scratch ws(args[5], pq_default_cross_entropy_backward_workspace_bytes(N, (int)B, (int)d, type), device);
+        if (dq.bad || dW.bad || ws.bad) return none();
+        const void *w = W->const_data_ptr(), *h = q->const_data_ptr();
+        const int* targets = t->const_data_ptr<int>();
+        const float *lse = e->const_data_ptr<float>(), *grad = g->const_data_ptr<float>();
+        void *out_h = dq.t->mutable_data_ptr(), *out_w = dW.t->mutable_data_ptr();
+        void* st = current_stream();
+        const int rc = without_gil([&]() {
+            return pq_default_cross_entropy_backward(w, h, targets, lse, grad, N, (int)B, (int)d, type, out_h, out_w, ws.p, ws.bytes, st);
+        });
+        return rc != PQ_OK ? PyLong_FromLong(rc) : pair(dq, dW);
+    });
+}
+
+// default_scores_q4(packed, scales, queries, out | None) -> scores, an error code, or None
+PyObject* default_scores_q4(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        if (n != 4) return none();
+        const int device = c10::hip::current_device();
+        const at::Tensor *p = plain(args[0], at::kByte, device), *s = plain(args[1], at::kBFloat16, device), *q = plain(args[2], at::kFloat, device);
+        if (!p || !s || !q || p->dim() != 2 || s->dim() != 2 || q->dim() != 2) return none();
+        const int64_t N = p->size(0), B = q->size(0), d = q->size(1), groups = s->size(1);
+        if (s->size(0) != N || p->size(1) * 2 != d || groups < 1 || d % groups != 0) return none();
+        int64_t ld = (N + 3) / 4 * 4;
+        if (args[3] != Py_None) {
+            const at::Tensor* given = plain(args[3], at::kFloat, device);
+            if (!given || given->dim() != 2) return none();
+            ld = given->size(1);
+        }
+        Output out(args[3], {B, ld}, at::kFloat, device);
+        if (out.bad) return none();
+        const uint8_t* packed = p->const_data_ptr<uint8_t>();
+        const uint16_t* scales = static_cast<const uint16_t*>(s->const_data_ptr());
+        const float* phi = q->const_data_ptr<float>();
+        float* scores = out.floats();
+        void* st = current_stream();
+        const int rc = without_gil([&]() { return pq_default_scores_q4(packed, scales, phi, N, (int)B, (int)d, (int)(d / groups), scores, ld, st); });
+        return rc != PQ_OK ? PyLong_FromLong(rc) : out.object();
+    });
+}
+
 // ---- Enqueue: an entry point with its arguments fixed; calling the object enqueues and returns `result`.  Base class of
 // binding.py's Prepared classes, which keep the tensors alive and say what an error code means (`failed`).
 enum Entry { kUnset, kSubitem, kTopK, kTopKU16, kTopKSubset };
@@ -279,6 +492,14 @@ PyMethodDef functions[] = {
     {"score_topk", (PyCFunction)(void (*)(void))score_topk<false>, METH_FASTCALL, nullptr},
     {"score_topk_u16", (PyCFunction)(void (*)(void))score_topk<true>, METH_FASTCALL, nullptr},
     {"score_topk_subset", (PyCFunction)(void (*)(void))score_topk_subset, METH_FASTCALL, nullptr},
+    {"cross_entropy", (PyCFunction)(void (*)(void))cross_entropy<false>, METH_FASTCALL, nullptr},
+    {"cross_entropy_u16", (PyCFunction)(void (*)(void))cross_entropy<true>, METH_FASTCALL, nullptr},
+    {"cross_entropy_backward", (PyCFunction)(void (*)(void))cross_entropy_backward<false>, METH_FASTCALL, nullptr},
+    {"cross_entropy_u16_backward", (PyCFunction)(void (*)(void))cross_entropy_backward<true>, METH_FASTCALL, nullptr},
+    {"subitem_scores_backward", (PyCFunction)(void (*)(void))subitem_scores_backward, METH_FASTCALL, nullptr},
+    {"default_cross_entropy", (PyCFunction)(void (*)(void))default_cross_entropy, METH_FASTCALL, nullptr},
+    {"default_cross_entropy_backward", (PyCFunction)(void (*)(void))default_cross_entropy_backward, METH_FASTCALL, nullptr},
+    {"default_scores_q4", (PyCFunction)(void (*)(void))default_scores_q4, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pqnative", nullptr, -1, functions, nullptr, nullptr, nullptr, nullptr};
 
