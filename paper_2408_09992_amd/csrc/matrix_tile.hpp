@@ -23,7 +23,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-static __device__ const uint4 kZeros = {0u, 0u, 0u, 0u};
+// A stage's loads see 2 GB from its first byte on (a tile's rows are at most 256 times 64 KB apart); an offset behind them reads 0.
+constexpr uint32_t kBufferBytes = 0x7FFFFFFFu, kPastEnd = 0x80000000u;
 
 constexpr int kStageBytes = 64, kStages = 3;
 
@@ -37,25 +38,24 @@ struct Operand {
     size_t to_next = 0;    //   to_next bytes on; 0: all of them
 };
 
-template <typename T> struct Mfma;
-template <> struct Mfma<__bf16> {
-    static __device__ __forceinline__ f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    }
-};
-template <> struct Mfma<_Float16> {
-    static __device__ __forceinline__ f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    }
-};
-template <> struct Mfma<float> {
-    static __device__ __forceinline__ f32x16 multiply(s16x8 a, s16x8 b, f32x16 c) {
-        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+// acc[mi][ni] += x[mi] y[ni].  float32: the four instructions of a pair are as far apart as the pairs allow, as each waits for
+// the sum that the one before it leaves.
+template <typename T, int MI, int NI>
+__device__ __forceinline__ void multiply(const s16x8 (&x)[MI], const s16x8 (&y)[NI], f32x16 (&acc)[MI][NI]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], c, 0, 0, 0);
-        return c;
-    }
-};
+    for (int i = 0; i < (sizeof(T) == 4 ? 4 : 1); ++i)
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) {
+                if constexpr (std::is_same<T, __bf16>::value)
+                    acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[mi]), __builtin_bit_cast(bf16x8, y[ni]), acc[mi][ni], 0, 0, 0);
+                else if constexpr (std::is_same<T, _Float16>::value)
+                    acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x[mi]), __builtin_bit_cast(f16x8, y[ni]), acc[mi][ni], 0, 0, 0);
+                else
+                    acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(f32x4, x[mi])[i], __builtin_bit_cast(f32x4, y[ni])[i], acc[mi][ni], 0, 0, 0);
+            }
+}
 
 // ROWS rows of an operand, as a workgroup of THREADS brings them to LDS and its waves read them.
 template <typename T, int ROWS, bool ALONG, int THREADS>
@@ -96,22 +96,29 @@ struct Side {
     }
     static __device__ __forceinline__ int swap(int chunk, int kk) { return sizeof(T) == 2 ? chunk ^ (4 * (kk % 4)) : chunk; }
 
+    // How many stages from k0 on hold nothing but operand.
+    static __device__ __forceinline__ int whole_stages(const Operand& o) { return (int)((o.k1 - o.k0) / kK); }
+
+    // The next stage, on its way; CHECKED: it may end, or lie, behind k1 (zeros).
+    template <bool CHECKED>
     __device__ __forceinline__ void load(unsigned char* stage) {
         unsigned char* to = stage + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (kLoads * kWave * 16);
-        auto bring = [&](int i, const char* from) {
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                             (__attribute__((address_space(3))) void*)(to + i * kWave * 16), 16, 0, 0);
+        // (as a buffer, whose offsets past the end read zeros; the compiler then also counts these loads one by one, where it
+        // waits for all of them to be done if they are global loads)
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, kBufferBytes, 0x00020000);
+        auto bring = [&](int i, uint32_t at) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + i * kWave * 16), 16, at, 0, 0, 0);
         };
-        if (__builtin_expect(k + kK <= k1, 1)) {                           // (the same for all lanes)
+        if (!CHECKED || k + kK <= k1) {                                    // (the same for all lanes)
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) bring(i, base + offset[i]);
+            for (int i = 0; i < kLoads; ++i) bring(i, offset[i]);
         } else {
             stay_a_branch();
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int at = (tid / kWave * kLoads + i) * kWave + tid % kWave;
                 const int kk = ALONG ? ((at % 4) ^ (at / 4 / 4 % 4)) * (16 / (int)sizeof(T)) : at / kRowChunks;
-                bring(i, k + kk >= k1 ? reinterpret_cast<const char*>(&kZeros) : base + offset[i]);
+                bring(i, k + kk >= k1 ? kPastEnd : offset[i]);
             }
         }
         k += kK;
@@ -179,11 +186,11 @@ struct MatrixTile {
         const int steps = (int)((oa.k1 - oa.k0 + A::kK - 1) / A::kK);
         const int row0 = wave_row(), col0 = wave_col();
 
-        auto load = [&](int stage) {
-            a.load(stage == 0 ? a0 : stage == 1 ? a1 : a2);
-            b.load(stage == 0 ? b0 : stage == 1 ? b1 : b2);
+        auto load = [&](int stage, auto checked) {
+            a.template load<decltype(checked)::value>(stage == 0 ? a0 : stage == 1 ? a1 : a2);
+            b.template load<decltype(checked)::value>(stage == 0 ? b0 : stage == 1 ? b1 : b2);
         };
-        auto step = [&](auto stage_c) {
+        auto step = [&](auto stage_c, auto checked) {
             constexpr int stage = decltype(stage_c)::value;
             const unsigned char* sa = stage == 0 ? a0 : stage == 1 ? a1 : a2;
             const unsigned char* sb = stage == 0 ? b0 : stage == 1 ? b1 : b2;
@@ -198,26 +205,31 @@ struct MatrixTile {
 #pragma unroll
                 for (int ni = 0; ni < NI; ++ni) y[u][ni] = B::read(sb, col0 + 32 * ni, u);
             }
-            __builtin_amdgcn_sched_barrier(0);
-            load((stage + 2) % 3);
+            __builtin_amdgcn_sched_barrier(0);                 // (reads behind a load into LDS would wait for that load)
+            load((stage + 2) % 3, checked);
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int mi = 0; mi < MI; ++mi)
-#pragma unroll
-                    for (int ni = 0; ni < NI; ++ni) acc[mi][ni] = Mfma<T>::multiply(x[u][mi], y[u][ni], acc[mi][ni]);
+            for (int u = 0; u < 2; ++u) multiply<T, MI, NI>(x[u], y[u], acc);
         };
+        using std::integral_constant;
         // Two stages more than there are get loaded (zeros): the count of loads in flight is the same in every step, and the
-        // compiler, which counts them too, finds nothing else to wait for.
-        load(0);
-        load(1);
-        for (int s = 0;;) {
-            step(std::integral_constant<int, 0>{});
+        // compiler, which counts them too, finds nothing else to wait for.  The loads of a step whose stages are whole are
+        // free of branches, and go out between its matrix instructions.
+        load(0, std::true_type{});
+        load(1, std::true_type{});
+        const int whole = min(A::whole_stages(oa), B::whole_stages(ob));
+        int s = 0;
+        for (; s + 4 < whole; s += 3) {
+            step(integral_constant<int, 0>{}, std::false_type{});
+            step(integral_constant<int, 1>{}, std::false_type{});
+            step(integral_constant<int, 2>{}, std::false_type{});
+        }
+        while (s < steps) {
+            step(integral_constant<int, 0>{}, std::true_type{});
             if (++s >= steps) break;
-            step(std::integral_constant<int, 1>{});
+            step(integral_constant<int, 1>{}, std::true_type{});
             if (++s >= steps) break;
-            step(std::integral_constant<int, 2>{});
-            if (++s >= steps) break;
+            step(integral_constant<int, 2>{}, std::true_type{});
+            ++s;
         }
         wait_loads<0>();                                       // nothing is on its way to LDS, or being read there, any more
     }
