@@ -1,0 +1,464 @@
+// Softmax cross entropy of the catalogue by the default scorer's W phi (pq_default_cross_entropy), and its gradients.
+//
+//   z = H W^T      lse_t = log sum_i exp z_ti      dz_ti = g_t (exp(z_ti - lse_t) - [i = target_t])
+//   dH = dz W      dW = dz^T H
+//
+// Everything is a matrix product whose one side is short: T positions, d elements, N items.  The loss keeps z in registers:
+// a workgroup multiplies a tile of items by a tile of positions and folds it into the positions' running sums.  The gradient
+// takes the items in pieces: z of a piece once more, its dz to a buffer that stays in the last-level cache, then the two
+// products from there.  8 T N d operations in all, 2 of them the loss's.
+#pragma once
+#include <type_traits>
+#include "pqtopk_train.h"
+#include "matrix_tile.hpp"
+
+namespace pqk {
+namespace head {
+
+constexpr float kHeadroom = 40.0f;                    // (log2) how far a score may rise over a lane's reference before that moves
+constexpr float kDzBits = 15.0f, kDzScale = 32768.0f;  // dz is stored times 2^15 over the largest |g|: types keep small probabilities
+constexpr int kItems = 256;                           // items of a tile of z and dW
+
+struct RowInfo { float at, scale; };                  // of a position: 2^(z log2e - at) is p 2^15; its g over the largest |g|
+
+// The tiles: z for kItems items and POS positions; dH for ROWS positions and COLS elements; dW for kItems items and COLS
+// elements.  Tiles of 256 x 256 by eight waves feed the matrix cores best (143 TFLOP/s in float32, 1040 to 1130 in bfloat16,
+// against 134 and 880 to 1090 with 256 x 128 by four); the smaller ones are for few positions and narrow embeddings.
+template <typename T, int POS> struct ScoresTile;
+template <typename T> struct ScoresTile<T, 64> : MatrixTile<T, kItems, 64, 64, 64, true, true> {};
+template <typename T> struct ScoresTile<T, 128> : MatrixTile<T, kItems, 128, 128, 64, true, true> {};
+template <typename T> struct ScoresTile<T, 256> : MatrixTile<T, kItems, 256, 128, 64, true, true> {};
+template <typename T, int COLS> struct TileW;
+template <typename T> struct TileW<T, 64> : MatrixTile<T, kItems, 64, 64, 64, false, false> {};
+template <typename T> struct TileW<T, 128> : MatrixTile<T, kItems, 128, 128, 64, false, false> {};
+template <typename T> struct TileW<T, 256> : MatrixTile<T, kItems, 256, 128, 64, false, false> {};
+template <typename T, int ROWS, int COLS> struct TileH;
+template <typename T> struct TileH<T, 64, 64> : MatrixTile<T, 64, 64, 32, 32, true, false> {};
+template <typename T> struct TileH<T, 64, 128> : MatrixTile<T, 64, 128, 32, 64, true, false> {};
+template <typename T> struct TileH<T, 64, 256> : MatrixTile<T, 64, 256, 64, 64, true, false> {};
+template <typename T> struct TileH<T, 128, 64> : MatrixTile<T, 128, 64, 64, 32, true, false> {};
+template <typename T> struct TileH<T, 128, 128> : MatrixTile<T, 128, 128, 64, 64, true, false> {};
+template <typename T> struct TileH<T, 128, 256> : MatrixTile<T, 128, 256, 64, 128, true, false> {};
+template <typename T> struct TileH<T, 256, 64> : MatrixTile<T, 256, 64, 64, 64, true, false> {};
+template <typename T> struct TileH<T, 256, 128> : MatrixTile<T, 256, 128, 128, 64, true, false> {};
+template <typename T> struct TileH<T, 256, 256> : MatrixTile<T, 256, 256, 128, 64, true, false> {};
+
+// Neighbouring workgroups run on different chiplets, each with its own L2: workgroup `id` of n per outer tile becomes
+// (outer, inner) such that all inner tiles of an outer one follow each other on one chiplet and share its rows there.
+__device__ __forceinline__ void chiplet_order(int id, int inner_tiles, int& outer, int& inner) {
+    const int chiplet = id % 8, local = id / 8;
+    inner = local % inner_tiles;
+    outer = local / inner_tiles * 8 + chiplet;
+}
+
+// How many of a wave's `rows` rows there are, given how many follow its first one.
+__device__ __forceinline__ int left_of(long long rest, int rows) { return (int)max(0LL, min(rest, (long long)rows)); }
+
+struct DenseArgs {
+    const void *W, *H;
+    const int* targets;
+    long long N;
+    int B, d;
+    // loss
+    long long item_tiles;
+    int tiles_each, groups, position_tiles;
+    float2* partial;                                   // [groups][B]
+    float *loss, *lse;
+    // gradient
+    const float *lse_in, *grad;
+    RowInfo* info;                                     // [positions, padded]
+    float* factor;                                     // what the products are multiplied with
+    void* dz;                                          // [tiles of a piece][positions, padded][kItems]
+    float* partial_h;                                  // [slices][B][d]
+    void *dH, *dW;
+    long long first_item;                              // of the piece
+    int piece, items;                                  // padded and actual items of it
+    int padded, slices, slice_items, more;             // positions padded; shares of a piece's items; partial_h holds earlier pieces
+    int tiles_m, tiles_n;                              // of the launch
+};
+
+template <typename T>
+__device__ __forceinline__ Operand items_of(const DenseArgs& a, long long item) {
+    return Operand{a.W, (size_t)a.d * sizeof(T), item, a.N, 0, a.d};
+}
+template <typename T>
+__device__ __forceinline__ Operand positions_of(const DenseArgs& a, int position) {
+    return Operand{a.H, (size_t)a.d * sizeof(T), position, a.B, 0, a.d};
+}
+
+// Statistics of a tile of positions over a group of item tiles, one after the other.  As in the loss by sub-ids a lane's
+// reference c moves only when a score passes it by 2^kHeadroom; lanes, halves and waves join once, at the end.
+template <typename T, int BN>
+__global__ __launch_bounds__((ScoresTile<T, BN>::kThreads), 2) void default_cross_entropy_kernel(DenseArgs a) {
+    using Tile = ScoresTile<T, BN>;
+    constexpr int MI = Tile::MI, NI = Tile::NI, kRowWaves = kItems / (32 * MI);
+    __shared__ float2 stat[kRowWaves][BN];
+    int group, pt;
+    chiplet_order(blockIdx.x, a.position_tiles, group, pt);
+    if (group >= a.groups) return;
+    const int lane = threadIdx.x % kWave;
+    float c[NI], s[NI];
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) { c[ni] = -__builtin_inff(); s[ni] = 0.0f; }
+    for (int i = 0; i < a.tiles_each; ++i) {
+        const long long tile = (long long)group * a.tiles_each + i;
+        if (tile >= a.item_tiles) break;
+        f32x16 acc[MI][NI];
+        Tile::run(items_of<T>(a, tile * kItems), positions_of<T>(a, pt * BN), acc);
+        const int left = left_of(a.N - tile * kItems - Tile::wave_row(), 32 * MI);
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) {
+            __builtin_amdgcn_sched_barrier(0);                 // (one column after the other: the registers hold no two of them)
+            float top = -__builtin_inff();
+            if (left < 32 * MI) {
+                stay_a_branch();
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (32 * mi + 8 * (e / 4) + e % 4 >= left - 4 * (lane / 32)) acc[mi][ni][e] = -__builtin_inff();
+            }
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[mi][ni][e]);
+            top *= kLog2e;
+            if (__any(top > c[ni] + kHeadroom)) {
+                if (top > c[ni] + kHeadroom) { s[ni] *= exp2_fast(c[ni] - top); c[ni] = top; }
+            }
+            const float at = c[ni] == -__builtin_inff() ? 0.0f : c[ni];
+            float sum = 0.0f;
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum += exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -at));
+            s[ni] += sum;
+        }
+    }
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+        const float c2 = __shfl_xor(c[ni], 32), s2 = __shfl_xor(s[ni], 32);
+        join_sums(c[ni], s[ni], c2, s2);
+        if (lane < 32) stat[Tile::wave_row() / (32 * MI)][Tile::wave_col() + 32 * ni + lane] = make_float2(c[ni], s[ni]);
+    }
+    __syncthreads();
+    const int q = pt * BN + threadIdx.x;
+    if ((int)threadIdx.x < BN && q < a.B) {
+        float2 t = stat[0][threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < kRowWaves; ++w) join_sums(t.x, t.y, stat[w][threadIdx.x].x, stat[w][threadIdx.x].y);
+        a.partial[(size_t)group * a.B + q] = t;
+    }
+}
+
+// One wave per position joins the groups' sums and takes the target's score.
+template <typename T>
+__global__ __launch_bounds__(kWave) void default_cross_entropy_join_kernel(DenseArgs a) {
+    const int q = blockIdx.x, lane = threadIdx.x;
+    float c = -__builtin_inff(), s = 0.0f;
+    for (int i = lane; i < a.groups; i += kWave) {
+        const float2 t = a.partial[(size_t)i * a.B + q];
+        join_sums(c, s, t.x, t.y);
+    }
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) {
+        const float c2 = __shfl_xor(c, x), s2 = __shfl_xor(s, x);
+        join_sums(c, s, c2, s2);
+    }
+    const float lse = (c + __log2f(s)) * kLn2;
+    const int t = a.targets[q];
+    float z = 0.0f;
+    const bool has = t >= 0 && t < a.N;
+    if (has) {
+        const T *w = static_cast<const T*>(a.W) + (size_t)t * a.d, *h = static_cast<const T*>(a.H) + (size_t)q * a.d;
+        for (int e = lane; e < a.d; e += kWave) z = fmaf((float)w[e], (float)h[e], z);
+#pragma unroll
+        for (int x = 1; x < kWave; x *= 2) z += __shfl_xor(z, x);
+    }
+    if (lane == 0) {
+        a.lse[q] = lse;
+        a.loss[q] = has ? lse - z : 0.0f;
+    }
+}
+
+// What the gradient's kernels need of a position, and the factor of their products.
+template <typename T>
+__global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
+    __shared__ float tops[16];
+    const int tid = threadIdx.x;
+    auto weight = [&](int q) { const int t = a.targets[q]; return t >= 0 && t < a.N ? a.grad[q] : 0.0f; };
+    float top = 0.0f;
+    for (int q = tid; q < a.B; q += 1024) top = fmaxf(top, fabsf(weight(q)));
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    if (tid % kWave == 0) tops[tid / kWave] = top;
+    __syncthreads();
+    top = tops[0];
+#pragma unroll
+    for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
+    for (int q = tid; q < a.padded; q += 1024) {
+        const float g = q < a.B ? weight(q) : 0.0f;
+        const bool live = g != 0.0f;
+        a.info[q] = RowInfo{live ? a.lse_in[q] * kLog2e - kDzBits : __builtin_inff(), live ? g / top : 0.0f};
+    }
+    if (tid == 0) *a.factor = top / kDzScale;
+}
+
+// dz of a piece of items: scores as in the loss, then (exp(z - lse) - [target]) g as the products' operands, position by
+// position.  For 16-bit operands dz is rounded to their type: it is the products' input as H and W are, and what they add up
+// (in float32) is rounded to that type once more at the end.
+template <typename T, int BN>
+__global__ __launch_bounds__((ScoresTile<T, BN>::kThreads), 2) void default_dz_kernel(DenseArgs a) {
+    using Tile = ScoresTile<T, BN>;
+    constexpr int MI = Tile::MI, NI = Tile::NI;
+    int tile, pt;
+    chiplet_order(blockIdx.x, a.tiles_n, tile, pt);
+    if (tile >= a.tiles_m) return;
+    const int lane = threadIdx.x % kWave;
+    const long long item0 = a.first_item + (long long)tile * kItems;
+    f32x16 acc[MI][NI];
+    Tile::run(items_of<T>(a, item0), positions_of<T>(a, pt * BN), acc);
+    const int left = left_of(a.N - item0 - Tile::wave_row(), 32 * MI) - 4 * (lane / 32);
+    unsigned char* own = Tile::own_memory();
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+        const int q0 = pt * BN + Tile::wave_col() + 32 * ni, q = q0 + lane % 32;
+        const RowInfo info = a.info[q];
+        const long long from_first = (q < a.B ? (long long)a.targets[q] : -1) - item0 - Tile::wave_row();
+        const int hit = from_first >= 0 && from_first < 32 * MI ? (int)from_first - 4 * (lane / 32) : -64;
+        const bool special = __any(hit > -64) || left < 32 * MI - 4;           // (rare: a target among these items, the catalogue's end)
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[mi][ni][e] = exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -info.at));
+        if (special) {
+            stay_a_branch();
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int at = 32 * mi + 8 * (e / 4) + e % 4;
+                    if (at == hit) acc[mi][ni][e] -= kDzScale;
+                    if (at >= left) acc[mi][ni][e] = 0.0f;
+                }
+        }
+        // 32 positions x 32 items at a time through the wave's LDS: positions leave in rows of 16-byte pieces.  The pieces of
+        // a row are swapped by its number, so that writes and reads spread over the banks.
+        constexpr int kPieces = 32 * (int)sizeof(T) / 16;
+        T* out = static_cast<T*>(a.dz) + ((size_t)tile * a.padded + q0) * kItems + Tile::wave_row();
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+            typedef T T4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int four = 0; four < 4; ++four) {
+                T4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = (T)(acc[mi][ni][4 * four + e] * info.scale);
+                const int byte = (8 * four + 4 * (lane / 32)) * (int)sizeof(T), piece = (byte / 16) ^ (lane % 32 / (8 / kPieces) % kPieces);
+                *reinterpret_cast<T4*>(own + (lane % 32 * kPieces + piece) * 16 + byte % 16) = v;
+            }
+            wave_reads_after_writes();
+#pragma unroll
+            for (int i = 0; i < kPieces / 2; ++i) {
+                const int at = i * kWave + lane, row = at / kPieces, piece = at % kPieces;
+                const uint4 v = *reinterpret_cast<const uint4*>(own + (row * kPieces + (piece ^ (row / (8 / kPieces) % kPieces))) * 16);
+                *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(out + (size_t)row * kItems + 32 * mi) + piece * 16) = v;
+            }
+            wave_reads_after_writes();
+        }
+    }
+}
+
+// dW of a piece: [items][d], summed over the positions.
+template <typename T, int COLS>
+__global__ __launch_bounds__((TileW<T, COLS>::kThreads), 2) void default_dw_kernel(DenseArgs a) {
+    using Tile = TileW<T, COLS>;
+    int tile, ct;
+    chiplet_order(blockIdx.x, a.tiles_n, tile, ct);
+    if (tile >= a.tiles_m) return;
+    const int lane = threadIdx.x % kWave;
+    f32x16 acc[Tile::MI][Tile::NI];
+    const Operand dz{static_cast<const T*>(a.dz) + (size_t)tile * a.padded * kItems, kItems * sizeof(T), 0, kItems, 0, a.padded};
+    const Operand h{a.H, (size_t)a.d * sizeof(T), (long long)ct * COLS, a.d, 0, a.B};
+    Tile::run(dz, h, acc);
+    const float factor = *a.factor;
+    const long long item0 = a.first_item + (long long)tile * kItems + Tile::wave_row();
+    const int left = left_of(a.N - item0, 32 * Tile::MI), col0 = ct * COLS + Tile::wave_col();
+    // 32 items x 32 elements at a time through the wave's LDS, as in default_dz_kernel
+    constexpr int kPieces = 32 * (int)sizeof(T) / 16;
+    unsigned char* own = Tile::own_memory();
+#pragma unroll
+    for (int mi = 0; mi < Tile::MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < Tile::NI; ++ni) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int row = 8 * (e / 4) + 4 * (lane / 32) + e % 4, byte = lane % 32 * (int)sizeof(T);
+                const int piece = (byte / 16) ^ (row / (8 / kPieces) % kPieces);
+                *reinterpret_cast<T*>(own + (row * kPieces + piece) * 16 + byte % 16) = (T)(acc[mi][ni][e] * factor);
+            }
+            wave_reads_after_writes();
+#pragma unroll
+            for (int i = 0; i < kPieces / 2; ++i) {
+                const int at = i * kWave + lane, row = at / kPieces, piece = at % kPieces;
+                const uint4 v = *reinterpret_cast<const uint4*>(own + (row * kPieces + (piece ^ (row / (8 / kPieces) % kPieces))) * 16);
+                const int col = col0 + 32 * ni + piece * (16 / (int)sizeof(T));
+                if (32 * mi + row < left && col < a.d)
+                    *reinterpret_cast<uint4*>(static_cast<T*>(a.dW) + (size_t)(item0 + 32 * mi + row) * a.d + col) = v;
+            }
+            wave_reads_after_writes();
+        }
+}
+
+// A slice's share of dH: [positions][d] summed over its items of the piece, added to what earlier pieces left there.
+template <typename T, int BM, int BN>
+__global__ __launch_bounds__((TileH<T, BM, BN>::kThreads), 2) void default_dh_kernel(DenseArgs a) {
+    using Tile = TileH<T, BM, BN>;
+    int slice, tile;
+    chiplet_order(blockIdx.x, a.tiles_m * a.tiles_n, slice, tile);
+    if (slice >= a.slices) return;
+    const int rt = tile / a.tiles_n, ct = tile % a.tiles_n;
+    const int lane = threadIdx.x % kWave;
+    const long long k0 = min((long long)slice * a.slice_items, (long long)a.items), k1 = min(k0 + a.slice_items, (long long)a.items);
+    if (a.more && k0 == k1) return;
+    f32x16 acc[Tile::MI][Tile::NI];
+    const Operand dz{a.dz, kItems * sizeof(T), (long long)rt * BM, a.padded, k0, k1, kItems, (size_t)a.padded * kItems * sizeof(T)};
+    const Operand w{static_cast<const T*>(a.W) + (size_t)a.first_item * a.d, (size_t)a.d * sizeof(T), (long long)ct * BN, a.d, k0,
+                    min(k1, a.N - a.first_item)};
+    if (k0 < k1) Tile::run(dz, w, acc);
+    else {
+#pragma unroll
+        for (int mi = 0; mi < Tile::MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < Tile::NI; ++ni) acc[mi][ni] = f32x16{};
+    }
+    const int q0 = rt * BM + Tile::wave_row(), left = left_of(a.B - q0, 32 * Tile::MI) - 4 * (lane / 32);
+    float* out = a.partial_h + ((size_t)slice * a.B + q0 + 4 * (lane / 32)) * a.d;
+    auto put = [&](auto whole_c) {
+        constexpr bool whole = decltype(whole_c)::value;
+#pragma unroll
+        for (int mi = 0; mi < Tile::MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < Tile::NI; ++ni) {
+                const int col = ct * BN + Tile::wave_col() + 32 * ni + lane % 32;
+                float* p = out + (size_t)(32 * mi) * a.d + min(col, a.d - 1);
+                auto row = [&](int e) { return 32 * mi + 8 * (e / 4) + e % 4; };
+                float old[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) old[e] = 0.0f;
+                if (a.more && (whole || left > 32 * mi)) {         // (all of them asked for at once; past the end the first row's)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) old[e] = p[(size_t)(whole || row(e) < left ? row(e) - 32 * mi : 0) * a.d];
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (col < a.d && (whole || row(e) < left)) p[(size_t)(row(e) - 32 * mi) * a.d] = old[e] + acc[mi][ni][e];
+            }
+    };
+    if (a.B - q0 >= 32 * Tile::MI) put(std::true_type{});
+    else put(std::false_type{});
+}
+
+// The slices' shares of dH, added: every eighth slice by one of eight threads, these in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
+    __shared__ float part[8][32];
+    const size_t n = (size_t)a.B * a.d, i = (size_t)blockIdx.x * 32 + threadIdx.x % 32;
+    const int lead = threadIdx.x / 32;
+    float sum = 0.0f;
+    if (i < n) {
+#pragma unroll 4
+        for (int s = lead; s < a.slices; s += 8) sum += a.partial_h[(size_t)s * n + i];
+    }
+    part[lead][threadIdx.x % 32] = sum;
+    __syncthreads();
+    if (lead != 0 || i >= n) return;
+#pragma unroll
+    for (int w = 1; w < 8; ++w) sum += part[w][threadIdx.x];
+    static_cast<T*>(a.dH)[i] = (T)(sum * *a.factor);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// host side, by type of the operands (a translation unit each)
+
+struct DensePlan {
+    int positions, position_tiles, tiles_each, groups; // loss: positions of a tile of z
+    long long item_tiles;
+    int piece, pieces, padded, dz_positions, dw_cols;  // gradient: positions of a tile of dz, columns of one of dW
+    int rows, cols, rows_tiles, cols_tiles, slices;    // a tile of dH, and how many share its items
+    size_t info_at, dz_at, partial_at, bytes;          // its workspace
+};
+
+inline int grid_of(long long outer, long long inner) { return (int)(ceil_div(outer, 8) * 8 * inner); }     // see chiplet_order()
+
+constexpr int kSliceItems = 64;                        // a slice of dH's items is a multiple of this
+
+template <typename T> hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st);
+template <typename T> hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st);
+
+#ifdef PQ_DENSE_INSTANCE
+template <typename T, int POS>
+hipError_t launch_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((default_cross_entropy_kernel<T, POS>), dim3(grid_of(p.groups, p.position_tiles)), dim3(ScoresTile<T, POS>::kThreads), 0, st, a);
+    return hipGetLastError();
+}
+template <typename T, int POS>
+hipError_t launch_dz(const DenseArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((default_dz_kernel<T, POS>), dim3(grid_of(a.tiles_m, a.tiles_n)), dim3(ScoresTile<T, POS>::kThreads), 0, st, a);
+    return hipGetLastError();
+}
+template <typename T, int COLS>
+hipError_t launch_dw(const DenseArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((default_dw_kernel<T, COLS>), dim3(grid_of(a.tiles_m, a.tiles_n)), dim3(TileW<T, COLS>::kThreads), 0, st, a);
+    return hipGetLastError();
+}
+template <typename T, int ROWS, int COLS>
+hipError_t launch_dh(const DenseArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((default_dh_kernel<T, ROWS, COLS>), dim3(grid_of(a.slices, (long long)a.tiles_m * a.tiles_n)), dim3(TileH<T, ROWS, COLS>::kThreads), 0, st, a);
+    return hipGetLastError();
+}
+template <typename T, int ROWS>
+hipError_t launch_dh_cols(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+    return p.cols == 256 ? launch_dh<T, ROWS, 256>(a, st) : p.cols == 128 ? launch_dh<T, ROWS, 128>(a, st) : launch_dh<T, ROWS, 64>(a, st);
+}
+
+template <typename T>
+hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+    const hipError_t e = p.positions == 256 ? launch_loss<T, 256>(p, a, st) : p.positions == 128 ? launch_loss<T, 128>(p, a, st) : launch_loss<T, 64>(p, a, st);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((default_cross_entropy_join_kernel<T>), dim3(a.B), dim3(kWave), 0, st, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
+    hipLaunchKernelGGL((default_rows_kernel<T>), dim3(1), dim3(1024), 0, st, a);
+    hipError_t e = hipGetLastError();
+    for (int i = 0; i < p.pieces && e == hipSuccess; ++i) {
+        a.first_item = (long long)i * p.piece;
+        const long long left = a.N - a.first_item;
+        a.items = (int)round_up((size_t)(left < p.piece ? left : p.piece), kItems);
+        a.more = i > 0;
+        a.tiles_m = a.items / kItems;
+        a.tiles_n = p.padded / p.dz_positions;
+        e = p.dz_positions == 256 ? launch_dz<T, 256>(a, st) : p.dz_positions == 128 ? launch_dz<T, 128>(a, st) : launch_dz<T, 64>(a, st);
+        if (e != hipSuccess) break;
+        a.tiles_n = (int)ceil_div(a.d, p.dw_cols);
+        e = p.dw_cols == 256 ? launch_dw<T, 256>(a, st) : p.dw_cols == 128 ? launch_dw<T, 128>(a, st) : launch_dw<T, 64>(a, st);
+        if (e != hipSuccess) break;
+        a.tiles_m = p.rows_tiles;
+        a.tiles_n = p.cols_tiles;
+        a.slice_items = (int)round_up((size_t)ceil_div(a.items, p.slices), kSliceItems);
+        e = p.rows == 256 ? launch_dh_cols<T, 256>(p, a, st) : p.rows == 128 ? launch_dh_cols<T, 128>(p, a, st) : launch_dh_cols<T, 64>(p, a, st);
+    }
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((default_dh_join_kernel<T>), dim3((unsigned)ceil_div((long long)a.B * a.d, 32)), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
+template hipError_t dense_loss<PQ_DENSE_INSTANCE>(const DensePlan&, const DenseArgs&, hipStream_t);
+template hipError_t dense_backward<PQ_DENSE_INSTANCE>(const DensePlan&, DenseArgs, hipStream_t);
+#endif
+
+}  // namespace head
+}  // namespace pqk

@@ -6,7 +6,8 @@
 // two stages are in flight while one is multiplied.  A stage's chunks of 16 bytes are swapped within their row so that the
 // reads of a matrix operand meet every bank: the load picks its source accordingly, as it writes LDS in lane order.
 //   along:  [row][4 chunks], chunk c of row r lies at c ^ (r / 4 % 4); an operand is one 16-byte read
-//   across: [k][chunks of the rows], 16-bit: chunk c of row k lies at c ^ 4 (k % 4); an operand is two transposing reads
+//   across: [k][chunks of the rows], 16-bit: chunk c of row k lies at c ^ 4 (k % 4), in rows of eight chunks at c ^ 4 (k / 2 % 2);
+//           an operand is two transposing reads
 // A lane's operand is 16 bytes in either case: row lane % 32, and of k eight (16-bit: one 32x32x16 instruction) or four
 // (float32: four 32x32x2 instructions, whose order of k is the same for A and B).
 #pragma once
@@ -34,7 +35,7 @@ struct Operand {
     long long row0;        // first row (r) of the tile
     long long rows;        // rows there are: past the last one the last is read again
     long long k0, k1;      // range of k: past k1 zeros are read
-    int block = 0;         // along: a stored row holds this many k (a power of two, k0 a multiple of it), the next ones lie
+    int block = 0;         // along: a stored row holds this many k (a multiple of a stage's, as k0 is), the next ones lie
     size_t to_next = 0;    //   to_next bytes on; 0: all of them
 };
 
@@ -64,6 +65,7 @@ struct Side {
     static constexpr int kK = kStageBytes / (int)sizeof(T);                // k of a stage
     static constexpr int kRowChunks = ROWS * (int)sizeof(T) / 16;          // across: chunks of a stored row
     static constexpr int kLoads = kBytes / 16 / THREADS;                   // asynchronous loads of a thread and stage
+    static_assert(ROWS >= 64, "rows of at least eight chunks");
     static_assert(kBytes % (16 * THREADS) == 0, "every wave loads as much");
 
     const char* base;                                                      // moves on stage by stage
@@ -79,7 +81,7 @@ struct Side {
         tid = threadIdx.x;
         asm volatile("" : "+v"(tid));                                      // (so that a loop over tiles does not keep all this in registers meanwhile)
         k = o.k0; k1 = o.k1; ld = o.ld; block = o.block; to_next = o.to_next;
-        if constexpr (ALONG) base = static_cast<const char*>(o.base) + (size_t)o.row0 * ld + (block ? (size_t)(o.k0 / block) * to_next : (size_t)o.k0 * sizeof(T));
+        if constexpr (ALONG) base = static_cast<const char*>(o.base) + (size_t)o.row0 * ld + (block ? (size_t)(o.k0 / block) * to_next + (size_t)(o.k0 % block) * sizeof(T) : (size_t)o.k0 * sizeof(T));
         else base = static_cast<const char*>(o.base) + (size_t)o.k0 * ld + (size_t)o.row0 * sizeof(T);
         const int last = (int)min((long long)ROWS, o.rows - o.row0) - 1;
 #pragma unroll
@@ -94,7 +96,9 @@ struct Side {
             }
         }
     }
-    static __device__ __forceinline__ int swap(int chunk, int kk) { return sizeof(T) == 2 ? chunk ^ (4 * (kk % 4)) : chunk; }
+    static __device__ __forceinline__ int swap(int chunk, int kk) {
+        return sizeof(T) != 2 ? chunk : kRowChunks >= 16 ? chunk ^ (4 * (kk % 4)) : chunk ^ (4 * (kk / 2 % 2));
+    }
 
     // How many stages from k0 on hold nothing but operand.
     static __device__ __forceinline__ int whole_stages(const Operand& o) { return (int)((o.k1 - o.k0) / kK); }
@@ -168,9 +172,11 @@ struct MatrixTile {
         __shared__ __align__(16) unsigned char memory[BYTES];
         return memory;
     }
-    // Between products: LDS of a wave's own, to lay a 32-row block of its part out in rows.
-    static constexpr int kOwnBytes = A::kBytes / (kThreads / kWave);
-    static __device__ __forceinline__ unsigned char* own_memory() { return stage_memory<0, A::kBytes>() + wave() * kOwnBytes; }
+    // Between products: 4 KB of LDS for a wave alone, to lay a 32 x 32 block of its part out in rows (tiles of 256 rows).
+    static __device__ __forceinline__ unsigned char* own_memory() {
+        static_assert(A::kBytes == 4 * 4096, "four waves' share of a stage");
+        return (wave() < 4 ? stage_memory<0, A::kBytes>() : stage_memory<1, A::kBytes>()) + wave() % 4 * 4096;
+    }
 
     static __device__ __forceinline__ void run(const Operand& oa, const Operand& ob, f32x16 (&acc)[MI][NI]) {
         unsigned char *a0 = stage_memory<0, A::kBytes>(), *a1 = stage_memory<1, A::kBytes>(), *a2 = stage_memory<2, A::kBytes>();
