@@ -62,6 +62,13 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
     long long slices = (big ? 1LL : 2LL) * kCUs / ((long long)p.rows_tiles * p.cols_tiles);
     const long long most = p.piece / kSliceItems;
     p.slices = (int)(slices < 1 ? 1 : slices > most ? most : slices);
+    p.few = size == 2 && B <= kFew && d <= 512;
+    if (p.few) {                                       // a workgroup per compute unit; dz stays in LDS
+        const long long few_tiles = ceil_div(N, kFewBytes / 2 / (d > 256 ? 512 : d > 128 ? 256 : d > 64 ? 128 : 64));
+        p.slices = (int)(few_tiles < kCUs ? few_tiles : kCUs);
+        p.padded = kFew;
+        p.piece = 0;
+    }
     p.info_at = 256;
     p.dz_at = round_up(p.info_at + (size_t)p.padded * sizeof(RowInfo), 256);
     p.partial_at = round_up(p.dz_at + (size_t)p.padded * p.piece * size, 256);

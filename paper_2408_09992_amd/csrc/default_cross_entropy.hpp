@@ -359,6 +359,167 @@ __global__ __launch_bounds__((TileH<T, BM, BN>::kThreads), 2) void default_dh_ke
     else put(std::false_type{});
 }
 
+// ---------------------------------------------------------------------------------------------------------------
+// Gradients for up to 64 positions of 16-bit operands, d <= 512: one pass over W.  With so few positions all three products of
+// a tile of items are done before the memory has brought the next one, so a workgroup takes the tile from LDS for z, for dH
+// and (as H lies there too) dW, and W is read once instead of twice, dz never leaves the chip.
+
+constexpr int kFew = 64, kFewThreads = 512, kFewBytes = 32768;         // positions; threads; bytes of a tile of W
+
+// Rows of CHUNKS 16-byte chunks in LDS, chunk c of row r at c ^ turn(r): sixteen rows' reads of one chunk (an operand with k
+// along the rows) meet different banks, and so do four rows' reads of four (k across them, transposed).
+template <int CHUNKS>
+struct Rows {
+    static constexpr int kBytes = CHUNKS * 16;
+    static __device__ __forceinline__ int turn(int row) {
+        return CHUNKS >= 16 ? row % 4 * 4 + row / 4 % 4 : CHUNKS == 8 ? row / 2 % 2 * 4 + row / 4 % 4 : row / 4 % 4;
+    }
+    static __device__ __forceinline__ int at(int row, int chunk) { return row * kBytes + ((chunk ^ turn(row)) * 16); }
+    static __device__ __forceinline__ s16x8 along(const unsigned char* p, int row, int chunk) { return *reinterpret_cast<const s16x8*>(p + at(row, chunk)); }
+    // of k0 .. k0 + 15 (stored rows) and 32 columns from col0 the lane's operand: column lane % 32, k 8 (lane / 32) .. + 7
+    static __device__ __forceinline__ s16x8 across(const unsigned char* p, int k0, int col0) {
+        const int lane = threadIdx.x % kWave, k = k0 + 8 * (lane / 32) + lane % 16 / 4, col = col0 + 16 * (lane / 16 % 2) + 4 * (lane % 4);
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + at(k, col / 8) + col % 8 * 2));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + at(k + 4, col / 8) + col % 8 * 2));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+template <typename T>
+__device__ __forceinline__ f32x4_t multiply16(s16x8 x, s16x8 y, f32x4_t c) {
+    if constexpr (std::is_same<T, __bf16>::value) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
+}
+
+// D: d rounded up to 64, 128, 256 or 512.  A tile holds 16384 / D items.  Bound by memory: W in, dW out, 2.6 GB for 1.27M items
+// of 512 elements.
+template <typename T, int D>
+__global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a) {
+    constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
+    using RowsD = Rows<D / 8>;                                 // W and H
+    using RowsI = Rows<IT / 8>;                                // dz: [position][item]
+    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2], dz[kFew * IT * 2];
+    __shared__ RowInfo info[kFew];
+    __shared__ int target[kFew];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const size_t ld = (size_t)a.d * sizeof(T);
+    const long long tiles = (a.N + IT - 1) / IT;
+
+    // rows of W or H from `row0` on into LDS
+    auto bring = [&](const void* base, long long row0, long long rows, unsigned char* to, auto loads_c) {
+        constexpr int kLoads = decltype(loads_c)::value;
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + (size_t)row0 * ld, 0, kBufferBytes, 0x00020000);
+        const int last = (int)min(rows - row0, 65536LL) - 1;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int piece = (wave * kLoads + i) * kWave + lane, row = piece / (D / 8), chunk = (piece % (D / 8)) ^ RowsD::turn(row);
+            const uint32_t offset = chunk * 8 < a.d ? (uint32_t)min(row, last) * (uint32_t)ld + (uint32_t)chunk * 16u : kPastEnd;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (wave * kLoads + i) * kWave * 16), 16, offset, 0, 0, 0);
+        }
+    };
+    constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
+    bring(a.H, 0, a.B, h, std::integral_constant<int, kLoadsH>{});
+    bring(a.W, (long long)blockIdx.x * IT, a.N, w0, std::integral_constant<int, kLoadsW>{});
+    if (tid < kFew) {
+        info[tid] = a.info[tid];
+        target[tid] = tid < a.B ? a.targets[tid] : -1;
+    }
+    const float factor = *a.factor;
+    // dH: 2 x D / 32 blocks of 32 positions x 32 elements, shared by the waves; D = 64 leaves half of them without one
+    constexpr int kBlocksH = D / 16 >= kWaves ? D / 16 / kWaves : 1;
+    f32x16 dh[kBlocksH];
+#pragma unroll
+    for (int i = 0; i < kBlocksH; ++i) dh[i] = f32x16{};
+    const int h_pos = wave % 2 * 32, h_col = wave / 2 * kBlocksH * 32;         // (a wave's blocks: one half of the positions)
+
+    int turn = 0;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
+        unsigned char* w = turn % 2 ? w1 : w0;
+        // every wave's part of the tile has come (below), and every wave is done with the other buffer
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        bring(a.W, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1, std::integral_constant<int, kLoadsW>{});
+
+        // z and dz: blocks of 16 items x 16 positions
+        constexpr int kBlocksZ = IT / 16 * 4 / kWaves;
+#pragma unroll
+        for (int i = 0; i < kBlocksZ; ++i) {
+            const int block = wave * kBlocksZ + i, item0 = block / 4 * 16, pos = block % 4 * 16 + lane % 16;
+            f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k)
+                z = multiply16<T>(RowsD::along(w, item0 + lane % 16, 4 * k + lane / 16), RowsD::along(h, pos, 4 * k + lane / 16), z);
+            const RowInfo r = info[pos];
+            const int first = item0 + lane / 16 * 4;
+            const long long hit = (long long)target[pos] - (tile * IT + first), left = a.N - (tile * IT + first);
+            typedef T T4 __attribute__((ext_vector_type(4)));
+            T4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float p = exp2_fast(fmaf(z[e], kLog2e, -r.at));
+                if (e == hit) p -= kDzScale;
+                if (e >= left) p = 0.0f;
+                v[e] = (T)(p * r.scale);
+            }
+            *reinterpret_cast<T4*>(dz + RowsI::at(pos, first / 8) + first % 8 * 2) = v;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+        if (D / 16 >= kWaves || wave < D / 16) {
+#pragma unroll
+            for (int k = 0; k < IT / 16; ++k) {
+                const s16x8 x = RowsI::along(dz, h_pos + lane % 32, 2 * k + lane / 32);
+#pragma unroll
+                for (int i = 0; i < kBlocksH; ++i) {
+                    const s16x8 xs[1] = {x}, ys[1] = {RowsD::across(w, 16 * k, h_col + 32 * i)};
+                    f32x16 c[1][1] = {{dh[i]}};
+                    multiply<T, 1, 1>(xs, ys, c);
+                    dh[i] = c[0][0];
+                }
+            }
+        }
+        // dW: the wave's 32 items x 64 elements
+        const int w_item = wave * 2 / (D / 32) * 32, w_col = wave * 2 % (D / 32) * 32;
+        f32x16 dw[1][2] = {{f32x16{}, f32x16{}}};
+#pragma unroll
+        for (int k = 0; k < kFew / 16; ++k) {
+            const s16x8 x[1] = {RowsI::across(dz, 16 * k, w_item)}, y[2] = {RowsD::across(h, 16 * k, w_col), RowsD::across(h, 16 * k, w_col + 32)};
+            multiply<T, 1, 2>(x, y, dw);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (nobody reads the tile any more: it is the waves' own memory now)
+        unsigned char* own = w + wave * 4096;
+#pragma unroll
+        for (int ni = 0; ni < 2; ++ni)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int row = 8 * (e / 4) + 4 * (lane / 32) + e % 4, byte = (32 * ni + lane % 32) * 2;
+                *reinterpret_cast<T*>(own + row * 128 + ((byte / 16) ^ (row % 8)) * 16 + byte % 16) = (T)(dw[0][ni][e] * factor);
+            }
+        // the wave's part of the next tile has come; what it stores from here on may take until then
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + lane / 8, piece = lane % 8, col = w_col + piece * 8;
+            const uint4 v = *reinterpret_cast<const uint4*>(own + row * 128 + ((piece ^ (row % 8)) * 16));
+            const long long item = tile * IT + w_item + row;
+            if (item < a.N && col < a.d) *reinterpret_cast<uint4*>(static_cast<T*>(a.dW) + (size_t)item * a.d + col) = v;
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");                 // (a last load into LDS may be under way)
+    if (D / 16 >= kWaves || wave < D / 16) {
+#pragma unroll
+        for (int i = 0; i < kBlocksH; ++i) {
+            const int col = h_col + 32 * i + lane % 32;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int q = h_pos + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
+                if (q < a.B && col < a.d) a.partial_h[((size_t)blockIdx.x * a.B + q) * a.d + col] = dh[i][e];
+            }
+        }
+    }
+}
+
 // The slices' shares of dH, added: every eighth slice by one of eight threads, these in their order.
 template <typename T>
 __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
@@ -386,6 +547,7 @@ struct DensePlan {
     long long item_tiles;
     int piece, pieces, padded, dz_positions, dw_cols;  // gradient: positions of a tile of dz, columns of one of dW
     int rows, cols, rows_tiles, cols_tiles, slices;    // a tile of dH, and how many share its items
+    bool few;                                          // by default_few_kernel
     size_t info_at, dz_at, partial_at, bytes;          // its workspace
 };
 
@@ -434,7 +596,17 @@ template <typename T>
 hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
     hipLaunchKernelGGL((default_rows_kernel<T>), dim3(1), dim3(1024), 0, st, a);
     hipError_t e = hipGetLastError();
-    for (int i = 0; i < p.pieces && e == hipSuccess; ++i) {
+    if constexpr (sizeof(T) == 2) {
+        if (p.few && e == hipSuccess) {
+            const dim3 grid(p.slices), threads(kFewThreads);
+            if (a.d > 256) hipLaunchKernelGGL((default_few_kernel<T, 512>), grid, threads, 0, st, a);
+            else if (a.d > 128) hipLaunchKernelGGL((default_few_kernel<T, 256>), grid, threads, 0, st, a);
+            else if (a.d > 64) hipLaunchKernelGGL((default_few_kernel<T, 128>), grid, threads, 0, st, a);
+            else hipLaunchKernelGGL((default_few_kernel<T, 64>), grid, threads, 0, st, a);
+            e = hipGetLastError();
+        }
+    }
+    for (int i = 0; !p.few && i < p.pieces && e == hipSuccess; ++i) {
         a.first_item = (long long)i * p.piece;
         const long long left = a.N - a.first_item;
         a.items = (int)round_up((size_t)(left < p.piece ? left : p.piece), kItems);

@@ -75,6 +75,13 @@ def test_pieces_of_the_catalogue(pq, type):
     check(pq, *draw(N, d, B, type, seed=2), type)
 
 
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("N,d,B", [(9001, 304, 40), (20_003, 8, 64), (8200, 328, 1), (5000, 200, 33), (7777, 392, 64), (16_385, 56, 17), (33_000, 120, 5), (3, 512, 64), (70_001, 512, 64), (40_000, 264, 9)])
+def test_few_positions(pq, N, d, B, type):
+    # several tiles a workgroup, widths that end inside a tile or leave whole parts of it empty
+    check(pq, *draw(N, d, B, type, seed=N + d + B), type)
+
+
 @pytest.mark.parametrize("d", [4, 12, 20, 36, 100])
 def test_float32_widths(pq, d):
     check(pq, *draw(900, d, 70, "f32", seed=d), "f32")
