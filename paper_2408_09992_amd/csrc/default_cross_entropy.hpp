@@ -392,6 +392,88 @@ __device__ __forceinline__ f32x4_t multiply16(s16x8 x, s16x8 y, f32x4_t c) {
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
 }
 
+// Rows of W or of the queries from `row0` on into LDS: LOADS 16-byte pieces a thread; past the last row the last one again,
+// past a row's end zeros.
+template <typename T, int D, int LOADS>
+__device__ __forceinline__ void bring_rows(const void* base, int d, long long row0, long long rows, unsigned char* to) {
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const size_t ld = (size_t)d * sizeof(T);
+    const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + (size_t)row0 * ld, 0, kBufferBytes, 0x00020000);
+    const int last = (int)min(rows - row0, 65536LL) - 1;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int piece = (wave * LOADS + i) * kWave + lane, row = piece / (D / 8), chunk = (piece % (D / 8)) ^ Rows<D / 8>::turn(row);
+        const uint32_t offset = chunk * 8 < d ? (uint32_t)min(row, last) * (uint32_t)ld + (uint32_t)chunk * 16u : kPastEnd;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (wave * LOADS + i) * kWave * 16), 16, offset, 0, 0, 0);
+    }
+}
+
+// The loss of up to 64 positions of 16-bit operands, d <= 512: as default_few_kernel below takes its tiles, so that loads do not
+// pause between them (1.3 GB of W: 271 us by default_cross_entropy_kernel's tiles).
+template <typename T, int D>
+__global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseArgs a) {
+    constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
+    using RowsD = Rows<D / 8>;
+    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2];
+    __shared__ float2 stat[kWaves][kFew];
+    constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
+    constexpr int kBlocksZ = IT / 16 * 4 / kWaves, kParts = kBlocksZ < 4 ? kBlocksZ : 4;       // a wave's blocks of 16 x 16; positions among them / 16
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const long long tiles = (a.N + IT - 1) / IT;
+    bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h);
+    bring_rows<T, D, kLoadsW>(a.W, a.d, (long long)blockIdx.x * IT, a.N, w0);
+    float c[kParts], s[kParts];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) { c[i] = -__builtin_inff(); s[i] = 0.0f; }
+    int turn = 0;
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
+        const unsigned char* w = turn % 2 ? w1 : w0;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the tile has come, its other buffer is free
+        bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
+#pragma unroll
+        for (int i = 0; i < kBlocksZ; ++i) {
+            const int block = wave * kBlocksZ + i, item0 = block / 4 * 16, pos = block % 4 * 16 + lane % 16;
+            f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k)
+                z = multiply16<T>(RowsD::along(w, item0 + lane % 16, 4 * k + lane / 16), RowsD::along(h, pos, 4 * k + lane / 16), z);
+            const int left = left_of(a.N - tile * IT - item0, 16) - lane / 16 * 4;
+            if (left < 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e >= left) z[e] = -__builtin_inff();
+            }
+            const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) * kLog2e;
+            const int part = i % kParts;
+            if (__any(top > c[part] + kHeadroom)) {
+                if (top > c[part] + kHeadroom) { s[part] *= exp2_fast(c[part] - top); c[part] = top; }
+            }
+            const float at = c[part] == -__builtin_inff() ? 0.0f : c[part];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[part] += exp2_fast(fmaf(z[e], kLog2e, -at));
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");                  // (a last load into LDS may be under way)
+    for (int q = lane; q < kFew; q += kWave) stat[wave][q] = make_float2(-__builtin_inff(), 0.0f);
+    wave_reads_after_writes();
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+#pragma unroll
+        for (int x = 16; x < kWave; x *= 2) {
+            const float c2 = __shfl_xor(c[i], x), s2 = __shfl_xor(s[i], x);
+            join_sums(c[i], s[i], c2, s2);
+        }
+        if (lane < 16) stat[wave][(wave * kBlocksZ + i) % 4 * 16 + lane] = make_float2(c[i], s[i]);
+    }
+    __syncthreads();
+    if (tid < a.B) {
+        float2 t = stat[0][tid];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) join_sums(t.x, t.y, stat[w][tid].x, stat[w][tid].y);
+        a.partial[(size_t)blockIdx.x * a.B + tid] = t;
+    }
+}
+
 // D: d rounded up to 64, 128, 256 or 512.  A tile holds 16384 / D items.  Bound by memory: W in, dW out, 2.6 GB for 1.27M items
 // of 512 elements.
 template <typename T, int D>
@@ -403,24 +485,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     __shared__ RowInfo info[kFew];
     __shared__ int target[kFew];
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const size_t ld = (size_t)a.d * sizeof(T);
     const long long tiles = (a.N + IT - 1) / IT;
-
-    // rows of W or H from `row0` on into LDS
-    auto bring = [&](const void* base, long long row0, long long rows, unsigned char* to, auto loads_c) {
-        constexpr int kLoads = decltype(loads_c)::value;
-        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + (size_t)row0 * ld, 0, kBufferBytes, 0x00020000);
-        const int last = (int)min(rows - row0, 65536LL) - 1;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int piece = (wave * kLoads + i) * kWave + lane, row = piece / (D / 8), chunk = (piece % (D / 8)) ^ RowsD::turn(row);
-            const uint32_t offset = chunk * 8 < a.d ? (uint32_t)min(row, last) * (uint32_t)ld + (uint32_t)chunk * 16u : kPastEnd;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (wave * kLoads + i) * kWave * 16), 16, offset, 0, 0, 0);
-        }
-    };
     constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
-    bring(a.H, 0, a.B, h, std::integral_constant<int, kLoadsH>{});
-    bring(a.W, (long long)blockIdx.x * IT, a.N, w0, std::integral_constant<int, kLoadsW>{});
+    bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h);
+    bring_rows<T, D, kLoadsW>(a.W, a.d, (long long)blockIdx.x * IT, a.N, w0);
     if (tid < kFew) {
         info[tid] = a.info[tid];
         target[tid] = tid < a.B ? a.targets[tid] : -1;
@@ -439,7 +507,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
         unsigned char* w = turn % 2 ? w1 : w0;
         // every wave's part of the tile has come (below), and every wave is done with the other buffer
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        bring(a.W, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1, std::integral_constant<int, kLoadsW>{});
+        bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
 
         // z and dz: blocks of 16 items x 16 positions
         constexpr int kBlocksZ = IT / 16 * 4 / kWaves;
@@ -585,8 +653,30 @@ hipError_t launch_dh_cols(const DensePlan& p, const DenseArgs& a, hipStream_t st
 }
 
 template <typename T>
+hipError_t launch_few_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+    const dim3 grid(p.groups), threads(kFewThreads);
+    if (a.d > 256) hipLaunchKernelGGL((default_few_loss_kernel<T, 512>), grid, threads, 0, st, a);
+    else if (a.d > 128) hipLaunchKernelGGL((default_few_loss_kernel<T, 256>), grid, threads, 0, st, a);
+    else if (a.d > 64) hipLaunchKernelGGL((default_few_loss_kernel<T, 128>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((default_few_loss_kernel<T, 64>), grid, threads, 0, st, a);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_few(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+    const dim3 grid(p.slices), threads(kFewThreads);
+    if (a.d > 256) hipLaunchKernelGGL((default_few_kernel<T, 512>), grid, threads, 0, st, a);
+    else if (a.d > 128) hipLaunchKernelGGL((default_few_kernel<T, 256>), grid, threads, 0, st, a);
+    else if (a.d > 64) hipLaunchKernelGGL((default_few_kernel<T, 128>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((default_few_kernel<T, 64>), grid, threads, 0, st, a);
+    return hipGetLastError();
+}
+
+template <typename T>
 hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
-    const hipError_t e = p.positions == 256 ? launch_loss<T, 256>(p, a, st) : p.positions == 128 ? launch_loss<T, 128>(p, a, st) : launch_loss<T, 64>(p, a, st);
+    hipError_t e;
+    if constexpr (sizeof(T) == 2) e = p.few ? launch_few_loss<T>(p, a, st) : hipSuccess;
+    if (sizeof(T) != 2 || !p.few)
+        e = p.positions == 256 ? launch_loss<T, 256>(p, a, st) : p.positions == 128 ? launch_loss<T, 128>(p, a, st) : launch_loss<T, 64>(p, a, st);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((default_cross_entropy_join_kernel<T>), dim3(a.B), dim3(kWave), 0, st, a);
     return hipGetLastError();
@@ -597,14 +687,7 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
     hipLaunchKernelGGL((default_rows_kernel<T>), dim3(1), dim3(1024), 0, st, a);
     hipError_t e = hipGetLastError();
     if constexpr (sizeof(T) == 2) {
-        if (p.few && e == hipSuccess) {
-            const dim3 grid(p.slices), threads(kFewThreads);
-            if (a.d > 256) hipLaunchKernelGGL((default_few_kernel<T, 512>), grid, threads, 0, st, a);
-            else if (a.d > 128) hipLaunchKernelGGL((default_few_kernel<T, 256>), grid, threads, 0, st, a);
-            else if (a.d > 64) hipLaunchKernelGGL((default_few_kernel<T, 128>), grid, threads, 0, st, a);
-            else hipLaunchKernelGGL((default_few_kernel<T, 64>), grid, threads, 0, st, a);
-            e = hipGetLastError();
-        }
+        if (p.few && e == hipSuccess) e = launch_few<T>(p, a, st);
     }
     for (int i = 0; !p.few && i < p.pieces && e == hipSuccess; ++i) {
         a.first_item = (long long)i * p.piece;
