@@ -76,10 +76,12 @@ int pq_cross_entropy_u16_backward(const uint16_t* codes, const float* S, const i
  *   dS float [B][m][b];  queries float [B][d];  centroids float [m][b][s];  dqueries float [B][d];  dcentroids float [m][b][s]
  * Sums in float32 by fused multiply-adds, in an order that depends on the shape alone.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (B, d, m, b < 1; d % m; b > 65536), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B, m > PQ_MAX_M),
- *         PQ_ERR_ALIGN, PQ_ERR_HIP.
+ *         PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
  */
+size_t pq_subitem_scores_backward_workspace_bytes(int B, int d, int m, int b);
 int pq_subitem_scores_backward(const float* dS, const float* queries, const float* centroids, float* dqueries,
-                               float* dcentroids, int B, int d, int m, int b, void* stream);
+                               float* dcentroids, int B, int d, int m, int b, void* workspace, size_t workspace_bytes,
+                               void* stream);
 
 #define PQ_FLOAT32  0        /* `type` of the calls below: what W, queries and their gradients hold */
 #define PQ_BFLOAT16 1

@@ -13,7 +13,7 @@ __all__ = ["workloads", "pq_subitem_scores", "pq_score_topk", "pq_score_topk_wor
            "pq_cross_entropy_u16_workspace_bytes", "pq_cross_entropy_u16_backward", "pq_cross_entropy_u16_backward_workspace_bytes",
            "pq_default_cross_entropy", "pq_default_cross_entropy_workspace_bytes", "pq_default_cross_entropy_backward",
            "pq_default_cross_entropy_backward_workspace_bytes",
-           "pq_subitem_scores_backward", "pq_quantise_items", "pq_default_scores_q4"]
+           "pq_subitem_scores_backward", "pq_subitem_scores_backward_workspace_bytes", "pq_quantise_items", "pq_default_scores_q4"]
 
 
 def __getattr__(name):

@@ -93,7 +93,9 @@ def lib() -> ctypes.CDLL:
                 size.argtypes, size.restype = [LL, I, I, I], SZ
                 getattr(L, call).argtypes = [P] * pointers + [LL, I, I, I] + [P] * outputs + [P, SZ, P]
                 getattr(L, call).restype = I
-        L.pq_subitem_scores_backward.argtypes = [P, P, P, P, P, I, I, I, I, P]
+        L.pq_subitem_scores_backward_workspace_bytes.argtypes = [I, I, I, I]
+        L.pq_subitem_scores_backward_workspace_bytes.restype = SZ
+        L.pq_subitem_scores_backward.argtypes = [P, P, P, P, P, I, I, I, I, P, SZ, P]
         L.pq_subitem_scores_backward.restype = I
         for call in ("pq_default_cross_entropy", "pq_default_cross_entropy_backward"):
             size = getattr(L, call + "_workspace_bytes")
@@ -657,10 +659,15 @@ def pq_default_cross_entropy_backward(W: torch.Tensor, queries: torch.Tensor, ta
     return dqueries, dW
 
 
-def pq_subitem_scores_backward(dS: torch.Tensor, queries: torch.Tensor, centroids: torch.Tensor, dqueries: Optional[torch.Tensor] = None,
-                               dcentroids: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+def pq_subitem_scores_backward_workspace_bytes(B: int, d: int, m: int, b: int) -> int:
+    return int(lib().pq_subitem_scores_backward_workspace_bytes(B, d, m, b))
+
+
+def pq_subitem_scores_backward(dS: torch.Tensor, queries: torch.Tensor, centroids: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+                               dqueries: Optional[torch.Tensor] = None, dcentroids: Optional[torch.Tensor] = None
+                               ) -> Tuple[torch.Tensor, torch.Tensor]:
     """Eq. 4's gradients: dS fp32 [B][m][b], queries [B][d], centroids [m][b][d/m] -> (dqueries [B][d], dcentroids [m][b][d/m])."""
-    r = (_native_module or _native()).subitem_scores_backward(dS, queries, centroids, dqueries, dcentroids)
+    r = (_native_module or _native()).subitem_scores_backward(dS, queries, centroids, workspace, dqueries, dcentroids)
     if r.__class__ is int:
         raise PQError(r, "pq_subitem_scores_backward")
     if r is not None:
@@ -676,9 +683,10 @@ def pq_subitem_scores_backward(dS: torch.Tensor, queries: torch.Tensor, centroid
     dcentroids = torch.empty_like(centroids) if dcentroids is None else _dev(dcentroids, torch.float32, "dcentroids")
     if dqueries.shape != queries.shape or dcentroids.shape != centroids.shape:
         raise ValueError("gradients must have the shapes of queries and centroids")
-    _same_device(dS, queries, centroids, dqueries, dcentroids)
+    workspace = _scratch(workspace, pq_subitem_scores_backward_workspace_bytes(B, d, m, b), dS)
+    _same_device(dS, queries, centroids, dqueries, dcentroids, workspace)
     rc = lib().pq_subitem_scores_backward(dS.data_ptr(), queries.data_ptr(), centroids.data_ptr(), dqueries.data_ptr(),
-                                          dcentroids.data_ptr(), B, d, m, b, _stream())
+                                          dcentroids.data_ptr(), B, d, m, b, workspace.data_ptr(), workspace.numel(), _stream())
     if rc != PQ_OK:
         raise PQError(rc, "pq_subitem_scores_backward")
     return dqueries, dcentroids

@@ -153,6 +153,14 @@ struct Side {
     }
 };
 
+// An array per stage and side: the compiler tells loads into one from reads of another, and waits for no more than it must.
+// (Tiles of equal sizes in one kernel share them.)
+template <int WHICH, int BYTES>
+__device__ __forceinline__ unsigned char* stage_memory() {
+    __shared__ __align__(16) unsigned char memory[BYTES];
+    return memory;
+}
+
 // BM x BN tile by waves in a grid of (BM / WM) x (BN / WN).  acc[mi][ni][i] is row 32 mi + 8 (i / 4) + 4 (lane / 32) + i % 4,
 // column 32 ni + lane % 32 of the wave's part.
 template <typename T, int BM, int BN, int WM, int WN, bool A_ALONG, bool B_ALONG>
@@ -166,12 +174,6 @@ struct MatrixTile {
     static __device__ __forceinline__ int wave_row() { return wave() / (BN / WN) * WM; }
     static __device__ __forceinline__ int wave_col() { return wave() % (BN / WN) * WN; }
 
-    // An array per stage and side: the compiler tells loads into one from reads of another, and waits for no more than it must.
-    template <int WHICH, int BYTES>
-    static __device__ __forceinline__ unsigned char* stage_memory() {
-        __shared__ __align__(16) unsigned char memory[BYTES];
-        return memory;
-    }
     // Between products: 4 KB of LDS for a wave alone, to lay a 32 x 32 block of its part out in rows (tiles of 256 rows).
     static __device__ __forceinline__ unsigned char* own_memory() {
         static_assert(A::kBytes == 4 * 4096, "four waves' share of a stage");

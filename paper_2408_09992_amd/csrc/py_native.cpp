@@ -297,21 +297,22 @@ PyObject* cross_entropy_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
     });
 }
 
-// subitem_scores_backward(dS, queries, centroids, dqueries | None, dcentroids | None) -> (dqueries, dcentroids), an error code, or None
+// subitem_scores_backward(dS, queries, centroids, workspace | None, dqueries | None, dcentroids | None) -> (dqueries, dcentroids), an error code, or None
 PyObject* subitem_scores_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
-        if (n != 5) return none();
+        if (n != 6) return none();
         const int device = c10::hip::current_device();
         const at::Tensor *g = plain(args[0], at::kFloat, device), *q = plain(args[1], at::kFloat, device), *c = plain(args[2], at::kFloat, device);
         if (!g || !q || !c || g->dim() != 3 || q->dim() != 2 || c->dim() != 3) return none();
         const int64_t B = q->size(0), d = q->size(1), m = c->size(0), b = c->size(1);
         if (m * c->size(2) != d || g->size(0) != B || g->size(1) != m || g->size(2) != b) return none();
-        Output dq(args[3], q->sizes(), at::kFloat, device), dc(args[4], c->sizes(), at::kFloat, device);
-        if (dq.bad || dc.bad) return none();
+        Output dq(args[4], q->sizes(), at::kFloat, device), dc(args[5], c->sizes(), at::kFloat, device);
+        Scratch ws(args[3], pq_subitem_scores_backward_workspace_bytes((int)B, (int)d, (int)m, (int)b), device);
+        if (dq.bad || dc.bad || ws.bad) return none();
         const float *dS = g->const_data_ptr<float>(), *phi = q->const_data_ptr<float>(), *psi = c->const_data_ptr<float>();
         float *dphi = dq.floats(), *dpsi = dc.floats();
         void* st = current_stream();
-        const int rc = without_gil([&]() { return pq_subitem_scores_backward(dS, phi, psi, dphi, dpsi, (int)B, (int)d, (int)m, (int)b, st); });
+        const int rc = without_gil([&]() { return pq_subitem_scores_backward(dS, phi, psi, dphi, dpsi, (int)B, (int)d, (int)m, (int)b, ws.p, ws.bytes, st); });
         return rc != PQ_OK ? PyLong_FromLong(rc) : pair(dq, dc);
     });
 }

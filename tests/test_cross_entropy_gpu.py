@@ -183,7 +183,7 @@ def test_in_a_graph(pq):
     codes, S, targets, grad = draw(30_000, 8, 256, 6, seed=10)
     c, s, t, g = on_gpu(codes, S, targets, grad)
     phi, psi = torch.randn(6, 64, device="cuda"), torch.randn(8, 256, 8, device="cuda")
-    size = max(pq.pq_cross_entropy_workspace_bytes(30_000, 6, 8, 256), pq.pq_cross_entropy_backward_workspace_bytes(30_000, 6, 8, 256))
+    size = max(pq.pq_cross_entropy_workspace_bytes(30_000, 6, 8, 256), pq.pq_cross_entropy_backward_workspace_bytes(30_000, 6, 8, 256), pq.pq_subitem_scores_backward_workspace_bytes(6, 64, 8, 256))
     ws = torch.empty(size, dtype=torch.uint8, device="cuda")
     loss, lse, dS = torch.empty(6, device="cuda"), torch.empty(6, device="cuda"), torch.empty_like(s)
     dphi, dpsi = torch.empty_like(phi), torch.empty_like(psi)
@@ -191,7 +191,7 @@ def test_in_a_graph(pq):
     def step():
         pq.pq_cross_entropy(c, s, t, ws, loss, lse)
         pq.pq_cross_entropy_backward(c, s, t, lse, g, ws, dS)
-        pq.pq_subitem_scores_backward(dS, phi, psi, dphi, dpsi)
+        pq.pq_subitem_scores_backward(dS, phi, psi, ws, dphi, dpsi)
 
     step()
     torch.cuda.synchronize()
@@ -228,7 +228,7 @@ def test_codes_beyond_32_bits_of_offset(pq):
     assert not dS[0, :, 1:255].any()
 
 
-@pytest.mark.parametrize("B,d,m,b", [(1, 1, 1, 1), (1, 64, 4, 256), (3, 24, 8, 5), (33, 512, 8, 256), (257, 128, 16, 64), (5, 96, 2, 1000), (64, 96, 3, 33), (1024, 512, 8, 256), (7, 40, 5, 257)])
+@pytest.mark.parametrize("B,d,m,b", [(1, 1, 1, 1), (1, 64, 4, 256), (3, 24, 8, 5), (33, 512, 8, 256), (257, 128, 16, 64), (5, 96, 2, 1000), (64, 96, 3, 33), (1024, 512, 8, 256), (7, 40, 5, 257), (130, 40, 5, 20), (1300, 96, 3, 260), (700, 34, 2, 100), (600, 64, 4, 1000), (2500, 128, 16, 64)])
 def test_gradients_of_queries_and_centroids(pq, B, d, m, b):
     rng = np.random.default_rng(B + d + m + b)
     s = d // m
@@ -241,14 +241,26 @@ def test_gradients_of_queries_and_centroids(pq, B, d, m, b):
         assert np.all(np.abs(got - want) <= U * (n + 8) * size + 1e-37)
 
 
-def test_one_gradient_alone(pq):
-    dS, phi, psi = torch.randn(5, 4, 256, device="cuda"), torch.randn(5, 64, device="cuda"), torch.randn(4, 256, 16, device="cuda")
+@pytest.mark.parametrize("B", [5, 1300])
+def test_one_gradient_alone(pq, B):
+    dS, phi, psi = torch.randn(B, 4, 256, device="cuda"), torch.randn(B, 64, device="cuda"), torch.randn(4, 256, 16, device="cuda")
     dphi, dpsi = pq.pq_subitem_scores_backward(dS, phi, psi)
     one, two = torch.zeros_like(phi), torch.zeros_like(psi)
+    size = pq.pq_subitem_scores_backward_workspace_bytes(B, 64, 4, 256)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
     stream = torch.cuda.current_stream().cuda_stream
-    assert pq.lib().pq_subitem_scores_backward(dS.data_ptr(), None, psi.data_ptr(), one.data_ptr(), None, 5, 64, 4, 256, stream) == 0
-    assert pq.lib().pq_subitem_scores_backward(dS.data_ptr(), phi.data_ptr(), None, None, two.data_ptr(), 5, 64, 4, 256, stream) == 0
+    assert pq.lib().pq_subitem_scores_backward(dS.data_ptr(), None, psi.data_ptr(), one.data_ptr(), None, B, 64, 4, 256, ws.data_ptr(), size, stream) == 0
+    assert pq.lib().pq_subitem_scores_backward(dS.data_ptr(), phi.data_ptr(), None, None, two.data_ptr(), B, 64, 4, 256, ws.data_ptr(), size, stream) == 0
     assert torch.equal(one, dphi) and torch.equal(two, dpsi)
+
+
+def test_rows_that_are_not_aligned(pq):
+    # queries whose rows begin between 16-byte pieces
+    B, m, b, s = 1200, 4, 64, 16
+    dS, psi = torch.randn(B, m, b, device="cuda"), torch.randn(m, b, s, device="cuda")
+    phi = torch.randn(B * m * s + 1, device="cuda")[1:].view(B, m * s)
+    for got, want in zip(pq.pq_subitem_scores_backward(dS, phi, psi), pq.pq_subitem_scores_backward(dS, phi.clone(), psi)):
+        assert (got - want).abs().max().item() <= 1e-4
 
 
 def test_refusals_of_the_functions(pq):
