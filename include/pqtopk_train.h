@@ -91,7 +91,8 @@ int pq_subitem_scores_backward(const float* dS, const float* queries, const floa
  * Loss and log-sum of B positions by the default scorer: r_qi = W[i] . phi_q.
  *   W        in   type [N][d]   (16-byte aligned);   queries  in  type [B][d]  (16-byte aligned)
  *   targets  in   int32 [B];    loss, lse  out  float [B]
- * Scores are float32 sums of the products on the matrix cores (16-bit inputs: exact products); they are never stored.
+ * Scores are float32 sums of the products on the matrix cores (16-bit inputs: exact products; float32: products to 2^-25 of
+ * themselves, from three bfloat16 pieces of each factor); they are never stored.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, B, d < 1; an unknown type; N >= 2^31), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B, d > 16384,
  *         d no multiple of 16 bytes of elements: 4 of float32, 8 of 16-bit types), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
  */

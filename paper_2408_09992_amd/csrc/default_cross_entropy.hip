@@ -10,12 +10,12 @@ constexpr long long kMaxPiece = 1LL << 22;
 
 
 // What a tile of 256 rows and `cols` columns takes a compute unit next to one of 256 x 256 that keeps the matrix cores as busy
-// as can be (the smaller ones' rates: 134 of 143 TFLOP/s and about 115 in float32; 880 of 1040 and about 600 in 16 bits).
+// as can be (the smaller ones' rates: 203 of 208 TFLOP/s and about 165 in float32; 880 of 1040 and about 600 in 16 bits).
 // Two workgroups of a smaller tile share a compute unit, but one alone has nearly all of it: what counts is how many a
 // compute unit gets.
 double tile_cost(int cols, int size) {
     const bool f32 = size == 4;
-    return cols == 256 ? 1.0 : cols == 128 ? 0.5 / (f32 ? 0.94 : 0.86) : 0.25 / (f32 ? 0.8 : 0.6);
+    return cols == 256 ? 1.0 : cols == 128 ? 0.5 / (f32 ? 0.97 : 0.86) : 0.25 / (f32 ? 0.8 : 0.6);
 }
 constexpr double kTileStart = 0.1;                     // what a workgroup takes besides its products
 

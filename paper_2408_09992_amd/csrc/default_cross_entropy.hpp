@@ -22,8 +22,8 @@ constexpr int kItems = 256;                           // items of a tile of z an
 struct RowInfo { float at, scale; };                  // of a position: 2^(z log2e - at) is p 2^15; its g over the largest |g|
 
 // The tiles: z for kItems items and POS positions; dH for ROWS positions and COLS elements; dW for kItems items and COLS
-// elements.  Tiles of 256 x 256 by eight waves feed the matrix cores best (143 TFLOP/s in float32, 1040 to 1130 in bfloat16,
-// against 134 and 880 to 1090 with 256 x 128 by four); the smaller ones are for few positions and narrow embeddings.
+// elements.  Tiles of 256 x 256 by eight waves feed the matrix cores best (208 TFLOP/s in float32, 1040 to 1130 in bfloat16,
+// against 203 and 880 to 1090 with 256 x 128 by four); the smaller ones are for few positions and narrow embeddings.
 template <typename T, int POS> struct ScoresTile;
 template <typename T> struct ScoresTile<T, 64> : MatrixTile<T, kItems, 64, 64, 64, true, true> {};
 template <typename T> struct ScoresTile<T, 128> : MatrixTile<T, kItems, 128, 128, 64, true, true> {};

@@ -8,8 +8,7 @@
 //   along:  [row][4 chunks], chunk c of row r lies at c ^ (r / 4 % 4); an operand is one 16-byte read
 //   across: [k][chunks of the rows], 16-bit: chunk c of row k lies at c ^ 4 (k % 4), in rows of eight chunks at c ^ 4 (k / 2 % 2);
 //           an operand is two transposing reads
-// A lane's operand is 16 bytes in either case: row lane % 32, and of k eight (16-bit: one 32x32x16 instruction) or four
-// (float32: four 32x32x2 instructions, whose order of k is the same for A and B).
+// A lane's operand of a 32x32x16 instruction is eight k of row lane % 32; float32 operands are multiplied in 16-bit pieces.
 #pragma once
 #include <type_traits>
 #include "head_common.hpp"
@@ -23,6 +22,9 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // A stage's loads see 2 GB from its first byte on (a tile's rows are at most 256 times 64 KB apart); an offset behind them reads 0.
 constexpr uint32_t kBufferBytes = 0x7FFFFFFFu, kPastEnd = 0x80000000u;
@@ -39,23 +41,62 @@ struct Operand {
     size_t to_next = 0;    //   to_next bytes on; 0: all of them
 };
 
-// acc[mi][ni] += x[mi] y[ni].  float32: the four instructions of a pair are as far apart as the pairs allow, as each waits for
-// the sum that the one before it leaves.
+// acc[mi][ni] += x[mi] y[ni], 16-bit operands of sixteen k.
 template <typename T, int MI, int NI>
 __device__ __forceinline__ void multiply(const s16x8 (&x)[MI], const s16x8 (&y)[NI], f32x16 (&acc)[MI][NI]) {
 #pragma unroll
-    for (int i = 0; i < (sizeof(T) == 4 ? 4 : 1); ++i)
+    for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi)
+        for (int ni = 0; ni < NI; ++ni) {
+            if constexpr (std::is_same<T, _Float16>::value)
+                acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x[mi]), __builtin_bit_cast(f16x8, y[ni]), acc[mi][ni], 0, 0, 0);
+            else
+                acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[mi]), __builtin_bit_cast(bf16x8, y[ni]), acc[mi][ni], 0, 0, 0);
+        }
+}
+
+// Eight floats as the sums of three bfloat16 each: x = p0 + p1 + p2 to 2^-26 |x| (each piece is what the ones before it leave,
+// rounded to nearest).
+struct Pieces { s16x8 p[3]; };
+__device__ __forceinline__ Pieces pieces_of(s16x8 a, s16x8 b) {
+    const f32x4 u = __builtin_bit_cast(f32x4, a), v = __builtin_bit_cast(f32x4, b);
+    float x[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+    Pieces r;
 #pragma unroll
-            for (int ni = 0; ni < NI; ++ni) {
-                if constexpr (std::is_same<T, __bf16>::value)
-                    acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x[mi]), __builtin_bit_cast(bf16x8, y[ni]), acc[mi][ni], 0, 0, 0);
-                else if constexpr (std::is_same<T, _Float16>::value)
-                    acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x[mi]), __builtin_bit_cast(f16x8, y[ni]), acc[mi][ni], 0, 0, 0);
-                else
-                    acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(f32x4, x[mi])[i], __builtin_bit_cast(f32x4, y[ni])[i], acc[mi][ni], 0, 0, 0);
+    for (int k = 0; k < 3; ++k) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2 * i], x[2 * i + 1]}), bf16x2));
+            if (k < 2) {
+                x[2 * i] -= __builtin_bit_cast(float, w[i] << 16);
+                x[2 * i + 1] -= __builtin_bit_cast(float, w[i] & 0xFFFF0000u);
             }
+        }
+        r.p[k] = __builtin_bit_cast(s16x8, w);
+    }
+    return r;
+}
+
+// The same for sixteen k of float32, x and y holding four k each.  A product is six of its pieces', all but those of 2^-24
+// and less of it (p1 q2, p2 q1, p2 q2: together below 2^-25 |x y|, half a unit of float32), the small ones first.  Six
+// instructions of the 16-bit rate take 37 % of the time of the eight float32 ones: 208 against 146 TFLOP/s at 4096^3.
+template <int MI, int NI>
+__device__ __forceinline__ void multiply_floats(const s16x8 (&x)[2][MI], const s16x8 (&y)[2][NI], f32x16 (&acc)[MI][NI]) {
+    constexpr int order[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+    Pieces q[NI];
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) q[ni] = pieces_of(y[0][ni], y[1][ni]);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+        const Pieces p = pieces_of(x[0][mi], x[1][mi]);
+#pragma unroll
+        for (int o = 0; o < 6; ++o)
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni)
+                acc[mi][ni] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, p.p[order[o][0]]), __builtin_bit_cast(bf16x8, q[ni].p[order[o][1]]),
+                                                                      acc[mi][ni], 0, 0, 0);
+    }
 }
 
 // ROWS rows of an operand, as a workgroup of THREADS brings them to LDS and its waves read them.
@@ -130,12 +171,13 @@ struct Side {
         if (ALONG && block && k % block == 0) base += to_next - (size_t)block * sizeof(T);
     }
 
-    // the operand of rows row0 .. + 31 and the u-th half of the stage
+    // rows row0 .. + 31: 16-bit, the operand of the u-th half of the stage; float32, the u-th half of the lane's eight k
     static __device__ __forceinline__ s16x8 read(const unsigned char* stage, int row0, int u) {
         const int lane = threadIdx.x % kWave;
         if constexpr (ALONG) {
             const int row = row0 + lane % 32;
-            return *reinterpret_cast<const s16x8*>(stage + row * kStageBytes + (((2 * u + lane / 32) ^ (row / 4 % 4)) * 16));
+            const int chunk = sizeof(T) == 2 ? 2 * u + lane / 32 : 2 * (lane / 32) + u;
+            return *reinterpret_cast<const s16x8*>(stage + row * kStageBytes + ((chunk ^ (row / 4 % 4)) * 16));
         } else if constexpr (sizeof(T) == 2) {
             // sixteen lanes read four stored rows of sixteen elements and get a column each
             const int kk = 16 * u + 8 * (lane / 32) + lane % 16 / 4, row = row0 + 16 * (lane / 16 % 2) + 4 * (lane % 4);
@@ -144,7 +186,7 @@ struct Side {
             const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 4 * (ROWS * 2)));
             return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         } else {
-            const unsigned char* p = stage + (8 * u + 4 * (lane / 32)) * (ROWS * 4) + (row0 + lane % 32) * 4;
+            const unsigned char* p = stage + (8 * (lane / 32) + 4 * u) * (ROWS * 4) + (row0 + lane % 32) * 4;
             f32x4 v;
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float*>(p + i * (ROWS * 4));
@@ -215,8 +257,10 @@ struct MatrixTile {
             }
             __builtin_amdgcn_sched_barrier(0);                 // (reads behind a load into LDS would wait for that load)
             load((stage + 2) % 3, checked);
+            if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) multiply<T, MI, NI>(x[u], y[u], acc);
+                for (int u = 0; u < 2; ++u) multiply<T, MI, NI>(x[u], y[u], acc);
+            } else multiply_floats<MI, NI>(x, y, acc);
         };
         using std::integral_constant;
         // Two stages more than there are get loaded (zeros): the count of loads in flight is the same in every step, and the
