@@ -15,7 +15,8 @@
  * Conventions are those of pqtopk.h (device pointers, row-major, caller's stream, no allocation, no synchronisation,
  * arguments checked before anything is enqueued), and besides:
  *   - targets are int32 item ids.  A position whose target lies outside [0, N) has none (padding): its lse is computed,
- *     its loss is 0 and it adds nothing to any gradient.
+ *     its loss is 0 and it adds nothing to any gradient, whatever its query holds (NaN too).  (Its rows of dS are zeros:
+ *     Eq. 4's gradients, which know of no targets, multiply these with its query, so there it has to be finite.)
  *   - grad_loss is float [B], the gradient of the final objective with respect to loss_q (1 / count for a mean).
  *   - Softmax statistics and all sums are held in 32 bits or more.  Every result is the same from run to run: no sum
  *     depends on the order in which workgroups or waves finish.
@@ -36,7 +37,8 @@ extern "C" {
  * Loss and log-sum of B positions by sub-ids: r_qi = sum_k S[q][k][codes[i][k]].
  *   codes    in   uint8 [N][m]     codebook G (Eq. 1), sub-ids < b (16-byte aligned);  uint16 [N][m] for the _u16 call
  *   S        in   float [B][m][b]  from pq_subitem_scores().  Entries may be -inf (a sub-id out of play: its items have
- *                                  probability 0); a position for which nothing is left has lse = -inf, loss 0, no gradient
+ *                                  probability 0); a position for which nothing is left has lse = -inf, loss 0, no gradient;
+ *                                  one that meets a NaN or +inf has lse, loss and gradient NaN, and no other position has
  *   targets  in   int32 [B]
  *   loss     out  float [B];  lse  out  float [B]
  * b <= 256 for one-byte sub-ids, <= 65536 for two bytes.  A sub-id >= b makes the result unspecified; nothing outside the

@@ -8,7 +8,6 @@ namespace {
 constexpr long long kDzElements = 1LL << 27;           // of the buffer: 256 MB of 16-bit dz, the size of the last-level cache
 constexpr long long kMaxPiece = 1LL << 22;
 
-
 // What a tile of 256 rows and `cols` columns takes a compute unit next to one of 256 x 256 that keeps the matrix cores as busy
 // as can be (the smaller ones' rates: 203 of 208 TFLOP/s and about 165 in float32; 880 of 1040 and about 600 in 16 bits).
 // Two workgroups of a smaller tile share a compute unit, but one alone has nearly all of it: what counts is how many a
@@ -70,7 +69,8 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
         p.piece = 0;
     }
     p.info_at = 256;
-    p.dz_at = round_up(p.info_at + (size_t)p.padded * sizeof(RowInfo), 256);
+    p.live_at = round_up(p.info_at + (size_t)p.padded * sizeof(RowInfo), 256);
+    p.dz_at = round_up(p.live_at + (size_t)B * d * size, 256);
     p.partial_at = round_up(p.dz_at + (size_t)p.padded * p.piece * size, 256);
     p.bytes = round_up(p.partial_at + (size_t)p.slices * B * d * sizeof(float), 256);
     return p;
@@ -139,6 +139,7 @@ int pq_default_cross_entropy_backward(const void* W, const void* queries, const 
     a.lse_in = lse; a.grad = grad_loss; a.dH = dqueries; a.dW = dW;
     a.factor = reinterpret_cast<float*>(ws);
     a.info = reinterpret_cast<RowInfo*>(ws + p.info_at);
+    a.live = ws + p.live_at;
     a.dz = ws + p.dz_at;
     a.partial_h = reinterpret_cast<float*>(ws + p.partial_at);
     a.piece = p.piece; a.padded = p.padded; a.slices = p.slices;

@@ -67,6 +67,7 @@ struct DenseArgs {
     // gradient
     const float *lse_in, *grad;
     RowInfo* info;                                     // [positions, padded]
+    void* live;                                        // [B][d]: the queries, zeros where a position adds nothing
     float* factor;                                     // what the products are multiplied with
     void* dz;                                          // [tiles of a piece][positions, padded][kItems]
     float* partial_h;                                  // [slices][B][d]
@@ -181,12 +182,21 @@ __global__ __launch_bounds__(kWave) void default_cross_entropy_join_kernel(Dense
     }
 }
 
-// What the gradient's kernels need of a position, and the factor of their products.
+// What the gradient's kernels need of a position, the factor of their products, and the queries they multiply: those of a
+// position without a target (padding: it may hold anything, NaN too) are zeros, as 0 NaN would be NaN in every dW.
+// A copy of the queries is B d elements beside the N d that the products read.
 template <typename T>
 __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
     __shared__ float tops[16];
     const int tid = threadIdx.x;
     auto weight = [&](int q) { const int t = a.targets[q]; return t >= 0 && t < a.N ? a.grad[q] : 0.0f; };
+    const int row_pieces = a.d * (int)sizeof(T) / 16;
+    const size_t pieces = (size_t)a.B * row_pieces;
+    for (size_t i = (size_t)blockIdx.x * 1024 + tid; i < pieces; i += (size_t)gridDim.x * 1024) {
+        const uint4 v = static_cast<const uint4*>(a.H)[i];
+        static_cast<uint4*>(a.live)[i] = weight((int)(i / row_pieces)) != 0.0f ? v : uint4{0, 0, 0, 0};
+    }
+    if (blockIdx.x != 0) return;
     float top = 0.0f;
     for (int q = tid; q < a.B; q += 1024) top = fmaxf(top, fabsf(weight(q)));
 #pragma unroll
@@ -616,7 +626,7 @@ struct DensePlan {
     int piece, pieces, padded, dz_positions, dw_cols;  // gradient: positions of a tile of dz, columns of one of dW
     int rows, cols, rows_tiles, cols_tiles, slices;    // a tile of dH, and how many share its items
     bool few;                                          // by default_few_kernel
-    size_t info_at, dz_at, partial_at, bytes;          // its workspace
+    size_t info_at, live_at, dz_at, partial_at, bytes;          // its workspace
 };
 
 inline int grid_of(long long outer, long long inner) { return (int)(ceil_div(outer, 8) * 8 * inner); }     // see chiplet_order()
@@ -649,7 +659,9 @@ hipError_t launch_dh(const DenseArgs& a, hipStream_t st) {
 }
 template <typename T, int ROWS>
 hipError_t launch_dh_cols(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
-    return p.cols == 256 ? launch_dh<T, ROWS, 256>(a, st) : p.cols == 128 ? launch_dh<T, ROWS, 128>(a, st) : launch_dh<T, ROWS, 64>(a, st);
+    // (64 positions of narrow 16-bit embeddings are default_few_kernel's)
+    if constexpr (ROWS == 64 && sizeof(T) == 2) return launch_dh<T, ROWS, 256>(a, st);
+    else return p.cols == 256 ? launch_dh<T, ROWS, 256>(a, st) : p.cols == 128 ? launch_dh<T, ROWS, 128>(a, st) : launch_dh<T, ROWS, 64>(a, st);
 }
 
 template <typename T>
@@ -684,8 +696,10 @@ hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
-    hipLaunchKernelGGL((default_rows_kernel<T>), dim3(1), dim3(1024), 0, st, a);
+    const long long row_blocks = ceil_div((long long)a.B * a.d * (long long)sizeof(T), 16 * 1024);
+    hipLaunchKernelGGL((default_rows_kernel<T>), dim3((unsigned)(row_blocks < kCUs ? row_blocks : kCUs)), dim3(1024), 0, st, a);
     hipError_t e = hipGetLastError();
+    a.H = a.live;
     if constexpr (sizeof(T) == 2) {
         if (p.few && e == hipSuccess) e = launch_few<T>(p, a, st);
     }

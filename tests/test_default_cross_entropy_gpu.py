@@ -100,6 +100,23 @@ def test_positions_without_a_target(pq, type):
 
 
 @pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,d,B", [(3000, 64, 64), (700, 520, 64), (3000, 64, 70), (1500, 128, 300)])
+def test_what_positions_without_a_target_hold_reaches_nothing(pq, N, d, B, type):
+    W, H, targets, grad = draw(N, d, B, type, seed=N + B)
+    targets[::3], targets[B - 1] = -1, N
+    clean, odd = H.clone(), H.clone()
+    clean[targets < 0], odd[targets < 0] = 0.0, float("nan")
+    clean[B - 1], odd[B - 1] = 0.0, float("inf")
+    loss, lse = pq.pq_default_cross_entropy(W, clean, targets)
+    loss2, lse2 = pq.pq_default_cross_entropy(W, odd, targets)
+    has = (targets >= 0) & (targets < N)
+    assert torch.equal(loss, loss2) and torch.equal(lse[has], lse2[has])
+    dH, dW = pq.pq_default_cross_entropy_backward(W, clean, targets, lse, grad)
+    dH2, dW2 = pq.pq_default_cross_entropy_backward(W, odd, targets, lse2, grad)
+    assert torch.equal(dH, dH2) and torch.equal(dW, dW2) and not dH2[~has].any() and torch.isfinite(dW2).all()
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("spread", [0.0, 30.0, 300.0])
 def test_scores_far_apart(pq, type, spread):
     check(pq, *draw(2000, 64, 20, type, seed=4, spread=spread), type)
