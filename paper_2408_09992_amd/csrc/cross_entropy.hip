@@ -293,7 +293,8 @@ __device__ __forceinline__ float gradient_of(const BackArgs& a, uint64_t sum, in
     if (!has_target(a, q)) return 0.0f;
     const size_t at = (size_t)a.targets[q] * a.m + k;
     const int g = code_bytes == 1 ? (int)static_cast<const uint8_t*>(a.codes)[at] : (int)static_cast<const uint16_t*>(a.codes)[at];
-    const double p = (double)sum * 0x1p-62 - (g == j ? 1.0 : 0.0);
+    // (a position whose scores hold a NaN has lse = NaN, of which its probabilities' whole numbers know nothing)
+    const double p = a.lse[q] == a.lse[q] ? (double)sum * 0x1p-62 - (g == j ? 1.0 : 0.0) : (double)a.lse[q];
     return (float)((double)a.grad[q] * p);
 }
 
@@ -332,7 +333,8 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackAr
 
     const uint32_t lo = blockIdx.x * a.share, hi = (uint32_t)min((long long)lo + a.share, a.N);
     const uint32_t last = (uint32_t)(a.N - 1), stride = kThreads * kUnitsBack, last_code = (uint32_t)E - 1u;
-    constexpr bool kTurned = sizeof(CT) == 1 && M >= 4 && M <= 32;
+    constexpr bool kTurned = sizeof(CT) == 1 && M >= 4 && M <= 32;          // (LDS holds all entries of these: no ranges)
+    static_assert(!(kTurned && kRanges), "an entry outside the range is told by its split");
     const uint32_t turn = threadIdx.x % P, split_turn = kTurned ? threadIdx.x / P % (M > 0 ? M : 1) : 0u;
     // LDS address of the lane's first place of split k's sums, sub-id 0
     const uint32_t sums_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)sums + turn * 8u;
@@ -374,9 +376,7 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackAr
             const uint32_t code = mine.code(k, last_code);
             uint32_t place = first + code * (P * 8u);
             if constexpr (kRanges) {
-                const uint32_t entry = (uint32_t)k * (uint32_t)E + code - e0;
-                if (!kTurned && entry >= e1 - e0) return;
-                if (kTurned && place - sums_at >= (e1 - e0) * 8u) return;
+                if ((uint32_t)k * (uint32_t)E + code - e0 >= e1 - e0) return;
             }
 #pragma unroll
             for (int r = 0; r < Q; ++r) {
@@ -546,17 +546,23 @@ hipError_t go_backward(const Plan& p, const BackArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((cross_entropy_backward_kernel<M, CT, Q, C>), dim3(p.shares, p.groups, p.ranges), dim3(kThreads), p.lds, st, a);
     return hipGetLastError();
 }
+// Whether a plan of the gradient can be Q queries with C copies: one-byte sub-ids of M splits take the most copies that fit.
+template <int M, typename CT>
+constexpr bool reached(int Q, int C) {
+    return M == 0 || sizeof(CT) == 2 || (fits<M, CT>(Q, Q * C) && (Q * C == 8 || !fits<M, CT>(Q, 2 * Q * C))) || (M == 64 && Q * C == 1);
+}
 template <int M, typename CT>
 hipError_t go_backward_q(const Plan& p, const BackArgs& a, hipStream_t st) {
-    if constexpr (fits<M, CT>(4, 8)) { if (p.Q == 4 && p.C == 2) return go_backward<M, CT, 4, 2>(p, a, st); }
-    if constexpr (fits<M, CT>(2, 8)) { if (p.Q == 2 && p.C == 4) return go_backward<M, CT, 2, 4>(p, a, st); }
-    if constexpr (fits<M, CT>(1, 8)) { if (p.C == 8) return go_backward<M, CT, 1, 8>(p, a, st); }
-    if constexpr (fits<M, CT>(4, 4)) { if (p.Q == 4) return go_backward<M, CT, 4, 1>(p, a, st); }
-    if constexpr (fits<M, CT>(2, 4)) { if (p.Q == 2 && p.C == 2) return go_backward<M, CT, 2, 2>(p, a, st); }
-    if constexpr (fits<M, CT>(2, 2)) { if (p.Q == 2) return go_backward<M, CT, 2, 1>(p, a, st); }
-    if constexpr (fits<M, CT>(1, 4)) { if (p.C == 4) return go_backward<M, CT, 1, 4>(p, a, st); }
-    if constexpr (fits<M, CT>(1, 2)) { if (p.C == 2) return go_backward<M, CT, 1, 2>(p, a, st); }
-    return go_backward<M, CT, 1, 1>(p, a, st);
+    if constexpr (reached<M, CT>(4, 2)) { if (p.Q == 4 && p.C == 2) return go_backward<M, CT, 4, 2>(p, a, st); }
+    if constexpr (reached<M, CT>(4, 1)) { if (p.Q == 4) return go_backward<M, CT, 4, 1>(p, a, st); }
+    if constexpr (reached<M, CT>(2, 4)) { if (p.Q == 2 && p.C == 4) return go_backward<M, CT, 2, 4>(p, a, st); }
+    if constexpr (reached<M, CT>(2, 2)) { if (p.Q == 2 && p.C == 2) return go_backward<M, CT, 2, 2>(p, a, st); }
+    if constexpr (reached<M, CT>(2, 1)) { if (p.Q == 2) return go_backward<M, CT, 2, 1>(p, a, st); }
+    if constexpr (reached<M, CT>(1, 8)) { if (p.C == 8) return go_backward<M, CT, 1, 8>(p, a, st); }
+    if constexpr (reached<M, CT>(1, 4)) { if (p.C == 4) return go_backward<M, CT, 1, 4>(p, a, st); }
+    if constexpr (reached<M, CT>(1, 2)) { if (p.C == 2) return go_backward<M, CT, 1, 2>(p, a, st); }
+    if constexpr (reached<M, CT>(1, 1)) return go_backward<M, CT, 1, 1>(p, a, st);
+    else return hipErrorInvalidValue;                          // (no plan asks for it)
 }
 
 template <typename CT>

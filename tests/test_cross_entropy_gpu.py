@@ -144,6 +144,25 @@ def test_sub_ids_out_of_play(pq, wide):
     assert np.isinf(loss[2]) and np.isfinite(dS[2]).all() and np.isfinite(dS[4]).all()
 
 
+@pytest.mark.parametrize("m,b,wide", [(8, 256, False), (3, 100, False), (4, 1000, True)])
+def test_scores_that_are_no_numbers(pq, m, b, wide):
+    # positions 1 and 4 meet a NaN, 3 an infinity; 4 has no target
+    codes, S, targets, grad = draw(3000, m, b, 7, seed=m + b, wide=wide)
+    targets[4] = -1
+    codes_t, S_t, targets_t, grad_t = on_gpu(codes, S, targets, grad)
+    loss, lse = (pq.pq_cross_entropy_u16 if wide else pq.pq_cross_entropy)(codes_t, S_t, targets_t)
+    dS = (pq.pq_cross_entropy_u16_backward if wide else pq.pq_cross_entropy_backward)(codes_t, S_t, targets_t, lse, grad_t)
+    odd = S_t.clone()
+    odd[1, 0, int(codes[5, 0])] = odd[4, m - 1, int(codes[7, m - 1])] = float("nan")
+    odd[3, 1, int(codes[9, 1])] = float("inf")
+    loss2, lse2 = (pq.pq_cross_entropy_u16 if wide else pq.pq_cross_entropy)(codes_t, odd, targets_t)
+    dS2 = (pq.pq_cross_entropy_u16_backward if wide else pq.pq_cross_entropy_backward)(codes_t, odd, targets_t, lse2, grad_t)
+    rest = [0, 2, 5, 6]
+    assert torch.isnan(lse2[[1, 3, 4]]).all() and torch.isnan(loss2[[1, 3]]).all() and torch.isnan(dS2[[1, 3]]).all()
+    assert loss2[4] == 0 and not dS2[4].any()
+    assert torch.equal(loss2[rest], loss[rest]) and torch.equal(lse2[rest], lse[rest]) and torch.equal(dS2[rest], dS[rest])
+
+
 def test_gradient_against_differences(pq):
     # along a direction that moves no score by more than 1: the third derivative of log-sum-exp is below 1, so central
     # differences are off by h^2 / 6 and by the losses' own errors over h
