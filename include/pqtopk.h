@@ -215,7 +215,7 @@ int pq_default_scores(const float* W, const float* queries, long long N, int B, 
  *   packed  out  uint8 [N][d / 2]         (16-byte aligned) element 2j in the low half of byte j, 2j + 1 in the high half
  *   scales  out  bfloat16 [N][d / group]  the group's largest absolute value / 7, rounded to bfloat16 (nearest even); weights
  *                                         are then rounded to the nearest multiple of the rounded scale (ties to even) and
- *                                         held within -8 .. 7 times it
+ *                                         held within -8 .. 7 times it.  A group with an infinity or a NaN has the scale NaN
  * group is 32, 64 or 128 and divides d.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, d < 1, another group, d % group, N >= 2^31), PQ_ERR_UNSUPPORTED (d > 16384),
  *         PQ_ERR_ALIGN, PQ_ERR_HIP.
@@ -226,8 +226,8 @@ int pq_quantise_items(const float* W, long long N, int d, int group, uint8_t* pa
  * Eq. 3's scores from such embeddings: scores[q][i] = sum_e scales[i][e / group] * (n[i][e] - 8) * phi_q[e], for
  * pq_topk_scores() to rank.  One pass over the embeddings serves up to 32 queries.
  *   queries in float [B][d];  scores out float [B][ld], ld >= N
- * A query's elements are taken as whole multiples of 2^-30 of a power of two above its largest one; sums within a group are
- * exact integers, the sum over groups is float32.  A query that holds an infinity or a NaN has NaN scores.
+ * A query's elements are taken as whole multiples of 2^-30 of a power of two above its largest one.  Sums within a group are
+ * exact, rounded to float32 as they leave the group; the sum over groups is float32.  A query that holds an infinity or a NaN has NaN scores.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (as above; B < 1, ld < N), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B; d > 9600: a query's
  *         digits would not fit LDS), PQ_ERR_ALIGN, PQ_ERR_HIP.
  */

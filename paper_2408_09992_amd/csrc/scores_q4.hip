@@ -31,8 +31,9 @@ __device__ __forceinline__ uint32_t four_digits(float x, int shift) {
     return ((uint32_t)v + 0x00808080u) ^ 0x00808080u;
 }
 
-// Scores on the integer matrix cores: both operands are exact, so are the sums of a group (below 2^24), and what is rounded
-// is the query (to 2^-31 of its largest element, less than its float32 rounding there) and the float32 sum over groups.
+// Scores on the integer matrix cores: both operands are whole numbers and a digit's sums are exact (below 2^21).  Rounded are
+// the query (to 2^-31 of a power of two above its largest element: less than float32 there), a group's sum, joined from its
+// four digits in float32, and the float32 sum over groups.
 // The instruction's 16 rows are four queries' four digits, its 16 columns items: a lane finishes one score, all its digits
 // at hand, with its item's scale.
 // Bound by the stream of nibbles, which comes in 16 bytes a lane, 64 neighbouring bytes of sixteen rows an instruction (with
@@ -231,14 +232,15 @@ __global__ __launch_bounds__(256) void quantise_items_kernel(const float* W, lon
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (long long)gridDim.x * 256) {
         const float4 x = reinterpret_cast<const float4*>(W)[2 * i], y = reinterpret_cast<const float4*>(W)[2 * i + 1];
         const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-        float top = 0.0f;
+        uint32_t top = 0;                                      // (magnitudes in the order of their bits: NaN above all)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+        for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
         // (a group's lanes are neighbours of one wave and run this together: the pieces are a multiple of a group's)
-        for (int s = 1; s < lanes_per_group; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
-        // the scale is rounded to bfloat16 (nearest even) first, the weights then to multiples of what is kept
-        const uint32_t bits = __float_as_uint(top / 7.0f);
-        const uint32_t kept = (bits + 0x7FFFu + (bits >> 16 & 1u)) >> 16;
+        for (int s = 1; s < lanes_per_group; s *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, s));
+        // the scale is rounded to bfloat16 (nearest even) first, the weights then to multiples of what is kept; infinities and
+        // NaN leave a scale of NaN
+        const uint32_t bits = __float_as_uint(__uint_as_float(top) / 7.0f);
+        const uint32_t kept = top >= 0x7F800000u ? 0x7FC0u : (bits + 0x7FFFu + (bits >> 16 & 1u)) >> 16;
         const float scale = __uint_as_float(kept << 16);
         uint32_t word = 0;
 #pragma unroll

@@ -113,6 +113,22 @@ def test_quantised_items(pq, N, d, group):
     assert np.all(err <= (0.5 + 7 * 2.0 ** -8) * want.double().numpy()[:, :, None] + 1e-44)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_groups_that_hold_no_numbers(pq, group):
+    W = torch.from_numpy(np.random.default_rng(9).standard_normal((50, 256)).astype(np.float32)).cuda()
+    packed, scales = pq.pq_quantise_items(W, group)
+    odd = W.clone()
+    odd[3, 200], odd[20, 0], odd[49, 255] = float("nan"), float("inf"), -float("inf")
+    packed2, scales2 = pq.pq_quantise_items(odd, group)
+    hit = torch.zeros(50, 256 // group, dtype=torch.bool, device="cuda")
+    hit[3, 200 // group] = hit[20, 0] = hit[49, 255 // group] = True
+    assert torch.equal(torch.isnan(scales2), hit) and torch.equal(scales2[~hit], scales[~hit])
+    rest = ~hit.repeat_interleave(group // 2, 1)
+    assert torch.equal(packed2[rest], packed[rest])
+    scores = pq.pq_default_scores_q4(packed2, scales2, W[:2].contiguous())[:, :50]
+    assert torch.isnan(scores[:, [3, 20, 49]]).all() and int(torch.isnan(scores).sum()) == 6
+
+
 def test_ranking_follows_the_scores(pq):
     # quantise, score, rank: the ids are those of the same scores sorted by hand
     W = torch.randn(5000, 128, device="cuda") * 128 ** -0.5
