@@ -42,9 +42,11 @@ __device__ __forceinline__ uint32_t four_digits(float x, int shift) {
 // time, as four queries ask for 2 PARTS instructions of 16 cycles per 1 KB of weights.
 // Scores are held back in LDS and leave a wave's tiles at a time: stores between the loads cost the stream more than their
 // bytes (1.3 GB read by 128 bytes stored per 8 KB: 207 us without stores, 262 with, 227 held back).
+// Registers leave room for two workgroups where one set of queries and its groups let them, but for groups of 32 with scales
+// of odd rows: held to 128 registers those spill (1.28M items of 96 elements, one query: 49.4 us, with one workgroup 45.4).
 // GROUP: weights that share a scale; SETS: sets of four queries a pass over the weights serves; WHOLE: d is a multiple of 128.
 template <int SETS, int GROUP, bool WHOLE>
-__global__ __launch_bounds__(kThreads, SETS * (kStep / GROUP) <= 4 ? 4 : 2) void default_scores_q4_kernel(Q4Args a) {
+__global__ __launch_bounds__(kThreads, SETS * (kStep / GROUP) <= 4 && (GROUP > 32 || WHOLE) ? 4 : 2) void default_scores_q4_kernel(Q4Args a) {
     constexpr int PARTS = kStep / GROUP;                       // groups a step
     constexpr int kAhead = 4;                                  // steps whose weights are on their way
     constexpr bool kHold = SETS <= 2;
