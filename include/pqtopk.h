@@ -228,7 +228,7 @@ int pq_quantise_items(const float* W, long long N, int d, int group, uint8_t* pa
  *   queries in float [B][d];  scores out float [B][ld], ld >= N
  * A query's elements are taken as whole multiples of 2^-30 of a power of two above its largest one.  Sums within a group are
  * exact, rounded to float32 as they leave the group; the sum over groups is float32.  A query that holds an infinity or a NaN has NaN scores.
- * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (as above; B < 1, ld < N), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B; d > 9600: a query's
+ * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (as above; B < 1, ld < N), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B; d > 9856: a query's
  *         digits would not fit LDS), PQ_ERR_ALIGN, PQ_ERR_HIP.
  */
 int pq_default_scores_q4(const uint8_t* packed, const uint16_t* scales, const float* queries, long long N, int B, int d,

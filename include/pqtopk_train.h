@@ -44,8 +44,8 @@ extern "C" {
  * b <= 256 for one-byte sub-ids, <= 65536 for two bytes.  A sub-id >= b makes the result unspecified; nothing outside the
  * arguments is touched.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, B, m, b < 1; b too large; N >= 2^31), PQ_ERR_UNSUPPORTED (m > PQ_MAX_M,
- *         B > PQ_MAX_B, or one query's table too large for LDS: m * max(b, 256) <= 36864 for one-byte sub-ids, m * b <=
- *         36864 for two), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
+ *         B > PQ_MAX_B, or for two-byte sub-ids one query's table too large for LDS: m * b > 36864), PQ_ERR_WORKSPACE,
+ *         PQ_ERR_ALIGN, PQ_ERR_HIP.
  */
 size_t pq_cross_entropy_workspace_bytes(long long N, int B, int m, int b);
 int pq_cross_entropy(const uint8_t* codes, const float* S, const int* targets, long long N, int B, int m, int b,
@@ -76,7 +76,8 @@ int pq_cross_entropy_u16_backward(const uint16_t* codes, const float* S, const i
  *     dqueries[q][k s + e] = sum_j dS[q][k][j] * psi[k][j][e]      dcentroids[k][j][e] = sum_q dS[q][k][j] * phi[q][k s + e]
  * with s = d / m.  Either output may be NULL (not both): it is not computed.
  *   dS float [B][m][b];  queries float [B][d];  centroids float [m][b][s];  dqueries float [B][d];  dcentroids float [m][b][s]
- * Sums in float32 by fused multiply-adds, in an order that depends on the shape alone.
+ * Sums in float32, in an order that depends on the shape alone; products exact or (a thousand queries and more) to 2^-25 of
+ * themselves, as in pq_default_cross_entropy().
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (B, d, m, b < 1; d % m; b > 65536), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B, m > PQ_MAX_M),
  *         PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
  */

@@ -39,10 +39,10 @@ __device__ __forceinline__ void join_waves(const f32x16& acc, float (*part)[kTil
     }
 }
 
-// Few queries, or rows that are not whole 16-byte pieces.  A workgroup makes one 32 x 32 tile; its eight waves share the summed index and are joined through LDS.  Operands go from
-// memory to the matrix cores' registers directly: a tile's rows are read once, in whole lines (rows of dS, of psi, of phi).
-// Bound by the latency of these loads: 4.8 us for one query, 6.5 for 256 and 15.4 for 1024 (d = 512, m = 8, b = 256), which is
-// why a thousand queries and more take the tiles below.
+// Few queries, or rows that are not whole 16-byte pieces.  A workgroup makes one 32 x 32 tile; its eight waves share the summed
+// index and are joined through LDS.  Operands go from memory to the matrix cores' registers directly: a tile's rows are read
+// once, in whole lines (rows of dS, of psi, of phi).  Bound by the latency of these loads: 4.8 us for one query, 6.5 for 256 and
+// 27 for 2048 (d = 512, m = 8, b = 256), where the tiles below take 17.6.
 __global__ __launch_bounds__(kThreads) void subitem_scores_backward_kernel(GradArgs a) {
     __shared__ float part[kWaves][kTile * kTile];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col = lane % 32, half = lane / 32;
@@ -134,6 +134,8 @@ __global__ __launch_bounds__(kThreads) void subitem_scores_backward_kernel(GradA
 }
 
 // Many queries: tiles of 64 x 64 through LDS (matrix_tile.hpp), those of dcentroids summed over a share of the queries each.
+// Products of float32 in three bfloat16 pieces a factor.  8192 queries (d = 512, m = 8, b = 256; 84 MB of tables and queries):
+// 46 us, 1.8 TB/s; fewer are bound by the latency of a share's few stages and of the second launch.
 using TileQ = MatrixTile<float, 64, 64, 32, 32, true, false>;
 using TileC = MatrixTile<float, 64, 64, 32, 32, false, false>;
 constexpr int kSide = 64;

@@ -42,7 +42,7 @@ def check(pq, packed, scales, queries):
 
 @pytest.mark.parametrize("N,d,group,B", [(1, 32, 32, 1), (1, 64, 64, 1), (3, 128, 128, 2), (16, 96, 32, 5), (17, 64, 32, 4), (33, 160, 32, 3), (1000, 512, 64, 1),
                                          (1003, 512, 128, 16), (4099, 512, 32, 33), (777, 256, 64, 9), (5000, 384, 128, 7), (257, 640, 64, 65), (20_011, 64, 64, 8),
-                                         (100, 4096, 128, 40), (50, 9600, 64, 2), (40, 4800, 32, 3), (15, 1088, 64, 12)])
+                                         (100, 4096, 128, 40), (50, 9600, 64, 2), (33, 9856, 128, 5), (40, 4800, 32, 3), (15, 1088, 64, 12)])
 def test_scores(pq, N, d, group, B):
     check(pq, *draw(N, d, group, B, seed=N + d + group + B))
 
