@@ -703,6 +703,41 @@ def matrix_cores_mode(args):
                       "eq4": eq4, "default_scorer": default}))
 
 
+def training_mode(args):
+    """The scoring head's training calls and the four-bit scores on the cases of perf/operators.py: GPU time of a pass (HIP
+    events around back-to-back passes, median of three), its bytes and operations per second."""
+    import importlib.util
+    import torch
+
+    spec = importlib.util.spec_from_file_location("operators", os.path.join(ROOT, "perf", "operators.py"))
+    ops = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ops)
+    ops.own = True
+    points = []
+    for case in ops.listed():
+        state = ops.prepare(case, 1)
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+
+        def timed(n):
+            e0.record()
+            for _ in range(n):
+                ops.run(state)
+            e1.record()
+            torch.cuda.synchronize()
+            return e0.elapsed_time(e1) / n * 1e3
+        timed(3)
+        n = max(3, min(500, int(50_000 / timed(3))))
+        us, work = sorted(timed(n) for _ in range(3))[1], ops.work(case)
+        points.append({"case": case["name"], "us_per_pass": us, "GBps": work["bytes"] / us / 1e3, "TFLOPs": work["flops"] / us / 1e6})
+        print(f"{case['name']:32s} {us:9.1f} us {points[-1]['GBps']:8.0f} GB/s {points[-1]['TFLOPs']:8.1f} TFLOP/s", file=sys.stderr, flush=True)
+        del state
+        torch.cuda.empty_cache()
+    dense = max((p for p in points if p["case"].startswith("dense")), key=lambda p: p["TFLOPs"])
+    print(json.dumps({"metric": "dense cross entropy with its gradients, operations/s", "value": dense["TFLOPs"], "unit": "TFLOP/s", "n_gpus": 1,
+                      "higher_is_better": True, "vs_baseline": None, "dtype": "bf16", "data": "synthetic", "config": {"workload": dense["case"]},
+                      "training": points}))
+
+
 def breakdown_mode(args):
     """Where the time of a step goes: the three launches of a single-query step (Eq. 4, scan, fold) are run with the
     kernels' stamping instances (wall-clock stamps at fixed points, lane 0 of every wave), back to back as in the timed
@@ -878,6 +913,8 @@ def main():
                     "at --batch")
     ap.add_argument("--matrix-cores", action="store_true", help="Eq. 4 and the default scorer (Eq. 3) on the matrix cores "
                     "against the scalar kernels, over batch sizes")
+    ap.add_argument("--training", action="store_true", help="cross entropy of the catalogue with its gradients, by sub-ids and by the default "
+                    "scorer, Eq. 4's gradients and scores from four bits, on the cases of perf/operators.py")
     ap.add_argument("--yardsticks", action="store_true", help="machine yardsticks: empty launch, plain streaming read, "
                     "random gathers from LDS")
     ap.add_argument("--rules", action="store_true", help="both sides of the rules that choose a scan, around each of their lines")
@@ -903,6 +940,9 @@ def main():
         return
     if args.breakdown:
         breakdown_mode(args)
+        return
+    if args.training:
+        training_mode(args)
         return
     if args.yardsticks:
         yardsticks_mode(args)
