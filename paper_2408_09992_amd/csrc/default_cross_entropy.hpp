@@ -182,6 +182,16 @@ __global__ __launch_bounds__(kWave) void default_cross_entropy_join_kernel(Dense
     }
 }
 
+__device__ __forceinline__ float wave_top(float v) {
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) v = fmaxf(v, __shfl_xor(v, x));
+    return v;
+}
+// Of a position with gradient g (0: it adds nothing), the largest of all being top.
+__device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
+    return g != 0.0f ? RowInfo{lse * kLog2e - kDzBits, g / top} : RowInfo{__builtin_inff(), 0.0f};
+}
+
 // What the gradient's kernels need of a position, the factor of their products, and the queries they multiply: those of a
 // position without a target (padding: it may hold anything, NaN too) are zeros, as 0 NaN would be NaN in every dW.
 // A copy of the queries is B d elements beside the N d that the products read.
@@ -199,17 +209,14 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
     if (blockIdx.x != 0) return;
     float top = 0.0f;
     for (int q = tid; q < a.B; q += 1024) top = fmaxf(top, fabsf(weight(q)));
-#pragma unroll
-    for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    top = wave_top(top);
     if (tid % kWave == 0) tops[tid / kWave] = top;
     __syncthreads();
     top = tops[0];
 #pragma unroll
     for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
     for (int q = tid; q < a.padded; q += 1024) {
-        const float g = q < a.B ? weight(q) : 0.0f;
-        const bool live = g != 0.0f;
-        a.info[q] = RowInfo{live ? a.lse_in[q] * kLog2e - kDzBits : __builtin_inff(), live ? g / top : 0.0f};
+        a.info[q] = row_info(q < a.B ? weight(q) : 0.0f, top, a.lse_in[min(q, a.B - 1)]);
     }
     if (tid == 0) *a.factor = top / kDzScale;
 }
@@ -499,11 +506,19 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
     bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h);
     bring_rows<T, D, kLoadsW>(a.W, a.d, (long long)blockIdx.x * IT, a.N, w0);
-    if (tid < kFew) {
-        info[tid] = a.info[tid];
-        target[tid] = tid < a.B ? a.targets[tid] : -1;
+    // what default_rows_kernel does for more positions: these are a wave's lanes
+    __shared__ float factor_of_all;
+    if (wave == 0) {
+        const int t = lane < a.B ? a.targets[lane] : -1;
+        const float g = t >= 0 && t < a.N ? a.grad[lane] : 0.0f;
+        const float top = wave_top(fabsf(g));
+        info[lane] = row_info(g, top, lane < a.B ? a.lse_in[lane] : 0.0f);
+        target[lane] = t;
+        if (lane == 0) {
+            factor_of_all = top / kDzScale;
+            if (blockIdx.x == 0) *a.factor = factor_of_all;
+        }
     }
-    const float factor = *a.factor;
     // dH: 2 x D / 32 blocks of 32 positions x 32 elements, shared by the waves; D = 64 leaves half of them without one
     constexpr int kBlocksH = D / 16 >= kWaves ? D / 16 / kWaves : 1;
     f32x16 dh[kBlocksH];
@@ -513,6 +528,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
 
     int turn = 0;
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    for (int i = tid; i < kFew * D / 8; i += kFewThreads)      // (a position that adds nothing may hold anything, NaN too)
+        if (info[i / (D / 8)].at == __builtin_inff()) reinterpret_cast<uint4*>(h)[i] = uint4{0, 0, 0, 0};
+    const float factor = factor_of_all;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
         unsigned char* w = turn % 2 ? w1 : w0;
         // every wave's part of the tile has come (below), and every wave is done with the other buffer
@@ -696,12 +714,15 @@ hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
 
 template <typename T>
 hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
-    const long long row_blocks = ceil_div((long long)a.B * a.d * (long long)sizeof(T), 16 * 1024);
-    hipLaunchKernelGGL((default_rows_kernel<T>), dim3((unsigned)(row_blocks < kCUs ? row_blocks : kCUs)), dim3(1024), 0, st, a);
-    hipError_t e = hipGetLastError();
-    a.H = a.live;
+    hipError_t e = hipSuccess;
     if constexpr (sizeof(T) == 2) {
-        if (p.few && e == hipSuccess) e = launch_few<T>(p, a, st);
+        if (p.few) e = launch_few<T>(p, a, st);
+    }
+    if (!p.few) {
+        const long long row_blocks = ceil_div((long long)a.B * a.d * (long long)sizeof(T), 16 * 1024);
+        hipLaunchKernelGGL((default_rows_kernel<T>), dim3((unsigned)(row_blocks < kCUs ? row_blocks : kCUs)), dim3(1024), 0, st, a);
+        e = hipGetLastError();
+        a.H = a.live;
     }
     for (int i = 0; !p.few && i < p.pieces && e == hipSuccess; ++i) {
         a.first_item = (long long)i * p.piece;
