@@ -20,7 +20,12 @@ constexpr double kTileStart = 0.1;                     // what a workgroup takes
 
 DensePlan plan_dense(long long N, int B, int d, int size) {
     DensePlan p;
-    p.item_tiles = ceil_div(N, kItems);
+    // Tiles of 64 x 64 where all of them run at once (loss and gradient, us: 10,000 items of 64 float32, 50 positions 42 with tiles
+    // of 256 x 64, 34 so; 5000 of 512, one position 81 and 54; 8000 of 512, 128 positions 98 and 73; 32,768 of 64, 64 positions
+    // 48 and 44).
+    auto small_tiles = [](long long items, long long width) { return ceil_div(items, 64) * ceil_div(width, 64) <= 2 * kCUs; };
+    p.loss_items = small_tiles(N, B) ? 64 : kItems;
+    p.item_tiles = ceil_div(N, p.loss_items);
     // loss: the tiles of positions, and how many tiles of items a workgroup takes, whose rounds over the chip take least
     double best = 1e300;
     for (int tile : {256, 128, 64})
@@ -32,6 +37,9 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
                 p.positions = tile; p.position_tiles = (int)position_tiles; p.tiles_each = each; p.groups = (int)groups;
             }
         }
+    if (p.loss_items == 64) {
+        p.positions = 64; p.position_tiles = (int)ceil_div(B, 64); p.tiles_each = 1; p.groups = (int)p.item_tiles;
+    }
     // gradient: pieces of the items, in balance
     const int small = B <= 64 ? 64 : 128;              // (positions are padded to a multiple of this or of 256)
     long long piece = kDzElements / (long long)round_up(B, small);
@@ -46,12 +54,15 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
         const double cost = (double)ceil_div(tiles * ceil_div(B, tile), kCUs) * (tile_cost(tile, size) + kTileStart);
         if (cost < best * 0.99) { best = cost; p.dz_positions = tile; }
     }
+    p.dz_items = small_tiles(p.piece, B) ? 64 : kItems;
+    if (p.dz_items == 64) p.dz_positions = 64;
     p.padded = (int)round_up(B, p.dz_positions);
     best = 1e300;
     for (int cols : {256, 128, 64}) {
         const double cost = (double)ceil_div(tiles * ceil_div(d, cols), kCUs) * (tile_cost(cols, size) * p.padded / 512.0 + kTileStart);
         if (cost < best * 0.99) { best = cost; p.dw_cols = cols; }
     }
+    p.dw_items = small_tiles(p.piece, d) ? 64 : kItems;
     // dH: as many slices of the items as fill the chip once
     p.rows = B > 128 ? 256 : B > 64 ? 128 : 64;
     p.cols = d > 128 ? 256 : d > 64 ? 128 : 64;

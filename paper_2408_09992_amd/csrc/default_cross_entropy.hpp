@@ -17,21 +17,25 @@ namespace head {
 
 constexpr float kHeadroom = 40.0f;                    // (log2) how far a score may rise over a lane's reference before that moves
 constexpr float kDzBits = 15.0f, kDzScale = 32768.0f;  // dz is stored times 2^15 over the largest |g|: types keep small probabilities
-constexpr int kItems = 256;                           // items of a tile of z and dW
+constexpr int kItems = 256;                           // items of a block of dz, and of most tiles of z and dW
 
 struct RowInfo { float at, scale; };                  // of a position: 2^(z log2e - at) is p 2^15; its g over the largest |g|
 
-// The tiles: z for kItems items and POS positions; dH for ROWS positions and COLS elements; dW for kItems items and COLS
+// The tiles: z for ITEMS items and POS positions; dH for ROWS positions and COLS elements; dW for ITEMS items and COLS
 // elements.  Tiles of 256 x 256 by eight waves feed the matrix cores best (208 TFLOP/s in float32, 1040 to 1130 in bfloat16,
-// against 203 and 880 to 1090 with 256 x 128 by four); the smaller ones are for few positions and narrow embeddings.
-template <typename T, int POS> struct ScoresTile;
-template <typename T> struct ScoresTile<T, 64> : MatrixTile<T, kItems, 64, 64, 64, true, true> {};
-template <typename T> struct ScoresTile<T, 128> : MatrixTile<T, kItems, 128, 128, 64, true, true> {};
-template <typename T> struct ScoresTile<T, 256> : MatrixTile<T, kItems, 256, 128, 64, true, true> {};
-template <typename T, int COLS> struct TileW;
-template <typename T> struct TileW<T, 64> : MatrixTile<T, kItems, 64, 64, 64, false, false> {};
-template <typename T> struct TileW<T, 128> : MatrixTile<T, kItems, 128, 128, 64, false, false> {};
-template <typename T> struct TileW<T, 256> : MatrixTile<T, kItems, 256, 128, 64, false, false> {};
+// against 203 and 880 to 1090 with 256 x 128 by four); the smaller ones are for few positions and narrow embeddings.  Those of
+// 64 x 64 are for products that do not fill the chip: it is the latency of a tile's stages that bounds them, and the share of the
+// memory's rate that few compute units have.
+template <typename T, int POS, int ITEMS> struct ScoresTile;
+template <typename T> struct ScoresTile<T, 64, 64> : MatrixTile<T, 64, 64, 32, 32, true, true> {};
+template <typename T> struct ScoresTile<T, 64, 256> : MatrixTile<T, 256, 64, 64, 64, true, true> {};
+template <typename T> struct ScoresTile<T, 128, 256> : MatrixTile<T, 256, 128, 128, 64, true, true> {};
+template <typename T> struct ScoresTile<T, 256, 256> : MatrixTile<T, 256, 256, 128, 64, true, true> {};
+template <typename T, int COLS, int ITEMS> struct TileW;
+template <typename T> struct TileW<T, 64, 64> : MatrixTile<T, 64, 64, 32, 32, false, false> {};
+template <typename T> struct TileW<T, 64, 256> : MatrixTile<T, 256, 64, 64, 64, false, false> {};
+template <typename T> struct TileW<T, 128, 256> : MatrixTile<T, 256, 128, 128, 64, false, false> {};
+template <typename T> struct TileW<T, 256, 256> : MatrixTile<T, 256, 256, 128, 64, false, false> {};
 template <typename T, int ROWS, int COLS> struct TileH;
 template <typename T> struct TileH<T, 64, 64> : MatrixTile<T, 64, 64, 32, 32, true, false> {};
 template <typename T> struct TileH<T, 64, 128> : MatrixTile<T, 64, 128, 32, 64, true, false> {};
@@ -89,10 +93,10 @@ __device__ __forceinline__ Operand positions_of(const DenseArgs& a, int position
 
 // Statistics of a tile of positions over a group of item tiles, one after the other.  As in the loss by sub-ids a lane's
 // reference c moves only when a score passes it by 2^kHeadroom; lanes, halves and waves join once, at the end.
-template <typename T, int BN>
-__global__ __launch_bounds__((ScoresTile<T, BN>::kThreads), 2) void default_cross_entropy_kernel(DenseArgs a) {
-    using Tile = ScoresTile<T, BN>;
-    constexpr int MI = Tile::MI, NI = Tile::NI, kRowWaves = kItems / (32 * MI);
+template <typename T, int BN, int ITEMS>
+__global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_cross_entropy_kernel(DenseArgs a) {
+    using Tile = ScoresTile<T, BN, ITEMS>;
+    constexpr int MI = Tile::MI, NI = Tile::NI, kRowWaves = ITEMS / (32 * MI);
     __shared__ float2 stat[kRowWaves][BN];
     int group, pt;
     chiplet_order(blockIdx.x, a.position_tiles, group, pt);
@@ -105,8 +109,8 @@ __global__ __launch_bounds__((ScoresTile<T, BN>::kThreads), 2) void default_cros
         const long long tile = (long long)group * a.tiles_each + i;
         if (tile >= a.item_tiles) break;
         f32x16 acc[MI][NI];
-        Tile::run(items_of<T>(a, tile * kItems), positions_of<T>(a, pt * BN), acc);
-        const int left = left_of(a.N - tile * kItems - Tile::wave_row(), 32 * MI);
+        Tile::run(items_of<T>(a, tile * ITEMS), positions_of<T>(a, pt * BN), acc);
+        const int left = left_of(a.N - tile * ITEMS - Tile::wave_row(), 32 * MI);
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) {
             __builtin_amdgcn_sched_barrier(0);                 // (one column after the other: the registers hold no two of them)
@@ -224,15 +228,15 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
 // dz of a piece of items: scores as in the loss, then (exp(z - lse) - [target]) g as the products' operands, position by
 // position.  For 16-bit operands dz is rounded to their type: it is the products' input as H and W are, and what they add up
 // (in float32) is rounded to that type once more at the end.
-template <typename T, int BN>
-__global__ __launch_bounds__((ScoresTile<T, BN>::kThreads), 2) void default_dz_kernel(DenseArgs a) {
-    using Tile = ScoresTile<T, BN>;
+template <typename T, int BN, int ITEMS>
+__global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_dz_kernel(DenseArgs a) {
+    using Tile = ScoresTile<T, BN, ITEMS>;
     constexpr int MI = Tile::MI, NI = Tile::NI;
     int tile, pt;
     chiplet_order(blockIdx.x, a.tiles_n, tile, pt);
     if (tile >= a.tiles_m) return;
     const int lane = threadIdx.x % kWave;
-    const long long item0 = a.first_item + (long long)tile * kItems;
+    const long long item0 = a.first_item + (long long)tile * ITEMS;
     f32x16 acc[MI][NI];
     Tile::run(items_of<T>(a, item0), positions_of<T>(a, pt * BN), acc);
     const int left = left_of(a.N - item0 - Tile::wave_row(), 32 * MI) - 4 * (lane / 32);
@@ -262,7 +266,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN>::kThreads), 2) void default_dz_k
         // 32 positions x 32 items at a time through the wave's LDS: positions leave in rows of 16-byte pieces.  The pieces of
         // a row are swapped by its number, so that writes and reads spread over the banks.
         constexpr int kPieces = 32 * (int)sizeof(T) / 16;
-        T* out = static_cast<T*>(a.dz) + ((size_t)tile * a.padded + q0) * kItems + Tile::wave_row();
+        T* out = static_cast<T*>(a.dz) + ((size_t)(tile / (kItems / ITEMS)) * a.padded + q0) * kItems + tile % (kItems / ITEMS) * ITEMS + Tile::wave_row();
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
             typedef T T4 __attribute__((ext_vector_type(4)));
@@ -287,19 +291,19 @@ __global__ __launch_bounds__((ScoresTile<T, BN>::kThreads), 2) void default_dz_k
 }
 
 // dW of a piece: [items][d], summed over the positions.
-template <typename T, int COLS>
-__global__ __launch_bounds__((TileW<T, COLS>::kThreads), 2) void default_dw_kernel(DenseArgs a) {
-    using Tile = TileW<T, COLS>;
+template <typename T, int COLS, int ITEMS>
+__global__ __launch_bounds__((TileW<T, COLS, ITEMS>::kThreads), 2) void default_dw_kernel(DenseArgs a) {
+    using Tile = TileW<T, COLS, ITEMS>;
     int tile, ct;
     chiplet_order(blockIdx.x, a.tiles_n, tile, ct);
     if (tile >= a.tiles_m) return;
     const int lane = threadIdx.x % kWave;
     f32x16 acc[Tile::MI][Tile::NI];
-    const Operand dz{static_cast<const T*>(a.dz) + (size_t)tile * a.padded * kItems, kItems * sizeof(T), 0, kItems, 0, a.padded};
+    const Operand dz{static_cast<const T*>(a.dz) + (size_t)(tile / (kItems / ITEMS)) * a.padded * kItems, kItems * sizeof(T), tile % (kItems / ITEMS) * ITEMS, kItems, 0, a.padded};
     const Operand h{a.H, (size_t)a.d * sizeof(T), (long long)ct * COLS, a.d, 0, a.B};
     Tile::run(dz, h, acc);
     const float factor = *a.factor;
-    const long long item0 = a.first_item + (long long)tile * kItems + Tile::wave_row();
+    const long long item0 = a.first_item + (long long)tile * ITEMS + Tile::wave_row();
     const int left = left_of(a.N - item0, 32 * Tile::MI), col0 = ct * COLS + Tile::wave_col();
     // 32 items x 32 elements at a time through the wave's LDS, as in default_dz_kernel
     constexpr int kPieces = 32 * (int)sizeof(T) / 16;
@@ -639,9 +643,9 @@ __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
 // host side, by type of the operands (a translation unit each)
 
 struct DensePlan {
-    int positions, position_tiles, tiles_each, groups; // loss: positions of a tile of z
+    int loss_items, positions, position_tiles, tiles_each, groups;   // loss: items and positions of a tile of z
     long long item_tiles;
-    int piece, pieces, padded, dz_positions, dw_cols;  // gradient: positions of a tile of dz, columns of one of dW
+    int piece, pieces, padded, dz_items, dz_positions, dw_items, dw_cols;  // gradient: items and positions of a tile of dz, columns of one of dW
     int rows, cols, rows_tiles, cols_tiles, slices;    // a tile of dH, and how many share its items
     bool few;                                          // by default_few_kernel
     size_t info_at, live_at, dz_at, partial_at, bytes;          // its workspace
@@ -655,19 +659,23 @@ template <typename T> hipError_t dense_loss(const DensePlan& p, const DenseArgs&
 template <typename T> hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st);
 
 #ifdef PQ_DENSE_INSTANCE
-template <typename T, int POS>
+template <typename T, int POS, int ITEMS>
 hipError_t launch_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((default_cross_entropy_kernel<T, POS>), dim3(grid_of(p.groups, p.position_tiles)), dim3(ScoresTile<T, POS>::kThreads), 0, st, a);
+    hipLaunchKernelGGL((default_cross_entropy_kernel<T, POS, ITEMS>), dim3(grid_of(p.groups, p.position_tiles)), dim3(ScoresTile<T, POS, ITEMS>::kThreads), 0, st, a);
     return hipGetLastError();
 }
-template <typename T, int POS>
-hipError_t launch_dz(const DenseArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((default_dz_kernel<T, POS>), dim3(grid_of(a.tiles_m, a.tiles_n)), dim3(ScoresTile<T, POS>::kThreads), 0, st, a);
+template <typename T, int POS, int ITEMS>
+hipError_t launch_dz(DenseArgs a, hipStream_t st) {
+    a.tiles_m = a.items / ITEMS;
+    a.tiles_n = a.padded / POS;
+    hipLaunchKernelGGL((default_dz_kernel<T, POS, ITEMS>), dim3(grid_of(a.tiles_m, a.tiles_n)), dim3(ScoresTile<T, POS, ITEMS>::kThreads), 0, st, a);
     return hipGetLastError();
 }
-template <typename T, int COLS>
-hipError_t launch_dw(const DenseArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((default_dw_kernel<T, COLS>), dim3(grid_of(a.tiles_m, a.tiles_n)), dim3(TileW<T, COLS>::kThreads), 0, st, a);
+template <typename T, int COLS, int ITEMS>
+hipError_t launch_dw(DenseArgs a, hipStream_t st) {
+    a.tiles_m = a.items / ITEMS;
+    a.tiles_n = (int)ceil_div(a.d, COLS);
+    hipLaunchKernelGGL((default_dw_kernel<T, COLS, ITEMS>), dim3(grid_of(a.tiles_m, a.tiles_n)), dim3(TileW<T, COLS, ITEMS>::kThreads), 0, st, a);
     return hipGetLastError();
 }
 template <typename T, int ROWS, int COLS>
@@ -706,7 +714,8 @@ hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
     hipError_t e;
     if constexpr (sizeof(T) == 2) e = p.few ? launch_few_loss<T>(p, a, st) : hipSuccess;
     if (sizeof(T) != 2 || !p.few)
-        e = p.positions == 256 ? launch_loss<T, 256>(p, a, st) : p.positions == 128 ? launch_loss<T, 128>(p, a, st) : launch_loss<T, 64>(p, a, st);
+        e = p.loss_items == 64 ? launch_loss<T, 64, 64>(p, a, st) : p.positions == 256 ? launch_loss<T, 256, 256>(p, a, st)
+            : p.positions == 128 ? launch_loss<T, 128, 256>(p, a, st) : launch_loss<T, 64, 256>(p, a, st);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((default_cross_entropy_join_kernel<T>), dim3(a.B), dim3(kWave), 0, st, a);
     return hipGetLastError();
@@ -729,12 +738,11 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
         const long long left = a.N - a.first_item;
         a.items = (int)round_up((size_t)(left < p.piece ? left : p.piece), kItems);
         a.more = i > 0;
-        a.tiles_m = a.items / kItems;
-        a.tiles_n = p.padded / p.dz_positions;
-        e = p.dz_positions == 256 ? launch_dz<T, 256>(a, st) : p.dz_positions == 128 ? launch_dz<T, 128>(a, st) : launch_dz<T, 64>(a, st);
+        e = p.dz_items == 64 ? launch_dz<T, 64, 64>(a, st) : p.dz_positions == 256 ? launch_dz<T, 256, 256>(a, st)
+            : p.dz_positions == 128 ? launch_dz<T, 128, 256>(a, st) : launch_dz<T, 64, 256>(a, st);
         if (e != hipSuccess) break;
-        a.tiles_n = (int)ceil_div(a.d, p.dw_cols);
-        e = p.dw_cols == 256 ? launch_dw<T, 256>(a, st) : p.dw_cols == 128 ? launch_dw<T, 128>(a, st) : launch_dw<T, 64>(a, st);
+        e = p.dw_items == 64 ? launch_dw<T, 64, 64>(a, st) : p.dw_cols == 256 ? launch_dw<T, 256, 256>(a, st)
+            : p.dw_cols == 128 ? launch_dw<T, 128, 256>(a, st) : launch_dw<T, 64, 256>(a, st);
         if (e != hipSuccess) break;
         a.tiles_m = p.rows_tiles;
         a.tiles_n = p.cols_tiles;
