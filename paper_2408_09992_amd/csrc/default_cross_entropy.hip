@@ -64,8 +64,12 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
     }
     p.dw_items = small_tiles(p.piece, d) ? 64 : kItems;
     // dH: as many slices of the items as fill the chip once
+    // dW and dH in one launch, by tiles of 64 x 64, up to 64 positions (16-bit types: of wide embeddings): a launch counts until
+    // there are some 4000 tiles of dW (float32, gradient, us: 5000 items of 512, one position 37 apart, 30 together; 50,000 of 256,
+    // 64 positions 72 and 59; 64,000 of 512, 64 positions 126 and 126; 500,000 of 64, 33 positions 153 and 172).
+    p.together = B <= 64 && ceil_div(p.piece, 64) * ceil_div(d, 64) <= 16 * kCUs;
     p.rows = B > 128 ? 256 : B > 64 ? 128 : 64;
-    p.cols = d > 128 ? 256 : d > 64 ? 128 : 64;
+    p.cols = p.together ? 64 : d > 128 ? 256 : d > 64 ? 128 : 64;
     p.rows_tiles = (int)ceil_div(B, p.rows);
     p.cols_tiles = (int)ceil_div(d, p.cols);
     const bool big = p.rows == 256 && p.cols == 256;

@@ -80,6 +80,7 @@ struct DenseArgs {
     int piece, items;                                  // padded and actual items of it
     int padded, slices, slice_items, more;             // positions padded; shares of a piece's items; partial_h holds earlier pieces
     int tiles_m, tiles_n;                              // of the launch
+    int h_rows, h_cols, w_blocks;                      // tiles of dH; workgroups that make dW, where one launch makes both
 };
 
 template <typename T>
@@ -290,12 +291,12 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     }
 }
 
-// dW of a piece: [items][d], summed over the positions.
+// A tile of dW of a piece: [items][d], summed over the positions.
 template <typename T, int COLS, int ITEMS>
-__global__ __launch_bounds__((TileW<T, COLS, ITEMS>::kThreads), 2) void default_dw_kernel(DenseArgs a) {
+__device__ __forceinline__ void dw_tile(const DenseArgs& a, int block) {
     using Tile = TileW<T, COLS, ITEMS>;
     int tile, ct;
-    chiplet_order(blockIdx.x, a.tiles_n, tile, ct);
+    chiplet_order(block, a.tiles_n, tile, ct);
     if (tile >= a.tiles_m) return;
     const int lane = threadIdx.x % kWave;
     f32x16 acc[Tile::MI][Tile::NI];
@@ -331,14 +332,17 @@ __global__ __launch_bounds__((TileW<T, COLS, ITEMS>::kThreads), 2) void default_
         }
 }
 
-// A slice's share of dH: [positions][d] summed over its items of the piece, added to what earlier pieces left there.
+template <typename T, int COLS, int ITEMS>
+__global__ __launch_bounds__((TileW<T, COLS, ITEMS>::kThreads), 2) void default_dw_kernel(DenseArgs a) { dw_tile<T, COLS, ITEMS>(a, blockIdx.x); }
+
+// A slice's share of a tile of dH: [positions][d] summed over its items of the piece, added to what earlier pieces left there.
 template <typename T, int BM, int BN>
-__global__ __launch_bounds__((TileH<T, BM, BN>::kThreads), 2) void default_dh_kernel(DenseArgs a) {
+__device__ __forceinline__ void dh_tile(const DenseArgs& a, int block) {
     using Tile = TileH<T, BM, BN>;
     int slice, tile;
-    chiplet_order(blockIdx.x, a.tiles_m * a.tiles_n, slice, tile);
+    chiplet_order(block, a.h_rows * a.h_cols, slice, tile);
     if (slice >= a.slices) return;
-    const int rt = tile / a.tiles_n, ct = tile % a.tiles_n;
+    const int rt = tile / a.h_cols, ct = tile % a.h_cols;
     const int lane = threadIdx.x % kWave;
     const long long k0 = min((long long)slice * a.slice_items, (long long)a.items), k1 = min(k0 + a.slice_items, (long long)a.items);
     if (a.more && k0 == k1) return;
@@ -378,6 +382,15 @@ __global__ __launch_bounds__((TileH<T, BM, BN>::kThreads), 2) void default_dh_ke
     };
     if (a.B - q0 >= 32 * Tile::MI) put(std::true_type{});
     else put(std::false_type{});
+}
+template <typename T, int BM, int BN>
+__global__ __launch_bounds__((TileH<T, BM, BN>::kThreads), 2) void default_dh_kernel(DenseArgs a) { dh_tile<T, BM, BN>(a, blockIdx.x); }
+
+// Both for few positions, by tiles of 64 x 64: neither fills the chip, and a launch takes as long as they do.
+template <typename T>
+__global__ __launch_bounds__((TileW<T, 64, 64>::kThreads), 2) void default_products_kernel(DenseArgs a) {
+    if ((int)blockIdx.x < a.w_blocks) dw_tile<T, 64, 64>(a, blockIdx.x);
+    else dh_tile<T, 64, 64>(a, blockIdx.x - a.w_blocks);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -647,7 +660,7 @@ struct DensePlan {
     long long item_tiles;
     int piece, pieces, padded, dz_items, dz_positions, dw_items, dw_cols;  // gradient: items and positions of a tile of dz, columns of one of dW
     int rows, cols, rows_tiles, cols_tiles, slices;    // a tile of dH, and how many share its items
-    bool few;                                          // by default_few_kernel
+    bool few, together;                                // by default_few_kernel; dW and dH in one launch
     size_t info_at, live_at, dz_at, partial_at, bytes;          // its workspace
 };
 
@@ -678,9 +691,17 @@ hipError_t launch_dw(DenseArgs a, hipStream_t st) {
     hipLaunchKernelGGL((default_dw_kernel<T, COLS, ITEMS>), dim3(grid_of(a.tiles_m, a.tiles_n)), dim3(TileW<T, COLS, ITEMS>::kThreads), 0, st, a);
     return hipGetLastError();
 }
+template <typename T>
+hipError_t launch_products(DenseArgs a, hipStream_t st) {
+    a.tiles_m = a.items / 64;
+    a.tiles_n = (int)ceil_div(a.d, 64);
+    a.w_blocks = grid_of(a.tiles_m, a.tiles_n);
+    hipLaunchKernelGGL((default_products_kernel<T>), dim3(a.w_blocks + grid_of(a.slices, (long long)a.h_rows * a.h_cols)), dim3(TileW<T, 64, 64>::kThreads), 0, st, a);
+    return hipGetLastError();
+}
 template <typename T, int ROWS, int COLS>
 hipError_t launch_dh(const DenseArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((default_dh_kernel<T, ROWS, COLS>), dim3(grid_of(a.slices, (long long)a.tiles_m * a.tiles_n)), dim3(TileH<T, ROWS, COLS>::kThreads), 0, st, a);
+    hipLaunchKernelGGL((default_dh_kernel<T, ROWS, COLS>), dim3(grid_of(a.slices, (long long)a.h_rows * a.h_cols)), dim3(TileH<T, ROWS, COLS>::kThreads), 0, st, a);
     return hipGetLastError();
 }
 template <typename T, int ROWS>
@@ -741,12 +762,16 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
         e = p.dz_items == 64 ? launch_dz<T, 64, 64>(a, st) : p.dz_positions == 256 ? launch_dz<T, 256, 256>(a, st)
             : p.dz_positions == 128 ? launch_dz<T, 128, 256>(a, st) : launch_dz<T, 64, 256>(a, st);
         if (e != hipSuccess) break;
+        a.h_rows = p.rows_tiles;
+        a.h_cols = p.cols_tiles;
+        a.slice_items = (int)round_up((size_t)ceil_div(a.items, p.slices), kSliceItems);
+        if (p.together) {
+            e = launch_products<T>(a, st);
+            continue;
+        }
         e = p.dw_items == 64 ? launch_dw<T, 64, 64>(a, st) : p.dw_cols == 256 ? launch_dw<T, 256, 256>(a, st)
             : p.dw_cols == 128 ? launch_dw<T, 128, 256>(a, st) : launch_dw<T, 64, 256>(a, st);
         if (e != hipSuccess) break;
-        a.tiles_m = p.rows_tiles;
-        a.tiles_n = p.cols_tiles;
-        a.slice_items = (int)round_up((size_t)ceil_div(a.items, p.slices), kSliceItems);
         e = p.rows == 256 ? launch_dh_cols<T, 256>(p, a, st) : p.rows == 128 ? launch_dh_cols<T, 128>(p, a, st) : launch_dh_cols<T, 64>(p, a, st);
     }
     if (e != hipSuccess) return e;
