@@ -197,6 +197,22 @@ __device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
     return g != 0.0f ? RowInfo{lse * kLog2e - kDzBits, g / top} : RowInfo{__builtin_inff(), 0.0f};
 }
 
+// A position's share of the gradient: 0 where there is none, no target or no position.
+__device__ __forceinline__ float row_weight(const DenseArgs& a, int q) {
+    const int t = q < a.B ? a.targets[q] : -1;
+    return t >= 0 && t < a.N ? a.grad[q] : 0.0f;
+}
+// The queries in pieces of 16 bytes, from piece `first` on every `stride`-th, with zeros for positions that add nothing.
+template <typename T>
+__device__ __forceinline__ void copy_live(const DenseArgs& a, size_t first, size_t stride) {
+    const int row_pieces = a.d * (int)sizeof(T) / 16;
+    const size_t pieces = (size_t)a.B * row_pieces;
+    for (size_t i = first; i < pieces; i += stride) {
+        const uint4 v = static_cast<const uint4*>(a.H)[i];
+        static_cast<uint4*>(a.live)[i] = row_weight(a, (int)(i / row_pieces)) != 0.0f ? v : uint4{0, 0, 0, 0};
+    }
+}
+
 // What the gradient's kernels need of a position, the factor of their products, and the queries they multiply: those of a
 // position without a target (padding: it may hold anything, NaN too) are zeros, as 0 NaN would be NaN in every dW.
 // A copy of the queries is B d elements beside the N d that the products read.
@@ -204,16 +220,10 @@ template <typename T>
 __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
     __shared__ float tops[16];
     const int tid = threadIdx.x;
-    auto weight = [&](int q) { const int t = a.targets[q]; return t >= 0 && t < a.N ? a.grad[q] : 0.0f; };
-    const int row_pieces = a.d * (int)sizeof(T) / 16;
-    const size_t pieces = (size_t)a.B * row_pieces;
-    for (size_t i = (size_t)blockIdx.x * 1024 + tid; i < pieces; i += (size_t)gridDim.x * 1024) {
-        const uint4 v = static_cast<const uint4*>(a.H)[i];
-        static_cast<uint4*>(a.live)[i] = weight((int)(i / row_pieces)) != 0.0f ? v : uint4{0, 0, 0, 0};
-    }
+    copy_live<T>(a, (size_t)blockIdx.x * 1024 + tid, (size_t)gridDim.x * 1024);
     if (blockIdx.x != 0) return;
     float top = 0.0f;
-    for (int q = tid; q < a.B; q += 1024) top = fmaxf(top, fabsf(weight(q)));
+    for (int q = tid; q < a.B; q += 1024) top = fmaxf(top, fabsf(row_weight(a, q)));
     top = wave_top(top);
     if (tid % kWave == 0) tops[tid / kWave] = top;
     __syncthreads();
@@ -221,7 +231,7 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
 #pragma unroll
     for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
     for (int q = tid; q < a.padded; q += 1024) {
-        a.info[q] = row_info(q < a.B ? weight(q) : 0.0f, top, a.lse_in[min(q, a.B - 1)]);
+        a.info[q] = row_info(row_weight(a, q), top, a.lse_in[min(q, a.B - 1)]);
     }
     if (tid == 0) *a.factor = top / kDzScale;
 }
@@ -229,14 +239,26 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
 // dz of a piece of items: scores as in the loss, then (exp(z - lse) - [target]) g as the products' operands, position by
 // position.  For 16-bit operands dz is rounded to their type: it is the products' input as H and W are, and what they add up
 // (in float32) is rounded to that type once more at the end.
-template <typename T, int BN, int ITEMS>
+// ROWS: up to 64 positions, whose rows (see default_rows_kernel) the workgroups make themselves.
+template <typename T, int BN, int ITEMS, bool ROWS>
 __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_dz_kernel(DenseArgs a) {
     using Tile = ScoresTile<T, BN, ITEMS>;
     constexpr int MI = Tile::MI, NI = Tile::NI;
+    static_assert(!ROWS || BN == kWave, "a position is a lane");
     int tile, pt;
     chiplet_order(blockIdx.x, a.tiles_n, tile, pt);
     if (tile >= a.tiles_m) return;
     const int lane = threadIdx.x % kWave;
+    RowInfo own_row{};
+    if constexpr (ROWS) {                                      // (every wave: lane q has position q's)
+        const float g = row_weight(a, lane);
+        const float top = wave_top(fabsf(g));
+        own_row = row_info(g, top, a.lse_in[min(lane, a.B - 1)]);
+        if (!a.more) {
+            copy_live<T>(a, (size_t)tile * Tile::kThreads + threadIdx.x, (size_t)a.tiles_m * Tile::kThreads);
+            if (tile == 0 && threadIdx.x == 0) *a.factor = top / kDzScale;
+        }
+    }
     const long long item0 = a.first_item + (long long)tile * ITEMS;
     f32x16 acc[MI][NI];
     Tile::run(items_of<T>(a, item0), positions_of<T>(a, pt * BN), acc);
@@ -245,14 +267,19 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) {
         const int q0 = pt * BN + Tile::wave_col() + 32 * ni, q = q0 + lane % 32;
-        const RowInfo info = a.info[q];
+        RowInfo info;
+        if constexpr (ROWS) info = RowInfo{__shfl(own_row.at, q0 + lane % 32), __shfl(own_row.scale, q0 + lane % 32)};
+        else info = a.info[q];
         const long long from_first = (q < a.B ? (long long)a.targets[q] : -1) - item0 - Tile::wave_row();
         const int hit = from_first >= 0 && from_first < 32 * MI ? (int)from_first - 4 * (lane / 32) : -64;
         const bool special = __any(hit > -64) || left < 32 * MI - 4;           // (rare: a target among these items, the catalogue's end)
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) acc[mi][ni][e] = exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -info.at));
+            for (int e = 0; e < 16; ++e) {
+                const float p = exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -info.at));
+                acc[mi][ni][e] = ROWS && info.at == __builtin_inff() ? 0.0f : p;       // (its query may be NaN: not a copy that is zeros)
+            }
         if (special) {
             stay_a_branch();
 #pragma unroll
@@ -526,11 +553,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     // what default_rows_kernel does for more positions: these are a wave's lanes
     __shared__ float factor_of_all;
     if (wave == 0) {
-        const int t = lane < a.B ? a.targets[lane] : -1;
-        const float g = t >= 0 && t < a.N ? a.grad[lane] : 0.0f;
+        const float g = row_weight(a, lane);
         const float top = wave_top(fabsf(g));
-        info[lane] = row_info(g, top, lane < a.B ? a.lse_in[lane] : 0.0f);
-        target[lane] = t;
+        info[lane] = row_info(g, top, a.lse_in[min(lane, a.B - 1)]);
+        target[lane] = lane < a.B ? a.targets[lane] : -1;
         if (lane == 0) {
             factor_of_all = top / kDzScale;
             if (blockIdx.x == 0) *a.factor = factor_of_all;
@@ -677,11 +703,11 @@ hipError_t launch_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((default_cross_entropy_kernel<T, POS, ITEMS>), dim3(grid_of(p.groups, p.position_tiles)), dim3(ScoresTile<T, POS, ITEMS>::kThreads), 0, st, a);
     return hipGetLastError();
 }
-template <typename T, int POS, int ITEMS>
+template <typename T, int POS, int ITEMS, bool ROWS = false>
 hipError_t launch_dz(DenseArgs a, hipStream_t st) {
     a.tiles_m = a.items / ITEMS;
     a.tiles_n = a.padded / POS;
-    hipLaunchKernelGGL((default_dz_kernel<T, POS, ITEMS>), dim3(grid_of(a.tiles_m, a.tiles_n)), dim3(ScoresTile<T, POS, ITEMS>::kThreads), 0, st, a);
+    hipLaunchKernelGGL((default_dz_kernel<T, POS, ITEMS, ROWS>), dim3(grid_of(a.tiles_m, a.tiles_n)), dim3(ScoresTile<T, POS, ITEMS>::kThreads), 0, st, a);
     return hipGetLastError();
 }
 template <typename T, int COLS, int ITEMS>
@@ -748,20 +774,25 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
     if constexpr (sizeof(T) == 2) {
         if (p.few) e = launch_few<T>(p, a, st);
     }
-    if (!p.few) {
+    const void* queries = a.H;
+    const bool own_rows = a.B <= 64;                           // (then dz's positions are those of one tile)
+    if (!p.few && !own_rows) {
         const long long row_blocks = ceil_div((long long)a.B * a.d * (long long)sizeof(T), 16 * 1024);
         hipLaunchKernelGGL((default_rows_kernel<T>), dim3((unsigned)(row_blocks < kCUs ? row_blocks : kCUs)), dim3(1024), 0, st, a);
         e = hipGetLastError();
-        a.H = a.live;
+        queries = a.live;
     }
     for (int i = 0; !p.few && i < p.pieces && e == hipSuccess; ++i) {
         a.first_item = (long long)i * p.piece;
         const long long left = a.N - a.first_item;
         a.items = (int)round_up((size_t)(left < p.piece ? left : p.piece), kItems);
         a.more = i > 0;
-        e = p.dz_items == 64 ? launch_dz<T, 64, 64>(a, st) : p.dz_positions == 256 ? launch_dz<T, 256, 256>(a, st)
+        a.H = queries;
+        if (own_rows) e = p.dz_items == 64 ? launch_dz<T, 64, 64, true>(a, st) : launch_dz<T, 64, 256, true>(a, st);
+        else e = p.dz_items == 64 ? launch_dz<T, 64, 64>(a, st) : p.dz_positions == 256 ? launch_dz<T, 256, 256>(a, st)
             : p.dz_positions == 128 ? launch_dz<T, 128, 256>(a, st) : launch_dz<T, 64, 256>(a, st);
         if (e != hipSuccess) break;
+        a.H = a.live;
         a.h_rows = p.rows_tiles;
         a.h_cols = p.cols_tiles;
         a.slice_items = (int)round_up((size_t)ceil_div(a.items, p.slices), kSliceItems);
