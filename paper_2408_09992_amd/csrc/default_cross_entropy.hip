@@ -64,11 +64,12 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
     }
     p.dw_items = small_tiles(p.piece, d) ? 64 : kItems;
     // dH: as many slices of the items as fill the chip once
-    // dW and dH in one launch, by tiles of 64 x 64, up to 64 positions (16-bit types: of wide embeddings): a launch counts until
-    // there are some 4000 tiles of dW (float32, gradient, us: 5000 items of 512, one position 37 apart, 30 together; 50,000 of 256,
-    // 64 positions 72 and 59; 64,000 of 512, 64 positions 126 and 126; 500,000 of 64, 33 positions 153 and 172).
-    p.together = B <= 64 && ceil_div(p.piece, 64) * ceil_div(d, 64) <= 16 * kCUs;
-    p.rows = B > 128 ? 256 : B > 64 ? 128 : 64;
+    // dW and dH in one launch, by tiles of 64 x 64, until there are enough of these that larger ones gain more than a launch takes
+    // (gradient, us, apart and together; float32: 5000 items of 512, one position 37 and 30; 10,000 of 256, 200 positions 68 and 51;
+    // 10,000 of 512, 300 positions 111 and 106; 60,000 of 128, 300 positions 144 and 144; 500,000 of 64, 33 positions 152 and 167;
+    // bfloat16: 10,000 of 256, 200 positions 40 and 28; 34,742 of 512, 128 positions 69 and 52; 5000 of 512, 1500 positions 98 and 102).
+    p.together = ceil_div(B, 64) * ceil_div(p.piece, 64) * ceil_div(d, 64) <= (size == 4 ? 24 : 48) * kCUs;
+    p.rows = p.together ? 64 : B > 128 ? 256 : B > 64 ? 128 : 64;
     p.cols = p.together ? 64 : d > 128 ? 256 : d > 64 ? 128 : 64;
     p.rows_tiles = (int)ceil_div(B, p.rows);
     p.cols_tiles = (int)ceil_div(d, p.cols);

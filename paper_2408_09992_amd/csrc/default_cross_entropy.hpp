@@ -413,7 +413,7 @@ __device__ __forceinline__ void dh_tile(const DenseArgs& a, int block) {
 template <typename T, int BM, int BN>
 __global__ __launch_bounds__((TileH<T, BM, BN>::kThreads), 2) void default_dh_kernel(DenseArgs a) { dh_tile<T, BM, BN>(a, blockIdx.x); }
 
-// Both for few positions, by tiles of 64 x 64: neither fills the chip, and a launch takes as long as they do.
+// Both, by tiles of 64 x 64, where neither fills the chip and a launch takes as long as they do.
 template <typename T>
 __global__ __launch_bounds__((TileW<T, 64, 64>::kThreads), 2) void default_products_kernel(DenseArgs a) {
     if ((int)blockIdx.x < a.w_blocks) dw_tile<T, 64, 64>(a, blockIdx.x);
