@@ -21,10 +21,11 @@ constexpr double kTileStart = 0.1;                     // what a workgroup takes
 DensePlan plan_dense(long long N, int B, int d, int size) {
     DensePlan p;
     // Tiles of 64 x 64 where all of them run at once (loss and gradient, us: 10,000 items of 64 float32, 50 positions 42 with tiles
-    // of 256 x 64, 34 so; 5000 of 512, one position 81 and 54; 8000 of 512, 128 positions 98 and 73; 32,768 of 64, 64 positions
-    // 48 and 44).
-    auto small_tiles = [](long long items, long long width) { return ceil_div(items, 64) * ceil_div(width, 64) <= 2 * kCUs; };
-    p.loss_items = small_tiles(N, B) ? 64 : kItems;
+    // of 256 x 64, 34 so; 5000 of 512, one position 81 and 54; 8000 of 512, 128 positions 98 and 73), and for dz somewhat longer
+    // (gradient: 5000 of 128, 1000 positions 57 and 49; 10,000 of 512, 500 positions 152 and 143; 8000 of 512, 900 positions 179 and
+    // 195, bfloat16 66 and 66).  The loss's larger tiles fold several tiles of items before they leave a sum.
+    auto small_tiles = [](long long items, long long width, int rounds) { return ceil_div(items, 64) * ceil_div(width, 64) <= rounds * kCUs; };
+    p.loss_items = small_tiles(N, B, 2) ? 64 : kItems;
     p.item_tiles = ceil_div(N, p.loss_items);
     // loss: the tiles of positions, and how many tiles of items a workgroup takes, whose rounds over the chip take least
     double best = 1e300;
@@ -54,7 +55,7 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
         const double cost = (double)ceil_div(tiles * ceil_div(B, tile), kCUs) * (tile_cost(tile, size) + kTileStart);
         if (cost < best * 0.99) { best = cost; p.dz_positions = tile; }
     }
-    p.dz_items = small_tiles(p.piece, B) ? 64 : kItems;
+    p.dz_items = small_tiles(p.piece, B, 5) ? 64 : kItems;
     if (p.dz_items == 64) p.dz_positions = 64;
     p.padded = (int)round_up(B, p.dz_positions);
     best = 1e300;
@@ -62,7 +63,7 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
         const double cost = (double)ceil_div(tiles * ceil_div(d, cols), kCUs) * (tile_cost(cols, size) * p.padded / 512.0 + kTileStart);
         if (cost < best * 0.99) { best = cost; p.dw_cols = cols; }
     }
-    p.dw_items = small_tiles(p.piece, d) ? 64 : kItems;
+    p.dw_items = small_tiles(p.piece, d, 2) ? 64 : kItems;
     // dH: as many slices of the items as fill the chip once
     // dW and dH in one launch, by tiles of 64 x 64, until there are enough of these that larger ones gain more than a launch takes
     // (gradient, us, apart and together; float32: 5000 items of 512, one position 37 and 30; 10,000 of 256, 200 positions 68 and 51;
