@@ -9,19 +9,22 @@ namespace head {
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
-constexpr int kStep = 128;                           // elements of an embedding per step: 64 bytes of a row, 16 for a lane
-constexpr int kTileItems = 16, kTiles = 2;           // items of a matrix instruction; instructions side by side
+constexpr int kStep = 128, kQuarters = 4;            // elements of a row per step: 64 bytes, a quarter (32 elements) for a lane
+constexpr int kMaxWidth = 9856;                      // of an embedding: four queries' digits in LDS
+constexpr int kTileRows = 32;                        // rows of a matrix instruction's other operand
 
 struct Q4Args {
     const uint8_t* packed;      // [N][d / 2]
     const uint16_t* scales;     // [N][d / group], bfloat16
     const float* queries;       // [B][d]
     float* scores;              // [B][ld]
-    long long N, ld, item_tiles;
-    int B, d, steps;            // steps = d / 128, rounded up
-    int held;                   // tile pairs whose scores a wave holds back
+    long long N, ld;
+    long long rows, tiles;      // rows of PACK items; tiles of 32 rows
+    int B, d, steps;            // steps of a row = elements / 128, rounded up
+    int held;                   // tiles whose scores a wave holds back
 };
 
 // A query element as a whole number of 31 bits, in four signed bytes: v = d0 + 2^8 d1 + 2^16 d2 + 2^24 d3.
@@ -31,202 +34,229 @@ __device__ __forceinline__ uint32_t four_digits(float x, int shift) {
     return ((uint32_t)v + 0x00808080u) ^ 0x00808080u;
 }
 
+// Queries that a pass over the weights serves: up to 8 by BLOCKS pairs, more by SETS eights.
+template <int BLOCKS, int SETS> constexpr int queries_of() { return SETS == 1 ? 2 * BLOCKS : 8 * SETS; }
+
 // Scores on the integer matrix cores: both operands are whole numbers and a digit's sums are exact (below 2^21).  Rounded are
 // the query (to 2^-31 of a power of two above its largest element: less than float32 there), a group's sum, joined from its
 // four digits in float32, and the float32 sum over groups.
-// The instruction's 16 rows are four queries' four digits, its 16 columns items: a lane finishes one score, all its digits
-// at hand, with its item's scale.
+// The instruction's 32 rows are eight queries' four digits, its 32 columns rows of weights, its 32 k a quarter of a step, which
+// is the smallest group: a lane gets all digits of its sums, and finishes a score with its column's scales.
 // Bound by the stream of nibbles, which comes in 16 bytes a lane, 64 neighbouring bytes of sixteen rows an instruction (with
-// 8 bytes a lane the same stream reached 4.4 TB/s instead of 5.9).  Those 64 bytes are 128 elements: two groups of 64, four of
-// 32.  Each group's sums are taken from all lanes' weights with the other groups' digits zeroed: the matrix cores have the
-// time, as four queries ask for 2 PARTS instructions of 16 cycles per 1 KB of weights.
+// 8 bytes a lane the same stream reached 4.4 TB/s instead of 5.9).  A lane so has a quarter of row lane % 16 or 16 + lane % 16;
+// eight swaps between lanes make of these, for each quarter, column lane % 32 with sixteen k by lane / 32.
 // Scores are held back in LDS and leave a wave's tiles at a time: stores between the loads cost the stream more than their
 // bytes (1.3 GB read by 128 bytes stored per 8 KB: 207 us without stores, 262 with, 227 held back).
-// Registers leave room for two workgroups where one set of queries and its groups let them, but for groups of 32 with scales
-// of odd rows: held to 128 registers those spill (1.28M items of 96 elements, one query: 49.4 us, with one workgroup 45.4).
-// GROUP: weights that share a scale; SETS: sets of four queries a pass over the weights serves; WHOLE: d is a multiple of 128.
-template <int SETS, int GROUP, bool WHOLE>
-__global__ __launch_bounds__(kThreads, SETS * (kStep / GROUP) <= 4 && (GROUP > 32 || WHOLE) ? 4 : 2) void default_scores_q4_kernel(Q4Args a) {
-    constexpr int PARTS = kStep / GROUP;                       // groups a step
+// GROUP: weights that share a scale.  PACK: items of a row of weights, 2 for d = 64, whose own rows are half a step: a group's
+// sum then belongs to one of the two.  WHOLE: rows are whole steps and their scales aligned.
+template <int BLOCKS, int SETS, int GROUP, int PACK, bool WHOLE>
+__global__ __launch_bounds__(kThreads, SETS <= 2 ? 4 : 2) void default_scores_q4_kernel(Q4Args a) {
+    constexpr int PARTS = kStep / GROUP, kOf = kQuarters / PARTS;              // groups a step, quarters a group
+    constexpr int kQueries = queries_of<BLOCKS, SETS>(), kRows = SETS == 1 ? 8 * BLOCKS : 32;      // digit rows kept of a set
     constexpr int kAhead = 4;                                  // steps whose weights are on their way
-    constexpr bool kHold = SETS <= 2;
+    constexpr bool kHold = kQueries <= 8;
+    constexpr int kItems = kTileRows * PACK;                   // of a tile
+    static_assert(PACK == 1 || PARTS % PACK == 0, "a group belongs to one item");
     extern __shared__ __align__(16) unsigned char smem[];
-    i32x4* digits = reinterpret_cast<i32x4*>(smem);            // [step][half][set][lane]: as the matrix instruction takes them
-    float* factor = reinterpret_cast<float*>(digits + (size_t)a.steps * 2 * SETS * kWave);       // [query]
-    int* shift = reinterpret_cast<int*>(factor + SETS * 4);
-    float* held = reinterpret_cast<float*>(shift + SETS * 4);                                    // [wave][tile pair][query][32 items]
-    const int groups = a.d / GROUP;
+    i32x4* digits = reinterpret_cast<i32x4*>(smem);            // [step][quarter][set][half][row]: as the matrix instruction takes them
+    float* factor = reinterpret_cast<float*>(digits + (size_t)a.steps * kQuarters * SETS * 2 * kRows);         // [query]
+    int* shift = reinterpret_cast<int*>(factor + kQueries);
+    float* held = reinterpret_cast<float*>(shift + kQueries);                                    // [wave][tile][query][items]
+    const int groups = a.d * PACK / GROUP;                     // of a row
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int q0 = blockIdx.y * SETS * 4;
+    const int q0 = blockIdx.y * kQueries;
 
     const int col = lane % 16, h = lane / 16;
-    const size_t row_bytes = (size_t)a.d / 2;
-    const long long last_item = a.N - 1, waves = (long long)gridDim.x * kWaves;
-    // A wave's work is one sequence of steps, those of a tile pair and then of the next one.  The weights of kAhead steps are
+    const size_t row_bytes = (size_t)a.d * PACK / 2, bytes = (size_t)a.N * a.d / 2;
+    const long long last_row = a.rows - 1, waves = (long long)gridDim.x * kWaves;
+    // A wave's work is one sequence of steps, those of a tile and then of the next one.  The weights of kAhead steps are
     // always on their way: waves that all waited for a round of loads would leave the memory idle while they compute.
     typedef uint16_t Scales __attribute__((ext_vector_type(PARTS)));
-    const long long tiles_end = (a.item_tiles + kTiles - 1) / kTiles, first_tile = (long long)blockIdx.x * kWaves + wave;
-    uint4 ring_w[kAhead][kTiles];
-    Scales ring_s[kAhead][kTiles];
+    const long long first_tile = (long long)blockIdx.x * kWaves + wave;
+    uint4 ring_w[kAhead][2];
+    Scales ring_s[kAhead];
     long long load_tile = first_tile;
     int load_step = 0;
     auto load = [&](int slot) {
 #pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            const long long item = min((load_tile * kTiles + u) * kTileItems + col, last_item);
-            // past the row's end the digits are zero: any weights will do
-            ring_w[slot][u] = *reinterpret_cast<const uint4*>(a.packed + (size_t)item * row_bytes + min(load_step * (kStep / 2) + 16 * h, (int)row_bytes - 16));
-            // every fourth step brings the scales of four, a step for each of the item's lanes
-            if (load_step % 4 == 0) {
-                const uint16_t* scale = a.scales + (size_t)item * groups;
-                const int step = min(load_step + h, a.steps - 1);
-                if constexpr (WHOLE) ring_s[slot][u] = *reinterpret_cast<const Scales*>(scale + step * PARTS);
-                else {
+        for (int u = 0; u < 2; ++u) {
+            // past the row's end the digits are zero, and past the last item nothing is kept: any weights will do
+            size_t at = (size_t)min(load_tile * kTileRows + 16 * u + col, last_row) * row_bytes + min(load_step * (kStep / 2) + 16 * h, (int)row_bytes - 16);
+            if (PACK > 1) at = min(at, bytes - 16);
+            ring_w[slot][u] = *reinterpret_cast<const uint4*>(a.packed + at);
+        }
+        // every second step brings the scales of two, a step for each of the column's lanes
+        if (load_step % 2 == 0) {
+            const size_t first = (size_t)min(load_tile * kTileRows + lane % 32, last_row) * groups;
+            const int step = min(load_step + lane / 32, a.steps - 1);
+            if constexpr (WHOLE) ring_s[slot] = *reinterpret_cast<const Scales*>(a.scales + first + step * PARTS);
+            else {
 #pragma unroll
-                    for (int p = 0; p < PARTS; ++p) ring_s[slot][u][p] = scale[min(step * PARTS + p, groups - 1)];
+                for (int p = 0; p < PARTS; ++p) {
+                    const size_t at = first + min(step * PARTS + p, groups - 1);
+                    ring_s[slot][p] = a.scales[PACK > 1 ? min(at, (size_t)a.N * (groups / PACK) - 1) : at];
                 }
             }
         }
         if (++load_step == a.steps) { load_step = 0; load_tile += waves; }
     };
-    if (first_tile < tiles_end) {
+    if (first_tile < a.tiles) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) load(i);              // (while the queries are laid out)
     }
 
-    // factors: one wave per query in turn
-    for (int s = wave; s < SETS * 4; s += kWaves) {
-        float top = 0.0f;
-        bool odd = false;
-        if (q0 + s < a.B)
-            for (int e = lane; e < a.d; e += kWave) {
-                const float x = a.queries[(size_t)(q0 + s) * a.d + e];
-                top = fmaxf(top, fabsf(x));
-                odd |= !(fabsf(x) < __builtin_inff());
-            }
+    // factors: a wave per query, or per query in turn
+    for (int s = wave; s < kQueries; s += kWaves) {
+        uint32_t top = 0;                                      // (magnitudes in the order of their bits)
+        if (q0 + s < a.B) {
+            const float* phi = a.queries + (size_t)(q0 + s) * a.d;
+#pragma unroll 4
+            for (int e = lane; e < a.d; e += kWave) top = max(top, __float_as_uint(phi[e]) & 0x7FFFFFFFu);
+        }
 #pragma unroll
-        for (int x = 1; x < kWave; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-        const bool any_odd = __any(odd);
+        for (int x = 1; x < kWave; x *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, x));
+        const bool odd = top >= 0x7F800000u;                   // an infinity or a NaN
         if (lane == 0) {
             int e = 0;
-            if (top > 0.0f && !any_odd) (void)frexpf(top, &e);           // top < 2^e
+            if (top > 0 && !odd) (void)frexpf(__uint_as_float(top), &e);           // top < 2^e
             // digits are of x 2^(30 - e); a nibble stands for 16 (n - 8) below.  A query of tiny numbers goes as far as float32 does.
-            shift[s] = any_odd ? 0 : e > -92 ? 30 - e : 122;
-            factor[s] = any_odd ? __builtin_nanf("") : ldexpf(1.0f, e > -92 ? e - 34 : -126);
+            shift[s] = odd ? 0 : e > -92 ? 30 - e : 122;
+            factor[s] = odd ? __builtin_nanf("") : ldexpf(1.0f, e > -92 ? e - 34 : -126);
         }
     }
     __syncthreads();
-    // row r of the instruction is digit r % 4 of query r / 4; a lane's 16 bytes are elements 32 (lane / 16) + 16 half .. + 15 of
-    // the step, the even and odd ones of each eight apart, as the nibbles of a word come out
-    for (int i = threadIdx.x; i < a.steps * 2 * SETS * kWave; i += kThreads) {
-        const int l = i % kWave, set = i / kWave % SETS, half = i / kWave / SETS % 2, step = i / kWave / SETS / 2;
-        const int row = l % 16, q = set * 4 + row / 4, first = step * kStep + 32 * (l / 16) + 16 * half;
-        uint32_t w[4] = {0, 0, 0, 0};
-        if (q0 + q < a.B && first < a.d && factor[q] == factor[q]) {     // (d is a multiple of 32: sixteen elements are there or not)
-            const float* phi = a.queries + (size_t)(q0 + q) * a.d + first;
+    // row r of the instruction is digit r % 4 of query r / 4; a lane's sixteen k are neighbouring elements of the quarter, the even
+    // and odd ones of each eight apart, as the nibbles of a word come out.  A thread makes a query's four digits of sixteen elements.
+    for (int i = threadIdx.x; i < a.steps * kQuarters * 2 * kQueries; i += kThreads) {
+        const int q = i % kQueries, half = i / kQueries % 2, quarter = i / kQueries / 2 % kQuarters, step = i / kQueries / 2 / kQuarters;
+        const int set = SETS == 1 ? 0 : q / 8, row = (SETS == 1 ? q : q % 8) * 4, first = step * kStep + 32 * quarter + 16 * half;
+        uint32_t w[4][4] = {};
+        if (q0 + q < a.B && first < a.d * PACK && factor[q] == factor[q]) {     // (d is a multiple of 32: sixteen elements are there or not)
+            const float* phi = a.queries + (size_t)(q0 + q) * a.d + (PACK > 1 ? first % a.d : first);
+            uint32_t v[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const uint32_t byte = (four_digits(phi[e], shift[q]) >> (8 * (row % 4))) & 255u;
-                w[e / 8 * 2 + e % 2] |= byte << (8 * (e % 8 / 2));
-            }
+            for (int e = 0; e < 16; ++e) v[e] = four_digits(phi[e], shift[q]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+#pragma unroll
+                for (int digit = 0; digit < 4; ++digit) w[digit][e / 8 * 2 + e % 2] |= ((v[e] >> (8 * digit)) & 255u) << (8 * (e % 8 / 2));
         }
-        digits[i] = i32x4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+#pragma unroll
+        for (int digit = 0; digit < 4; ++digit)
+            digits[(((size_t)step * kQuarters + quarter) * SETS + set) * 2 * kRows + half * kRows + row + digit] = i32x4{(int)w[digit][0], (int)w[digit][1], (int)w[digit][2], (int)w[digit][3]};
     }
     __syncthreads();
 
-    int mine[PARTS];                                           // all ones where the lane's elements belong to the step's group p
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) mine[p] = h * PARTS / 4 == p ? -1 : 0;
-    float sum[kTiles][SETS];
+    float sum[PACK][SETS][BLOCKS];
     auto clear = [&] {
 #pragma unroll
-        for (int u = 0; u < kTiles; ++u)
+        for (int o = 0; o < PACK; ++o)
 #pragma unroll
-            for (int s = 0; s < SETS; ++s) sum[u][s] = 0.0f;
+            for (int s = 0; s < SETS; ++s)
+#pragma unroll
+                for (int k = 0; k < BLOCKS; ++k) sum[o][s][k] = 0.0f;
     };
     clear();
     long long tile = first_tile;
-    int step = 0, pairs = 0;
-    Scales four_steps[kTiles] = {};
-    const int queries = min(SETS * 4, a.B - q0);
-    held += (size_t)wave * a.held * queries * 32;
+    int step = 0, tiles = 0;
+    Scales two_steps = {};
+    const int queries = min(kQueries, a.B - q0);
+    held += (size_t)wave * a.held * queries * kItems;
     auto release = [&](long long last_tile) {                  // the held scores, the last of them of last_tile
         wave_reads_after_writes();
-        for (int r = lane / 32; r < pairs * queries; r += 2) {
-            const int pair = r / queries, q = r - pair * queries;
-            const long long item = (last_tile - (long long)(pairs - 1 - pair) * waves) * kTiles * kTileItems + lane % 32;
-            if (item < a.N) a.scores[(size_t)(q0 + q) * a.ld + item] = held[r * 32 + lane % 32];
+        for (int r = lane / kItems; r < tiles * queries; r += kWave / kItems) {
+            const int t = r / queries, q = r - t * queries;
+            const long long item = (last_tile - (long long)(tiles - 1 - t) * waves) * kItems + lane % kItems;
+            if (item < a.N) a.scores[(size_t)(q0 + q) * a.ld + item] = held[r * kItems + lane % kItems];
         }
         wave_reads_after_writes();
-        pairs = 0;
+        tiles = 0;
     };
-    // (whole rounds of the ring: steps past the wave's last tile are of items past the last one and leave nothing)
-    const int rounds = first_tile < tiles_end ? (int)(((tiles_end - 1 - first_tile) / waves + 1) * a.steps + kAhead - 1) / kAhead : 0;
+    // (whole rounds of the ring: steps past the wave's last tile are of rows past the last one and leave nothing)
+    const int rounds = first_tile < a.tiles ? (int)(((a.tiles - 1 - first_tile) / waves + 1) * a.steps + kAhead - 1) / kAhead : 0;
     for (int round = 0; round < rounds; ++round) {
 #pragma unroll
         for (int slot = 0; slot < kAhead; ++slot) {
             __builtin_amdgcn_sched_barrier(0);                 // (steps one after the other: their accumulators share registers)
-            i32x4 n[2][kTiles];
-            float scale[kTiles][PARTS];
+            uint32_t m[kQuarters][2];                          // column lane % 32, sixteen elements of each quarter
+            {
+                // rows of sixteen lanes: x[j] has quarters 0 .. 3 of rows 0 .. 15 (A), y[j] those of rows 16 .. 31 (B)
+                uint32_t x[4] = {ring_w[slot][0].x, ring_w[slot][0].y, ring_w[slot][0].z, ring_w[slot][0].w};
+                uint32_t y[4] = {ring_w[slot][1].x, ring_w[slot][1].y, ring_w[slot][1].z, ring_w[slot][1].w};
 #pragma unroll
-            for (int u = 0; u < kTiles; ++u) {
-                // a nibble's two's complement of n - 8 in the high half of a byte: 16 (n - 8)
-                const uint4 w = ring_w[slot][u];
-                const uint32_t v[4] = {w.x ^ 0x88888888u, w.y ^ 0x88888888u, w.z ^ 0x88888888u, w.w ^ 0x88888888u};
+                for (int j = 0; j < 4; ++j) {                  // x: A0 B0 A2 B2, y: A1 B1 A3 B3
+                    const auto r = __builtin_amdgcn_permlane16_swap(x[j], y[j], false, false);
+                    x[j] = r[0];
+                    y[j] = r[1];
+                }
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
-                    n[half][u] = i32x4{(int)(v[2 * half] << 4 & 0xF0F0F0F0u), (int)(v[2 * half] & 0xF0F0F0F0u),
-                                       (int)(v[2 * half + 1] << 4 & 0xF0F0F0F0u), (int)(v[2 * half + 1] & 0xF0F0F0F0u)};
-                if (step % 4 == 0) four_steps[u] = ring_s[slot][u];
-                uint32_t words[(PARTS + 1) / 2] = {};
-                __builtin_memcpy(words, &four_steps[u], sizeof(Scales));
-#pragma unroll
-                for (int p = 0; p < PARTS; p += 2) {
-                    const uint32_t word = (uint32_t)__shfl((int)words[p / 2], col + 16 * (step % 4));
-                    scale[u][p] = __uint_as_float(word << 16);
-                    if (p + 1 < PARTS) scale[u][p + 1] = __uint_as_float(word & 0xFFFF0000u);
+                for (int j = 0; j < 2; ++j) {                  // first and second eight bytes of a quarter: A0 B0 | A0 B0, A2 B2 | A2 B2
+                    const auto r = __builtin_amdgcn_permlane32_swap(x[j], x[j + 2], false, false), t = __builtin_amdgcn_permlane32_swap(y[j], y[j + 2], false, false);
+                    m[0][j] = r[0]; m[2][j] = r[1];
+                    m[1][j] = t[0]; m[3][j] = t[1];
                 }
             }
+            if (step % 2 == 0) two_steps = ring_s[slot];
+            float scale[PARTS];
+            uint32_t words[(PARTS + 1) / 2] = {};
+            __builtin_memcpy(words, &two_steps, sizeof(Scales));
+#pragma unroll
+            for (int p = 0; p < PARTS; p += 2) {
+                const uint32_t word = (uint32_t)__shfl((int)words[p / 2], lane % 32 + 32 * (step % 2));
+                scale[p] = __uint_as_float(word << 16);
+                if (p + 1 < PARTS) scale[p + 1] = __uint_as_float(word & 0xFFFF0000u);
+            }
             load(slot);
+            // a nibble's two's complement of n - 8 in the high half of a byte: 16 (n - 8)
+            i32x4 n[kQuarters];
+#pragma unroll
+            for (int g = 0; g < kQuarters; ++g) {
+                const uint32_t v[2] = {m[g][0] ^ 0x88888888u, m[g][1] ^ 0x88888888u};
+                n[g] = i32x4{(int)(v[0] << 4 & 0xF0F0F0F0u), (int)(v[0] & 0xF0F0F0F0u), (int)(v[1] << 4 & 0xF0F0F0F0u), (int)(v[1] & 0xF0F0F0F0u)};
+            }
 #pragma unroll
             for (int s = 0; s < SETS; ++s) {
-                const i32x4 x = digits[((size_t)step * 2 * SETS + s) * kWave + lane], y = digits[((size_t)(step * 2 + 1) * SETS + s) * kWave + lane];
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p) {
-                    const i32x4 xp = PARTS == 1 ? x : x & mine[p], yp = PARTS == 1 ? y : y & mine[p];
-                    i32x4 acc[kTiles];
+                    i32x16 acc = {};
 #pragma unroll
-                    for (int u = 0; u < kTiles; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xp, n[0][u], i32x4{0, 0, 0, 0}, 0, 0, 0);
+                    for (int g = p * kOf; g < (p + 1) * kOf; ++g) {
+                        // (rows that are not kept repeat others: their sums are not used)
+                        const i32x4 x = digits[(((size_t)step * kQuarters + g) * SETS + s) * 2 * kRows + lane / 32 * kRows + lane % kRows];
+                        acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, n[g], acc, 0, 0, 0);
+                    }
 #pragma unroll
-                    for (int u = 0; u < kTiles; ++u) acc[u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(yp, n[1][u], acc[u], 0, 0, 0);
-#pragma unroll
-                    for (int u = 0; u < kTiles; ++u) {
-                        const float high = (float)((acc[u][3] << 8) + acc[u][2]), low = (float)((acc[u][1] << 8) + acc[u][0]);
-                        const float z = fmaf(high, 65536.0f, low);
-                        sum[u][s] = fmaf(z, scale[u][p], sum[u][s]);
+                    for (int k = 0; k < BLOCKS; ++k) {
+                        const float high = (float)((acc[4 * k + 3] << 8) + acc[4 * k + 2]), low = (float)((acc[4 * k + 1] << 8) + acc[4 * k]);
+                        float& to = sum[PACK > 1 ? p / (PARTS / PACK > 0 ? PARTS / PACK : 1) : 0][s][k];
+                        to = fmaf(fmaf(high, 65536.0f, low), scale[p], to);
                     }
                 }
             }
             if (++step == a.steps) {
 #pragma unroll
-                for (int u = 0; u < kTiles; ++u) {
-                    const long long item = (tile * kTiles + u) * kTileItems + col;
+                for (int s = 0; s < SETS; ++s)
 #pragma unroll
-                    for (int s = 0; s < SETS; ++s) {
-                        const int q = s * 4 + h;
-                        const float z = sum[u][s] * factor[q];
-                        if (kHold) { if (q < queries) held[(pairs * queries + q) * 32 + u * kTileItems + col] = z; }
-                        else if (item < a.N && q < queries) a.scores[(size_t)(q0 + q) * a.ld + item] = z;
+                    for (int k = 0; k < BLOCKS; ++k) {
+                        const int q = s * 8 + 2 * k + lane / 32;
+                        if (q >= queries) continue;
+#pragma unroll
+                        for (int o = 0; o < PACK; ++o) {
+                            const int at = lane % 32 * PACK + o;
+                            const float z = sum[o][s][k] * factor[q];
+                            const long long item = tile * kItems + at;
+                            if (kHold) held[(tiles * queries + q) * kItems + at] = z;
+                            else if (item < a.N) a.scores[(size_t)(q0 + q) * a.ld + item] = z;
+                        }
                     }
-                }
-                if (kHold && ++pairs == a.held) release(tile);
+                if (kHold && ++tiles == a.held) release(tile);
                 clear();
                 step = 0;
                 tile += waves;
             }
         }
     }
-    if (kHold && pairs > 0) release(tile - waves);
+    if (kHold && tiles > 0) release(tile - waves);
 }
 
 // Eight elements a lane; the lanes of a group share its largest absolute value.  A stream of 4 N d bytes in.
@@ -262,38 +292,49 @@ int check_q4(long long N, int B, int d, int group) {
 }
 
 // digits, factors and shifts; then the scores that are held back
-size_t q4_lds(int sets, int d) { return (size_t)ceil_div(d, kStep) * 2 * sets * kWave * 16 + (size_t)sets * 4 * 8; }
-size_t held_bytes(int queries) { return (size_t)kWaves * queries * 32 * sizeof(float); }          // a tile pair of every wave
+size_t q4_lds(int queries, int elements) { return (size_t)ceil_div(elements, kStep) * kQuarters * 2 * queries * 4 * 16 + (size_t)queries * 8; }
+size_t held_bytes(int queries, int pack) { return (size_t)kWaves * queries * kTileRows * pack * sizeof(float); }         // a tile of every wave
 
-template <int SETS, int GROUP, bool WHOLE>
+template <int BLOCKS, int SETS, int GROUP, int PACK, bool WHOLE>
 hipError_t go_q4(Q4Args a, hipStream_t st) {
-    const size_t fixed = q4_lds(SETS, a.d), pair = SETS <= 2 ? held_bytes(a.B < SETS * 4 ? a.B : SETS * 4) : 16;
-    a.item_tiles = ceil_div(a.N, kTileItems);
-    const int query_groups = (int)ceil_div(a.B, SETS * 4), per_cu = fixed + pair > kMaxLds / 2 ? 1 : 2;
-    const long long pairs = ceil_div(a.item_tiles, kTiles);
-    long long blocks = ceil_div(pairs, kWaves);
+    constexpr int kQueries = queries_of<BLOCKS, SETS>();
+    const size_t fixed = q4_lds(kQueries, a.d * PACK), tile = kQueries <= 8 ? held_bytes(a.B < kQueries ? a.B : kQueries, PACK) : 16;
+    a.rows = ceil_div(a.N, PACK);
+    a.tiles = ceil_div(a.rows, kTileRows);
+    a.steps = (int)ceil_div(a.d * PACK, kStep);
+    const int query_groups = (int)ceil_div(a.B, kQueries), per_cu = fixed + tile > kMaxLds / 2 ? 1 : 2;
+    long long blocks = ceil_div(a.tiles, kWaves);
     if (blocks > (long long)per_cu * kCUs) blocks = (long long)per_cu * kCUs;
-    const long long each = ceil_div(pairs, blocks * kWaves), room = (long long)((kMaxLds / per_cu - fixed) / pair);
+    const long long each = ceil_div(a.tiles, blocks * kWaves), room = (long long)((kMaxLds / per_cu - fixed) / tile);
     a.held = (int)(each < room ? each : room);
-    const size_t lds = fixed + a.held * pair;
-    hipError_t e = allow_lds(default_scores_q4_kernel<SETS, GROUP, WHOLE>, lds);
+    const size_t lds = fixed + a.held * tile;
+    hipError_t e = allow_lds(default_scores_q4_kernel<BLOCKS, SETS, GROUP, PACK, WHOLE>, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((default_scores_q4_kernel<SETS, GROUP, WHOLE>), dim3((unsigned)blocks, query_groups), dim3(kThreads), lds, st, a);
+    hipLaunchKernelGGL((default_scores_q4_kernel<BLOCKS, SETS, GROUP, PACK, WHOLE>), dim3((unsigned)blocks, query_groups), dim3(kThreads), lds, st, a);
     return hipGetLastError();
 }
 
-template <int GROUP, bool WHOLE>
+template <int GROUP, int PACK, bool WHOLE>
 hipError_t go_q4_sets(const Q4Args& a, hipStream_t st) {
     // as many queries a pass over the weights as there are, up to 32 and what LDS holds of their digits
-    int sets = a.B <= 4 ? 1 : a.B <= 8 ? 2 : a.B <= 16 ? 4 : 8;
-    while (sets > 1 && q4_lds(sets, a.d) + held_bytes(sets * 4) > kMaxLds) sets /= 2;
-    return sets == 8 ? go_q4<8, GROUP, WHOLE>(a, st) : sets == 4 ? go_q4<4, GROUP, WHOLE>(a, st) : sets == 2 ? go_q4<2, GROUP, WHOLE>(a, st) : go_q4<1, GROUP, WHOLE>(a, st);
+    int queries = a.B <= 2 ? 2 : a.B <= 4 ? 4 : a.B <= 8 ? 8 : a.B <= 16 ? 16 : 32;
+    while (queries > 2 && q4_lds(queries, a.d * PACK) + held_bytes(queries, PACK) > kMaxLds) queries /= 2;
+    switch (queries) {
+        case 2: return go_q4<1, 1, GROUP, PACK, WHOLE>(a, st);
+        case 4: return go_q4<2, 1, GROUP, PACK, WHOLE>(a, st);
+        case 8: return go_q4<4, 1, GROUP, PACK, WHOLE>(a, st);
+        case 16: return go_q4<4, 2, GROUP, PACK, WHOLE>(a, st);
+        default: return go_q4<4, 4, GROUP, PACK, WHOLE>(a, st);
+    }
 }
 
 template <int GROUP>
 hipError_t go_q4_group(const Q4Args& a, hipStream_t st) {
-    if (GROUP == kStep || (a.d % kStep == 0 && ((uintptr_t)a.scales & 7) == 0)) return go_q4_sets<GROUP, true>(a, st);
-    return go_q4_sets<GROUP, GROUP == kStep>(a, st);
+    if constexpr (GROUP <= 64) {
+        if (a.d == kStep / 2) return go_q4_sets<GROUP, 2, false>(a, st);
+    }
+    if (GROUP == kStep || (a.d % kStep == 0 && ((uintptr_t)a.scales & 7) == 0)) return go_q4_sets<GROUP, 1, true>(a, st);
+    return go_q4_sets<GROUP, 1, GROUP == kStep>(a, st);
 }
 
 }  // namespace
@@ -323,9 +364,9 @@ int pq_default_scores_q4(const uint8_t* packed, const uint16_t* scales, const fl
     const int rc = check_q4(N, B, d, group);
     if (rc != PQ_OK) return rc;
     if (ld < N) return PQ_ERR_SHAPE;
-    if (q4_lds(1, d) + held_bytes(4) > kMaxLds) return PQ_ERR_UNSUPPORTED;
+    if (d > kMaxWidth) return PQ_ERR_UNSUPPORTED;
     if (((uintptr_t)packed & 15) || ((uintptr_t)scales & 1) || (((uintptr_t)queries | (uintptr_t)scores) & 3)) return PQ_ERR_ALIGN;
-    const Q4Args a{packed, scales, queries, scores, N, ld, 0, B, d, (int)ceil_div(d, kStep)};
+    const Q4Args a{packed, scales, queries, scores, N, ld, 0, 0, B, d, 0, 0};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return pqk::record_hip_error(group == 32 ? go_q4_group<32>(a, st) : group == 64 ? go_q4_group<64>(a, st) : go_q4_group<128>(a, st));
 }
