@@ -24,7 +24,7 @@ struct Q4Args {
     long long N, ld;
     long long rows, tiles;      // rows of PACK items; tiles of 32 rows
     int B, d, steps;            // steps of a row = elements / 128, rounded up
-    int held;                   // tiles whose scores a wave holds back
+    int held;                   // tiles whose scores a wave holds back, or 0
 };
 
 // A query element as a whole number of 31 bits, in four signed bytes: v = d0 + 2^8 d1 + 2^16 d2 + 2^24 d3.
@@ -45,8 +45,9 @@ template <int BLOCKS, int SETS> constexpr int queries_of() { return SETS == 1 ? 
 // Bound by the stream of nibbles, which comes in 16 bytes a lane, 64 neighbouring bytes of sixteen rows an instruction (with
 // 8 bytes a lane the same stream reached 4.4 TB/s instead of 5.9).  A lane so has a quarter of row lane % 16 or 16 + lane % 16;
 // eight swaps between lanes make of these, for each quarter, column lane % 32 with sixteen k by lane / 32.
-// Scores are held back in LDS and leave a wave's tiles at a time: stores between the loads cost the stream more than their
-// bytes (1.3 GB read by 128 bytes stored per 8 KB: 207 us without stores, 262 with, 227 held back).
+// One query's scores are held back in LDS and leave a wave's tiles at a time: stores between the loads cost a long stream more
+// than their bytes (5M items of 256: 136 us held back, 143 as they come).  More queries' leave at once (four 159 and 153, eight
+// 175 and 164).
 // GROUP: weights that share a scale.  PACK: items of a row of weights, 2 for d = 64, whose own rows are half a step: a group's
 // sum then belongs to one of the two.  WHOLE: rows are whole steps and their scales aligned.
 template <int BLOCKS, int SETS, int GROUP, int PACK, bool WHOLE>
@@ -54,14 +55,14 @@ __global__ __launch_bounds__(kThreads, SETS <= 2 ? 4 : 2) void default_scores_q4
     constexpr int PARTS = kStep / GROUP, kOf = kQuarters / PARTS;              // groups a step, quarters a group
     constexpr int kQueries = queries_of<BLOCKS, SETS>(), kRows = SETS == 1 ? 8 * BLOCKS : 32;      // digit rows kept of a set
     constexpr int kAhead = 4;                                  // steps whose weights are on their way
-    constexpr bool kHold = kQueries <= 8;
+    constexpr bool kHold = kQueries == 2 && PACK == 1;
     constexpr int kItems = kTileRows * PACK;                   // of a tile
     static_assert(PACK == 1 || PARTS % PACK == 0, "a group belongs to one item");
     extern __shared__ __align__(16) unsigned char smem[];
     i32x4* digits = reinterpret_cast<i32x4*>(smem);            // [step][quarter][set][half][row]: as the matrix instruction takes them
     float* factor = reinterpret_cast<float*>(digits + (size_t)a.steps * kQuarters * SETS * 2 * kRows);         // [query]
     int* shift = reinterpret_cast<int*>(factor + kQueries);
-    float* held = reinterpret_cast<float*>(shift + kQueries);                                    // [wave][tile][query][items]
+    float* held = reinterpret_cast<float*>(shift + kQueries);                                    // [wave][tile][items]
     const int groups = a.d * PACK / GROUP;                     // of a row
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int q0 = blockIdx.y * kQueries;
@@ -161,13 +162,12 @@ __global__ __launch_bounds__(kThreads, SETS <= 2 ? 4 : 2) void default_scores_q4
     int step = 0, tiles = 0;
     Scales two_steps = {};
     const int queries = min(kQueries, a.B - q0);
-    held += (size_t)wave * a.held * queries * kItems;
-    auto release = [&](long long last_tile) {                  // the held scores, the last of them of last_tile
+    held += (size_t)wave * a.held * kItems;
+    auto release = [&](long long last_tile) {                  // one query's held scores, the last of them of last_tile
         wave_reads_after_writes();
-        for (int r = lane / kItems; r < tiles * queries; r += kWave / kItems) {
-            const int t = r / queries, q = r - t * queries;
+        for (int t = lane / kItems; t < tiles; t += kWave / kItems) {
             const long long item = (last_tile - (long long)(tiles - 1 - t) * waves) * kItems + lane % kItems;
-            if (item < a.N) a.scores[(size_t)(q0 + q) * a.ld + item] = held[r * kItems + lane % kItems];
+            if (item < a.N) a.scores[(size_t)q0 * a.ld + item] = held[t * kItems + lane % kItems];
         }
         wave_reads_after_writes();
         tiles = 0;
@@ -245,11 +245,11 @@ __global__ __launch_bounds__(kThreads, SETS <= 2 ? 4 : 2) void default_scores_q4
                             const int at = lane % 32 * PACK + o;
                             const float z = sum[o][s][k] * factor[q];
                             const long long item = tile * kItems + at;
-                            if (kHold) held[(tiles * queries + q) * kItems + at] = z;
+                            if (kHold && a.held > 0) held[tiles * kItems + at] = z;
                             else if (item < a.N) a.scores[(size_t)(q0 + q) * a.ld + item] = z;
                         }
                     }
-                if (kHold && ++tiles == a.held) release(tile);
+                if (kHold && a.held > 0 && ++tiles == a.held) release(tile);
                 clear();
                 step = 0;
                 tile += waves;
@@ -293,19 +293,19 @@ int check_q4(long long N, int B, int d, int group) {
 
 // digits, factors and shifts; then the scores that are held back
 size_t q4_lds(int queries, int elements) { return (size_t)ceil_div(elements, kStep) * kQuarters * 2 * queries * 4 * 16 + (size_t)queries * 8; }
-size_t held_bytes(int queries, int pack) { return (size_t)kWaves * queries * kTileRows * pack * sizeof(float); }         // a tile of every wave
+size_t held_bytes() { return (size_t)kWaves * kTileRows * sizeof(float); }         // a tile of every wave
 
 template <int BLOCKS, int SETS, int GROUP, int PACK, bool WHOLE>
 hipError_t go_q4(Q4Args a, hipStream_t st) {
     constexpr int kQueries = queries_of<BLOCKS, SETS>();
-    const size_t fixed = q4_lds(kQueries, a.d * PACK), tile = kQueries <= 8 ? held_bytes(a.B < kQueries ? a.B : kQueries, PACK) : 16;
+    const size_t fixed = q4_lds(kQueries, a.d * PACK), tile = kQueries == 2 && a.B == 1 && PACK == 1 ? held_bytes() : 0;
     a.rows = ceil_div(a.N, PACK);
     a.tiles = ceil_div(a.rows, kTileRows);
     a.steps = (int)ceil_div(a.d * PACK, kStep);
     const int query_groups = (int)ceil_div(a.B, kQueries), per_cu = fixed + tile > kMaxLds / 2 ? 1 : 2;
     long long blocks = ceil_div(a.tiles, kWaves);
     if (blocks > (long long)per_cu * kCUs) blocks = (long long)per_cu * kCUs;
-    const long long each = ceil_div(a.tiles, blocks * kWaves), room = (long long)((kMaxLds / per_cu - fixed) / tile);
+    const long long each = ceil_div(a.tiles, blocks * kWaves), room = tile ? (long long)((kMaxLds / per_cu - fixed) / tile) : 0;
     a.held = (int)(each < room ? each : room);
     const size_t lds = fixed + a.held * tile;
     hipError_t e = allow_lds(default_scores_q4_kernel<BLOCKS, SETS, GROUP, PACK, WHOLE>, lds);
@@ -318,7 +318,7 @@ template <int GROUP, int PACK, bool WHOLE>
 hipError_t go_q4_sets(const Q4Args& a, hipStream_t st) {
     // as many queries a pass over the weights as there are, up to 32 and what LDS holds of their digits
     int queries = a.B <= 2 ? 2 : a.B <= 4 ? 4 : a.B <= 8 ? 8 : a.B <= 16 ? 16 : 32;
-    while (queries > 2 && q4_lds(queries, a.d * PACK) + held_bytes(queries, PACK) > kMaxLds) queries /= 2;
+    while (queries > 2 && q4_lds(queries, a.d * PACK) + held_bytes() > kMaxLds) queries /= 2;
     switch (queries) {
         case 2: return go_q4<1, 1, GROUP, PACK, WHOLE>(a, st);
         case 4: return go_q4<2, 1, GROUP, PACK, WHOLE>(a, st);
