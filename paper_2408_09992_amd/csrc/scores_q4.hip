@@ -51,7 +51,7 @@ template <int BLOCKS, int SETS> constexpr int queries_of() { return SETS == 1 ? 
 // GROUP: weights that share a scale.  PACK: items of a row of weights, 2 for d = 64, whose own rows are half a step: a group's
 // sum then belongs to one of the two.  WHOLE: rows are whole steps and their scales aligned.
 template <int BLOCKS, int SETS, int GROUP, int PACK, bool WHOLE>
-__global__ __launch_bounds__(kThreads, SETS <= 2 ? 4 : 2) void default_scores_q4_kernel(Q4Args a) {
+__global__ __launch_bounds__(kThreads, SETS * PACK <= 2 ? 4 : 2) void default_scores_q4_kernel(Q4Args a) {
     constexpr int PARTS = kStep / GROUP, kOf = kQuarters / PARTS;              // groups a step, quarters a group
     constexpr int kQueries = queries_of<BLOCKS, SETS>(), kRows = SETS == 1 ? 8 * BLOCKS : 32;      // digit rows kept of a set
     constexpr int kAhead = 4;                                  // steps whose weights are on their way
@@ -214,24 +214,26 @@ __global__ __launch_bounds__(kThreads, SETS <= 2 ? 4 : 2) void default_scores_q4
                 const uint32_t v[2] = {m[g][0] ^ 0x88888888u, m[g][1] ^ 0x88888888u};
                 n[g] = i32x4{(int)(v[0] << 4 & 0xF0F0F0F0u), (int)(v[0] & 0xF0F0F0F0u), (int)(v[1] << 4 & 0xF0F0F0F0u), (int)(v[1] & 0xF0F0F0F0u)};
             }
+            if (tile < a.tiles) {                              // (else past the wave's last tile: 20,000 items of 128, 32 queries 13 us without
+                stay_a_branch();                               //  this, 10 with; long streams of wide rows lose 0.7 %)
 #pragma unroll
-            for (int s = 0; s < SETS; ++s) {
+                for (int s = 0; s < SETS; ++s) {
 #pragma unroll
-                for (int p = 0; p < PARTS; ++p) {
-                    i32x16 acc = {};
+                    for (int p = 0; p < PARTS; ++p) {
+                        i32x16 acc = {};
 #pragma unroll
-                    for (int g = p * kOf; g < (p + 1) * kOf; ++g) {
-                        // (rows that are not kept repeat others: their sums are not used)
-                        const i32x4 x = digits[(((size_t)step * kQuarters + g) * SETS + s) * 2 * kRows + lane / 32 * kRows + lane % kRows];
-                        acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, n[g], acc, 0, 0, 0);
+                        for (int g = p * kOf; g < (p + 1) * kOf; ++g) {
+                            // (rows that are not kept repeat others: their sums are not used)
+                            const i32x4 x = digits[(((size_t)step * kQuarters + g) * SETS + s) * 2 * kRows + lane / 32 * kRows + lane % kRows];
+                            acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, n[g], acc, 0, 0, 0);
+                        }
+#pragma unroll
+                        for (int k = 0; k < BLOCKS; ++k) {
+                            const float high = (float)((acc[4 * k + 3] << 8) + acc[4 * k + 2]), low = (float)((acc[4 * k + 1] << 8) + acc[4 * k]);
+                            float& to = sum[PACK > 1 ? p / (PARTS / PACK > 0 ? PARTS / PACK : 1) : 0][s][k];
+                            to = fmaf(fmaf(high, 65536.0f, low), scale[p], to);
+                        }
                     }
-#pragma unroll
-                    for (int k = 0; k < BLOCKS; ++k) {
-                        const float high = (float)((acc[4 * k + 3] << 8) + acc[4 * k + 2]), low = (float)((acc[4 * k + 1] << 8) + acc[4 * k]);
-                        float& to = sum[PACK > 1 ? p / (PARTS / PACK > 0 ? PARTS / PACK : 1) : 0][s][k];
-                        to = fmaf(fmaf(high, 65536.0f, low), scale[p], to);
-                    }
-                }
             }
             if (++step == a.steps) {
 #pragma unroll
