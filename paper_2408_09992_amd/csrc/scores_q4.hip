@@ -234,6 +234,7 @@ __global__ __launch_bounds__(kThreads, SETS * PACK <= 2 ? 4 : 2) void default_sc
                             to = fmaf(fmaf(high, 65536.0f, low), scale[p], to);
                         }
                     }
+                }
             }
             if (++step == a.steps) {
 #pragma unroll
