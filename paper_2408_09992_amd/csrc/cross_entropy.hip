@@ -432,13 +432,29 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackAr
     }
 }
 
-// The shares' sums of every table entry, added and turned into gradients.
-__global__ __launch_bounds__(256) void cross_entropy_backward_join_kernel(BackArgs a, int shares, int code_bytes) {
+// The shares' sums of every table entry, added and turned into gradients, by LEADS threads an entry, each of them every LEADS-th
+// share (the sums are whole numbers: any order gives the same).  One thread alone would wait for many shares one after the
+// other: 5M items, one position 85 us for the gradient with one, 27 with eight; with few shares eight have nothing to do.
+constexpr int kJoinThreads = 256, kJoinLeads = 8;
+template <int LEADS>
+__global__ __launch_bounds__(kJoinThreads) void cross_entropy_backward_join_kernel(BackArgs a, int shares, int code_bytes) {
+    constexpr int kEntries = kJoinThreads / LEADS;
+    __shared__ uint64_t part[LEADS][kEntries];
     const size_t entries = (size_t)a.B * a.m * a.b;
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= entries) return;
+    const size_t i = (size_t)blockIdx.x * kEntries + threadIdx.x % kEntries;
+    const int lead = threadIdx.x / kEntries;
     uint64_t total = 0;
-    for (int s = 0; s < shares; ++s) total += a.partial[(size_t)s * entries + i];
+    if (i < entries) {
+#pragma unroll 8
+        for (int s = lead; s < shares; s += LEADS) total += a.partial[(size_t)s * entries + i];
+    }
+    if constexpr (LEADS > 1) {
+        part[lead][threadIdx.x % kEntries] = total;
+        __syncthreads();
+#pragma unroll
+        for (int l = 1; l < LEADS; ++l) total += part[l][threadIdx.x % kEntries];              // (the first thread of an entry has the whole)
+    }
+    if (lead != 0 || i >= entries) return;
     const size_t row = i / a.b;
     a.dS[i] = gradient_of(a, total, (int)(row / a.m), (int)(row % a.m), (int)(i - row * a.b), code_bytes);
 }
@@ -616,7 +632,10 @@ int backward(const CT* codes, const float* S, const int* targets, const float* l
     else e = go_backward_q<0, CT>(p, a, st);
     if (e == hipSuccess && p.shares > 1) {
         const size_t entries = (size_t)B * m * b;
-        hipLaunchKernelGGL(cross_entropy_backward_join_kernel, dim3((unsigned)ceil_div(entries, 256)), dim3(256), 0, st, a, p.shares, (int)sizeof(CT));
+        if (p.shares > kJoinLeads)
+            hipLaunchKernelGGL(cross_entropy_backward_join_kernel<kJoinLeads>, dim3((unsigned)ceil_div(entries, kJoinThreads / kJoinLeads)), dim3(kJoinThreads), 0, st, a, p.shares, (int)sizeof(CT));
+        else
+            hipLaunchKernelGGL(cross_entropy_backward_join_kernel<1>, dim3((unsigned)ceil_div(entries, kJoinThreads)), dim3(kJoinThreads), 0, st, a, p.shares, (int)sizeof(CT));
         e = hipGetLastError();
     }
     return record_hip_error(e);
