@@ -94,6 +94,8 @@ __device__ __forceinline__ Operand positions_of(const DenseArgs& a, int position
 
 // Statistics of a tile of positions over a group of item tiles, one after the other.  As in the loss by sub-ids a lane's
 // reference c moves only when a score passes it by 2^kHeadroom; lanes, halves and waves join once, at the end.
+// Bound by the matrix cores: 1024 positions, 1.28M items of 512 bfloat16, 1.44 to 1.56 ms, 860 to 930 TFLOP/s with an exponential
+// per score; 2048 positions, 34,742 items of 512 float32, 404 to 439 us, 166 to 181 TFLOP/s (4.25 rounds of tiles).
 template <typename T, int BN, int ITEMS>
 __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_cross_entropy_kernel(DenseArgs a) {
     using Tile = ScoresTile<T, BN, ITEMS>;
@@ -239,6 +241,7 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
 // dz of a piece of items: scores as in the loss, then (exp(z - lse) - [target]) g as the products' operands, position by
 // position.  For 16-bit operands dz is rounded to their type: it is the products' input as H and W are, and what they add up
 // (in float32) is rounded to that type once more at the end.
+// A piece of 131,072 items, 1024 positions of 512 bfloat16: 179 to 187 us, 750 TFLOP/s, and 268 MB written.
 // ROWS: up to 64 positions, whose rows (see default_rows_kernel) the workgroups make themselves.
 template <typename T, int BN, int ITEMS, bool ROWS>
 __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_dz_kernel(DenseArgs a) {
@@ -318,7 +321,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     }
 }
 
-// A tile of dW of a piece: [items][d], summed over the positions.
+// A tile of dW of a piece: [items][d], summed over the positions.  The piece above: 133 to 145 us, about 1000 TFLOP/s.
 template <typename T, int COLS, int ITEMS>
 __device__ __forceinline__ void dw_tile(const DenseArgs& a, int block) {
     using Tile = TileW<T, COLS, ITEMS>;
@@ -363,6 +366,7 @@ template <typename T, int COLS, int ITEMS>
 __global__ __launch_bounds__((TileW<T, COLS, ITEMS>::kThreads), 2) void default_dw_kernel(DenseArgs a) { dw_tile<T, COLS, ITEMS>(a, blockIdx.x); }
 
 // A slice's share of a tile of dH: [positions][d] summed over its items of the piece, added to what earlier pieces left there.
+// The piece above: 139 to 145 us, about 960 TFLOP/s.
 template <typename T, int BM, int BN>
 __device__ __forceinline__ void dh_tile(const DenseArgs& a, int block) {
     using Tile = TileH<T, BM, BN>;
@@ -413,7 +417,8 @@ __device__ __forceinline__ void dh_tile(const DenseArgs& a, int block) {
 template <typename T, int BM, int BN>
 __global__ __launch_bounds__((TileH<T, BM, BN>::kThreads), 2) void default_dh_kernel(DenseArgs a) { dh_tile<T, BM, BN>(a, blockIdx.x); }
 
-// Both, by tiles of 64 x 64, where neither fills the chip and a launch takes as long as they do.
+// Both, by tiles of 64 x 64, where neither fills the chip and a launch takes as long as they do (10,000 items of 64, 50 positions
+// in float32: 6.4 us, and the step 29 us instead of 34).
 template <typename T>
 __global__ __launch_bounds__((TileW<T, 64, 64>::kThreads), 2) void default_products_kernel(DenseArgs a) {
     if ((int)blockIdx.x < a.w_blocks) dw_tile<T, 64, 64>(a, blockIdx.x);
@@ -470,7 +475,7 @@ __device__ __forceinline__ void bring_rows(const void* base, int d, long long ro
 }
 
 // The loss of up to 64 positions of 16-bit operands, d <= 512: as default_few_kernel below takes its tiles, so that loads do not
-// pause between them (1.3 GB of W: 271 us by default_cross_entropy_kernel's tiles).
+// pause between them (64 positions, 1.3 GB of W: 250 to 262 us, 5.0 to 5.2 TB/s; 271 by default_cross_entropy_kernel's tiles).
 template <typename T, int D>
 __global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseArgs a) {
     constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
@@ -536,7 +541,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseA
 }
 
 // D: d rounded up to 64, 128, 256 or 512.  A tile holds 16384 / D items.  Bound by memory: W in, dW out, 2.6 GB for 1.27M items
-// of 512 elements.
+// of 512 elements in 515 to 550 us, 4.7 to 5.1 TB/s, where a copy reaches 4.73.
 template <typename T, int D>
 __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a) {
     constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
@@ -659,7 +664,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     }
 }
 
-// The slices' shares of dH, added: every eighth slice by one of eight threads, these in their order.
+// The slices' shares of dH, added: every eighth slice by one of eight threads, these in their order.  64 positions of 512, 256
+// slices: 7.5 us for 34 MB.
 template <typename T>
 __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
     __shared__ float part[8][32];

@@ -187,6 +187,12 @@ def test_rows_of_the_gradient_sum_to_zero(pq):
     assert np.all(np.abs(dS.astype(np.float64).sum(2)) <= np.abs(grad)[:, None] * (2 * tol + 512 * U))
 
 
+@pytest.mark.parametrize("m,b,B,wide", [(8, 256, 1, False), (4, 200, 3, False), (2, 1000, 2, True)])
+def test_many_shares(pq, m, b, B, wide):
+    # more shares of the items than the threads that join an entry's
+    check(pq, *draw(150_001, m, b, B, seed=m + B, wide=wide))
+
+
 def test_same_bits_every_time_and_on_any_stream(pq):
     codes, S, targets, grad = draw(60_000, 8, 256, 10, seed=9, zipf=True)
     first = run(pq, codes, S, targets, grad)

@@ -82,6 +82,14 @@ def test_few_positions(pq, N, d, B, type):
     check(pq, *draw(N, d, B, type, seed=N + d + B), type)
 
 
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,d,B", [(400_003, 64, 33), (200_100, 128, 40), (50_007, 512, 64), (100_000, 520, 5), (400_000, 56, 100), (200_001, 128, 120), (50_001, 512, 100), (160_007, 64, 300), (80_003, 128, 300),
+                                   (9000, 512, 700)])
+def test_products_that_fill_the_chip(pq, N, d, B, type):
+    # tiles of every height and width, each product in a launch of its own
+    check(pq, *draw(N, d, B, type, seed=N + d + B), type)
+
+
 @pytest.mark.parametrize("d", [4, 12, 20, 36, 100])
 def test_float32_widths(pq, d):
     check(pq, *draw(900, d, 70, "f32", seed=d), "f32")
