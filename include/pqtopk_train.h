@@ -108,7 +108,7 @@ int pq_default_cross_entropy(const void* W, const void* queries, const int* targ
  *     dz_qi = grad_loss[q] * (exp(r_qi - lse_q) - [i = t_q])     dqueries = dz W     dW = dz^T queries
  *   lse  in  float [B]  as returned by pq_default_cross_entropy() for the same W and queries
  *   dqueries  out  type [B][d];  dW  out  type [N][d]  (both 16-byte aligned, every element written)
- * The items are taken in pieces whose dz fits the workspace (2^27 elements, or 2048 items of every position).  dz is
+ * The items are taken in pieces whose dz fits the workspace (1 GB of it, or 2048 items of every position).  dz is
  * held in the inputs' type, scaled so that float16 keeps probabilities down to 2^-39; the products' sums are float32,
  * rounded to the type once.
  * Errors: as pq_default_cross_entropy().

@@ -5,7 +5,11 @@ namespace pqk {
 namespace head {
 namespace {
 
-constexpr long long kDzElements = 1LL << 27;           // of the buffer: 256 MB of 16-bit dz, the size of the last-level cache
+// Bytes of dz's buffer.  Fewer, longer launches gain more than a buffer of the last-level cache's size (gradient, us, 256 MB and
+// 1 GB of bfloat16: 1.28M items of 128, 256 positions 756 and 660; of 512, 1024 positions 4550 and 4410; 600,000 of 256, 512
+// positions 794 and 708; float32, 512 MB and 1 GB, 1 to 4 %), but for short rows, whose products wait for dz alone (bfloat16,
+// 1.28M of 64, 512 positions 943 and 995).
+constexpr long long kDzBytes = 1LL << 30, kDzBytesShort = 1LL << 28;
 constexpr long long kMaxPiece = 1LL << 22;
 
 // What a tile of 256 rows and `cols` columns takes a compute unit next to one of 256 x 256 that keeps the matrix cores as busy
@@ -29,7 +33,11 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
     p.item_tiles = ceil_div(N, p.loss_items);
     // loss: the tiles of positions, and how many tiles of items a workgroup takes, whose rounds over the chip take least
     double best = 1e300;
-    for (int tile : {256, 128, 64})
+    for (int tile : {256, 128, 64}) {
+        // (of short rows in 16 bits a tile's exponentials take longer than its products: two workgroups of 128 positions on a compute
+        // unit do one while the other does the other; 300,000 items of 64, 2048 positions 235 and 201 us, of 128, 1024 positions
+        // 143 and 136, of 256 the same)
+        if (tile == 256 && size == 2 && d <= 128) continue;
         for (int each = 1; each <= 64; each *= 2) {
             const long long position_tiles = ceil_div(B, tile), groups = ceil_div(p.item_tiles, each);
             const double cost = (double)ceil_div(groups * position_tiles, kCUs) * (each * tile_cost(tile, size) + kTileStart);
@@ -38,12 +46,13 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
                 p.positions = tile; p.position_tiles = (int)position_tiles; p.tiles_each = each; p.groups = (int)groups;
             }
         }
+    }
     if (p.loss_items == 64) {
         p.positions = 64; p.position_tiles = (int)ceil_div(B, 64); p.tiles_each = 1; p.groups = (int)p.item_tiles;
     }
     // gradient: pieces of the items, in balance
     const int small = B <= 64 ? 64 : 128;              // (positions are padded to a multiple of this or of 256)
-    long long piece = kDzElements / (long long)round_up(B, small);
+    long long piece = (size == 2 && d <= 64 ? kDzBytesShort : kDzBytes) / size / (long long)round_up(B, small);
     if (piece < 2048) piece = 2048;
     if (piece > kMaxPiece) piece = kMaxPiece;
     p.pieces = (int)ceil_div(N, piece);

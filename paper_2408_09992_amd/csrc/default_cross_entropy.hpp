@@ -5,8 +5,8 @@
 //
 // Everything is a matrix product whose one side is short: T positions, d elements, N items.  The loss keeps z in registers:
 // a workgroup multiplies a tile of items by a tile of positions and folds it into the positions' running sums.  The gradient
-// takes the items in pieces: z of a piece once more, its dz to a buffer that stays in the last-level cache, then the two
-// products from there.  8 T N d operations in all, 2 of them the loss's.
+// takes the items in pieces: z of a piece once more, its dz to a buffer, then the two products from there.  8 T N d operations
+// in all, 2 of them the loss's.
 #pragma once
 #include <type_traits>
 #include "pqtopk_train.h"
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
 // dz of a piece of items: scores as in the loss, then (exp(z - lse) - [target]) g as the products' operands, position by
 // position.  For 16-bit operands dz is rounded to their type: it is the products' input as H and W are, and what they add up
 // (in float32) is rounded to that type once more at the end.
-// A piece of 131,072 items, 1024 positions of 512 bfloat16: 179 to 187 us, 750 TFLOP/s, and 268 MB written.
+// 131,072 items, 1024 positions of 512 bfloat16: 179 to 187 us, 750 TFLOP/s, and 268 MB written.
 // ROWS: up to 64 positions, whose rows (see default_rows_kernel) the workgroups make themselves.
 template <typename T, int BN, int ITEMS, bool ROWS>
 __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_dz_kernel(DenseArgs a) {
@@ -321,7 +321,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     }
 }
 
-// A tile of dW of a piece: [items][d], summed over the positions.  The piece above: 133 to 145 us, about 1000 TFLOP/s.
+// A tile of dW of a piece: [items][d], summed over the positions.  As many: 133 to 145 us, about 1000 TFLOP/s.
 template <typename T, int COLS, int ITEMS>
 __device__ __forceinline__ void dw_tile(const DenseArgs& a, int block) {
     using Tile = TileW<T, COLS, ITEMS>;
@@ -366,7 +366,7 @@ template <typename T, int COLS, int ITEMS>
 __global__ __launch_bounds__((TileW<T, COLS, ITEMS>::kThreads), 2) void default_dw_kernel(DenseArgs a) { dw_tile<T, COLS, ITEMS>(a, blockIdx.x); }
 
 // A slice's share of a tile of dH: [positions][d] summed over its items of the piece, added to what earlier pieces left there.
-// The piece above: 139 to 145 us, about 960 TFLOP/s.
+// As many: 139 to 145 us, about 960 TFLOP/s.
 template <typename T, int BM, int BN>
 __device__ __forceinline__ void dh_tile(const DenseArgs& a, int block) {
     using Tile = TileH<T, BM, BN>;

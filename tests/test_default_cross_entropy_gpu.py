@@ -75,6 +75,13 @@ def test_pieces_of_the_catalogue(pq, type):
     check(pq, *draw(N, d, B, type, seed=2), type)
 
 
+@pytest.mark.parametrize("N,d,type", [(70_003, 32, "f32"), (140_003, 72, "bf16")])
+def test_pieces_of_longer_rows(pq, N, d, type):
+    # more than a gigabyte of dz
+    assert N * 4224 * (4 if type == "f32" else 2) > 2 ** 30
+    check(pq, *draw(N, d, 4100, type, seed=6), type)
+
+
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 @pytest.mark.parametrize("N,d,B", [(9001, 304, 40), (20_003, 8, 64), (8200, 328, 1), (5000, 200, 33), (7777, 392, 64), (16_385, 56, 17), (33_000, 120, 5), (3, 512, 64), (70_001, 512, 64), (40_000, 264, 9)])
 def test_few_positions(pq, N, d, B, type):
