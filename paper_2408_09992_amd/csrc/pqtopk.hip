@@ -1972,11 +1972,11 @@ const char* pq_strerror(int code) {
         case PQ_ERR_NULL: return "a required pointer is NULL";
         case PQ_ERR_SHAPE:
             return "bad shape: need B,d,m,b,K,N >= 1, d % m == 0, b <= 256 (65536 with 16-bit sub-ids), K <= N (K <= |V| <= N with a "
-                   "candidate list), N < 2^31";
+                   "candidate list), N < 2^31, groups of 32, 64 or 128 that divide d";
         case PQ_ERR_UNSUPPORTED:
-            return "unsupported: K > 512, m > 128, B > 65535, or score tables plus candidate lists exceed LDS";
-        case PQ_ERR_WORKSPACE: return "workspace smaller than pq_score_topk_workspace_bytes()";
-        case PQ_ERR_ALIGN: return "pointer alignment: codes and workspace 16 bytes, float/int arrays 4 bytes";
+            return "unsupported: K > 512, m > 128, B > 65535, an embedding's width (see the call), or score tables (with candidate lists) exceed LDS";
+        case PQ_ERR_WORKSPACE: return "workspace smaller than the call's _workspace_bytes() function names";
+        case PQ_ERR_ALIGN: return "pointer alignment: codes, item embeddings and workspace 16 bytes, float/int arrays 4 bytes";
         case PQ_ERR_HIP: return g_hip_error;
         case PQ_ERR_TOO_LARGE: return "problem needs more scratch than the library's built-in array holds (PQ_STATIC_SCRATCH_BYTES)";
         default: return "unknown pqtopk error code";
