@@ -33,8 +33,8 @@ template <typename T> struct ScoresTile<T, 128, 256> : MatrixTile<T, 256, 128, 1
 template <typename T> struct ScoresTile<T, 256, 256> : MatrixTile<T, 256, 256, 128, 64, true, true> {};
 template <typename T, int COLS, int ITEMS> struct TileW;
 template <typename T> struct TileW<T, 64, 64> : MatrixTile<T, 64, 64, 32, 32, false, false> {};
-template <typename T> struct TileW<T, 64, 256> : MatrixTile<T, 256, 64, 64, 64, false, false> {};
-template <typename T> struct TileW<T, 128, 256> : MatrixTile<T, 256, 128, 128, 64, false, false> {};
+template <typename T> struct TileW<T, 64, 256> : MatrixTile<T, 64, 256, 64, 64, false, false> {};
+template <typename T> struct TileW<T, 128, 256> : MatrixTile<T, 128, 256, 128, 64, false, false> {};
 template <typename T> struct TileW<T, 256, 256> : MatrixTile<T, 256, 256, 128, 64, false, false> {};
 template <typename T, int ROWS, int COLS> struct TileH;
 template <typename T> struct TileH<T, 64, 64> : MatrixTile<T, 64, 64, 32, 32, true, false> {};
@@ -238,6 +238,37 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
     if (tid == 0) *a.factor = top / kDzScale;
 }
 
+// Blocks of 32 x 32 results leave through the wave's LDS, N of them at a time, in rows of 16-byte pieces: row lane % 32 of a block
+// is a column of the product, element 8 (e / 4) + 4 (lane / 32) + e % 4 of it is value(block, e), and put(block, row, piece, its
+// 16 bytes) takes them on.  The pieces of a row are swapped by its number, so that writes and reads spread over the banks.
+template <typename T, int MI> constexpr int kBlocks = sizeof(T) == 2 && MI % 2 == 0 ? 2 : 1;          // (4 KB a wave)
+template <int N, typename Value, typename Put>
+__device__ __forceinline__ void store_blocks(unsigned char* own, Value value, Put put) {
+    typedef decltype(value(0, 0)) T;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    constexpr int kPieces = 32 * (int)sizeof(T) / 16, kBytes = 32 * 32 * (int)sizeof(T);
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int four = 0; four < 4; ++four) {
+            T4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = value(k, 4 * four + e);
+            const int byte = (8 * four + 4 * (lane / 32)) * (int)sizeof(T), piece = (byte / 16) ^ (lane % 32 / (8 / kPieces) % kPieces);
+            *reinterpret_cast<T4*>(own + k * kBytes + (lane % 32 * kPieces + piece) * 16 + byte % 16) = v;
+        }
+    wave_reads_after_writes();
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int i = 0; i < kPieces / 2; ++i) {
+            const int at = i * kWave + lane, row = at / kPieces, piece = at % kPieces;
+            put(k, row, piece, *reinterpret_cast<const uint4*>(own + k * kBytes + (row * kPieces + (piece ^ (row / (8 / kPieces) % kPieces))) * 16));
+        }
+    wave_reads_after_writes();
+}
+
 // dz of a piece of items: scores as in the loss, then (exp(z - lse) - [target]) g as the products' operands, position by
 // position.  For 16-bit operands dz is rounded to their type: it is the products' input as H and W are, and what they add up
 // (in float32) is rounded to that type once more at the end.
@@ -294,30 +325,13 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
                     if (at >= left) acc[mi][ni][e] = 0.0f;
                 }
         }
-        // 32 positions x 32 items at a time through the wave's LDS: positions leave in rows of 16-byte pieces.  The pieces of
-        // a row are swapped by its number, so that writes and reads spread over the banks.
-        constexpr int kPieces = 32 * (int)sizeof(T) / 16;
         T* out = static_cast<T*>(a.dz) + ((size_t)(tile / (kItems / ITEMS)) * a.padded + q0) * kItems + tile % (kItems / ITEMS) * ITEMS + Tile::wave_row();
 #pragma unroll
-        for (int mi = 0; mi < MI; ++mi) {
-            typedef T T4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-            for (int four = 0; four < 4; ++four) {
-                T4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (T)(acc[mi][ni][4 * four + e] * info.scale);
-                const int byte = (8 * four + 4 * (lane / 32)) * (int)sizeof(T), piece = (byte / 16) ^ (lane % 32 / (8 / kPieces) % kPieces);
-                *reinterpret_cast<T4*>(own + (lane % 32 * kPieces + piece) * 16 + byte % 16) = v;
-            }
-            wave_reads_after_writes();
-#pragma unroll
-            for (int i = 0; i < kPieces / 2; ++i) {
-                const int at = i * kWave + lane, row = at / kPieces, piece = at % kPieces;
-                const uint4 v = *reinterpret_cast<const uint4*>(own + (row * kPieces + (piece ^ (row / (8 / kPieces) % kPieces))) * 16);
-                *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(out + (size_t)row * kItems + 32 * mi) + piece * 16) = v;
-            }
-            wave_reads_after_writes();
-        }
+        for (int mi = 0; mi < MI; mi += kBlocks<T, MI>)
+            store_blocks<kBlocks<T, MI>>(own, [&](int k, int e) { return (T)(acc[mi + k][ni][e] * info.scale); },
+                                         [&](int k, int row, int piece, uint4 v) {
+                                             *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(out + (size_t)row * kItems + 32 * (mi + k)) + piece * 16) = v;
+                                         });
     }
 }
 
@@ -328,38 +342,25 @@ __device__ __forceinline__ void dw_tile(const DenseArgs& a, int block) {
     int tile, ct;
     chiplet_order(block, a.tiles_n, tile, ct);
     if (tile >= a.tiles_m) return;
-    const int lane = threadIdx.x % kWave;
     f32x16 acc[Tile::MI][Tile::NI];
     const Operand dz{static_cast<const T*>(a.dz) + (size_t)(tile / (kItems / ITEMS)) * a.padded * kItems, kItems * sizeof(T), tile % (kItems / ITEMS) * ITEMS, kItems, 0, a.padded};
     const Operand h{a.H, (size_t)a.d * sizeof(T), (long long)ct * COLS, a.d, 0, a.B};
-    Tile::run(dz, h, acc);
+    Tile::run(h, dz, acc);                             // (elements by items: a lane has four neighbouring elements of an item)
     const float factor = *a.factor;
-    const long long item0 = a.first_item + (long long)tile * ITEMS + Tile::wave_row();
-    const int left = left_of(a.N - item0, 32 * Tile::MI), col0 = ct * COLS + Tile::wave_col();
-    // 32 items x 32 elements at a time through the wave's LDS, as in default_dz_kernel
-    constexpr int kPieces = 32 * (int)sizeof(T) / 16;
+    const long long item0 = a.first_item + (long long)tile * ITEMS + Tile::wave_col();
+    const int left = left_of(a.N - item0, 32 * Tile::NI), col0 = ct * COLS + Tile::wave_row();
     unsigned char* own = Tile::own_memory();
+    constexpr int kOf = kBlocks<T, Tile::MI>;
 #pragma unroll
-    for (int mi = 0; mi < Tile::MI; ++mi)
+    for (int ni = 0; ni < Tile::NI; ++ni)
 #pragma unroll
-        for (int ni = 0; ni < Tile::NI; ++ni) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int row = 8 * (e / 4) + 4 * (lane / 32) + e % 4, byte = lane % 32 * (int)sizeof(T);
-                const int piece = (byte / 16) ^ (row / (8 / kPieces) % kPieces);
-                *reinterpret_cast<T*>(own + (row * kPieces + piece) * 16 + byte % 16) = (T)(acc[mi][ni][e] * factor);
-            }
-            wave_reads_after_writes();
-#pragma unroll
-            for (int i = 0; i < kPieces / 2; ++i) {
-                const int at = i * kWave + lane, row = at / kPieces, piece = at % kPieces;
-                const uint4 v = *reinterpret_cast<const uint4*>(own + (row * kPieces + (piece ^ (row / (8 / kPieces) % kPieces))) * 16);
-                const int col = col0 + 32 * ni + piece * (16 / (int)sizeof(T));
-                if (32 * mi + row < left && col < a.d)
-                    *reinterpret_cast<uint4*>(static_cast<T*>(a.dW) + (size_t)(item0 + 32 * mi + row) * a.d + col) = v;
-            }
-            wave_reads_after_writes();
-        }
+        for (int mi = 0; mi < Tile::MI; mi += kOf)
+            store_blocks<kOf>(own, [&](int k, int e) { return (T)(acc[mi + k][ni][e] * factor); },
+                              [&](int k, int row, int piece, uint4 v) {
+                                  const int col = col0 + 32 * (mi + k) + piece * (16 / (int)sizeof(T));
+                                  if (32 * ni + row < left && col < a.d)
+                                      *reinterpret_cast<uint4*>(static_cast<T*>(a.dW) + (size_t)(item0 + 32 * ni + row) * a.d + col) = v;
+                              });
 }
 
 template <typename T, int COLS, int ITEMS>

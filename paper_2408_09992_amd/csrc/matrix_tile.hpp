@@ -216,16 +216,17 @@ struct MatrixTile {
     static __device__ __forceinline__ int wave_row() { return wave() / (BN / WN) * WM; }
     static __device__ __forceinline__ int wave_col() { return wave() % (BN / WN) * WN; }
 
-    // Between products: 4 KB of LDS for a wave alone, to lay a 32 x 32 block of its part out in rows (tiles of 256 rows, and of
-    // 64 x 64).
+    // Between products: 4 KB of LDS for a wave alone, to lay blocks of its part out in rows (tiles with a side of 256, and 64 x 64).
     static __device__ __forceinline__ unsigned char* own_memory() {
         if constexpr (BM == 64 && BN == 64) {
             static_assert(kThreads == 4 * kWave, "a stage for each of four waves");
             return wave() < 2 ? (wave() == 0 ? stage_memory<0, A::kBytes>() : stage_memory<1, A::kBytes>())
                               : (wave() == 2 ? stage_memory<3, B::kBytes>() : stage_memory<4, B::kBytes>());
-        } else {
-            static_assert(A::kBytes == 4 * 4096, "four waves' share of a stage");
+        } else if constexpr (BM == 256) {
             return (wave() < 4 ? stage_memory<0, A::kBytes>() : stage_memory<1, A::kBytes>()) + wave() % 4 * 4096;
+        } else {
+            static_assert(BN == 256, "a stage for four waves");
+            return (wave() < 4 ? stage_memory<3, B::kBytes>() : stage_memory<4, B::kBytes>()) + wave() % 4 * 4096;
         }
     }
 
