@@ -543,12 +543,15 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseA
 
 // D: d rounded up to 64, 128, 256 or 512.  A tile holds 16384 / D items.  Bound by memory: W in, dW out, 2.6 GB for 1.27M items
 // of 512 elements in 515 to 550 us, 4.7 to 5.1 TB/s, where a copy reaches 4.73.
-template <typename T, int D>
+// REST: up to 32 positions.  A row of dW is then a sum of so few terms that rounding dz to 16 bits shows beside the row's own
+// rounding (one position, 17,902 items of 64 float16: 4.4e-5 off instead of 2.8e-5); what the rounding leaves is multiplied too,
+// in the place of the other 32 positions.
+template <typename T, int D, bool REST>
 __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a) {
     constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
     using RowsD = Rows<D / 8>;                                 // W and H
     using RowsI = Rows<IT / 8>;                                // dz: [position][item]
-    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2], dz[kFew * IT * 2];
+    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2], dz[kFew * IT * 2], dz_rest[REST ? kFew * IT * 2 : 16];
     __shared__ RowInfo info[kFew];
     __shared__ int target[kFew];
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -599,15 +602,17 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
             const int first = item0 + lane / 16 * 4;
             const long long hit = (long long)target[pos] - (tile * IT + first), left = a.N - (tile * IT + first);
             typedef T T4 __attribute__((ext_vector_type(4)));
-            T4 v;
+            T4 v, rest{};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float p = exp2_fast(fmaf(z[e], kLog2e, -r.at));
                 if (e == hit) p -= kDzScale;
                 if (e >= left) p = 0.0f;
                 v[e] = (T)(p * r.scale);
+                if (REST) rest[e] = (T)fmaf(p, r.scale, -(float)v[e]);
             }
             *reinterpret_cast<T4*>(dz + RowsI::at(pos, first / 8) + first % 8 * 2) = v;
+            if (REST) *reinterpret_cast<T4*>(dz_rest + RowsI::at(pos, first / 8) + first % 8 * 2) = rest;
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
@@ -628,8 +633,12 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
         const int w_item = wave * 2 / (D / 32) * 32, w_col = wave * 2 % (D / 32) * 32;
         f32x16 dw[1][2] = {{f32x16{}, f32x16{}}};
 #pragma unroll
-        for (int k = 0; k < kFew / 16; ++k) {
+        for (int k = 0; k < (REST ? 2 : kFew / 16); ++k) {
             const s16x8 x[1] = {RowsI::across(dz, 16 * k, w_item)}, y[2] = {RowsD::across(h, 16 * k, w_col), RowsD::across(h, 16 * k, w_col + 32)};
+            if constexpr (REST) {
+                const s16x8 rest[1] = {RowsI::across(dz_rest, 16 * k, w_item)};
+                multiply<T, 1, 2>(rest, y, dw);
+            }
             multiply<T, 1, 2>(x, y, dw);
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (nobody reads the tile any more: it is the waves' own memory now)
@@ -753,15 +762,17 @@ hipError_t launch_few_loss(const DensePlan& p, const DenseArgs& a, hipStream_t s
     else hipLaunchKernelGGL((default_few_loss_kernel<T, 64>), grid, threads, 0, st, a);
     return hipGetLastError();
 }
-template <typename T>
-hipError_t launch_few(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+template <typename T, bool REST>
+hipError_t launch_few_of(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
     const dim3 grid(p.slices), threads(kFewThreads);
-    if (a.d > 256) hipLaunchKernelGGL((default_few_kernel<T, 512>), grid, threads, 0, st, a);
-    else if (a.d > 128) hipLaunchKernelGGL((default_few_kernel<T, 256>), grid, threads, 0, st, a);
-    else if (a.d > 64) hipLaunchKernelGGL((default_few_kernel<T, 128>), grid, threads, 0, st, a);
-    else hipLaunchKernelGGL((default_few_kernel<T, 64>), grid, threads, 0, st, a);
+    if (a.d > 256) hipLaunchKernelGGL((default_few_kernel<T, 512, REST>), grid, threads, 0, st, a);
+    else if (a.d > 128) hipLaunchKernelGGL((default_few_kernel<T, 256, REST>), grid, threads, 0, st, a);
+    else if (a.d > 64) hipLaunchKernelGGL((default_few_kernel<T, 128, REST>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((default_few_kernel<T, 64, REST>), grid, threads, 0, st, a);
     return hipGetLastError();
 }
+template <typename T>
+hipError_t launch_few(const DensePlan& p, const DenseArgs& a, hipStream_t st) { return a.B <= 32 ? launch_few_of<T, true>(p, a, st) : launch_few_of<T, false>(p, a, st); }
 
 template <typename T>
 hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
