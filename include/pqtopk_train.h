@@ -18,6 +18,8 @@
  *     its loss is 0 and it adds nothing to any gradient, whatever its query holds (NaN too).  (Its rows of dS are zeros:
  *     Eq. 4's gradients, which know of no targets, multiply these with its query, so there it has to be finite.)
  *   - grad_loss is float [B], the gradient of the final objective with respect to loss_q (1 / count for a mean).
+ *   - Scores are float32 numbers of magnitude below 5.8e6 (2^23 ln 2; probabilities of larger ones would be rounding alone): those
+ *     below count as -inf (also a mask of some other large number, -1e30 say), those above as +inf.
  *   - Softmax statistics and all sums are held in 32 bits or more.  Every result is the same from run to run: no sum
  *     depends on the order in which workgroups or waves finish.
  *   - workspace: at least the bytes that the call's _workspace_bytes function names, 16-byte aligned; contents on entry

@@ -133,7 +133,7 @@ __device__ __forceinline__ void fill_tables(float* table, const float* S, int q0
 __device__ __forceinline__ void finish_position(float c, float s, const void* codes, int code_bytes, const float* S, const int* targets,
                                                 long long N, int m, int b, int q, float* loss, float* lse) {
     const int lane = threadIdx.x % kWave, t = targets[q];
-    const float l = (c == -__builtin_inff() && s == 0.0f) ? c : (c + __log2f(s)) * kLn2;
+    const float l = log_sum(c, s);
     const bool has = t >= 0 && t < N && l != -__builtin_inff();
     float z = 0.0f;
     if (has) {
@@ -183,7 +183,7 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_kernel(LossArgs a) {
     const uint32_t lo = blockIdx.x * a.share, hi = (uint32_t)min((long long)lo + a.share, a.N);
     float c[Q], s[Q];
 #pragma unroll
-    for (int r = 0; r < Q; ++r) { c[r] = -__builtin_inff(); s[r] = 0.0f; }
+    for (int r = 0; r < Q; ++r) { c[r] = kLowest; s[r] = 0.0f; }
 
     auto step = [&](const Row<M, CT> (&row)[kUnits], uint32_t first, auto whole) {
         float z[kUnits][Q];
@@ -208,15 +208,13 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_kernel(LossArgs a) {
         if (__any(rise)) {
 #pragma unroll
             for (int r = 0; r < Q; ++r) {
-                if (top[r] > c[r] + kHeadroom) { s[r] *= exp2_fast(c[r] - top[r]); c[r] = top[r]; }
+                if (top[r] > c[r] + kHeadroom) raise_reference(c[r], s[r], top[r]);
             }
         }
 #pragma unroll
-        for (int r = 0; r < Q; ++r) {
-            const float at = c[r] == -__builtin_inff() ? 0.0f : c[r];
+        for (int r = 0; r < Q; ++r)
 #pragma unroll
-            for (int u = 0; u < kUnits; ++u) s[r] += exp2_fast(fmaf(z[u][r], kLog2e, -at));
-        }
+            for (int u = 0; u < kUnits; ++u) s[r] += exp2_fast(fmaf(z[u][r], kLog2e, -c[r]));
     };
 
     Row<M, CT> row[kUnits];
@@ -259,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_kernel(LossArgs a) {
 // One wave per position joins the shares' sums: 4 us, a launch.
 __global__ __launch_bounds__(kWave) void cross_entropy_join_kernel(LossArgs a, int shares, int code_bytes) {
     const int q = blockIdx.x, lane = threadIdx.x;
-    float c = -__builtin_inff(), s = 0.0f;
+    float c = kLowest, s = 0.0f;
     for (int i = lane; i < shares; i += kWave) {
         const float2 t = a.partial[(size_t)i * a.B + q];
         join_sums(c, s, t.x, t.y);

@@ -107,7 +107,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     const int lane = threadIdx.x % kWave;
     float c[NI], s[NI];
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) { c[ni] = -__builtin_inff(); s[ni] = 0.0f; }
+    for (int ni = 0; ni < NI; ++ni) { c[ni] = kLowest; s[ni] = 0.0f; }
     for (int i = 0; i < a.tiles_each; ++i) {
         const long long tile = (long long)group * a.tiles_each + i;
         if (tile >= a.item_tiles) break;
@@ -132,14 +132,13 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
                 for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[mi][ni][e]);
             top *= kLog2e;
             if (__any(top > c[ni] + kHeadroom)) {
-                if (top > c[ni] + kHeadroom) { s[ni] *= exp2_fast(c[ni] - top); c[ni] = top; }
+                if (top > c[ni] + kHeadroom) raise_reference(c[ni], s[ni], top);
             }
-            const float at = c[ni] == -__builtin_inff() ? 0.0f : c[ni];
             float sum = 0.0f;
 #pragma unroll
             for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum += exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -at));
+                for (int e = 0; e < 16; ++e) sum += exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -c[ni]));
             s[ni] += sum;
         }
     }
@@ -163,7 +162,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
 template <typename T>
 __global__ __launch_bounds__(kWave) void default_cross_entropy_join_kernel(DenseArgs a) {
     const int q = blockIdx.x, lane = threadIdx.x;
-    float c = -__builtin_inff(), s = 0.0f;
+    float c = kLowest, s = 0.0f;
     for (int i = lane; i < a.groups; i += kWave) {
         const float2 t = a.partial[(size_t)i * a.B + q];
         join_sums(c, s, t.x, t.y);
@@ -173,7 +172,7 @@ __global__ __launch_bounds__(kWave) void default_cross_entropy_join_kernel(Dense
         const float c2 = __shfl_xor(c, x), s2 = __shfl_xor(s, x);
         join_sums(c, s, c2, s2);
     }
-    const float lse = (c + __log2f(s)) * kLn2;
+    const float lse = log_sum(c, s);
     const int t = a.targets[q];
     float z = 0.0f;
     const bool has = t >= 0 && t < a.N;
@@ -491,7 +490,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseA
     bring_rows<T, D, kLoadsW>(a.W, a.d, (long long)blockIdx.x * IT, a.N, w0);
     float c[kParts], s[kParts];
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) { c[i] = -__builtin_inff(); s[i] = 0.0f; }
+    for (int i = 0; i < kParts; ++i) { c[i] = kLowest; s[i] = 0.0f; }
     int turn = 0;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
         const unsigned char* w = turn % 2 ? w1 : w0;
@@ -513,15 +512,14 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseA
             const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) * kLog2e;
             const int part = i % kParts;
             if (__any(top > c[part] + kHeadroom)) {
-                if (top > c[part] + kHeadroom) { s[part] *= exp2_fast(c[part] - top); c[part] = top; }
+                if (top > c[part] + kHeadroom) raise_reference(c[part], s[part], top);
             }
-            const float at = c[part] == -__builtin_inff() ? 0.0f : c[part];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[part] += exp2_fast(fmaf(z[e], kLog2e, -at));
+            for (int e = 0; e < 4; ++e) s[part] += exp2_fast(fmaf(z[e], kLog2e, -c[part]));
         }
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");                  // (a last load into LDS may be under way)
-    for (int q = lane; q < kFew; q += kWave) stat[wave][q] = make_float2(-__builtin_inff(), 0.0f);
+    for (int q = lane; q < kFew; q += kWave) stat[wave][q] = make_float2(kLowest, 0.0f);
     wave_reads_after_writes();
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {

@@ -28,12 +28,24 @@ __device__ __forceinline__ void wave_reads_after_writes() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// A sum of exponentials held as scale and mantissa: total = s * 2^c.  c = -inf: nothing yet (s = 0).
+// A sum of exponentials held as reference and mantissa: total = s * 2^c.  The reference is kept within +-2^23, where float32 resolves
+// a half: 2^(x log2e - c) is the exact product's distance from it, so with a rounded reference far outside (a mask of -1e30) the terms
+// would be 2 to the power of that rounding, inf or 0.  Scores below the range so count as -inf, those above it as +inf.
+constexpr float kLowest = -8388608.0f, kHighest = 8388608.0f;
 __device__ __forceinline__ void join_sums(float& c, float& s, float c2, float s2) {
     const float top = fmaxf(c, c2);
-    const float at = top == -__builtin_inff() ? 0.0f : top;
-    s = s * exp2_fast(c - at) + s2 * exp2_fast(c2 - at);
+    s = s * exp2_fast(c - top) + s2 * exp2_fast(c2 - top);
     c = top;
+}
+// The reference moves up to `top`, the largest of the next scores (base 2; +inf too), where these pass it by more than there is room for.
+__device__ __forceinline__ void raise_reference(float& c, float& s, float top) {
+    const float to = fminf(top, kHighest);
+    s *= exp2_fast(c - to);
+    c = to;
+}
+// log-sum: -inf where no score counts, NaN where one is NaN, +inf or counts as that.
+__device__ __forceinline__ float log_sum(float c, float s) {
+    return s == 0.0f ? -__builtin_inff() : s < __builtin_inff() ? (c + __log2f(s)) * kLn2 : __builtin_nanf("");
 }
 
 template <typename F>

@@ -144,6 +144,59 @@ def test_sub_ids_out_of_play(pq, wide):
     assert np.isinf(loss[2]) and np.isfinite(dS[2]).all() and np.isfinite(dS[4]).all()
 
 
+LOWEST = float(np.finfo(np.float32).min)
+
+
+@pytest.mark.parametrize("mask", [-1e7, -1e9, -1e10, -1e12, -1e20, -1e30, -1e38, LOWEST])
+@pytest.mark.parametrize("m,B,wide", [(8, 1, False), (4, 2, True), (8, 6, False), (3, 5, True), (64, 2, False)])
+def test_masks_of_large_finite_numbers(pq, mask, m, B, wide):
+    # a score far below any other's counts as -inf, whether a lane meets it before or after the scores that are in play
+    codes, S, targets, grad = draw(9000, m, 200, B, seed=m + B, wide=wide)
+    codes[:3000, 1] = codes[:3000, 1] // 2
+    codes[3000:, 1] = np.where(np.arange(6000) % 3 == 0, codes[3000:, 1] // 2, 100 + codes[3000:, 1] // 2)
+    targets[:] = 5000 + 3 * np.arange(B) + 2
+    masked, out = S.copy(), S.copy()
+    masked[:, 1, :100], out[:, 1, :100] = mask, -np.inf
+    if B > 1:
+        masked[1, 0, :], out[1, 0, :] = mask, -np.inf            # nothing is left
+    got, want = run(pq, codes, masked, targets, grad), check(pq, codes, out, targets, grad)
+    for a, b in zip(got, want):
+        assert np.array_equal(a, b)
+    if B > 1:
+        assert got[1][1] == -np.inf and got[0][1] == 0.0 and not got[2][1].any()
+
+
+@pytest.mark.parametrize("top", [1e7, 1e9, 1e10, 1e12, 1e20, 1e30, -LOWEST])
+def test_scores_too_large_for_a_loss(pq, top):
+    # float32 scores of that size are whole multiples of a half or more: what they would make of a probability is NaN
+    codes, S, targets, grad = draw(5000, 4, 256, 5, seed=12)
+    want = run(pq, codes, S, targets, grad)
+    S[1, 2, codes[77, 2]] = top
+    S[3, 0, :] = top
+    loss, lse, dS = run(pq, codes, S, targets, grad)
+    rest = [0, 2, 4]
+    assert np.isnan(lse[[1, 3]]).all() and np.isnan(loss[[1, 3]]).all() and np.isnan(dS[[1, 3]]).all()
+    assert np.array_equal(loss[rest], want[0][rest]) and np.array_equal(lse[rest], want[1][rest]) and np.array_equal(dS[rest], want[2][rest])
+
+
+@pytest.mark.parametrize("offset", [-4e6, -3e5, 3e5, 4e6])
+def test_large_scores_leave_a_gradient(pq, offset):
+    # the log-sum is a float32 of that size: probabilities are off by what its rounding is, and no sum of them wraps around
+    codes, S, targets, grad = draw(6007, 8, 256, 5, seed=13)
+    S = S + np.float32(offset / 8)
+    loss, lse, dS = run(pq, codes, S, targets, np.ones_like(grad))
+    _, want_lse, _, _, _ = reference(codes, S, targets, np.ones_like(grad))
+    unit = float(np.spacing(np.float32(abs(offset))))
+    # m roundings of a score's partial sums; the reference's, log-sum's and its product's
+    assert np.all(np.abs(lse - want_lse) <= 8 * unit / 2 + 3 * unit)
+    for q in range(5):
+        sums = dS[q].astype(np.float64)
+        sums[np.arange(8), codes[targets[q]]] += 1.0
+        sums = sums.sum(1)
+        # log-sum, its product with log2 e and the exponent's sum are each rounded by up to a quarter (base 2) at the largest of these
+        assert np.all(np.abs(np.log2(sums)) <= 3 * unit * np.log2(np.e)) and np.ptp(sums) <= 1e-5
+
+
 @pytest.mark.parametrize("m,b,wide", [(8, 256, False), (3, 100, False), (4, 1000, True)])
 def test_scores_that_are_no_numbers(pq, m, b, wide):
     # positions 1 and 4 meet a NaN, 3 an infinity; 4 has no target

@@ -137,6 +137,37 @@ def test_scores_far_apart(pq, type, spread):
     check(pq, *draw(2000, 64, 20, type, seed=4, spread=spread), type)
 
 
+@pytest.mark.parametrize("type,mask", [(t, x) for t in ("f32", "bf16", "f16") for x in (-3e4, -1e10, -1e20, -1e30, -1e38) if t != "f16" or x == -3e4])
+@pytest.mark.parametrize("N,d,B", [(5000, 64, 40), (2500, 520, 20), (5000, 64, 300), (70_000, 64, 300)])
+def test_items_far_below_any_other(pq, N, d, B, type, mask):
+    # an element that is 1 in every query (float16: 30000) takes items out of play, in front of others and between them
+    W, H, targets, grad = draw(N, d, B, type, seed=N + d + B)
+    H[:, 0], W[:, 0] = (30_000.0 if type == "f16" else 1e4 if mask == -3e4 else 1.0), 0.0
+    masked = torch.zeros(N, dtype=torch.bool, device="cuda")
+    masked[:N // 3] = True
+    masked[N // 2::3] = True
+    targets[:] = N // 2 + 1
+    targets[1::2] = N // 3 + torch.arange(targets[1::2].numel(), device="cuda", dtype=torch.int32)
+    live = torch.nonzero(~masked).view(-1)
+    only = W[live].contiguous()
+    W[masked, 0] = mask
+    among = (torch.cumsum(~masked, 0) - 1)[targets.long()].int()
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+    assert not dW[masked].any()
+    if type != "f16":                                          # (float16: many targets times 30000 is no float16 any more)
+        check(pq, only, H, among, grad, type)
+    loss2, lse2 = pq.pq_default_cross_entropy(only, H, among)
+    dH2, dW2 = pq.pq_default_cross_entropy_backward(only, H, among, lse2, grad)
+    # the same sums in other lanes: some hundred units of a log-sum of about 10, of what makes a gradient besides its type's own
+    assert ((lse - lse2).abs() <= 200 * U * 10).all() and ((loss - loss2).abs() <= 200 * U * 20).all()
+    unit = TYPES[type][1]
+    size = grad.abs()[:, None] * 2 * only[:, 1:].float().abs().max()
+    assert ((dH - dH2)[:, 1:].float().abs() <= (6 * unit + 4000 * U) * size).all()
+    size = (grad.abs()[:, None] * H[:, 1:].float().abs()).sum(0).max()
+    assert ((dW[live] - dW2)[:, 1:].float().abs() <= (6 * unit + 4000 * U) * size).all()
+
+
 def test_gradients_of_very_different_size(pq):
     W, H, targets, grad = draw(2000, 64, 80, "f16", seed=5)
     grad *= torch.logspace(-6, 6, 80, device="cuda")
