@@ -19,7 +19,8 @@
  *     Eq. 4's gradients, which know of no targets, multiply these with its query, so there it has to be finite.)
  *   - grad_loss is float [B], the gradient of the final objective with respect to loss_q (1 / count for a mean).
  *   - Scores are float32 numbers of magnitude below 5.8e6 (2^23 ln 2; probabilities of larger ones would be rounding alone): those
- *     below count as -inf (also a mask of some other large number, -1e30 say), those above as +inf.
+ *     below count as -inf (also a mask of some other large number, -1e30 say), those above as +inf.  A position all of whose
+ *     scores are -inf has lse = -inf, loss 0 and no gradient.
  *   - Softmax statistics and all sums are held in 32 bits or more.  Every result is the same from run to run: no sum
  *     depends on the order in which workgroups or waves finish.
  *   - workspace: at least the bytes that the call's _workspace_bytes function names, 16-byte aligned; contents on entry
@@ -39,8 +40,8 @@ extern "C" {
  * Loss and log-sum of B positions by sub-ids: r_qi = sum_k S[q][k][codes[i][k]].
  *   codes    in   uint8 [N][m]     codebook G (Eq. 1), sub-ids < b (16-byte aligned);  uint16 [N][m] for the _u16 call
  *   S        in   float [B][m][b]  from pq_subitem_scores().  Entries may be -inf (a sub-id out of play: its items have
- *                                  probability 0); a position for which nothing is left has lse = -inf, loss 0, no gradient;
- *                                  one that meets a NaN or +inf has lse, loss and gradient NaN, and no other position has
+ *                                  probability 0); a position that meets a NaN or +inf has lse, loss and gradient NaN, and no other
+ *                                  position has
  *   targets  in   int32 [B]
  *   loss     out  float [B];  lse  out  float [B]
  * b <= 256 for one-byte sub-ids, <= 65536 for two bytes.  A sub-id >= b makes the result unspecified; nothing outside the

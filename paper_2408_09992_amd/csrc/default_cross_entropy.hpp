@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kWave) void default_cross_entropy_join_kernel(Dense
     const float lse = log_sum(c, s);
     const int t = a.targets[q];
     float z = 0.0f;
-    const bool has = t >= 0 && t < a.N;
+    const bool has = t >= 0 && t < a.N && lse != -__builtin_inff();
     if (has) {
         const T *w = static_cast<const T*>(a.W) + (size_t)t * a.d, *h = static_cast<const T*>(a.H) + (size_t)q * a.d;
         for (int e = lane; e < a.d; e += kWave) z = fmaf((float)w[e], (float)h[e], z);
@@ -198,10 +198,10 @@ __device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
     return g != 0.0f ? RowInfo{lse * kLog2e - kDzBits, g / top} : RowInfo{__builtin_inff(), 0.0f};
 }
 
-// A position's share of the gradient: 0 where there is none, no target or no position.
+// A position's share of the gradient: 0 where there is none, no target, no item in play or no position.
 __device__ __forceinline__ float row_weight(const DenseArgs& a, int q) {
     const int t = q < a.B ? a.targets[q] : -1;
-    return t >= 0 && t < a.N ? a.grad[q] : 0.0f;
+    return t >= 0 && t < a.N && a.lse_in[q] != -__builtin_inff() ? a.grad[q] : 0.0f;
 }
 // The queries in pieces of 16 bytes, from piece `first` on every `stride`-th, with zeros for positions that add nothing.
 template <typename T>

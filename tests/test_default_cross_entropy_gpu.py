@@ -168,6 +168,26 @@ def test_items_far_below_any_other(pq, N, d, B, type, mask):
     assert ((dW[live] - dW2)[:, 1:].float().abs() <= (6 * unit + 4000 * U) * size).all()
 
 
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("N,d,B", [(3000, 64, 20), (3000, 64, 50), (700, 520, 20), (700, 520, 50), (1500, 128, 300)])
+def test_positions_for_which_nothing_is_left(pq, N, d, B, type):
+    # as in the loss by sub-ids: log-sum -inf, loss 0, no gradient
+    W, H, targets, grad = draw(N, d, B, type, seed=N + B)
+    W[:, 0], H[:, 0] = -30_000.0, 0.0
+    H[::3, 0], H[::3, 1:] = 60_000.0, 0.0
+    targets[1] = -1
+    rest = torch.ones(B, dtype=torch.bool, device="cuda")
+    rest[::3] = False
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+    assert (lse[::3] == -float("inf")).all() and not loss[::3].any() and not dH[::3].any()
+    targets[::3] = -1
+    loss2, lse2 = pq.pq_default_cross_entropy(W, H, targets)
+    dH2, dW2 = pq.pq_default_cross_entropy_backward(W, H, targets, lse2, grad)
+    assert torch.isfinite(lse2[rest]).all() and torch.isfinite(dW).all()
+    assert torch.equal(loss, loss2) and torch.equal(lse[rest], lse2[rest]) and torch.equal(dH, dH2) and torch.equal(dW, dW2)
+
+
 def test_gradients_of_very_different_size(pq):
     W, H, targets, grad = draw(2000, 64, 80, "f16", seed=5)
     grad *= torch.logspace(-6, 6, 80, device="cuda")
