@@ -51,6 +51,7 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
         p.positions = 64; p.position_tiles = (int)ceil_div(B, 64); p.tiles_each = 1; p.groups = (int)p.item_tiles;
     }
     // gradient: pieces of the items, in balance
+    p.parts = size == 2 && B <= kTwoParts ? 2 : 1;
     const int small = B <= 64 ? 64 : 128;              // (positions are padded to a multiple of this or of 256)
     long long piece = (size == 2 && d <= 64 ? kDzBytesShort : kDzBytes) / size / (long long)round_up(B, small);
     if (piece < 2048) piece = 2048;
@@ -96,9 +97,9 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
     }
     p.info_at = 256;
     p.live_at = round_up(p.info_at + (size_t)p.padded * sizeof(RowInfo), 256);
-    p.dz_at = round_up(p.live_at + (size_t)B * d * size, 256);
+    p.dz_at = round_up(p.live_at + (size_t)B * p.parts * d * size, 256);
     p.partial_at = round_up(p.dz_at + (size_t)p.padded * p.piece * size, 256);
-    p.bytes = round_up(p.partial_at + (size_t)p.slices * B * d * sizeof(float), 256);
+    p.bytes = round_up(p.partial_at + (size_t)p.slices * B * p.parts * d * sizeof(float), 256);
     return p;
 }
 
@@ -168,7 +169,7 @@ int pq_default_cross_entropy_backward(const void* W, const void* queries, const 
     a.live = ws + p.live_at;
     a.dz = ws + p.dz_at;
     a.partial_h = reinterpret_cast<float*>(ws + p.partial_at);
-    a.piece = p.piece; a.padded = p.padded; a.slices = p.slices;
+    a.parts = p.parts; a.piece = p.piece; a.padded = p.padded; a.slices = p.slices;
     hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e;
     if (type == PQ_FLOAT32) e = dense_backward<float>(p, a, st);

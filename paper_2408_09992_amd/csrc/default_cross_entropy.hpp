@@ -70,15 +70,16 @@ struct DenseArgs {
     float *loss, *lse;
     // gradient
     const float *lse_in, *grad;
-    RowInfo* info;                                     // [positions, padded]
-    void* live;                                        // [B][d]: the queries, zeros where a position adds nothing
+    int parts;                                         // rows of dz that a position has (see dz_rows)
+    RowInfo* info;                                     // [rows of dz, padded]
+    void* live;                                        // [rows of dz][d]: the queries, zeros where a position adds nothing
     float* factor;                                     // what the products are multiplied with
-    void* dz;                                          // [tiles of a piece][positions, padded][kItems]
-    float* partial_h;                                  // [slices][B][d]
+    void* dz;                                          // [tiles of a piece][rows of dz, padded][kItems]
+    float* partial_h;                                  // [slices][rows of dz][d]
     void *dH, *dW;
     long long first_item;                              // of the piece
     int piece, items;                                  // padded and actual items of it
-    int padded, slices, slice_items, more;             // positions padded; shares of a piece's items; partial_h holds earlier pieces
+    int padded, slices, slice_items, more;             // rows of dz padded; shares of a piece's items; partial_h holds earlier pieces
     int tiles_m, tiles_n;                              // of the launch
     int h_rows, h_cols, w_blocks;                      // tiles of dH; workgroups that make dW, where one launch makes both
 };
@@ -91,6 +92,14 @@ template <typename T>
 __device__ __forceinline__ Operand positions_of(const DenseArgs& a, int position) {
     return Operand{a.H, (size_t)a.d * sizeof(T), position, a.B, 0, a.d};
 }
+
+// dz in 16 bits has two rows a position where there are up to 32 positions, B rounded values and then B of what their rounding
+// leaves.  A row of dqueries is then (and a row of dW may be) little more than one value of dz times one row, whose error that
+// rounding would double (one position, 17,902 items of 64 float16: dW 4.4e-5 off instead of 2.8e-5).  Tiles have 64 rows anyway.  With more
+// positions the errors of their rows are independent: together with the result's own rounding at most sqrt(2) of it in the mean square.
+constexpr int kTwoParts = 32;
+__device__ __forceinline__ int dz_rows(const DenseArgs& a) { return a.B * a.parts; }
+__device__ __forceinline__ int position_of(const DenseArgs& a, int row) { return row < a.B ? row : row - a.B; }
 
 // Statistics of a tile of positions over a group of item tiles, one after the other.  As in the loss by sub-ids a lane's
 // reference c moves only when a score passes it by 2^kHeadroom; lanes, halves and waves join once, at the end.
@@ -198,18 +207,18 @@ __device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
     return g != 0.0f ? RowInfo{lse * kLog2e - kDzBits, g / top} : RowInfo{__builtin_inff(), 0.0f};
 }
 
-// A position's share of the gradient: 0 where there is none, no target, no item in play or no position.
-__device__ __forceinline__ float row_weight(const DenseArgs& a, int q) {
-    const int t = q < a.B ? a.targets[q] : -1;
+// The share of the gradient of a row's position: 0 where there is none, no target, no item in play or no position.
+__device__ __forceinline__ float row_weight(const DenseArgs& a, int row) {
+    const int q = position_of(a, row), t = row < dz_rows(a) ? a.targets[q] : -1;
     return t >= 0 && t < a.N && a.lse_in[q] != -__builtin_inff() ? a.grad[q] : 0.0f;
 }
 // The queries in pieces of 16 bytes, from piece `first` on every `stride`-th, with zeros for positions that add nothing.
 template <typename T>
 __device__ __forceinline__ void copy_live(const DenseArgs& a, size_t first, size_t stride) {
     const int row_pieces = a.d * (int)sizeof(T) / 16;
-    const size_t pieces = (size_t)a.B * row_pieces;
+    const size_t pieces = (size_t)dz_rows(a) * row_pieces, position_pieces = (size_t)a.B * row_pieces;
     for (size_t i = first; i < pieces; i += stride) {
-        const uint4 v = static_cast<const uint4*>(a.H)[i];
+        const uint4 v = static_cast<const uint4*>(a.H)[i < position_pieces ? i : i - position_pieces];
         static_cast<uint4*>(a.live)[i] = row_weight(a, (int)(i / row_pieces)) != 0.0f ? v : uint4{0, 0, 0, 0};
     }
 }
@@ -270,23 +279,24 @@ __device__ __forceinline__ void store_blocks(unsigned char* own, Value value, Pu
 
 // dz of a piece of items: scores as in the loss, then (exp(z - lse) - [target]) g as the products' operands, position by
 // position.  For 16-bit operands dz is rounded to their type: it is the products' input as H and W are, and what they add up
-// (in float32) is rounded to that type once more at the end.
+// (in float32) is rounded to that type once more at the end (up to 32 positions keep what the first rounding leaves: kTwoParts).
 // 131,072 items, 1024 positions of 512 bfloat16: 179 to 187 us, 750 TFLOP/s, and 268 MB written.
-// ROWS: up to 64 positions, whose rows (see default_rows_kernel) the workgroups make themselves.
+// ROWS: up to 64 rows of dz, whose info (see default_rows_kernel) the workgroups make themselves.
 template <typename T, int BN, int ITEMS, bool ROWS>
 __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_dz_kernel(DenseArgs a) {
     using Tile = ScoresTile<T, BN, ITEMS>;
     constexpr int MI = Tile::MI, NI = Tile::NI;
-    static_assert(!ROWS || BN == kWave, "a position is a lane");
+    static_assert(!ROWS || BN == kWave, "a row is a lane");
+    constexpr bool kParts = ROWS && sizeof(T) == 2;            // (whether there may be two a position)
     int tile, pt;
     chiplet_order(blockIdx.x, a.tiles_n, tile, pt);
     if (tile >= a.tiles_m) return;
     const int lane = threadIdx.x % kWave;
     RowInfo own_row{};
-    if constexpr (ROWS) {                                      // (every wave: lane q has position q's)
+    if constexpr (ROWS) {                                      // (every wave: lane r has row r's)
         const float g = row_weight(a, lane);
         const float top = wave_top(fabsf(g));
-        own_row = row_info(g, top, a.lse_in[min(lane, a.B - 1)]);
+        own_row = row_info(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
         if (!a.more) {
             copy_live<T>(a, (size_t)tile * Tile::kThreads + threadIdx.x, (size_t)a.tiles_m * Tile::kThreads);
             if (tile == 0 && threadIdx.x == 0) *a.factor = top / kDzScale;
@@ -294,7 +304,9 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     }
     const long long item0 = a.first_item + (long long)tile * ITEMS;
     f32x16 acc[MI][NI];
-    Tile::run(items_of<T>(a, item0), positions_of<T>(a, pt * BN), acc);
+    Operand positions = positions_of<T>(a, pt * BN);
+    if constexpr (kParts) positions.again = a.parts > 1 ? a.B : 0;
+    Tile::run(items_of<T>(a, item0), positions, acc);
     const int left = left_of(a.N - item0 - Tile::wave_row(), 32 * MI) - 4 * (lane / 32);
     unsigned char* own = Tile::own_memory();
 #pragma unroll
@@ -303,7 +315,8 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
         RowInfo info;
         if constexpr (ROWS) info = RowInfo{__shfl(own_row.at, q0 + lane % 32), __shfl(own_row.scale, q0 + lane % 32)};
         else info = a.info[q];
-        const long long from_first = (q < a.B ? (long long)a.targets[q] : -1) - item0 - Tile::wave_row();
+        const bool rest = kParts && q >= a.B;
+        const long long from_first = (q < (kParts ? dz_rows(a) : a.B) ? (long long)a.targets[rest ? q - a.B : q] : -1) - item0 - Tile::wave_row();
         const int hit = from_first >= 0 && from_first < 32 * MI ? (int)from_first - 4 * (lane / 32) : -64;
         const bool special = __any(hit > -64) || left < 32 * MI - 4;           // (rare: a target among these items, the catalogue's end)
 #pragma unroll
@@ -324,6 +337,19 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
                     if (at >= left) acc[mi][ni][e] = 0.0f;
                 }
         }
+        if constexpr (kParts) {
+            if (a.parts > 1) {
+                stay_a_branch();
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float x = acc[mi][ni][e] * info.scale;
+                        acc[mi][ni][e] = rest ? fmaf(acc[mi][ni][e], info.scale, -(float)(T)x) : x;
+                    }
+                info.scale = 1.0f;
+            }
+        }
         T* out = static_cast<T*>(a.dz) + ((size_t)(tile / (kItems / ITEMS)) * a.padded + q0) * kItems + tile % (kItems / ITEMS) * ITEMS + Tile::wave_row();
 #pragma unroll
         for (int mi = 0; mi < MI; mi += kBlocks<T, MI>)
@@ -334,7 +360,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     }
 }
 
-// A tile of dW of a piece: [items][d], summed over the positions.  As many: 133 to 145 us, about 1000 TFLOP/s.
+// A tile of dW of a piece: [items][d], summed over dz's rows.  As many: 133 to 145 us, about 1000 TFLOP/s.
 template <typename T, int COLS, int ITEMS>
 __device__ __forceinline__ void dw_tile(const DenseArgs& a, int block) {
     using Tile = TileW<T, COLS, ITEMS>;
@@ -343,7 +369,7 @@ __device__ __forceinline__ void dw_tile(const DenseArgs& a, int block) {
     if (tile >= a.tiles_m) return;
     f32x16 acc[Tile::MI][Tile::NI];
     const Operand dz{static_cast<const T*>(a.dz) + (size_t)(tile / (kItems / ITEMS)) * a.padded * kItems, kItems * sizeof(T), tile % (kItems / ITEMS) * ITEMS, kItems, 0, a.padded};
-    const Operand h{a.H, (size_t)a.d * sizeof(T), (long long)ct * COLS, a.d, 0, a.B};
+    const Operand h{a.H, (size_t)a.d * sizeof(T), (long long)ct * COLS, a.d, 0, dz_rows(a)};
     Tile::run(h, dz, acc);                             // (elements by items: a lane has four neighbouring elements of an item)
     const float factor = *a.factor;
     const long long item0 = a.first_item + (long long)tile * ITEMS + Tile::wave_col();
@@ -365,7 +391,7 @@ __device__ __forceinline__ void dw_tile(const DenseArgs& a, int block) {
 template <typename T, int COLS, int ITEMS>
 __global__ __launch_bounds__((TileW<T, COLS, ITEMS>::kThreads), 2) void default_dw_kernel(DenseArgs a) { dw_tile<T, COLS, ITEMS>(a, blockIdx.x); }
 
-// A slice's share of a tile of dH: [positions][d] summed over its items of the piece, added to what earlier pieces left there.
+// A slice's share of a tile of dH: [rows of dz][d] summed over its items of the piece, added to what earlier pieces left there.
 // As many: 139 to 145 us, about 960 TFLOP/s.
 template <typename T, int BM, int BN>
 __device__ __forceinline__ void dh_tile(const DenseArgs& a, int block) {
@@ -388,8 +414,8 @@ __device__ __forceinline__ void dh_tile(const DenseArgs& a, int block) {
 #pragma unroll
             for (int ni = 0; ni < Tile::NI; ++ni) acc[mi][ni] = f32x16{};
     }
-    const int q0 = rt * BM + Tile::wave_row(), left = left_of(a.B - q0, 32 * Tile::MI) - 4 * (lane / 32);
-    float* out = a.partial_h + ((size_t)slice * a.B + q0 + 4 * (lane / 32)) * a.d;
+    const int rows = dz_rows(a), q0 = rt * BM + Tile::wave_row(), left = left_of(rows - q0, 32 * Tile::MI) - 4 * (lane / 32);
+    float* out = a.partial_h + ((size_t)slice * rows + q0 + 4 * (lane / 32)) * a.d;
     auto put = [&](auto whole_c) {
         constexpr bool whole = decltype(whole_c)::value;
 #pragma unroll
@@ -411,7 +437,7 @@ __device__ __forceinline__ void dh_tile(const DenseArgs& a, int block) {
                     if (col < a.d && (whole || row(e) < left)) p[(size_t)(row(e) - 32 * mi) * a.d] = old[e] + acc[mi][ni][e];
             }
     };
-    if (a.B - q0 >= 32 * Tile::MI) put(std::true_type{});
+    if (rows - q0 >= 32 * Tile::MI) put(std::true_type{});
     else put(std::false_type{});
 }
 template <typename T, int BM, int BN>
@@ -458,10 +484,10 @@ __device__ __forceinline__ f32x4_t multiply16(s16x8 x, s16x8 y, f32x4_t c) {
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
 }
 
-// Rows of W or of the queries from `row0` on into LDS: LOADS 16-byte pieces a thread; past the last row the last one again,
-// past a row's end zeros.
+// Rows of W or of the queries from `row0` on into LDS: LOADS 16-byte pieces a thread; past the last row the last one again
+// (from the again-th, if not 0, the first ones), past a row's end zeros.
 template <typename T, int D, int LOADS>
-__device__ __forceinline__ void bring_rows(const void* base, int d, long long row0, long long rows, unsigned char* to) {
+__device__ __forceinline__ void bring_rows(const void* base, int d, long long row0, long long rows, unsigned char* to, int again = 0) {
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const size_t ld = (size_t)d * sizeof(T);
     const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + (size_t)row0 * ld, 0, kBufferBytes, 0x00020000);
@@ -469,7 +495,7 @@ __device__ __forceinline__ void bring_rows(const void* base, int d, long long ro
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
         const int piece = (wave * LOADS + i) * kWave + lane, row = piece / (D / 8), chunk = (piece % (D / 8)) ^ Rows<D / 8>::turn(row);
-        const uint32_t offset = chunk * 8 < d ? (uint32_t)min(row, last) * (uint32_t)ld + (uint32_t)chunk * 16u : kPastEnd;
+        const uint32_t offset = chunk * 8 < d ? (uint32_t)min(again && row >= again ? row - again : row, last) * (uint32_t)ld + (uint32_t)chunk * 16u : kPastEnd;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)(to + (wave * LOADS + i) * kWave * 16), 16, offset, 0, 0, 0);
     }
 }
@@ -541,40 +567,38 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseA
 
 // D: d rounded up to 64, 128, 256 or 512.  A tile holds 16384 / D items.  Bound by memory: W in, dW out, 2.6 GB for 1.27M items
 // of 512 elements in 515 to 550 us, 4.7 to 5.1 TB/s, where a copy reaches 4.73.
-// REST: up to 32 positions.  A row of dW is then a sum of so few terms that rounding dz to 16 bits shows beside the row's own
-// rounding (one position, 17,902 items of 64 float16: 4.4e-5 off instead of 2.8e-5); what the rounding leaves is multiplied too,
-// in the place of the other 32 positions.
-template <typename T, int D, bool REST>
+// PARTS: two rows of dz a position (kTwoParts), in the place of the other 32 positions.
+template <typename T, int D, bool PARTS>
 __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a) {
     constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
     using RowsD = Rows<D / 8>;                                 // W and H
-    using RowsI = Rows<IT / 8>;                                // dz: [position][item]
-    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2], dz[kFew * IT * 2], dz_rest[REST ? kFew * IT * 2 : 16];
+    using RowsI = Rows<IT / 8>;                                // dz: [row][item]
+    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2], dz[kFew * IT * 2];
     __shared__ RowInfo info[kFew];
     __shared__ int target[kFew];
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const long long tiles = (a.N + IT - 1) / IT;
     constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
-    bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h);
+    bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h, PARTS ? a.B : 0);
     bring_rows<T, D, kLoadsW>(a.W, a.d, (long long)blockIdx.x * IT, a.N, w0);
-    // what default_rows_kernel does for more positions: these are a wave's lanes
+    // what default_rows_kernel does for more positions: these rows are a wave's lanes
     __shared__ float factor_of_all;
     if (wave == 0) {
         const float g = row_weight(a, lane);
         const float top = wave_top(fabsf(g));
-        info[lane] = row_info(g, top, a.lse_in[min(lane, a.B - 1)]);
-        target[lane] = lane < a.B ? a.targets[lane] : -1;
+        info[lane] = row_info(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
+        target[lane] = lane < dz_rows(a) ? a.targets[position_of(a, lane)] : -1;
         if (lane == 0) {
             factor_of_all = top / kDzScale;
             if (blockIdx.x == 0) *a.factor = factor_of_all;
         }
     }
-    // dH: 2 x D / 32 blocks of 32 positions x 32 elements, shared by the waves; D = 64 leaves half of them without one
+    // dH: 2 x D / 32 blocks of 32 rows x 32 elements, shared by the waves; D = 64 leaves half of them without one
     constexpr int kBlocksH = D / 16 >= kWaves ? D / 16 / kWaves : 1;
     f32x16 dh[kBlocksH];
 #pragma unroll
     for (int i = 0; i < kBlocksH; ++i) dh[i] = f32x16{};
-    const int h_pos = wave % 2 * 32, h_col = wave / 2 * kBlocksH * 32;         // (a wave's blocks: one half of the positions)
+    const int h_pos = wave % 2 * 32, h_col = wave / 2 * kBlocksH * 32;         // (a wave's blocks: one half of the rows)
 
     int turn = 0;
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -587,7 +611,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
 
-        // z and dz: blocks of 16 items x 16 positions
+        // z and dz: blocks of 16 items x 16 rows
         constexpr int kBlocksZ = IT / 16 * 4 / kWaves;
 #pragma unroll
         for (int i = 0; i < kBlocksZ; ++i) {
@@ -600,17 +624,16 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
             const int first = item0 + lane / 16 * 4;
             const long long hit = (long long)target[pos] - (tile * IT + first), left = a.N - (tile * IT + first);
             typedef T T4 __attribute__((ext_vector_type(4)));
-            T4 v, rest{};
+            T4 v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float p = exp2_fast(fmaf(z[e], kLog2e, -r.at));
                 if (e == hit) p -= kDzScale;
                 if (e >= left) p = 0.0f;
                 v[e] = (T)(p * r.scale);
-                if (REST) rest[e] = (T)fmaf(p, r.scale, -(float)v[e]);
+                if (PARTS && pos >= a.B) v[e] = (T)fmaf(p, r.scale, -(float)v[e]);
             }
             *reinterpret_cast<T4*>(dz + RowsI::at(pos, first / 8) + first % 8 * 2) = v;
-            if (REST) *reinterpret_cast<T4*>(dz_rest + RowsI::at(pos, first / 8) + first % 8 * 2) = rest;
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
@@ -631,12 +654,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
         const int w_item = wave * 2 / (D / 32) * 32, w_col = wave * 2 % (D / 32) * 32;
         f32x16 dw[1][2] = {{f32x16{}, f32x16{}}};
 #pragma unroll
-        for (int k = 0; k < (REST ? 2 : kFew / 16); ++k) {
+        for (int k = 0; k < kFew / 16; ++k) {
             const s16x8 x[1] = {RowsI::across(dz, 16 * k, w_item)}, y[2] = {RowsD::across(h, 16 * k, w_col), RowsD::across(h, 16 * k, w_col + 32)};
-            if constexpr (REST) {
-                const s16x8 rest[1] = {RowsI::across(dz_rest, 16 * k, w_item)};
-                multiply<T, 1, 2>(rest, y, dw);
-            }
             multiply<T, 1, 2>(x, y, dw);
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (nobody reads the tile any more: it is the waves' own memory now)
@@ -666,13 +685,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int q = h_pos + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
-                if (q < a.B && col < a.d) a.partial_h[((size_t)blockIdx.x * a.B + q) * a.d + col] = dh[i][e];
+                if (q < dz_rows(a) && col < a.d) a.partial_h[((size_t)blockIdx.x * dz_rows(a) + q) * a.d + col] = dh[i][e];
             }
         }
     }
 }
 
-// The slices' shares of dH, added: every eighth slice by one of eight threads, these in their order.  64 positions of 512, 256
+// The slices' shares of dH (a slice's parts follow each other), added: every eighth by one of eight threads, these in their order.  64 positions of 512, 256
 // slices: 7.5 us for 34 MB.
 template <typename T>
 __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
@@ -682,7 +701,7 @@ __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
     float sum = 0.0f;
     if (i < n) {
 #pragma unroll 4
-        for (int s = lead; s < a.slices; s += 8) sum += a.partial_h[(size_t)s * n + i];
+        for (int s = lead; s < a.slices * a.parts; s += 8) sum += a.partial_h[(size_t)s * n + i];
     }
     part[lead][threadIdx.x % 32] = sum;
     __syncthreads();
@@ -698,7 +717,7 @@ __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
 struct DensePlan {
     int loss_items, positions, position_tiles, tiles_each, groups;   // loss: items and positions of a tile of z
     long long item_tiles;
-    int piece, pieces, padded, dz_items, dz_positions, dw_items, dw_cols;  // gradient: items and positions of a tile of dz, columns of one of dW
+    int parts, piece, pieces, padded, dz_items, dz_positions, dw_items, dw_cols;  // gradient: items and positions of a tile of dz, columns of one of dW
     int rows, cols, rows_tiles, cols_tiles, slices;    // a tile of dH, and how many share its items
     bool few, together;                                // by default_few_kernel; dW and dH in one launch
     size_t info_at, live_at, dz_at, partial_at, bytes;          // its workspace
@@ -760,17 +779,17 @@ hipError_t launch_few_loss(const DensePlan& p, const DenseArgs& a, hipStream_t s
     else hipLaunchKernelGGL((default_few_loss_kernel<T, 64>), grid, threads, 0, st, a);
     return hipGetLastError();
 }
-template <typename T, bool REST>
+template <typename T, bool PARTS>
 hipError_t launch_few_of(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
     const dim3 grid(p.slices), threads(kFewThreads);
-    if (a.d > 256) hipLaunchKernelGGL((default_few_kernel<T, 512, REST>), grid, threads, 0, st, a);
-    else if (a.d > 128) hipLaunchKernelGGL((default_few_kernel<T, 256, REST>), grid, threads, 0, st, a);
-    else if (a.d > 64) hipLaunchKernelGGL((default_few_kernel<T, 128, REST>), grid, threads, 0, st, a);
-    else hipLaunchKernelGGL((default_few_kernel<T, 64, REST>), grid, threads, 0, st, a);
+    if (a.d > 256) hipLaunchKernelGGL((default_few_kernel<T, 512, PARTS>), grid, threads, 0, st, a);
+    else if (a.d > 128) hipLaunchKernelGGL((default_few_kernel<T, 256, PARTS>), grid, threads, 0, st, a);
+    else if (a.d > 64) hipLaunchKernelGGL((default_few_kernel<T, 128, PARTS>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((default_few_kernel<T, 64, PARTS>), grid, threads, 0, st, a);
     return hipGetLastError();
 }
 template <typename T>
-hipError_t launch_few(const DensePlan& p, const DenseArgs& a, hipStream_t st) { return a.B <= 32 ? launch_few_of<T, true>(p, a, st) : launch_few_of<T, false>(p, a, st); }
+hipError_t launch_few(const DensePlan& p, const DenseArgs& a, hipStream_t st) { return a.parts > 1 ? launch_few_of<T, true>(p, a, st) : launch_few_of<T, false>(p, a, st); }
 
 template <typename T>
 hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
@@ -791,7 +810,7 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
         if (p.few) e = launch_few<T>(p, a, st);
     }
     const void* queries = a.H;
-    const bool own_rows = a.B <= 64;                           // (then dz's positions are those of one tile)
+    const bool own_rows = a.B <= 64;                           // (then dz's rows are those of one tile)
     if (!p.few && !own_rows) {
         const long long row_blocks = ceil_div((long long)a.B * a.d * (long long)sizeof(T), 16 * 1024);
         hipLaunchKernelGGL((default_rows_kernel<T>), dim3((unsigned)(row_blocks < kCUs ? row_blocks : kCUs)), dim3(1024), 0, st, a);

@@ -39,6 +39,7 @@ struct Operand {
     long long k0, k1;      // range of k: past k1 zeros are read
     int block = 0;         // along: a stored row holds this many k (a multiple of a stage's, as k0 is), the next ones lie
     size_t to_next = 0;    //   to_next bytes on; 0: all of them
+    int again = 0;         // along, row0 = 0: rows from this one on are the first ones again; 0: none
 };
 
 // acc[mi][ni] += x[mi] y[ni], 16-bit operands of sixteen k.
@@ -130,7 +131,7 @@ struct Side {
             const int at = (tid / kWave * kLoads + i) * kWave + tid % kWave;
             if constexpr (ALONG) {
                 const int row = at / 4, chunk = (at % 4) ^ (row / 4 % 4);
-                offset[i] = (uint32_t)min(row, last) * (uint32_t)ld + (uint32_t)chunk * 16u;
+                offset[i] = (uint32_t)min(o.again && row >= o.again ? row - o.again : row, last) * (uint32_t)ld + (uint32_t)chunk * 16u;
             } else {
                 const int kk = at / kRowChunks, chunk = swap(at % kRowChunks, kk), most = last * (int)sizeof(T) / 16;
                 offset[i] = (uint32_t)kk * (uint32_t)ld + (uint32_t)min(chunk, most) * 16u;

@@ -197,6 +197,42 @@ def test_gradients_of_very_different_size(pq):
     check(pq, W.bfloat16(), H.bfloat16(), targets, grad, "bf16")
 
 
+def gradients_in_64_bits(W, H, targets, grad):
+    """dz, dH, dW and a bound of a probability's relative error (see the head of this file)."""
+    (N, d), B = W.shape, H.shape[0]
+    w, h = W.double(), H.double()
+    z = h @ w.t().contiguous()
+    size = (h.abs() @ w.abs().t().contiguous()).max().item()
+    dz = torch.exp(z - torch.logsumexp(z, 1)[:, None])
+    p = dz.clone()
+    dz[torch.arange(B, device="cuda"), targets.long()] -= 1.0
+    dz *= grad.double()[:, None]
+    score = (d + 2) * U * size
+    rel = 2 * score + U * (N / 512 + 128 + 8 * size + 4 * np.log(max(N, 2)))
+    return p, dz, dz @ w, dz.t().contiguous() @ h, rel
+
+
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128, 200, 256, 512, 520, 1032])
+@pytest.mark.parametrize("N,B", [(50, 1), (700, 1), (60, 2), (1003, 8), (40, 31), (2000, 32), (20_011, 3)])
+def test_up_to_32_positions_lose_nothing_to_a_rounded_dz(pq, N, d, B, type):
+    # dz is multiplied with what its rounding leaves, so what is left of that rounding is a unit of a unit; then the result's own rounding
+    W, H, targets, grad = draw(N, d, B, type, seed=N + d + B, spread=4.0)
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+    p, dz, want_h, want_w, rel = gradients_in_64_bits(W, H, targets, grad)
+    unit, g, w, h = TYPES[type][1], grad.double().abs()[:, None], W.double().abs(), H.double().abs()
+    tiny = 2.0 ** -39 if type == "f16" else 0.0
+    floor = 2.0 ** -24 if type == "f16" else 1e-40
+    off = g * p * rel + dz.abs() * (unit * unit + 4 * U)
+    for got, want, o, a, other, n in ((dH, want_h, off + tiny * g, dz.abs(), w, N),
+                                      (dW, want_w, (off + tiny * g.max()).t().contiguous(), dz.abs().t().contiguous(), h, B)):
+        tol = o @ other + (n + 8) * U * ((a + o) @ other) + unit * want.abs() * (1 + 2 * unit) + floor
+        if type == "f16" and got is dW:
+            tol = tol + (dz.abs() / g).sum(0)[:, None] * 2.0 ** -38 * (g * h).max()
+        assert ((got.double() - want).abs() <= tol).all()
+
+
 def test_gradients_against_differences(pq):
     # float32; see the sub-ids' test: directions that move no score by more than 1
     N, d, B = 3000, 64, 9
