@@ -22,8 +22,11 @@ double tile_cost(int cols, int size) {
 }
 constexpr double kTileStart = 0.1;                     // what a workgroup takes besides its products
 
-DensePlan plan_dense(long long N, int B, int d, int size) {
+int size_of(int type) { return type == PQ_FLOAT32 ? 4 : type == PQ_BFLOAT16 || type == PQ_FLOAT16 ? 2 : 0; }
+
+DensePlan plan_dense(long long N, int B, int d, int type) {
     DensePlan p;
+    const int size = size_of(type);
     // Tiles of 64 x 64 where all of them run at once (loss and gradient, us: 10,000 items of 64 float32, 50 positions 42 with tiles
     // of 256 x 64, 34 so; 5000 of 512, one position 81 and 54; 8000 of 512, 128 positions 98 and 73), and for dz somewhat longer
     // (gradient: 5000 of 128, 1000 positions 57 and 49; 10,000 of 512, 500 positions 152 and 143; 8000 of 512, 900 positions 179 and
@@ -95,15 +98,15 @@ DensePlan plan_dense(long long N, int B, int d, int size) {
         p.padded = kFew;
         p.piece = 0;
     }
-    p.info_at = 256;
+    const size_t query_bytes = (size_t)B * p.parts * d * size;
+    p.info_at = 256 + kCUs * sizeof(int);              // (dW's factor, the blocks' powers)
     p.live_at = round_up(p.info_at + (size_t)p.padded * sizeof(RowInfo), 256);
-    p.dz_at = round_up(p.live_at + (size_t)B * p.parts * d * size, 256);
+    p.scaled_at = round_up(p.live_at + (p.few ? 0 : query_bytes), 256);
+    p.dz_at = round_up(p.scaled_at + (p.few || type != PQ_FLOAT16 ? 0 : query_bytes), 256);
     p.partial_at = round_up(p.dz_at + (size_t)p.padded * p.piece * size, 256);
     p.bytes = round_up(p.partial_at + (size_t)p.slices * B * p.parts * d * sizeof(float), 256);
     return p;
 }
-
-int size_of(int type) { return type == PQ_FLOAT32 ? 4 : type == PQ_BFLOAT16 || type == PQ_FLOAT16 ? 2 : 0; }
 
 int check_dense(long long N, int B, int d, int type) {
     if (N < 1 || B < 1 || d < 1 || N >= 2147483648LL || size_of(type) == 0) return PQ_ERR_SHAPE;
@@ -122,7 +125,7 @@ using namespace pqk::head;
 extern "C" {
 
 size_t pq_default_cross_entropy_workspace_bytes(long long N, int B, int d, int type) {
-    return check_dense(N, B, d, type) == PQ_OK ? loss_bytes(plan_dense(N, B, d, size_of(type)), B) : 0;
+    return check_dense(N, B, d, type) == PQ_OK ? loss_bytes(plan_dense(N, B, d, type), B) : 0;
 }
 
 int pq_default_cross_entropy(const void* W, const void* queries, const int* targets, long long N, int B, int d, int type, float* loss,
@@ -131,7 +134,7 @@ int pq_default_cross_entropy(const void* W, const void* queries, const int* targ
     const int rc = check_dense(N, B, d, type);
     if (rc != PQ_OK) return rc;
     if ((((uintptr_t)W | (uintptr_t)queries | (uintptr_t)workspace) & 15) || (((uintptr_t)targets | (uintptr_t)loss | (uintptr_t)lse) & 3)) return PQ_ERR_ALIGN;
-    const DensePlan p = plan_dense(N, B, d, size_of(type));
+    const DensePlan p = plan_dense(N, B, d, type);
     if (workspace_bytes < loss_bytes(p, B)) return PQ_ERR_WORKSPACE;
     DenseArgs a{};
     a.W = W; a.H = queries; a.targets = targets; a.N = N; a.B = B; a.d = d;
@@ -146,7 +149,7 @@ int pq_default_cross_entropy(const void* W, const void* queries, const int* targ
 }
 
 size_t pq_default_cross_entropy_backward_workspace_bytes(long long N, int B, int d, int type) {
-    return check_dense(N, B, d, type) == PQ_OK ? plan_dense(N, B, d, size_of(type)).bytes : 0;
+    return check_dense(N, B, d, type) == PQ_OK ? plan_dense(N, B, d, type).bytes : 0;
 }
 
 int pq_default_cross_entropy_backward(const void* W, const void* queries, const int* targets, const float* lse, const float* grad_loss,
@@ -158,15 +161,17 @@ int pq_default_cross_entropy_backward(const void* W, const void* queries, const 
     if ((((uintptr_t)W | (uintptr_t)queries | (uintptr_t)workspace) & 15) ||
         (((uintptr_t)targets | (uintptr_t)lse | (uintptr_t)grad_loss) & 3) || (((uintptr_t)dqueries | (uintptr_t)dW) & 15))
         return PQ_ERR_ALIGN;
-    const DensePlan p = plan_dense(N, B, d, size_of(type));
+    const DensePlan p = plan_dense(N, B, d, type);
     if (workspace_bytes < p.bytes) return PQ_ERR_WORKSPACE;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     DenseArgs a{};
     a.W = W; a.H = queries; a.targets = targets; a.N = N; a.B = B; a.d = d;
     a.lse_in = lse; a.grad = grad_loss; a.dH = dqueries; a.dW = dW;
     a.factor = reinterpret_cast<float*>(ws);
+    a.block_powers = reinterpret_cast<int*>(ws + 256);
     a.info = reinterpret_cast<RowInfo*>(ws + p.info_at);
     a.live = ws + p.live_at;
+    a.scaled = ws + p.scaled_at;
     a.dz = ws + p.dz_at;
     a.partial_h = reinterpret_cast<float*>(ws + p.partial_at);
     a.parts = p.parts; a.piece = p.piece; a.padded = p.padded; a.slices = p.slices;

@@ -16,10 +16,14 @@ namespace pqk {
 namespace head {
 
 constexpr float kHeadroom = 40.0f;                    // (log2) how far a score may rise over a lane's reference before that moves
-constexpr float kDzBits = 15.0f, kDzScale = 32768.0f;  // dz is stored times 2^15 over the largest |g|: types keep small probabilities
+constexpr float kDzBits = 15.0f, kDzScale = 32768.0f;  // dz is stored times 2^15 over a weight (RowInfo): types keep small probabilities
 constexpr int kItems = 256;                           // items of a block of dz, and of most tiles of z and dW
 
-struct RowInfo { float at, scale; };                  // of a position: 2^(z log2e - at) is p 2^15; its g over the largest |g|
+// Of a row of dz: 2^(z log2e - at) is p 2^15; its g over what dz is stored over; what its row of dH is multiplied with.  dz is stored over
+// the largest |g| of all positions, but in float16, whose exponents would not reach far below that (a position of a millionth of the
+// largest weight would keep probabilities down to 2^-19 alone), over the power of two above the position's own |g|.
+struct RowInfo { float at, scale, factor; };
+template <typename T> constexpr bool kOwnPowers = std::is_same<T, _Float16>::value;
 
 // The tiles: z for ITEMS items and POS positions; dH for ROWS positions and COLS elements; dW for ITEMS items and COLS
 // elements.  Tiles of 256 x 256 by eight waves feed the matrix cores best (208 TFLOP/s in float32, 1040 to 1130 in bfloat16,
@@ -73,7 +77,9 @@ struct DenseArgs {
     int parts;                                         // rows of dz that a position has (see dz_rows)
     RowInfo* info;                                     // [rows of dz, padded]
     void* live;                                        // [rows of dz][d]: the queries, zeros where a position adds nothing
-    float* factor;                                     // what the products are multiplied with
+    float* factor;                                     // what dW is multiplied with
+    int* block_powers;                                 // float16: of the blocks of default_rows_kernel, see scale_rows_kernel
+    void* scaled;                                      // float16: [rows of dz][d], the queries that dW is made of
     void* dz;                                          // [tiles of a piece][rows of dz, padded][kItems]
     float* partial_h;                                  // [slices][rows of dz][d]
     void *dH, *dW;
@@ -202,9 +208,20 @@ __device__ __forceinline__ float wave_top(float v) {
     for (int x = 1; x < kWave; x *= 2) v = fmaxf(v, __shfl_xor(v, x));
     return v;
 }
+// The power of two above |x|, x a number but 0: |x| 2^-power is at least a half.
+__device__ __forceinline__ int power_of(float x) {
+    int e;
+    (void)frexpf(x, &e);
+    return e;
+}
+// Of a gradient: 0 where it is no number.
+__device__ __forceinline__ int weight_power(float g) { return fabsf(g) < __builtin_inff() ? power_of(g) : 0; }
 // Of a position with gradient g (0: it adds nothing), the largest of all being top.
+template <typename T>
 __device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
-    return g != 0.0f ? RowInfo{lse * kLog2e - kDzBits, g / top} : RowInfo{__builtin_inff(), 0.0f};
+    if (g == 0.0f) return RowInfo{__builtin_inff(), 0.0f, 0.0f};
+    if constexpr (kOwnPowers<T>) return RowInfo{lse * kLog2e - kDzBits, ldexpf(g, -weight_power(g)), ldexpf(1.0f / kDzScale, weight_power(g))};
+    else return RowInfo{lse * kLog2e - kDzBits, g / top, top / kDzScale};
 }
 
 // The share of the gradient of a row's position: 0 where there is none, no target, no item in play or no position.
@@ -213,14 +230,32 @@ __device__ __forceinline__ float row_weight(const DenseArgs& a, int row) {
     return t >= 0 && t < a.N && a.lse_in[q] != -__builtin_inff() ? a.grad[q] : 0.0f;
 }
 // The queries in pieces of 16 bytes, from piece `first` on every `stride`-th, with zeros for positions that add nothing.
+// Float16: returns the power of two above these pieces' largest product of weight and query.
+constexpr int kNoPower = -100000;
 template <typename T>
-__device__ __forceinline__ void copy_live(const DenseArgs& a, size_t first, size_t stride) {
+__device__ __forceinline__ int copy_live(const DenseArgs& a, size_t first, size_t stride) {
     const int row_pieces = a.d * (int)sizeof(T) / 16;
     const size_t pieces = (size_t)dz_rows(a) * row_pieces, position_pieces = (size_t)a.B * row_pieces;
+    int power = kNoPower;
     for (size_t i = first; i < pieces; i += stride) {
-        const uint4 v = static_cast<const uint4*>(a.H)[i < position_pieces ? i : i - position_pieces];
-        static_cast<uint4*>(a.live)[i] = row_weight(a, (int)(i / row_pieces)) != 0.0f ? v : uint4{0, 0, 0, 0};
+        uint4 v = static_cast<const uint4*>(a.H)[i < position_pieces ? i : i - position_pieces];
+        const float g = row_weight(a, (int)(i / row_pieces));
+        if (g == 0.0f) v = uint4{0, 0, 0, 0};
+        static_cast<uint4*>(a.live)[i] = v;
+        if constexpr (kOwnPowers<T>) {
+            const f16x8 h = __builtin_bit_cast(f16x8, v);
+            float largest = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf((float)h[e]) < __builtin_inff() ? fabsf((float)h[e]) : 0.0f);
+            if (largest > 0.0f) power = max(power, weight_power(g) + power_of(largest));
+        }
     }
+    return power;
+}
+__device__ __forceinline__ int wave_max(int v) {
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) v = max(v, __shfl_xor(v, x));
+    return v;
 }
 
 // What the gradient's kernels need of a position, the factor of their products, and the queries they multiply: those of a
@@ -229,8 +264,17 @@ __device__ __forceinline__ void copy_live(const DenseArgs& a, size_t first, size
 template <typename T>
 __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
     __shared__ float tops[16];
+    __shared__ int powers[16];
     const int tid = threadIdx.x;
-    copy_live<T>(a, (size_t)blockIdx.x * 1024 + tid, (size_t)gridDim.x * 1024);
+    int power = wave_max(copy_live<T>(a, (size_t)blockIdx.x * 1024 + tid, (size_t)gridDim.x * 1024));
+    if constexpr (kOwnPowers<T>) {
+        if (tid % kWave == 0) powers[tid / kWave] = power;
+        __syncthreads();
+        if (tid < kWave) {
+            power = wave_max(powers[tid % 16]);
+            if (tid == 0) a.block_powers[blockIdx.x] = power;
+        }
+    }
     if (blockIdx.x != 0) return;
     float top = 0.0f;
     for (int q = tid; q < a.B; q += 1024) top = fmaxf(top, fabsf(row_weight(a, q)));
@@ -241,9 +285,30 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
 #pragma unroll
     for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
     for (int q = tid; q < a.padded; q += 1024) {
-        a.info[q] = row_info(row_weight(a, q), top, a.lse_in[min(q, a.B - 1)]);
+        a.info[q] = row_info<T>(row_weight(a, q), top, a.lse_in[min(position_of(a, q), a.B - 1)]);
     }
-    if (tid == 0) *a.factor = top / kDzScale;
+    if (!kOwnPowers<T> && tid == 0) *a.factor = top / kDzScale;
+}
+
+// Float16: the queries that dW is made of, each times the power of two that its position's dz was stored over, and all times the one that
+// brings the largest below 2^15.  So what float16 cannot hold of a small weight's queries is 2^-40 of the largest product of weight and query.
+template <typename T>
+__global__ __launch_bounds__(1024) void scale_rows_kernel(DenseArgs a) {
+    const int lane = threadIdx.x % kWave;
+    int power = kNoPower;
+    for (int i = lane; i < (int)gridDim.x; i += kWave) power = max(power, a.block_powers[i]);          // (as many blocks made them)
+    power = wave_max(power);
+    const int row_pieces = a.d * (int)sizeof(T) / 16;
+    const size_t pieces = (size_t)dz_rows(a) * row_pieces;
+    for (size_t i = (size_t)blockIdx.x * 1024 + threadIdx.x; i < pieces; i += (size_t)gridDim.x * 1024) {
+        f16x8 h = static_cast<const f16x8*>(a.live)[i];
+        const float g = row_weight(a, (int)(i / row_pieces));
+        const int by = g == 0.0f ? 0 : weight_power(g) + 15 - power;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = (_Float16)ldexpf((float)h[e], by);
+        static_cast<f16x8*>(a.scaled)[i] = h;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.factor = power == kNoPower ? 0.0f : ldexpf(1.0f, power - 30);
 }
 
 // Blocks of 32 x 32 results leave through the wave's LDS, N of them at a time, in rows of 16-byte pieces: row lane % 32 of a block
@@ -287,7 +352,8 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     using Tile = ScoresTile<T, BN, ITEMS>;
     constexpr int MI = Tile::MI, NI = Tile::NI;
     static_assert(!ROWS || BN == kWave, "a row is a lane");
-    constexpr bool kParts = ROWS && sizeof(T) == 2;            // (whether there may be two a position)
+    static_assert(!ROWS || !kOwnPowers<T>, "scale_rows_kernel comes after default_rows_kernel");
+    constexpr bool kParts = BN == kWave && sizeof(T) == 2;     // (whether there may be two a position)
     int tile, pt;
     chiplet_order(blockIdx.x, a.tiles_n, tile, pt);
     if (tile >= a.tiles_m) return;
@@ -296,9 +362,10 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     if constexpr (ROWS) {                                      // (every wave: lane r has row r's)
         const float g = row_weight(a, lane);
         const float top = wave_top(fabsf(g));
-        own_row = row_info(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
+        own_row = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
         if (!a.more) {
             copy_live<T>(a, (size_t)tile * Tile::kThreads + threadIdx.x, (size_t)a.tiles_m * Tile::kThreads);
+            if (tile == 0 && threadIdx.x < kWave) a.info[lane] = own_row;
             if (tile == 0 && threadIdx.x == 0) *a.factor = top / kDzScale;
         }
     }
@@ -574,6 +641,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     using RowsD = Rows<D / 8>;                                 // W and H
     using RowsI = Rows<IT / 8>;                                // dz: [row][item]
     __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2], dz[kFew * IT * 2];
+    // float16: dH's rows are stored over their own weights, for dW all over the largest
+    constexpr bool kOwn = kOwnPowers<T>;
+    __shared__ __align__(16) unsigned char dz_over_top[kOwn ? kFew * IT * 2 : 16];
+    __shared__ float over_top[kFew];
+    unsigned char* dz_w = kOwn ? dz_over_top : dz;
     __shared__ RowInfo info[kFew];
     __shared__ int target[kFew];
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -586,12 +658,11 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     if (wave == 0) {
         const float g = row_weight(a, lane);
         const float top = wave_top(fabsf(g));
-        info[lane] = row_info(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
+        info[lane] = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
+        if (blockIdx.x == 0) a.info[lane] = info[lane];
+        if (kOwn) over_top[lane] = g == 0.0f ? 0.0f : g / top;
         target[lane] = lane < dz_rows(a) ? a.targets[position_of(a, lane)] : -1;
-        if (lane == 0) {
-            factor_of_all = top / kDzScale;
-            if (blockIdx.x == 0) *a.factor = factor_of_all;
-        }
+        if (lane == 0) factor_of_all = top / kDzScale;
     }
     // dH: 2 x D / 32 blocks of 32 rows x 32 elements, shared by the waves; D = 64 leaves half of them without one
     constexpr int kBlocksH = D / 16 >= kWaves ? D / 16 / kWaves : 1;
@@ -624,7 +695,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
             const int first = item0 + lane / 16 * 4;
             const long long hit = (long long)target[pos] - (tile * IT + first), left = a.N - (tile * IT + first);
             typedef T T4 __attribute__((ext_vector_type(4)));
-            T4 v;
+            T4 v, u;
+            const float over = kOwn ? over_top[pos] : 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float p = exp2_fast(fmaf(z[e], kLog2e, -r.at));
@@ -632,8 +704,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
                 if (e >= left) p = 0.0f;
                 v[e] = (T)(p * r.scale);
                 if (PARTS && pos >= a.B) v[e] = (T)fmaf(p, r.scale, -(float)v[e]);
+                if (kOwn) {
+                    u[e] = (T)(p * over);
+                    if (PARTS && pos >= a.B) u[e] = (T)fmaf(p, over, -(float)u[e]);
+                }
             }
             *reinterpret_cast<T4*>(dz + RowsI::at(pos, first / 8) + first % 8 * 2) = v;
+            if (kOwn) *reinterpret_cast<T4*>(dz_w + RowsI::at(pos, first / 8) + first % 8 * 2) = u;
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
@@ -655,7 +732,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
         f32x16 dw[1][2] = {{f32x16{}, f32x16{}}};
 #pragma unroll
         for (int k = 0; k < kFew / 16; ++k) {
-            const s16x8 x[1] = {RowsI::across(dz, 16 * k, w_item)}, y[2] = {RowsD::across(h, 16 * k, w_col), RowsD::across(h, 16 * k, w_col + 32)};
+            const s16x8 x[1] = {RowsI::across(dz_w, 16 * k, w_item)}, y[2] = {RowsD::across(h, 16 * k, w_col), RowsD::across(h, 16 * k, w_col + 32)};
             multiply<T, 1, 2>(x, y, dw);
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (nobody reads the tile any more: it is the waves' own memory now)
@@ -708,7 +785,7 @@ __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
     if (lead != 0 || i >= n) return;
 #pragma unroll
     for (int w = 1; w < 8; ++w) sum += part[w][threadIdx.x];
-    static_cast<T*>(a.dH)[i] = (T)(sum * *a.factor);
+    static_cast<T*>(a.dH)[i] = (T)(sum * a.info[(uint32_t)i / (uint32_t)a.d].factor);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -720,7 +797,7 @@ struct DensePlan {
     int parts, piece, pieces, padded, dz_items, dz_positions, dw_items, dw_cols;  // gradient: items and positions of a tile of dz, columns of one of dW
     int rows, cols, rows_tiles, cols_tiles, slices;    // a tile of dH, and how many share its items
     bool few, together;                                // by default_few_kernel; dW and dH in one launch
-    size_t info_at, live_at, dz_at, partial_at, bytes;          // its workspace
+    size_t info_at, live_at, scaled_at, dz_at, partial_at, bytes;          // its workspace
 };
 
 inline int grid_of(long long outer, long long inner) { return (int)(ceil_div(outer, 8) * 8 * inner); }     // see chiplet_order()
@@ -810,12 +887,19 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
         if (p.few) e = launch_few<T>(p, a, st);
     }
     const void* queries = a.H;
-    const bool own_rows = a.B <= 64;                           // (then dz's rows are those of one tile)
+    const bool own_rows = a.B <= 64 && !kOwnPowers<T>;         // (then dz's rows are those of one tile)
     if (!p.few && !own_rows) {
-        const long long row_blocks = ceil_div((long long)a.B * a.d * (long long)sizeof(T), 16 * 1024);
-        hipLaunchKernelGGL((default_rows_kernel<T>), dim3((unsigned)(row_blocks < kCUs ? row_blocks : kCUs)), dim3(1024), 0, st, a);
+        const long long row_blocks = ceil_div((long long)a.B * a.parts * a.d * (long long)sizeof(T), 16 * 1024);
+        const dim3 grid((unsigned)(row_blocks < kCUs ? row_blocks : kCUs));
+        hipLaunchKernelGGL((default_rows_kernel<T>), grid, dim3(1024), 0, st, a);
         e = hipGetLastError();
         queries = a.live;
+        if constexpr (kOwnPowers<T>) {
+            if (e == hipSuccess) {
+                hipLaunchKernelGGL((scale_rows_kernel<T>), grid, dim3(1024), 0, st, a);
+                e = hipGetLastError();
+            }
+        }
     }
     for (int i = 0; !p.few && i < p.pieces && e == hipSuccess; ++i) {
         a.first_item = (long long)i * p.piece;
@@ -823,11 +907,13 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
         a.items = (int)round_up((size_t)(left < p.piece ? left : p.piece), kItems);
         a.more = i > 0;
         a.H = queries;
-        if (own_rows) e = p.dz_items == 64 ? launch_dz<T, 64, 64, true>(a, st) : launch_dz<T, 64, 256, true>(a, st);
-        else e = p.dz_items == 64 ? launch_dz<T, 64, 64>(a, st) : p.dz_positions == 256 ? launch_dz<T, 256, 256>(a, st)
+        if constexpr (!kOwnPowers<T>) {
+            if (own_rows) e = p.dz_items == 64 ? launch_dz<T, 64, 64, true>(a, st) : launch_dz<T, 64, 256, true>(a, st);
+        }
+        if (!own_rows) e = p.dz_items == 64 ? launch_dz<T, 64, 64>(a, st) : p.dz_positions == 256 ? launch_dz<T, 256, 256>(a, st)
             : p.dz_positions == 128 ? launch_dz<T, 128, 256>(a, st) : launch_dz<T, 64, 256>(a, st);
         if (e != hipSuccess) break;
-        a.H = a.live;
+        a.H = kOwnPowers<T> ? a.scaled : a.live;
         a.h_rows = p.rows_tiles;
         a.h_cols = p.cols_tiles;
         a.slice_items = (int)round_up((size_t)ceil_div(a.items, p.slices), kSliceItems);

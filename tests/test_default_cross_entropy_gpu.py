@@ -212,6 +212,29 @@ def gradients_in_64_bits(W, H, targets, grad):
     return p, dz, dz @ w, dz.t().contiguous() @ h, rel
 
 
+@pytest.mark.parametrize("N,d,B", [(20_000, 64, 80), (20_000, 64, 40), (20_000, 64, 20), (5000, 512, 64), (3000, 520, 33), (3000, 520, 7), (2000, 128, 300), (100_000, 64, 1030)])
+def test_float16_gradients_of_a_position_by_its_own_weight(pq, N, d, B):
+    # Weights from 2^12 down to a ten millionth of that.  Every row of dqueries keeps probabilities down to 2^-39 of its own weight (dz is a
+    # float16 of p 2^15 and a mantissa of at least a half: half its smallest number is 2^-39 of a probability), dW down to 2^-39 of the largest.
+    # For dW queries take their weights' powers of two, below 2^15 and at least 2^14 where that is most: half the smallest is 2^-40 of 2^15, and
+    # 2^15 stands for less than four times the largest product of weight and query.
+    # (Embeddings of a common mean and scores close together: all probabilities alike, so their roundings do not cancel.)
+    W, H, targets, grad = draw(N, d, B, "f16", seed=N + d + B, spread=0.25)
+    W += 0.125
+    grad = torch.logspace(0, -7, B, device="cuda")[torch.randperm(B, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))] * 4096.0
+    grad[::2] *= -1.0
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+    p, dz, want_h, want_w, rel = gradients_in_64_bits(W, H, targets, grad)
+    unit, g, w, h = TYPES["f16"][1], grad.double().abs()[:, None], W.double().abs(), H.double().abs()
+    off = g * p * rel + dz.abs() * (unit + 4 * U)
+    tol = (off + 2.0 ** -39 * g) @ w + (N + 8) * U * (dz.abs() @ w) + unit * want_h.abs() + 2.0 ** -24
+    assert ((dH.double() - want_h).abs() <= tol).all()
+    off = (off + 2.0 ** -39 * g.max()).t().contiguous() @ h
+    tol = off + (dz.abs() / g).sum(0)[:, None] * 2.0 ** -38 * (g * h).max() + (B + 8) * U * (dz.abs().t().contiguous() @ h) + unit * want_w.abs() + 2.0 ** -24
+    assert ((dW.double() - want_w).abs() <= tol).all()
+
+
 @pytest.mark.parametrize("type", ["bf16", "f16"])
 @pytest.mark.parametrize("d", [64, 128, 200, 256, 512, 520, 1032])
 @pytest.mark.parametrize("N,B", [(50, 1), (700, 1), (60, 2), (1003, 8), (40, 31), (2000, 32), (20_011, 3)])
