@@ -216,6 +216,8 @@ __device__ __forceinline__ int power_of(float x) {
 }
 // Of a gradient: 0 where it is no number.
 __device__ __forceinline__ int weight_power(float g) { return fabsf(g) < __builtin_inff() ? power_of(g) : 0; }
+// What a gradient is to the largest of all: an infinite one is none, or it would be what all other positions are stored over.
+__device__ __forceinline__ float weight_size(float g) { return fabsf(g) < __builtin_inff() ? fabsf(g) : 0.0f; }
 // Of a position with gradient g (0: it adds nothing), the largest of all being top.
 template <typename T>
 __device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
@@ -277,7 +279,7 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
     }
     if (blockIdx.x != 0) return;
     float top = 0.0f;
-    for (int q = tid; q < a.B; q += 1024) top = fmaxf(top, fabsf(row_weight(a, q)));
+    for (int q = tid; q < a.B; q += 1024) top = fmaxf(top, weight_size(row_weight(a, q)));
     top = wave_top(top);
     if (tid % kWave == 0) tops[tid / kWave] = top;
     __syncthreads();
@@ -361,7 +363,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     RowInfo own_row{};
     if constexpr (ROWS) {                                      // (every wave: lane r has row r's)
         const float g = row_weight(a, lane);
-        const float top = wave_top(fabsf(g));
+        const float top = wave_top(weight_size(g));
         own_row = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
         if (!a.more) {
             copy_live<T>(a, (size_t)tile * Tile::kThreads + threadIdx.x, (size_t)a.tiles_m * Tile::kThreads);
@@ -657,7 +659,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     __shared__ float factor_of_all;
     if (wave == 0) {
         const float g = row_weight(a, lane);
-        const float top = wave_top(fabsf(g));
+        const float top = wave_top(weight_size(g));
         info[lane] = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
         if (blockIdx.x == 0) a.info[lane] = info[lane];
         if (kOwn) over_top[lane] = g == 0.0f ? 0.0f : g / top;

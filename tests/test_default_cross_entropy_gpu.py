@@ -197,6 +197,21 @@ def test_gradients_of_very_different_size(pq):
     check(pq, W.bfloat16(), H.bfloat16(), targets, grad, "bf16")
 
 
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("odd", [float("inf"), float("nan")])
+@pytest.mark.parametrize("N,d,B", [(3000, 64, 20), (3000, 64, 50), (700, 520, 20), (700, 520, 50), (1500, 128, 300)])
+def test_weights_that_are_no_numbers_stay_with_their_position(pq, N, d, B, type, odd):
+    W, H, targets, grad = draw(N, d, B, type, seed=N + B)
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    grad[7] = odd
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+    assert not torch.isfinite(dH[7]).any() and not torch.isfinite(dW[targets[7]]).any()
+    grad[7] = 0.0
+    dH2, _ = pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+    rest = torch.arange(B, device="cuda") != 7
+    assert torch.isfinite(dH[rest]).all() and torch.equal(dH[rest], dH2[rest])
+
+
 def gradients_in_64_bits(W, H, targets, grad):
     """dz, dH, dW and a bound of a probability's relative error (see the head of this file)."""
     (N, d), B = W.shape, H.shape[0]
