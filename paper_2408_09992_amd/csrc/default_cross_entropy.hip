@@ -11,6 +11,7 @@ namespace {
 // 1.28M of 64, 512 positions 943 and 995).
 constexpr long long kDzBytes = 1LL << 30, kDzBytesShort = 1LL << 28;
 constexpr long long kMaxPiece = 1LL << 22;
+constexpr long long kMostLossBlocks = 64 * kCUs;
 
 // What a tile of 256 rows and `cols` columns takes a compute unit next to one of 256 x 256 that keeps the matrix cores as busy
 // as can be (the smaller ones' rates: 203 of 208 TFLOP/s and about 165 in float32; 880 of 1040 and about 600 in 16 bits).
@@ -49,6 +50,12 @@ DensePlan plan_dense(long long N, int B, int d, int type) {
                 p.positions = tile; p.position_tiles = (int)position_tiles; p.tiles_each = each; p.groups = (int)groups;
             }
         }
+    }
+    // (a workgroup more is nothing to gain where there are many to a compute unit, but a sum more to keep: long catalogues of many
+    // positions would launch 2^32 threads, which HIP refuses, and ask for gigabytes of sums)
+    while ((long long)p.groups * p.position_tiles > kMostLossBlocks) {
+        p.tiles_each *= 2;
+        p.groups = (int)ceil_div(p.item_tiles, p.tiles_each);
     }
     if (p.loss_items == 64) {
         p.positions = 64; p.position_tiles = (int)ceil_div(B, 64); p.tiles_each = 1; p.groups = (int)p.item_tiles;

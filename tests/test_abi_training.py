@@ -122,6 +122,14 @@ def test_cross_entropy_by_the_default_scorer(lib, type, backward):
         assert size(*bad) == 0, bad
 
 
+@pytest.mark.parametrize("type", [F32, BF16, F16])
+@pytest.mark.parametrize("N,B,d", [(2 ** 27, 65535, 64), (2 ** 31 - 1, 65535, 8), (2 ** 31 - 1, 1000, 512), (2 ** 24, 2048, 128), (10 ** 7, 65535, 64), (2 ** 31 - 1, 1, 8)])
+def test_loss_of_long_catalogues_fits_a_launch(lib, type, N, B, d):
+    # a sum of 8 bytes a group of items and position; a group has at most 512 threads for 64 positions, and groups come in eights
+    groups = lib.pq_default_cross_entropy_workspace_bytes(N, B, d, type) // (8 * B)
+    assert groups >= 1 and (groups + 7) // 8 * 8 * ((B + 63) // 64) * 512 < 2 ** 32 and groups * B * 8 < 2 ** 27
+
+
 def test_four_bit_embeddings(lib):
     make = caller(lib.pq_quantise_items, dict(W=P, N=100, d=128, group=64, packed=P, scales=P, stream=None))
     for x in ("W", "packed", "scales"):
