@@ -775,19 +775,24 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
 template <typename T>
 __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
     __shared__ float part[8][32];
-    const size_t n = (size_t)a.B * a.d, i = (size_t)blockIdx.x * 32 + threadIdx.x % 32;
+    const size_t n = (size_t)a.B * a.d;
     const int lead = threadIdx.x / 32;
-    float sum = 0.0f;
-    if (i < n) {
+    for (size_t first = (size_t)blockIdx.x * 32; first < n; first += (size_t)gridDim.x * 32) {
+        const size_t i = first + threadIdx.x % 32;
+        float sum = 0.0f;
+        if (i < n) {
 #pragma unroll 4
-        for (int s = lead; s < a.slices * a.parts; s += 8) sum += a.partial_h[(size_t)s * n + i];
-    }
-    part[lead][threadIdx.x % 32] = sum;
-    __syncthreads();
-    if (lead != 0 || i >= n) return;
+            for (int s = lead; s < a.slices * a.parts; s += 8) sum += a.partial_h[(size_t)s * n + i];
+        }
+        part[lead][threadIdx.x % 32] = sum;
+        __syncthreads();
+        if (lead == 0 && i < n) {
 #pragma unroll
-    for (int w = 1; w < 8; ++w) sum += part[w][threadIdx.x];
-    static_cast<T*>(a.dH)[i] = (T)(sum * a.info[(uint32_t)i / (uint32_t)a.d].factor);
+            for (int w = 1; w < 8; ++w) sum += part[w][threadIdx.x];
+            static_cast<T*>(a.dH)[i] = (T)(sum * a.info[(uint32_t)i / (uint32_t)a.d].factor);
+        }
+        __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -805,6 +810,7 @@ struct DensePlan {
 inline int grid_of(long long outer, long long inner) { return (int)(ceil_div(outer, 8) * 8 * inner); }     // see chiplet_order()
 
 constexpr int kSliceItems = 64;                        // a slice of dH's items is a multiple of this
+constexpr long long kMostJoinBlocks = 1LL << 20;       // (a launch has fewer than 2^32 threads)
 
 template <typename T> hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st);
 template <typename T> hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st);
@@ -929,7 +935,8 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
         e = p.rows == 256 ? launch_dh_cols<T, 256>(p, a, st) : p.rows == 128 ? launch_dh_cols<T, 128>(p, a, st) : launch_dh_cols<T, 64>(p, a, st);
     }
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((default_dh_join_kernel<T>), dim3((unsigned)ceil_div((long long)a.B * a.d, 32)), dim3(256), 0, st, a);
+    const long long join_blocks = ceil_div((long long)a.B * a.d, 32);
+    hipLaunchKernelGGL((default_dh_join_kernel<T>), dim3((unsigned)(join_blocks < kMostJoinBlocks ? join_blocks : kMostJoinBlocks)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 

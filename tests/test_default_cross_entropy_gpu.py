@@ -356,6 +356,21 @@ def test_embeddings_beyond_32_bits_of_offset(pq):
     assert abs(dH[0, 0].item() - (p - 1)) <= 2.0 ** -7 and abs(dH[1, 0].item() - p) <= 2.0 ** -7
 
 
+def test_queries_of_more_than_half_a_billion_elements(pq):
+    N, d, B = 40, 8200, 65535
+    assert B * d > 2 ** 29
+    W, H, targets, grad = draw(N, d, B, "bf16", seed=9, spread=1.0)
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+    rows = torch.cat([torch.arange(50), torch.arange(30_000, 30_050), torch.arange(B - 50, B)]).cuda()
+    p, dz, want_h, _, rel = gradients_in_64_bits(W, H[rows], targets[rows], grad[rows])
+    unit = TYPES["bf16"][1]
+    off = grad[rows].double().abs()[:, None] * p * rel + dz.abs() * (unit + 4 * U)
+    tol = off @ W.double().abs() + (N + 8) * U * (dz.abs() @ W.double().abs()) + unit * want_h.abs() + 1e-40
+    assert ((dH[rows].double() - want_h).abs() <= tol).all() and torch.isfinite(dH).all() and torch.isfinite(dW).all()
+    assert (dH.abs().amax(1) > 0).all()
+
+
 def test_refusals(pq):
     W, H, targets, grad = draw(100, 64, 3, "bf16", seed=1)
     lse = torch.zeros(3, device="cuda")
