@@ -81,8 +81,8 @@ int pq_cross_entropy_u16_backward(const uint16_t* codes, const float* S, const i
  *   dS float [B][m][b];  queries float [B][d];  centroids float [m][b][s];  dqueries float [B][d];  dcentroids float [m][b][s]
  * Sums in float32, in an order that depends on the shape alone; products exact or (a thousand queries and more) to 2^-25 of
  * themselves, as in pq_default_cross_entropy().
- * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (B, d, m, b < 1; d % m; b > 65536), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B, m > PQ_MAX_M),
- *         PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
+ * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (B, d, m, b < 1; d % m; b > 65536), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B, m > PQ_MAX_M,
+ *         or gradients of 2^33 elements and more), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
  */
 size_t pq_subitem_scores_backward_workspace_bytes(int B, int d, int m, int b);
 int pq_subitem_scores_backward(const float* dS, const float* queries, const float* centroids, float* dqueries,

@@ -238,7 +238,7 @@ extern "C" int pq_subitem_scores_backward(const float* dS, const float* queries,
     a.shares = (int)ceil_div(B, a.share);
     a.partial = static_cast<float*>(workspace);
     const long long by_centroid = dcentroids ? (long long)a.tiles_e * a.tiles_j * m * a.shares : 0, by_query = dqueries ? (long long)a.tiles_e * a.tiles_q * m : 0;
-    if (by_centroid + by_query > 2147483647LL) return PQ_ERR_UNSUPPORTED;
+    if ((by_centroid + by_query) * (tiles ? (int)TileQ::kThreads : kThreads) > 0xFFFFFFFFLL) return PQ_ERR_UNSUPPORTED;       // (a launch's threads)
     a.centroid_blocks = (int)by_centroid;
     const dim3 grid((unsigned)(by_centroid + by_query));
     hipStream_t st = static_cast<hipStream_t>(stream);

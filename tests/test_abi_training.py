@@ -92,6 +92,13 @@ def test_gradients_of_eq4(lib):
     assert size(0, 512, 8, 256) == 0 and size(1, 511, 8, 256) == 0 and size(1, 512, 8, 65537) == 0 and size(65536, 512, 8, 256) == 0
 
 
+@pytest.mark.parametrize("B", [1, 1000])
+def test_gradients_of_eq4_beyond_a_launch(lib, B):
+    # 128 splits of 65,536 sub-ids of 1056 elements: more than 2^33 elements of a gradient, 512 threads for every 1024
+    good = dict(dS=P, queries=P, centroids=P, dq=P, dc=P, B=B, d=128 * 1056, m=128, b=65536, ws=P, wsb=BIG, stream=None)
+    assert caller(lib.pq_subitem_scores_backward, good)() == UNSUPPORTED
+
+
 @pytest.mark.parametrize("type", [F32, BF16, F16])
 @pytest.mark.parametrize("backward", [False, True])
 def test_cross_entropy_by_the_default_scorer(lib, type, backward):
