@@ -79,8 +79,8 @@ int pq_cross_entropy_u16_backward(const uint16_t* codes, const float* S, const i
  *     dqueries[q][k s + e] = sum_j dS[q][k][j] * psi[k][j][e]      dcentroids[k][j][e] = sum_q dS[q][k][j] * phi[q][k s + e]
  * with s = d / m.  Either output may be NULL (not both): it is not computed.
  *   dS float [B][m][b];  queries float [B][d];  centroids float [m][b][s];  dqueries float [B][d];  dcentroids float [m][b][s]
- * Sums in float32, in an order that depends on the shape alone; products exact or (a thousand queries and more) to 2^-25 of
- * themselves, as in pq_default_cross_entropy().
+ * Sums in float32, in an order that depends on the shape alone.  From 1024 queries on, products are made of bfloat16 pieces, with
+ * the limits that pq_default_cross_entropy() states for float32; below that they are float32 products.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (B, d, m, b < 1; d % m; b > 65536), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B, m > PQ_MAX_M,
  *         or gradients of 2^33 elements and more), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
  */
@@ -97,8 +97,9 @@ int pq_subitem_scores_backward(const float* dS, const float* queries, const floa
  * Loss and log-sum of B positions by the default scorer: r_qi = W[i] . phi_q.
  *   W        in   type [N][d]   (16-byte aligned);   queries  in  type [B][d]  (16-byte aligned)
  *   targets  in   int32 [B];    loss, lse  out  float [B]
- * Scores are float32 sums of the products on the matrix cores (16-bit inputs: exact products; float32: products to 2^-25 of
- * themselves, from three bfloat16 pieces of each factor); they are never stored.
+ * Scores are float32 sums of the products on the matrix cores; they are never stored.  Products of 16-bit inputs are exact.  Those
+ * of float32 are made of three bfloat16 pieces of each factor: to 2^-24 of themselves for factors of 2^-100 and more (a smaller
+ * one's last piece, below 2^-126, may be lost), and a factor that is infinite or above 3.396e38 makes NaN of the sums it enters.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, B, d < 1; an unknown type; N >= 2^31), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B, d > 16384,
  *         d no multiple of 16 bytes of elements: 4 of float32, 8 of 16-bit types), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
  */

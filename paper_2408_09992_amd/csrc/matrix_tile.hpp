@@ -56,8 +56,8 @@ __device__ __forceinline__ void multiply(const s16x8 (&x)[MI], const s16x8 (&y)[
         }
 }
 
-// Eight floats as the sums of three bfloat16 each: x = p0 + p1 + p2 to 2^-26 |x| (each piece is what the ones before it leave,
-// rounded to nearest).
+// Eight floats as the sums of three bfloat16 each, x = p0 + p1 + p2 (each piece is what the ones before it leave, rounded to nearest:
+// 24 bits are 8 and 8 and 8).  For x of 1 to 2 a piece leaves at most 2^-8, then 2^-17, then nothing.
 struct Pieces { s16x8 p[3]; };
 __device__ __forceinline__ Pieces pieces_of(s16x8 a, s16x8 b) {
     const f32x4 u = __builtin_bit_cast(f32x4, a), v = __builtin_bit_cast(f32x4, b);
@@ -79,8 +79,8 @@ __device__ __forceinline__ Pieces pieces_of(s16x8 a, s16x8 b) {
     return r;
 }
 
-// The same for sixteen k of float32, x and y holding four k each.  A product is six of its pieces', all but those of 2^-24
-// and less of it (p1 q2, p2 q1, p2 q2: together below 2^-25 |x y|, half a unit of float32), the small ones first.  Six
+// The same for sixteen k of float32, x and y holding four k each.  A product is six of its pieces', all but the smallest
+// (p1 q2, p2 q1, p2 q2: together below 2^-24 |x y|, as p1 is at most 2^-8 and p2 2^-17 of a power of two below x), the small ones first.  Six
 // instructions of the 16-bit rate take 37 % of the time of the eight float32 ones: 208 against 146 TFLOP/s at 4096^3.
 template <int MI, int NI>
 __device__ __forceinline__ void multiply_floats(const s16x8 (&x)[2][MI], const s16x8 (&y)[2][NI], f32x16 (&acc)[MI][NI]) {
