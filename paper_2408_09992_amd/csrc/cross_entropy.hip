@@ -167,7 +167,7 @@ struct LossArgs {
 // reference c and sum s per query (total s 2^c); the reference moves only when a score passes it by 2^kHeadroom, which the
 // sum's exponent has room for, so the usual step has no maximum to carry.
 // Bound by the lookups in LDS: 1024 positions of 1.27M items, m = 8, 742 us, 0.044 cycles each and compute unit; 16 of 5M items,
-// m = 16, whose tables leave LDS one workgroup, 120 us, 0.058.
+// m = 16, whose registers (71 a lane) leave a compute unit one workgroup, 113 us, 0.054.
 template <int M, typename CT, int Q>
 __global__ __launch_bounds__(kThreads) void cross_entropy_kernel(LossArgs a) {
     constexpr int kUnits = units_of<M>();
@@ -499,8 +499,13 @@ bool plan_loss(Plan& p, long long N, int B, int m, int b, int code_bytes) {
     p.lds = entry_floats * 4 * p.Q + kStatBytes;
     if (p.lds > kMaxLds) return false;
     p.groups = (int)ceil_div(B, p.Q);
+    // Two workgroups run on a compute unit where LDS holds the tables of both and its registers (64 a lane then) the rows, which those of 16
+    // and 32 bytes are too long for.  (Counted as two, they came in two rounds of half the items: 1.28M items, m = 16, one position 19.4 us
+    // instead of 15.0, 300,000 and 64 positions 46 instead of 36; 5M, m = 16, 16 positions 124 instead of 117.)
+    const bool long_rows = m == 16 || (m == 8 && code_bytes == 2) || (m == 32 && code_bytes == 1);
+    const bool two = p.lds <= kMaxLds / 2 && !long_rows;
     // a lookup takes a compute unit 0.04 cycles a query (0.08 for one query alone); tables come in at some 20 bytes a cycle
-    cut_items(p, N, p.groups, (p.lds <= kMaxLds / 2 ? 2 : 1) * kCUs, m * (p.Q == 1 ? 0.08 : 0.045 * p.Q), 2000 + p.lds / 20.0);
+    cut_items(p, N, p.groups, (two ? 2 : 1) * kCUs, m * (p.Q == 1 ? 0.08 : 0.045 * p.Q), 2000 + p.lds / 20.0);
     return true;
 }
 
