@@ -307,7 +307,8 @@ hipError_t go_q4(Q4Args a, hipStream_t st) {
     a.rows = ceil_div(a.N, PACK);
     a.tiles = ceil_div(a.rows, kTileRows);
     a.steps = (int)ceil_div(a.d * PACK, kStep);
-    const int query_groups = (int)ceil_div(a.B, kQueries), per_cu = fixed + tile > kMaxLds / 2 ? 1 : 2;
+    // (32 queries take 154 to 170 registers a lane, where two workgroups have 128; counted as two, 200,000 items of 128 took 23 us instead of 17)
+    const int query_groups = (int)ceil_div(a.B, kQueries), per_cu = SETS == 4 || fixed + tile > kMaxLds / 2 ? 1 : 2;
     // neighbouring tiles to a workgroup's waves; where a wave has one at most, to as many compute units as there are (20,000 items of
     // 512, groups of 64: one query 7.2 and 5.6 us, 32 queries 15.5 and 12.3)
     long long blocks = ceil_div(a.tiles, kWaves);
