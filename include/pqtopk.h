@@ -218,7 +218,7 @@ int pq_default_scores(const float* W, const float* queries, long long N, int B, 
  *                                         held within -8 .. 7 times it.  A group with an infinity or a NaN has the scale NaN
  * group is 32, 64 or 128 and divides d.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, d < 1, another group, d % group, N >= 2^31), PQ_ERR_UNSUPPORTED (d > 16384),
- *         PQ_ERR_ALIGN, PQ_ERR_HIP.
+ *         PQ_ERR_ALIGN, PQ_ERR_HIP.  (pq_default_scores_q4() reads embeddings of up to 9856 elements.)
  */
 int pq_quantise_items(const float* W, long long N, int d, int group, uint8_t* packed, uint16_t* scales, void* stream);
 
@@ -228,8 +228,8 @@ int pq_quantise_items(const float* W, long long N, int d, int group, uint8_t* pa
  *   queries in float [B][d];  scores out float [B][ld], ld >= N
  * A query's elements are taken as whole multiples of 2^-30 of a power of two above its largest one.  Sums within a group are
  * exact, rounded to float32 as they leave the group; the sum over groups is float32.  A query that holds an infinity or a NaN has NaN scores.
- * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (as above; B < 1, ld < N), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B; d > 9856: a query's
- *         digits would not fit LDS), PQ_ERR_ALIGN, PQ_ERR_HIP.
+ * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (as above; B < 1, ld < N), PQ_ERR_UNSUPPORTED (B > PQ_MAX_B; d > 9856, up to
+ *         which LDS holds the digits of four queries), PQ_ERR_ALIGN, PQ_ERR_HIP.
  */
 int pq_default_scores_q4(const uint8_t* packed, const uint16_t* scales, const float* queries, long long N, int B, int d,
                          int group, float* scores, long long ld, void* stream);

@@ -13,7 +13,7 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
 constexpr int kStep = 128, kQuarters = 4;            // elements of a row per step: 64 bytes, a quarter (32 elements) for a lane
-constexpr int kMaxWidth = 9856;                      // of an embedding: four queries' digits in LDS
+constexpr int kMaxWidth = 9856;                      // of an embedding: up to here LDS surely holds the digits of four queries (158 KB)
 constexpr int kTileRows = 32;                        // rows of a matrix instruction's other operand
 
 struct Q4Args {
@@ -325,9 +325,9 @@ hipError_t go_q4(Q4Args a, hipStream_t st) {
 
 template <int GROUP, int PACK, bool WHOLE>
 hipError_t go_q4_sets(const Q4Args& a, hipStream_t st) {
-    // as many queries a pass over the weights as there are, up to 32 and what LDS holds of their digits
+    // as many queries a pass over the weights as there are, up to 32 and what LDS holds of their digits (four always: kMaxWidth)
     int queries = a.B <= 2 ? 2 : a.B <= 4 ? 4 : a.B <= 8 ? 8 : a.B <= 16 ? 16 : 32;
-    while (queries > 2 && q4_lds(queries, a.d * PACK) + held_bytes() > kMaxLds) queries /= 2;
+    while (queries > 4 && q4_lds(queries, a.d * PACK) + held_bytes() > kMaxLds) queries /= 2;
     switch (queries) {
         case 2: return go_q4<1, 1, GROUP, PACK, WHOLE>(a, st);
         case 4: return go_q4<2, 1, GROUP, PACK, WHOLE>(a, st);
