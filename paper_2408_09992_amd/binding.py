@@ -28,6 +28,14 @@ _lib = None
 _native_module = None
 
 
+class _Count:
+    """An int argument; what no int holds becomes the largest, which every call rejects (ctypes would cut it off)."""
+
+    @classmethod
+    def from_param(cls, n):
+        return ctypes.c_int(min(n, 2 ** 31 - 1))
+
+
 class PQError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -42,7 +50,7 @@ def lib() -> ctypes.CDLL:
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2408_09992_amd.build` "
                                "(there is no fallback path)")
         L = ctypes.CDLL(LIB_PATH)
-        P, I, LL, SZ = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_size_t
+        P, I, LL, SZ, C = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_size_t, _Count
         L.pq_subitem_scores.argtypes = [P, P, P, I, I, I, I, P]
         L.pq_subitem_scores.restype = I
         L.pq_score_topk_workspace_bytes.argtypes = [LL, I, I, I, I]
@@ -90,21 +98,21 @@ def lib() -> ctypes.CDLL:
         for width in ("", "_u16"):
             for call, pointers, outputs in (("pq_cross_entropy" + width, 3, 2), ("pq_cross_entropy" + width + "_backward", 5, 1)):
                 size = getattr(L, call + "_workspace_bytes")
-                size.argtypes, size.restype = [LL, I, I, I], SZ
-                getattr(L, call).argtypes = [P] * pointers + [LL, I, I, I] + [P] * outputs + [P, SZ, P]
+                size.argtypes, size.restype = [LL, C, C, C], SZ
+                getattr(L, call).argtypes = [P] * pointers + [LL, C, C, C] + [P] * outputs + [P, SZ, P]
                 getattr(L, call).restype = I
-        L.pq_subitem_scores_backward_workspace_bytes.argtypes = [I, I, I, I]
+        L.pq_subitem_scores_backward_workspace_bytes.argtypes = [C, C, C, C]
         L.pq_subitem_scores_backward_workspace_bytes.restype = SZ
-        L.pq_subitem_scores_backward.argtypes = [P, P, P, P, P, I, I, I, I, P, SZ, P]
+        L.pq_subitem_scores_backward.argtypes = [P, P, P, P, P, C, C, C, C, P, SZ, P]
         L.pq_subitem_scores_backward.restype = I
         for call in ("pq_default_cross_entropy", "pq_default_cross_entropy_backward"):
             size = getattr(L, call + "_workspace_bytes")
-            size.argtypes, size.restype = [LL, I, I, I], SZ
-            getattr(L, call).argtypes = [P] * (3 if call.endswith("entropy") else 5) + [LL, I, I, I, P, P, P, SZ, P]
+            size.argtypes, size.restype = [LL, C, C, C], SZ
+            getattr(L, call).argtypes = [P] * (3 if call.endswith("entropy") else 5) + [LL, C, C, C, P, P, P, SZ, P]
             getattr(L, call).restype = I
-        L.pq_quantise_items.argtypes = [P, LL, I, I, P, P, P]
+        L.pq_quantise_items.argtypes = [P, LL, C, C, P, P, P]
         L.pq_quantise_items.restype = I
-        L.pq_default_scores_q4.argtypes = [P, P, P, LL, I, I, I, P, LL, P]
+        L.pq_default_scores_q4.argtypes = [P, P, P, LL, C, C, C, P, LL, P]
         L.pq_default_scores_q4.restype = I
         L.pq_strerror.argtypes = [I]
         L.pq_strerror.restype = ctypes.c_char_p

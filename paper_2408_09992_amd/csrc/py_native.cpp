@@ -7,6 +7,8 @@
 // shape that disagrees) is answered with None, and binding.py's own code reports it.
 #include <Python.h>
 
+#include <limits.h>
+
 #include <ATen/core/Tensor.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/core/Allocator.h>
@@ -190,6 +192,9 @@ PyObject* score_topk_subset(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 // ---- the scoring head's training and its four-bit form
 
+// A size as the C ABI takes it.  One that no int holds becomes the largest, which every call rejects: cut off it might be a valid one.
+int narrow(int64_t n) { return n > INT_MAX ? INT_MAX : (int)n; }
+
 // An output of a call: the caller's tensor, checked, or one made here; bad: there is one and it does not fit.
 struct Output {
     PyObject* given = nullptr;
@@ -255,7 +260,7 @@ PyObject* cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t n) {
         if (!g || !S || g->dim() != 2 || S->dim() != 3 || S->size(1) != g->size(1) || !vector_of(t, S->size(0))) return none();
         const int64_t N = g->size(0), m = g->size(1), B = S->size(0), b = S->size(2);
         Output loss(args[4], {B}, at::kFloat, device), lse(args[5], {B}, at::kFloat, device);
-        Scratch ws(args[3], WIDE ? pq_cross_entropy_u16_workspace_bytes(N, (int)B, (int)m, (int)b) : pq_cross_entropy_workspace_bytes(N, (int)B, (int)m, (int)b), device);
+        Scratch ws(args[3], WIDE ? pq_cross_entropy_u16_workspace_bytes(N, narrow(B), narrow(m), narrow(b)) : pq_cross_entropy_workspace_bytes(N, narrow(B), narrow(m), narrow(b)), device);
         if (loss.bad || lse.bad || ws.bad) return none();
         const void* codes = g->const_data_ptr();
         const float* s = S->const_data_ptr<float>();
@@ -263,8 +268,8 @@ PyObject* cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t n) {
         float *l = loss.floats(), *e = lse.floats();
         void* st = current_stream();
         const int rc = without_gil([&]() {
-            return WIDE ? pq_cross_entropy_u16(static_cast<const uint16_t*>(codes), s, targets, N, (int)B, (int)m, (int)b, l, e, ws.p, ws.bytes, st)
-                        : pq_cross_entropy(static_cast<const uint8_t*>(codes), s, targets, N, (int)B, (int)m, (int)b, l, e, ws.p, ws.bytes, st);
+            return WIDE ? pq_cross_entropy_u16(static_cast<const uint16_t*>(codes), s, targets, N, narrow(B), narrow(m), narrow(b), l, e, ws.p, ws.bytes, st)
+                        : pq_cross_entropy(static_cast<const uint8_t*>(codes), s, targets, N, narrow(B), narrow(m), narrow(b), l, e, ws.p, ws.bytes, st);
         });
         return rc != PQ_OK ? PyLong_FromLong(rc) : pair(loss, lse);
     });
@@ -282,7 +287,7 @@ PyObject* cross_entropy_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
         const int64_t N = g->size(0), m = g->size(1), B = S->size(0), b = S->size(2);
         if (!vector_of(t, B) || !vector_of(e, B) || !vector_of(w, B)) return none();
         Output dS(args[6], S->sizes(), at::kFloat, device);
-        Scratch ws(args[5], WIDE ? pq_cross_entropy_u16_backward_workspace_bytes(N, (int)B, (int)m, (int)b) : pq_cross_entropy_backward_workspace_bytes(N, (int)B, (int)m, (int)b), device);
+        Scratch ws(args[5], WIDE ? pq_cross_entropy_u16_backward_workspace_bytes(N, narrow(B), narrow(m), narrow(b)) : pq_cross_entropy_backward_workspace_bytes(N, narrow(B), narrow(m), narrow(b)), device);
         if (dS.bad || ws.bad) return none();
         const void* codes = g->const_data_ptr();
         const float *s = S->const_data_ptr<float>(), *lse = e->const_data_ptr<float>(), *grad = w->const_data_ptr<float>();
@@ -290,8 +295,8 @@ PyObject* cross_entropy_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
         float* out = dS.floats();
         void* st = current_stream();
         const int rc = without_gil([&]() {
-            return WIDE ? pq_cross_entropy_u16_backward(static_cast<const uint16_t*>(codes), s, targets, lse, grad, N, (int)B, (int)m, (int)b, out, ws.p, ws.bytes, st)
-                        : pq_cross_entropy_backward(static_cast<const uint8_t*>(codes), s, targets, lse, grad, N, (int)B, (int)m, (int)b, out, ws.p, ws.bytes, st);
+            return WIDE ? pq_cross_entropy_u16_backward(static_cast<const uint16_t*>(codes), s, targets, lse, grad, N, narrow(B), narrow(m), narrow(b), out, ws.p, ws.bytes, st)
+                        : pq_cross_entropy_backward(static_cast<const uint8_t*>(codes), s, targets, lse, grad, N, narrow(B), narrow(m), narrow(b), out, ws.p, ws.bytes, st);
         });
         return rc != PQ_OK ? PyLong_FromLong(rc) : dS.object();
     });
@@ -307,12 +312,12 @@ PyObject* subitem_scores_backward(PyObject*, PyObject* const* args, Py_ssize_t n
         const int64_t B = q->size(0), d = q->size(1), m = c->size(0), b = c->size(1);
         if (m * c->size(2) != d || g->size(0) != B || g->size(1) != m || g->size(2) != b) return none();
         Output dq(args[4], q->sizes(), at::kFloat, device), dc(args[5], c->sizes(), at::kFloat, device);
-        Scratch ws(args[3], pq_subitem_scores_backward_workspace_bytes((int)B, (int)d, (int)m, (int)b), device);
+        Scratch ws(args[3], pq_subitem_scores_backward_workspace_bytes(narrow(B), narrow(d), narrow(m), narrow(b)), device);
         if (dq.bad || dc.bad || ws.bad) return none();
         const float *dS = g->const_data_ptr<float>(), *phi = q->const_data_ptr<float>(), *psi = c->const_data_ptr<float>();
         float *dphi = dq.floats(), *dpsi = dc.floats();
         void* st = current_stream();
-        const int rc = without_gil([&]() { return pq_subitem_scores_backward(dS, phi, psi, dphi, dpsi, (int)B, (int)d, (int)m, (int)b, ws.p, ws.bytes, st); });
+        const int rc = without_gil([&]() { return pq_subitem_scores_backward(dS, phi, psi, dphi, dpsi, narrow(B), narrow(d), narrow(m), narrow(b), ws.p, ws.bytes, st); });
         return rc != PQ_OK ? PyLong_FromLong(rc) : pair(dq, dc);
     });
 }
@@ -334,13 +339,13 @@ PyObject* default_cross_entropy(PyObject*, PyObject* const* args, Py_ssize_t n) 
         if (!W || !q || W->dim() != 2 || q->dim() != 2 || W->size(1) != q->size(1) || !vector_of(t, q->size(0))) return none();
         const int64_t N = W->size(0), d = W->size(1), B = q->size(0);
         Output loss(args[4], {B}, at::kFloat, device), lse(args[5], {B}, at::kFloat, device);
-        Scratch ws(args[3], pq_default_cross_entropy_workspace_bytes(N, (int)B, (int)d, type), device);
+        Scratch ws(args[3], pq_default_cross_entropy_workspace_bytes(N, narrow(B), narrow(d), type), device);
         if (loss.bad || lse.bad || ws.bad) return none();
         const void *w = W->const_data_ptr(), *h = q->const_data_ptr();
         const int* targets = t->const_data_ptr<int>();
         float *l = loss.floats(), *e = lse.floats();
         void* st = current_stream();
-        const int rc = without_gil([&]() { return pq_default_cross_entropy(w, h, targets, N, (int)B, (int)d, type, l, e, ws.p, ws.bytes, st); });
+        const int rc = without_gil([&]() { return pq_default_cross_entropy(w, h, targets, N, narrow(B), narrow(d), type, l, e, ws.p, ws.bytes, st); });
         return rc != PQ_OK ? PyLong_FromLong(rc) : pair(loss, lse);
     });
 }
@@ -360,7 +365,7 @@ PyObject* default_cross_entropy_backward(PyObject*, PyObject* const* args, Py_ss
         const int64_t N = W->size(0), d = W->size(1), B = q->size(0);
         if (!vector_of(t, B) || !vector_of(e, B) || !vector_of(g, B)) return none();
         Output dq(args[6], q->sizes(), scalar, device), dW(args[7], W->sizes(), scalar, device);
-        Scratch ws(args[5], pq_default_cross_entropy_backward_workspace_bytes(N, (int)B, (int)d, type), device);
+        Scratch ws(args[5], pq_default_cross_entropy_backward_workspace_bytes(N, narrow(B), narrow(d), type), device);
         if (dq.bad || dW.bad || ws.bad) return none();
         const void *w = W->const_data_ptr(), *h = q->const_data_ptr();
         const int* targets = t->const_data_ptr<int>();
@@ -368,7 +373,7 @@ PyObject* default_cross_entropy_backward(PyObject*, PyObject* const* args, Py_ss
         void *out_h = dq.t->mutable_data_ptr(), *out_w = dW.t->mutable_data_ptr();
         void* st = current_stream();
         const int rc = without_gil([&]() {
-            return pq_default_cross_entropy_backward(w, h, targets, lse, grad, N, (int)B, (int)d, type, out_h, out_w, ws.p, ws.bytes, st);
+            return pq_default_cross_entropy_backward(w, h, targets, lse, grad, N, narrow(B), narrow(d), type, out_h, out_w, ws.p, ws.bytes, st);
         });
         return rc != PQ_OK ? PyLong_FromLong(rc) : pair(dq, dW);
     });
@@ -396,7 +401,7 @@ PyObject* default_scores_q4(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const float* phi = q->const_data_ptr<float>();
         float* scores = out.floats();
         void* st = current_stream();
-        const int rc = without_gil([&]() { return pq_default_scores_q4(packed, scales, phi, N, (int)B, (int)d, (int)(d / groups), scores, ld, st); });
+        const int rc = without_gil([&]() { return pq_default_scores_q4(packed, scales, phi, N, narrow(B), narrow(d), narrow(d / groups), scores, ld, st); });
         return rc != PQ_OK ? PyLong_FromLong(rc) : out.object();
     });
 }

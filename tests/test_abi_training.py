@@ -68,6 +68,17 @@ def test_cross_entropy_by_sub_ids(lib, u16, backward):
         assert 16 <= need < 2 ** 33 and need % 16 == 0, (N, B, m, b)
 
 
+def test_python_cuts_no_count_off(pqlib_path):
+    from paper_2408_09992_amd import binding as pq
+    many = 2 ** 32 + 1                                           # (cut off to an int, one)
+    for size in (pq.pq_cross_entropy_workspace_bytes, pq.pq_cross_entropy_backward_workspace_bytes, pq.pq_cross_entropy_u16_workspace_bytes, pq.pq_cross_entropy_u16_backward_workspace_bytes):
+        assert size(100, 1, 8, 256) > 0 and size(100, many, 8, 256) == size(100, 1, many, 256) == size(100, 1, 8, many) == 0
+    for size in (pq.pq_default_cross_entropy_workspace_bytes, pq.pq_default_cross_entropy_backward_workspace_bytes):
+        assert size(100, 1, 64, F32) > 0 and size(100, many, 64, F32) == size(100, 1, 2 ** 32 + 64, F32) == size(100, 1, 64, 2 ** 32) == 0
+    size = pq.pq_subitem_scores_backward_workspace_bytes
+    assert size(4, 64, 4, 256) > 0 and size(many, 64, 4, 256) == size(4, 64, many, 256) == size(4, 64, 4, many) == 0
+
+
 def test_largest_tables_by_sub_ids(lib):
     for m, b in ((1, 36864), (2, 18432), (8, 4608), (9, 4096)):
         assert lib.pq_cross_entropy_u16_workspace_bytes(10 ** 5, 3, m, b) > 0 and lib.pq_cross_entropy_u16_backward_workspace_bytes(10 ** 5, 3, m, b) > 0, (m, b)

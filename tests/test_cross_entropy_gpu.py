@@ -365,3 +365,20 @@ def test_refusals_of_the_functions(pq):
     with pytest.raises(pq.PQError) as e:
         pq.pq_subitem_scores_backward(S, torch.zeros(3, 30, device="cuda"), torch.zeros(8, 256, 4, device="cuda"))
     assert e.value.code == pq.PQ_ERR_SHAPE
+
+
+def test_more_positions_than_an_int_counts(pq):
+    # 2^32 + 1 of them are not one (the tensors are 17 GB each, of which nothing is read)
+    B = 2 ** 32 + 1
+    codes = torch.zeros((10, 1), dtype=torch.uint8, device="cuda")
+    S, targets = torch.empty((B, 1, 1), device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")
+    with pytest.raises(pq.PQError) as e:
+        pq.pq_cross_entropy(codes, S, targets)
+    assert e.value.code == pq.PQ_ERR_UNSUPPORTED
+    H = S.view(B, 1)
+    with pytest.raises(pq.PQError) as e:
+        pq.pq_default_cross_entropy(torch.zeros((10, 1), device="cuda"), H, targets)
+    assert e.value.code == pq.PQ_ERR_UNSUPPORTED
+    with pytest.raises(pq.PQError) as e:
+        pq.pq_subitem_scores_backward(S, H, torch.zeros((1, 1, 1), device="cuda"))
+    assert e.value.code == pq.PQ_ERR_UNSUPPORTED
