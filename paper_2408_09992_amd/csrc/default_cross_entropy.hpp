@@ -228,8 +228,9 @@ __device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
 
 // The share of the gradient of a row's position: 0 where there is none, no target, no item in play or no position.
 __device__ __forceinline__ float row_weight(const DenseArgs& a, int row) {
-    const int q = position_of(a, row), t = row < dz_rows(a) ? a.targets[q] : -1;
-    return t >= 0 && t < a.N && a.lse_in[q] != -__builtin_inff() ? a.grad[q] : 0.0f;
+    const int q = min(position_of(a, row), a.B - 1), t = a.targets[q];
+    const float g = a.grad[q], lse = a.lse_in[q];              // (all three asked for at once)
+    return row < dz_rows(a) && t >= 0 && t < a.N && lse != -__builtin_inff() ? g : 0.0f;
 }
 // The queries in pieces of 16 bytes, from piece `first` on every `stride`-th, with zeros for positions that add nothing.
 // Float16: returns the power of two above these pieces' largest product of weight and query.
@@ -779,6 +780,7 @@ __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
     const int lead = threadIdx.x / 32;
     for (size_t first = (size_t)blockIdx.x * 32; first < n; first += (size_t)gridDim.x * 32) {
         const size_t i = first + threadIdx.x % 32;
+        const float factor = a.info[(uint32_t)min(i, n - 1) / (uint32_t)a.d].factor;
         float sum = 0.0f;
         if (i < n) {
 #pragma unroll 4
@@ -789,7 +791,7 @@ __global__ __launch_bounds__(256) void default_dh_join_kernel(DenseArgs a) {
         if (lead == 0 && i < n) {
 #pragma unroll
             for (int w = 1; w < 8; ++w) sum += part[w][threadIdx.x];
-            static_cast<T*>(a.dH)[i] = (T)(sum * a.info[(uint32_t)i / (uint32_t)a.d].factor);
+            static_cast<T*>(a.dH)[i] = (T)(sum * factor);
         }
         __syncthreads();
     }
