@@ -113,10 +113,10 @@ int pq_default_cross_entropy(const void* W, const void* queries, const int* targ
  *   lse  in  float [B]  as returned by pq_default_cross_entropy() for the same W and queries
  *   dqueries  out  type [B][d];  dW  out  type [N][d]  (both 16-byte aligned, every element written)
  * The items are taken in pieces whose dz fits the workspace (1 GB of it, or 2048 items of every position).  dz is
- * held in the inputs' type (for up to 32 positions of 16 bits together with what that rounding leaves).  For dqueries float16 keeps
- * probabilities down to 2^-39, however small a position's weight is beside others; for dW down to 2^-39 of a share of the largest
- * weight (up to 64 positions and 512 elements), or it keeps 2^-40 of the largest product of a weight and a query's element.  The
- * products' sums are float32, rounded to the type once.
+ * held in the inputs' type (for up to 32 positions of 16 bits together with what that rounding leaves).  Float16 keeps probabilities
+ * down to 2^-39 in dqueries, however small a position's weight is beside others.  In dW it keeps them down to 2^-39 times the
+ * largest weight over the position's own (up to 64 positions and 512 elements), or keeps the position's query elements down to
+ * 2^-39 of the largest product of a weight and an element.  The products' sums are float32, rounded to the type once.
  * Errors: as pq_default_cross_entropy().
  */
 size_t pq_default_cross_entropy_backward_workspace_bytes(long long N, int B, int d, int type);

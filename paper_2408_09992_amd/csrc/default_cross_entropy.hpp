@@ -21,7 +21,9 @@ constexpr int kItems = 256;                           // items of a block of dz,
 
 // Of a row of dz: 2^(z log2e - at) is p 2^15; its g over what dz is stored over; what its row of dH is multiplied with.  dz is stored over
 // the largest |g| of all positions, but in float16, whose exponents would not reach far below that (a position of a millionth of the
-// largest weight would keep probabilities down to 2^-19 alone), over the power of two above the position's own |g|.
+// largest weight would keep probabilities down to 2^-19 alone), over that times a power of two of the position's own: what is left
+// of its weight is over a half, and 1 where all weights are the same.  (Over powers of two alone the same mantissa would be rounded in all
+// rows, and with it the whole gradient be off by up to a unit.)
 struct RowInfo { float at, scale, factor; };
 template <typename T> constexpr bool kOwnPowers = std::is_same<T, _Float16>::value;
 
@@ -214,16 +216,22 @@ __device__ __forceinline__ int power_of(float x) {
     (void)frexpf(x, &e);
     return e;
 }
-// Of a gradient: 0 where it is no number.
-__device__ __forceinline__ int weight_power(float g) { return fabsf(g) < __builtin_inff() ? power_of(g) : 0; }
+// Of a weight over the largest: that its own |g| over it is above a half of, and at most; 0 where it is no number.
+__device__ __forceinline__ int weight_power(float over_top) {
+    if (!(fabsf(over_top) < __builtin_inff())) return 0;
+    int e;
+    return frexpf(fabsf(over_top), &e) == 0.5f ? e - 1 : e;
+}
 // What a gradient is to the largest of all: an infinite one is none, or it would be what all other positions are stored over.
 __device__ __forceinline__ float weight_size(float g) { return fabsf(g) < __builtin_inff() ? fabsf(g) : 0.0f; }
 // Of a position with gradient g (0: it adds nothing), the largest of all being top.
 template <typename T>
 __device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
     if (g == 0.0f) return RowInfo{__builtin_inff(), 0.0f, 0.0f};
-    if constexpr (kOwnPowers<T>) return RowInfo{lse * kLog2e - kDzBits, ldexpf(g, -weight_power(g)), ldexpf(1.0f / kDzScale, weight_power(g))};
-    else return RowInfo{lse * kLog2e - kDzBits, g / top, top / kDzScale};
+    if constexpr (kOwnPowers<T>) {
+        const int power = weight_power(g / top);
+        return RowInfo{lse * kLog2e - kDzBits, ldexpf(g / top, -power), top * ldexpf(1.0f / kDzScale, power)};
+    } else return RowInfo{lse * kLog2e - kDzBits, g / top, top / kDzScale};
 }
 
 // The share of the gradient of a row's position: 0 where there is none, no target, no item in play or no position.
@@ -233,10 +241,10 @@ __device__ __forceinline__ float row_weight(const DenseArgs& a, int row) {
     return row < dz_rows(a) && t >= 0 && t < a.N && lse != -__builtin_inff() ? g : 0.0f;
 }
 // The queries in pieces of 16 bytes, from piece `first` on every `stride`-th, with zeros for positions that add nothing.
-// Float16: returns the power of two above these pieces' largest product of weight and query.
+// Float16: returns the power of two above these pieces' largest product of a query's element and its position's power.
 constexpr int kNoPower = -100000;
 template <typename T>
-__device__ __forceinline__ int copy_live(const DenseArgs& a, size_t first, size_t stride) {
+__device__ __forceinline__ int copy_live(const DenseArgs& a, size_t first, size_t stride, float top = 0.0f) {
     const int row_pieces = a.d * (int)sizeof(T) / 16;
     const size_t pieces = (size_t)dz_rows(a) * row_pieces, position_pieces = (size_t)a.B * row_pieces;
     int power = kNoPower;
@@ -250,7 +258,7 @@ __device__ __forceinline__ int copy_live(const DenseArgs& a, size_t first, size_
             float largest = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf((float)h[e]) < __builtin_inff() ? fabsf((float)h[e]) : 0.0f);
-            if (largest > 0.0f) power = max(power, weight_power(g) + power_of(largest));
+            if (largest > 0.0f) power = max(power, weight_power(g / top) + power_of(largest));
         }
     }
     return power;
@@ -269,16 +277,11 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
     __shared__ float tops[16];
     __shared__ int powers[16];
     const int tid = threadIdx.x;
-    int power = wave_max(copy_live<T>(a, (size_t)blockIdx.x * 1024 + tid, (size_t)gridDim.x * 1024));
-    if constexpr (kOwnPowers<T>) {
-        if (tid % kWave == 0) powers[tid / kWave] = power;
-        __syncthreads();
-        if (tid < kWave) {
-            power = wave_max(powers[tid % 16]);
-            if (tid == 0) a.block_powers[blockIdx.x] = power;
-        }
+    const size_t first = (size_t)blockIdx.x * 1024 + tid, stride = (size_t)gridDim.x * 1024;
+    if constexpr (!kOwnPowers<T>) {
+        copy_live<T>(a, first, stride);
+        if (blockIdx.x != 0) return;
     }
-    if (blockIdx.x != 0) return;
     float top = 0.0f;
     for (int q = tid; q < a.B; q += 1024) top = fmaxf(top, weight_size(row_weight(a, q)));
     top = wave_top(top);
@@ -287,31 +290,42 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
     top = tops[0];
 #pragma unroll
     for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
+    if constexpr (kOwnPowers<T>) {
+        int power = wave_max(copy_live<T>(a, first, stride, top));
+        if (tid % kWave == 0) powers[tid / kWave] = power;
+        __syncthreads();
+        if (tid < kWave) {
+            power = wave_max(powers[tid % 16]);
+            if (tid == 0) a.block_powers[blockIdx.x] = power;
+        }
+        if (blockIdx.x != 0) return;
+    }
     for (int q = tid; q < a.padded; q += 1024) {
         a.info[q] = row_info<T>(row_weight(a, q), top, a.lse_in[min(position_of(a, q), a.B - 1)]);
     }
-    if (!kOwnPowers<T> && tid == 0) *a.factor = top / kDzScale;
+    if (tid == 0) a.factor[kOwnPowers<T> ? 1 : 0] = kOwnPowers<T> ? top : top / kDzScale;
 }
 
 // Float16: the queries that dW is made of, each times the power of two that its position's dz was stored over, and all times the one that
-// brings the largest below 2^15.  So what float16 cannot hold of a small weight's queries is 2^-40 of the largest product of weight and query.
+// brings the largest below 2^15 (factor[1]: the largest weight).  So what float16 cannot hold of a small weight's queries is 2^-40 of the largest product of weight and query.
 template <typename T>
 __global__ __launch_bounds__(1024) void scale_rows_kernel(DenseArgs a) {
     const int lane = threadIdx.x % kWave;
     int power = kNoPower;
     for (int i = lane; i < (int)gridDim.x; i += kWave) power = max(power, a.block_powers[i]);          // (as many blocks made them)
     power = wave_max(power);
+    const float top = a.factor[1];
     const int row_pieces = a.d * (int)sizeof(T) / 16;
     const size_t pieces = (size_t)dz_rows(a) * row_pieces;
     for (size_t i = (size_t)blockIdx.x * 1024 + threadIdx.x; i < pieces; i += (size_t)gridDim.x * 1024) {
         f16x8 h = static_cast<const f16x8*>(a.live)[i];
         const float g = row_weight(a, (int)(i / row_pieces));
-        const int by = g == 0.0f ? 0 : weight_power(g) + 15 - power;
+        const int by = g == 0.0f ? 0 : weight_power(g / top) + 15 - power;
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] = (_Float16)ldexpf((float)h[e], by);
         static_cast<f16x8*>(a.scaled)[i] = h;
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.factor = power == kNoPower ? 0.0f : ldexpf(1.0f, power - 30);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.factor = power == kNoPower ? 0.0f : ldexpf(top, power - 30);
 }
 
 // Blocks of 32 x 32 results leave through the wave's LDS, N of them at a time, in rows of 16-byte pieces: row lane % 32 of a block

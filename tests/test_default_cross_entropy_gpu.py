@@ -271,6 +271,22 @@ def test_up_to_32_positions_lose_nothing_to_a_rounded_dz(pq, N, d, B, type):
         assert ((got.double() - want).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("type", ["bf16", "f16"])
+@pytest.mark.parametrize("weight", [1 / 501, 1 / 110, 1 / 103, 1 / 108, 1.0, 3.0])
+@pytest.mark.parametrize("N,d,B", [(5000, 256, 501), (5000, 128, 110), (3000, 512, 50), (3000, 64, 64), (700, 520, 40), (2000, 64, 20)])
+def test_one_weight_for_all_adds_no_error_of_its_own(pq, N, d, B, type, weight):
+    # The mean square of a gradient's error is that of its own rounding, and of as many independent roundings of dz: below twice the first.
+    # (A weight rounded alike in every row of dz would be a common factor.)  A tenth more for what 32 bits do and the draw.
+    W, H, targets, grad = draw(N, d, B, type, seed=N + d + B)
+    grad.fill_(weight)
+    loss, lse = pq.pq_default_cross_entropy(W, H, targets)
+    dH, dW = pq.pq_default_cross_entropy_backward(W, H, targets, lse, grad)
+    p, dz, want_h, want_w, rel = gradients_in_64_bits(W, H, targets, grad)
+    for got, want in ((dH, want_h), (dW, want_w)):
+        own = want.to(W.dtype).double() - want
+        assert (got.double() - want).square().sum() <= 1.1 * 2 * own.square().sum()
+
+
 def test_gradients_against_differences(pq):
     # float32; see the sub-ids' test: directions that move no score by more than 1
     N, d, B = 3000, 64, 9
