@@ -112,7 +112,8 @@ int pq_default_cross_entropy(const void* W, const void* queries, const int* targ
  *     dz_qi = grad_loss[q] * (exp(r_qi - lse_q) - [i = t_q])     dqueries = dz W     dW = dz^T queries
  *   lse  in  float [B]  as returned by pq_default_cross_entropy() for the same W and queries
  *   dqueries  out  type [B][d];  dW  out  type [N][d]  (both 16-byte aligned, every element written)
- * The items are taken in pieces whose dz fits the workspace (1 GB of it, or 2048 items of every position).  dz is
+ * The items are taken in pieces whose dz fits the workspace: about 1 GB of it (at most a third more, where positions are padded;
+ * a quarter for 16-bit rows of up to 64 elements), or 2048 items of every position.  dz is
  * held in the inputs' type (for up to 32 positions of 16 bits together with what that rounding leaves).  Float16 keeps probabilities
  * down to 2^-39 in dqueries, however small a position's weight is beside others.  In dW it keeps them down to 2^-39 times the
  * largest weight over the position's own (up to 64 positions and 512 elements), or keeps the position's query elements down to

@@ -135,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void subitem_scores_backward_kernel(GradA
 
 // Many queries: tiles of 64 x 64 through LDS (matrix_tile.hpp), those of dcentroids summed over a share of the queries each.
 // Products of float32 in three bfloat16 pieces a factor.  8192 queries (d = 512, m = 8, b = 256; 84 MB of tables and queries):
-// 46 us, 1.8 TB/s; fewer are bound by the latency of a share's few stages and of the second launch.
+// 43 us, 2.0 TB/s (40 without the join); fewer are bound by the latency of a share's few stages and of the second launch.
 using TileQ = MatrixTile<float, 64, 64, 32, 32, true, false>;
 using TileC = MatrixTile<float, 64, 64, 32, 32, false, false>;
 constexpr int kSide = 64;
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(256) void subitem_scores_backward_join_kernel(GradA
 }
 
 // From how many queries on the tiles pay (both ways, d = 512, m = 8, b = 256: 256 queries 6.6 us without them, 10.0 with;
-// 1024 15.4 and 15.6; 2048 27.2 and 17.6; 8192 97 and 46).
+// 1024 15.4 and 15.6; 2048 27.2 and 17.5; 8192 97 and 43).
 constexpr int kTilesMinQueries = 1024;
 // Shares of the queries: as many as bring workgroups for half the chip, of 128 queries at least.
 int shares_of(int B, int m, int b, int s) {
