@@ -105,6 +105,7 @@ __device__ __forceinline__ Operand positions_of(const DenseArgs& a, int position
 // leaves.  A row of dqueries is then (and a row of dW may be) little more than one value of dz times one row, whose error that
 // rounding would double (one position, 17,902 items of 64 float16: dW 4.4e-5 off instead of 2.8e-5).  Tiles have 64 rows anyway.  With more
 // positions the errors of their rows are independent: together with the result's own rounding at most sqrt(2) of it in the mean square.
+// (Positions that share a weight share its rounding too, where it is no power of two of the largest.)
 constexpr int kTwoParts = 32;
 __device__ __forceinline__ int dz_rows(const DenseArgs& a) { return a.B * a.parts; }
 __device__ __forceinline__ int position_of(const DenseArgs& a, int row) { return row < a.B ? row : row - a.B; }
@@ -216,13 +217,13 @@ __device__ __forceinline__ int power_of(float x) {
     (void)frexpf(x, &e);
     return e;
 }
-// Of a weight over the largest: that its own |g| over it is above a half of, and at most; 0 where it is no number.
+// The power of two that a weight over the largest is more than half of, and at most; 0 where it is no number.
 __device__ __forceinline__ int weight_power(float over_top) {
     if (!(fabsf(over_top) < __builtin_inff())) return 0;
     int e;
     return frexpf(fabsf(over_top), &e) == 0.5f ? e - 1 : e;
 }
-// What a gradient is to the largest of all: an infinite one is none, or it would be what all other positions are stored over.
+// What a number is to the largest of its kind: an infinite one is none.  (As a weight it would be what all other positions are stored over.)
 __device__ __forceinline__ float weight_size(float g) { return fabsf(g) < __builtin_inff() ? fabsf(g) : 0.0f; }
 // Of a position with gradient g (0: it adds nothing), the largest of all being top.
 template <typename T>
@@ -257,7 +258,7 @@ __device__ __forceinline__ int copy_live(const DenseArgs& a, size_t first, size_
             const f16x8 h = __builtin_bit_cast(f16x8, v);
             float largest = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf((float)h[e]) < __builtin_inff() ? fabsf((float)h[e]) : 0.0f);
+            for (int e = 0; e < 8; ++e) largest = fmaxf(largest, weight_size((float)h[e]));
             if (largest > 0.0f) power = max(power, weight_power(g / top) + power_of(largest));
         }
     }
