@@ -110,6 +110,21 @@ def lib() -> ctypes.CDLL:
             size.argtypes, size.restype = [LL, C, C, C], SZ
             getattr(L, call).argtypes = [P] * (3 if call.endswith("entropy") else 5) + [LL, C, C, C, P, P, P, SZ, P]
             getattr(L, call).restype = I
+        F = ctypes.c_float
+        for width in ("", "_u16"):
+            for call, sizes, args in (("pq_log_probs", 4, [P] * 3 + [LL] + [C] * 5 + [F] + [P] * 6),
+                                      ("pq_distillation", 4, [P] * 4 + [LL] + [C] * 4 + [F] + [P] * 3),
+                                      ("pq_distillation_backward", 4, [P] * 6 + [LL] + [C] * 4 + [F] + [P] * 2)):
+                call = call.replace("_backward", "") + width + ("_backward" if call.endswith("_backward") else "")
+                getattr(L, call + "_workspace_bytes").argtypes = [LL] + [C] * sizes
+                getattr(L, call + "_workspace_bytes").restype = SZ
+                getattr(L, call).argtypes, getattr(L, call).restype = args + [SZ, P], I
+        for call, args in (("pq_default_log_probs", [P] * 3 + [LL] + [C] * 5 + [F] + [P] * 6),
+                           ("pq_default_distillation", [P] * 4 + [LL] + [C] * 4 + [F] + [P] * 3),
+                           ("pq_default_distillation_backward", [P] * 6 + [LL] + [C] * 4 + [F] + [P] * 3)):
+            getattr(L, call + "_workspace_bytes").argtypes = [LL] + [C] * 4
+            getattr(L, call + "_workspace_bytes").restype = SZ
+            getattr(L, call).argtypes, getattr(L, call).restype = args + [SZ, P], I
         L.pq_quantise_items.argtypes = [P, LL, C, C, P, P, P]
         L.pq_quantise_items.restype = I
         L.pq_default_scores_q4.argtypes = [P, P, P, LL, C, C, C, P, LL, P]
@@ -698,6 +713,200 @@ def pq_subitem_scores_backward(dS: torch.Tensor, queries: torch.Tensor, centroid
     if rc != PQ_OK:
         raise PQError(rc, "pq_subitem_scores_backward")
     return dqueries, dcentroids
+
+
+def _lists(t: torch.Tensor, B: int, dtype: torch.dtype, what: str) -> torch.Tensor:
+    _dev(t, dtype, what)
+    if t.dim() != 2 or t.shape[0] != B:
+        raise ValueError(f"{what} must have a row per position")
+    return t
+
+
+def _output(t: Optional[torch.Tensor], shape, dtype: torch.dtype, like: torch.Tensor, what: str) -> torch.Tensor:
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _dev(t, dtype, what)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must have the shape {tuple(shape)}")
+    return t
+
+
+def _head_shape(entry: str, dense: bool, code_type, first, second):
+    """(N, B and the sizes between them and n or K) of a call by sub-ids (codes, S) or by the default scorer (W, queries)."""
+    if dense:
+        if first.dtype not in _TYPES:
+            raise ValueError("W must be float32, bfloat16 or float16")
+        _dev(first, first.dtype, "W"), _dev(second, first.dtype, "queries")
+        if first.dim() != 2 or second.dim() != 2 or first.shape[1] != second.shape[1]:
+            raise PQError(PQ_ERR_SHAPE, entry)
+        return first.shape[0], second.shape[0], (first.shape[1], _TYPES[first.dtype])
+    _dev(first, code_type, "codes"), _dev(second, torch.float32, "S")
+    if first.dim() != 2 or second.dim() != 3 or second.shape[1] != first.shape[1]:
+        raise PQError(PQ_ERR_SHAPE, entry)
+    return first.shape[0], second.shape[0], (first.shape[1], second.shape[2])
+
+
+def _call(entry: str, first: torch.Tensor, *args) -> None:
+    with torch.cuda.device(first.device):                          # (the stream is the one current there)
+        rc = getattr(lib(), entry)(*args, _stream())
+    if rc != PQ_OK:
+        raise PQError(rc, entry)
+
+
+def _log_probs(entry, dense, code_type, first, second, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs):
+    N, B, sizes = _head_shape(entry, dense, code_type, first, second)
+    if items is None:
+        items = torch.empty((B, 0), dtype=torch.int32, device=first.device)
+    n, K = _lists(items, B, torch.int32, "items").shape[1], int(K)
+    if K < 0:
+        raise PQError(PQ_ERR_SHAPE, entry)
+    log_probs = _output(log_probs, (B, n), torch.float32, first, "log_probs")
+    entropy, lse = _output(entropy, (B,), torch.float32, first, "entropy"), _output(lse, (B,), torch.float32, first, "lse")
+    workspace = _scratch(workspace, int(getattr(lib(), entry + "_workspace_bytes")(N, B, *sizes, K)), first)
+    top_items = _output(top_items, (B, K), torch.int32, first, "top_items")
+    top_log_probs = _output(top_log_probs, (B, K), torch.float32, first, "top_log_probs")
+    _same_device(first, second, items, workspace, log_probs, entropy, lse, top_items, top_log_probs)
+    _call(entry, first, first.data_ptr(), second.data_ptr(), items.data_ptr(), N, B, *sizes, n, K, temperature, log_probs.data_ptr(), entropy.data_ptr(),
+          lse.data_ptr(), top_items.data_ptr(), top_log_probs.data_ptr(), workspace.data_ptr(), workspace.numel())
+    return log_probs, entropy, lse, top_items, top_log_probs
+
+
+def _distillation(entry, dense, code_type, first, second, teacher_items, teacher_scores, temperature, workspace, loss, lse):
+    N, B, sizes = _head_shape(entry, dense, code_type, first, second)
+    K = _lists(teacher_items, B, torch.int32, "teacher_items").shape[1]
+    if _lists(teacher_scores, B, torch.float32, "teacher_scores").shape[1] != K:
+        raise ValueError("teacher_scores must have a score per item")
+    loss, lse = _output(loss, (B,), torch.float32, first, "loss"), _output(lse, (B,), torch.float32, first, "lse")
+    workspace = _scratch(workspace, int(getattr(lib(), entry + "_workspace_bytes")(N, B, *sizes, K)), first)
+    _same_device(first, second, teacher_items, teacher_scores, loss, lse, workspace)
+    _call(entry, first, first.data_ptr(), second.data_ptr(), teacher_items.data_ptr(), teacher_scores.data_ptr(), N, B, *sizes, K, temperature,
+          loss.data_ptr(), lse.data_ptr(), workspace.data_ptr(), workspace.numel())
+    return loss, lse
+
+
+def _distillation_backward(entry, dense, code_type, first, second, teacher_items, teacher_scores, lse, grad_loss, temperature, workspace, *outputs):
+    N, B, sizes = _head_shape(entry, dense, code_type, first, second)
+    K = _lists(teacher_items, B, torch.int32, "teacher_items").shape[1]
+    if _lists(teacher_scores, B, torch.float32, "teacher_scores").shape[1] != K:
+        raise ValueError("teacher_scores must have a score per item")
+    _per_position(lse, B, first, "lse"), _per_position(grad_loss, B, first, "grad_loss")
+    shapes = ((second, "dqueries"), (first, "dW")) if dense else ((second, "dS"),)
+    outputs = [_output(out, like.shape, like.dtype, first, what) for out, (like, what) in zip(outputs, shapes)]
+    workspace = _scratch(workspace, int(getattr(lib(), entry + "_workspace_bytes")(N, B, *sizes, K)), first)
+    _same_device(first, second, teacher_items, teacher_scores, lse, grad_loss, workspace, *outputs)
+    _call(entry, first, first.data_ptr(), second.data_ptr(), teacher_items.data_ptr(), teacher_scores.data_ptr(), lse.data_ptr(), grad_loss.data_ptr(), N, B,
+          *sizes, K, temperature, *(out.data_ptr() for out in outputs), workspace.data_ptr(), workspace.numel())
+    return tuple(outputs) if dense else outputs[0]
+
+
+_Probs = Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]
+
+
+def pq_log_probs_workspace_bytes(N: int, B: int, m: int, b: int, K: int) -> int:
+    return int(lib().pq_log_probs_workspace_bytes(N, B, m, b, K))
+
+
+def pq_log_probs(codes: torch.Tensor, S: torch.Tensor, items: Optional[torch.Tensor] = None, K: int = 0, temperature: float = 1.0,
+                 workspace: Optional[torch.Tensor] = None, log_probs: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, top_items: Optional[torch.Tensor] = None, top_log_probs: Optional[torch.Tensor] = None) -> _Probs:
+    """What the softmax of the whole catalogue's scores over `temperature` says, by sub-ids: codes uint8 [N][m], S [B][m][b], items int32 [B][n] or
+    None (an id outside [0, N): no item, log-probability 0) -> (log_probs fp32 [B][n], entropy [B], lse [B], and of the K likeliest items
+    top_items int32 [B][K] and top_log_probs [B][K])."""
+    return _log_probs("pq_log_probs", False, torch.uint8, codes, S, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs)
+
+
+def pq_log_probs_u16_workspace_bytes(N: int, B: int, m: int, b: int, K: int) -> int:
+    return int(lib().pq_log_probs_u16_workspace_bytes(N, B, m, b, K))
+
+
+def pq_log_probs_u16(codes: torch.Tensor, S: torch.Tensor, items: Optional[torch.Tensor] = None, K: int = 0, temperature: float = 1.0,
+                     workspace: Optional[torch.Tensor] = None, log_probs: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, top_items: Optional[torch.Tensor] = None, top_log_probs: Optional[torch.Tensor] = None) -> _Probs:
+    """pq_log_probs over 16-bit sub-ids: codes uint16 [N][m]."""
+    return _log_probs("pq_log_probs_u16", False, torch.uint16, codes, S, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs)
+
+
+def pq_default_log_probs_workspace_bytes(N: int, B: int, d: int, type: int, K: int) -> int:
+    return int(lib().pq_default_log_probs_workspace_bytes(N, B, d, type, K))
+
+
+def pq_default_log_probs(W: torch.Tensor, queries: torch.Tensor, items: Optional[torch.Tensor] = None, K: int = 0, temperature: float = 1.0,
+                         workspace: Optional[torch.Tensor] = None, log_probs: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                         lse: Optional[torch.Tensor] = None, top_items: Optional[torch.Tensor] = None, top_log_probs: Optional[torch.Tensor] = None
+                         ) -> _Probs:
+    """pq_log_probs by the default scorer: W [N][d], queries [B][d] (both fp32, bf16 or fp16).  The K likeliest items and the given ones are scored in
+    64 bits."""
+    return _log_probs("pq_default_log_probs", True, None, W, queries, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs)
+
+
+def pq_distillation_workspace_bytes(N: int, B: int, m: int, b: int, K: int) -> int:
+    return int(lib().pq_distillation_workspace_bytes(N, B, m, b, K))
+
+
+def pq_distillation(codes: torch.Tensor, S: torch.Tensor, teacher_items: torch.Tensor, teacher_scores: torch.Tensor, temperature: float = 1.0,
+                    workspace: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
+                    ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Distillation by sub-ids: temperature^2 times the divergence of the catalogue's softmax from a teacher's list, teacher_items int32 [B][K] (an id
+    outside [0, N): no entry) with teacher_scores fp32 [B][K], whose softmax over the list are the weights -> (loss fp32 [B], lse fp32 [B])."""
+    return _distillation("pq_distillation", False, torch.uint8, codes, S, teacher_items, teacher_scores, temperature, workspace, loss, lse)
+
+
+def pq_distillation_backward_workspace_bytes(N: int, B: int, m: int, b: int, K: int) -> int:
+    return int(lib().pq_distillation_backward_workspace_bytes(N, B, m, b, K))
+
+
+def pq_distillation_backward(codes: torch.Tensor, S: torch.Tensor, teacher_items: torch.Tensor, teacher_scores: torch.Tensor, lse: torch.Tensor,
+                             grad_loss: torch.Tensor, temperature: float = 1.0, workspace: Optional[torch.Tensor] = None,
+                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of sum(grad_loss * loss) with respect to S: lse as pq_distillation returned it -> dS fp32 [B][m][b]."""
+    return _distillation_backward("pq_distillation_backward", False, torch.uint8, codes, S, teacher_items, teacher_scores, lse, grad_loss, temperature,
+                                  workspace, out)
+
+
+def pq_distillation_u16_workspace_bytes(N: int, B: int, m: int, b: int, K: int) -> int:
+    return int(lib().pq_distillation_u16_workspace_bytes(N, B, m, b, K))
+
+
+def pq_distillation_u16(codes: torch.Tensor, S: torch.Tensor, teacher_items: torch.Tensor, teacher_scores: torch.Tensor, temperature: float = 1.0,
+                        workspace: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
+                        ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """pq_distillation over 16-bit sub-ids: codes uint16 [N][m]."""
+    return _distillation("pq_distillation_u16", False, torch.uint16, codes, S, teacher_items, teacher_scores, temperature, workspace, loss, lse)
+
+
+def pq_distillation_u16_backward_workspace_bytes(N: int, B: int, m: int, b: int, K: int) -> int:
+    return int(lib().pq_distillation_u16_backward_workspace_bytes(N, B, m, b, K))
+
+
+def pq_distillation_u16_backward(codes: torch.Tensor, S: torch.Tensor, teacher_items: torch.Tensor, teacher_scores: torch.Tensor, lse: torch.Tensor,
+                                 grad_loss: torch.Tensor, temperature: float = 1.0, workspace: Optional[torch.Tensor] = None,
+                                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """pq_distillation_backward over 16-bit sub-ids: codes uint16 [N][m]."""
+    return _distillation_backward("pq_distillation_u16_backward", False, torch.uint16, codes, S, teacher_items, teacher_scores, lse, grad_loss, temperature,
+                                  workspace, out)
+
+
+def pq_default_distillation_workspace_bytes(N: int, B: int, d: int, type: int, K: int) -> int:
+    return int(lib().pq_default_distillation_workspace_bytes(N, B, d, type, K))
+
+
+def pq_default_distillation(W: torch.Tensor, queries: torch.Tensor, teacher_items: torch.Tensor, teacher_scores: torch.Tensor, temperature: float = 1.0,
+                            workspace: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
+                            ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """pq_distillation by the default scorer: W [N][d], queries [B][d] (both fp32, bf16 or fp16)."""
+    return _distillation("pq_default_distillation", True, None, W, queries, teacher_items, teacher_scores, temperature, workspace, loss, lse)
+
+
+def pq_default_distillation_backward_workspace_bytes(N: int, B: int, d: int, type: int, K: int) -> int:
+    return int(lib().pq_default_distillation_backward_workspace_bytes(N, B, d, type, K))
+
+
+def pq_default_distillation_backward(W: torch.Tensor, queries: torch.Tensor, teacher_items: torch.Tensor, teacher_scores: torch.Tensor, lse: torch.Tensor,
+                                     grad_loss: torch.Tensor, temperature: float = 1.0, workspace: Optional[torch.Tensor] = None,
+                                     dqueries: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Gradients of sum(grad_loss * loss) with respect to queries and W, in their type: lse as pq_default_distillation returned it."""
+    return _distillation_backward("pq_default_distillation_backward", True, None, W, queries, teacher_items, teacher_scores, lse, grad_loss, temperature,
+                                  workspace, dqueries, dW)
 
 
 def pq_score_topk_profile(codes: torch.Tensor, S: torch.Tensor, K: int, iters: int,

@@ -25,6 +25,8 @@ constexpr double kTileStart = 0.1;                     // what a workgroup takes
 
 int size_of(int type) { return type == PQ_FLOAT32 ? 4 : type == PQ_BFLOAT16 || type == PQ_FLOAT16 ? 2 : 0; }
 
+}  // namespace
+
 DensePlan plan_dense(long long N, int B, int d, int type) {
     DensePlan p;
     const int size = size_of(type);
@@ -121,6 +123,21 @@ int check_dense(long long N, int B, int d, int type) {
     return PQ_OK;
 }
 
+// What the gradient's kernels have in the workspace.
+void set_gradient(DenseArgs& a, const DensePlan& p, void* workspace) {
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    a.factor = reinterpret_cast<float*>(ws);
+    a.block_powers = reinterpret_cast<int*>(ws + 256);
+    a.info = reinterpret_cast<RowInfo*>(ws + p.info_at);
+    a.live = ws + p.live_at;
+    a.scaled = ws + p.scaled_at;
+    a.dz = ws + p.dz_at;
+    a.partial_h = reinterpret_cast<float*>(ws + p.partial_at);
+    a.parts = p.parts; a.piece = p.piece; a.padded = p.padded; a.slices = p.slices;
+}
+
+namespace {
+
 size_t loss_bytes(const DensePlan& p, int B) { return round_up((size_t)p.groups * B * sizeof(float2), 16); }
 
 }  // namespace
@@ -144,7 +161,7 @@ int pq_default_cross_entropy(const void* W, const void* queries, const int* targ
     const DensePlan p = plan_dense(N, B, d, type);
     if (workspace_bytes < loss_bytes(p, B)) return PQ_ERR_WORKSPACE;
     DenseArgs a{};
-    a.W = W; a.H = queries; a.targets = targets; a.N = N; a.B = B; a.d = d;
+    a.W = W; a.H = queries; a.targets = targets; a.N = N; a.B = B; a.d = d; a.scale = kLog2e;
     a.item_tiles = p.item_tiles; a.tiles_each = p.tiles_each; a.groups = p.groups; a.position_tiles = p.position_tiles;
     a.partial = static_cast<float2*>(workspace); a.loss = loss; a.lse = lse;
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -170,18 +187,10 @@ int pq_default_cross_entropy_backward(const void* W, const void* queries, const 
         return PQ_ERR_ALIGN;
     const DensePlan p = plan_dense(N, B, d, type);
     if (workspace_bytes < p.bytes) return PQ_ERR_WORKSPACE;
-    unsigned char* ws = static_cast<unsigned char*>(workspace);
     DenseArgs a{};
-    a.W = W; a.H = queries; a.targets = targets; a.N = N; a.B = B; a.d = d;
+    a.W = W; a.H = queries; a.targets = targets; a.N = N; a.B = B; a.d = d; a.scale = kLog2e;
     a.lse_in = lse; a.grad = grad_loss; a.dH = dqueries; a.dW = dW;
-    a.factor = reinterpret_cast<float*>(ws);
-    a.block_powers = reinterpret_cast<int*>(ws + 256);
-    a.info = reinterpret_cast<RowInfo*>(ws + p.info_at);
-    a.live = ws + p.live_at;
-    a.scaled = ws + p.scaled_at;
-    a.dz = ws + p.dz_at;
-    a.partial_h = reinterpret_cast<float*>(ws + p.partial_at);
-    a.parts = p.parts; a.piece = p.piece; a.padded = p.padded; a.slices = p.slices;
+    set_gradient(a, p, workspace);
     hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e;
     if (type == PQ_FLOAT32) e = dense_backward<float>(p, a, st);

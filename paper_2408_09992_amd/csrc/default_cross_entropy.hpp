@@ -19,7 +19,7 @@ constexpr float kHeadroom = 40.0f;                    // (log2) how far a score 
 constexpr float kDzBits = 15.0f, kDzScale = 32768.0f;  // dz is stored times 2^15 over a weight (RowInfo): types keep small probabilities
 constexpr int kItems = 256;                           // items of a block of dz, and of most tiles of z and dW
 
-// Of a row of dz: 2^(z log2e - at) is p 2^15; its g over what dz is stored over; what its row of dH is multiplied with.  dz is stored over
+// Of a row of dz: 2^(z scale - at) is p 2^15; its g over what dz is stored over; what its row of dH is multiplied with.  dz is stored over
 // the largest |g| of all positions, but in float16, whose exponents would not reach far below that (a position of a millionth of the
 // largest weight would keep probabilities down to 2^-19 alone), over that times a power of two of the position's own: what is left
 // of its weight is over a half, and 1 where all weights are the same.  (Over powers of two alone the same mantissa would be rounded in all
@@ -90,7 +90,15 @@ struct DenseArgs {
     int padded, slices, slice_items, more;             // rows of dz padded; shares of a piece's items; partial_h holds earlier pieces
     int tiles_m, tiles_n;                              // of the launch
     int h_rows, h_cols, w_blocks;                      // tiles of dH; workgroups that make dW, where one launch makes both
+    float scale;                                       // what scores are multiplied with: log2 e over the temperature
+    // distillation: a position's gradient over its dz (0: it adds nothing; NULL: grad of those that have targets), and the entries of its
+    // list, by item (kNoItem after the last): what p less the teacher's probability is there
+    const float* share;
+    const int* entry_items;                            // [B][entries]
+    const float* entry_values;
+    int entries;
 };
+constexpr int kNoItem = 0x7FFFFFFF;
 
 template <typename T>
 __device__ __forceinline__ Operand items_of(const DenseArgs& a, long long item) {
@@ -148,7 +156,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
             for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[mi][ni][e]);
-            top *= kLog2e;
+            top *= a.scale;
             if (__any(top > c[ni] + kHeadroom)) {
                 if (top > c[ni] + kHeadroom) raise_reference(c[ni], s[ni], top);
             }
@@ -156,7 +164,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
 #pragma unroll
             for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum += exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -c[ni]));
+                for (int e = 0; e < 16; ++e) sum += exp2_fast(fmaf(acc[mi][ni][e], a.scale, -c[ni]));
             s[ni] += sum;
         }
     }
@@ -237,7 +245,9 @@ __device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
 
 // The share of the gradient of a row's position: 0 where there is none, no target, no item in play or no position.
 __device__ __forceinline__ float row_weight(const DenseArgs& a, int row) {
-    const int q = min(position_of(a, row), a.B - 1), t = a.targets[q];
+    const int q = min(position_of(a, row), a.B - 1);
+    if (a.share) return row < dz_rows(a) ? a.share[q] : 0.0f;
+    const int t = a.targets[q];
     const float g = a.grad[q], lse = a.lse_in[q];              // (all three asked for at once)
     return row < dz_rows(a) && t >= 0 && t < a.N && lse != -__builtin_inff() ? g : 0.0f;
 }
@@ -401,14 +411,14 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
         if constexpr (ROWS) info = RowInfo{__shfl(own_row.at, q0 + lane % 32), __shfl(own_row.scale, q0 + lane % 32)};
         else info = a.info[q];
         const bool rest = kParts && q >= a.B;
-        const long long from_first = (q < (kParts ? dz_rows(a) : a.B) ? (long long)a.targets[rest ? q - a.B : q] : -1) - item0 - Tile::wave_row();
+        const long long from_first = (a.targets && q < (kParts ? dz_rows(a) : a.B) ? (long long)a.targets[rest ? q - a.B : q] : -1) - item0 - Tile::wave_row();
         const int hit = from_first >= 0 && from_first < 32 * MI ? (int)from_first - 4 * (lane / 32) : -64;
         const bool special = __any(hit > -64) || left < 32 * MI - 4;           // (rare: a target among these items, the catalogue's end)
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const float p = exp2_fast(fmaf(acc[mi][ni][e], kLog2e, -info.at));
+                const float p = exp2_fast(fmaf(acc[mi][ni][e], a.scale, -info.at));
                 acc[mi][ni][e] = ROWS && info.at == __builtin_inff() ? 0.0f : p;       // (its query may be NaN: not a copy that is zeros)
             }
         if (special) {
@@ -443,6 +453,22 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
                                              *reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(out + (size_t)row * kItems + 32 * (mi + k)) + piece * 16) = v;
                                          });
     }
+}
+
+// Distillation: dz of the lists' items in a piece, in the place of what default_dz_kernel left there.  A thread an entry; an item that is
+// listed twice has the same value in both.
+template <typename T>
+__global__ __launch_bounds__(256) void teacher_dz_kernel(DenseArgs a) {
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (size_t)a.B * a.entries) return;
+    const int q = (int)(i / a.entries), item = a.entry_items[i];
+    if (item == kNoItem || item < a.first_item || item >= a.first_item + a.items) return;
+    const int at = (int)(item - a.first_item);
+    T* out = static_cast<T*>(a.dz) + ((size_t)(at / kItems) * a.padded + q) * kItems + at % kItems;
+    const float x = a.entry_values[i] * kDzScale, scale = a.info[q].scale;
+    const T v = (T)(x * scale);
+    out[0] = v;
+    if (a.parts > 1) out[(size_t)a.B * kItems] = (T)fmaf(x, scale, -(float)v);
 }
 
 // A tile of dW of a piece: [items][d], summed over dz's rows.  As many: 133 to 145 us, about 1000 TFLOP/s.
@@ -620,13 +646,13 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseA
                 for (int e = 0; e < 4; ++e)
                     if (e >= left) z[e] = -__builtin_inff();
             }
-            const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) * kLog2e;
+            const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) * a.scale;
             const int part = i % kParts;
             if (__any(top > c[part] + kHeadroom)) {
                 if (top > c[part] + kHeadroom) raise_reference(c[part], s[part], top);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[part] += exp2_fast(fmaf(z[e], kLog2e, -c[part]));
+            for (int e = 0; e < 4; ++e) s[part] += exp2_fast(fmaf(z[e], a.scale, -c[part]));
         }
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");                  // (a last load into LDS may be under way)
@@ -653,7 +679,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseA
 // D: d rounded up to 64, 128, 256 or 512.  A tile holds 16384 / D items.  Bound by memory: W in, dW out, 2.6 GB for 1.27M items
 // of 512 elements in 515 to 550 us, 4.7 to 5.1 TB/s, where a copy reaches 4.73.
 // PARTS: two rows of dz a position (kTwoParts), in the place of the other 32 positions.
-template <typename T, int D, bool PARTS>
+// DISTIL: dz of a tile's items that are listed is put right in LDS.  A workgroup's tiles follow each other then, and a lane of its first wave
+// goes along its position's list, which is in the order of the items, with the next two entries in registers.
+template <typename T, int D, bool PARTS, bool DISTIL>
 __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a) {
     constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
     using RowsD = Rows<D / 8>;                                 // W and H
@@ -669,8 +697,30 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const long long tiles = (a.N + IT - 1) / IT;
     constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
+    const long long each = DISTIL ? (tiles + gridDim.x - 1) / gridDim.x : 1, tile0 = (long long)blockIdx.x * each;
+    const long long by = DISTIL ? 1 : gridDim.x, end = DISTIL ? min(tiles, tile0 + each) : tiles;
     bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h, PARTS ? a.B : 0);
-    bring_rows<T, D, kLoadsW>(a.W, a.d, (long long)blockIdx.x * IT, a.N, w0);
+    bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile0, tiles - 1) * IT, a.N, w0);
+    __shared__ int listed[2];
+    int cursor = 0, item[2] = {kNoItem, kNoItem};
+    float value[2] = {0.0f, 0.0f};
+    const size_t list = (size_t)min(lane, a.B - 1) * a.entries;
+    auto entry = [&](int i, int& to, float& v) {               // (behind the list's end there are no items)
+        const size_t at = list + min(cursor + i, a.entries - 1);
+        to = cursor + i < a.entries ? a.entry_items[at] : kNoItem;
+        v = a.entry_values[at];
+    };
+    if (DISTIL && wave == 0 && lane < a.B) {
+        for (int first = 0, count = a.entries; count > 0;) {   // the first entry that is not before the workgroup's tiles
+            const int half = count / 2;
+            const bool before = a.entry_items[list + first + half] < tile0 * IT;
+            first = before ? first + half + 1 : first;
+            count = before ? count - half - 1 : half;
+            cursor = first;
+        }
+        entry(0, item[0], value[0]);
+        entry(1, item[1], value[1]);
+    }
     // what default_rows_kernel does for more positions: these rows are a wave's lanes
     __shared__ float factor_of_all;
     if (wave == 0) {
@@ -679,7 +729,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
         info[lane] = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
         if (blockIdx.x == 0) a.info[lane] = info[lane];
         if (kOwn) over_top[lane] = g == 0.0f ? 0.0f : g / top;
-        target[lane] = lane < dz_rows(a) ? a.targets[position_of(a, lane)] : -1;
+        target[lane] = !DISTIL && lane < dz_rows(a) ? a.targets[position_of(a, lane)] : -1;
         if (lane == 0) factor_of_all = top / kDzScale;
     }
     // dH: 2 x D / 32 blocks of 32 rows x 32 elements, shared by the waves; D = 64 leaves half of them without one
@@ -694,11 +744,15 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     for (int i = tid; i < kFew * D / 8; i += kFewThreads)      // (a position that adds nothing may hold anything, NaN too)
         if (info[i / (D / 8)].at == __builtin_inff()) reinterpret_cast<uint4*>(h)[i] = uint4{0, 0, 0, 0};
     const float factor = factor_of_all;
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
+    for (long long tile = tile0; tile < end; tile += by, ++turn) {
         unsigned char* w = turn % 2 ? w1 : w0;
+        if (DISTIL && wave == 0) {
+            const int any = __any(item[0] < min((tile + 1) * IT, a.N));
+            if (lane == 0) listed[turn % 2] = any;
+        }
         // every wave's part of the tile has come (below), and every wave is done with the other buffer
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
+        bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + by, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
 
         // z and dz: blocks of 16 items x 16 rows
         constexpr int kBlocksZ = IT / 16 * 4 / kWaves;
@@ -717,7 +771,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
             const float over = kOwn ? over_top[pos] : 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float p = exp2_fast(fmaf(z[e], kLog2e, -r.at));
+                float p = exp2_fast(fmaf(z[e], a.scale, -r.at));
                 if (e == hit) p -= kDzScale;
                 if (e >= left) p = 0.0f;
                 v[e] = (T)(p * r.scale);
@@ -731,6 +785,28 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
             if (kOwn) *reinterpret_cast<T4*>(dz_w + RowsI::at(pos, first / 8) + first % 8 * 2) = u;
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (DISTIL && listed[turn % 2]) {                      // (the same for all waves)
+            if (wave == 0) {
+                const RowInfo r = info[lane];
+                while (item[0] < min((tile + 1) * IT, a.N)) {          // (kNoItem is not below any N)
+                    const int at = (int)(item[0] - tile * IT);
+                    const float p = value[0] * kDzScale;
+                    const T v = (T)(p * r.scale);
+                    *reinterpret_cast<T*>(dz + RowsI::at(lane, at / 8) + at % 8 * 2) = v;
+                    if (PARTS) *reinterpret_cast<T*>(dz + RowsI::at(lane + a.B, at / 8) + at % 8 * 2) = (T)fmaf(p, r.scale, -(float)v);
+                    if (kOwn) {
+                        const T u = (T)(p * over_top[lane]);
+                        *reinterpret_cast<T*>(dz_w + RowsI::at(lane, at / 8) + at % 8 * 2) = u;
+                        if (PARTS) *reinterpret_cast<T*>(dz_w + RowsI::at(lane + a.B, at / 8) + at % 8 * 2) = (T)fmaf(p, over_top[lane], -(float)u);
+                    }
+                    ++cursor;
+                    item[0] = item[1];
+                    value[0] = value[1];
+                    entry(1, item[1], value[1]);
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        }
 
         if (D / 16 >= kWaves || wave < D / 16) {
 #pragma unroll
@@ -824,6 +900,11 @@ struct DensePlan {
     size_t info_at, live_at, scaled_at, dz_at, partial_at, bytes;          // its workspace
 };
 
+// default_cross_entropy.hip
+__attribute__((visibility("hidden"))) DensePlan plan_dense(long long N, int B, int d, int type);
+__attribute__((visibility("hidden"))) int check_dense(long long N, int B, int d, int type);
+__attribute__((visibility("hidden"))) void set_gradient(DenseArgs& a, const DensePlan& p, void* workspace);
+
 inline int grid_of(long long outer, long long inner) { return (int)(ceil_div(outer, 8) * 8 * inner); }     // see chiplet_order()
 
 constexpr int kSliceItems = 64;                        // a slice of dH's items is a multiple of this
@@ -881,17 +962,20 @@ hipError_t launch_few_loss(const DensePlan& p, const DenseArgs& a, hipStream_t s
     else hipLaunchKernelGGL((default_few_loss_kernel<T, 64>), grid, threads, 0, st, a);
     return hipGetLastError();
 }
-template <typename T, bool PARTS>
+template <typename T, bool PARTS, bool DISTIL>
 hipError_t launch_few_of(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
     const dim3 grid(p.slices), threads(kFewThreads);
-    if (a.d > 256) hipLaunchKernelGGL((default_few_kernel<T, 512, PARTS>), grid, threads, 0, st, a);
-    else if (a.d > 128) hipLaunchKernelGGL((default_few_kernel<T, 256, PARTS>), grid, threads, 0, st, a);
-    else if (a.d > 64) hipLaunchKernelGGL((default_few_kernel<T, 128, PARTS>), grid, threads, 0, st, a);
-    else hipLaunchKernelGGL((default_few_kernel<T, 64, PARTS>), grid, threads, 0, st, a);
+    if (a.d > 256) hipLaunchKernelGGL((default_few_kernel<T, 512, PARTS, DISTIL>), grid, threads, 0, st, a);
+    else if (a.d > 128) hipLaunchKernelGGL((default_few_kernel<T, 256, PARTS, DISTIL>), grid, threads, 0, st, a);
+    else if (a.d > 64) hipLaunchKernelGGL((default_few_kernel<T, 128, PARTS, DISTIL>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((default_few_kernel<T, 64, PARTS, DISTIL>), grid, threads, 0, st, a);
     return hipGetLastError();
 }
 template <typename T>
-hipError_t launch_few(const DensePlan& p, const DenseArgs& a, hipStream_t st) { return a.parts > 1 ? launch_few_of<T, true>(p, a, st) : launch_few_of<T, false>(p, a, st); }
+hipError_t launch_few(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+    if (a.entries) return a.parts > 1 ? launch_few_of<T, true, true>(p, a, st) : launch_few_of<T, false, true>(p, a, st);
+    return a.parts > 1 ? launch_few_of<T, true, false>(p, a, st) : launch_few_of<T, false, false>(p, a, st);
+}
 
 template <typename T>
 hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
@@ -900,7 +984,7 @@ hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
     if (sizeof(T) != 2 || !p.few)
         e = p.loss_items == 64 ? launch_loss<T, 64, 64>(p, a, st) : p.positions == 256 ? launch_loss<T, 256, 256>(p, a, st)
             : p.positions == 128 ? launch_loss<T, 128, 256>(p, a, st) : launch_loss<T, 64, 256>(p, a, st);
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || !a.targets) return e;               // (the sums alone are asked for)
     hipLaunchKernelGGL((default_cross_entropy_join_kernel<T>), dim3(a.B), dim3(kWave), 0, st, a);
     return hipGetLastError();
 }
@@ -937,6 +1021,10 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
         }
         if (!own_rows) e = p.dz_items == 64 ? launch_dz<T, 64, 64>(a, st) : p.dz_positions == 256 ? launch_dz<T, 256, 256>(a, st)
             : p.dz_positions == 128 ? launch_dz<T, 128, 256>(a, st) : launch_dz<T, 64, 256>(a, st);
+        if (e == hipSuccess && a.entries) {
+            hipLaunchKernelGGL((teacher_dz_kernel<T>), dim3((unsigned)ceil_div((long long)a.B * a.entries, 256)), dim3(256), 0, st, a);
+            e = hipGetLastError();
+        }
         if (e != hipSuccess) break;
         a.H = kOwnPowers<T> ? a.scaled : a.live;
         a.h_rows = p.rows_tiles;

@@ -1,0 +1,298 @@
+// Log-probabilities of given items, entropy and the likeliest items by the default scorer's W phi (pq_default_log_probs): the cross entropy's pass
+// over W (default_cross_entropy.hpp) with one more sum, and with candidates for the K best (alternatives.hpp).
+#pragma once
+#include "pqtopk_probs.h"
+#include "default_cross_entropy.hpp"
+#include "alternatives.hpp"
+#include "teacher.hpp"
+
+namespace pqk {
+namespace head {
+
+struct DenseProbsArgs {
+    const void *W, *H;
+    long long N;
+    int B, d;
+    float scale;                                       // log2 e over the temperature
+    long long first, end;                              // the piece's items
+    int store;                                         // whether all its scores go to the lists
+    long long item_tiles;
+    int tiles_each, groups, position_tiles;
+    float4* partial;                                   // [groups][B]: (reference, sum, weighted sum)
+    Lists lists;
+};
+
+// A score that passes its position's floor to the list, or every one of the first piece.
+__device__ __forceinline__ void offer(const DenseProbsArgs& a, int q, float z, long long item) {
+    if (a.store) a.lists.keys[(size_t)q * a.lists.cap + (size_t)(item - a.first)] = key_of(z, (uint32_t)item);
+    else append(a.lists, q, z, (uint32_t)item);
+}
+
+template <typename T, int BN, int ITEMS>
+__global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_log_probs_kernel(DenseProbsArgs a) {
+    using Tile = ScoresTile<T, BN, ITEMS>;
+    constexpr int MI = Tile::MI, NI = Tile::NI, kRowWaves = ITEMS / (32 * MI);
+    __shared__ float4 stat[kRowWaves][BN];
+    int group, pt;
+    chiplet_order(blockIdx.x, a.position_tiles, group, pt);
+    if (group >= a.groups) return;
+    const int lane = threadIdx.x % kWave;
+    float c[NI], s[NI], t[NI], floor[NI];
+    const int q0 = pt * BN + Tile::wave_col() + lane % 32;
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+        c[ni] = kLowest; s[ni] = 0.0f; t[ni] = 0.0f;
+        floor[ni] = __builtin_inff();
+        if (a.lists.keep && !a.store && q0 + 32 * ni < a.B) floor[ni] = a.lists.floor[q0 + 32 * ni];
+    }
+    for (int i = 0; i < a.tiles_each; ++i) {
+        const long long tile = (long long)group * a.tiles_each + i;
+        if (tile >= a.item_tiles) break;
+        const long long item0 = a.first + tile * ITEMS;
+        f32x16 acc[MI][NI];
+        Tile::run(Operand{a.W, (size_t)a.d * sizeof(T), item0, a.N, 0, a.d}, Operand{a.H, (size_t)a.d * sizeof(T), pt * BN, a.B, 0, a.d}, acc);
+        const int left = left_of(a.end - item0 - Tile::wave_row(), 32 * MI);
+        const long long mine = item0 + Tile::wave_row() + 4 * (lane / 32);
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) {
+            __builtin_amdgcn_sched_barrier(0);                 // (one column after the other: the registers hold no two of them)
+            float top = -__builtin_inff();
+            if (left < 32 * MI) {
+                stay_a_branch();
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (32 * mi + 8 * (e / 4) + e % 4 >= left - 4 * (lane / 32)) acc[mi][ni][e] = -__builtin_inff();
+            }
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[mi][ni][e]);
+            if (a.store || __any(top > floor[ni])) {
+                stay_a_branch();
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int at = 32 * mi + 8 * (e / 4) + e % 4;
+                        if (a.store ? q0 + 32 * ni < a.B && at < left - 4 * (lane / 32) : acc[mi][ni][e] > floor[ni]) offer(a, q0 + 32 * ni, acc[mi][ni][e], mine + at);
+                    }
+            }
+            top *= a.scale;
+            if (__any(top > c[ni] + kHeadroom)) {
+                if (top > c[ni] + kHeadroom) raise_reference(c[ni], s[ni], t[ni], top);
+            }
+            float sum = 0.0f, sum_x = 0.0f;
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float x = fmaf(acc[mi][ni][e], a.scale, -c[ni]), p = exp2_fast(x);
+                    sum += p;
+                    sum_x = weighted(p, x, sum_x);
+                }
+            s[ni] += sum;
+            t[ni] += sum_x;
+        }
+    }
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+        join_sums(c[ni], s[ni], t[ni], __shfl_xor(c[ni], 32), __shfl_xor(s[ni], 32), __shfl_xor(t[ni], 32));
+        if (lane < 32) stat[Tile::wave_row() / (32 * MI)][Tile::wave_col() + 32 * ni + lane] = make_float4(c[ni], s[ni], t[ni], 0.0f);
+    }
+    __syncthreads();
+    const int q = pt * BN + threadIdx.x;
+    if ((int)threadIdx.x < BN && q < a.B) {
+        float4 v = stat[0][threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < kRowWaves; ++w) join_sums(v.x, v.y, v.z, stat[w][threadIdx.x].x, stat[w][threadIdx.x].y, stat[w][threadIdx.x].z);
+        a.partial[(size_t)group * a.B + q] = v;
+    }
+}
+
+// The same for up to 64 positions of 16-bit operands, d <= 512 (default_few_loss_kernel's tiles).
+template <typename T, int D>
+__global__ __launch_bounds__(kFewThreads, 2) void default_few_log_probs_kernel(DenseProbsArgs a) {
+    constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
+    using RowsD = Rows<D / 8>;
+    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2];
+    __shared__ float4 stat[kWaves][kFew];
+    constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
+    constexpr int kBlocksZ = IT / 16 * 4 / kWaves, kParts = kBlocksZ < 4 ? kBlocksZ : 4;       // a wave's blocks of 16 x 16; positions among them / 16
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const long long tiles = (a.end - a.first + IT - 1) / IT;
+    bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h);
+    bring_rows<T, D, kLoadsW>(a.W, a.d, a.first + (long long)blockIdx.x * IT, a.N, w0);
+    float c[kParts], s[kParts], t[kParts], floor[kParts];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        c[i] = kLowest; s[i] = 0.0f; t[i] = 0.0f;
+        const int pos = (wave * kBlocksZ + i) % 4 * 16 + lane % 16;
+        floor[i] = a.lists.keep && !a.store && pos < a.B ? a.lists.floor[pos] : __builtin_inff();
+    }
+    int turn = 0;
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
+        const unsigned char* w = turn % 2 ? w1 : w0;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the tile has come, its other buffer is free
+        bring_rows<T, D, kLoadsW>(a.W, a.d, a.first + min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
+#pragma unroll
+        for (int i = 0; i < kBlocksZ; ++i) {
+            const int block = wave * kBlocksZ + i, item0 = block / 4 * 16, pos = block % 4 * 16 + lane % 16;
+            f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k)
+                z = multiply16<T>(RowsD::along(w, item0 + lane % 16, 4 * k + lane / 16), RowsD::along(h, pos, 4 * k + lane / 16), z);
+            const int left = left_of(a.end - a.first - tile * IT - item0, 16) - lane / 16 * 4;
+            if (left < 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e >= left) z[e] = -__builtin_inff();
+            }
+            const float raw = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), top = raw * a.scale;
+            const int part = i % kParts;
+            if (a.store || __any(raw > floor[part])) {
+                stay_a_branch();
+                const long long mine = a.first + tile * IT + item0 + lane / 16 * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (a.store ? pos < a.B && e < left : z[e] > floor[part]) offer(a, pos, z[e], mine + e);
+            }
+            if (__any(top > c[part] + kHeadroom)) {
+                if (top > c[part] + kHeadroom) raise_reference(c[part], s[part], t[part], top);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = fmaf(z[e], a.scale, -c[part]), p = exp2_fast(x);
+                s[part] += p;
+                t[part] = weighted(p, x, t[part]);
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");                  // (a last load into LDS may be under way)
+    for (int q = lane; q < kFew; q += kWave) stat[wave][q] = make_float4(kLowest, 0.0f, 0.0f, 0.0f);
+    wave_reads_after_writes();
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+#pragma unroll
+        for (int x = 16; x < kWave; x *= 2) join_sums(c[i], s[i], t[i], __shfl_xor(c[i], x), __shfl_xor(s[i], x), __shfl_xor(t[i], x));
+        if (lane < 16) stat[wave][(wave * kBlocksZ + i) % 4 * 16 + lane] = make_float4(c[i], s[i], t[i], 0.0f);
+    }
+    __syncthreads();
+    if (tid < a.B) {
+        float4 v = stat[0][tid];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) join_sums(v.x, v.y, v.z, stat[w][tid].x, stat[w][tid].y, stat[w][tid].z);
+        a.partial[(size_t)blockIdx.x * a.B + tid] = v;
+    }
+}
+
+struct DenseFinishArgs {
+    const void *W, *H;
+    const int* items;
+    long long N;
+    int B, d, n, K;
+    float temperature;
+    const float4* partial;     // [groups][B], of all pieces
+    int groups, stored;
+    Lists lists;
+    float *log_probs, *entropy, *lse;
+    int* top_items;
+    float* top_log_probs;
+};
+
+// grid = positions: joins the groups' sums, scores the given items and the list's best in 64 bits, puts these in order.
+template <typename T>
+__global__ __launch_bounds__(kSelectThreads) void default_log_probs_finish_kernel(DenseFinishArgs a) {
+    __shared__ SelectMemory mem;
+    __shared__ uint64_t kept[kMostKept];
+    __shared__ double score[kMostKept];
+    __shared__ int count;
+    __shared__ float4 sums[kSelectWaves];
+    const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    float c = kLowest, s = 0.0f, t = 0.0f;
+    for (int i = tid; i < a.groups; i += kSelectThreads) {
+        const float4 v = a.partial[(size_t)i * a.B + q];
+        join_sums(c, s, t, v.x, v.y, v.z);
+    }
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) join_sums(c, s, t, __shfl_xor(c, x), __shfl_xor(s, x), __shfl_xor(t, x));
+    if (lane == 0) sums[wave] = make_float4(c, s, t, 0.0f);
+    __syncthreads();
+    c = sums[0].x; s = sums[0].y; t = sums[0].z;
+    for (int w = 1; w < kSelectWaves; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
+    const float lse = log_sum(c, s);
+    if (tid == 0) {
+        a.lse[q] = lse;
+        a.entropy[q] = entropy_of(s, t);
+    }
+    auto log_prob = [&](double z) { return lse == -__builtin_inff() ? lse : (float)(z / (double)a.temperature - (double)lse); };
+    const T *W = static_cast<const T*>(a.W), *h = static_cast<const T*>(a.H) + (size_t)q * a.d;
+    for (int i = tid / 16; i < a.n; i += kSelectThreads / 16) {
+        const int item = a.items[(size_t)q * a.n + i];
+        const bool there = item >= 0 && item < a.N;            // (the same for the sixteen)
+        const double z = there ? dot64(W + (size_t)item * a.d, h, a.d) : 0.0;
+        if (tid % 16 == 0) a.log_probs[(size_t)q * a.n + i] = there ? log_prob(z) : 0.0f;
+    }
+    if (a.K == 0) return;
+    const int n = last_cut(a.lists, q, a.stored, kept, count, mem);
+    for (int i = tid / 16; i < n; i += kSelectThreads / 16) {
+        const double z = dot64(W + (size_t)item_of(kept[i]) * a.d, h, a.d);
+        if (tid % 16 == 0) score[i] = z;
+    }
+    __syncthreads();
+    if (tid < n) {
+        // (a NaN, of which no rank comes, is taken for the lowest)
+        const double mine = score[tid] == score[tid] ? score[tid] : -__builtin_inf();
+        int rank = 0;
+        for (int i = 0; i < n; ++i) {
+            const double other = score[i] == score[i] ? score[i] : -__builtin_inf();
+            rank += other > mine || (other == mine && item_of(kept[i]) < item_of(kept[tid]));
+        }
+        if (rank < a.K) {
+            a.top_items[(size_t)q * a.K + rank] = (int)item_of(kept[tid]);
+            a.top_log_probs[(size_t)q * a.K + rank] = log_prob(score[tid]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// host side, by type of the operands (a translation unit each)
+
+template <typename T> hipError_t dense_probs(const DensePlan& p, const DenseProbsArgs& a, hipStream_t st);
+template <typename T> hipError_t dense_probs_finish(const DenseFinishArgs& a, hipStream_t st);
+
+#ifdef PQ_PROBS_INSTANCE
+template <typename T, int POS, int ITEMS>
+hipError_t launch_probs(const DensePlan& p, const DenseProbsArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((default_log_probs_kernel<T, POS, ITEMS>), dim3(grid_of(p.groups, p.position_tiles)), dim3(ScoresTile<T, POS, ITEMS>::kThreads), 0, st, a);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_few_probs(const DensePlan& p, const DenseProbsArgs& a, hipStream_t st) {
+    const dim3 grid(p.groups), threads(kFewThreads);
+    if (a.d > 256) hipLaunchKernelGGL((default_few_log_probs_kernel<T, 512>), grid, threads, 0, st, a);
+    else if (a.d > 128) hipLaunchKernelGGL((default_few_log_probs_kernel<T, 256>), grid, threads, 0, st, a);
+    else if (a.d > 64) hipLaunchKernelGGL((default_few_log_probs_kernel<T, 128>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((default_few_log_probs_kernel<T, 64>), grid, threads, 0, st, a);
+    return hipGetLastError();
+}
+template <typename T>
+hipError_t dense_probs(const DensePlan& p, const DenseProbsArgs& a, hipStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if (p.few) return launch_few_probs<T>(p, a, st);
+    }
+    return p.loss_items == 64 ? launch_probs<T, 64, 64>(p, a, st) : p.positions == 256 ? launch_probs<T, 256, 256>(p, a, st)
+           : p.positions == 128 ? launch_probs<T, 128, 256>(p, a, st) : launch_probs<T, 64, 256>(p, a, st);
+}
+template <typename T>
+hipError_t dense_probs_finish(const DenseFinishArgs& a, hipStream_t st) {
+    hipLaunchKernelGGL((default_log_probs_finish_kernel<T>), dim3(a.B), dim3(kSelectThreads), 0, st, a);
+    return hipGetLastError();
+}
+template hipError_t dense_probs<PQ_PROBS_INSTANCE>(const DensePlan&, const DenseProbsArgs&, hipStream_t);
+template hipError_t dense_probs_finish<PQ_PROBS_INSTANCE>(const DenseFinishArgs&, hipStream_t);
+#endif
+
+}  // namespace head
+}  // namespace pqk

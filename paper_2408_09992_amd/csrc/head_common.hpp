@@ -43,6 +43,24 @@ __device__ __forceinline__ void raise_reference(float& c, float& s, float top) {
     s *= exp2_fast(c - to);
     c = to;
 }
+// Besides, a sum of terms 2^x x (what an entropy is made of): total = 2^c (t + c s).  A term's x is held over -200, where 2^x is 0 and -inf would make NaN.
+__device__ __forceinline__ float weighted(float p, float x, float t) { return fmaf(p, fmaxf(x, -200.0f), t); }
+__device__ __forceinline__ void join_sums(float& c, float& s, float& t, float c2, float s2, float t2) {
+    const float top = fmaxf(c, c2), f = exp2_fast(c - top), f2 = exp2_fast(c2 - top);
+    t = f * fmaf(c - top, s, t) + f2 * fmaf(c2 - top, s2, t2);
+    s = s * f + s2 * f2;
+    c = top;
+}
+__device__ __forceinline__ void raise_reference(float& c, float& s, float& t, float top) {
+    const float to = fminf(top, kHighest), f = exp2_fast(c - to);
+    t = f * fmaf(c - to, s, t);
+    s *= f;
+    c = to;
+}
+// - sum_i p log p in nats: log p = ln 2 (x - log2 s).  0 where no score counts.
+__device__ __forceinline__ float entropy_of(float s, float t) {
+    return s == 0.0f ? 0.0f : s < __builtin_inff() ? fmaxf((__log2f(s) - t / s) * kLn2, 0.0f) : __builtin_nanf("");
+}
 // log-sum: -inf where no score counts, NaN where one is NaN, +inf or counts as that.
 __device__ __forceinline__ float log_sum(float c, float s) {
     return s == 0.0f ? -__builtin_inff() : s < __builtin_inff() ? (c + __log2f(s)) * kLn2 : __builtin_nanf("");
@@ -53,6 +71,11 @@ inline hipError_t allow_lds(F* kernel, size_t bytes) {
     if (bytes <= 64 * 1024) return hipSuccess;
     return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
+
+// Temperatures and how many items a position may be given (pqtopk_probs.h).
+constexpr double kLog2eDouble = 1.4426950408889634;
+constexpr int kMostGiven = 65536;
+inline bool temperature_fits(float t) { return t >= 1e-4f && t <= 1e4f; }
 
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 inline size_t round_up(size_t a, size_t to) { return (a + to - 1) / to * to; }

@@ -1,0 +1,3 @@
+// Instantiates the dense log-probabilities' kernels for one type of W and queries.
+#define PQ_PROBS_INSTANCE float
+#include "default_log_probs.hpp"

@@ -1,0 +1,206 @@
+// Log-probabilities of given items, entropy and the likeliest items by sub-ids (pq_log_probs*): one pass over the codebook whose lookups
+// serve all of them.
+//
+//   r_qi = sum_k S[q][k][G[i][k]]   lse = log sum_i exp(r_i / T)   log p_i = r_i / T - lse   entropy = lse - sum_i p_i r_i / T
+//
+// The pass is the cross entropy's (cross_entropy.hpp) with one more sum; what scores pass a position's floor goes to its list (alternatives.hpp).
+#include "pqtopk_probs.h"
+#include "cross_entropy.hpp"
+
+namespace pqk {
+namespace head {
+namespace subids {
+namespace {
+
+template <int M, typename CT, int Q>
+__global__ __launch_bounds__(kThreads) void log_probs_kernel(ProbsArgs a) { sum_items<M, CT, Q, true>(a); }
+
+struct FinishArgs {
+    const void* codes;
+    const float* S;
+    const int* items;
+    long long N;
+    int B, m, b, n, K, code_bytes;
+    float temperature;
+    const float4* partial;     // [shares][B]
+    int shares, stored;
+    Lists lists;
+    float *log_probs, *entropy, *lse;
+    int* top_items;
+    float* top_log_probs;
+};
+
+// Eq. 5's chain of one item, from the tables where they lie.
+__device__ __forceinline__ float score_of_item(const FinishArgs& a, int q, int item) {
+    float z = 0.0f;
+    for (int k = 0; k < a.m; ++k) {
+        const size_t at = (size_t)item * a.m + k;
+        const uint32_t g = a.code_bytes == 1 ? (uint32_t)static_cast<const uint8_t*>(a.codes)[at] : (uint32_t)static_cast<const uint16_t*>(a.codes)[at];
+        const float v = a.S[((size_t)q * a.m + k) * a.b + min(g, (uint32_t)a.b - 1u)];
+        z = k == 0 ? v : z + v;
+    }
+    return z;
+}
+
+// grid = positions: joins the shares' sums, scores the given items, cuts the list to the K best and puts them in order.
+__global__ __launch_bounds__(kSelectThreads) void log_probs_finish_kernel(FinishArgs a) {
+    __shared__ SelectMemory mem;
+    __shared__ uint64_t kept[kMostKept];
+    __shared__ int count;
+    __shared__ float4 sums[kSelectWaves];
+    const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    float c = kLowest, s = 0.0f, t = 0.0f;
+    for (int i = tid; i < a.shares; i += kSelectThreads) {
+        const float4 v = a.partial[(size_t)i * a.B + q];
+        join_sums(c, s, t, v.x, v.y, v.z);
+    }
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) join_sums(c, s, t, __shfl_xor(c, x), __shfl_xor(s, x), __shfl_xor(t, x));
+    if (lane == 0) sums[wave] = make_float4(c, s, t, 0.0f);
+    __syncthreads();
+    c = sums[0].x; s = sums[0].y; t = sums[0].z;
+    for (int w = 1; w < kSelectWaves; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
+    const float lse = log_sum(c, s);
+    if (tid == 0) {
+        a.lse[q] = lse;
+        a.entropy[q] = entropy_of(s, t);
+    }
+    auto log_prob = [&](float z) { return lse == -__builtin_inff() ? lse : (float)((double)z / (double)a.temperature - (double)lse); };
+    for (int i = tid; i < a.n; i += kSelectThreads) {
+        const int item = a.items[(size_t)q * a.n + i];
+        a.log_probs[(size_t)q * a.n + i] = item >= 0 && item < a.N ? log_prob(score_of_item(a, q, item)) : 0.0f;
+    }
+    if (a.K == 0) return;
+    const int n = last_cut(a.lists, q, a.stored, kept, count, mem);
+    if (tid < n) {
+        const uint64_t mine = kept[tid];
+        int rank = 0;
+        for (int i = 0; i < n; ++i) rank += kept[i] > mine;
+        if (rank < a.K) {
+            a.top_items[(size_t)q * a.K + rank] = (int)item_of(mine);
+            a.top_log_probs[(size_t)q * a.K + rank] = log_prob(score_of(mine));
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// host side
+
+template <int M, typename CT, int Q>
+hipError_t go(const Plan& p, const ProbsArgs& a, hipStream_t st) {
+    hipError_t e = allow_lds(log_probs_kernel<M, CT, Q>, p.lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((log_probs_kernel<M, CT, Q>), dim3(p.shares, p.groups), dim3(kThreads), p.lds, st, a);
+    return hipGetLastError();
+}
+template <int M, typename CT>
+hipError_t go_q(const Plan& p, const ProbsArgs& a, hipStream_t st) {
+    if constexpr (fits<M, CT>(4, 0)) { if (p.Q == 4) return go<M, CT, 4>(p, a, st); }
+    if (p.Q == 2) return go<M, CT, 2>(p, a, st);
+    return go<M, CT, 1>(p, a, st);
+}
+template <typename CT>
+hipError_t go_m(const Plan& p, const ProbsArgs& a, hipStream_t st) {
+    if (a.m == 4) return go_q<4, CT>(p, a, st);
+    if (a.m == 8) return go_q<8, CT>(p, a, st);
+    if (a.m == 16) return go_q<16, CT>(p, a, st);
+    if (a.m == 2 && sizeof(CT) == 1) return go_q<2, uint8_t>(p, a, st);
+    if (a.m == 32 && sizeof(CT) == 1) return go_q<32, uint8_t>(p, a, st);
+    if (a.m == 64 && sizeof(CT) == 1) return go_q<64, uint8_t>(p, a, st);
+    return go_q<0, CT>(p, a, st);
+}
+
+// Where the workspace's parts lie.
+struct Layout {
+    Passes pieces;
+    int shares;
+    size_t keys_at, count_at, floor_at, bytes;
+};
+bool lay_out(Layout& l, long long N, int B, int m, int b, int K, int code_bytes) {
+    l.pieces = pieces_of(N, B, K);
+    l.shares = 0;
+    for (long long done = 0; done < N; done += l.pieces.after(done)) {
+        Plan p;
+        if (!plan_loss(p, l.pieces.after(done), B, m, b, code_bytes, true)) return false;
+        l.shares += p.shares;
+    }
+    l.keys_at = round_up((size_t)l.shares * B * sizeof(float4), 256);
+    l.count_at = l.keys_at + l.pieces.key_bytes(B);
+    l.floor_at = l.count_at + (K ? round_up((size_t)B * sizeof(int), 256) : 0);
+    l.bytes = l.floor_at + (K ? round_up((size_t)B * sizeof(float), 256) : 0);
+    return true;
+}
+
+int check(long long N, int B, int m, int b, int K, int code_bytes) {
+    if (K < 0 || K > N) return PQ_ERR_SHAPE;
+    const int rc = check_shape(N, B, m, b, code_bytes);
+    return rc != PQ_OK ? rc : K > PQ_MAX_K ? PQ_ERR_UNSUPPORTED : PQ_OK;
+}
+
+size_t bytes_of(long long N, int B, int m, int b, int K, int code_bytes) {
+    Layout l;
+    return check(N, B, m, b, K, code_bytes) == PQ_OK && lay_out(l, N, B, m, b, K, code_bytes) ? l.bytes : 0;
+}
+
+template <typename CT>
+int log_probs(const CT* codes, const float* S, const int* items, long long N, int B, int m, int b, int n, int K, float temperature, float* out,
+              float* entropy, float* lse, int* top_items, float* top_log_probs, void* workspace, size_t ws_bytes, void* stream) {
+    if (!codes || !S || !entropy || !lse || !workspace || (n != 0 && (!items || !out)) || (K != 0 && (!top_items || !top_log_probs))) return PQ_ERR_NULL;
+    if (n < 0 || !(temperature > 0.0f)) return PQ_ERR_SHAPE;
+    int rc = check(N, B, m, b, K, sizeof(CT));
+    if (rc != PQ_OK) return rc;
+    Layout l;
+    if (n > kMostGiven || !temperature_fits(temperature) || !lay_out(l, N, B, m, b, K, sizeof(CT))) return PQ_ERR_UNSUPPORTED;
+    if ((((uintptr_t)codes | (uintptr_t)workspace) & 15) || (((uintptr_t)S | (uintptr_t)entropy | (uintptr_t)lse) & 3) ||
+        (n && (((uintptr_t)items | (uintptr_t)out) & 3)) || (K && (((uintptr_t)top_items | (uintptr_t)top_log_probs) & 3)))
+        return PQ_ERR_ALIGN;
+    if (ws_bytes < l.bytes) return PQ_ERR_WORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    const Lists lists{reinterpret_cast<uint64_t*>(ws + l.keys_at), reinterpret_cast<int*>(ws + l.count_at), reinterpret_cast<float*>(ws + l.floor_at),
+                      (uint32_t)l.pieces.cap, l.pieces.keep};
+    ProbsArgs a{codes, S, N, B, m, b, 0, (float)(kLog2eDouble / temperature), 0, 0, 0, reinterpret_cast<float4*>(ws), lists};
+    hipError_t e = hipSuccess;
+    for (long long done = 0; done < N && e == hipSuccess; done = a.end) {
+        Plan p;
+        const long long items_now = l.pieces.after(done);
+        plan_loss(p, items_now, B, m, b, sizeof(CT), true);
+        a.first = (uint32_t)done;
+        a.end = (uint32_t)(done + items_now);
+        a.share = p.share;
+        a.store = K != 0 && done == 0;
+        e = go_m<CT>(p, a, st);
+        a.partial += (size_t)p.shares * B;
+        if (e == hipSuccess && K && a.end < N) e = launch_select(lists, B, done == 0 ? (int)items_now : 0, st);
+    }
+    if (e == hipSuccess) {
+        const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), temperature, reinterpret_cast<const float4*>(ws), l.shares,
+                           l.pieces.first == N ? (int)N : 0, lists, out, entropy, lse, top_items, top_log_probs};
+        hipLaunchKernelGGL(log_probs_finish_kernel, dim3(B), dim3(kSelectThreads), 0, st, f);
+        e = hipGetLastError();
+    }
+    return record_hip_error(e);
+}
+
+}  // namespace
+}  // namespace subids
+}  // namespace head
+}  // namespace pqk
+
+using namespace pqk::head::subids;
+
+extern "C" {
+
+size_t pq_log_probs_workspace_bytes(long long N, int B, int m, int b, int K) { return bytes_of(N, B, m, b, K, 1); }
+size_t pq_log_probs_u16_workspace_bytes(long long N, int B, int m, int b, int K) { return bytes_of(N, B, m, b, K, 2); }
+
+int pq_log_probs(const uint8_t* codes, const float* S, const int* items, long long N, int B, int m, int b, int n, int K, float temperature,
+                 float* out, float* entropy, float* lse, int* top_items, float* top_log_probs, void* workspace, size_t workspace_bytes, void* stream) {
+    return log_probs<uint8_t>(codes, S, items, N, B, m, b, n, K, temperature, out, entropy, lse, top_items, top_log_probs, workspace, workspace_bytes, stream);
+}
+int pq_log_probs_u16(const uint16_t* codes, const float* S, const int* items, long long N, int B, int m, int b, int n, int K, float temperature,
+                     float* out, float* entropy, float* lse, int* top_items, float* top_log_probs, void* workspace, size_t workspace_bytes, void* stream) {
+    return log_probs<uint16_t>(codes, S, items, N, B, m, b, n, K, temperature, out, entropy, lse, top_items, top_log_probs, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,95 @@
+// A teacher's list of one position as probabilities, by one workgroup, in 64 bits (512 entries at most: nothing beside a pass over the items).
+#pragma once
+#include "head_common.hpp"
+
+namespace pqk {
+namespace head {
+
+constexpr int kMostEntries = 512;
+
+// Two numbers of every thread, each joined over the workgroup by `f` (which does not ask for an order); `part` is shared, a place a wave.
+template <int THREADS, typename V, typename F>
+__device__ __forceinline__ V over_workgroup(V v, V* part, F f) {
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) v = f(v, __shfl_xor(v, x));
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / kWave; ++w) v = f(v, part[w]);
+    return v;
+}
+
+// Every THREADS-th entry of a list from the thread's own on: the item (-1: no entry), its probability w and log w.
+template <int THREADS>
+struct Teacher {
+    static constexpr int kEach = (kMostEntries + THREADS - 1) / THREADS;
+    int item[kEach];
+    double weight[kEach], log_weight[kEach];
+    bool any;                  // whether an entry has weight, or is a NaN
+    bool odd;                  // whether the list holds a NaN or +inf: all its weights are NaN
+};
+template <int THREADS>
+__device__ __forceinline__ Teacher<THREADS> teacher_of(const int* items, const float* scores, int q, int K, long long N, float temperature, double* part) {
+    constexpr int kEach = Teacher<THREADS>::kEach;
+    Teacher<THREADS> t;
+    double x[kEach], top = -__builtin_inf(), any = 0.0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int k = (int)threadIdx.x + j * THREADS;
+        const size_t at = (size_t)q * K + (k < K ? k : 0);
+        const int item = items[at];
+        const float u = scores[at];
+        const bool entry = k < K && item >= 0 && item < N;
+        t.item[j] = entry ? item : -1;
+        x[j] = entry ? (double)u / (double)temperature : -__builtin_inf();
+        if (x[j] != -__builtin_inf()) any = 1.0;
+        top = fmax(top, x[j]);
+    }
+    any = over_workgroup<THREADS>(any, part, [](double a, double b) { return fmax(a, b); });
+    top = over_workgroup<THREADS>(top, part, [](double a, double b) { return fmax(a, b); });
+    t.any = any != 0.0;
+    double sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        x[j] = t.any ? x[j] - top : x[j];
+        t.weight[j] = x[j] == -__builtin_inf() ? 0.0 : exp(x[j]);
+        sum += t.weight[j];
+    }
+    // (one order whatever the lanes': a sum of two is the same both ways)
+    sum = over_workgroup<THREADS>(sum, part, [](double a, double b) { return a + b; });
+    t.odd = t.any && !(sum < __builtin_inf());
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        t.weight[j] = t.any ? t.weight[j] / sum : 0.0;
+        t.log_weight[j] = x[j] - log(sum);
+    }
+    return t;
+}
+
+// What an entry adds to sum_k w_k (log w_k - log p_k), log p_k = score / T - lse.
+__device__ __forceinline__ double entry_loss(double weight, double log_weight, double score, float temperature, double lse) {
+    return weight == 0.0 ? 0.0 : weight * (log_weight - (score / (double)temperature - lse));
+}
+
+// The sum of the products of two rows of d elements, in 64 bits (those of 16-bit elements are exact, and nearly always their sum), by sixteen
+// lanes of a wave; all sixteen have it.  Rows are multiples of 16 bytes, and aligned.
+template <typename T>
+__device__ __forceinline__ double dot64(const T* x, const T* y, int d) {
+    constexpr int kOf = 16 / (int)sizeof(T);
+    typedef T Piece __attribute__((ext_vector_type(kOf)));
+    double sum = 0.0;
+#pragma unroll 4
+    for (int i = (int)threadIdx.x % 16; i < d / kOf; i += 16) {
+        const Piece u = reinterpret_cast<const Piece*>(x)[i], v = reinterpret_cast<const Piece*>(y)[i];
+#pragma unroll
+        for (int e = 0; e < kOf; ++e) sum = fma((double)(float)u[e], (double)(float)v[e], sum);
+    }
+#pragma unroll
+    for (int w = 1; w < 16; w *= 2) sum += __shfl_xor(sum, w);
+    return sum;
+}
+
+}  // namespace head
+}  // namespace pqk
