@@ -3,7 +3,10 @@
 // The items are taken in pieces, in the order of their ids.  Of the first piece every score goes to the position's list; of the
 // others those above its floor, a score that `keep` earlier items reach.  Between the pieces select_kernel cuts the lists back to
 // little more than `keep` keys and raises the floors.  A later item that only ties with the floor ranks behind those `keep`, so the test
-// is z > floor: no order of the scores makes a list overflow that holds what was kept and a piece, and equal scores add nothing.
+// is z > floor: equal scores add nothing, and whatever order the scores come in, the result is right.
+//
+// A workgroup has a region of each of its positions' lists, as long as it has items, and counts in LDS what it puts there.  (Counters of all workgroups
+// in memory took the longest part of a pass: 64 of them, 53,000 candidates, 280 us.)
 #pragma once
 #include "head_common.hpp"
 
@@ -12,12 +15,16 @@ namespace head {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
 constexpr int kMostKept = 1024;                      // keys that a cut leaves at most
+constexpr int kMostRegions = 2048;                   // workgroups that share the items of a piece
+constexpr int kLocalKeys = 4096;                     // keys that a cut brings to LDS at once; of more each pass reads all again
 
 struct Lists {
-    uint64_t* keys;            // [B][cap]
-    int* count;                // [B]
+    uint64_t* keys;            // [B][cap]: all keys of the first piece, or the regions of a later one
+    int* counts;               // [regions][B]
+    uint64_t* kept;            // [B][kMostKept]: of the pieces before
+    int* kept_count;           // [B]
     float* floor;              // [B]
-    uint32_t cap;
+    long long cap;
     int keep;                  // 0: no alternatives are asked for
 };
 
@@ -33,27 +40,71 @@ __device__ __forceinline__ float score_of(uint64_t key) {
     if (order <= 0x007FFFFFu) return -__builtin_inff();           // (also what ranked as a NaN)
     return __builtin_bit_cast(float, (order & 0x80000000u) ? order & 0x7FFFFFFFu : ~order);
 }
-__device__ __forceinline__ void append(const Lists& l, int q, float z, uint32_t item) {
-    const int at = atomicAdd(l.count + q, 1);                     // (what order the lists are in changes no result)
-    if ((uint32_t)at < l.cap) l.keys[(size_t)q * l.cap + at] = key_of(z, item);
+
+// A candidate to the workgroup's region, which begins at `region` and counts in *count (LDS).
+__device__ __forceinline__ void append(const Lists& l, int q, long long region, int* count, float z, uint32_t item) {
+    l.keys[(size_t)q * l.cap + region + atomicAdd(count, 1)] = key_of(z, item);       // (what order a region is in changes no result)
 }
 
 struct SelectMemory {
+    uint64_t local[kLocalKeys];
     uint32_t histogram[2048];
+    int begin[kMostRegions];                         // where a region's keys begin among all of them
     uint64_t part[kSelectWaves][2];
     uint32_t sums[kSelectWaves];
-    uint64_t low, high;
-    int above, taken, chosen;
+    int above, taken, chosen, count;
 };
 
-// A key that at least `keep` of keys[0 .. n - 1], and no more than `most` (most > keep), reach; 0 if n <= keep.  By histograms of 2048 bins over
+// What lies before the thread's own value among those of all threads.
+__device__ __forceinline__ uint32_t sums_before(uint32_t own, SelectMemory& mem, uint32_t& all) {
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    uint32_t sum = own;
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) {
+        const uint32_t v = __shfl_up(sum, x);
+        if (lane >= x) sum += v;
+    }
+    if (lane == kWave - 1) mem.sums[wave] = sum;
+    __syncthreads();
+    uint32_t before = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < kSelectWaves; ++w) {
+        const uint32_t v = mem.sums[w];
+        if (w < wave) before += v;
+        all += v;
+    }
+    return before + sum - own;
+}
+
+// The keys of a position's list: those kept, then the regions'.
+struct Keys {
+    const uint64_t *kept, *keys;
+    const int* begin;
+    long long region;
+    int kept_n, regions, n;
+    __device__ __forceinline__ uint64_t operator()(int i) const {
+        if (i < kept_n) return kept[i];
+        int first = 0, count = regions;                          // (the last region that begins at i or before)
+        while (count > 1) {
+            const int half = count / 2;
+            const bool there = begin[first + half] <= i;
+            first = there ? first + half : first;
+            count = there ? count - half : half;
+        }
+        return keys[first * region + (i - begin[first])];
+    }
+};
+
+// A key that at least `keep` of n keys, and no more than `most` (over `keep`) of them, reach; 0 if n <= keep.  By histograms of 2048 bins over
 // the range that is left, each pass a look at all keys: one or two in the usual case, six at most (keys differ).
-__device__ __forceinline__ uint64_t cut(const uint64_t* keys, int n, int keep, int most, SelectMemory& mem) {
+template <typename K>
+__device__ __forceinline__ uint64_t cut(const K& key, int n, int keep, int most, SelectMemory& mem) {
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     if (n <= keep) return 0;
     uint64_t low = ~0ull, high = 0;
     for (int i = tid; i < n; i += kSelectThreads) {
-        const uint64_t k = keys[i];
+        const uint64_t k = key(i);
         low = k < low ? k : low;
         high = k > high ? k : high;
     }
@@ -72,28 +123,19 @@ __device__ __forceinline__ uint64_t cut(const uint64_t* keys, int n, int keep, i
     }
     int above = 0;                                                // keys over the range
     while (true) {
-        const int bits = 64 - __clzll((long long)(high - low | 1)), shift = bits > 11 ? bits - 11 : 0;
+        const int bits = 64 - __clzll((long long)((high - low) | 1)), shift = bits > 11 ? bits - 11 : 0;
         mem.histogram[tid] = 0;
         mem.histogram[tid + 1024] = 0;
         __syncthreads();
         for (int i = tid; i < n; i += kSelectThreads) {
-            const uint64_t k = keys[i];
+            const uint64_t k = key(i);
             if (k >= low && k <= high) atomicAdd(&mem.histogram[(uint32_t)((k - low) >> shift)], 1u);
         }
         __syncthreads();
         // thread t has the bins 2047 - 2t and 2046 - 2t: what lies over them by a scan
         const uint32_t upper = mem.histogram[2047 - 2 * tid], lower = mem.histogram[2046 - 2 * tid];
-        uint32_t sum = upper + lower;
-#pragma unroll
-        for (int x = 1; x < kWave; x *= 2) {
-            const uint32_t v = __shfl_up(sum, x);
-            if (lane >= x) sum += v;
-        }
-        if (lane == kWave - 1) mem.sums[wave] = sum;
-        __syncthreads();
-        uint32_t before = (uint32_t)above;
-        for (int w = 0; w < wave; ++w) before += mem.sums[w];
-        const uint32_t end = before + sum, begin = end - upper - lower;
+        uint32_t all;
+        const uint32_t begin = (uint32_t)above + sums_before(upper + lower, mem, all), end = begin + upper + lower;
         if (begin < (uint32_t)keep && end >= (uint32_t)keep) {    // (one thread: the keep-th key is in its bins)
             const bool first = begin + upper >= (uint32_t)keep;
             mem.chosen = first ? 2047 - 2 * tid : 2046 - 2 * tid;
@@ -112,46 +154,56 @@ __device__ __forceinline__ uint64_t cut(const uint64_t* keys, int n, int keep, i
 }
 
 // How many keys a cut to `keep` may leave: a few more save a pass.
-__device__ __forceinline__ int most_of(int keep) { return min(kMostKept, keep + keep / 4 + 32); }
+__host__ __device__ constexpr int most_of(int keep) { return keep + keep / 4 + 32 < kMostKept ? keep + keep / 4 + 32 : kMostKept; }
 
-// grid = positions.  stored: how many keys the first piece left, or 0: the counts say.  Leaves kept keys, their count and the floor.
-template <int>                                        // (a template: only what launches it has it)
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(Lists l, int stored) {
-    __shared__ SelectMemory mem;
-    __shared__ uint64_t kept[kMostKept];
-    __shared__ int count;
-    const int q = blockIdx.x, tid = threadIdx.x;
-    uint64_t* keys = l.keys + (size_t)q * l.cap;
-    const int n = stored ? stored : min(l.count[q], (int)l.cap);
-    if (tid == 0) count = 0;
-    const uint64_t least = cut(keys, n, l.keep, most_of(l.keep), mem);
-    __syncthreads();
-    for (int i = tid; i < n; i += kSelectThreads) {
-        const uint64_t k = keys[i];
-        if (k >= least) kept[atomicAdd(&count, 1)] = k;
+// Cuts a position's list: what is left in out[] (the order is none), `keep` at least (or all) and most_of(keep) at most; returns how many, and in `least` what
+// they reach (0: as good as nothing was cut).  last: no floor is asked for.  stored: how many keys the first piece left, if that was the last piece; else regions of `region` keys each.
+__device__ __forceinline__ int cut_list(const Lists& l, int q, int B, int stored, int regions, long long region, bool last, uint64_t* out, uint64_t& least, SelectMemory& mem) {
+    const int tid = threadIdx.x, most = most_of(l.keep);
+    const uint64_t* keys = l.keys + (size_t)q * l.cap;
+    Keys all{l.kept + (size_t)q * kMostKept, keys, mem.begin, region, stored, 1, stored};
+    if (stored) all.kept = keys;
+    else {
+        all.kept_n = l.kept_count[q];
+        all.regions = regions;
+        const int a = 2 * tid < regions ? l.counts[(size_t)(2 * tid) * B + q] : 0, b = 2 * tid + 1 < regions ? l.counts[(size_t)(2 * tid + 1) * B + q] : 0;
+        uint32_t total;
+        const int before = all.kept_n + (int)sums_before((uint32_t)(a + b), mem, total);
+        mem.begin[2 * tid] = before;
+        mem.begin[2 * tid + 1] = before + a;
+        all.n = all.kept_n + (int)total;
     }
+    if (tid == 0) mem.count = 0;
     __syncthreads();
-    for (int i = tid; i < count; i += kSelectThreads) keys[i] = kept[i];
-    if (tid == 0) {
-        l.count[q] = count;
-        l.floor[q] = score_of(least);
-    }
+    const int n = all.n;
+    auto local = [&](int i) { return mem.local[i]; };
+    if (n <= kLocalKeys) {
+        for (int i = tid; i < n; i += kSelectThreads) mem.local[i] = all(i);
+        __syncthreads();
+        least = last && n <= most ? 0 : cut(local, n, l.keep, most, mem);
+    } else least = cut(all, n, l.keep, most, mem);
+    auto take = [&](uint64_t k) {
+        if (k >= least) out[atomicAdd(&mem.count, 1)] = k;
+    };
+    if (n <= kLocalKeys) for (int i = tid; i < n; i += kSelectThreads) take(mem.local[i]);
+    else for (int i = tid; i < n; i += kSelectThreads) take(all(i));
+    __syncthreads();
+    return mem.count;
 }
 
-// The last cut: the keys that are left, in kept[]; returns how many, `keep` (or all) at least and kMostKept at most.
-__device__ __forceinline__ int last_cut(const Lists& l, int q, int stored, uint64_t* kept, int& count, SelectMemory& mem) {
-    const int tid = threadIdx.x;
-    const uint64_t* keys = l.keys + (size_t)q * l.cap;
-    const int n = stored ? stored : min(l.count[q], (int)l.cap), most = most_of(l.keep);
-    if (tid == 0) count = 0;
-    const uint64_t least = n <= most ? 0 : cut(keys, n, l.keep, most, mem);
-    __syncthreads();
-    for (int i = tid; i < n; i += kSelectThreads) {
-        const uint64_t k = keys[i];
-        if (k >= least) kept[atomicAdd(&count, 1)] = k;
+// grid = positions: cuts the lists between two pieces and sets the floors.
+template <int>                                        // (a template: only what launches it has it)
+__global__ __launch_bounds__(kSelectThreads) void select_kernel(Lists l, int B, int stored, int regions, long long region) {
+    __shared__ SelectMemory mem;
+    __shared__ uint64_t out[kMostKept];
+    const int q = blockIdx.x, tid = threadIdx.x;
+    uint64_t least;
+    const int n = cut_list(l, q, B, stored, regions, region, false, out, least, mem);
+    for (int i = tid; i < n; i += kSelectThreads) l.kept[(size_t)q * kMostKept + i] = out[i];
+    if (tid == 0) {
+        l.kept_count[q] = n;
+        if (least != 0) l.floor[q] = score_of(least);          // (a list of `keep` keys, of which nothing is cut, has the floor that it had)
     }
-    __syncthreads();
-    return count;
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -161,31 +213,49 @@ __device__ __forceinline__ int last_cut(const Lists& l, int q, int stored, uint6
 // times the items before them, so that a list gets some kGrowth * keep new keys.
 constexpr long long kOnePiece = 16384, kGrowth = 32, kListBytes = 1LL << 31;
 struct Passes {
-    long long N, first, cap;
+    long long N, first, room;
     int keep;
     long long after(long long done) const {                      // items of the piece after `done` items
         if (done == 0) return first;
-        long long n = done * kGrowth < cap - kMostKept ? done * kGrowth : cap - kMostKept;
+        const long long n = done * kGrowth < room ? done * kGrowth : room;
         return n < N - done ? n : N - done;
     }
-    size_t key_bytes(int B) const { return keep ? round_up((size_t)B * cap * sizeof(uint64_t), 256) : 0; }
 };
-inline Passes pieces_of(long long N, int B, int keep) {
-    Passes p{N, N, 0, (int)(keep < N ? keep : N)};
+inline Passes passes_of(long long N, int B, int keep) {
+    Passes p{N, N, N, (int)(keep < N ? keep : N)};
     if (keep == 0) return p;
     const long long least = (long long)round_up(8 * (size_t)keep, 4096);
     if (N > kOnePiece && N > 2 * least) p.first = least;
-    p.cap = N;
-    if (p.first < N) {
-        const long long room = kListBytes / 8 / B, need = p.first + 2 * kMostKept;
-        p.cap = room > need ? room : need;
-        if (p.cap > N + kMostKept) p.cap = N + kMostKept;
-    }
+    p.room = kListBytes / 8 / B > p.first ? kListBytes / 8 / B : p.first;
     return p;
 }
 
-inline hipError_t launch_select(const Lists& l, int B, int stored, hipStream_t st) {
-    hipLaunchKernelGGL(select_kernel<0>, dim3(B), dim3(kSelectThreads), 0, st, l, stored);
+// Where the lists lie in a workspace, behind `at` bytes.
+struct ListLayout {
+    long long cap = 0;
+    int regions = 0;
+    size_t keys_at, counts_at, kept_at, kept_count_at, floor_at, bytes;
+    void piece(long long keys, int n) {                          // a piece whose n workgroups' regions take so many keys
+        cap = keys > cap ? keys : cap;
+        regions = n > regions ? n : regions;
+    }
+    void lay_out(size_t at, int B, int keep) {
+        const size_t on = keep ? 1 : 0;
+        keys_at = round_up(at, 256);
+        counts_at = keys_at + round_up(on * B * cap * sizeof(uint64_t), 256);
+        kept_at = counts_at + round_up(on * B * regions * sizeof(int), 256);
+        kept_count_at = kept_at + round_up(on * B * kMostKept * sizeof(uint64_t), 256);
+        floor_at = kept_count_at + round_up(on * B * sizeof(int), 256);
+        bytes = floor_at + round_up(on * B * sizeof(float), 256);
+    }
+    Lists lists(unsigned char* ws, int keep) const {
+        return Lists{reinterpret_cast<uint64_t*>(ws + keys_at), reinterpret_cast<int*>(ws + counts_at), reinterpret_cast<uint64_t*>(ws + kept_at),
+                     reinterpret_cast<int*>(ws + kept_count_at), reinterpret_cast<float*>(ws + floor_at), cap, keep};
+    }
+};
+
+inline hipError_t launch_select(const Lists& l, int B, int stored, int regions, long long region, hipStream_t st) {
+    hipLaunchKernelGGL(select_kernel<0>, dim3(B), dim3(kSelectThreads), 0, st, l, B, stored, regions, region);
     return hipGetLastError();
 }
 

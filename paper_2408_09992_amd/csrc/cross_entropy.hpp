@@ -197,12 +197,14 @@ __device__ __forceinline__ void sum_items(const Args& a) {
     const int q0 = blockIdx.y * Q;
     const CT* codes = static_cast<const CT*>(a.codes);
     fill_tables<CT, Q>(table, a.S, q0, a.B, a.m, a.b);
-    __syncthreads();
 
     uint32_t from = 0, end = (uint32_t)a.N;
     if constexpr (PROBS) { from = a.first; end = a.end; }
     const uint32_t lo = from + blockIdx.x * a.share, hi = (uint32_t)min((long long)lo + a.share, (long long)end);
     float c[Q], s[Q], t[Q], floor[Q];
+    __shared__ int listed[PROBS ? Q : 1];
+    if (PROBS && (int)threadIdx.x < Q) listed[threadIdx.x] = 0;
+    const long long region = (long long)blockIdx.x * a.share;
 #pragma unroll
     for (int r = 0; r < Q; ++r) {
         c[r] = kLowest; s[r] = 0.0f; t[r] = 0.0f;
@@ -211,6 +213,7 @@ __device__ __forceinline__ void sum_items(const Args& a) {
             if (a.lists.keep && !a.store && q0 + r < a.B) floor[r] = a.lists.floor[q0 + r];
         }
     }
+    __syncthreads();
 
     auto step = [&](const Row<M, CT> (&row)[kUnits], uint32_t first, auto whole) {
         float z[kUnits][Q];
@@ -231,7 +234,7 @@ __device__ __forceinline__ void sum_items(const Args& a) {
             for (int u = 1; u < kUnits; ++u) top[r] = fmaxf(top[r], z[u][r]);
             if constexpr (PROBS) pass |= top[r] > floor[r];
             top[r] *= a.scale;
-            rise |= top[r] > c[r] + kHeadroom;
+            rise |= top[r] > c[r] + (PROBS ? kNearHeadroom : kHeadroom);
         }
         if constexpr (PROBS) {
             if (a.store) {
@@ -248,13 +251,13 @@ __device__ __forceinline__ void sum_items(const Args& a) {
                 for (int u = 0; u < kUnits; ++u)
 #pragma unroll
                     for (int r = 0; r < Q; ++r)
-                        if (z[u][r] > floor[r]) append(a.lists, q0 + r, z[u][r], first + u * kThreads);
+                        if (z[u][r] > floor[r]) append(a.lists, q0 + r, region, &listed[r], z[u][r], first + u * kThreads);
             }
         }
         if (__any(rise)) {
 #pragma unroll
             for (int r = 0; r < Q; ++r) {
-                if (top[r] > c[r] + kHeadroom) {
+                if (top[r] > c[r] + (PROBS ? kNearHeadroom : kHeadroom)) {
                     if constexpr (PROBS) raise_reference(c[r], s[r], t[r], top[r]);
                     else raise_reference(c[r], s[r], top[r]);
                 }
@@ -307,7 +310,10 @@ __device__ __forceinline__ void sum_items(const Args& a) {
         const int q = q0 + wave;
         if constexpr (PROBS) {
             for (int w = 1; w < kWaves; ++w) join_sums(sums.x, sums.y, sums.z, stat[w * Q + wave].x, stat[w * Q + wave].y, stat[w * Q + wave].z);
-            if (lane == 0) a.partial[(size_t)blockIdx.x * a.B + q] = sums;
+            if (lane == 0) {
+                a.partial[(size_t)blockIdx.x * a.B + q] = sums;
+                if (a.lists.keep && !a.store) a.lists.counts[(size_t)blockIdx.x * a.B + q] = listed[wave];
+            }
         } else {
             for (int w = 1; w < kWaves; ++w) join_sums(sums.x, sums.y, stat[w * Q + wave].x, stat[w * Q + wave].y);
             if (gridDim.x == 1 && a.targets) finish_position(sums.x, sums.y, a.codes, sizeof(CT), a.S, a.targets, a.N, a.m, a.b, q, a.loss, a.lse);

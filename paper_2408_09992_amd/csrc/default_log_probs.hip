@@ -8,22 +8,39 @@ namespace {
 // How many candidates for the K best are scored in 64 bits at least: float32 scores may put neighbours in another order, not items that far apart
 // (neighbours among the best 100 of 1.28M lie some 1e-3 of their scores apart, a sum's rounding 1e-6).
 int keep_of(int K) { return K ? K + 16 + K / 8 : 0; }
-static_assert(PQ_MAX_K + 16 + PQ_MAX_K / 8 + (PQ_MAX_K + 16 + PQ_MAX_K / 8) / 4 + 32 <= kMostKept, "a cut leaves no more");
+static_assert(most_of(PQ_MAX_K + 16 + PQ_MAX_K / 8) < kMostKept, "a cut leaves no more");
 
-struct Layout {
-    Passes pieces;
+// The cross entropy's plan of a piece, in no more groups than a list has regions; how many items' places a group has.
+DensePlan plan_piece(long long items, int B, int d, int type, long long& region) {
+    DensePlan p = plan_dense(items, B, d, type);
+    if (p.few) {
+        const long long of = kFewBytes / 2 / (d > 256 ? 512 : d > 128 ? 256 : d > 64 ? 128 : 64);
+        region = ceil_div(ceil_div(items, of), p.groups) * of;
+        return p;
+    }
+    while (p.groups > kMostRegions) {
+        p.tiles_each *= 2;
+        p.groups = (int)ceil_div(p.item_tiles, p.tiles_each);
+    }
+    region = (long long)p.tiles_each * p.loss_items;
+    return p;
+}
+
+struct Layout : ListLayout {
+    Passes passes;
     int groups;
-    size_t keys_at, count_at, floor_at, bytes;
 };
 Layout lay_out(long long N, int B, int d, int type, int K) {
     Layout l;
-    l.pieces = pieces_of(N, B, keep_of(K));
+    l.passes = passes_of(N, B, keep_of(K));
     l.groups = 0;
-    for (long long done = 0; done < N; done += l.pieces.after(done)) l.groups += plan_dense(l.pieces.after(done), B, d, type).groups;
-    l.keys_at = round_up((size_t)l.groups * B * sizeof(float4), 256);
-    l.count_at = l.keys_at + l.pieces.key_bytes(B);
-    l.floor_at = l.count_at + (K ? round_up((size_t)B * sizeof(int), 256) : 0);
-    l.bytes = l.floor_at + (K ? round_up((size_t)B * sizeof(float), 256) : 0);
+    for (long long done = 0, now, region; done < N; done += now) {
+        now = l.passes.after(done);
+        const DensePlan p = plan_piece(now, B, d, type, region);
+        l.groups += p.groups;
+        l.piece(done == 0 ? now : p.groups * region, p.groups);
+    }
+    l.ListLayout::lay_out((size_t)l.groups * B * sizeof(float4), B, K);
     return l;
 }
 
@@ -37,14 +54,18 @@ template <typename T>
 hipError_t pass(const Layout& l, DenseProbsArgs a, DenseFinishArgs f, int type, hipStream_t st) {
     hipError_t e = hipSuccess;
     for (long long done = 0; done < a.N && e == hipSuccess; done = a.end) {
-        const DensePlan p = plan_dense(l.pieces.after(done), a.B, a.d, type);
+        const long long now = l.passes.after(done);
+        const DensePlan p = plan_piece(now, a.B, a.d, type, a.region);
         a.first = done;
-        a.end = done + l.pieces.after(done);
+        a.end = done + now;
         a.store = f.K != 0 && done == 0;
         a.item_tiles = p.item_tiles; a.tiles_each = p.tiles_each; a.groups = p.groups; a.position_tiles = p.position_tiles;
         e = dense_probs<T>(p, a, st);
         a.partial += (size_t)p.groups * a.B;
-        if (e == hipSuccess && f.K && a.end < a.N) e = launch_select(a.lists, a.B, done == 0 ? (int)a.end : 0, st);
+        if (e == hipSuccess && f.K && a.end < a.N) e = launch_select(a.lists, a.B, a.store ? (int)now : 0, p.groups, a.region, st);
+        f.stored = a.store ? (int)now : 0;
+        f.regions = p.groups;
+        f.region = a.region;
     }
     return e != hipSuccess ? e : dense_probs_finish<T>(f, st);
 }
@@ -78,10 +99,8 @@ int pq_default_log_probs(const void* W, const void* queries, const int* items, l
     DenseProbsArgs a{};
     a.W = W; a.H = queries; a.N = N; a.B = B; a.d = d; a.scale = (float)(kLog2eDouble / temperature);
     a.partial = reinterpret_cast<float4*>(ws);
-    a.lists = Lists{reinterpret_cast<uint64_t*>(ws + l.keys_at), reinterpret_cast<int*>(ws + l.count_at), reinterpret_cast<float*>(ws + l.floor_at),
-                    (uint32_t)l.pieces.cap, l.pieces.keep};
-    const DenseFinishArgs f{W, queries, items, N, B, d, n, K, temperature, a.partial, l.groups, l.pieces.first == N ? (int)N : 0, a.lists,
-                            log_probs, entropy, lse, top_items, top_log_probs};
+    a.lists = l.lists(ws, l.passes.keep);
+    const DenseFinishArgs f{W, queries, items, N, B, d, n, K, temperature, a.partial, l.groups, 0, 0, 0, a.lists, log_probs, entropy, lse, top_items, top_log_probs};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return pqk::record_hip_error(type == PQ_FLOAT32 ? pass<float>(l, a, f, type, st) : type == PQ_BFLOAT16 ? pass<__bf16>(l, a, f, type, st) : pass<_Float16>(l, a, f, type, st));
 }

@@ -20,12 +20,13 @@ struct DenseProbsArgs {
     int tiles_each, groups, position_tiles;
     float4* partial;                                   // [groups][B]: (reference, sum, weighted sum)
     Lists lists;
+    long long region;                                  // items of a group
 };
 
-// A score that passes its position's floor to the list, or every one of the first piece.
-__device__ __forceinline__ void offer(const DenseProbsArgs& a, int q, float z, long long item) {
+// A score that passes its position's floor to the group's region of the list, or every one of the first piece.
+__device__ __forceinline__ void offer(const DenseProbsArgs& a, int q, int group, int* count, float z, long long item) {
     if (a.store) a.lists.keys[(size_t)q * a.lists.cap + (size_t)(item - a.first)] = key_of(z, (uint32_t)item);
-    else append(a.lists, q, z, (uint32_t)item);
+    else append(a.lists, q, group * a.region, count, z, (uint32_t)item);
 }
 
 template <typename T, int BN, int ITEMS>
@@ -33,6 +34,8 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     using Tile = ScoresTile<T, BN, ITEMS>;
     constexpr int MI = Tile::MI, NI = Tile::NI, kRowWaves = ITEMS / (32 * MI);
     __shared__ float4 stat[kRowWaves][BN];
+    __shared__ int listed[BN];
+    for (int i = threadIdx.x; i < BN; i += Tile::kThreads) listed[i] = 0;          // (the products' barriers come before any use)
     int group, pt;
     chiplet_order(blockIdx.x, a.position_tiles, group, pt);
     if (group >= a.groups) return;
@@ -76,12 +79,12 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int at = 32 * mi + 8 * (e / 4) + e % 4;
-                        if (a.store ? q0 + 32 * ni < a.B && at < left - 4 * (lane / 32) : acc[mi][ni][e] > floor[ni]) offer(a, q0 + 32 * ni, acc[mi][ni][e], mine + at);
+                        if (a.store ? q0 + 32 * ni < a.B && at < left - 4 * (lane / 32) : acc[mi][ni][e] > floor[ni]) offer(a, q0 + 32 * ni, group, &listed[Tile::wave_col() + 32 * ni + lane % 32], acc[mi][ni][e], mine + at);
                     }
             }
             top *= a.scale;
-            if (__any(top > c[ni] + kHeadroom)) {
-                if (top > c[ni] + kHeadroom) raise_reference(c[ni], s[ni], t[ni], top);
+            if (__any(top > c[ni] + kNearHeadroom)) {
+                if (top > c[ni] + kNearHeadroom) raise_reference(c[ni], s[ni], t[ni], top);
             }
             float sum = 0.0f, sum_x = 0.0f;
 #pragma unroll
@@ -108,6 +111,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
 #pragma unroll
         for (int w = 1; w < kRowWaves; ++w) join_sums(v.x, v.y, v.z, stat[w][threadIdx.x].x, stat[w][threadIdx.x].y, stat[w][threadIdx.x].z);
         a.partial[(size_t)group * a.B + q] = v;
+        if (a.lists.keep && !a.store) a.lists.counts[(size_t)group * a.B + q] = listed[threadIdx.x];
     }
 }
 
@@ -118,6 +122,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_log_probs_kernel(D
     using RowsD = Rows<D / 8>;
     __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2];
     __shared__ float4 stat[kWaves][kFew];
+    __shared__ int listed[kFew];
+    if (threadIdx.x < kFew) listed[threadIdx.x] = 0;
     constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
     constexpr int kBlocksZ = IT / 16 * 4 / kWaves, kParts = kBlocksZ < 4 ? kBlocksZ : 4;       // a wave's blocks of 16 x 16; positions among them / 16
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -156,10 +162,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_log_probs_kernel(D
                 const long long mine = a.first + tile * IT + item0 + lane / 16 * 4;
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (a.store ? pos < a.B && e < left : z[e] > floor[part]) offer(a, pos, z[e], mine + e);
+                    if (a.store ? pos < a.B && e < left : z[e] > floor[part]) offer(a, pos, blockIdx.x, &listed[pos], z[e], mine + e);
             }
-            if (__any(top > c[part] + kHeadroom)) {
-                if (top > c[part] + kHeadroom) raise_reference(c[part], s[part], t[part], top);
+            if (__any(top > c[part] + kNearHeadroom)) {
+                if (top > c[part] + kNearHeadroom) raise_reference(c[part], s[part], t[part], top);
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -184,6 +190,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_log_probs_kernel(D
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) join_sums(v.x, v.y, v.z, stat[w][tid].x, stat[w][tid].y, stat[w][tid].z);
         a.partial[(size_t)blockIdx.x * a.B + tid] = v;
+        if (a.lists.keep && !a.store) a.lists.counts[(size_t)blockIdx.x * a.B + tid] = listed[tid];
     }
 }
 
@@ -194,7 +201,8 @@ struct DenseFinishArgs {
     int B, d, n, K;
     float temperature;
     const float4* partial;     // [groups][B], of all pieces
-    int groups, stored;
+    int groups, stored, regions;                       // groups of all pieces; of the last piece what cut_list() takes
+    long long region;
     Lists lists;
     float *log_probs, *entropy, *lse;
     int* top_items;
@@ -207,7 +215,6 @@ __global__ __launch_bounds__(kSelectThreads) void default_log_probs_finish_kerne
     __shared__ SelectMemory mem;
     __shared__ uint64_t kept[kMostKept];
     __shared__ double score[kMostKept];
-    __shared__ int count;
     __shared__ float4 sums[kSelectWaves];
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     float c = kLowest, s = 0.0f, t = 0.0f;
@@ -235,7 +242,8 @@ __global__ __launch_bounds__(kSelectThreads) void default_log_probs_finish_kerne
         if (tid % 16 == 0) a.log_probs[(size_t)q * a.n + i] = there ? log_prob(z) : 0.0f;
     }
     if (a.K == 0) return;
-    const int n = last_cut(a.lists, q, a.stored, kept, count, mem);
+    uint64_t least;
+    const int n = cut_list(a.lists, q, a.B, a.stored, a.regions, a.region, true, kept, least, mem);
     for (int i = tid / 16; i < n; i += kSelectThreads / 16) {
         const double z = dot64(W + (size_t)item_of(kept[i]) * a.d, h, a.d);
         if (tid % 16 == 0) score[i] = z;

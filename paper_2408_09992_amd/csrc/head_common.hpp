@@ -44,6 +44,8 @@ __device__ __forceinline__ void raise_reference(float& c, float& s, float top) {
     c = to;
 }
 // Besides, a sum of terms 2^x x (what an entropy is made of): total = 2^c (t + c s).  A term's x is held over -200, where 2^x is 0 and -inf would make NaN.
+// An entropy is the small difference of log2 s and t / s where few items have most of the mass, so the reference stays near the largest score.
+constexpr float kNearHeadroom = 4.0f;
 __device__ __forceinline__ float weighted(float p, float x, float t) { return fmaf(p, fmaxf(x, -200.0f), t); }
 __device__ __forceinline__ void join_sums(float& c, float& s, float& t, float c2, float s2, float t2) {
     const float top = fmaxf(c, c2), f = exp2_fast(c - top), f2 = exp2_fast(c2 - top);
@@ -59,7 +61,7 @@ __device__ __forceinline__ void raise_reference(float& c, float& s, float& t, fl
 }
 // - sum_i p log p in nats: log p = ln 2 (x - log2 s).  0 where no score counts.
 __device__ __forceinline__ float entropy_of(float s, float t) {
-    return s == 0.0f ? 0.0f : s < __builtin_inff() ? fmaxf((__log2f(s) - t / s) * kLn2, 0.0f) : __builtin_nanf("");
+    return s == 0.0f ? 0.0f : s < __builtin_inff() ? (float)fmax((log2((double)s) - (double)t / (double)s) / 1.4426950408889634, 0.0) : __builtin_nanf("");
 }
 // log-sum: -inf where no score counts, NaN where one is NaN, +inf or counts as that.
 __device__ __forceinline__ float log_sum(float c, float s) {

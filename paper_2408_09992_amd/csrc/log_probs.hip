@@ -23,7 +23,8 @@ struct FinishArgs {
     int B, m, b, n, K, code_bytes;
     float temperature;
     const float4* partial;     // [shares][B]
-    int shares, stored;
+    int shares, stored, regions;                       // shares of all pieces; of the last piece what cut_list() takes
+    long long region;
     Lists lists;
     float *log_probs, *entropy, *lse;
     int* top_items;
@@ -46,7 +47,6 @@ __device__ __forceinline__ float score_of_item(const FinishArgs& a, int q, int i
 __global__ __launch_bounds__(kSelectThreads) void log_probs_finish_kernel(FinishArgs a) {
     __shared__ SelectMemory mem;
     __shared__ uint64_t kept[kMostKept];
-    __shared__ int count;
     __shared__ float4 sums[kSelectWaves];
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     float c = kLowest, s = 0.0f, t = 0.0f;
@@ -71,7 +71,8 @@ __global__ __launch_bounds__(kSelectThreads) void log_probs_finish_kernel(Finish
         a.log_probs[(size_t)q * a.n + i] = item >= 0 && item < a.N ? log_prob(score_of_item(a, q, item)) : 0.0f;
     }
     if (a.K == 0) return;
-    const int n = last_cut(a.lists, q, a.stored, kept, count, mem);
+    uint64_t least;
+    const int n = cut_list(a.lists, q, a.B, a.stored, a.regions, a.region, true, kept, least, mem);
     if (tid < n) {
         const uint64_t mine = kept[tid];
         int rank = 0;
@@ -111,23 +112,21 @@ hipError_t go_m(const Plan& p, const ProbsArgs& a, hipStream_t st) {
 }
 
 // Where the workspace's parts lie.
-struct Layout {
-    Passes pieces;
+struct Layout : ListLayout {
+    Passes passes;
     int shares;
-    size_t keys_at, count_at, floor_at, bytes;
 };
 bool lay_out(Layout& l, long long N, int B, int m, int b, int K, int code_bytes) {
-    l.pieces = pieces_of(N, B, K);
+    l.passes = passes_of(N, B, K);
     l.shares = 0;
-    for (long long done = 0; done < N; done += l.pieces.after(done)) {
+    for (long long done = 0, now; done < N; done += now) {
         Plan p;
-        if (!plan_loss(p, l.pieces.after(done), B, m, b, code_bytes, true)) return false;
+        now = l.passes.after(done);
+        if (!plan_loss(p, now, B, m, b, code_bytes, true)) return false;
         l.shares += p.shares;
+        l.piece(done == 0 ? now : (long long)p.shares * p.share, p.shares);
     }
-    l.keys_at = round_up((size_t)l.shares * B * sizeof(float4), 256);
-    l.count_at = l.keys_at + l.pieces.key_bytes(B);
-    l.floor_at = l.count_at + (K ? round_up((size_t)B * sizeof(int), 256) : 0);
-    l.bytes = l.floor_at + (K ? round_up((size_t)B * sizeof(float), 256) : 0);
+    l.ListLayout::lay_out((size_t)l.shares * B * sizeof(float4), B, K);
     return true;
 }
 
@@ -157,25 +156,24 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
     if (ws_bytes < l.bytes) return PQ_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
-    const Lists lists{reinterpret_cast<uint64_t*>(ws + l.keys_at), reinterpret_cast<int*>(ws + l.count_at), reinterpret_cast<float*>(ws + l.floor_at),
-                      (uint32_t)l.pieces.cap, l.pieces.keep};
+    const Lists lists = l.lists(ws, l.passes.keep);
     ProbsArgs a{codes, S, N, B, m, b, 0, (float)(kLog2eDouble / temperature), 0, 0, 0, reinterpret_cast<float4*>(ws), lists};
     hipError_t e = hipSuccess;
+    Plan p;
     for (long long done = 0; done < N && e == hipSuccess; done = a.end) {
-        Plan p;
-        const long long items_now = l.pieces.after(done);
-        plan_loss(p, items_now, B, m, b, sizeof(CT), true);
+        const long long now = l.passes.after(done);
+        plan_loss(p, now, B, m, b, sizeof(CT), true);
         a.first = (uint32_t)done;
-        a.end = (uint32_t)(done + items_now);
+        a.end = (uint32_t)(done + now);
         a.share = p.share;
         a.store = K != 0 && done == 0;
         e = go_m<CT>(p, a, st);
         a.partial += (size_t)p.shares * B;
-        if (e == hipSuccess && K && a.end < N) e = launch_select(lists, B, done == 0 ? (int)items_now : 0, st);
+        if (e == hipSuccess && K && a.end < N) e = launch_select(lists, B, a.store ? (int)now : 0, p.shares, p.share, st);
     }
     if (e == hipSuccess) {
         const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), temperature, reinterpret_cast<const float4*>(ws), l.shares,
-                           l.pieces.first == N ? (int)N : 0, lists, out, entropy, lse, top_items, top_log_probs};
+                           a.store ? (int)N : 0, p.shares, p.share, lists, out, entropy, lse, top_items, top_log_probs};
         hipLaunchKernelGGL(log_probs_finish_kernel, dim3(B), dim3(kSelectThreads), 0, st, f);
         e = hipGetLastError();
     }
