@@ -16,7 +16,7 @@ namespace head {
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
 constexpr int kMostKept = 1024;                      // keys that a cut leaves at most
 constexpr int kMostRegions = 2048;                   // workgroups that share the items of a piece
-constexpr int kLocalKeys = 4096;                     // keys that a cut brings to LDS at once; of more each pass reads all again
+constexpr int kFewKeys = 4, kManyKeys = 16;          // keys that a thread of a cut holds; where a list has more each pass reads them again
 
 struct Lists {
     uint64_t* keys;            // [B][cap]: all keys of the first piece, or the regions of a later one
@@ -47,7 +47,6 @@ __device__ __forceinline__ void append(const Lists& l, int q, long long region, 
 }
 
 struct SelectMemory {
-    uint64_t local[kLocalKeys];
     uint32_t histogram[2048];
     int begin[kMostRegions];                         // where a region's keys begin among all of them
     uint64_t part[kSelectWaves][2];
@@ -96,18 +95,48 @@ struct Keys {
     }
 };
 
-// A key that at least `keep` of n keys, and no more than `most` (over `keep`) of them, reach; 0 if n <= keep.  By histograms of 2048 bins over
-// the range that is left, each pass a look at all keys: one or two in the usual case, six at most (keys differ).
-template <typename K>
-__device__ __forceinline__ uint64_t cut(const K& key, int n, int keep, int most, SelectMemory& mem) {
+// A list's keys as a cut's passes meet them: R a thread in registers, or each from where it lies.
+template <int R>
+struct HeldKeys {
+    uint64_t k[R];
+    int n;
+    __device__ __forceinline__ HeldKeys(const Keys& all) : n(all.n) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int i = (int)threadIdx.x + r * kSelectThreads;
+            k[r] = i < n ? all(i) : 0;
+        }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if ((int)threadIdx.x + r * kSelectThreads < n) f(k[r]);
+    }
+};
+struct FarKeys {
+    const Keys& all;
+    int n;
+    __device__ __forceinline__ FarKeys(const Keys& keys) : all(keys), n(keys.n) {}
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        for (int i = threadIdx.x; i < n; i += kSelectThreads) f(all(i));
+    }
+};
+
+// A key that at least `keep` of the keys, and no more than `most` (over `keep`) of them, reach; 0 if there are no more than `keep`.  By histograms of 2048
+// bins over the range that is left, each pass a look at all keys: one or two in the usual case, six at most (keys differ).
+template <typename H>
+__device__ __forceinline__ uint64_t cut(const H& held, int keep, int most, SelectMemory& mem) {
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    if (n <= keep) return 0;
+    if (held.n <= keep) return 0;
     uint64_t low = ~0ull, high = 0;
-    for (int i = tid; i < n; i += kSelectThreads) {
-        const uint64_t k = key(i);
+    held.each([&](uint64_t k) {
         low = k < low ? k : low;
         high = k > high ? k : high;
-    }
+    });
+    mem.histogram[tid] = 0;
+    mem.histogram[tid + 1024] = 0;
 #pragma unroll
     for (int x = 1; x < kWave; x *= 2) {
         const uint64_t l = __shfl_xor(low, x), h = __shfl_xor(high, x);
@@ -116,21 +145,20 @@ __device__ __forceinline__ uint64_t cut(const K& key, int n, int keep, int most,
     }
     if (lane == 0) { mem.part[wave][0] = low; mem.part[wave][1] = high; }
     __syncthreads();
+    low = mem.part[lane % kSelectWaves][0];
+    high = mem.part[lane % kSelectWaves][1];
 #pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) {
-        low = mem.part[w][0] < low ? mem.part[w][0] : low;
-        high = mem.part[w][1] > high ? mem.part[w][1] : high;
+    for (int x = 1; x < kSelectWaves; x *= 2) {
+        const uint64_t l = __shfl_xor(low, x), h = __shfl_xor(high, x);
+        low = l < low ? l : low;
+        high = h > high ? h : high;
     }
     int above = 0;                                                // keys over the range
     while (true) {
         const int bits = 64 - __clzll((long long)((high - low) | 1)), shift = bits > 11 ? bits - 11 : 0;
-        mem.histogram[tid] = 0;
-        mem.histogram[tid + 1024] = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += kSelectThreads) {
-            const uint64_t k = key(i);
+        held.each([&](uint64_t k) {
             if (k >= low && k <= high) atomicAdd(&mem.histogram[(uint32_t)((k - low) >> shift)], 1u);
-        }
+        });
         __syncthreads();
         // thread t has the bins 2047 - 2t and 2046 - 2t: what lies over them by a scan
         const uint32_t upper = mem.histogram[2047 - 2 * tid], lower = mem.histogram[2046 - 2 * tid];
@@ -142,6 +170,8 @@ __device__ __forceinline__ uint64_t cut(const K& key, int n, int keep, int most,
             mem.above = (int)(first ? begin : begin + upper);
             mem.taken = (int)(first ? begin + upper : end);
         }
+        mem.histogram[2047 - 2 * tid] = 0;                        // (its own two)
+        mem.histogram[2046 - 2 * tid] = 0;
         __syncthreads();
         low += (uint64_t)mem.chosen << shift;
         above = mem.above;
@@ -175,18 +205,15 @@ __device__ __forceinline__ int cut_list(const Lists& l, int q, int B, int stored
     }
     if (tid == 0) mem.count = 0;
     __syncthreads();
-    const int n = all.n;
-    auto local = [&](int i) { return mem.local[i]; };
-    if (n <= kLocalKeys) {
-        for (int i = tid; i < n; i += kSelectThreads) mem.local[i] = all(i);
-        __syncthreads();
-        least = last && n <= most ? 0 : cut(local, n, l.keep, most, mem);
-    } else least = cut(all, n, l.keep, most, mem);
-    auto take = [&](uint64_t k) {
-        if (k >= least) out[atomicAdd(&mem.count, 1)] = k;
+    auto run = [&](const auto& held) {
+        least = last && held.n <= most ? 0 : cut(held, l.keep, most, mem);
+        held.each([&](uint64_t k) {
+            if (k >= least) out[atomicAdd(&mem.count, 1)] = k;
+        });
     };
-    if (n <= kLocalKeys) for (int i = tid; i < n; i += kSelectThreads) take(mem.local[i]);
-    else for (int i = tid; i < n; i += kSelectThreads) take(all(i));
+    if (all.n <= kFewKeys * kSelectThreads) run(HeldKeys<kFewKeys>(all));
+    else if (all.n <= kManyKeys * kSelectThreads) run(HeldKeys<kManyKeys>(all));
+    else run(FarKeys(all));
     __syncthreads();
     return mem.count;
 }

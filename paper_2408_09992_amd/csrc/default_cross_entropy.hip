@@ -102,7 +102,7 @@ DensePlan plan_dense(long long N, int B, int d, int type) {
     p.slices = (int)(slices < 1 ? 1 : slices > most ? most : slices);
     p.few = size == 2 && B <= kFew && d <= 512;
     if (p.few) {                                       // a workgroup per compute unit; dz stays in LDS
-        const long long few_tiles = ceil_div(N, kFewBytes / 2 / (d > 256 ? 512 : d > 128 ? 256 : d > 64 ? 128 : 64));
+        const long long few_tiles = ceil_div(N, few_items(d));
         p.slices = p.groups = (int)(few_tiles < kCUs ? few_tiles : kCUs);
         p.padded = kFew;
         p.piece = 0;

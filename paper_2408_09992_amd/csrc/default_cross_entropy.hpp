@@ -11,6 +11,7 @@
 #include <type_traits>
 #include "pqtopk_train.h"
 #include "matrix_tile.hpp"
+#include "alternatives.hpp"
 
 namespace pqk {
 namespace head {
@@ -99,6 +100,8 @@ struct DenseArgs {
     int entries;
 };
 constexpr int kNoItem = 0x7FFFFFFF;
+// Which of `groups` workgroups of default_few_kernel has an item, tiles of `of` items taken by turns.
+__device__ __forceinline__ int few_owner(int item, int of, int groups) { return item == kNoItem ? kNoItem : item / of % groups; }
 
 template <typename T>
 __device__ __forceinline__ Operand items_of(const DenseArgs& a, long long item) {
@@ -611,76 +614,188 @@ __device__ __forceinline__ void bring_rows(const void* base, int d, long long ro
     }
 }
 
-// The loss of up to 64 positions of 16-bit operands, d <= 512: as default_few_kernel below takes its tiles, so that loads do not
-// pause between them (64 positions, 1.3 GB of W: 250 to 262 us, 5.0 to 5.2 TB/s; 271 by default_cross_entropy_kernel's tiles).
-template <typename T, int D>
-__global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseArgs a) {
+// The sums of up to 64 positions of 16-bit operands, d <= 512, over the items from..end - 1: a workgroup a compute unit, tiles of 32 KB of W by turns.
+// What a wave multiplies of the queries stays in its registers (64 of them; 32 for D = 64), so that LDS holds four tiles, three of them on their way: 24 MB
+// in flight over the chip, where the memory's rate times its latency is some 13.  Every lane's products and sums are in the order of the tiles.
+// PROBS: the entropy's sum besides, and scores over the floors (all of a first piece: a.store) to the lists.  Candidates wait in LDS until the tiles are
+// done, as a store between the loads would have to be waited for with them.
+constexpr int kFewWaiting = 1024;
+// (In assembly: the compiler takes these places in LDS for ones that a load under way may write, and would wait for all of them.)
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
+__device__ __forceinline__ int lds_count(int* counter) {
+    int old;
+    asm volatile("ds_add_rtn_u32 %0, %1, %2\n\ts_waitcnt lgkmcnt(0)" : "=&v"(old) : "v"(lds_address(counter)), "v"(1) : "memory");
+    return old;
+}
+__device__ __forceinline__ void lds_put(uint64_t* key_at, uint64_t key, unsigned char* position_at, int position) {
+    asm volatile("ds_write_b64 %0, %1\n\tds_write_b8 %2, %3" ::"v"(lds_address(key_at)), "v"(key), "v"(lds_address(position_at)), "v"(position) : "memory");
+}
+template <typename T, int D, bool PROBS, typename Args>
+__device__ __forceinline__ void few_sums(const Args& a, long long from, long long end) {
     constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
     using RowsD = Rows<D / 8>;
-    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2];
-    __shared__ float2 stat[kWaves][kFew];
-    constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
+    using Sums = typename std::conditional<PROBS, float4, float2>::type;
+    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], w2[kFewBytes], w3[kFewBytes];
+    __shared__ uint64_t waiting[PROBS ? kFewWaiting : 1];
+    __shared__ unsigned char waiting_for[PROBS ? kFewWaiting : 1];
+    __shared__ int listed[PROBS ? kFew : 1], waits;
+    constexpr int kLoadsW = kFewBytes / 16 / kFewThreads;
     constexpr int kBlocksZ = IT / 16 * 4 / kWaves, kParts = kBlocksZ < 4 ? kBlocksZ : 4;       // a wave's blocks of 16 x 16; positions among them / 16
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const long long tiles = (a.N + IT - 1) / IT;
-    bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h);
-    bring_rows<T, D, kLoadsW>(a.W, a.d, (long long)blockIdx.x * IT, a.N, w0);
-    float c[kParts], s[kParts];
+    const long long tiles = (end - from + IT - 1) / IT;
+    if constexpr (PROBS) {
+        if (tid < kFew) listed[tid] = 0;
+        if (tid == 0) waits = 0;
+    }
+    // the queries' operands: position lane % 16 of a block's sixteen, eight k of every 32
+    s16x8 h[kParts][D / 32];
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) { c[i] = kLowest; s[i] = 0.0f; }
-    int turn = 0;
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
-        const unsigned char* w = turn % 2 ? w1 : w0;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the tile has come, its other buffer is free
-        bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
+    for (int i = 0; i < kParts; ++i) {
+        const int pos = min((wave * kBlocksZ + i) % 4 * 16 + lane % 16, a.B - 1);
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) {
+            const int at = (4 * k + lane / 16) * 8;
+            h[i][k] = s16x8{};
+            if (at < a.d) h[i][k] = *reinterpret_cast<const s16x8*>(static_cast<const T*>(a.H) + (size_t)pos * a.d + at);
+        }
+    }
+    float c[kParts], s[kParts], t[kParts], floor[kParts];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        c[i] = kLowest; s[i] = 0.0f; t[i] = 0.0f;
+        floor[i] = __builtin_inff();
+        if constexpr (PROBS) {
+            const int pos = (wave * kBlocksZ + i) % 4 * 16 + lane % 16;
+            if (a.lists.keep && !a.store && pos < a.B) floor[i] = a.lists.floor[pos];
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (only W's loads are counted from here on, also by the compiler)
+#pragma unroll
+    for (int i = 0; i < kParts; ++i)
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) asm volatile("" : "+v"(h[i][k]));
+    auto bring = [&](long long tile, unsigned char* to) { bring_rows<T, D, kLoadsW>(a.W, a.d, from + min(tile, tiles - 1) * IT, a.N, to); };
+    const long long by = gridDim.x;
+    auto step = [&](long long tile, const unsigned char* w, unsigned char* next) {
+        // the tile has come when two later ones alone are on their way; past the barrier that holds for all waves, which are done with `next`, too
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kLoadsW) : "memory");
+        bring(tile + 3 * by, next);
 #pragma unroll
         for (int i = 0; i < kBlocksZ; ++i) {
-            const int block = wave * kBlocksZ + i, item0 = block / 4 * 16, pos = block % 4 * 16 + lane % 16;
+            const int block = wave * kBlocksZ + i, item0 = block / 4 * 16, part = i % kParts;
             f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k)
-                z = multiply16<T>(RowsD::along(w, item0 + lane % 16, 4 * k + lane / 16), RowsD::along(h, pos, 4 * k + lane / 16), z);
-            const int left = left_of(a.N - tile * IT - item0, 16) - lane / 16 * 4;
+            for (int k = 0; k < D / 32; ++k) z = multiply16<T>(RowsD::along(w, item0 + lane % 16, 4 * k + lane / 16), h[part][k], z);
+            const int left = left_of(end - from - tile * IT - item0, 16) - lane / 16 * 4;
             if (left < 4) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (e >= left) z[e] = -__builtin_inff();
             }
-            const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) * a.scale;
-            const int part = i % kParts;
-            if (__any(top > c[part] + kHeadroom)) {
-                if (top > c[part] + kHeadroom) raise_reference(c[part], s[part], top);
+            const float raw = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), top = raw * a.scale;
+            if constexpr (PROBS) {
+                const int pos = block % 4 * 16 + lane % 16;
+                const long long mine = from + tile * IT + item0 + lane / 16 * 4;
+                if (a.store) {
+                    stay_a_branch();
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (pos < a.B && e < left) a.lists.keys[(size_t)pos * a.lists.cap + (size_t)(mine + e - from)] = key_of(z[e], (uint32_t)(mine + e));
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                } else if (__any(raw > floor[part])) {
+                    stay_a_branch();
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (z[e] > floor[part]) {
+                            const int at = lds_count(&waits);
+                            if (at < kFewWaiting) lds_put(&waiting[at], key_of(z[e], (uint32_t)(mine + e)), &waiting_for[at], pos);
+                            else {
+                                append(a.lists, pos, blockIdx.x * a.region, &listed[pos], z[e], (uint32_t)(mine + e));
+                                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                            }
+                        }
+                }
+            }
+            constexpr float kRoom = PROBS ? kNearHeadroom : kHeadroom;
+            if (__any(top > c[part] + kRoom)) {
+                if (top > c[part] + kRoom) {
+                    if constexpr (PROBS) raise_reference(c[part], s[part], t[part], top);
+                    else raise_reference(c[part], s[part], top);
+                }
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[part] += exp2_fast(fmaf(z[e], a.scale, -c[part]));
+            for (int e = 0; e < 4; ++e) {
+                const float x = fmaf(z[e], a.scale, -c[part]), p = exp2_fast(x);
+                s[part] += p;
+                if constexpr (PROBS) t[part] = weighted(p, x, t[part]);
+            }
         }
+    };
+    const long long first = blockIdx.x;
+    bring(first, w0);
+    bring(first + by, w1);
+    bring(first + 2 * by, w2);
+    // (without a way out of the loop's middle, from which the compiler would count fewer loads under way at its start)
+    long long turns = first < tiles ? (tiles - first + by - 1) / by : 0, tile = first;
+    for (; turns >= 4; turns -= 4, tile += 4 * by) {
+        step(tile, w0, w3);
+        step(tile + by, w1, w0);
+        step(tile + 2 * by, w2, w1);
+        step(tile + 3 * by, w3, w2);
     }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");                  // (a last load into LDS may be under way)
-    for (int q = lane; q < kFew; q += kWave) stat[wave][q] = make_float2(kLowest, 0.0f);
+    if (turns > 0) step(tile, w0, w3);
+    if (turns > 1) step(tile + by, w1, w0);
+    if (turns > 2) step(tile + 2 * by, w2, w1);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (the last loads into LDS may be under way)
+    Sums (*stat)[kFew] = reinterpret_cast<Sums (*)[kFew]>(w0);                  // [kWaves][kFew]
+    for (int q = lane; q < kFew; q += kWave) {
+        if constexpr (PROBS) stat[wave][q] = make_float4(kLowest, 0.0f, 0.0f, 0.0f);
+        else stat[wave][q] = make_float2(kLowest, 0.0f);
+    }
     wave_reads_after_writes();
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
 #pragma unroll
         for (int x = 16; x < kWave; x *= 2) {
             const float c2 = __shfl_xor(c[i], x), s2 = __shfl_xor(s[i], x);
-            join_sums(c[i], s[i], c2, s2);
+            if constexpr (PROBS) join_sums(c[i], s[i], t[i], c2, s2, __shfl_xor(t[i], x));
+            else join_sums(c[i], s[i], c2, s2);
         }
-        if (lane < 16) stat[wave][(wave * kBlocksZ + i) % 4 * 16 + lane] = make_float2(c[i], s[i]);
+        if (lane < 16) {
+            const int pos = (wave * kBlocksZ + i) % 4 * 16 + lane;
+            if constexpr (PROBS) stat[wave][pos] = make_float4(c[i], s[i], t[i], 0.0f);
+            else stat[wave][pos] = make_float2(c[i], s[i]);
+        }
+    }
+    if constexpr (PROBS) {
+        for (int i = tid; i < min(waits, kFewWaiting); i += kFewThreads) {
+            const int pos = waiting_for[i];
+            a.lists.keys[(size_t)pos * a.lists.cap + blockIdx.x * a.region + atomicAdd(&listed[pos], 1)] = waiting[i];
+        }
     }
     __syncthreads();
     if (tid < a.B) {
-        float2 t = stat[0][tid];
+        Sums v = stat[0][tid];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) join_sums(t.x, t.y, stat[w][tid].x, stat[w][tid].y);
-        a.partial[(size_t)blockIdx.x * a.B + tid] = t;
+        for (int w = 1; w < kWaves; ++w) {
+            if constexpr (PROBS) join_sums(v.x, v.y, v.z, stat[w][tid].x, stat[w][tid].y, stat[w][tid].z);
+            else join_sums(v.x, v.y, stat[w][tid].x, stat[w][tid].y);
+        }
+        a.partial[(size_t)blockIdx.x * a.B + tid] = v;
+        if constexpr (PROBS) {
+            if (a.lists.keep && !a.store) a.lists.counts[(size_t)blockIdx.x * a.B + tid] = listed[tid];
+        }
     }
 }
+
+template <typename T, int D>
+__global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseArgs a) { few_sums<T, D, false>(a, 0, a.N); }
 
 // D: d rounded up to 64, 128, 256 or 512.  A tile holds 16384 / D items.  Bound by memory: W in, dW out, 2.6 GB for 1.27M items
 // of 512 elements in 515 to 550 us, 4.7 to 5.1 TB/s, where a copy reaches 4.73.
 // PARTS: two rows of dz a position (kTwoParts), in the place of the other 32 positions.
-// DISTIL: dz of a tile's items that are listed is put right in LDS.  A workgroup's tiles follow each other then, and a lane of its first wave
-// goes along its position's list, which is in the order of the items, with the next two entries in registers.
+// DISTIL: dz of a tile's items that are listed is put right in LDS.  A lane of a workgroup's first wave goes along its position's list, which is in
+// the order of the workgroups and of the items of each (few_owner), with the next two entries in registers.
 template <typename T, int D, bool PARTS, bool DISTIL>
 __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a) {
     constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
@@ -697,23 +812,22 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const long long tiles = (a.N + IT - 1) / IT;
     constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
-    const long long each = DISTIL ? (tiles + gridDim.x - 1) / gridDim.x : 1, tile0 = (long long)blockIdx.x * each;
-    const long long by = DISTIL ? 1 : gridDim.x, end = DISTIL ? min(tiles, tile0 + each) : tiles;
     bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h, PARTS ? a.B : 0);
-    bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile0, tiles - 1) * IT, a.N, w0);
+    bring_rows<T, D, kLoadsW>(a.W, a.d, (long long)blockIdx.x * IT, a.N, w0);
     __shared__ int listed[2];
     int cursor = 0, item[2] = {kNoItem, kNoItem};
     float value[2] = {0.0f, 0.0f};
     const size_t list = (size_t)min(lane, a.B - 1) * a.entries;
     auto entry = [&](int i, int& to, float& v) {               // (behind the list's end there are no items)
         const size_t at = list + min(cursor + i, a.entries - 1);
-        to = cursor + i < a.entries ? a.entry_items[at] : kNoItem;
+        const int x = cursor + i < a.entries ? a.entry_items[at] : kNoItem;
+        to = few_owner(x, IT, (int)gridDim.x) == (int)blockIdx.x ? x : kNoItem;
         v = a.entry_values[at];
     };
     if (DISTIL && wave == 0 && lane < a.B) {
-        for (int first = 0, count = a.entries; count > 0;) {   // the first entry that is not before the workgroup's tiles
+        for (int first = 0, count = a.entries; count > 0;) {   // the first entry that is not an earlier workgroup's
             const int half = count / 2;
-            const bool before = a.entry_items[list + first + half] < tile0 * IT;
+            const bool before = few_owner(a.entry_items[list + first + half], IT, (int)gridDim.x) < (int)blockIdx.x;
             first = before ? first + half + 1 : first;
             count = before ? count - half - 1 : half;
             cursor = first;
@@ -744,7 +858,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     for (int i = tid; i < kFew * D / 8; i += kFewThreads)      // (a position that adds nothing may hold anything, NaN too)
         if (info[i / (D / 8)].at == __builtin_inff()) reinterpret_cast<uint4*>(h)[i] = uint4{0, 0, 0, 0};
     const float factor = factor_of_all;
-    for (long long tile = tile0; tile < end; tile += by, ++turn) {
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
         unsigned char* w = turn % 2 ? w1 : w0;
         if (DISTIL && wave == 0) {
             const int any = __any(item[0] < min((tile + 1) * IT, a.N));
@@ -752,7 +866,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
         }
         // every wave's part of the tile has come (below), and every wave is done with the other buffer
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + by, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
+        bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
 
         // z and dz: blocks of 16 items x 16 rows
         constexpr int kBlocksZ = IT / 16 * 4 / kWaves;
@@ -905,6 +1019,7 @@ __attribute__((visibility("hidden"))) DensePlan plan_dense(long long N, int B, i
 __attribute__((visibility("hidden"))) int check_dense(long long N, int B, int d, int type);
 __attribute__((visibility("hidden"))) void set_gradient(DenseArgs& a, const DensePlan& p, void* workspace);
 
+inline int few_items(int d) { return kFewBytes / 2 / (d > 256 ? 512 : d > 128 ? 256 : d > 64 ? 128 : 64); }     // of a tile of the kernels for few positions
 inline int grid_of(long long outer, long long inner) { return (int)(ceil_div(outer, 8) * 8 * inner); }     // see chiplet_order()
 
 constexpr int kSliceItems = 64;                        // a slice of dH's items is a multiple of this

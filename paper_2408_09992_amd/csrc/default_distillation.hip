@@ -29,6 +29,7 @@ struct ListArgs {
     float* share;
     int* entry_items;
     float* entry_values;
+    int few_items, few_groups;                         // default_few_kernel's tiles and workgroups, where it makes the gradient
 };
 
 // The list's items' scores in score[], sixteen lanes an entry.
@@ -76,12 +77,13 @@ __global__ __launch_bounds__(kListThreads) void default_distillation_join_kernel
     }
 }
 
-// grid = positions: the position's share of the gradient and its list in the order of the items, each with p less what the teacher gives the
+// grid = positions: the position's share of the gradient and its list in the order of the items (of default_few_kernel's workgroups first), each with p less what the teacher gives the
 // item (all its entries together, in the list's order: the same in each of them).
 template <typename T>
 __global__ __launch_bounds__(kListThreads) void default_list_kernel(ListArgs a) {
     __shared__ double part[kListWaves], score[kMostEntries], weight[kMostEntries];
     __shared__ int item[kMostEntries];
+    __shared__ long long order[kMostEntries];
     const int q = blockIdx.x, tid = threadIdx.x;
     const Teacher<kListThreads> t = teacher_of<kListThreads>(a.items, a.scores, q, a.K, a.N, a.temperature, part);
     const float lse = a.lse_in[q];
@@ -92,14 +94,17 @@ __global__ __launch_bounds__(kListThreads) void default_list_kernel(ListArgs a) 
     __syncthreads();
     score_list<T>(a, q, item, score);
     __syncthreads();
-    if (tid >= a.K) return;
     const int mine = item[tid] < 0 ? kNoItem : item[tid];
+    // (what orders the entries: the workgroup over the item)
+    auto order_of = [&](int i) { return (long long)(a.few_groups ? few_owner(i, a.few_items, a.few_groups) : 0) << 32 | i; };
+    order[tid] = order_of(mine);
+    __syncthreads();
+    if (tid >= a.K) return;
     double all = 0.0;
     int rank = 0;
     for (int k = 0; k < a.K; ++k) {
-        const int other = item[k] < 0 ? kNoItem : item[k];
-        rank += other < mine || (other == mine && k < tid);
-        if (other == mine) all += weight[k];
+        rank += order[k] < order[tid] || (order[k] == order[tid] && k < tid);
+        if (order[k] == order[tid]) all += weight[k];
     }
     const size_t at = (size_t)q * a.K + rank;
     a.entry_items[at] = mine;
@@ -107,9 +112,9 @@ __global__ __launch_bounds__(kListThreads) void default_list_kernel(ListArgs a) 
 }
 
 // What the gradient's workspace holds besides.
-struct ListLayout { size_t share_at, items_at, values_at, bytes; };
-ListLayout lists_of(const DensePlan& p, int B, int K) {
-    ListLayout l;
+struct EntryLayout { size_t share_at, items_at, values_at, bytes; };
+EntryLayout lists_of(const DensePlan& p, int B, int K) {
+    EntryLayout l;
     l.share_at = round_up(p.bytes, 256);
     l.items_at = round_up(l.share_at + (size_t)B * sizeof(float), 256);
     l.values_at = round_up(l.items_at + (size_t)B * K * sizeof(int), 256);
@@ -167,7 +172,7 @@ int pq_default_distillation(const void* W, const void* queries, const int* teach
     a.W = W; a.H = queries; a.N = N; a.B = B; a.d = d; a.scale = (float)(kLog2eDouble / temperature);
     a.item_tiles = p.item_tiles; a.tiles_each = p.tiles_each; a.groups = p.groups; a.position_tiles = p.position_tiles;
     a.partial = static_cast<float2*>(workspace);
-    const ListArgs l{W, queries, teacher_items, teacher_scores, N, B, d, K, temperature, a.partial, p.groups, loss, lse, nullptr, nullptr, nullptr, nullptr, nullptr};
+    const ListArgs l{W, queries, teacher_items, teacher_scores, N, B, d, K, temperature, a.partial, p.groups, loss, lse, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return pqk::record_hip_error(type == PQ_FLOAT32 ? forward<float>(p, a, l, st) : type == PQ_BFLOAT16 ? forward<__bf16>(p, a, l, st) : forward<_Float16>(p, a, l, st));
 }
@@ -188,7 +193,7 @@ int pq_default_distillation_backward(const void* W, const void* queries, const i
         (((uintptr_t)teacher_items | (uintptr_t)teacher_scores | (uintptr_t)lse | (uintptr_t)grad_loss) & 3))
         return PQ_ERR_ALIGN;
     const DensePlan p = plan_dense(N, B, d, type);
-    const ListLayout at = lists_of(p, B, K);
+    const EntryLayout at = lists_of(p, B, K);
     if (workspace_bytes < at.bytes) return PQ_ERR_WORKSPACE;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     DenseArgs a{};
@@ -199,7 +204,7 @@ int pq_default_distillation_backward(const void* W, const void* queries, const i
     int* entry_items = reinterpret_cast<int*>(ws + at.items_at);
     float* entry_values = reinterpret_cast<float*>(ws + at.values_at);
     a.share = share; a.entry_items = entry_items; a.entry_values = entry_values; a.entries = K;
-    const ListArgs l{W, queries, teacher_items, teacher_scores, N, B, d, K, temperature, nullptr, 0, nullptr, nullptr, lse, grad_loss, share, entry_items, entry_values};
+    const ListArgs l{W, queries, teacher_items, teacher_scores, N, B, d, K, temperature, nullptr, 0, nullptr, nullptr, lse, grad_loss, share, entry_items, entry_values, p.few ? few_items(d) : 0, p.few ? p.slices : 0};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return pqk::record_hip_error(type == PQ_FLOAT32 ? backward<float>(p, a, l, st) : type == PQ_BFLOAT16 ? backward<__bf16>(p, a, l, st) : backward<_Float16>(p, a, l, st));
 }

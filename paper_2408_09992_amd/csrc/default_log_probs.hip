@@ -14,7 +14,7 @@ static_assert(most_of(PQ_MAX_K + 16 + PQ_MAX_K / 8) < kMostKept, "a cut leaves n
 DensePlan plan_piece(long long items, int B, int d, int type, long long& region) {
     DensePlan p = plan_dense(items, B, d, type);
     if (p.few) {
-        const long long of = kFewBytes / 2 / (d > 256 ? 512 : d > 128 ? 256 : d > 64 ? 128 : 64);
+        const long long of = few_items(d);
         region = ceil_div(ceil_div(items, of), p.groups) * of;
         return p;
     }

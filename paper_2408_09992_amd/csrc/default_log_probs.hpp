@@ -68,19 +68,24 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
                     for (int e = 0; e < 16; ++e)
                         if (32 * mi + 8 * (e / 4) + e % 4 >= left - 4 * (lane / 32)) acc[mi][ni][e] = -__builtin_inff();
             }
+            float tops[MI];                                    // (of a block of 32 x 32)
 #pragma unroll
-            for (int mi = 0; mi < MI; ++mi)
+            for (int mi = 0; mi < MI; ++mi) {
+                tops[mi] = acc[mi][ni][0];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[mi][ni][e]);
-            if (a.store || __any(top > floor[ni])) {
-                stay_a_branch();
+                for (int e = 1; e < 16; ++e) tops[mi] = fmaxf(tops[mi], acc[mi][ni][e]);
+                top = fmaxf(top, tops[mi]);
+            }
 #pragma unroll
-                for (int mi = 0; mi < MI; ++mi)
+            for (int mi = 0; mi < MI; ++mi) {
+                if (a.store || __any(tops[mi] > floor[ni])) {
+                    stay_a_branch();
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int at = 32 * mi + 8 * (e / 4) + e % 4;
                         if (a.store ? q0 + 32 * ni < a.B && at < left - 4 * (lane / 32) : acc[mi][ni][e] > floor[ni]) offer(a, q0 + 32 * ni, group, &listed[Tile::wave_col() + 32 * ni + lane % 32], acc[mi][ni][e], mine + at);
                     }
+                }
             }
             top *= a.scale;
             if (__any(top > c[ni] + kNearHeadroom)) {
@@ -93,8 +98,19 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
                 for (int e = 0; e < 16; ++e) {
                     const float x = fmaf(acc[mi][ni][e], a.scale, -c[ni]), p = exp2_fast(x);
                     sum += p;
-                    sum_x = weighted(p, x, sum_x);
+                    sum_x = fmaf(p, x, sum_x);
                 }
+            if (__any(sum_x != sum_x)) {                       // (0 times -inf: a score that counts as -inf, rare enough to look for it here)
+                stay_a_branch();
+                sum_x = 0.0f;
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float x = fmaf(acc[mi][ni][e], a.scale, -c[ni]);
+                        sum_x = weighted(exp2_fast(x), x, sum_x);
+                    }
+            }
             s[ni] += sum;
             t[ni] += sum_x;
         }
@@ -115,84 +131,9 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     }
 }
 
-// The same for up to 64 positions of 16-bit operands, d <= 512 (default_few_loss_kernel's tiles).
+// The same for up to 64 positions of 16-bit operands, d <= 512.
 template <typename T, int D>
-__global__ __launch_bounds__(kFewThreads, 2) void default_few_log_probs_kernel(DenseProbsArgs a) {
-    constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
-    using RowsD = Rows<D / 8>;
-    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2];
-    __shared__ float4 stat[kWaves][kFew];
-    __shared__ int listed[kFew];
-    if (threadIdx.x < kFew) listed[threadIdx.x] = 0;
-    constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
-    constexpr int kBlocksZ = IT / 16 * 4 / kWaves, kParts = kBlocksZ < 4 ? kBlocksZ : 4;       // a wave's blocks of 16 x 16; positions among them / 16
-    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const long long tiles = (a.end - a.first + IT - 1) / IT;
-    bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h);
-    bring_rows<T, D, kLoadsW>(a.W, a.d, a.first + (long long)blockIdx.x * IT, a.N, w0);
-    float c[kParts], s[kParts], t[kParts], floor[kParts];
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-        c[i] = kLowest; s[i] = 0.0f; t[i] = 0.0f;
-        const int pos = (wave * kBlocksZ + i) % 4 * 16 + lane % 16;
-        floor[i] = a.lists.keep && !a.store && pos < a.B ? a.lists.floor[pos] : __builtin_inff();
-    }
-    int turn = 0;
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
-        const unsigned char* w = turn % 2 ? w1 : w0;
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the tile has come, its other buffer is free
-        bring_rows<T, D, kLoadsW>(a.W, a.d, a.first + min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
-#pragma unroll
-        for (int i = 0; i < kBlocksZ; ++i) {
-            const int block = wave * kBlocksZ + i, item0 = block / 4 * 16, pos = block % 4 * 16 + lane % 16;
-            f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k)
-                z = multiply16<T>(RowsD::along(w, item0 + lane % 16, 4 * k + lane / 16), RowsD::along(h, pos, 4 * k + lane / 16), z);
-            const int left = left_of(a.end - a.first - tile * IT - item0, 16) - lane / 16 * 4;
-            if (left < 4) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (e >= left) z[e] = -__builtin_inff();
-            }
-            const float raw = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), top = raw * a.scale;
-            const int part = i % kParts;
-            if (a.store || __any(raw > floor[part])) {
-                stay_a_branch();
-                const long long mine = a.first + tile * IT + item0 + lane / 16 * 4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (a.store ? pos < a.B && e < left : z[e] > floor[part]) offer(a, pos, blockIdx.x, &listed[pos], z[e], mine + e);
-            }
-            if (__any(top > c[part] + kNearHeadroom)) {
-                if (top > c[part] + kNearHeadroom) raise_reference(c[part], s[part], t[part], top);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float x = fmaf(z[e], a.scale, -c[part]), p = exp2_fast(x);
-                s[part] += p;
-                t[part] = weighted(p, x, t[part]);
-            }
-        }
-    }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");                  // (a last load into LDS may be under way)
-    for (int q = lane; q < kFew; q += kWave) stat[wave][q] = make_float4(kLowest, 0.0f, 0.0f, 0.0f);
-    wave_reads_after_writes();
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-#pragma unroll
-        for (int x = 16; x < kWave; x *= 2) join_sums(c[i], s[i], t[i], __shfl_xor(c[i], x), __shfl_xor(s[i], x), __shfl_xor(t[i], x));
-        if (lane < 16) stat[wave][(wave * kBlocksZ + i) % 4 * 16 + lane] = make_float4(c[i], s[i], t[i], 0.0f);
-    }
-    __syncthreads();
-    if (tid < a.B) {
-        float4 v = stat[0][tid];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) join_sums(v.x, v.y, v.z, stat[w][tid].x, stat[w][tid].y, stat[w][tid].z);
-        a.partial[(size_t)blockIdx.x * a.B + tid] = v;
-        if (a.lists.keep && !a.store) a.lists.counts[(size_t)blockIdx.x * a.B + tid] = listed[tid];
-    }
-}
+__global__ __launch_bounds__(kFewThreads, 2) void default_few_log_probs_kernel(DenseProbsArgs a) { few_sums<T, D, true>(a, a.first, a.end); }
 
 struct DenseFinishArgs {
     const void *W, *H;
