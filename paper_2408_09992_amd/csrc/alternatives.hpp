@@ -13,7 +13,7 @@
 namespace pqk {
 namespace head {
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / kWave;
+constexpr int kBins = 2048;
 constexpr int kMostKept = 1024;                      // keys that a cut leaves at most
 constexpr int kMostRegions = 2048;                   // workgroups that share the items of a piece
 constexpr int kFewKeys = 4, kManyKeys = 16;          // keys that a thread of a cut holds; where a list has more each pass reads them again
@@ -46,16 +46,19 @@ __device__ __forceinline__ void append(const Lists& l, int q, long long region, 
     l.keys[(size_t)q * l.cap + region + atomicAdd(count, 1)] = key_of(z, item);       // (what order a region is in changes no result)
 }
 
+// A cut is made by a workgroup of 1024 threads, or of 256 where there are positions enough to give a compute unit several.
+template <int THREADS>
 struct SelectMemory {
-    uint32_t histogram[2048];
+    uint32_t histogram[kBins];
     int begin[kMostRegions];                         // where a region's keys begin among all of them
-    uint64_t part[kSelectWaves][2];
-    uint32_t sums[kSelectWaves];
+    uint64_t part[THREADS / kWave][2];
+    uint32_t sums[THREADS / kWave];
     int above, taken, chosen, count;
 };
 
 // What lies before the thread's own value among those of all threads.
-__device__ __forceinline__ uint32_t sums_before(uint32_t own, SelectMemory& mem, uint32_t& all) {
+template <int THREADS>
+__device__ __forceinline__ uint32_t sums_before(uint32_t own, SelectMemory<THREADS>& mem, uint32_t& all) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     uint32_t sum = own;
 #pragma unroll
@@ -68,7 +71,7 @@ __device__ __forceinline__ uint32_t sums_before(uint32_t own, SelectMemory& mem,
     uint32_t before = 0;
     all = 0;
 #pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) {
+    for (int w = 0; w < THREADS / kWave; ++w) {
         const uint32_t v = mem.sums[w];
         if (w < wave) before += v;
         all += v;
@@ -96,14 +99,14 @@ struct Keys {
 };
 
 // A list's keys as a cut's passes meet them: R a thread in registers, or each from where it lies.
-template <int R>
+template <int THREADS, int R>
 struct HeldKeys {
     uint64_t k[R];
     int n;
     __device__ __forceinline__ HeldKeys(const Keys& all) : n(all.n) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int i = (int)threadIdx.x + r * kSelectThreads;
+            const int i = (int)threadIdx.x + r * THREADS;
             k[r] = i < n ? all(i) : 0;
         }
     }
@@ -111,23 +114,25 @@ struct HeldKeys {
     __device__ __forceinline__ void each(F f) const {
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if ((int)threadIdx.x + r * kSelectThreads < n) f(k[r]);
+            if ((int)threadIdx.x + r * THREADS < n) f(k[r]);
     }
 };
+template <int THREADS>
 struct FarKeys {
     const Keys& all;
     int n;
     __device__ __forceinline__ FarKeys(const Keys& keys) : all(keys), n(keys.n) {}
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-        for (int i = threadIdx.x; i < n; i += kSelectThreads) f(all(i));
+        for (int i = threadIdx.x; i < n; i += THREADS) f(all(i));
     }
 };
 
 // A key that at least `keep` of the keys, and no more than `most` (over `keep`) of them, reach; 0 if there are no more than `keep`.  By histograms of 2048
 // bins over the range that is left, each pass a look at all keys: one or two in the usual case, six at most (keys differ).
-template <typename H>
-__device__ __forceinline__ uint64_t cut(const H& held, int keep, int most, SelectMemory& mem) {
+template <int THREADS, typename H>
+__device__ __forceinline__ uint64_t cut(const H& held, int keep, int most, SelectMemory<THREADS>& mem) {
+    constexpr int kWaves = THREADS / kWave, kOwn = kBins / THREADS;
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     if (held.n <= keep) return 0;
     uint64_t low = ~0ull, high = 0;
@@ -135,8 +140,8 @@ __device__ __forceinline__ uint64_t cut(const H& held, int keep, int most, Selec
         low = k < low ? k : low;
         high = k > high ? k : high;
     });
-    mem.histogram[tid] = 0;
-    mem.histogram[tid + 1024] = 0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) mem.histogram[tid + i * THREADS] = 0;
 #pragma unroll
     for (int x = 1; x < kWave; x *= 2) {
         const uint64_t l = __shfl_xor(low, x), h = __shfl_xor(high, x);
@@ -145,10 +150,10 @@ __device__ __forceinline__ uint64_t cut(const H& held, int keep, int most, Selec
     }
     if (lane == 0) { mem.part[wave][0] = low; mem.part[wave][1] = high; }
     __syncthreads();
-    low = mem.part[lane % kSelectWaves][0];
-    high = mem.part[lane % kSelectWaves][1];
+    low = mem.part[lane % kWaves][0];
+    high = mem.part[lane % kWaves][1];
 #pragma unroll
-    for (int x = 1; x < kSelectWaves; x *= 2) {
+    for (int x = 1; x < kWaves; x *= 2) {
         const uint64_t l = __shfl_xor(low, x), h = __shfl_xor(high, x);
         low = l < low ? l : low;
         high = h > high ? h : high;
@@ -160,18 +165,25 @@ __device__ __forceinline__ uint64_t cut(const H& held, int keep, int most, Selec
             if (k >= low && k <= high) atomicAdd(&mem.histogram[(uint32_t)((k - low) >> shift)], 1u);
         });
         __syncthreads();
-        // thread t has the bins 2047 - 2t and 2046 - 2t: what lies over them by a scan
-        const uint32_t upper = mem.histogram[2047 - 2 * tid], lower = mem.histogram[2046 - 2 * tid];
-        uint32_t all;
-        const uint32_t begin = (uint32_t)above + sums_before(upper + lower, mem, all), end = begin + upper + lower;
-        if (begin < (uint32_t)keep && end >= (uint32_t)keep) {    // (one thread: the keep-th key is in its bins)
-            const bool first = begin + upper >= (uint32_t)keep;
-            mem.chosen = first ? 2047 - 2 * tid : 2046 - 2 * tid;
-            mem.above = (int)(first ? begin : begin + upper);
-            mem.taken = (int)(first ? begin + upper : end);
+        // thread t has the bins from kBins - 1 - kOwn t downwards: what lies over them by a scan
+        uint32_t bin[kOwn], sum = 0, all;
+        const int top = kBins - 1 - kOwn * tid;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            bin[i] = mem.histogram[top - i];
+            mem.histogram[top - i] = 0;
+            sum += bin[i];
         }
-        mem.histogram[2047 - 2 * tid] = 0;                        // (its own two)
-        mem.histogram[2046 - 2 * tid] = 0;
+        uint32_t begin = (uint32_t)above + sums_before(sum, mem, all);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            if (begin < (uint32_t)keep && begin + bin[i] >= (uint32_t)keep) {       // (one bin of one thread: the keep-th key is in it)
+                mem.chosen = top - i;
+                mem.above = (int)begin;
+                mem.taken = (int)(begin + bin[i]);
+            }
+            begin += bin[i];
+        }
         __syncthreads();
         low += (uint64_t)mem.chosen << shift;
         above = mem.above;
@@ -188,7 +200,8 @@ __host__ __device__ constexpr int most_of(int keep) { return keep + keep / 4 + 3
 
 // Cuts a position's list: what is left in out[] (the order is none), `keep` at least (or all) and most_of(keep) at most; returns how many, and in `least` what
 // they reach (0: as good as nothing was cut).  last: no floor is asked for.  stored: how many keys the first piece left, if that was the last piece; else regions of `region` keys each.
-__device__ __forceinline__ int cut_list(const Lists& l, int q, int B, int stored, int regions, long long region, bool last, uint64_t* out, uint64_t& least, SelectMemory& mem) {
+template <int THREADS>
+__device__ __forceinline__ int cut_list(const Lists& l, int q, int B, int stored, int regions, long long region, bool last, uint64_t* out, uint64_t& least, SelectMemory<THREADS>& mem) {
     const int tid = threadIdx.x, most = most_of(l.keep);
     const uint64_t* keys = l.keys + (size_t)q * l.cap;
     Keys all{l.kept + (size_t)q * kMostKept, keys, mem.begin, region, stored, 1, stored};
@@ -196,37 +209,46 @@ __device__ __forceinline__ int cut_list(const Lists& l, int q, int B, int stored
     else {
         all.kept_n = l.kept_count[q];
         all.regions = regions;
-        const int a = 2 * tid < regions ? l.counts[(size_t)(2 * tid) * B + q] : 0, b = 2 * tid + 1 < regions ? l.counts[(size_t)(2 * tid + 1) * B + q] : 0;
+        constexpr int kOwn = kMostRegions / THREADS;
+        int own[kOwn], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            own[i] = kOwn * tid + i < regions ? l.counts[(size_t)(kOwn * tid + i) * B + q] : 0;
+            sum += own[i];
+        }
         uint32_t total;
-        const int before = all.kept_n + (int)sums_before((uint32_t)(a + b), mem, total);
-        mem.begin[2 * tid] = before;
-        mem.begin[2 * tid + 1] = before + a;
+        int before = all.kept_n + (int)sums_before((uint32_t)sum, mem, total);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            mem.begin[kOwn * tid + i] = before;
+            before += own[i];
+        }
         all.n = all.kept_n + (int)total;
     }
     if (tid == 0) mem.count = 0;
     __syncthreads();
     auto run = [&](const auto& held) {
-        least = last && held.n <= most ? 0 : cut(held, l.keep, most, mem);
+        least = last && held.n <= most ? 0 : cut<THREADS>(held, l.keep, most, mem);
         held.each([&](uint64_t k) {
             if (k >= least) out[atomicAdd(&mem.count, 1)] = k;
         });
     };
-    if (all.n <= kFewKeys * kSelectThreads) run(HeldKeys<kFewKeys>(all));
-    else if (all.n <= kManyKeys * kSelectThreads) run(HeldKeys<kManyKeys>(all));
-    else run(FarKeys(all));
+    if (all.n <= kFewKeys * THREADS) run(HeldKeys<THREADS, kFewKeys>(all));
+    else if (all.n <= kManyKeys * THREADS) run(HeldKeys<THREADS, kManyKeys>(all));
+    else run(FarKeys<THREADS>(all));
     __syncthreads();
     return mem.count;
 }
 
 // grid = positions: cuts the lists between two pieces and sets the floors.
-template <int>                                        // (a template: only what launches it has it)
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(Lists l, int B, int stored, int regions, long long region) {
-    __shared__ SelectMemory mem;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void select_kernel(Lists l, int B, int stored, int regions, long long region) {
+    __shared__ SelectMemory<THREADS> mem;
     __shared__ uint64_t out[kMostKept];
     const int q = blockIdx.x, tid = threadIdx.x;
     uint64_t least;
     const int n = cut_list(l, q, B, stored, regions, region, false, out, least, mem);
-    for (int i = tid; i < n; i += kSelectThreads) l.kept[(size_t)q * kMostKept + i] = out[i];
+    for (int i = tid; i < n; i += THREADS) l.kept[(size_t)q * kMostKept + i] = out[i];
     if (tid == 0) {
         l.kept_count[q] = n;
         if (least != 0) l.floor[q] = score_of(least);          // (a list of `keep` keys, of which nothing is cut, has the floor that it had)
@@ -236,23 +258,28 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(Lists l, int B, 
 // ---------------------------------------------------------------------------------------------------------------
 // host side
 
-// The pieces of a pass over N items: `first` items, whose scores are all stored, then as many as the lists have room for and no more than kGrowth
-// times the items before them, so that a list gets some kGrowth * keep new keys.
-constexpr long long kOnePiece = 16384, kGrowth = 32, kListBytes = 1LL << 31;
+inline bool many_lists(int B) { return B > kCUs; }
+
+// The pieces of a pass over N items: `first` items, whose scores are all stored, then as many as the lists have room for and no more than `growth`
+// times the items before them: a list gets some growth * keep new keys in each.  A candidate of many positions costs more than a cut (1024 positions, 128 kept:
+// some 30 ps each over the chip), few positions' candidates less.
+constexpr long long kOnePiece = 16384, kListBytes = 1LL << 31;
 struct Passes {
-    long long N, first, room;
+    long long N, first, room, growth;
     int keep;
     long long after(long long done) const {                      // items of the piece after `done` items
         if (done == 0) return first;
-        const long long n = done * kGrowth < room ? done * kGrowth : room;
+        const long long n = done * growth < room ? done * growth : room;
         return n < N - done ? n : N - done;
     }
 };
 inline Passes passes_of(long long N, int B, int keep) {
-    Passes p{N, N, N, (int)(keep < N ? keep : N)};
+    Passes p{N, N, N, 1, (int)(keep < N ? keep : N)};
     if (keep == 0) return p;
-    const long long least = (long long)round_up(8 * (size_t)keep, 4096);
+    const long long least = B <= 128 ? kOnePiece : (long long)round_up(8 * (size_t)keep, 4096);
     if (N > kOnePiece && N > 2 * least) p.first = least;
+    p.growth = 4096 / keep;
+    p.growth = (long long)keep * B >= 32768 || p.growth < 8 ? 8 : p.growth > 128 ? 128 : p.growth;
     p.room = kListBytes / 8 / B > p.first ? kListBytes / 8 / B : p.first;
     return p;
 }
@@ -282,7 +309,8 @@ struct ListLayout {
 };
 
 inline hipError_t launch_select(const Lists& l, int B, int stored, int regions, long long region, hipStream_t st) {
-    hipLaunchKernelGGL(select_kernel<0>, dim3(B), dim3(kSelectThreads), 0, st, l, B, stored, regions, region);
+    if (many_lists(B)) hipLaunchKernelGGL(select_kernel<256>, dim3(B), dim3(256), 0, st, l, B, stored, regions, region);
+    else hipLaunchKernelGGL(select_kernel<1024>, dim3(B), dim3(1024), 0, st, l, B, stored, regions, region);
     return hipGetLastError();
 }
 

@@ -188,7 +188,8 @@ struct ProbsArgs {
 // PROBS: sum_i 2^x_i x_i besides, x = score scale - c, which the entropy is made of, and scores over the floors to the lists.
 template <int M, typename CT, int Q, bool PROBS, typename Args>
 __device__ __forceinline__ void sum_items(const Args& a) {
-    constexpr int kUnits = units_of<M>();
+    // (PROBS keeps three numbers more a query: half the items leave room for two workgroups a compute unit)
+    constexpr int kUnits = PROBS && M * (int)sizeof(CT) <= 8 && Q * units_of<M>() >= 8 ? 2 : units_of<M>();
     extern __shared__ __align__(16) unsigned char smem[];
     float* table = reinterpret_cast<float*>(smem);
     // [kWaves][Q]
@@ -204,7 +205,6 @@ __device__ __forceinline__ void sum_items(const Args& a) {
     float c[Q], s[Q], t[Q], floor[Q];
     __shared__ int listed[PROBS ? Q : 1];
     if (PROBS && (int)threadIdx.x < Q) listed[threadIdx.x] = 0;
-    const long long region = (long long)blockIdx.x * a.share;
 #pragma unroll
     for (int r = 0; r < Q; ++r) {
         c[r] = kLowest; s[r] = 0.0f; t[r] = 0.0f;
@@ -238,20 +238,26 @@ __device__ __forceinline__ void sum_items(const Args& a) {
         }
         if constexpr (PROBS) {
             if (a.store) {
-                stay_a_branch();
+                int q = q0;
+                asm volatile("" : "+s"(q));                    // (so that no address is kept in registers for a branch that is rarely taken)
 #pragma unroll
-                for (int u = 0; u < kUnits; ++u)
+                for (int r = 0; r < Q; ++r) {
+                    if (q + r >= a.B) break;
+                    uint64_t* keys = a.lists.keys + (size_t)(q + r) * a.lists.cap - from;
 #pragma unroll
-                    for (int r = 0; r < Q; ++r)
-                        if (first + u * kThreads < hi && q0 + r < a.B)
-                            a.lists.keys[(size_t)(q0 + r) * a.lists.cap + (first + u * kThreads - from)] = key_of(z[u][r], first + u * kThreads);
+                    for (int u = 0; u < kUnits; ++u)
+                        if (first + u * kThreads < hi) keys[first + u * kThreads] = key_of(z[u][r], first + u * kThreads);
+                }
             } else if (__any(pass)) {
-                stay_a_branch();
+                int q = q0;
+                asm volatile("" : "+s"(q));
 #pragma unroll
-                for (int u = 0; u < kUnits; ++u)
+                for (int r = 0; r < Q; ++r) {
+                    const float limit = floor[r];
 #pragma unroll
-                    for (int r = 0; r < Q; ++r)
-                        if (z[u][r] > floor[r]) append(a.lists, q0 + r, region, &listed[r], z[u][r], first + u * kThreads);
+                    for (int u = 0; u < kUnits; ++u)
+                        if (z[u][r] > limit) append(a.lists, q + r, (long long)blockIdx.x * a.share, &listed[r], z[u][r], first + u * kThreads);
+                }
             }
         }
         if (__any(rise)) {
@@ -309,6 +315,7 @@ __device__ __forceinline__ void sum_items(const Args& a) {
         auto sums = stat[wave];
         const int q = q0 + wave;
         if constexpr (PROBS) {
+#pragma unroll 2                                               // (fifteen at once would be the kernel's most registers)
             for (int w = 1; w < kWaves; ++w) join_sums(sums.x, sums.y, sums.z, stat[w * Q + wave].x, stat[w * Q + wave].y, stat[w * Q + wave].z);
             if (lane == 0) {
                 a.partial[(size_t)blockIdx.x * a.B + q] = sums;
@@ -550,7 +557,7 @@ inline void cut_items(Plan& p, long long N, long long workgroups, long long slot
 
 constexpr size_t kStatBytes = (size_t)kWaves * 8 * sizeof(float2);
 
-inline bool plan_loss(Plan& p, long long N, int B, int m, int b, int code_bytes, bool probs = false) {
+inline bool plan_loss(Plan& p, long long N, int B, int m, int b, int code_bytes) {
     const size_t entry_floats = (size_t)m * entries_of(b, code_bytes);
     p.Q = B >= 3 ? 4 : B;
     while (p.Q > 1 && entry_floats * 4 * p.Q + kStatBytes > kMaxLds) p.Q /= 2;
@@ -564,7 +571,7 @@ inline bool plan_loss(Plan& p, long long N, int B, int m, int b, int code_bytes,
     // and 32 bytes are too long for.  (Counted as two, they came in two rounds of half the items: 1.28M items, m = 16, one position 19.4 us
     // instead of 15.0, 300,000 and 64 positions 46 instead of 36; 5M, m = 16, 16 positions 124 instead of 117.)
     const bool long_rows = m == 16 || (m == 8 && code_bytes == 2) || (m == 32 && code_bytes == 1);
-    const bool two = p.lds <= kMaxLds / 2 && !long_rows && !probs;
+    const bool two = p.lds <= kMaxLds / 2 && !long_rows;
     // a lookup takes a compute unit 0.04 cycles a query (0.08 for one query alone); tables come in at some 20 bytes a cycle
     cut_items(p, N, p.groups, (two ? 2 : 1) * kCUs, m * (p.Q == 1 ? 0.08 : 0.045 * p.Q), 2000 + p.lds / 20.0);
     return true;

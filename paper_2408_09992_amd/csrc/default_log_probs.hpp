@@ -151,15 +151,15 @@ struct DenseFinishArgs {
 };
 
 // grid = positions: joins the groups' sums, scores the given items and the list's best in 64 bits, puts these in order.
-template <typename T>
-__global__ __launch_bounds__(kSelectThreads) void default_log_probs_finish_kernel(DenseFinishArgs a) {
-    __shared__ SelectMemory mem;
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(DenseFinishArgs a) {
+    __shared__ SelectMemory<THREADS> mem;
     __shared__ uint64_t kept[kMostKept];
     __shared__ double score[kMostKept];
-    __shared__ float4 sums[kSelectWaves];
+    __shared__ float4 sums[THREADS / kWave];
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     float c = kLowest, s = 0.0f, t = 0.0f;
-    for (int i = tid; i < a.groups; i += kSelectThreads) {
+    for (int i = tid; i < a.groups; i += THREADS) {
         const float4 v = a.partial[(size_t)i * a.B + q];
         join_sums(c, s, t, v.x, v.y, v.z);
     }
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kSelectThreads) void default_log_probs_finish_kerne
     if (lane == 0) sums[wave] = make_float4(c, s, t, 0.0f);
     __syncthreads();
     c = sums[0].x; s = sums[0].y; t = sums[0].z;
-    for (int w = 1; w < kSelectWaves; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
+    for (int w = 1; w < THREADS / kWave; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
     const float lse = log_sum(c, s);
     if (tid == 0) {
         a.lse[q] = lse;
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kSelectThreads) void default_log_probs_finish_kerne
     }
     auto log_prob = [&](double z) { return lse == -__builtin_inff() ? lse : (float)(z / (double)a.temperature - (double)lse); };
     const T *W = static_cast<const T*>(a.W), *h = static_cast<const T*>(a.H) + (size_t)q * a.d;
-    for (int i = tid / 16; i < a.n; i += kSelectThreads / 16) {
+    for (int i = tid / 16; i < a.n; i += THREADS / 16) {
         const int item = a.items[(size_t)q * a.n + i];
         const bool there = item >= 0 && item < a.N;            // (the same for the sixteen)
         const double z = there ? dot64(W + (size_t)item * a.d, h, a.d) : 0.0;
@@ -184,23 +184,23 @@ __global__ __launch_bounds__(kSelectThreads) void default_log_probs_finish_kerne
     }
     if (a.K == 0) return;
     uint64_t least;
-    const int n = cut_list(a.lists, q, a.B, a.stored, a.regions, a.region, true, kept, least, mem);
-    for (int i = tid / 16; i < n; i += kSelectThreads / 16) {
+    const int n = cut_list<THREADS>(a.lists, q, a.B, a.stored, a.regions, a.region, true, kept, least, mem);
+    for (int i = tid / 16; i < n; i += THREADS / 16) {
         const double z = dot64(W + (size_t)item_of(kept[i]) * a.d, h, a.d);
         if (tid % 16 == 0) score[i] = z;
     }
     __syncthreads();
-    if (tid < n) {
+    for (int at = tid; at < n; at += THREADS) {
         // (a NaN, of which no rank comes, is taken for the lowest)
-        const double mine = score[tid] == score[tid] ? score[tid] : -__builtin_inf();
+        const double mine = score[at] == score[at] ? score[at] : -__builtin_inf();
         int rank = 0;
         for (int i = 0; i < n; ++i) {
             const double other = score[i] == score[i] ? score[i] : -__builtin_inf();
-            rank += other > mine || (other == mine && item_of(kept[i]) < item_of(kept[tid]));
+            rank += other > mine || (other == mine && item_of(kept[i]) < item_of(kept[at]));
         }
         if (rank < a.K) {
-            a.top_items[(size_t)q * a.K + rank] = (int)item_of(kept[tid]);
-            a.top_log_probs[(size_t)q * a.K + rank] = log_prob(score[tid]);
+            a.top_items[(size_t)q * a.K + rank] = (int)item_of(kept[at]);
+            a.top_log_probs[(size_t)q * a.K + rank] = log_prob(score[at]);
         }
     }
 }
@@ -236,7 +236,8 @@ hipError_t dense_probs(const DensePlan& p, const DenseProbsArgs& a, hipStream_t 
 }
 template <typename T>
 hipError_t dense_probs_finish(const DenseFinishArgs& a, hipStream_t st) {
-    hipLaunchKernelGGL((default_log_probs_finish_kernel<T>), dim3(a.B), dim3(kSelectThreads), 0, st, a);
+    if (many_lists(a.B)) hipLaunchKernelGGL((default_log_probs_finish_kernel<T, 256>), dim3(a.B), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((default_log_probs_finish_kernel<T, 1024>), dim3(a.B), dim3(1024), 0, st, a);
     return hipGetLastError();
 }
 template hipError_t dense_probs<PQ_PROBS_INSTANCE>(const DensePlan&, const DenseProbsArgs&, hipStream_t);

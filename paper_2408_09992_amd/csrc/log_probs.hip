@@ -12,8 +12,10 @@ namespace head {
 namespace subids {
 namespace {
 
+// Two workgroups a compute unit, 64 registers a lane, but for rows of 16 and 32 bytes (as the loss has it, see plan_loss()).
+template <int M, typename CT> constexpr int waves_of() { return M * (int)sizeof(CT) >= 16 && M != 64 ? 4 : 8; }
 template <int M, typename CT, int Q>
-__global__ __launch_bounds__(kThreads) void log_probs_kernel(ProbsArgs a) { sum_items<M, CT, Q, true>(a); }
+__global__ __launch_bounds__(kThreads, (waves_of<M, CT>())) void log_probs_kernel(ProbsArgs a) { sum_items<M, CT, Q, true>(a); }
 
 struct FinishArgs {
     const void* codes;
@@ -44,13 +46,14 @@ __device__ __forceinline__ float score_of_item(const FinishArgs& a, int q, int i
 }
 
 // grid = positions: joins the shares' sums, scores the given items, cuts the list to the K best and puts them in order.
-__global__ __launch_bounds__(kSelectThreads) void log_probs_finish_kernel(FinishArgs a) {
-    __shared__ SelectMemory mem;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a) {
+    __shared__ SelectMemory<THREADS> mem;
     __shared__ uint64_t kept[kMostKept];
-    __shared__ float4 sums[kSelectWaves];
+    __shared__ float4 sums[THREADS / kWave];
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     float c = kLowest, s = 0.0f, t = 0.0f;
-    for (int i = tid; i < a.shares; i += kSelectThreads) {
+    for (int i = tid; i < a.shares; i += THREADS) {
         const float4 v = a.partial[(size_t)i * a.B + q];
         join_sums(c, s, t, v.x, v.y, v.z);
     }
@@ -59,22 +62,22 @@ __global__ __launch_bounds__(kSelectThreads) void log_probs_finish_kernel(Finish
     if (lane == 0) sums[wave] = make_float4(c, s, t, 0.0f);
     __syncthreads();
     c = sums[0].x; s = sums[0].y; t = sums[0].z;
-    for (int w = 1; w < kSelectWaves; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
+    for (int w = 1; w < THREADS / kWave; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
     const float lse = log_sum(c, s);
     if (tid == 0) {
         a.lse[q] = lse;
         a.entropy[q] = entropy_of(s, t);
     }
     auto log_prob = [&](float z) { return lse == -__builtin_inff() ? lse : (float)((double)z / (double)a.temperature - (double)lse); };
-    for (int i = tid; i < a.n; i += kSelectThreads) {
+    for (int i = tid; i < a.n; i += THREADS) {
         const int item = a.items[(size_t)q * a.n + i];
         a.log_probs[(size_t)q * a.n + i] = item >= 0 && item < a.N ? log_prob(score_of_item(a, q, item)) : 0.0f;
     }
     if (a.K == 0) return;
     uint64_t least;
-    const int n = cut_list(a.lists, q, a.B, a.stored, a.regions, a.region, true, kept, least, mem);
-    if (tid < n) {
-        const uint64_t mine = kept[tid];
+    const int n = cut_list<THREADS>(a.lists, q, a.B, a.stored, a.regions, a.region, true, kept, least, mem);
+    for (int at = tid; at < n; at += THREADS) {
+        const uint64_t mine = kept[at];
         int rank = 0;
         for (int i = 0; i < n; ++i) rank += kept[i] > mine;
         if (rank < a.K) {
@@ -122,7 +125,7 @@ bool lay_out(Layout& l, long long N, int B, int m, int b, int K, int code_bytes)
     for (long long done = 0, now; done < N; done += now) {
         Plan p;
         now = l.passes.after(done);
-        if (!plan_loss(p, now, B, m, b, code_bytes, true)) return false;
+        if (!plan_loss(p, now, B, m, b, code_bytes)) return false;
         l.shares += p.shares;
         l.piece(done == 0 ? now : (long long)p.shares * p.share, p.shares);
     }
@@ -162,7 +165,7 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
     Plan p;
     for (long long done = 0; done < N && e == hipSuccess; done = a.end) {
         const long long now = l.passes.after(done);
-        plan_loss(p, now, B, m, b, sizeof(CT), true);
+        plan_loss(p, now, B, m, b, sizeof(CT));
         a.first = (uint32_t)done;
         a.end = (uint32_t)(done + now);
         a.share = p.share;
@@ -174,7 +177,8 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
     if (e == hipSuccess) {
         const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), temperature, reinterpret_cast<const float4*>(ws), l.shares,
                            a.store ? (int)N : 0, p.shares, p.share, lists, out, entropy, lse, top_items, top_log_probs};
-        hipLaunchKernelGGL(log_probs_finish_kernel, dim3(B), dim3(kSelectThreads), 0, st, f);
+        if (many_lists(B)) hipLaunchKernelGGL(log_probs_finish_kernel<256>, dim3(B), dim3(256), 0, st, f);
+        else hipLaunchKernelGGL(log_probs_finish_kernel<1024>, dim3(B), dim3(1024), 0, st, f);
         e = hipGetLastError();
     }
     return record_hip_error(e);
