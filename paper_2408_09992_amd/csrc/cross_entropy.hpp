@@ -112,8 +112,12 @@ __device__ __forceinline__ void item_scores(const Row<M, CT>& row, const float* 
     }
 }
 
+// Sums over 2^x x (PROBS below) have no place for x = -inf, whose term would be NaN: table entries below -1e32 are held as that, which 128 splits and
+// the lowest temperature leave finite.  Scores below kNoScore are those: they are -inf in the lists.
+constexpr float kLeastEntry = -1e32f, kNoScore = -5e31f;
+
 // Tables of Q queries to LDS, [k][j][q]; queries past the batch repeat its last one, sub-ids from b to E are 0.
-template <typename CT, int Q>
+template <typename CT, int Q, bool FINITE = false>
 __device__ __forceinline__ void fill_tables(float* table, const float* S, int q0, int B, int m, int b) {
     const int E = entries<CT>(b);
     const size_t per_query = (size_t)m * b;
@@ -124,7 +128,10 @@ __device__ __forceinline__ void fill_tables(float* table, const float* S, int q0
         const int k = i / E, j = i - k * E;
         float v[Q];
 #pragma unroll
-        for (int r = 0; r < Q; ++r) v[r] = j < b ? src[r][(size_t)k * b + j] : 0.0f;
+        for (int r = 0; r < Q; ++r) {
+            v[r] = j < b ? src[r][(size_t)k * b + j] : 0.0f;
+            if (FINITE) v[r] = v[r] < kLeastEntry ? kLeastEntry : v[r];          // (a NaN stays one)
+        }
 #pragma unroll
         for (int r = 0; r < Q; ++r) table[(size_t)i * Q + r] = v[r];
     }
@@ -177,6 +184,7 @@ struct ProbsArgs {
     int store;                 // whether all its scores go to the lists
     float4* partial;           // [gridDim.x][B]: (reference, sum, weighted sum)
     Lists lists;
+    float* finite;             // [B][m][b], or NULL: the tables as a ranking takes them, held within +-1e32, 0 for a NaN
 };
 
 // grid = (shares of the items, groups of Q queries).
@@ -197,7 +205,7 @@ __device__ __forceinline__ void sum_items(const Args& a) {
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int q0 = blockIdx.y * Q;
     const CT* codes = static_cast<const CT*>(a.codes);
-    fill_tables<CT, Q>(table, a.S, q0, a.B, a.m, a.b);
+    fill_tables<CT, Q, PROBS>(table, a.S, q0, a.B, a.m, a.b);
 
     uint32_t from = 0, end = (uint32_t)a.N;
     if constexpr (PROBS) { from = a.first; end = a.end; }
@@ -210,10 +218,20 @@ __device__ __forceinline__ void sum_items(const Args& a) {
         c[r] = kLowest; s[r] = 0.0f; t[r] = 0.0f;
         floor[r] = __builtin_inff();
         if constexpr (PROBS) {
-            if (a.lists.keep && !a.store && q0 + r < a.B) floor[r] = a.lists.floor[q0 + r];
+            if (a.lists.keep && !a.store && q0 + r < a.B) floor[r] = fmaxf(a.lists.floor[q0 + r], kNoScore);
         }
     }
     __syncthreads();
+    if constexpr (PROBS) {
+        if (a.finite && blockIdx.x == 0) {
+            const int E = entries<CT>(a.b);
+            for (int i = threadIdx.x; i < a.m * a.b * Q; i += kThreads) {
+                const int r = i / (a.m * a.b), at = i - r * a.m * a.b, k = at / a.b;
+                const float v = table[(size_t)(k * E + at - k * a.b) * Q + r];
+                if (q0 + r < a.B) a.finite[(size_t)(q0 + r) * a.m * a.b + at] = v != v ? 0.0f : fminf(v, -kLeastEntry);
+            }
+        }
+    }
 
     auto step = [&](const Row<M, CT> (&row)[kUnits], uint32_t first, auto whole) {
         float z[kUnits][Q];
@@ -222,7 +240,7 @@ __device__ __forceinline__ void sum_items(const Args& a) {
             item_scores<M, CT, Q>(row[u], table, a.m, a.b, z[u]);
             if (!decltype(whole)::value && first + u * kThreads >= hi) {
 #pragma unroll
-                for (int r = 0; r < Q; ++r) z[u][r] = -__builtin_inff();
+                for (int r = 0; r < Q; ++r) z[u][r] = PROBS ? kLeastEntry : -__builtin_inff();
             }
         }
         bool rise = false, pass = false;
@@ -246,7 +264,7 @@ __device__ __forceinline__ void sum_items(const Args& a) {
                     uint64_t* keys = a.lists.keys + (size_t)(q + r) * a.lists.cap - from;
 #pragma unroll
                     for (int u = 0; u < kUnits; ++u)
-                        if (first + u * kThreads < hi) keys[first + u * kThreads] = key_of(z[u][r], first + u * kThreads);
+                        if (first + u * kThreads < hi) keys[first + u * kThreads] = key_of(z[u][r] < kNoScore ? -__builtin_inff() : z[u][r], first + u * kThreads);
                 }
             } else if (__any(pass)) {
                 int q = q0;
@@ -275,7 +293,7 @@ __device__ __forceinline__ void sum_items(const Args& a) {
             for (int u = 0; u < kUnits; ++u) {
                 const float x = fmaf(z[u][r], a.scale, -c[r]), p = exp2_fast(x);
                 s[r] += p;
-                if constexpr (PROBS) t[r] = weighted(p, x, t[r]);
+                if constexpr (PROBS) t[r] = fmaf(p, x, t[r]);
             }
     };
 

@@ -3,7 +3,10 @@
 //
 //   r_qi = sum_k S[q][k][G[i][k]]   lse = log sum_i exp(r_i / T)   log p_i = r_i / T - lse   entropy = lse - sum_i p_i r_i / T
 //
-// The pass is the cross entropy's (cross_entropy.hpp) with one more sum; what scores pass a position's floor goes to its list (alternatives.hpp).
+// The pass is the cross entropy's (cross_entropy.hpp) with one more sum.  The likeliest items come from it too, what scores pass a position's floor going to
+// its list (alternatives.hpp), or, where the lookups are few, from the ranking's own scan, whose bounds of one byte need no first piece and no cut:
+// what either adds to the pass, us, lists and scan: 1.28M items, m = 8, K = 10: one position 22 and 10, 64 34 and 32, 128 36 and 47; K = 100: 16 55 and 27, 64 58 and 43, 128 62
+// and 65; m = 16, K = 10: 64 35 and 50; 5M, m = 8, K = 10: 16 47 and 31, 64 50 and 63.
 #include "pqtopk_probs.h"
 #include "cross_entropy.hpp"
 
@@ -28,6 +31,7 @@ struct FinishArgs {
     int shares, stored, regions;                       // shares of all pieces; of the last piece what cut_list() takes
     long long region;
     Lists lists;
+    const float* ranked;       // [B][K], or NULL: the scores of top_items, which a ranking has found
     float *log_probs, *entropy, *lse;
     int* top_items;
     float* top_log_probs;
@@ -42,7 +46,7 @@ __device__ __forceinline__ float score_of_item(const FinishArgs& a, int q, int i
         const float v = a.S[((size_t)q * a.m + k) * a.b + min(g, (uint32_t)a.b - 1u)];
         z = k == 0 ? v : z + v;
     }
-    return z;
+    return z + 0.0f;
 }
 
 // grid = positions: joins the shares' sums, scores the given items, cuts the list to the K best and puts them in order.
@@ -74,6 +78,29 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
         a.log_probs[(size_t)q * a.n + i] = item >= 0 && item < a.N ? log_prob(score_of_item(a, q, item)) : 0.0f;
     }
     if (a.K == 0) return;
+    if (a.ranked) {
+        // (the ranking took scores of -inf for sums of large numbers: fewer than K others mean that K - 1 ids hold enough of them, the lowest ones)
+        __shared__ int below[PQ_MAX_K];
+        const float last = a.ranked[(size_t)q * a.K + a.K - 1];
+        for (int i = tid; i < a.K; i += THREADS) {
+            const float z = a.ranked[(size_t)q * a.K + i];
+            if (z >= kNoScore) a.top_log_probs[(size_t)q * a.K + i] = log_prob(z);
+            if (last < kNoScore) below[i] = score_of_item(a, q, i) < kNoScore;
+        }
+        __syncthreads();
+        if (last >= kNoScore) return;
+        int others = 0;
+        for (int i = 0; i < a.K; ++i) others += a.ranked[(size_t)q * a.K + i] >= kNoScore;
+        for (int i = tid; i < a.K; i += THREADS) {
+            int rank = others;
+            for (int j = 0; j < i; ++j) rank += below[j];
+            if (below[i] && rank < a.K) {
+                a.top_items[(size_t)q * a.K + rank] = i;
+                a.top_log_probs[(size_t)q * a.K + rank] = -__builtin_inff();
+            }
+        }
+        return;
+    }
     uint64_t least;
     const int n = cut_list<THREADS>(a.lists, q, a.B, a.stored, a.regions, a.region, true, kept, least, mem);
     for (int at = tid; at < n; at += THREADS) {
@@ -118,9 +145,15 @@ hipError_t go_m(const Plan& p, const ProbsArgs& a, hipStream_t st) {
 struct Layout : ListLayout {
     Passes passes;
     int shares;
+    size_t topk_bytes, finite_at, ranked_at, topk_at;          // (topk_bytes: 0 where lists are kept)
 };
+size_t topk_bytes_of(long long N, int B, int m, int b, int K, int code_bytes) {
+    if (K == 0 || N <= kOnePiece || (double)N * B * m > 1e9) return 0;
+    return code_bytes == 1 ? pq_score_topk_workspace_bytes(N, B, m, b, K) : pq_score_topk_u16_workspace_bytes(N, B, m, b, K);
+}
 bool lay_out(Layout& l, long long N, int B, int m, int b, int K, int code_bytes) {
-    l.passes = passes_of(N, B, K);
+    l.topk_bytes = topk_bytes_of(N, B, m, b, K, code_bytes);
+    l.passes = passes_of(N, B, l.topk_bytes ? 0 : K);
     l.shares = 0;
     for (long long done = 0, now; done < N; done += now) {
         Plan p;
@@ -129,7 +162,13 @@ bool lay_out(Layout& l, long long N, int B, int m, int b, int K, int code_bytes)
         l.shares += p.shares;
         l.piece(done == 0 ? now : (long long)p.shares * p.share, p.shares);
     }
-    l.ListLayout::lay_out((size_t)l.shares * B * sizeof(float4), B, K);
+    l.ListLayout::lay_out((size_t)l.shares * B * sizeof(float4), B, l.passes.keep);
+    if (l.topk_bytes) {
+        l.finite_at = l.bytes;
+        l.ranked_at = l.finite_at + round_up((size_t)B * m * b * sizeof(float), 256);
+        l.topk_at = l.ranked_at + round_up((size_t)B * K * sizeof(float), 256);
+        l.bytes = l.topk_at + round_up(l.topk_bytes, 256);
+    }
     return true;
 }
 
@@ -160,7 +199,9 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
     hipStream_t st = static_cast<hipStream_t>(stream);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     const Lists lists = l.lists(ws, l.passes.keep);
-    ProbsArgs a{codes, S, N, B, m, b, 0, (float)(kLog2eDouble / temperature), 0, 0, 0, reinterpret_cast<float4*>(ws), lists};
+    ProbsArgs a{codes, S, N, B, m, b, 0, (float)(kLog2eDouble / temperature), 0, 0, 0, reinterpret_cast<float4*>(ws), lists,
+                l.topk_bytes ? reinterpret_cast<float*>(ws + l.finite_at) : nullptr};
+    float* ranked = l.topk_bytes ? reinterpret_cast<float*>(ws + l.ranked_at) : nullptr;
     hipError_t e = hipSuccess;
     Plan p;
     for (long long done = 0; done < N && e == hipSuccess; done = a.end) {
@@ -169,15 +210,20 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
         a.first = (uint32_t)done;
         a.end = (uint32_t)(done + now);
         a.share = p.share;
-        a.store = K != 0 && done == 0;
+        a.store = lists.keep != 0 && done == 0;
         e = go_m<CT>(p, a, st);
         a.partial += (size_t)p.shares * B;
-        if (e == hipSuccess && K && a.end < N) e = launch_select(lists, B, a.store ? (int)now : 0, p.shares, p.share, st);
+        if (e == hipSuccess && lists.keep && a.end < N) e = launch_select(lists, B, a.store ? (int)now : 0, p.shares, p.share, st);
+    }
+    if (e == hipSuccess && ranked) {
+        if (sizeof(CT) == 1) rc = pq_score_topk(reinterpret_cast<const uint8_t*>(codes), a.finite, N, B, m, b, K, top_items, ranked, ws + l.topk_at, l.topk_bytes, stream);
+        else rc = pq_score_topk_u16(reinterpret_cast<const uint16_t*>(codes), a.finite, N, B, m, b, K, top_items, ranked, ws + l.topk_at, l.topk_bytes, stream);
+        if (rc != PQ_OK) return rc;
     }
     if (e == hipSuccess) {
         const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), temperature, reinterpret_cast<const float4*>(ws), l.shares,
-                           a.store ? (int)N : 0, p.shares, p.share, lists, out, entropy, lse, top_items, top_log_probs};
-        if (many_lists(B)) hipLaunchKernelGGL(log_probs_finish_kernel<256>, dim3(B), dim3(256), 0, st, f);
+                           a.store ? (int)N : 0, p.shares, p.share, lists, ranked, out, entropy, lse, top_items, top_log_probs};
+        if (many_lists(B) || lists.keep == 0) hipLaunchKernelGGL(log_probs_finish_kernel<256>, dim3(B), dim3(256), 0, st, f);
         else hipLaunchKernelGGL(log_probs_finish_kernel<1024>, dim3(B), dim3(1024), 0, st, f);
         e = hipGetLastError();
     }
