@@ -147,6 +147,8 @@ class _Marshalling:
     score_topk = score_topk_u16 = score_topk_subset = subitem_scores
     cross_entropy = cross_entropy_u16 = cross_entropy_backward = cross_entropy_u16_backward = subitem_scores
     subitem_scores_backward = default_cross_entropy = default_cross_entropy_backward = default_scores_q4 = subitem_scores
+    log_probs = log_probs_u16 = default_log_probs = distillation = distillation_u16 = default_distillation = subitem_scores
+    distillation_backward = distillation_u16_backward = default_distillation_backward = subitem_scores
 
     class Enqueue:
         def _bind(self, which, in0, in1, in2, n, N, B, d, m, b, K, out0, out1, ws, ws_bytes, stream, result, failed):
@@ -812,6 +814,11 @@ def pq_log_probs(codes: torch.Tensor, S: torch.Tensor, items: Optional[torch.Ten
     """What the softmax of the whole catalogue's scores over `temperature` says, by sub-ids: codes uint8 [N][m], S [B][m][b], items int32 [B][n] or
     None (an id outside [0, N): no item, log-probability 0) -> (log_probs fp32 [B][n], entropy [B], lse [B], and of the K likeliest items
     top_items int32 [B][K] and top_log_probs [B][K])."""
+    r = (_native_module or _native()).log_probs(codes, S, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs)
+    if r.__class__ is int:
+        raise PQError(r, "pq_log_probs")
+    if r is not None:
+        return r
     return _log_probs("pq_log_probs", False, torch.uint8, codes, S, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs)
 
 
@@ -823,6 +830,11 @@ def pq_log_probs_u16(codes: torch.Tensor, S: torch.Tensor, items: Optional[torch
                      workspace: Optional[torch.Tensor] = None, log_probs: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
                      lse: Optional[torch.Tensor] = None, top_items: Optional[torch.Tensor] = None, top_log_probs: Optional[torch.Tensor] = None) -> _Probs:
     """pq_log_probs over 16-bit sub-ids: codes uint16 [N][m]."""
+    r = (_native_module or _native()).log_probs_u16(codes, S, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs)
+    if r.__class__ is int:
+        raise PQError(r, "pq_log_probs_u16")
+    if r is not None:
+        return r
     return _log_probs("pq_log_probs_u16", False, torch.uint16, codes, S, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs)
 
 
@@ -836,6 +848,11 @@ def pq_default_log_probs(W: torch.Tensor, queries: torch.Tensor, items: Optional
                          ) -> _Probs:
     """pq_log_probs by the default scorer: W [N][d], queries [B][d] (both fp32, bf16 or fp16).  The K likeliest items and the given ones are scored in
     64 bits."""
+    r = (_native_module or _native()).default_log_probs(W, queries, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs)
+    if r.__class__ is int:
+        raise PQError(r, "pq_default_log_probs")
+    if r is not None:
+        return r
     return _log_probs("pq_default_log_probs", True, None, W, queries, items, K, temperature, workspace, log_probs, entropy, lse, top_items, top_log_probs)
 
 
@@ -848,6 +865,11 @@ def pq_distillation(codes: torch.Tensor, S: torch.Tensor, teacher_items: torch.T
                     ) -> Tuple[torch.Tensor, torch.Tensor]:
     """Distillation by sub-ids: temperature^2 times the divergence of the catalogue's softmax from a teacher's list, teacher_items int32 [B][K] (an id
     outside [0, N): no entry) with teacher_scores fp32 [B][K], whose softmax over the list are the weights -> (loss fp32 [B], lse fp32 [B])."""
+    r = (_native_module or _native()).distillation(codes, S, teacher_items, teacher_scores, temperature, workspace, loss, lse)
+    if r.__class__ is int:
+        raise PQError(r, "pq_distillation")
+    if r is not None:
+        return r
     return _distillation("pq_distillation", False, torch.uint8, codes, S, teacher_items, teacher_scores, temperature, workspace, loss, lse)
 
 
@@ -859,6 +881,11 @@ def pq_distillation_backward(codes: torch.Tensor, S: torch.Tensor, teacher_items
                              grad_loss: torch.Tensor, temperature: float = 1.0, workspace: Optional[torch.Tensor] = None,
                              out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of sum(grad_loss * loss) with respect to S: lse as pq_distillation returned it -> dS fp32 [B][m][b]."""
+    r = (_native_module or _native()).distillation_backward(codes, S, teacher_items, teacher_scores, lse, grad_loss, temperature, workspace, out)
+    if r.__class__ is int:
+        raise PQError(r, "pq_distillation_backward")
+    if r is not None:
+        return r
     return _distillation_backward("pq_distillation_backward", False, torch.uint8, codes, S, teacher_items, teacher_scores, lse, grad_loss, temperature,
                                   workspace, out)
 
@@ -871,6 +898,11 @@ def pq_distillation_u16(codes: torch.Tensor, S: torch.Tensor, teacher_items: tor
                         workspace: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
                         ) -> Tuple[torch.Tensor, torch.Tensor]:
     """pq_distillation over 16-bit sub-ids: codes uint16 [N][m]."""
+    r = (_native_module or _native()).distillation_u16(codes, S, teacher_items, teacher_scores, temperature, workspace, loss, lse)
+    if r.__class__ is int:
+        raise PQError(r, "pq_distillation_u16")
+    if r is not None:
+        return r
     return _distillation("pq_distillation_u16", False, torch.uint16, codes, S, teacher_items, teacher_scores, temperature, workspace, loss, lse)
 
 
@@ -882,6 +914,11 @@ def pq_distillation_u16_backward(codes: torch.Tensor, S: torch.Tensor, teacher_i
                                  grad_loss: torch.Tensor, temperature: float = 1.0, workspace: Optional[torch.Tensor] = None,
                                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """pq_distillation_backward over 16-bit sub-ids: codes uint16 [N][m]."""
+    r = (_native_module or _native()).distillation_u16_backward(codes, S, teacher_items, teacher_scores, lse, grad_loss, temperature, workspace, out)
+    if r.__class__ is int:
+        raise PQError(r, "pq_distillation_u16_backward")
+    if r is not None:
+        return r
     return _distillation_backward("pq_distillation_u16_backward", False, torch.uint16, codes, S, teacher_items, teacher_scores, lse, grad_loss, temperature,
                                   workspace, out)
 
@@ -894,6 +931,11 @@ def pq_default_distillation(W: torch.Tensor, queries: torch.Tensor, teacher_item
                             workspace: Optional[torch.Tensor] = None, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None
                             ) -> Tuple[torch.Tensor, torch.Tensor]:
     """pq_distillation by the default scorer: W [N][d], queries [B][d] (both fp32, bf16 or fp16)."""
+    r = (_native_module or _native()).default_distillation(W, queries, teacher_items, teacher_scores, temperature, workspace, loss, lse)
+    if r.__class__ is int:
+        raise PQError(r, "pq_default_distillation")
+    if r is not None:
+        return r
     return _distillation("pq_default_distillation", True, None, W, queries, teacher_items, teacher_scores, temperature, workspace, loss, lse)
 
 
@@ -905,6 +947,11 @@ def pq_default_distillation_backward(W: torch.Tensor, queries: torch.Tensor, tea
                                      grad_loss: torch.Tensor, temperature: float = 1.0, workspace: Optional[torch.Tensor] = None,
                                      dqueries: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Gradients of sum(grad_loss * loss) with respect to queries and W, in their type: lse as pq_default_distillation returned it."""
+    r = (_native_module or _native()).default_distillation_backward(W, queries, teacher_items, teacher_scores, lse, grad_loss, temperature, workspace, dqueries, dW)
+    if r.__class__ is int:
+        raise PQError(r, "pq_default_distillation_backward")
+    if r is not None:
+        return r
     return _distillation_backward("pq_default_distillation_backward", True, None, W, queries, teacher_items, teacher_scores, lse, grad_loss, temperature,
                                   workspace, dqueries, dW)
 

@@ -18,6 +18,7 @@
 
 #include "pqtopk.h"
 #include "pqtopk_train.h"
+#include "pqtopk_probs.h"
 
 namespace {
 
@@ -490,6 +491,160 @@ void enqueue_dealloc(PyObject* self) {
     Py_TYPE(self)->tp_free(self);
 }
 
+// A call by sub-ids of one or two bytes (first: codes, second: S) or by the default scorer (W, queries): its sizes as the C ABI takes them.
+enum Head { SUB_IDS, WIDE_SUB_IDS, DENSE };
+struct HeadArgs {
+    const at::Tensor *first = nullptr, *second = nullptr;
+    int64_t N = 0, B = 0;
+    int x = 0, y = 0;                                            // m, b or d, type
+    const void *p = nullptr, *q = nullptr;
+
+    template <Head H>
+    bool set(PyObject* a, PyObject* b, int device) {
+        if (H == DENSE) {
+            if (!THPVariable_Check(a)) return false;
+            const at::Tensor& W = THPVariable_Unpack(a);
+            y = dense_type(W);
+            if (y < 0 || !(first = plain(a, W.scalar_type(), device)) || !(second = plain(b, W.scalar_type(), device))) return false;
+            if (first->dim() != 2 || second->dim() != 2 || first->size(1) != second->size(1)) return false;
+            x = narrow(first->size(1));
+        } else {
+            first = plain(a, H == WIDE_SUB_IDS ? at::kUInt16 : at::kByte, device);
+            second = plain(b, at::kFloat, device);
+            if (!first || !second || first->dim() != 2 || second->dim() != 3 || second->size(1) != first->size(1)) return false;
+            x = narrow(first->size(1));
+            y = narrow(second->size(2));
+        }
+        N = first->size(0);
+        B = second->size(0);
+        p = first->const_data_ptr();
+        q = second->const_data_ptr();
+        return true;
+    }
+    const uint8_t* codes() const { return static_cast<const uint8_t*>(p); }
+    const uint16_t* wide_codes() const { return static_cast<const uint16_t*>(p); }
+    const float* S() const { return static_cast<const float*>(q); }
+};
+
+bool rows_of(const at::Tensor* t, int64_t B) { return t && t->dim() == 2 && t->size(0) == B; }
+
+// A number argument; false (and no error set) if it is none.
+bool number(PyObject* o, float& x) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) { PyErr_Clear(); return false; }
+    x = (float)v;
+    return true;
+}
+
+// log_probs(first, second, items | None, K, temperature, workspace | None, log_probs | None, entropy | None, lse | None, top_items | None,
+//           top_log_probs | None) -> (log_probs, entropy, lse, top_items, top_log_probs), an error code, or None
+template <Head H>
+PyObject* log_probs(PyObject*, PyObject* const* args, Py_ssize_t count) {
+    return guarded([&]() -> PyObject* {
+        if (count != 11) return none();
+        const int device = c10::hip::current_device();
+        HeadArgs a;
+        if (!a.set<H>(args[0], args[1], device) || !PyLong_Check(args[3])) return none();
+        const long long K = PyLong_AsLongLong(args[3]);
+        if (K == -1 && PyErr_Occurred()) { PyErr_Clear(); return none(); }
+        float T;
+        if (K < 0 || K > INT_MAX || !number(args[4], T)) return none();
+        const at::Tensor* items = nullptr;
+        if (args[2] != Py_None && !rows_of(items = plain(args[2], at::kInt, device), a.B)) return none();
+        const int64_t n = items ? items->size(1) : 0;
+        const int B = narrow(a.B);
+        Scratch ws(args[5], H == DENSE ? pq_default_log_probs_workspace_bytes(a.N, B, a.x, a.y, (int)K) : H == WIDE_SUB_IDS
+                   ? pq_log_probs_u16_workspace_bytes(a.N, B, a.x, a.y, (int)K) : pq_log_probs_workspace_bytes(a.N, B, a.x, a.y, (int)K), device);
+        Output lp(args[6], {a.B, n}, at::kFloat, device), entropy(args[7], {a.B}, at::kFloat, device), lse(args[8], {a.B}, at::kFloat, device);
+        Output top(args[9], {a.B, (int64_t)K}, at::kInt, device), top_lp(args[10], {a.B, (int64_t)K}, at::kFloat, device);
+        if (ws.bad || lp.bad || entropy.bad || lse.bad || top.bad || top_lp.bad) return none();
+        const int* ids = items ? items->const_data_ptr<int>() : nullptr;
+        float *l = lp.floats(), *h = entropy.floats(), *e = lse.floats(), *tl = top_lp.floats();
+        int* ti = top.t->mutable_data_ptr<int>();
+        void* st = current_stream();
+        const int rc = without_gil([&]() {
+            if (H == DENSE) return pq_default_log_probs(a.p, a.q, ids, a.N, B, a.x, a.y, narrow(n), (int)K, T, l, h, e, ti, tl, ws.p, ws.bytes, st);
+            if (H == WIDE_SUB_IDS) return pq_log_probs_u16(a.wide_codes(), a.S(), ids, a.N, B, a.x, a.y, narrow(n), (int)K, T, l, h, e, ti, tl, ws.p, ws.bytes, st);
+            return pq_log_probs(a.codes(), a.S(), ids, a.N, B, a.x, a.y, narrow(n), (int)K, T, l, h, e, ti, tl, ws.p, ws.bytes, st);
+        });
+        if (rc != PQ_OK) return PyLong_FromLong(rc);
+        PyObject* r = PyTuple_New(5);
+        if (!r) return nullptr;
+        Output* outputs[5] = {&lp, &entropy, &lse, &top, &top_lp};
+        for (int i = 0; i < 5; ++i) PyTuple_SET_ITEM(r, i, outputs[i]->object());
+        return r;
+    });
+}
+
+// distillation(first, second, teacher_items, teacher_scores, temperature, workspace | None, loss | None, lse | None) -> (loss, lse), an error code, or None
+template <Head H>
+PyObject* distillation(PyObject*, PyObject* const* args, Py_ssize_t count) {
+    return guarded([&]() -> PyObject* {
+        if (count != 8) return none();
+        const int device = c10::hip::current_device();
+        HeadArgs a;
+        float T;
+        if (!a.set<H>(args[0], args[1], device) || !number(args[4], T)) return none();
+        const at::Tensor *items = plain(args[2], at::kInt, device), *scores = plain(args[3], at::kFloat, device);
+        if (!rows_of(items, a.B) || !rows_of(scores, a.B) || items->size(1) != scores->size(1)) return none();
+        const int B = narrow(a.B), K = narrow(items->size(1));
+        Scratch ws(args[5], H == DENSE ? pq_default_distillation_workspace_bytes(a.N, B, a.x, a.y, K) : H == WIDE_SUB_IDS
+                   ? pq_distillation_u16_workspace_bytes(a.N, B, a.x, a.y, K) : pq_distillation_workspace_bytes(a.N, B, a.x, a.y, K), device);
+        Output loss(args[6], {a.B}, at::kFloat, device), lse(args[7], {a.B}, at::kFloat, device);
+        if (ws.bad || loss.bad || lse.bad) return none();
+        const int* ids = items->const_data_ptr<int>();
+        const float* u = scores->const_data_ptr<float>();
+        float *l = loss.floats(), *e = lse.floats();
+        void* st = current_stream();
+        const int rc = without_gil([&]() {
+            if (H == DENSE) return pq_default_distillation(a.p, a.q, ids, u, a.N, B, a.x, a.y, K, T, l, e, ws.p, ws.bytes, st);
+            if (H == WIDE_SUB_IDS) return pq_distillation_u16(a.wide_codes(), a.S(), ids, u, a.N, B, a.x, a.y, K, T, l, e, ws.p, ws.bytes, st);
+            return pq_distillation(a.codes(), a.S(), ids, u, a.N, B, a.x, a.y, K, T, l, e, ws.p, ws.bytes, st);
+        });
+        return rc != PQ_OK ? PyLong_FromLong(rc) : pair(loss, lse);
+    });
+}
+
+// distillation_backward(first, second, teacher_items, teacher_scores, lse, grad_loss, temperature, workspace | None, dS | None) -> dS, or with
+// dqueries | None, dW | None at the end -> (dqueries, dW); an error code, or None
+template <Head H>
+PyObject* distillation_backward(PyObject*, PyObject* const* args, Py_ssize_t count) {
+    return guarded([&]() -> PyObject* {
+        if (count != (H == DENSE ? 10 : 9)) return none();
+        const int device = c10::hip::current_device();
+        HeadArgs a;
+        float T;
+        if (!a.set<H>(args[0], args[1], device) || !number(args[6], T)) return none();
+        const at::Tensor *items = plain(args[2], at::kInt, device), *scores = plain(args[3], at::kFloat, device);
+        const at::Tensor *e = plain(args[4], at::kFloat, device), *g = plain(args[5], at::kFloat, device);
+        if (!rows_of(items, a.B) || !rows_of(scores, a.B) || items->size(1) != scores->size(1) || !vector_of(e, a.B) || !vector_of(g, a.B)) return none();
+        const int B = narrow(a.B), K = narrow(items->size(1));
+        Scratch ws(args[7], H == DENSE ? pq_default_distillation_backward_workspace_bytes(a.N, B, a.x, a.y, K) : H == WIDE_SUB_IDS
+                   ? pq_distillation_u16_backward_workspace_bytes(a.N, B, a.x, a.y, K) : pq_distillation_backward_workspace_bytes(a.N, B, a.x, a.y, K), device);
+        const int* ids = items->const_data_ptr<int>();
+        const float *u = scores->const_data_ptr<float>(), *lse = e->const_data_ptr<float>(), *grad = g->const_data_ptr<float>();
+        void* st = current_stream();
+        Output one(args[8], a.second->sizes(), a.second->scalar_type(), device);                       // dS, or dqueries
+        if (ws.bad || one.bad) return none();
+        void* first_out = one.t->mutable_data_ptr();
+        if (H == DENSE) {
+            Output dW(args[9], a.first->sizes(), a.first->scalar_type(), device);
+            if (dW.bad) return none();
+            void* second_out = dW.t->mutable_data_ptr();
+            const int rc = without_gil([&]() {
+                return pq_default_distillation_backward(a.p, a.q, ids, u, lse, grad, a.N, B, a.x, a.y, K, T, first_out, second_out, ws.p, ws.bytes, st);
+            });
+            return rc != PQ_OK ? PyLong_FromLong(rc) : pair(one, dW);
+        }
+        float* dS = static_cast<float*>(first_out);
+        const int rc = without_gil([&]() {
+            if (H == WIDE_SUB_IDS) return pq_distillation_u16_backward(a.wide_codes(), a.S(), ids, u, lse, grad, a.N, B, a.x, a.y, K, T, dS, ws.p, ws.bytes, st);
+            return pq_distillation_backward(a.codes(), a.S(), ids, u, lse, grad, a.N, B, a.x, a.y, K, T, dS, ws.p, ws.bytes, st);
+        });
+        return rc != PQ_OK ? PyLong_FromLong(rc) : one.object();
+    });
+}
+
 PyMethodDef enqueue_methods[] = {{"_bind", enqueue_bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyTypeObject enqueue_type = {PyVarObject_HEAD_INIT(nullptr, 0) "_pqnative.Enqueue"};
 
@@ -498,6 +653,15 @@ PyMethodDef functions[] = {
     {"score_topk", (PyCFunction)(void (*)(void))score_topk<false>, METH_FASTCALL, nullptr},
     {"score_topk_u16", (PyCFunction)(void (*)(void))score_topk<true>, METH_FASTCALL, nullptr},
     {"score_topk_subset", (PyCFunction)(void (*)(void))score_topk_subset, METH_FASTCALL, nullptr},
+    {"log_probs", (PyCFunction)(void (*)(void))log_probs<SUB_IDS>, METH_FASTCALL, nullptr},
+    {"log_probs_u16", (PyCFunction)(void (*)(void))log_probs<WIDE_SUB_IDS>, METH_FASTCALL, nullptr},
+    {"default_log_probs", (PyCFunction)(void (*)(void))log_probs<DENSE>, METH_FASTCALL, nullptr},
+    {"distillation", (PyCFunction)(void (*)(void))distillation<SUB_IDS>, METH_FASTCALL, nullptr},
+    {"distillation_u16", (PyCFunction)(void (*)(void))distillation<WIDE_SUB_IDS>, METH_FASTCALL, nullptr},
+    {"default_distillation", (PyCFunction)(void (*)(void))distillation<DENSE>, METH_FASTCALL, nullptr},
+    {"distillation_backward", (PyCFunction)(void (*)(void))distillation_backward<SUB_IDS>, METH_FASTCALL, nullptr},
+    {"distillation_u16_backward", (PyCFunction)(void (*)(void))distillation_backward<WIDE_SUB_IDS>, METH_FASTCALL, nullptr},
+    {"default_distillation_backward", (PyCFunction)(void (*)(void))distillation_backward<DENSE>, METH_FASTCALL, nullptr},
     {"cross_entropy", (PyCFunction)(void (*)(void))cross_entropy<false>, METH_FASTCALL, nullptr},
     {"cross_entropy_u16", (PyCFunction)(void (*)(void))cross_entropy<true>, METH_FASTCALL, nullptr},
     {"cross_entropy_backward", (PyCFunction)(void (*)(void))cross_entropy_backward<false>, METH_FASTCALL, nullptr},
