@@ -10,19 +10,19 @@ namespace {
 int keep_of(int K) { return K ? K + 16 + K / 8 : 0; }
 static_assert(most_of(PQ_MAX_K + 16 + PQ_MAX_K / 8) < kMostKept, "a cut leaves no more");
 
-// The cross entropy's plan of a piece, in no more groups than a list has regions; how many items' places a group has.
-DensePlan plan_piece(long long items, int B, int d, int type, long long& region) {
+// The cross entropy's plan of a piece, whose lists have no more regions than there are places for: how many these are, and the places of each.
+DensePlan plan_piece(long long items, int B, int d, int type, int& regions, long long& region) {
     DensePlan p = plan_dense(items, B, d, type);
-    if (p.few) {
-        const long long of = few_items(d);
-        region = ceil_div(ceil_div(items, of), p.groups) * of;
-        return p;
+    const int shares = shares_of(p);
+    if (p.few) region = ceil_div(ceil_div(items, few_items(d)), p.groups) * few_items(d);
+    else {
+        while (p.groups * shares > kMostRegions) {
+            p.tiles_each *= 2;
+            p.groups = (int)ceil_div(p.item_tiles, p.tiles_each);
+        }
+        region = (long long)p.tiles_each * p.loss_items / shares;
     }
-    while (p.groups > kMostRegions) {
-        p.tiles_each *= 2;
-        p.groups = (int)ceil_div(p.item_tiles, p.tiles_each);
-    }
-    region = (long long)p.tiles_each * p.loss_items;
+    regions = p.groups * shares;
     return p;
 }
 
@@ -35,10 +35,10 @@ Layout lay_out(long long N, int B, int d, int type, int K) {
     l.passes = passes_of(N, B, keep_of(K));
     l.groups = 0;
     for (long long done = 0, now, region; done < N; done += now) {
+        int regions;
         now = l.passes.after(done);
-        const DensePlan p = plan_piece(now, B, d, type, region);
-        l.groups += p.groups;
-        l.piece(done == 0 ? now : p.groups * region, p.groups);
+        l.groups += plan_piece(now, B, d, type, regions, region).groups;
+        l.piece(done == 0 ? now : regions * region, regions);
     }
     l.ListLayout::lay_out((size_t)l.groups * B * sizeof(float4), B, K);
     return l;
@@ -55,16 +55,15 @@ hipError_t pass(const Layout& l, DenseProbsArgs a, DenseFinishArgs f, int type, 
     hipError_t e = hipSuccess;
     for (long long done = 0; done < a.N && e == hipSuccess; done = a.end) {
         const long long now = l.passes.after(done);
-        const DensePlan p = plan_piece(now, a.B, a.d, type, a.region);
+        const DensePlan p = plan_piece(now, a.B, a.d, type, f.regions, a.region);
         a.first = done;
         a.end = done + now;
         a.store = f.K != 0 && done == 0;
         a.item_tiles = p.item_tiles; a.tiles_each = p.tiles_each; a.groups = p.groups; a.position_tiles = p.position_tiles;
         e = dense_probs<T>(p, a, st);
         a.partial += (size_t)p.groups * a.B;
-        if (e == hipSuccess && f.K && a.end < a.N) e = launch_select(a.lists, a.B, a.store ? (int)now : 0, p.groups, a.region, st);
+        if (e == hipSuccess && f.K && a.end < a.N) e = launch_select(a.lists, a.B, a.store ? (int)now : 0, f.regions, a.region, st);
         f.stored = a.store ? (int)now : 0;
-        f.regions = p.groups;
         f.region = a.region;
     }
     return e != hipSuccess ? e : dense_probs_finish<T>(f, st);

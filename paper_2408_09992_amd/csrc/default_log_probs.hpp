@@ -20,31 +20,30 @@ struct DenseProbsArgs {
     int tiles_each, groups, position_tiles;
     float4* partial;                                   // [groups][B]: (reference, sum, weighted sum)
     Lists lists;
-    long long region;                                  // items of a group
+    long long region;                                  // places of a region
 };
 
-// A score that passes its position's floor to the group's region of the list, or every one of the first piece.
-__device__ __forceinline__ void offer(const DenseProbsArgs& a, int q, int group, int* count, float z, long long item) {
-    if (a.store) a.lists.keys[(size_t)q * a.lists.cap + (size_t)(item - a.first)] = key_of(z, (uint32_t)item);
-    else append(a.lists, q, group * a.region, count, z, (uint32_t)item);
-}
+// A group's region of a position's list is divided between the lanes that have scores of it (kShares of them), so that each counts its own in a register: a
+// counter in LDS, whose answer every candidate waits for, took 180 us of the 1.9 ms of 1024 positions' best 100 of 1.28M items, where this takes 110.
+template <typename Tile, int ITEMS> constexpr int kShares = ITEMS / (32 * Tile::MI) * 2;
 
 template <typename T, int BN, int ITEMS>
 __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_log_probs_kernel(DenseProbsArgs a) {
     using Tile = ScoresTile<T, BN, ITEMS>;
     constexpr int MI = Tile::MI, NI = Tile::NI, kRowWaves = ITEMS / (32 * MI);
     __shared__ float4 stat[kRowWaves][BN];
-    __shared__ int listed[BN];
-    for (int i = threadIdx.x; i < BN; i += Tile::kThreads) listed[i] = 0;          // (the products' barriers come before any use)
     int group, pt;
     chiplet_order(blockIdx.x, a.position_tiles, group, pt);
     if (group >= a.groups) return;
     const int lane = threadIdx.x % kWave;
     float c[NI], s[NI], t[NI], floor[NI];
+    int listed[NI];
+    const int share = Tile::wave_row() / (32 * MI) * 2 + lane / 32;
     const int q0 = pt * BN + Tile::wave_col() + lane % 32;
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) {
         c[ni] = kLowest; s[ni] = 0.0f; t[ni] = 0.0f;
+        listed[ni] = 0;
         floor[ni] = __builtin_inff();
         if (a.lists.keep && !a.store && q0 + 32 * ni < a.B) floor[ni] = a.lists.floor[q0 + 32 * ni];
     }
@@ -68,24 +67,40 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
                     for (int e = 0; e < 16; ++e)
                         if (32 * mi + 8 * (e / 4) + e % 4 >= left - 4 * (lane / 32)) acc[mi][ni][e] = -__builtin_inff();
             }
-            float tops[MI];                                    // (of a block of 32 x 32)
+            float tops[MI][4];                                 // (of four items each)
 #pragma unroll
-            for (int mi = 0; mi < MI; ++mi) {
-                tops[mi] = acc[mi][ni][0];
+            for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
-                for (int e = 1; e < 16; ++e) tops[mi] = fmaxf(tops[mi], acc[mi][ni][e]);
-                top = fmaxf(top, tops[mi]);
-            }
-#pragma unroll
-            for (int mi = 0; mi < MI; ++mi) {
-                if (a.store || __any(tops[mi] > floor[ni])) {
-                    stay_a_branch();
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int at = 32 * mi + 8 * (e / 4) + e % 4;
-                        if (a.store ? q0 + 32 * ni < a.B && at < left - 4 * (lane / 32) : acc[mi][ni][e] > floor[ni]) offer(a, q0 + 32 * ni, group, &listed[Tile::wave_col() + 32 * ni + lane % 32], acc[mi][ni][e], mine + at);
-                    }
+                for (int four = 0; four < 4; ++four) {
+                    tops[mi][four] = fmaxf(fmaxf(acc[mi][ni][4 * four], acc[mi][ni][4 * four + 1]), fmaxf(acc[mi][ni][4 * four + 2], acc[mi][ni][4 * four + 3]));
+                    top = fmaxf(top, tops[mi][four]);
                 }
+            if (a.store || __any(top > floor[ni])) {
+                int q = q0 + 32 * ni;
+                asm volatile("" : "+v"(q));                    // (so that no address is kept in registers for a branch that is rarely taken)
+                uint64_t* keys = a.lists.keys + (size_t)q * a.lists.cap;
+                if (a.store) keys += mine - a.first;
+                else keys += ((size_t)group * kShares<Tile, ITEMS> + share) * a.region + listed[ni];
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int four = 0; four < 4; ++four) {
+                        if (a.store) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const int at = 32 * mi + 8 * four + e;
+                                if (q < a.B && at < left - 4 * (lane / 32)) keys[at] = key_of(acc[mi][ni][4 * four + e], (uint32_t)(mine + at));
+                            }
+                        } else if (__any(tops[mi][four] > floor[ni])) {
+                            stay_a_branch();
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (acc[mi][ni][4 * four + e] > floor[ni]) {
+                                    *keys++ = key_of(acc[mi][ni][4 * four + e], (uint32_t)(mine + 32 * mi + 8 * four + e));
+                                    ++listed[ni];
+                                }
+                        }
+                    }
             }
             top *= a.scale;
             if (__any(top > c[ni] + kNearHeadroom)) {
@@ -115,6 +130,11 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
             t[ni] += sum_x;
         }
     }
+    if (a.lists.keep && !a.store) {
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni)
+            if (q0 + 32 * ni < a.B) a.lists.counts[((size_t)group * kShares<Tile, ITEMS> + share) * a.B + q0 + 32 * ni] = listed[ni];
+    }
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) {
         join_sums(c[ni], s[ni], t[ni], __shfl_xor(c[ni], 32), __shfl_xor(s[ni], 32), __shfl_xor(t[ni], 32));
@@ -127,7 +147,6 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
 #pragma unroll
         for (int w = 1; w < kRowWaves; ++w) join_sums(v.x, v.y, v.z, stat[w][threadIdx.x].x, stat[w][threadIdx.x].y, stat[w][threadIdx.x].z);
         a.partial[(size_t)group * a.B + q] = v;
-        if (a.lists.keep && !a.store) a.lists.counts[(size_t)group * a.B + q] = listed[threadIdx.x];
     }
 }
 
@@ -207,6 +226,14 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
 
 // ---------------------------------------------------------------------------------------------------------------
 // host side, by type of the operands (a translation unit each)
+
+// Shares of a group's region, by the tile that a plan takes (few positions' kernel does not divide it).
+inline int shares_of(const DensePlan& p) {
+    if (p.few) return 1;
+    return p.loss_items == 64 || p.positions >= 128 ? 4 : 8;
+}
+static_assert(kShares<ScoresTile<__bf16, 64, 64>, 64> == 4 && kShares<ScoresTile<__bf16, 64, 256>, 256> == 8 && kShares<ScoresTile<__bf16, 128, 256>, 256> == 4 &&
+              kShares<ScoresTile<__bf16, 256, 256>, 256> == 4, "as shares_of() has it");
 
 template <typename T> hipError_t dense_probs(const DensePlan& p, const DenseProbsArgs& a, hipStream_t st);
 template <typename T> hipError_t dense_probs_finish(const DenseFinishArgs& a, hipStream_t st);
