@@ -20,7 +20,7 @@ constexpr int kFewKeys = 4, kManyKeys = 16;          // keys that a thread of a 
 
 struct Lists {
     uint64_t* keys;            // [B][cap]: all keys of the first piece, or the regions of a later one
-    int* counts;               // [regions][B]
+    int* counts;               // [B][kMostRegions]: a position's side by side, which a cut reads
     uint64_t* kept;            // [B][kMostKept]: of the pieces before
     int* kept_count;           // [B]
     float* floor;              // [B]
@@ -201,8 +201,8 @@ __host__ __device__ constexpr int most_of(int keep) { return keep + keep / 4 + 3
 // Cuts a position's list: what is left in out[] (the order is none), `keep` at least (or all) and most_of(keep) at most; returns how many, and in `least` what
 // they reach (0: as good as nothing was cut).  last: no floor is asked for.  stored: how many keys the first piece left, if that was the last piece; else regions of `region` keys each.
 template <int THREADS>
-__device__ __forceinline__ int cut_list(const Lists& l, int q, int B, int stored, int regions, long long region, bool last, uint64_t* out, uint64_t& least, SelectMemory<THREADS>& mem) {
-    const int tid = threadIdx.x, most = most_of(l.keep);
+__device__ __forceinline__ int cut_list(const Lists& l, int q, int stored, int regions, long long region, bool last, uint64_t* out, uint64_t& least, SelectMemory<THREADS>& mem) {
+    const int tid = threadIdx.x, most = last ? l.keep + 16 : most_of(l.keep);       // (of the last every key is scored again)
     const uint64_t* keys = l.keys + (size_t)q * l.cap;
     Keys all{l.kept + (size_t)q * kMostKept, keys, mem.begin, region, stored, 1, stored};
     if (stored) all.kept = keys;
@@ -213,7 +213,7 @@ __device__ __forceinline__ int cut_list(const Lists& l, int q, int B, int stored
         int own[kOwn], sum = 0;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-            own[i] = kOwn * tid + i < regions ? l.counts[(size_t)(kOwn * tid + i) * B + q] : 0;
+            own[i] = kOwn * tid + i < regions ? l.counts[(size_t)q * kMostRegions + kOwn * tid + i] : 0;
             sum += own[i];
         }
         uint32_t total;
@@ -242,12 +242,12 @@ __device__ __forceinline__ int cut_list(const Lists& l, int q, int B, int stored
 
 // grid = positions: cuts the lists between two pieces and sets the floors.
 template <int THREADS>
-__global__ __launch_bounds__(THREADS) void select_kernel(Lists l, int B, int stored, int regions, long long region) {
+__global__ __launch_bounds__(THREADS) void select_kernel(Lists l, int stored, int regions, long long region) {
     __shared__ SelectMemory<THREADS> mem;
     __shared__ uint64_t out[kMostKept];
     const int q = blockIdx.x, tid = threadIdx.x;
     uint64_t least;
-    const int n = cut_list(l, q, B, stored, regions, region, false, out, least, mem);
+    const int n = cut_list(l, q, stored, regions, region, false, out, least, mem);
     for (int i = tid; i < n; i += THREADS) l.kept[(size_t)q * kMostKept + i] = out[i];
     if (tid == 0) {
         l.kept_count[q] = n;
@@ -287,17 +287,13 @@ inline Passes passes_of(long long N, int B, int keep) {
 // Where the lists lie in a workspace, behind `at` bytes.
 struct ListLayout {
     long long cap = 0;
-    int regions = 0;
     size_t keys_at, counts_at, kept_at, kept_count_at, floor_at, bytes;
-    void piece(long long keys, int n) {                          // a piece whose n workgroups' regions take so many keys
-        cap = keys > cap ? keys : cap;
-        regions = n > regions ? n : regions;
-    }
+    void piece(long long keys) { cap = keys > cap ? keys : cap; }     // a piece whose regions take so many keys
     void lay_out(size_t at, int B, int keep) {
         const size_t on = keep ? 1 : 0;
         keys_at = round_up(at, 256);
         counts_at = keys_at + round_up(on * B * cap * sizeof(uint64_t), 256);
-        kept_at = counts_at + round_up(on * B * regions * sizeof(int), 256);
+        kept_at = counts_at + round_up(on * B * kMostRegions * sizeof(int), 256);
         kept_count_at = kept_at + round_up(on * B * kMostKept * sizeof(uint64_t), 256);
         floor_at = kept_count_at + round_up(on * B * sizeof(int), 256);
         bytes = floor_at + round_up(on * B * sizeof(float), 256);
@@ -309,8 +305,8 @@ struct ListLayout {
 };
 
 inline hipError_t launch_select(const Lists& l, int B, int stored, int regions, long long region, hipStream_t st) {
-    if (many_lists(B)) hipLaunchKernelGGL(select_kernel<256>, dim3(B), dim3(256), 0, st, l, B, stored, regions, region);
-    else hipLaunchKernelGGL(select_kernel<1024>, dim3(B), dim3(1024), 0, st, l, B, stored, regions, region);
+    if (many_lists(B)) hipLaunchKernelGGL(select_kernel<256>, dim3(B), dim3(256), 0, st, l, stored, regions, region);
+    else hipLaunchKernelGGL(select_kernel<1024>, dim3(B), dim3(1024), 0, st, l, stored, regions, region);
     return hipGetLastError();
 }
 

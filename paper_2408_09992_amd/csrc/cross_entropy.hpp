@@ -182,7 +182,8 @@ struct ProbsArgs {
     float scale;
     uint32_t first, end;       // the piece's items
     int store;                 // whether all its scores go to the lists
-    float4* partial;           // [gridDim.x][B]: (reference, sum, weighted sum)
+    float4* partial;           // [B][partials], of all pieces: (reference, sum, weighted sum); of this one from `done` on
+    int partials, done;
     Lists lists;
     float* finite;             // [B][m][b], or NULL: the tables as a ranking takes them, held within +-1e32, 0 for a NaN
 };
@@ -336,8 +337,8 @@ __device__ __forceinline__ void sum_items(const Args& a) {
 #pragma unroll 2                                               // (fifteen at once would be the kernel's most registers)
             for (int w = 1; w < kWaves; ++w) join_sums(sums.x, sums.y, sums.z, stat[w * Q + wave].x, stat[w * Q + wave].y, stat[w * Q + wave].z);
             if (lane == 0) {
-                a.partial[(size_t)blockIdx.x * a.B + q] = sums;
-                if (a.lists.keep && !a.store) a.lists.counts[(size_t)blockIdx.x * a.B + q] = listed[wave];
+                a.partial[(size_t)q * a.partials + a.done + blockIdx.x] = sums;
+                if (a.lists.keep && !a.store) a.lists.counts[(size_t)q * kMostRegions + blockIdx.x] = listed[wave];
             }
         } else {
             for (int w = 1; w < kWaves; ++w) join_sums(sums.x, sums.y, stat[w * Q + wave].x, stat[w * Q + wave].y);

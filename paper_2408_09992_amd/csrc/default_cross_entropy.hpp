@@ -781,10 +781,10 @@ __device__ __forceinline__ void few_sums(const Args& a, long long from, long lon
             if constexpr (PROBS) join_sums(v.x, v.y, v.z, stat[w][tid].x, stat[w][tid].y, stat[w][tid].z);
             else join_sums(v.x, v.y, stat[w][tid].x, stat[w][tid].y);
         }
-        a.partial[(size_t)blockIdx.x * a.B + tid] = v;
         if constexpr (PROBS) {
-            if (a.lists.keep && !a.store) a.lists.counts[(size_t)blockIdx.x * a.B + tid] = listed[tid];
-        }
+            a.partial[(size_t)tid * a.partials + a.done + blockIdx.x] = v;
+            if (a.lists.keep && !a.store) a.lists.counts[(size_t)tid * kMostRegions + blockIdx.x] = listed[tid];
+        } else a.partial[(size_t)blockIdx.x * a.B + tid] = v;
     }
 }
 

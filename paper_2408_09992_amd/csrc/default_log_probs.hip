@@ -7,17 +7,23 @@ namespace {
 
 // How many candidates for the K best are scored in 64 bits at least: float32 scores may put neighbours in another order, not items that far apart
 // (neighbours among the best 100 of 1.28M lie some 1e-3 of their scores apart, a sum's rounding 1e-6).
-int keep_of(int K) { return K ? K + 16 + K / 8 : 0; }
-static_assert(most_of(PQ_MAX_K + 16 + PQ_MAX_K / 8) < kMostKept, "a cut leaves no more");
+int keep_of(int K) { return K ? K + 16 : 0; }
+static_assert(most_of(PQ_MAX_K + 16) < kMostKept, "a cut leaves no more");
 
 // The cross entropy's plan of a piece, whose lists have no more regions than there are places for: how many these are, and the places of each.
-DensePlan plan_piece(long long items, int B, int d, int type, int& regions, long long& region) {
+DensePlan plan_piece(long long items, int B, int d, int type, bool listed, int& regions, long long& region) {
     DensePlan p = plan_dense(items, B, d, type);
     const int shares = shares_of(p);
     if (p.few) region = ceil_div(ceil_div(items, few_items(d)), p.groups) * few_items(d);
     else {
-        while (p.groups * shares > kMostRegions) {
-            p.tiles_each *= 2;
+        if (listed && (long long)p.groups * shares > kMostRegions) {
+            // the rounds over the chip that take least, a tile of items a unit; of as good ones the fewest groups
+            double best = 1e300;
+            const long long least = ceil_div(p.item_tiles * shares, kMostRegions);
+            for (long long each = least; each <= 2 * least + 16; ++each) {
+                const double cost = (double)ceil_div(ceil_div(p.item_tiles, each) * p.position_tiles, kCUs) * (each + 0.1);
+                if (cost <= best) { best = cost; p.tiles_each = (int)each; }
+            }
             p.groups = (int)ceil_div(p.item_tiles, p.tiles_each);
         }
         region = (long long)p.tiles_each * p.loss_items / shares;
@@ -37,8 +43,8 @@ Layout lay_out(long long N, int B, int d, int type, int K) {
     for (long long done = 0, now, region; done < N; done += now) {
         int regions;
         now = l.passes.after(done);
-        l.groups += plan_piece(now, B, d, type, regions, region).groups;
-        l.piece(done == 0 ? now : regions * region, regions);
+        l.groups += plan_piece(now, B, d, type, K != 0, regions, region).groups;
+        l.piece(done == 0 ? now : regions * region);
     }
     l.ListLayout::lay_out((size_t)l.groups * B * sizeof(float4), B, K);
     return l;
@@ -55,13 +61,13 @@ hipError_t pass(const Layout& l, DenseProbsArgs a, DenseFinishArgs f, int type, 
     hipError_t e = hipSuccess;
     for (long long done = 0; done < a.N && e == hipSuccess; done = a.end) {
         const long long now = l.passes.after(done);
-        const DensePlan p = plan_piece(now, a.B, a.d, type, f.regions, a.region);
+        const DensePlan p = plan_piece(now, a.B, a.d, type, f.K != 0, f.regions, a.region);
         a.first = done;
         a.end = done + now;
         a.store = f.K != 0 && done == 0;
         a.item_tiles = p.item_tiles; a.tiles_each = p.tiles_each; a.groups = p.groups; a.position_tiles = p.position_tiles;
         e = dense_probs<T>(p, a, st);
-        a.partial += (size_t)p.groups * a.B;
+        a.done += p.groups;
         if (e == hipSuccess && f.K && a.end < a.N) e = launch_select(a.lists, a.B, a.store ? (int)now : 0, f.regions, a.region, st);
         f.stored = a.store ? (int)now : 0;
         f.region = a.region;
@@ -98,6 +104,7 @@ int pq_default_log_probs(const void* W, const void* queries, const int* items, l
     DenseProbsArgs a{};
     a.W = W; a.H = queries; a.N = N; a.B = B; a.d = d; a.scale = (float)(kLog2eDouble / temperature);
     a.partial = reinterpret_cast<float4*>(ws);
+    a.partials = l.groups;
     a.lists = l.lists(ws, l.passes.keep);
     const DenseFinishArgs f{W, queries, items, N, B, d, n, K, temperature, a.partial, l.groups, 0, 0, 0, a.lists, log_probs, entropy, lse, top_items, top_log_probs};
     hipStream_t st = static_cast<hipStream_t>(stream);

@@ -18,7 +18,8 @@ struct DenseProbsArgs {
     int store;                                         // whether all its scores go to the lists
     long long item_tiles;
     int tiles_each, groups, position_tiles;
-    float4* partial;                                   // [groups][B]: (reference, sum, weighted sum)
+    float4* partial;                                   // [B][partials], of all pieces: (reference, sum, weighted sum); of this one from `done` on
+    int partials, done;
     Lists lists;
     long long region;                                  // places of a region
 };
@@ -133,7 +134,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     if (a.lists.keep && !a.store) {
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni)
-            if (q0 + 32 * ni < a.B) a.lists.counts[((size_t)group * kShares<Tile, ITEMS> + share) * a.B + q0 + 32 * ni] = listed[ni];
+            if (q0 + 32 * ni < a.B) a.lists.counts[(size_t)(q0 + 32 * ni) * kMostRegions + group * kShares<Tile, ITEMS> + share] = listed[ni];
     }
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) {
@@ -146,7 +147,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
         float4 v = stat[0][threadIdx.x];
 #pragma unroll
         for (int w = 1; w < kRowWaves; ++w) join_sums(v.x, v.y, v.z, stat[w][threadIdx.x].x, stat[w][threadIdx.x].y, stat[w][threadIdx.x].z);
-        a.partial[(size_t)group * a.B + q] = v;
+        a.partial[(size_t)q * a.partials + a.done + group] = v;
     }
 }
 
@@ -160,7 +161,7 @@ struct DenseFinishArgs {
     long long N;
     int B, d, n, K;
     float temperature;
-    const float4* partial;     // [groups][B], of all pieces
+    const float4* partial;     // [B][groups], of all pieces
     int groups, stored, regions;                       // groups of all pieces; of the last piece what cut_list() takes
     long long region;
     Lists lists;
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     float c = kLowest, s = 0.0f, t = 0.0f;
     for (int i = tid; i < a.groups; i += THREADS) {
-        const float4 v = a.partial[(size_t)i * a.B + q];
+        const float4 v = a.partial[(size_t)q * a.groups + i];
         join_sums(c, s, t, v.x, v.y, v.z);
     }
 #pragma unroll
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
     }
     if (a.K == 0) return;
     uint64_t least;
-    const int n = cut_list<THREADS>(a.lists, q, a.B, a.stored, a.regions, a.region, true, kept, least, mem);
+    const int n = cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem);
     for (int i = tid / 16; i < n; i += THREADS / 16) {
         const double z = dot64(W + (size_t)item_of(kept[i]) * a.d, h, a.d);
         if (tid % 16 == 0) score[i] = z;

@@ -27,7 +27,7 @@ struct FinishArgs {
     long long N;
     int B, m, b, n, K, code_bytes;
     float temperature;
-    const float4* partial;     // [shares][B]
+    const float4* partial;     // [B][shares]
     int shares, stored, regions;                       // shares of all pieces; of the last piece what cut_list() takes
     long long region;
     Lists lists;
@@ -58,7 +58,7 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     float c = kLowest, s = 0.0f, t = 0.0f;
     for (int i = tid; i < a.shares; i += THREADS) {
-        const float4 v = a.partial[(size_t)i * a.B + q];
+        const float4 v = a.partial[(size_t)q * a.shares + i];
         join_sums(c, s, t, v.x, v.y, v.z);
     }
 #pragma unroll
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
         return;
     }
     uint64_t least;
-    const int n = cut_list<THREADS>(a.lists, q, a.B, a.stored, a.regions, a.region, true, kept, least, mem);
+    const int n = cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem);
     for (int at = tid; at < n; at += THREADS) {
         const uint64_t mine = kept[at];
         int rank = 0;
@@ -160,7 +160,7 @@ bool lay_out(Layout& l, long long N, int B, int m, int b, int K, int code_bytes)
         now = l.passes.after(done);
         if (!plan_loss(p, now, B, m, b, code_bytes)) return false;
         l.shares += p.shares;
-        l.piece(done == 0 ? now : (long long)p.shares * p.share, p.shares);
+        l.piece(done == 0 ? now : (long long)p.shares * p.share);
     }
     l.ListLayout::lay_out((size_t)l.shares * B * sizeof(float4), B, l.passes.keep);
     if (l.topk_bytes) {
@@ -199,7 +199,7 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
     hipStream_t st = static_cast<hipStream_t>(stream);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     const Lists lists = l.lists(ws, l.passes.keep);
-    ProbsArgs a{codes, S, N, B, m, b, 0, (float)(kLog2eDouble / temperature), 0, 0, 0, reinterpret_cast<float4*>(ws), lists,
+    ProbsArgs a{codes, S, N, B, m, b, 0, (float)(kLog2eDouble / temperature), 0, 0, 0, reinterpret_cast<float4*>(ws), l.shares, 0, lists,
                 l.topk_bytes ? reinterpret_cast<float*>(ws + l.finite_at) : nullptr};
     float* ranked = l.topk_bytes ? reinterpret_cast<float*>(ws + l.ranked_at) : nullptr;
     hipError_t e = hipSuccess;
@@ -212,7 +212,7 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
         a.share = p.share;
         a.store = lists.keep != 0 && done == 0;
         e = go_m<CT>(p, a, st);
-        a.partial += (size_t)p.shares * B;
+        a.done += p.shares;
         if (e == hipSuccess && lists.keep && a.end < N) e = launch_select(lists, B, a.store ? (int)now : 0, p.shares, p.share, st);
     }
     if (e == hipSuccess && ranked) {
