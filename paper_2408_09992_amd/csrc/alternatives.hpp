@@ -8,6 +8,7 @@
 // A workgroup has a region of each of its positions' lists, as long as it has items, and counts in LDS what it puts there.  (Counters of all workgroups
 // in memory took the longest part of a pass: 64 of them, 53,000 candidates, 280 us.)
 #pragma once
+#include <math.h>
 #include "head_common.hpp"
 
 namespace pqk {
@@ -261,15 +262,16 @@ __global__ __launch_bounds__(THREADS) void select_kernel(Lists l, int stored, in
 inline bool many_lists(int B) { return B > kCUs; }
 
 // The pieces of a pass over N items: `first` items, whose scores are all stored, then as many as the lists have room for and no more than `growth`
-// times the items before them: a list gets some growth * keep new keys in each.  A candidate of many positions costs more than a cut (1024 positions, 128 kept:
-// some 30 ps each over the chip), few positions' candidates less.
+// times the items before them: a list gets some growth * keep new keys in each.  How many pieces: a cut and what it stops take some 25 us, a candidate 40 to
+// 150 ps over the chip (1024 positions, 116 kept, 840,000 candidates beside 262,144 items of 512 bfloat16 46 us; 300,000 items of 256 bfloat16, 300 positions, K = 20 in one piece of 295,904 after the first: 780,000 candidates, 120 us).
 constexpr long long kOnePiece = 16384, kListBytes = 1LL << 31;
 struct Passes {
     long long N, first, room, growth;
     int keep;
     long long after(long long done) const {                      // items of the piece after `done` items
         if (done == 0) return first;
-        const long long n = done * growth < room ? done * growth : room;
+        const long long most = done * growth < room ? done * growth : room;
+        const long long n = most > 16384 ? most / 16384 * 16384 : most;          // (whole rounds of 256 x 256 tiles over the chip)
         return n < N - done ? n : N - done;
     }
 };
@@ -278,8 +280,11 @@ inline Passes passes_of(long long N, int B, int keep) {
     if (keep == 0) return p;
     const long long least = B <= 128 ? kOnePiece : (long long)round_up(8 * (size_t)keep, 4096);
     if (N > kOnePiece && N > 2 * least) p.first = least;
-    p.growth = 4096 / keep;
-    p.growth = (long long)keep * B >= 32768 || p.growth < 8 ? 8 : p.growth > 128 ? 128 : p.growth;
+    double best = 1e300;
+    for (int pieces = 1; pieces <= 8; ++pieces) {
+        const double growth = pow((double)N / (double)p.first, 1.0 / pieces), cost = pieces * (25.0 + 5e-5 * (double)B * keep * growth);
+        if (cost < best) { best = cost; p.growth = (long long)growth + 1; }
+    }
     p.room = kListBytes / 8 / B > p.first ? kListBytes / 8 / B : p.first;
     return p;
 }
