@@ -11,6 +11,7 @@
 #include "pqtopk_train.h"
 #include "head_common.hpp"
 #include "alternatives.hpp"
+#include "teacher.hpp"
 
 namespace pqk {
 namespace head {
@@ -137,40 +138,79 @@ __device__ __forceinline__ void fill_tables(float* table, const float* S, int q0
     }
 }
 
+struct LossArgs {
+    const void* codes;
+    const float* S;
+    const int* targets;
+    long long N;
+    int B, m, b;
+    uint32_t share;            // items per workgroup
+    float2* partial;           // [gridDim.x][B]: (reference, sum), where the items are shared
+    float *loss, *lse;
+    float scale;               // what scores are multiplied with: log2 e over the temperature
+};
+
 // What one position's statistics make of it, by one wave: lse, and the loss with the target's score (its m sub-item scores are
 // fetched by as many lanes at once).
-__device__ __forceinline__ void finish_position(float c, float s, const void* codes, int code_bytes, const float* S, const int* targets,
-                                                long long N, int m, int b, int q, float* loss, float* lse) {
-    const int lane = threadIdx.x % kWave, t = targets[q];
+__device__ __forceinline__ void finish_position(const LossArgs& a, float c, float s, int code_bytes, int q) {
+    const int lane = threadIdx.x % kWave, t = a.targets[q];
     const float l = log_sum(c, s);
-    const bool has = t >= 0 && t < N && l != -__builtin_inff();
+    const bool has = t >= 0 && t < a.N && l != -__builtin_inff();
     float z = 0.0f;
     if (has) {
-        for (int k = lane; k < m; k += kWave) {
-            const size_t at = (size_t)t * m + k;
-            const uint32_t g = code_bytes == 1 ? (uint32_t)static_cast<const uint8_t*>(codes)[at] : (uint32_t)static_cast<const uint16_t*>(codes)[at];
-            z += S[((size_t)q * m + k) * b + min(g, (uint32_t)b - 1u)];
+        for (int k = lane; k < a.m; k += kWave) {
+            const size_t at = (size_t)t * a.m + k;
+            const uint32_t g = code_bytes == 1 ? (uint32_t)static_cast<const uint8_t*>(a.codes)[at] : (uint32_t)static_cast<const uint16_t*>(a.codes)[at];
+            z += a.S[((size_t)q * a.m + k) * a.b + min(g, (uint32_t)a.b - 1u)];
         }
 #pragma unroll
         for (int x = 1; x < kWave; x *= 2) z += __shfl_xor(z, x);
     }
     if (lane == 0) {
-        lse[q] = l;
-        loss[q] = has ? l - z : 0.0f;
+        a.lse[q] = l;
+        a.loss[q] = has ? l - z : 0.0f;
     }
 }
 
-struct LossArgs {
-    const void* codes;
-    const float* S;
-    const int* targets;        // NULL: the sums alone are asked for
-    long long N;
-    int B, m, b;
-    uint32_t share;            // items per workgroup
-    float2* partial;           // [gridDim.x][B]: (reference, sum), where the items are shared or no targets given
-    float *loss, *lse;
-    float scale;               // what scores are multiplied with: log2 e over the temperature
+// The same where the target is a teacher's list.
+struct TeacherLossArgs : LossArgs {
+    const int* items;
+    const float* scores;
+    int K;
+    float temperature;
 };
+template <typename Args>
+__device__ __forceinline__ uint32_t code_of(const Args& a, int code_bytes, int item, int k) {
+    const size_t at = (size_t)item * a.m + k;
+    const uint32_t g = code_bytes == 1 ? (uint32_t)static_cast<const uint8_t*>(a.codes)[at] : (uint32_t)static_cast<const uint16_t*>(a.codes)[at];
+    return min(g, (uint32_t)a.b - 1u);
+}
+__device__ __forceinline__ void finish_position(const TeacherLossArgs& a, float c, float s, int code_bytes, int q) {
+    const int lane = threadIdx.x % kWave;
+    const WaveTeacher t = wave_teacher(a.items, a.scores, q, a.K, a.N, a.temperature);
+    const float lse = log_sum(c, s);
+    double loss = 0.0;
+    if (t.any && lse != -__builtin_inff()) {
+        const double lse64 = lse == lse ? ((double)c + log2((double)s)) / kLog2eDouble : (double)lse;
+        for (int e = lane; e < a.K; e += kWave) {
+            const int item = a.items[(size_t)q * a.K + e];
+            if (item < 0 || item >= a.N) continue;
+            float z = 0.0f;
+            for (int k = 0; k < a.m; ++k) {
+                const float v = a.S[((size_t)q * a.m + k) * a.b + code_of(a, code_bytes, item, k)];
+                z = k == 0 ? v : z + v;
+            }
+            const double x = (double)a.scores[(size_t)q * a.K + e] / (double)a.temperature - t.top;
+            loss += entry_loss(t.weight(x), x - t.log_sum, z, a.temperature, lse64);
+        }
+#pragma unroll
+        for (int x = 1; x < kWave; x *= 2) loss += __shfl_xor(loss, x);
+    }
+    if (lane == 0) {
+        a.lse[q] = lse;
+        a.loss[q] = (float)(loss * (double)a.temperature * (double)a.temperature);
+    }
+}
 
 // The same with what an entropy and alternatives take.
 struct ProbsArgs {
@@ -342,14 +382,33 @@ __device__ __forceinline__ void sum_items(const Args& a) {
             }
         } else {
             for (int w = 1; w < kWaves; ++w) join_sums(sums.x, sums.y, stat[w * Q + wave].x, stat[w * Q + wave].y);
-            if (gridDim.x == 1 && a.targets) finish_position(sums.x, sums.y, a.codes, sizeof(CT), a.S, a.targets, a.N, a.m, a.b, q, a.loss, a.lse);
+            if (gridDim.x == 1) finish_position(a, sums.x, sums.y, sizeof(CT), q);
             else if (lane == 0) a.partial[(size_t)blockIdx.x * a.B + q] = sums;
         }
     }
 }
 
-template <int M, typename CT, int Q>
-__global__ __launch_bounds__(kThreads) void cross_entropy_kernel(LossArgs a) { sum_items<M, CT, Q, false>(a); }
+// (a list's finish, which one wave does once, may not take the registers that two workgroups a compute unit need: 64 a lane)
+template <int M, typename CT, typename Args> constexpr int waves_of() { return std::is_same<Args, LossArgs>::value || (M * (int)sizeof(CT) >= 16 && M != 64) ? 4 : 8; }
+template <int M, typename CT, int Q, typename Args>
+__global__ __launch_bounds__(kThreads, (waves_of<M, CT, Args>())) void cross_entropy_kernel(Args a) { sum_items<M, CT, Q, false>(a); }
+
+// One wave per position joins the shares' sums: 4 us, a launch.
+template <typename Args>
+__global__ __launch_bounds__(kWave) void cross_entropy_join_kernel(Args a, int shares, int code_bytes) {
+    const int q = blockIdx.x, lane = threadIdx.x;
+    float c = kLowest, s = 0.0f;
+    for (int i = lane; i < shares; i += kWave) {
+        const float2 t = a.partial[(size_t)i * a.B + q];
+        join_sums(c, s, t.x, t.y);
+    }
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) {
+        const float c2 = __shfl_xor(c, x), s2 = __shfl_xor(s, x);
+        join_sums(c, s, c2, s2);
+    }
+    finish_position(a, c, s, code_bytes, q);
+}
 
 struct BackArgs {
     const void* codes;
@@ -360,16 +419,20 @@ struct BackArgs {
     int B, m, b;
     int kept;                  // table entries whose sums a workgroup keeps (the others are other workgroups': blockIdx.z)
     uint32_t share;
-    uint64_t* partial;         // [gridDim.x][B][m][b], where the items are shared or there are weights
+    uint64_t* partial;         // [gridDim.x][B][m][b], where the items are shared
     float* dS;
-    // distillation: a position's gradient of the scores over its probabilities (0: it adds nothing); the teacher's probabilities
-    // are one more share of the sums, below 0
-    const float* weight;
     float scale;               // log2 e over the temperature
+};
+// The same where the target is a teacher's list: its probabilities are taken from the sums, whole multiples of 2^-62 as these are.
+struct TeacherBackArgs : BackArgs {
+    const int* items;
+    const float* scores;
+    int K;
+    float temperature;
+    float* weight;             // [B], written by the kernel: the gradient of the scores over p less the teacher's; 0: the position adds nothing
 };
 
 __device__ __forceinline__ bool has_target(const BackArgs& a, int q) {
-    if (a.weight) return a.weight[q] != 0.0f;
     const int t = a.targets[q];
     return t >= 0 && t < a.N && a.lse[q] != -__builtin_inff();
 }
@@ -377,12 +440,17 @@ __device__ __forceinline__ bool has_target(const BackArgs& a, int q) {
 // A table entry's sum of probabilities (multiples of 2^-62) to its gradient.
 __device__ __forceinline__ float gradient_of(const BackArgs& a, uint64_t sum, int q, int k, int j, int code_bytes) {
     if (!has_target(a, q)) return 0.0f;
-    if (a.weight) return a.lse[q] == a.lse[q] ? (float)((double)a.weight[q] * ((double)(int64_t)sum * 0x1p-62)) : a.lse[q];
     const size_t at = (size_t)a.targets[q] * a.m + k;
     const int g = code_bytes == 1 ? (int)static_cast<const uint8_t*>(a.codes)[at] : (int)static_cast<const uint16_t*>(a.codes)[at];
     // (a position whose scores hold a NaN has lse = NaN, of which its probabilities' whole numbers know nothing)
     const double p = a.lse[q] == a.lse[q] ? (double)sum * 0x1p-62 - (g == j ? 1.0 : 0.0) : (double)a.lse[q];
     return (float)((double)a.grad[q] * p);
+}
+
+__device__ __forceinline__ bool has_target(const TeacherBackArgs& a, int q) { return a.weight[q] != 0.0f; }
+__device__ __forceinline__ float gradient_of(const TeacherBackArgs& a, uint64_t sum, int q, int, int, int) {
+    if (!has_target(a, q)) return 0.0f;
+    return a.lse[q] == a.lse[q] ? (float)((double)a.weight[q] * ((double)(int64_t)sum * 0x1p-62)) : a.lse[q];
 }
 
 // grid = (shares of the items, groups of Q queries, ranges of table entries: one but for the largest tables, Q = C = 1).
@@ -395,9 +463,11 @@ __device__ __forceinline__ float gradient_of(const BackArgs& a, uint64_t sum, in
 // met by a P-th of the lanes at a time.  With fewer than four queries the C places of a query are summed at the end.
 // For the same reason neighbouring lanes start at different splits (one-byte sub-ids): a sub-id that a fifth of the items
 // share is met by a lane or two of an instruction instead of a fifth of them.
-template <int M, typename CT, int Q, int C>
-__global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackArgs a) {
+// A teacher's list: a wave a query makes its weights; the workgroups of the first share take them from their sums.
+template <int M, typename CT, int Q, int C, typename Args>
+__global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(Args a) {
     constexpr int P = Q * C, kUnitsBack = units_back_of<M, CT>();
+    constexpr bool kTeacher = std::is_same<Args, TeacherBackArgs>::value;
     extern __shared__ __align__(16) unsigned char smem[];
     const int E = entries<CT>(a.b);
     unsigned long long* sums = reinterpret_cast<unsigned long long*>(smem);
@@ -408,6 +478,28 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackAr
     const CT* codes = static_cast<const CT*>(a.codes);
     fill_tables<CT, Q>(table, a.S, q0, a.B, a.m, a.b);
     for (int i = threadIdx.x; i < a.kept * P; i += kThreads) sums[i] = 0;
+    if constexpr (kTeacher) {
+        __syncthreads();
+        const int r = threadIdx.x / kWave, q = q0 + r;
+        if (r < Q && q < a.B) {
+            const WaveTeacher t = wave_teacher(a.items, a.scores, q, a.K, a.N, a.temperature);
+            const bool live = t.any && a.lse[q] != -__builtin_inff(), odd = !(t.sum < __builtin_inf());
+            // (every workgroup of the query writes the same)
+            if (threadIdx.x % kWave == 0) a.weight[q] = !live ? 0.0f : odd ? __builtin_nanf("") : a.grad[q] * a.temperature;
+            if (live && !odd && blockIdx.x == 0) {
+                for (int e = threadIdx.x % kWave; e < a.K; e += kWave) {
+                    const int item = a.items[(size_t)q * a.K + e];
+                    if (item < 0 || item >= a.N) continue;
+                    const unsigned long long fixed = (unsigned long long)(t.weight((double)a.scores[(size_t)q * a.K + e] / (double)a.temperature - t.top) * 0x1p62);
+                    for (int k = 0; k < a.m; ++k) {
+                        const uint32_t place = (uint32_t)k * (uint32_t)E + code_of(a, sizeof(CT), item, k);
+                        if (place >= e0 && place < e1) atomicAdd(&sums[(place - e0) * P + r], 0ull - fixed);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
     float at[Q];                                               // exp2(z scale - at) is p 2^30
     bool any = false;
 #pragma unroll
@@ -514,7 +606,7 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackAr
 #pragma unroll
             for (int copy = 0; copy < C; ++copy) total += sums[i * P + copy * Q + r];
             const size_t out = ((size_t)q * a.m + k) * a.b + j;
-            if (gridDim.x > 1 || a.weight) a.partial[(size_t)blockIdx.x * a.B * a.m * a.b + out] = total;
+            if (gridDim.x > 1) a.partial[(size_t)blockIdx.x * a.B * a.m * a.b + out] = total;
             else a.dS[out] = gradient_of(a, total, q, k, j, sizeof(CT));
         }
     }
@@ -524,8 +616,8 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(BackAr
 // share (the sums are whole numbers: any order gives the same).  One thread alone would wait for many shares one after the
 // other: 5M items, one position 85 us for the gradient with one, 27 with eight; with few shares eight have nothing to do.
 constexpr int kJoinThreads = 256, kJoinLeads = 8;
-template <int LEADS>
-__global__ __launch_bounds__(kJoinThreads) void cross_entropy_backward_join_kernel(BackArgs a, int shares, int code_bytes) {
+template <int LEADS, typename Args>
+__global__ __launch_bounds__(kJoinThreads) void cross_entropy_backward_join_kernel(Args a, int shares, int code_bytes) {
     constexpr int kEntries = kJoinThreads / LEADS;
     __shared__ uint64_t part[LEADS][kEntries];
     const size_t entries = (size_t)a.B * a.m * a.b;
@@ -634,10 +726,86 @@ inline size_t backward_workspace(const Plan& p, int B, int m, int b) {
 template <int M, typename CT>
 constexpr bool fits(int Q, int P) { return sizeof(CT) == 2 || (size_t)M * 256 * (4 * Q + 8 * P) <= kMaxLds; }
 
-// cross_entropy.hip: the pass that a plan is for, and the gradient's.  The gradient's join takes `shares` shares (p.shares and, of a
-// distillation, the teacher's).
-__attribute__((visibility("hidden"))) hipError_t launch_loss(const Plan& p, const LossArgs& a, int code_bytes, hipStream_t st);
-__attribute__((visibility("hidden"))) hipError_t launch_backward(const Plan& p, const BackArgs& a, int code_bytes, int shares, hipStream_t st);
+template <int M, typename CT, int Q, typename Args>
+hipError_t go_loss(const Plan& p, const Args& a, hipStream_t st) {
+    hipError_t e = allow_lds(cross_entropy_kernel<M, CT, Q, Args>, p.lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((cross_entropy_kernel<M, CT, Q, Args>), dim3(p.shares, p.groups), dim3(kThreads), p.lds, st, a);
+    return hipGetLastError();
+}
+template <int M, typename CT, typename Args>
+hipError_t go_loss_q(const Plan& p, const Args& a, hipStream_t st) {
+    if constexpr (fits<M, CT>(4, 0)) { if (p.Q == 4) return go_loss<M, CT, 4>(p, a, st); }
+    if (p.Q == 2) return go_loss<M, CT, 2>(p, a, st);
+    return go_loss<M, CT, 1>(p, a, st);
+}
+
+template <int M, typename CT, int Q, int C, typename Args>
+hipError_t go_backward(const Plan& p, const Args& a, hipStream_t st) {
+    hipError_t e = allow_lds(cross_entropy_backward_kernel<M, CT, Q, C, Args>, p.lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((cross_entropy_backward_kernel<M, CT, Q, C, Args>), dim3(p.shares, p.groups, p.ranges), dim3(kThreads), p.lds, st, a);
+    return hipGetLastError();
+}
+// Whether a plan of the gradient can be Q queries with C copies: one-byte sub-ids of M splits take the most copies that fit.
+template <int M, typename CT>
+constexpr bool reached(int Q, int C) {
+    return M == 0 || sizeof(CT) == 2 || (fits<M, CT>(Q, Q * C) && (Q * C == 8 || !fits<M, CT>(Q, 2 * Q * C))) || (M == 64 && Q * C == 1);
+}
+template <int M, typename CT, typename Args>
+hipError_t go_backward_q(const Plan& p, const Args& a, hipStream_t st) {
+    if constexpr (reached<M, CT>(4, 2)) { if (p.Q == 4 && p.C == 2) return go_backward<M, CT, 4, 2>(p, a, st); }
+    if constexpr (reached<M, CT>(4, 1)) { if (p.Q == 4) return go_backward<M, CT, 4, 1>(p, a, st); }
+    if constexpr (reached<M, CT>(2, 4)) { if (p.Q == 2 && p.C == 4) return go_backward<M, CT, 2, 4>(p, a, st); }
+    if constexpr (reached<M, CT>(2, 2)) { if (p.Q == 2 && p.C == 2) return go_backward<M, CT, 2, 2>(p, a, st); }
+    if constexpr (reached<M, CT>(2, 1)) { if (p.Q == 2) return go_backward<M, CT, 2, 1>(p, a, st); }
+    if constexpr (reached<M, CT>(1, 8)) { if (p.C == 8) return go_backward<M, CT, 1, 8>(p, a, st); }
+    if constexpr (reached<M, CT>(1, 4)) { if (p.C == 4) return go_backward<M, CT, 1, 4>(p, a, st); }
+    if constexpr (reached<M, CT>(1, 2)) { if (p.C == 2) return go_backward<M, CT, 1, 2>(p, a, st); }
+    if constexpr (reached<M, CT>(1, 1)) return go_backward<M, CT, 1, 1>(p, a, st);
+    else return hipErrorInvalidValue;                          // (no plan asks for it)
+}
+
+template <typename CT, typename Args>
+hipError_t go_loss_m(const Plan& p, const Args& a, hipStream_t st) {
+    if (a.m == 4) return go_loss_q<4, CT>(p, a, st);
+    if (a.m == 8) return go_loss_q<8, CT>(p, a, st);
+    if (a.m == 16) return go_loss_q<16, CT>(p, a, st);
+    if (a.m == 2 && sizeof(CT) == 1) return go_loss_q<2, uint8_t>(p, a, st);
+    if (a.m == 32 && sizeof(CT) == 1) return go_loss_q<32, uint8_t>(p, a, st);
+    if (a.m == 64 && sizeof(CT) == 1) return go_loss_q<64, uint8_t>(p, a, st);
+    return go_loss_q<0, CT>(p, a, st);
+}
+template <typename CT, typename Args>
+hipError_t go_backward_m(const Plan& p, const Args& a, hipStream_t st) {
+    if (a.m == 4) return go_backward_q<4, CT>(p, a, st);
+    if (a.m == 8) return go_backward_q<8, CT>(p, a, st);
+    if (a.m == 16) return go_backward_q<16, CT>(p, a, st);
+    if (a.m == 2 && sizeof(CT) == 1) return go_backward_q<2, uint8_t>(p, a, st);
+    if (a.m == 32 && sizeof(CT) == 1) return go_backward_q<32, uint8_t>(p, a, st);
+    if (a.m == 64 && sizeof(CT) == 1) return go_backward_q<64, uint8_t>(p, a, st);
+    return go_backward_q<0, CT>(p, a, st);
+}
+
+// The pass that a plan is for with its join, and the gradient's.
+template <typename CT, typename Args>
+hipError_t launch_loss(const Plan& p, const Args& a, hipStream_t st) {
+    const hipError_t e = go_loss_m<CT>(p, a, st);
+    if (e != hipSuccess || p.shares == 1) return e;
+    hipLaunchKernelGGL(cross_entropy_join_kernel<Args>, dim3(a.B), dim3(kWave), 0, st, a, p.shares, (int)sizeof(CT));
+    return hipGetLastError();
+}
+template <typename CT, typename Args>
+hipError_t launch_backward(const Plan& p, const Args& a, hipStream_t st) {
+    const hipError_t e = go_backward_m<CT>(p, a, st);
+    if (e != hipSuccess || p.shares == 1) return e;
+    const size_t entries = (size_t)a.B * a.m * a.b;
+    if (p.shares > kJoinLeads)
+        hipLaunchKernelGGL((cross_entropy_backward_join_kernel<kJoinLeads, Args>), dim3((unsigned)ceil_div(entries, kJoinThreads / kJoinLeads)), dim3(kJoinThreads), 0, st, a, p.shares, (int)sizeof(CT));
+    else
+        hipLaunchKernelGGL((cross_entropy_backward_join_kernel<1, Args>), dim3((unsigned)ceil_div(entries, kJoinThreads)), dim3(kJoinThreads), 0, st, a, p.shares, (int)sizeof(CT));
+    return hipGetLastError();
+}
 
 }  // namespace subids
 }  // namespace head

@@ -16,9 +16,8 @@ namespace subids {
 namespace {
 
 // Two workgroups a compute unit, 64 registers a lane, but for rows of 16 and 32 bytes (as the loss has it, see plan_loss()).
-template <int M, typename CT> constexpr int waves_of() { return M * (int)sizeof(CT) >= 16 && M != 64 ? 4 : 8; }
 template <int M, typename CT, int Q>
-__global__ __launch_bounds__(kThreads, (waves_of<M, CT>())) void log_probs_kernel(ProbsArgs a) { sum_items<M, CT, Q, true>(a); }
+__global__ __launch_bounds__(kThreads, (waves_of<M, CT, ProbsArgs>())) void log_probs_kernel(ProbsArgs a) { sum_items<M, CT, Q, true>(a); }
 
 struct FinishArgs {
     const void* codes;

@@ -68,6 +68,38 @@ __device__ __forceinline__ Teacher<THREADS> teacher_of(const int* items, const f
     return t;
 }
 
+// The same list by one wave, which keeps no entry: the largest score over T, the sum of the exponentials and its logarithm.
+struct WaveTeacher {
+    double top, sum, log_sum;
+    bool any;
+    // of an entry's score over T less `top`
+    __device__ __forceinline__ double weight(double x) const { return x == -__builtin_inf() ? 0.0 : exp(x) / sum; }
+};
+__device__ __forceinline__ WaveTeacher wave_teacher(const int* items, const float* scores, int q, int K, long long N, float temperature) {
+    WaveTeacher t{-__builtin_inf(), 0.0, 0.0, false};
+    auto each = [&](auto f) {
+        for (int k = (int)threadIdx.x % kWave; k < K; k += kWave) {
+            const int item = items[(size_t)q * K + k];
+            if (item >= 0 && item < N) f((double)scores[(size_t)q * K + k] / (double)temperature);
+        }
+    };
+    each([&](double x) {
+        t.any |= x != -__builtin_inf();
+        t.top = fmax(t.top, x);
+    });
+    t.any = __any(t.any);
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) t.top = fmax(t.top, __shfl_xor(t.top, x));
+    if (!t.any) return t;
+    each([&](double x) {
+        if (x != -__builtin_inf()) t.sum += exp(x - t.top);
+    });
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) t.sum += __shfl_xor(t.sum, x);
+    t.log_sum = log(t.sum);
+    return t;
+}
+
 // What an entry adds to sum_k w_k (log w_k - log p_k), log p_k = score / T - lse.
 __device__ __forceinline__ double entry_loss(double weight, double log_weight, double score, float temperature, double lse) {
     return weight == 0.0 ? 0.0 : weight * (log_weight - (score / (double)temperature - lse));
