@@ -32,15 +32,11 @@ struct ListArgs {
     int few_items, few_groups;                         // default_few_kernel's tiles and workgroups, where it makes the gradient
 };
 
-// The list's items' scores in score[], sixteen lanes an entry.
+// The list's items' scores in score[].
 template <typename T>
 __device__ __forceinline__ void score_list(const ListArgs& a, int q, const int* item, double* score) {
-    const T* h = static_cast<const T*>(a.H) + (size_t)q * a.d;
-    for (int k = (int)threadIdx.x / 16; k < a.K; k += kListThreads / 16) {
-        if (item[k] < 0) continue;                             // (the same for the sixteen)
-        const double z = dot64(static_cast<const T*>(a.W) + (size_t)item[k] * a.d, h, a.d);
-        if (threadIdx.x % 16 == 0) score[k] = z;
-    }
+    score_rows<kListThreads>(static_cast<const T*>(a.W), static_cast<const T*>(a.H) + (size_t)q * a.d, a.d, a.K, [&](int k) { return (long long)item[k]; },
+                             [&](int k, bool there, double z) { if (there) score[k] = z; });
 }
 
 // grid = positions: joins the groups' sums, scores the list, adds the loss up.
@@ -59,7 +55,7 @@ __global__ __launch_bounds__(kListThreads) void default_distillation_join_kernel
     for (int x = 1; x < kWave; x *= 2) join_sums(c, s, __shfl_xor(c, x), __shfl_xor(s, x));
     if (lane == 0) sums[wave] = make_float2(c, s);
     const Teacher<kListThreads> t = teacher_of<kListThreads>(a.items, a.scores, q, a.K, a.N, a.temperature, part);
-    item[tid] = t.weight[0] != 0.0 ? t.item[0] : -1;           // (of the others no score is asked; NaN is not 0)
+    if (tid < a.K) item[tid] = t.weight[0] != 0.0 ? t.item[0] : -1;       // (of the others no score is asked; NaN is not 0)
     __syncthreads();
     score_list<T>(a, q, item, score);
     __syncthreads();
@@ -69,7 +65,7 @@ __global__ __launch_bounds__(kListThreads) void default_distillation_join_kernel
     const float lse = log_sum(c, s);
     const bool live = t.any && lse != -__builtin_inff();
     const double lse64 = lse == lse ? ((double)c + log2((double)s)) / kLog2eDouble : (double)lse;
-    double loss = live && item[tid] >= 0 ? entry_loss(t.weight[0], t.log_weight[0], score[tid], a.temperature, lse64) : 0.0;
+    double loss = live && tid < a.K && item[tid] >= 0 ? entry_loss(t.weight[0], t.log_weight[0], score[tid], a.temperature, lse64) : 0.0;
     loss = over_workgroup<kListThreads>(loss, part, [](double x, double y) { return x + y; });
     if (tid == 0) {
         a.lse[q] = lse;
@@ -88,20 +84,23 @@ __global__ __launch_bounds__(kListThreads) void default_list_kernel(ListArgs a) 
     const Teacher<kListThreads> t = teacher_of<kListThreads>(a.items, a.scores, q, a.K, a.N, a.temperature, part);
     const float lse = a.lse_in[q];
     const bool live = t.any && lse != -__builtin_inff() && a.grad[q] != 0.0f;
-    item[tid] = live ? t.item[0] : -1;
-    weight[tid] = t.weight[0];
+    if (tid < a.K) {
+        item[tid] = live ? t.item[0] : -1;
+        weight[tid] = t.weight[0];
+    }
     if (tid == 0) a.share[q] = live ? a.grad[q] * a.temperature : 0.0f;
     __syncthreads();
     score_list<T>(a, q, item, score);
     __syncthreads();
-    const int mine = item[tid] < 0 ? kNoItem : item[tid];
+    const int mine = tid >= a.K || item[tid] < 0 ? kNoItem : item[tid];
     // (what orders the entries: the workgroup over the item)
     auto order_of = [&](int i) { return (long long)(a.few_groups ? few_owner(i, a.few_items, a.few_groups) : 0) << 32 | i; };
-    order[tid] = order_of(mine);
+    if (tid < a.K) order[tid] = order_of(mine);
     __syncthreads();
     if (tid >= a.K) return;
     double all = 0.0;
     int rank = 0;
+#pragma unroll 8                                               // (their reads of LDS on their way together)
     for (int k = 0; k < a.K; ++k) {
         rank += order[k] < order[tid] || (order[k] == order[tid] && k < tid);
         if (order[k] == order[tid]) all += weight[k];

@@ -196,27 +196,21 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
     }
     auto log_prob = [&](double z) { return lse == -__builtin_inff() ? lse : (float)(z / (double)a.temperature - (double)lse); };
     const T *W = static_cast<const T*>(a.W), *h = static_cast<const T*>(a.H) + (size_t)q * a.d;
-    for (int i = tid / 16; i < a.n; i += THREADS / 16) {
-        const int item = a.items[(size_t)q * a.n + i];
-        const bool there = item >= 0 && item < a.N;            // (the same for the sixteen)
-        const double z = there ? dot64(W + (size_t)item * a.d, h, a.d) : 0.0;
-        if (tid % 16 == 0) a.log_probs[(size_t)q * a.n + i] = there ? log_prob(z) : 0.0f;
-    }
+    score_rows<THREADS>(W, h, a.d, a.n, [&](int i) { const int item = a.items[(size_t)q * a.n + i]; return item < a.N ? (long long)item : -1LL; },
+                        [&](int i, bool there, double z) { a.log_probs[(size_t)q * a.n + i] = there ? log_prob(z) : 0.0f; });
     if (a.K == 0) return;
     uint64_t least;
     const int n = cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem);
-    for (int i = tid / 16; i < n; i += THREADS / 16) {
-        const double z = dot64(W + (size_t)item_of(kept[i]) * a.d, h, a.d);
-        if (tid % 16 == 0) score[i] = z;
-    }
+    score_rows<THREADS>(W, h, a.d, n, [&](int i) { return (long long)item_of(kept[i]); }, [&](int i, bool, double z) { score[i] = z; });
     __syncthreads();
     for (int at = tid; at < n; at += THREADS) {
         // (a NaN, of which no rank comes, is taken for the lowest)
         const double mine = score[at] == score[at] ? score[at] : -__builtin_inf();
         int rank = 0;
+#pragma unroll 8                                               // (their reads of LDS on their way together)
         for (int i = 0; i < n; ++i) {
             const double other = score[i] == score[i] ? score[i] : -__builtin_inf();
-            rank += other > mine || (other == mine && item_of(kept[i]) < item_of(kept[at]));
+            rank += (other > mine) | ((other == mine) & (kept[i] << 32 > kept[at] << 32));          // (the lower id's key is the larger)
         }
         if (rank < a.K) {
             a.top_items[(size_t)q * a.K + rank] = (int)item_of(kept[at]);

@@ -105,6 +105,7 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
     for (int at = tid; at < n; at += THREADS) {
         const uint64_t mine = kept[at];
         int rank = 0;
+#pragma unroll 8                                               // (their reads of LDS on their way together)
         for (int i = 0; i < n; ++i) rank += kept[i] > mine;
         if (rank < a.K) {
             a.top_items[(size_t)q * a.K + rank] = (int)item_of(mine);

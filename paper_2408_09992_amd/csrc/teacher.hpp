@@ -105,22 +105,42 @@ __device__ __forceinline__ double entry_loss(double weight, double log_weight, d
     return weight == 0.0 ? 0.0 : weight * (log_weight - (score / (double)temperature - lse));
 }
 
-// The sum of the products of two rows of d elements, in 64 bits (those of 16-bit elements are exact, and nearly always their sum), by sixteen
-// lanes of a wave; all sixteen have it.  Rows are multiples of 16 bytes, and aligned.
+// Rows of W by one query in 64 bits (products of 16-bit elements are exact, and nearly always their sum): sums of d products by sixteen lanes of a wave, which
+// all sixteen get, of two rows at once, whose loads are on their way together.  Rows are multiples of 16 bytes, and aligned.
 template <typename T>
-__device__ __forceinline__ double dot64(const T* x, const T* y, int d) {
+__device__ __forceinline__ void dots64(const T* x0, const T* x1, const T* y, int d, double& sum0, double& sum1) {
     constexpr int kOf = 16 / (int)sizeof(T);
     typedef T Piece __attribute__((ext_vector_type(kOf)));
-    double sum = 0.0;
+    sum0 = sum1 = 0.0;
 #pragma unroll 4
     for (int i = (int)threadIdx.x % 16; i < d / kOf; i += 16) {
-        const Piece u = reinterpret_cast<const Piece*>(x)[i], v = reinterpret_cast<const Piece*>(y)[i];
+        const Piece u0 = reinterpret_cast<const Piece*>(x0)[i], u1 = reinterpret_cast<const Piece*>(x1)[i], v = reinterpret_cast<const Piece*>(y)[i];
 #pragma unroll
-        for (int e = 0; e < kOf; ++e) sum = fma((double)(float)u[e], (double)(float)v[e], sum);
+        for (int e = 0; e < kOf; ++e) {
+            sum0 = fma((double)(float)u0[e], (double)(float)v[e], sum0);
+            sum1 = fma((double)(float)u1[e], (double)(float)v[e], sum1);
+        }
     }
 #pragma unroll
-    for (int w = 1; w < 16; w *= 2) sum += __shfl_xor(sum, w);
-    return sum;
+    for (int w = 1; w < 16; w *= 2) {
+        sum0 += __shfl_xor(sum0, w);
+        sum1 += __shfl_xor(sum1, w);
+    }
+}
+// The same of the rows item(0 .. n - 1) (below 0: none), by a workgroup of THREADS; put(i, sum) by one lane each.
+template <int THREADS, typename T, typename Item, typename Put>
+__device__ __forceinline__ void score_rows(const T* W, const T* h, int d, int n, Item item, Put put) {
+    constexpr int kRows = THREADS / 16;
+    for (int i = (int)threadIdx.x / 16; i < n; i += 2 * kRows) {
+        const bool two = i + kRows < n;
+        const long long r0 = item(i), r1 = two ? item(i + kRows) : -1;       // (the same for the sixteen)
+        double s0, s1;
+        if (r0 >= 0 || r1 >= 0) dots64(W + (size_t)(r0 >= 0 ? r0 : r1) * d, W + (size_t)(r1 >= 0 ? r1 : r0) * d, h, d, s0, s1);
+        if (threadIdx.x % 16 == 0) {
+            put(i, r0 >= 0, s0);
+            if (two) put(i + kRows, r1 >= 0, s1);
+        }
+    }
 }
 
 }  // namespace head
