@@ -196,12 +196,19 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
     }
     auto log_prob = [&](double z) { return lse == -__builtin_inff() ? lse : (float)(z / (double)a.temperature - (double)lse); };
     const T *W = static_cast<const T*>(a.W), *h = static_cast<const T*>(a.H) + (size_t)q * a.d;
-    score_rows<THREADS>(W, h, a.d, a.n, [&](int i) { const int item = a.items[(size_t)q * a.n + i]; return item < a.N ? (long long)item : -1LL; },
-                        [&](int i, bool there, double z) { a.log_probs[(size_t)q * a.n + i] = there ? log_prob(z) : 0.0f; });
-    if (a.K == 0) return;
     uint64_t least;
-    const int n = cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem);
-    score_rows<THREADS>(W, h, a.d, n, [&](int i) { return (long long)item_of(kept[i]); }, [&](int i, bool, double z) { score[i] = z; });
+    const int n = a.K ? cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem) : 0;
+    // (the given items and the candidates at once: a row's way here is most of what either takes)
+    score_rows<THREADS>(W, h, a.d, a.n + n,
+                        [&](int i) {
+                            const int item = i < a.n ? a.items[(size_t)q * a.n + i] : (int)item_of(kept[i - a.n]);
+                            return item < a.N ? (long long)item : -1LL;
+                        },
+                        [&](int i, bool there, double z) {
+                            if (i < a.n) a.log_probs[(size_t)q * a.n + i] = there ? log_prob(z) : 0.0f;
+                            else score[i - a.n] = z;
+                        });
+    if (a.K == 0) return;
     __syncthreads();
     for (int at = tid; at < n; at += THREADS) {
         // (a NaN, of which no rank comes, is taken for the lowest)
