@@ -34,7 +34,7 @@ extern "C" {
  *   lse            out  float [B]
  *   top_items      out  int32 [B][K]       by score descending, then id ascending, as pq_score_topk() ranks them.  K may be 0 (top_items and
  *   top_log_probs  out  float [B][K]         top_log_probs may be NULL then)
- * Table entries may be -inf (a sub-id out of play): items of score -inf have the log-probability -inf and come last, by id.  Of a position
+ * Table entries may be -inf (a sub-id out of play; entries below -1e32 count as that): items of score -inf have the log-probability -inf and come last, by id.  Of a position
  * that meets a NaN or +inf every number is NaN, top_items are different items of the catalogue in no particular order; no other position is touched by it.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, B, m, b < 1; n, K < 0; b too large; K > N; N >= 2^31; T no positive number), PQ_ERR_UNSUPPORTED
  *         (K > PQ_MAX_K, n > 65536, T out of its range, and as pq_cross_entropy()), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.

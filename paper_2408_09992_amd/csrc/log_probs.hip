@@ -80,6 +80,10 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
     if (a.ranked) {
         // (the ranking took scores of -inf for sums of large numbers: fewer than K others mean that K - 1 ids hold enough of them, the lowest ones)
         __shared__ int below[PQ_MAX_K];
+        if (lse != lse) {                                      // (its ids are some items)
+            for (int i = tid; i < a.K; i += THREADS) a.top_log_probs[(size_t)q * a.K + i] = lse;
+            return;
+        }
         const float last = a.ranked[(size_t)q * a.K + a.K - 1];
         for (int i = tid; i < a.K; i += THREADS) {
             const float z = a.ranked[(size_t)q * a.K + i];

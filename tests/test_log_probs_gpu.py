@@ -163,6 +163,30 @@ def test_sub_ids_out_of_play(pq, wide):
     check(pq, codes, S, items, 200)
 
 
+@pytest.mark.parametrize("N,m,b,B,wide", [(16_000, 4, 256, 5, False), (600_000, 16, 256, 110, False), (1_100_000, 8, 300, 130, True)])
+def test_sub_ids_out_of_play_where_scores_go_to_lists(pq, N, m, b, B, wide):
+    codes, S, items = draw_codes(N, m, b, B, 2, seed=N, wide=wide)
+    S[0, 1, 5:] = -np.inf
+    S[1, 2] = -np.inf
+    S[2, 0, ::2] = -np.inf
+    S[3, :2, 1:] = -np.inf                                      # a few items: fewer than asked for
+    S[4, 0, 3] = -1e30                                          # a mask that is a number
+    check(pq, codes, S, items, 60)
+
+
+@pytest.mark.parametrize("N", [10_000, 30_000])
+def test_a_nan_beside_sub_ids_out_of_play(pq, N):
+    codes, S, items = draw_codes(N, 4, 256, 3, 2, seed=N)
+    clean = call(pq, codes, S, items, 100)                       # (of as many positions: what is summed in which order goes by the shape)
+    S[1, :2, 1:] = -np.inf
+    S[1, 3, ::3] = float("nan")
+    got = call(pq, codes, S, items, 100)
+    for a, b in zip(got, clean):
+        assert torch.equal(a[::2], b[::2])
+    ids = got[3][1].tolist()
+    assert got[2][1].isnan() and got[4][1].isnan().all() and len(set(ids)) == 100 and all(0 <= i < N for i in ids)
+
+
 def test_positions_that_are_all_the_lowest_number(pq):
     codes, S, items = draw_codes(20_000, 4, 256, 3, 2, seed=5)
     S[1] = -1e30
