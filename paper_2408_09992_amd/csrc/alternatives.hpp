@@ -136,17 +136,23 @@ __device__ __forceinline__ uint64_t cut(const H& held, int keep, int most, Selec
     constexpr int kWaves = THREADS / kWave, kOwn = kBins / THREADS;
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     if (held.n <= keep) return 0;
-    uint64_t low = ~0ull, high = 0;
+    // The range to look in: up to the largest key, and from the least of the largest keys that groups of lanes have, if there are `keep` groups, which
+    // hold a key each.  (Counted over the whole range, most of a long list's keys would queue up at a few bins.)
+    const int group = held.n < THREADS ? 1 : keep <= THREADS / 64 ? 64 : keep <= THREADS / 16 ? 16 : keep <= THREADS / 4 ? 4 : 1;
+    uint64_t low = 0, high = 0;
+    const bool grouped = held.n >= THREADS && keep <= THREADS;
+    if (!grouped) low = ~0ull;
     held.each([&](uint64_t k) {
-        low = k < low ? k : low;
+        if (!grouped) low = k < low ? k : low;
         high = k > high ? k : high;
     });
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) mem.histogram[tid + i * THREADS] = 0;
+    if (grouped) low = high;
 #pragma unroll
     for (int x = 1; x < kWave; x *= 2) {
         const uint64_t l = __shfl_xor(low, x), h = __shfl_xor(high, x);
-        low = l < low ? l : low;
+        low = grouped && x < group ? (l > low ? l : low) : (l < low ? l : low);
         high = h > high ? h : high;
     }
     if (lane == 0) { mem.part[wave][0] = low; mem.part[wave][1] = high; }
