@@ -196,6 +196,7 @@ __device__ __forceinline__ void finish_position(const TeacherLossArgs& a, float 
             const int item = a.items[(size_t)q * a.K + e];
             if (item < 0 || item >= a.N) continue;
             float z = 0.0f;
+#pragma unroll 4                                               // (a chain of additions, but not of loads)
             for (int k = 0; k < a.m; ++k) {
                 const float v = a.S[((size_t)q * a.m + k) * a.b + code_of(a, code_bytes, item, k)];
                 z = k == 0 ? v : z + v;

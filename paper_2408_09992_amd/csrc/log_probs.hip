@@ -39,6 +39,7 @@ struct FinishArgs {
 // Eq. 5's chain of one item, from the tables where they lie.
 __device__ __forceinline__ float score_of_item(const FinishArgs& a, int q, int item) {
     float z = 0.0f;
+#pragma unroll 8                                               // (a chain of additions, but not of loads)
     for (int k = 0; k < a.m; ++k) {
         const size_t at = (size_t)item * a.m + k;
         const uint32_t g = a.code_bytes == 1 ? (uint32_t)static_cast<const uint8_t*>(a.codes)[at] : (uint32_t)static_cast<const uint16_t*>(a.codes)[at];
