@@ -98,12 +98,22 @@ __global__ __launch_bounds__(kListThreads) void default_list_kernel(ListArgs a) 
     if (tid < a.K) order[tid] = order_of(mine);
     __syncthreads();
     if (tid >= a.K) return;
-    double all = 0.0;
-    int rank = 0;
-#pragma unroll 8                                               // (their reads of LDS on their way together)
+    const long long own = order[tid];
+    int rank = 0, alike = 0;
+#pragma unroll 8                                               // (reads of LDS on their way together, and no branch between them)
     for (int k = 0; k < a.K; ++k) {
-        rank += order[k] < order[tid] || (order[k] == order[tid] && k < tid);
-        if (order[k] == order[tid]) all += weight[k];
+        const long long other = order[k];
+        rank += (other < own) | ((other == own) & (k < tid));
+        alike += other == own;
+    }
+    double all = weight[tid];
+    if (alike > 1 && mine != kNoItem) {
+        all = 0.0;
+#pragma unroll 8
+        for (int k = 0; k < a.K; ++k) {
+            const double w = weight[k];
+            all += order[k] == own ? w : 0.0;
+        }
     }
     const size_t at = (size_t)q * a.K + rank;
     a.entry_items[at] = mine;

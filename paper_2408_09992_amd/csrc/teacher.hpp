@@ -112,13 +112,26 @@ __device__ __forceinline__ void dots64(const T* x0, const T* x1, const T* y, int
     constexpr int kOf = 16 / (int)sizeof(T);
     typedef T Piece __attribute__((ext_vector_type(kOf)));
     sum0 = sum1 = 0.0;
-#pragma unroll 4
-    for (int i = (int)threadIdx.x % 16; i < d / kOf; i += 16) {
-        const Piece u0 = reinterpret_cast<const Piece*>(x0)[i], u1 = reinterpret_cast<const Piece*>(x1)[i], v = reinterpret_cast<const Piece*>(y)[i];
+    constexpr int kAtOnce = 4;                                  // pieces of each row that a lane has on their way
+    const int pieces = d / kOf;
+    for (int first = (int)threadIdx.x % 16; first < pieces; first += 16 * kAtOnce) {
+        Piece u0[kAtOnce], u1[kAtOnce], v[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < kOf; ++e) {
-            sum0 = fma((double)(float)u0[e], (double)(float)v[e], sum0);
-            sum1 = fma((double)(float)u1[e], (double)(float)v[e], sum1);
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int i = min(first + 16 * j, pieces - 1);
+            u0[j] = reinterpret_cast<const Piece*>(x0)[i];
+            u1[j] = reinterpret_cast<const Piece*>(x1)[i];
+            v[j] = reinterpret_cast<const Piece*>(y)[i];
+        }
+        __builtin_amdgcn_sched_barrier(0);                     // (not one piece after the other)
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (first + 16 * j >= pieces) break;
+#pragma unroll
+            for (int e = 0; e < kOf; ++e) {
+                sum0 = fma((double)(float)u0[j][e], (double)(float)v[j][e], sum0);
+                sum1 = fma((double)(float)u1[j][e], (double)(float)v[j][e], sum1);
+            }
         }
     }
 #pragma unroll
