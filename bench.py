@@ -703,13 +703,13 @@ def matrix_cores_mode(args):
                       "eq4": eq4, "default_scorer": default}))
 
 
-def training_mode(args):
-    """The scoring head's training calls and the four-bit scores on the cases of perf/operators.py: GPU time of a pass (HIP
-    events around back-to-back passes, median of three), its bytes and operations per second."""
+def operators_mode(file, metric, pick, key):
+    """The cases of a file under perf/: GPU time of a pass (HIP events around back-to-back passes, median of three), its bytes and
+    operations per second; the value is the operations per second of the fastest case whose name begins with `pick`."""
     import importlib.util
     import torch
 
-    spec = importlib.util.spec_from_file_location("operators", os.path.join(ROOT, "perf", "operators.py"))
+    spec = importlib.util.spec_from_file_location(file, os.path.join(ROOT, "perf", file + ".py"))
     ops = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(ops)
     ops.own = True
@@ -729,13 +729,23 @@ def training_mode(args):
         n = max(3, min(500, int(50_000 / timed(3))))
         us, work = sorted(timed(n) for _ in range(3))[1], ops.work(case)
         points.append({"case": case["name"], "us_per_pass": us, "GBps": work["bytes"] / us / 1e3, "TFLOPs": work["flops"] / us / 1e6})
-        print(f"{case['name']:32s} {us:9.1f} us {points[-1]['GBps']:8.0f} GB/s {points[-1]['TFLOPs']:8.1f} TFLOP/s", file=sys.stderr, flush=True)
+        print(f"{case['name']:36s} {us:9.1f} us {points[-1]['GBps']:8.0f} GB/s {points[-1]['TFLOPs']:8.1f} TFLOP/s", file=sys.stderr, flush=True)
         del state
         torch.cuda.empty_cache()
-    dense = max((p for p in points if p["case"].startswith("dense")), key=lambda p: p["TFLOPs"])
-    print(json.dumps({"metric": "dense cross entropy with its gradients, operations/s", "value": dense["TFLOPs"], "unit": "TFLOP/s", "n_gpus": 1,
-                      "higher_is_better": True, "vs_baseline": None, "dtype": "bf16", "data": "synthetic", "config": {"workload": dense["case"]},
-                      "training": points}))
+    best = max((p for p in points if p["case"].startswith(pick)), key=lambda p: p["TFLOPs"])
+    print(json.dumps({"metric": metric, "value": best["TFLOPs"], "unit": "TFLOP/s", "n_gpus": 1,
+                      "higher_is_better": True, "vs_baseline": None, "dtype": "bf16", "data": "synthetic", "config": {"workload": best["case"]},
+                      key: points}))
+
+
+def training_mode(args):
+    """The scoring head's training calls and the four-bit scores."""
+    operators_mode("operators", "dense cross entropy with its gradients, operations/s", "dense", "training")
+
+
+def probabilities_mode(args):
+    """Log-probabilities with entropy and the likeliest items, and distillation with its gradients."""
+    operators_mode("more_operators", "log-probabilities by the default scorer, operations/s", "probs dense", "probabilities")
 
 
 def breakdown_mode(args):
@@ -915,6 +925,8 @@ def main():
                     "against the scalar kernels, over batch sizes")
     ap.add_argument("--training", action="store_true", help="cross entropy of the catalogue with its gradients, by sub-ids and by the default "
                     "scorer, Eq. 4's gradients and scores from four bits, on the cases of perf/operators.py")
+    ap.add_argument("--probabilities", action="store_true", help="log-probabilities of given items with entropy and the likeliest items, and distillation "
+                    "from a teacher's lists, by sub-ids and by the default scorer, on the cases of perf/more_operators.py")
     ap.add_argument("--yardsticks", action="store_true", help="machine yardsticks: empty launch, plain streaming read, "
                     "random gathers from LDS")
     ap.add_argument("--rules", action="store_true", help="both sides of the rules that choose a scan, around each of their lines")
@@ -943,6 +955,9 @@ def main():
         return
     if args.training:
         training_mode(args)
+        return
+    if args.probabilities:
+        probabilities_mode(args)
         return
     if args.yardsticks:
         yardsticks_mode(args)

@@ -331,6 +331,19 @@ def test_from_teacher_to_student(pq):
     assert abs(drop - step * dH.double().pow(2).sum().item()) <= 0.05 * drop
 
 
+def test_the_example_runs(pq):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_and_serve.py")
+    spec = importlib.util.spec_from_file_location("train_and_serve", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    W, H, _, _, _ = draw_dense(1003, 32, 20, 1, "f32", seed=14)
+    losses, alike, log_probs, entropy = example.distillation(W, H, torch.arange(20, dtype=torch.int32, device="cuda"), 32, 4, 256, 3, 5, 2.0, lambda line: None)
+    assert len(losses) == 3 and np.isfinite(losses).all() and 0 <= alike <= 1
+    assert log_probs.isfinite().all() and (log_probs <= 0).all() and (entropy >= 0).all() and (entropy <= np.log(1003) * (1 + 1e-6)).all()
+
+
 def test_embeddings_beyond_32_bits_of_offset(pq):
     N, d, B = 4_300_000, 512, 2                                  # 4.4 GB of W and of dW
     W = torch.zeros((N, d), dtype=torch.bfloat16, device="cuda")
