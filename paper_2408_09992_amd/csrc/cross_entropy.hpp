@@ -188,10 +188,9 @@ __device__ __forceinline__ uint32_t code_of(const Args& a, int code_bytes, int i
 __device__ __forceinline__ void finish_position(const TeacherLossArgs& a, float c, float s, int code_bytes, int q) {
     const int lane = threadIdx.x % kWave;
     const WaveTeacher t = wave_teacher(a.items, a.scores, q, a.K, a.N, a.temperature);
-    const float lse = log_sum(c, s);
+    const double lse = log_sum64(c, s);
     double loss = 0.0;
-    if (t.any && lse != -__builtin_inff()) {
-        const double lse64 = lse == lse ? ((double)c + log2((double)s)) / kLog2eDouble : (double)lse;
+    if (t.any && lse != -__builtin_inf()) {
         for (int e = lane; e < a.K; e += kWave) {
             const int item = a.items[(size_t)q * a.K + e];
             if (item < 0 || item >= a.N) continue;
@@ -202,13 +201,13 @@ __device__ __forceinline__ void finish_position(const TeacherLossArgs& a, float 
                 z = k == 0 ? v : z + v;
             }
             const double x = (double)a.scores[(size_t)q * a.K + e] / (double)a.temperature - t.top;
-            loss += entry_loss(t.weight(x), x - t.log_sum, z, a.temperature, lse64);
+            loss += entry_loss(t.weight(x), x - t.log_sum, z, a.temperature, lse);
         }
 #pragma unroll
         for (int x = 1; x < kWave; x *= 2) loss += __shfl_xor(loss, x);
     }
     if (lane == 0) {
-        a.lse[q] = lse;
+        a.lse[q] = (float)lse;
         a.loss[q] = (float)(loss * (double)a.temperature * (double)a.temperature);
     }
 }

@@ -62,13 +62,12 @@ __global__ __launch_bounds__(kListThreads) void default_distillation_join_kernel
     c = sums[0].x; s = sums[0].y;
 #pragma unroll
     for (int w = 1; w < kListWaves; ++w) join_sums(c, s, sums[w].x, sums[w].y);
-    const float lse = log_sum(c, s);
-    const bool live = t.any && lse != -__builtin_inff();
-    const double lse64 = lse == lse ? ((double)c + log2((double)s)) / kLog2eDouble : (double)lse;
-    double loss = live && tid < a.K && item[tid] >= 0 ? entry_loss(t.weight[0], t.log_weight[0], score[tid], a.temperature, lse64) : 0.0;
+    const double lse = log_sum64(c, s);
+    const bool live = t.any && lse != -__builtin_inf();
+    double loss = live && tid < a.K && item[tid] >= 0 ? entry_loss(t.weight[0], t.log_weight[0], score[tid], a.temperature, lse) : 0.0;
     loss = over_workgroup<kListThreads>(loss, part, [](double x, double y) { return x + y; });
     if (tid == 0) {
-        a.lse[q] = lse;
+        a.lse[q] = (float)lse;
         a.loss[q] = (float)(loss * (double)a.temperature * (double)a.temperature);
     }
 }

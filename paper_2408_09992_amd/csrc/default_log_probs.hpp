@@ -189,12 +189,12 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
     __syncthreads();
     c = sums[0].x; s = sums[0].y; t = sums[0].z;
     for (int w = 1; w < THREADS / kWave; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
-    const float lse = log_sum(c, s);
+    const double lse = log_sum64(c, s);
     if (tid == 0) {
-        a.lse[q] = lse;
+        a.lse[q] = (float)lse;
         a.entropy[q] = entropy_of(s, t);
     }
-    auto log_prob = [&](double z) { return lse == -__builtin_inff() ? lse : (float)(z / (double)a.temperature - (double)lse); };
+    auto log_prob = [&](double z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(z / (double)a.temperature - lse); };
     const T *W = static_cast<const T*>(a.W), *h = static_cast<const T*>(a.H) + (size_t)q * a.d;
     uint64_t least;
     const int n = a.K ? cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem) : 0;

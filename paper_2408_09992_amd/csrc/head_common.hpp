@@ -14,6 +14,7 @@ namespace head {
 constexpr int kWave = 64;
 constexpr int kCUs = 256;                            // MI355X; only sizes grids and workspaces
 constexpr size_t kMaxLds = 160 * 1024;               // LDS per workgroup on gfx950
+constexpr double kLog2eDouble = 1.4426950408889634;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // v_exp_f32: 1 ulp, results below 2^-126 become 0
@@ -61,11 +62,16 @@ __device__ __forceinline__ void raise_reference(float& c, float& s, float& t, fl
 }
 // - sum_i p log p in nats: log p = ln 2 (x - log2 s).  0 where no score counts.
 __device__ __forceinline__ float entropy_of(float s, float t) {
-    return s == 0.0f ? 0.0f : s < __builtin_inff() ? (float)fmax((log2((double)s) - (double)t / (double)s) / 1.4426950408889634, 0.0) : __builtin_nanf("");
+    return s == 0.0f ? 0.0f : s < __builtin_inff() ? (float)fmax((log2((double)s) - (double)t / (double)s) / kLog2eDouble, 0.0) : __builtin_nanf("");
 }
 // log-sum: -inf where no score counts, NaN where one is NaN, +inf or counts as that.
 __device__ __forceinline__ float log_sum(float c, float s) {
     return s == 0.0f ? -__builtin_inff() : s < __builtin_inff() ? (c + __log2f(s)) * kLn2 : __builtin_nanf("");
+}
+
+// The same in 64 bits: reference and logarithm of some 20 each lose no bits to their sum.
+__device__ __forceinline__ double log_sum64(float c, float s) {
+    return s == 0.0f ? -__builtin_inf() : s < __builtin_inff() ? ((double)c + log2((double)s)) / kLog2eDouble : __builtin_nan("");
 }
 
 template <typename F>
@@ -75,7 +81,6 @@ inline hipError_t allow_lds(F* kernel, size_t bytes) {
 }
 
 // Temperatures and how many items a position may be given (pqtopk_probs.h).
-constexpr double kLog2eDouble = 1.4426950408889634;
 constexpr int kMostGiven = 65536;
 inline bool temperature_fits(float t) { return t >= 1e-4f && t <= 1e4f; }
 

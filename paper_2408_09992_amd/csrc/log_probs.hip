@@ -67,12 +67,12 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
     __syncthreads();
     c = sums[0].x; s = sums[0].y; t = sums[0].z;
     for (int w = 1; w < THREADS / kWave; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
-    const float lse = log_sum(c, s);
+    const double lse = log_sum64(c, s);
     if (tid == 0) {
-        a.lse[q] = lse;
+        a.lse[q] = (float)lse;
         a.entropy[q] = entropy_of(s, t);
     }
-    auto log_prob = [&](float z) { return lse == -__builtin_inff() ? lse : (float)((double)z / (double)a.temperature - (double)lse); };
+    auto log_prob = [&](float z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)((double)z / (double)a.temperature - lse); };
     for (int i = tid; i < a.n; i += THREADS) {
         const int item = a.items[(size_t)q * a.n + i];
         a.log_probs[(size_t)q * a.n + i] = item >= 0 && item < a.N ? log_prob(score_of_item(a, q, item)) : 0.0f;
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
         // (the ranking took scores of -inf for sums of large numbers: fewer than K others mean that K - 1 ids hold enough of them, the lowest ones)
         __shared__ int below[PQ_MAX_K];
         if (lse != lse) {                                      // (its ids are some items)
-            for (int i = tid; i < a.K; i += THREADS) a.top_log_probs[(size_t)q * a.K + i] = lse;
+            for (int i = tid; i < a.K; i += THREADS) a.top_log_probs[(size_t)q * a.K + i] = (float)lse;
             return;
         }
         const float last = a.ranked[(size_t)q * a.K + a.K - 1];
