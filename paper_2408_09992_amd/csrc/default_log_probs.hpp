@@ -177,6 +177,7 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
     __shared__ uint64_t kept[kMostKept];
     __shared__ double score[kMostKept];
     __shared__ float4 sums[THREADS / kWave];
+    __shared__ double lse_of_all;
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     float c = kLowest, s = 0.0f, t = 0.0f;
     for (int i = tid; i < a.groups; i += THREADS) {
@@ -189,15 +190,17 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
     __syncthreads();
     c = sums[0].x; s = sums[0].y; t = sums[0].z;
     for (int w = 1; w < THREADS / kWave; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
-    const double lse = log_sum64(c, s);
-    if (tid == 0) {
-        a.lse[q] = (float)lse;
+    if (tid == 0) {                                            // (64-bit logarithms, by one wave: the others go on to the list)
+        lse_of_all = log_sum64(c, s);
+        a.lse[q] = (float)lse_of_all;
         a.entropy[q] = entropy_of(s, t);
     }
-    auto log_prob = [&](double z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(z / (double)a.temperature - lse); };
     const T *W = static_cast<const T*>(a.W), *h = static_cast<const T*>(a.H) + (size_t)q * a.d;
     uint64_t least;
     const int n = a.K ? cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem) : 0;
+    __syncthreads();
+    const double lse = lse_of_all;
+    auto log_prob = [&](double z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(z / (double)a.temperature - lse); };
     // (the given items and the candidates at once: a row's way here is most of what either takes)
     score_rows<THREADS>(W, h, a.d, a.n + n,
                         [&](int i) {

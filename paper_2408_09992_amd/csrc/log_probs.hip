@@ -55,6 +55,7 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
     __shared__ SelectMemory<THREADS> mem;
     __shared__ uint64_t kept[kMostKept];
     __shared__ float4 sums[THREADS / kWave];
+    __shared__ double lse_of_all;
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     float c = kLowest, s = 0.0f, t = 0.0f;
     for (int i = tid; i < a.shares; i += THREADS) {
@@ -67,11 +68,15 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
     __syncthreads();
     c = sums[0].x; s = sums[0].y; t = sums[0].z;
     for (int w = 1; w < THREADS / kWave; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
-    const double lse = log_sum64(c, s);
-    if (tid == 0) {
-        a.lse[q] = (float)lse;
+    if (tid == 0) {                                            // (64-bit logarithms, by one wave: the others go on to the list)
+        lse_of_all = log_sum64(c, s);
+        a.lse[q] = (float)lse_of_all;
         a.entropy[q] = entropy_of(s, t);
     }
+    uint64_t least;
+    const int n = a.lists.keep ? cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem) : 0;
+    __syncthreads();
+    const double lse = lse_of_all;
     auto log_prob = [&](float z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)((double)z / (double)a.temperature - lse); };
     for (int i = tid; i < a.n; i += THREADS) {
         const int item = a.items[(size_t)q * a.n + i];
@@ -105,8 +110,6 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
         }
         return;
     }
-    uint64_t least;
-    const int n = cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem);
     for (int at = tid; at < n; at += THREADS) {
         const uint64_t mine = kept[at];
         int rank = 0;
