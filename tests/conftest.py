@@ -1,3 +1,4 @@
+import gc
 import os
 import shutil
 import sys
@@ -11,6 +12,13 @@ if ROOT not in sys.path:
 
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a real MI355X (run with -m gpu)")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def no_tensors_of_earlier_files():
+    """A file's refusals leave tensors in cycles (an exception's traceback holds its frames); they go before the next file, whose tests may count memory."""
+    yield
+    gc.collect()
 
 
 @pytest.fixture(scope="session")
