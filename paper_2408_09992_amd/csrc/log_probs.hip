@@ -36,17 +36,18 @@ struct FinishArgs {
     float* top_log_probs;
 };
 
-// Eq. 5's chain of one item, from the tables where they lie.
+// Eq. 5's chain of one item, from the tables where they lie; -inf where a sub-id is out of play.
 __device__ __forceinline__ float score_of_item(const FinishArgs& a, int q, int item) {
     float z = 0.0f;
 #pragma unroll 8                                               // (a chain of additions, but not of loads)
     for (int k = 0; k < a.m; ++k) {
         const size_t at = (size_t)item * a.m + k;
         const uint32_t g = a.code_bytes == 1 ? (uint32_t)static_cast<const uint8_t*>(a.codes)[at] : (uint32_t)static_cast<const uint16_t*>(a.codes)[at];
-        const float v = a.S[((size_t)q * a.m + k) * a.b + min(g, (uint32_t)a.b - 1u)];
+        float v = a.S[((size_t)q * a.m + k) * a.b + min(g, (uint32_t)a.b - 1u)];
+        v = v < kLeastEntry ? kLeastEntry : v;
         z = k == 0 ? v : z + v;
     }
-    return z + 0.0f;
+    return z < kNoScore ? -__builtin_inff() : z + 0.0f;
 }
 
 // grid = positions: joins the shares' sums, scores the given items, cuts the list to the K best and puts them in order.

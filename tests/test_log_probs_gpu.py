@@ -195,6 +195,20 @@ def test_positions_that_are_all_the_lowest_number(pq):
     assert torch.equal(top[1].cpu(), torch.arange(5, dtype=torch.int32))
 
 
+@pytest.mark.parametrize("N", [9_000, 30_000])
+@pytest.mark.parametrize("lowest", [-2e32, float(np.finfo(np.float32).min)])
+def test_masks_of_the_lowest_number_are_masks(pq, N, lowest):
+    codes, S, items = draw_codes(N, 4, 256, 3, 40, seed=7)
+    S[0, 1, ::2] = lowest                                       # one masked sub-id of an item's, or two
+    S[0, 2, ::2] = lowest
+    S[1, 3, 1:] = lowest                                        # fewer items than asked for
+    S[2] = lowest
+    masked = S.clone()
+    masked[S == lowest] = -np.inf
+    for got, want in zip(call(pq, codes, S, items, 200), call(pq, codes, masked, items, 200)):
+        assert torch.equal(got, want)
+
+
 @pytest.mark.parametrize("odd", [float("nan"), float("inf")])
 @pytest.mark.parametrize("kind", ["u8", "f32", "bf16", "f16", "many"])
 def test_scores_that_are_no_numbers_stay_with_their_position(pq, kind, odd):
