@@ -15,6 +15,7 @@ namespace pqk {
 namespace head {
 
 constexpr int kBins = 2048;
+constexpr int kGroups = 64, kFewKept = 40;           // see cut_to_few()
 constexpr int kMostKept = 1024;                      // keys that a cut leaves at most
 constexpr int kMostRegions = 2048;                   // workgroups that share the items of a piece
 constexpr int kFewKeys = 4, kManyKeys = 16;          // keys that a thread of a cut holds; where a list has more each pass reads them again
@@ -50,11 +51,14 @@ __device__ __forceinline__ void append(const Lists& l, int q, long long region, 
 // A cut is made by a workgroup of 1024 threads, or of 256 where there are positions enough to give a compute unit several.
 template <int THREADS>
 struct SelectMemory {
-    uint32_t histogram[kBins];
+    alignas(16) uint32_t histogram[kBins];
+    alignas(16) uint32_t tops[kGroups];
     int begin[kMostRegions];                         // where a region's keys begin among all of them
     uint64_t part[THREADS / kWave][2];
     uint32_t sums[THREADS / kWave];
     int above, taken, chosen, count;
+    uint32_t low;
+    uint64_t least;
 };
 
 // What lies before the thread's own value among those of all threads.
@@ -80,7 +84,7 @@ __device__ __forceinline__ uint32_t sums_before(uint32_t own, SelectMemory<THREA
     return before + sum - own;
 }
 
-// The keys of a position's list: those kept, then the regions'.
+// The keys of a position's list: those kept, then the regions' (a list without regions: `kept` alone).
 struct Keys {
     const uint64_t *kept, *keys;
     const int* begin;
@@ -103,19 +107,34 @@ struct Keys {
 template <int THREADS, int R>
 struct HeldKeys {
     uint64_t k[R];
-    int n;
-    __device__ __forceinline__ HeldKeys(const Keys& all) : n(all.n) {
+    int n, own;                                                // of the list, of the thread
+    __device__ __forceinline__ HeldKeys(const Keys& all) : n(all.n), own(0) {
+        typedef uint64_t Pair __attribute__((ext_vector_type(2), aligned(8)));
+        if (all.regions == 0) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int i = (int)threadIdx.x + r * THREADS;
-            k[r] = i < n ? all(i) : 0;
+            for (int r = 0; r < R; r += 2) {
+                const int i = 2 * ((int)threadIdx.x + r / 2 * THREADS);
+                Pair two = {0, 0};
+                own += min(max(n - i, 0), 2);
+                if (i + 1 < n) two = *reinterpret_cast<const Pair*>(all.kept + i);
+                else if (i < n) two[0] = all.kept[i];
+                k[r] = two[0];
+                k[r + 1] = two[1];
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int i = (int)threadIdx.x + r * THREADS;
+                own += i < n;
+                k[r] = i < n ? all(i) : 0;
+            }
         }
     }
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if ((int)threadIdx.x + r * THREADS < n) f(k[r]);
+            if (r < own) f(k[r]);
     }
 };
 template <int THREADS>
@@ -205,13 +224,62 @@ __device__ __forceinline__ uint64_t cut(const H& held, int keep, int most, Selec
 // How many keys a cut to `keep` may leave: a few more save a pass.
 __host__ __device__ constexpr int most_of(int keep) { return keep + keep / 4 + 32 < kMostKept ? keep + keep / 4 + 32 : kMostKept; }
 
-// Cuts a position's list: what is left in out[] (the order is none), `keep` at least (or all) and most_of(keep) at most; returns how many, and in `least` what
+// A list's `keep` largest keys, where these are few (kFewKept: 63 to be expected), without histograms: of the largest scores of 64 groups of keys (those that come to a
+// lane's number in all waves) the keep-th largest is one that `keep` keys reach, and little more do: 64 ln(64 / (64 - keep)) are to be expected.  These come to LDS and are
+// put in order.  mem.tops holds the groups' largest, with the group's number for the last bits, so that no two are the same.
+// Returns whether they were few enough (of equal scores there may be more); then out[] is in order.
+// 10,000 keys, 10 of them kept: 2 us of the finish less than by histograms.  (256 groups for up to 140 kept took 2 us off 10,000 keys of one position, and cost 300 positions, whose
+// lists keep the lanes busy, 5.)
+constexpr int kFewTaken = 256;
+template <int THREADS, typename H>
+__device__ __forceinline__ bool cut_to_few(const H& held, int keep, uint64_t* out, SelectMemory<THREADS>& mem) {
+    const int tid = threadIdx.x;
+    uint64_t* taken = reinterpret_cast<uint64_t*>(mem.histogram);
+    if (tid < kGroups) {
+        const uint32_t own = mem.tops[tid];
+        int above = 0;
+#pragma unroll
+        for (int i = 0; i < kGroups / 4; ++i) {
+            const uint4 t = reinterpret_cast<const uint4*>(mem.tops)[i];
+            above += (t.x > own) + (t.y > own) + (t.z > own) + (t.w > own);
+        }
+        if (above == keep - 1) mem.low = own & ~(kGroups - 1u);
+    }
+    __syncthreads();
+    const uint64_t low = (uint64_t)mem.low << 32;
+    held.each([&](uint64_t k) {
+        if (k >= low) {
+            const int at = atomicAdd(&mem.count, 1);
+            if (at < kFewTaken) taken[at] = k;
+        }
+    });
+    __syncthreads();
+    const int n = mem.count;
+    if (n > kFewTaken) {
+        __syncthreads();
+        if (tid == 0) mem.count = 0;
+        return false;
+    }
+    if (tid < n) {
+        const uint64_t mine = taken[tid];
+        int rank = 0;
+#pragma unroll 8                                               // (their reads of LDS on their way together)
+        for (int i = 0; i < n; ++i) rank += taken[i] > mine;
+        if (rank < keep) out[rank] = mine;
+        if (rank == keep - 1) mem.least = mine;
+    }
+    return true;
+}
+
+// Cuts a position's list: what is left in out[] (in order, or in none: `sorted`), `keep` at least (or all) and most_of(keep) at most; returns how many, and in `least` what
 // they reach (0: as good as nothing was cut).  last: no floor is asked for.  stored: how many keys the first piece left, if that was the last piece; else regions of `region` keys each.
-template <int THREADS>
-__device__ __forceinline__ int cut_list(const Lists& l, int q, int stored, int regions, long long region, bool last, uint64_t* out, uint64_t& least, SelectMemory<THREADS>& mem) {
+// meanwhile() is called while the keys are on their way, and after a barrier aside(), while the first wave (of the others little is asked) looks for the cut.
+template <int THREADS, typename Meanwhile, typename Aside>
+__device__ __forceinline__ int cut_list(const Lists& l, int q, int stored, int regions, long long region, bool last, uint64_t* out, bool& sorted, uint64_t& least, SelectMemory<THREADS>& mem,
+                                        Meanwhile meanwhile, Aside aside) {
     const int tid = threadIdx.x, most = last ? l.keep + 16 : most_of(l.keep);       // (of the last every key is scored again)
     const uint64_t* keys = l.keys + (size_t)q * l.cap;
-    Keys all{l.kept + (size_t)q * kMostKept, keys, mem.begin, region, stored, 1, stored};
+    Keys all{l.kept + (size_t)q * kMostKept, keys, mem.begin, region, stored, 0, stored};
     if (stored) all.kept = keys;
     else {
         all.kept_n = l.kept_count[q];
@@ -232,19 +300,35 @@ __device__ __forceinline__ int cut_list(const Lists& l, int q, int stored, int r
         }
         all.n = all.kept_n + (int)total;
     }
+    if (tid < kGroups) mem.tops[tid] = 0;
     if (tid == 0) mem.count = 0;
     __syncthreads();
+    int left = 0;
     auto run = [&](const auto& held) {
-        least = last && held.n <= most ? 0 : cut<THREADS>(held, l.keep, most, mem);
-        held.each([&](uint64_t k) {
-            if (k >= least) out[atomicAdd(&mem.count, 1)] = k;
-        });
+        meanwhile();
+        const bool any = held.n > (last ? most : l.keep), few = any && l.keep <= kFewKept;
+        if (few) {
+            uint32_t top = 0;
+            held.each([&](uint64_t k) { top = max(top, (uint32_t)(k >> 32)); });
+            atomicMax(&mem.tops[tid % kGroups], (top & ~(kGroups - 1u)) | (uint32_t)(tid % kGroups));
+        }
+        __syncthreads();
+        aside();
+        sorted = few && cut_to_few<THREADS>(held, l.keep, out, mem);
+        if (!sorted) {
+            least = any ? cut<THREADS>(held, l.keep, most, mem) : 0;
+            held.each([&](uint64_t k) {
+                if (k >= least) out[atomicAdd(&mem.count, 1)] = k;
+            });
+        }
+        __syncthreads();
+        left = mem.count;
+        if (sorted) { left = l.keep; least = mem.least; }
     };
     if (all.n <= kFewKeys * THREADS) run(HeldKeys<THREADS, kFewKeys>(all));
     else if (all.n <= kManyKeys * THREADS) run(HeldKeys<THREADS, kManyKeys>(all));
     else run(FarKeys<THREADS>(all));
-    __syncthreads();
-    return mem.count;
+    return left;
 }
 
 // grid = positions: cuts the lists between two pieces and sets the floors.
@@ -254,7 +338,8 @@ __global__ __launch_bounds__(THREADS) void select_kernel(Lists l, int stored, in
     __shared__ uint64_t out[kMostKept];
     const int q = blockIdx.x, tid = threadIdx.x;
     uint64_t least;
-    const int n = cut_list(l, q, stored, regions, region, false, out, least, mem);
+    bool sorted;
+    const int n = cut_list(l, q, stored, regions, region, false, out, sorted, least, mem, [] {}, [] {});
     for (int i = tid; i < n; i += THREADS) l.kept[(size_t)q * kMostKept + i] = out[i];
     if (tid == 0) {
         l.kept_count[q] = n;

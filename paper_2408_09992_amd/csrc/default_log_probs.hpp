@@ -160,7 +160,7 @@ struct DenseFinishArgs {
     const int* items;
     long long N;
     int B, d, n, K;
-    float temperature;
+    double per_temperature;                            // 1 / T
     const float4* partial;     // [B][groups], of all pieces
     int groups, stored, regions;                       // groups of all pieces; of the last piece what cut_list() takes
     long long region;
@@ -178,29 +178,40 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
     __shared__ double score[kMostKept];
     __shared__ float4 sums[THREADS / kWave];
     __shared__ double lse_of_all;
+    constexpr int kWaves = THREADS / kWave;
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    float c = kLowest, s = 0.0f, t = 0.0f;
-    for (int i = tid; i < a.groups; i += THREADS) {
-        const float4 v = a.partial[(size_t)q * a.groups + i];
-        join_sums(c, s, t, v.x, v.y, v.z);
-    }
-#pragma unroll
-    for (int x = 1; x < kWave; x *= 2) join_sums(c, s, t, __shfl_xor(c, x), __shfl_xor(s, x), __shfl_xor(t, x));
-    if (lane == 0) sums[wave] = make_float4(c, s, t, 0.0f);
-    __syncthreads();
-    c = sums[0].x; s = sums[0].y; t = sums[0].z;
-    for (int w = 1; w < THREADS / kWave; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
-    if (tid == 0) {                                            // (64-bit logarithms, by one wave: the others go on to the list)
-        lse_of_all = log_sum64(c, s);
-        a.lse[q] = (float)lse_of_all;
-        a.entropy[q] = entropy_of(s, t);
-    }
+    auto own_sums = [&] {
+        float c = kLowest, s = 0.0f, t = 0.0f;
+        for (int i = tid; i < a.groups; i += THREADS) {
+            const float4 v = a.partial[(size_t)q * a.groups + i];
+            join_sums(c, s, t, v.x, v.y, v.z);
+        }
+        if (wave * kWave < a.groups) join_wave(c, s, t);
+        if (lane == 0) sums[wave] = make_float4(c, s, t, 0.0f);
+    };
+    auto aside = [&] {                                         // (64-bit logarithms, by one wave)
+        if (wave != kWaves - 1) return;
+        float4 v = sums[lane % kWaves];
+        join_wave<kWaves>(v.x, v.y, v.z);
+        if (lane == 0) {
+            lse_of_all = log_sum64(v.x, v.y);
+            a.lse[q] = (float)lse_of_all;
+            a.entropy[q] = entropy_of(v.y, v.z);
+        }
+    };
     const T *W = static_cast<const T*>(a.W), *h = static_cast<const T*>(a.H) + (size_t)q * a.d;
     uint64_t least;
-    const int n = a.K ? cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem) : 0;
-    __syncthreads();
+    bool sorted;
+    int n = 0;
+    if (a.K) n = cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, sorted, least, mem, own_sums, aside);
+    else {
+        own_sums();
+        __syncthreads();
+        aside();
+        __syncthreads();
+    }
     const double lse = lse_of_all;
-    auto log_prob = [&](double z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(z / (double)a.temperature - lse); };
+    auto log_prob = [&](double z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(z * a.per_temperature - lse); };
     // (the given items and the candidates at once: a row's way here is most of what either takes)
     score_rows<THREADS>(W, h, a.d, a.n + n,
                         [&](int i) {

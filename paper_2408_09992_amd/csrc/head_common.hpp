@@ -60,6 +60,12 @@ __device__ __forceinline__ void raise_reference(float& c, float& s, float& t, fl
     s *= f;
     c = to;
 }
+// Those of OF lanes of a wave, which all of them get.
+template <int OF = kWave>
+__device__ __forceinline__ void join_wave(float& c, float& s, float& t) {
+#pragma unroll
+    for (int x = 1; x < OF; x *= 2) join_sums(c, s, t, __shfl_xor(c, x), __shfl_xor(s, x), __shfl_xor(t, x));
+}
 // - sum_i p log p in nats: log p = ln 2 (x - log2 s).  0 where no score counts.
 __device__ __forceinline__ float entropy_of(float s, float t) {
     return s == 0.0f ? 0.0f : s < __builtin_inff() ? (float)fmax((log2((double)s) - (double)t / (double)s) / kLog2eDouble, 0.0) : __builtin_nanf("");

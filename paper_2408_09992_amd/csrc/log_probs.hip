@@ -25,7 +25,7 @@ struct FinishArgs {
     const int* items;
     long long N;
     int B, m, b, n, K, code_bytes;
-    float temperature;
+    double per_temperature;                            // 1 / T
     const float4* partial;     // [B][shares]
     int shares, stored, regions;                       // shares of all pieces; of the last piece what cut_list() takes
     long long region;
@@ -57,31 +57,52 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
     __shared__ uint64_t kept[kMostKept];
     __shared__ float4 sums[THREADS / kWave];
     __shared__ double lse_of_all;
+    constexpr int kWaves = THREADS / kWave;
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    float c = kLowest, s = 0.0f, t = 0.0f;
-    for (int i = tid; i < a.shares; i += THREADS) {
-        const float4 v = a.partial[(size_t)q * a.shares + i];
-        join_sums(c, s, t, v.x, v.y, v.z);
-    }
-#pragma unroll
-    for (int x = 1; x < kWave; x *= 2) join_sums(c, s, t, __shfl_xor(c, x), __shfl_xor(s, x), __shfl_xor(t, x));
-    if (lane == 0) sums[wave] = make_float4(c, s, t, 0.0f);
-    __syncthreads();
-    c = sums[0].x; s = sums[0].y; t = sums[0].z;
-    for (int w = 1; w < THREADS / kWave; ++w) join_sums(c, s, t, sums[w].x, sums[w].y, sums[w].z);
-    if (tid == 0) {                                            // (64-bit logarithms, by one wave: the others go on to the list)
-        lse_of_all = log_sum64(c, s);
-        a.lse[q] = (float)lse_of_all;
-        a.entropy[q] = entropy_of(s, t);
-    }
+    // the given item that a thread scores aside, in a wave that has no other work there: what its row takes to come is over by then
+    const int own = (tid + THREADS / 2) % THREADS;
+    int item = own < a.n ? a.items[(size_t)q * a.n + own] : -1;
+    uint8_t touched = 0;
+    float given = 0.0f;
+    auto own_sums = [&] {
+        float c = kLowest, s = 0.0f, t = 0.0f;
+        for (int i = tid; i < a.shares; i += THREADS) {
+            const float4 v = a.partial[(size_t)q * a.shares + i];
+            join_sums(c, s, t, v.x, v.y, v.z);
+        }
+        if (wave * kWave < a.shares) join_wave(c, s, t);
+        if (lane == 0) sums[wave] = make_float4(c, s, t, 0.0f);
+        item = item < a.N ? item : -1;
+        if (item >= 0) touched = static_cast<const uint8_t*>(a.codes)[(size_t)item * a.m * a.code_bytes];
+    };
+    auto aside = [&] {
+        asm volatile("" ::"v"((int)touched));
+        if (item >= 0) given = score_of_item(a, q, item);
+        if (wave != kWaves - 1) return;
+        float4 v = sums[lane % kWaves];                        // (64-bit logarithms, by one wave)
+        join_wave<kWaves>(v.x, v.y, v.z);
+        if (lane == 0) {
+            lse_of_all = log_sum64(v.x, v.y);
+            a.lse[q] = (float)lse_of_all;
+            a.entropy[q] = entropy_of(v.y, v.z);
+        }
+    };
     uint64_t least;
-    const int n = a.lists.keep ? cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, least, mem) : 0;
-    __syncthreads();
+    bool sorted = false;
+    int n = 0;
+    if (a.lists.keep) n = cut_list<THREADS>(a.lists, q, a.stored, a.regions, a.region, true, kept, sorted, least, mem, own_sums, aside);
+    else {
+        own_sums();
+        __syncthreads();
+        aside();
+        __syncthreads();
+    }
     const double lse = lse_of_all;
-    auto log_prob = [&](float z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)((double)z / (double)a.temperature - lse); };
-    for (int i = tid; i < a.n; i += THREADS) {
-        const int item = a.items[(size_t)q * a.n + i];
-        a.log_probs[(size_t)q * a.n + i] = item >= 0 && item < a.N ? log_prob(score_of_item(a, q, item)) : 0.0f;
+    auto log_prob = [&](float z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)((double)z * a.per_temperature - lse); };
+    if (own < a.n) a.log_probs[(size_t)q * a.n + own] = item >= 0 ? log_prob(given) : 0.0f;
+    for (int i = own + THREADS; i < a.n; i += THREADS) {
+        const int next = a.items[(size_t)q * a.n + i];
+        a.log_probs[(size_t)q * a.n + i] = next >= 0 && next < a.N ? log_prob(score_of_item(a, q, next)) : 0.0f;
     }
     if (a.K == 0) return;
     if (a.ranked) {
@@ -113,9 +134,11 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
     }
     for (int at = tid; at < n; at += THREADS) {
         const uint64_t mine = kept[at];
-        int rank = 0;
+        int rank = sorted ? at : 0;
+        if (!sorted) {
 #pragma unroll 8                                               // (their reads of LDS on their way together)
-        for (int i = 0; i < n; ++i) rank += kept[i] > mine;
+            for (int i = 0; i < n; ++i) rank += kept[i] > mine;
+        }
         if (rank < a.K) {
             a.top_items[(size_t)q * a.K + rank] = (int)item_of(mine);
             a.top_log_probs[(size_t)q * a.K + rank] = log_prob(score_of(mine));
@@ -230,7 +253,7 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
         if (rc != PQ_OK) return rc;
     }
     if (e == hipSuccess) {
-        const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), temperature, reinterpret_cast<const float4*>(ws), l.shares,
+        const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), 1.0 / temperature, reinterpret_cast<const float4*>(ws), l.shares,
                            a.store ? (int)N : 0, p.shares, p.share, lists, ranked, out, entropy, lse, top_items, top_log_probs};
         if (many_lists(B) || lists.keep == 0) hipLaunchKernelGGL(log_probs_finish_kernel<256>, dim3(B), dim3(256), 0, st, f);
         else hipLaunchKernelGGL(log_probs_finish_kernel<1024>, dim3(B), dim3(1024), 0, st, f);

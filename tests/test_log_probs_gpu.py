@@ -144,6 +144,16 @@ def test_scores_in_the_worst_orders(pq, kind):
     assert torch.allclose(lp[2].double(), torch.full((K,), -np.log(N), dtype=torch.float64, device="cuda"), rtol=0, atol=U * (N / 512 + 128))
 
 
+@pytest.mark.parametrize("N", [45, 300, 700, 5_000, 16_000, 20_000])
+@pytest.mark.parametrize("K", [1, 10, 40, 41])
+@pytest.mark.parametrize("B", [2, 300])
+def test_few_different_scores(pq, N, K, B):
+    codes, S, items = draw_codes(N, 2, 3, B, 2, seed=N + K)
+    S.copy_(S.round())                                          # (sums of them are exact)
+    S[1] = 0.5
+    check(pq, codes, S, items, K)
+
+
 @pytest.mark.parametrize("type", list(TYPES))
 @pytest.mark.parametrize("B", [5, 100])
 def test_items_twice_in_the_catalogue(pq, B, type):
