@@ -331,7 +331,7 @@ __device__ __forceinline__ int cut_list(const Lists& l, int q, int stored, int r
     return left;
 }
 
-// grid = positions: cuts the lists between two pieces and sets the floors.
+// grid = positions: cuts the lists between two pieces and sets the floors.  Chains of latencies again: 6 to 10 us for 203 positions of 10 + 16 keys or 512 of 100, 9 to 15 for 1024 of 116.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void select_kernel(Lists l, int stored, int regions, long long region) {
     __shared__ SelectMemory<THREADS> mem;

@@ -1,5 +1,7 @@
 // Log-probabilities of given items, entropy and the likeliest items by the default scorer's W phi (pq_default_log_probs): the cross entropy's pass
 // over W (default_cross_entropy.hpp) with one more sum, and with candidates for the K best (alternatives.hpp).
+//
+//   r_qi = W[i] . phi_q   lse = log sum_i exp(r_i / T)   log p_i = r_i / T - lse   entropy = ln 2 (log2 s - t / s), s = sum 2^x, t = sum 2^x x, x = r log2 e / T - c
 #pragma once
 #include "pqtopk_probs.h"
 #include "default_cross_entropy.hpp"
@@ -28,6 +30,8 @@ struct DenseProbsArgs {
 // counter in LDS, whose answer every candidate waits for, took 180 us of the 1.9 ms of 1024 positions' best 100 of 1.28M items, where this takes 110.
 template <typename Tile, int ITEMS> constexpr int kShares = ITEMS / (32 * Tile::MI) * 2;
 
+// grid: groups of tiles of items x tiles of positions, one of which a chiplet takes one after the other (chiplet_order).  Bound by the matrix cores and the exponentials between the
+// products: 262,144 items of 512 bfloat16 and 1024 positions 305 to 314 us, 880 to 900 TFLOP/s with the candidates (the loss alone 920).
 template <typename T, int BN, int ITEMS>
 __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_log_probs_kernel(DenseProbsArgs a) {
     using Tile = ScoresTile<T, BN, ITEMS>;
@@ -151,7 +155,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     }
 }
 
-// The same for up to 64 positions of 16-bit operands, d <= 512.
+// The same for up to 64 positions of 16-bit operands, d <= 512: 64 positions, 1.3 GB of W, 221 us, 5.9 TB/s.
 template <typename T, int D>
 __global__ __launch_bounds__(kFewThreads, 2) void default_few_log_probs_kernel(DenseProbsArgs a) { few_sums<T, D, true>(a, a.first, a.end); }
 
@@ -170,7 +174,8 @@ struct DenseFinishArgs {
     float* top_log_probs;
 };
 
-// grid = positions: joins the groups' sums, scores the given items and the list's best in 64 bits, puts these in order.
+// grid = positions: joins the groups' sums, scores the given items and the list's best in 64 bits, puts these in order.  A chain of latencies: one position 8.2 us; 1024 positions, whose
+// 117 rows each come from memory as a rule, 40.
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(DenseFinishArgs a) {
     __shared__ SelectMemory<THREADS> mem;

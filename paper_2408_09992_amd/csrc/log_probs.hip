@@ -4,9 +4,9 @@
 //   r_qi = sum_k S[q][k][G[i][k]]   lse = log sum_i exp(r_i / T)   log p_i = r_i / T - lse   entropy = lse - sum_i p_i r_i / T
 //
 // The pass is the cross entropy's (cross_entropy.hpp) with one more sum.  The likeliest items come from it too, what scores pass a position's floor going to
-// its list (alternatives.hpp), or, where the lookups are few, from the ranking's own scan, whose bounds of one byte need no first piece and no cut:
-// what either adds to the pass, us, lists and scan: 1.28M items, m = 8, K = 10: one position 22 and 10, 64 34 and 32, 128 36 and 47; K = 100: 16 55 and 27, 64 58 and 43, 128 62
-// and 65; m = 16, K = 10: 64 35 and 50; 5M, m = 8, K = 10: 16 47 and 31, 64 50 and 63.
+// its list (alternatives.hpp), or, where the lookups are few, from the ranking's own scan, whose bounds of one byte need no first piece and no cut (by_ranking()).
+// Bound by the lookups in LDS and the exponentials beside them: 512 positions of 1.28M items, m = 8, K = 100, 517 to 553 us; two launches of 6.9 and 5.9 us for one
+// position of 10,000.
 #include "pqtopk_probs.h"
 #include "cross_entropy.hpp"
 
@@ -179,8 +179,13 @@ struct Layout : ListLayout {
     int shares;
     size_t topk_bytes, finite_at, ranked_at, topk_at;          // (topk_bytes: 0 where lists are kept)
 };
+// Whether the ranking's scan follows the pass instead of lists.  It looks the items up again, in chains that grow with m; lists take launches, more of them for a larger K, and cuts
+// of up to kFewKept keys take less.  All of a call, us, lists and scan, K = 10 and 100: 1.28M items, m = 8: 4 positions 42 | 39, 57 | 44; 16 50 | 55, 65 | 60; 64 94 | 105,
+// 113 | 118; m = 16: 4 55 | 50, 68 | 56; 16 70 | 74, 84 | 81; 64 147 | 178, 165 | 195; m = 4: 16 45 | 44, 62 | 48; 64 77 | 79, 102 | 86; 400,000 items, m = 32: 4 58 | 56,
+// 66 | 60; 16 58 | 82, 66 | 89; 200,000, m = 8: 32 42 | 39, 51 | 47; 64 46 | 49, 56 | 55; 5M, m = 8: 4 57 | 56, 149 | 61; 16 97 | 105, 186 | 112; 64 270 | 292, 301 | 330.
+bool by_ranking(long long N, int B, int m, int K) { return K > 0 && N > kOnePiece && (double)N * B * m * m <= (K <= kFewKept ? 1e9 : 6e9); }
 size_t topk_bytes_of(long long N, int B, int m, int b, int K, int code_bytes) {
-    if (K == 0 || N <= kOnePiece || (double)N * B * m > 1e9) return 0;
+    if (!by_ranking(N, B, m, K)) return 0;
     return code_bytes == 1 ? pq_score_topk_workspace_bytes(N, B, m, b, K) : pq_score_topk_u16_workspace_bytes(N, B, m, b, K);
 }
 bool lay_out(Layout& l, long long N, int B, int m, int b, int K, int code_bytes) {
