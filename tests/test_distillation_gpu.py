@@ -382,3 +382,42 @@ def test_refusals(pq):
             for bad in ((items.long(), scores), (items, scores.double()), (items, scores[:, :1].contiguous()), (items[:2], scores[:2]), (items.cpu(), scores)):
                 with pytest.raises(ValueError):
                     call(pq, first, second, *bad, *rest)
+
+
+@pytest.mark.parametrize("kind", ["u8", "f32", "bf16", "f16", "many"])
+def test_one_item_in_every_entry(pq, kind):
+    N, K, type = 3_001, 512, "bf16" if kind == "many" else kind
+    first, second, items, scores, grad = draw_codes(N, 4, 256, 5, K, seed=21) if kind == "u8" else draw_dense(N, 64, 130 if kind == "many" else 5, K, type, seed=21)
+    items[0] = 17                                               # all its entries together have the weight 1
+    items[1, ::2] = 0
+    items[2] = N - 1
+    scores[2] = -np.inf                                         # ... or none
+    scores[2, 5] = 1.0
+    check(pq, first, second, items, scores, grad, 1.5, None if kind == "u8" else type)
+
+
+@pytest.mark.parametrize("kind", ["u8", "f32", "bf16", "f16", "many"])
+def test_two_steps_at_once(pq, kind):
+    type = "bf16" if kind == "many" else kind
+
+    def inputs(seed):
+        return draw_codes(60_001, 8, 256, 9, 20, seed) if kind == "u8" else draw_dense(60_001, 64, 200 if kind == "many" else 9, 20, type, seed)
+
+    def step(args):
+        loss, lse = forward(pq, *args[:4], 2.0)
+        out = backward(pq, *args[:4], lse, args[4], 2.0)
+        return [loss, lse, *([out] if kind == "u8" else out)]
+
+    both = [inputs(1), inputs(2)]
+    want = [step(each) for each in both]
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i, side in enumerate(sides):
+            with torch.cuda.stream(side):
+                got[i].append(step(both[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for each in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(want[i], each))

@@ -361,3 +361,73 @@ def test_refusals(pq):
         pq.pq_default_log_probs(W.double(), H.double(), items)
     with pytest.raises(pq.PQError):
         pq.pq_default_log_probs(W, H[:, :32].contiguous(), items)
+
+
+def test_by_lists_of_sub_ids_again_and_in_a_graph(pq):
+    N, m, B, K = 50_001, 32, 40, 30                             # (more lookups than the ranking is asked for: pieces, cuts, lists)
+    codes, S, items = draw_codes(N, m, 256, B, 2, seed=1)
+    want = [t.clone() for t in check(pq, codes, S, items, K)]
+    outputs = [t.clone() for t in want]
+    workspace = torch.empty(pq.pq_log_probs_workspace_bytes(N, B, m, 256, K), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call(pq, codes, S, items, K, 1.0, workspace, *outputs)
+    for seed in (1, 2, 3):
+        for to, new in zip((codes, S, items), draw_codes(N, m, 256, B, 2, seed)):
+            to.copy_(new)
+        workspace.random_(0, 256)
+        if seed > 1:
+            want = [t.clone() for t in call(pq, codes, S, items, K)]
+        for t in outputs:
+            t.fill_(-7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outputs))
+
+
+@pytest.mark.parametrize("kind", ["u8", "lists", "f32", "bf16", "many"])
+def test_two_calls_at_once(pq, kind):
+    def inputs(seed):
+        if kind in ("u8", "lists"):
+            return draw_codes(60_001, 32 if kind == "lists" else 4, 256, 40, 3, seed=seed)
+        return draw_dense(60_001, 64, 200 if kind == "many" else 9, 3, "f32" if kind == "f32" else "bf16", seed=seed)
+
+    both = [inputs(1), inputs(2)]
+    want = [call(pq, *each, 20) for each in both]
+    sides = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i, side in enumerate(sides):
+            with torch.cuda.stream(side):
+                got[i].append(call(pq, *both[i], 20))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for each in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(want[i], each))
+
+
+@pytest.mark.parametrize("kind", ["u8", "f32", "bf16", "many"])
+def test_entropy_alone(pq, kind):
+    first, second, _ = draw_codes(30_001, 4, 256, 5, 1, seed=3) if kind == "u8" else draw_dense(30_001, 64, 130 if kind == "many" else 5, 1, "f32" if kind == "f32" else "bf16", seed=3)
+    log_probs, entropy, lse, top_items, top_log_probs = call(pq, first, second)
+    B = second.shape[0]
+    assert log_probs.shape == top_items.shape == top_log_probs.shape == (B, 0)
+    check(pq, first, second, torch.empty((B, 0), dtype=torch.int32, device="cuda"), 0)
+
+
+@pytest.mark.parametrize("B", [3, 300])
+@pytest.mark.parametrize("type", list(TYPES))
+def test_as_many_likeliest_items_as_can_be_asked_for(pq, type, B):
+    check(pq, *draw_dense(513 if B == 3 else 9_001, 24, B, 2, type, seed=B), 512)
+
+
+@pytest.mark.parametrize("B", [1, 5, 100, 300])
+@pytest.mark.parametrize("type", list(TYPES))
+def test_items_that_the_catalogue_holds_hundreds_of_times(pq, type, B):
+    W, H, items = draw_dense(130, 96, B, 2, type, seed=B)
+    N = 60_001
+    W = W[torch.from_numpy(np.random.default_rng(4).integers(0, 130, N)).cuda()].contiguous()
+    z64 = H.double() @ W.double().t().contiguous()
+    assert torch.equal(call(pq, W, H, items, 20)[3], ranks(z64, 20))      # (of as good ones the lowest ids: equal rows have equal sums wherever they are)
