@@ -353,8 +353,9 @@ __global__ __launch_bounds__(THREADS) void select_kernel(Lists l, int stored, in
 inline bool many_lists(int B) { return B > kCUs; }
 
 // The pieces of a pass over N items: `first` items, whose scores are all stored, then as many as the lists have room for and no more than `growth`
-// times the items before them: a list gets some growth * keep new keys in each.  How many pieces: a cut and what it stops take some 25 us, a candidate 40 to
-// 150 ps over the chip (1024 positions, 116 kept, 840,000 candidates beside 262,144 items of 512 bfloat16 46 us; 300,000 items of 256 bfloat16, 300 positions, K = 20 in one piece of 295,904 after the first: 780,000 candidates, 120 us).
+// times the items before them: a list gets some growth * keep new keys in each.  How many pieces: a cut and what it stops take some 25 us, a candidate 25 to 150 ps over the chip (1024
+// positions, 116 kept, 840,000 candidates beside 262,144 items of 512 bfloat16 46 us; 512 positions by sub-ids, K = 100, counted at 25 547 us, at 50, which makes a piece more, 556).
+// `most`: of the candidates of a piece, where more than that take much longer each.
 constexpr long long kOnePiece = 16384, kListBytes = 1LL << 31;
 struct Passes {
     long long N, first, room, growth;
@@ -366,15 +367,15 @@ struct Passes {
         return n < N - done ? n : N - done;
     }
 };
-inline Passes passes_of(long long N, int B, int keep) {
+inline Passes passes_of(long long N, int B, int keep, double most = 1e300) {
     Passes p{N, N, N, 1, (int)(keep < N ? keep : N)};
     if (keep == 0) return p;
     const long long least = B <= 128 ? kOnePiece : (long long)round_up(8 * (size_t)keep, 4096);
     if (N > kOnePiece && N > 2 * least) p.first = least;
     double best = 1e300;
     for (int pieces = 1; pieces <= 8; ++pieces) {
-        const double growth = pow((double)N / (double)p.first, 1.0 / pieces), cost = pieces * (25.0 + 5e-5 * (double)B * keep * growth);
-        if (cost < best) { best = cost; p.growth = (long long)growth + 1; }
+        const double growth = pow((double)N / (double)p.first, 1.0 / pieces), candidates = (double)B * keep * growth, cost = pieces * (25.0 + 2.5e-5 * candidates);
+        if (cost < best || (double)B * keep * (double)p.growth > most) { best = cost; p.growth = (long long)ceil(growth); }
     }
     p.room = kListBytes / 8 / B > p.first ? kListBytes / 8 / B : p.first;
     return p;

@@ -38,7 +38,8 @@ struct Layout : ListLayout {
 };
 Layout lay_out(long long N, int B, int d, int type, int K) {
     Layout l;
-    l.passes = passes_of(N, B, keep_of(K));
+    // (few positions' candidates wait in LDS: 64 positions of 1.28M items of 128, K = 100, one piece after the first 187 us, two 145)
+    l.passes = passes_of(N, B, keep_of(K), plan_dense(N, B, d, type).few ? 0.8 * kFewWaiting * kCUs : 1e300);
     l.groups = 0;
     for (long long done = 0, now, region; done < N; done += now) {
         int regions;
