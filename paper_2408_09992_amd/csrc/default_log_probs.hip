@@ -18,10 +18,13 @@ DensePlan plan_piece(long long items, int B, int d, int type, bool listed, int& 
     else {
         if (listed && (long long)p.groups * shares > kMostRegions) {
             // the rounds over the chip that take least, a tile of items a unit; of as good ones the fewest groups
+            // (two workgroups a compute unit of those that leave room for it: one alone has nothing to do while its candidates are on their way; 1.28M items of 64 bfloat16,
+            // 100 positions, K = 10 and 100: 161 and 229 us by one, 121 and 160 by two)
+            const int slots = p.positions == 256 ? kCUs : 2 * kCUs;
             double best = 1e300;
             const long long least = ceil_div(p.item_tiles * shares, kMostRegions);
             for (long long each = least; each <= 2 * least + 16; ++each) {
-                const double cost = (double)ceil_div(ceil_div(p.item_tiles, each) * p.position_tiles, kCUs) * (each + 0.1);
+                const double cost = (double)ceil_div(ceil_div(p.item_tiles, each) * p.position_tiles, slots) * (each + 0.1);
                 if (cost <= best) { best = cost; p.tiles_each = (int)each; }
             }
             p.groups = (int)ceil_div(p.item_tiles, p.tiles_each);
