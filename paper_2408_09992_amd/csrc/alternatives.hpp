@@ -18,7 +18,9 @@ constexpr int kBins = 2048;
 constexpr int kGroups = 64, kFewKept = 40;           // see cut_to_few()
 constexpr int kMostKept = 1024;                      // keys that a cut leaves at most
 constexpr int kMostRegions = 2048;                   // workgroups that share the items of a piece
-constexpr int kFewKeys = 4, kManyKeys = 16;          // keys that a thread of a cut holds; where a list has more each pass reads them again
+// Keys that a thread of a cut holds; where a list has more each pass reads them again.  (kMostKeys by 1024 threads: 30,000 items of 128, 10 positions, K = 10, 30.4 and, held, 20.3 us; by
+// 256, whose registers then leave a compute unit fewer workgroups, 400 positions of 25,000 59.5 and 60.9.)
+constexpr int kFewKeys = 4, kManyKeys = 16, kMostKeys = 32;
 
 struct Lists {
     uint64_t* keys;            // [B][cap]: all keys of the first piece, or the regions of a later one
@@ -327,6 +329,7 @@ __device__ __forceinline__ int cut_list(const Lists& l, int q, int stored, int r
     };
     if (all.n <= kFewKeys * THREADS) run(HeldKeys<THREADS, kFewKeys>(all));
     else if (all.n <= kManyKeys * THREADS) run(HeldKeys<THREADS, kManyKeys>(all));
+    else if (THREADS == 1024 && all.n <= kMostKeys * THREADS) run(HeldKeys<THREADS, THREADS == 1024 ? kMostKeys : kManyKeys>(all));
     else run(FarKeys<THREADS>(all));
     return left;
 }
