@@ -13,7 +13,7 @@ namespace head {
 namespace {
 
 constexpr int kListThreads = 512, kListWaves = kListThreads / kWave;
-static_assert(PQ_MAX_K <= kMostEntries && Teacher<kListThreads>::kEach == 1, "a thread an entry");
+static_assert(PQ_MAX_K <= kMostEntries && kMostEntries <= kListThreads && kMostEntries <= 512, "a thread an entry, whose number has nine bits");
 
 struct ListArgs {
     const void *W, *H;
@@ -32,19 +32,56 @@ struct ListArgs {
     int few_items, few_groups;                         // default_few_kernel's tiles and workgroups, where it makes the gradient
 };
 
-// The list's items' scores in score[].
-template <typename T>
-__device__ __forceinline__ void score_list(const ListArgs& a, int q, const int* item, double* score) {
-    score_rows<kListThreads>(static_cast<const T*>(a.W), static_cast<const T*>(a.H) + (size_t)q * a.d, a.d, a.K, [&](int k) { return (long long)item[k]; },
-                             [&](int k, bool there, double z) { if (there) score[k] = z; });
+// A list by a workgroup, a thread an entry: its item (-1: none), its weight and the weight's logarithm, and in score[] its score.  The first wave adds the weights up
+// while the others score the items; alone() is called by it after that.
+struct Entry {
+    int item;
+    double weight, log_weight;
+    bool any;                  // whether an entry of the list has weight, or is a NaN
+};
+struct ListMemory {
+    double x[kMostEntries], score[kMostEntries];               // of an entry over T; of its item
+    int item[kMostEntries];
+    WaveTeacher teacher;
+};
+template <typename T, typename Alone>
+__device__ __forceinline__ Entry entry_of(const ListArgs& a, int q, ListMemory& mem, Alone alone) {
+    const int tid = threadIdx.x;
+    const size_t at = (size_t)q * a.K + min(tid, a.K - 1);
+    Entry e;
+    e.item = a.items[at];
+    const float u = a.scores[at];
+    if (tid >= a.K || e.item < 0 || e.item >= a.N) e.item = -1;
+    double x = e.item >= 0 ? (double)u / (double)a.temperature : -__builtin_inf();
+    if (tid < a.K) {
+        mem.item[tid] = e.item;
+        mem.x[tid] = x;
+    }
+    __syncthreads();
+    if (tid < kWave) {
+        const WaveTeacher t = wave_teacher(a.K, [&](int k) { return mem.x[k]; });
+        if (tid == 0) mem.teacher = t;
+        alone();
+    } else {
+        score_rows<kWave, kListThreads>(static_cast<const T*>(a.W), static_cast<const T*>(a.H) + (size_t)q * a.d, a.d, a.K, [&](int k) { return (long long)mem.item[k]; },
+                                        [&](int k, bool there, double z) { if (there) mem.score[k] = z; });
+    }
+    __syncthreads();
+    const WaveTeacher t = mem.teacher;
+    e.any = t.any;
+    if (e.item >= 0) x -= t.top;
+    e.weight = !t.any ? 0.0 : t.sum < __builtin_inf() ? t.weight(x) : __builtin_nan("");       // (a list with a NaN or +inf: all of it)
+    e.log_weight = x - t.log_sum;
+    return e;
 }
 
-// grid = positions: joins the groups' sums, scores the list, adds the loss up.  64 positions with 100 entries 13 us, 1024 with 32 23: rows from memory.
+// grid = positions: joins the groups' sums, scores the list, adds the loss up.  Chains of latencies: one position with 10 entries 4.5 us, 64 with 100 10, 1024 with
+// 32 19 (rows from memory).
 template <typename T>
 __global__ __launch_bounds__(kListThreads) void default_distillation_join_kernel(ListArgs a) {
-    __shared__ double part[kListWaves], score[kMostEntries];
+    __shared__ ListMemory mem;
+    __shared__ double part[kListWaves], lse_of_all;
     __shared__ float2 sums[kListWaves];
-    __shared__ int item[kMostEntries];
     const int q = blockIdx.x, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     float c = kLowest, s = 0.0f;
     for (int i = tid; i < a.groups; i += kListThreads) {
@@ -54,69 +91,74 @@ __global__ __launch_bounds__(kListThreads) void default_distillation_join_kernel
 #pragma unroll
     for (int x = 1; x < kWave; x *= 2) join_sums(c, s, __shfl_xor(c, x), __shfl_xor(s, x));
     if (lane == 0) sums[wave] = make_float2(c, s);
-    const Teacher<kListThreads> t = teacher_of<kListThreads>(a.items, a.scores, q, a.K, a.N, a.temperature, part);
-    if (tid < a.K) item[tid] = t.weight[0] != 0.0 ? t.item[0] : -1;       // (of the others no score is asked; NaN is not 0)
-    __syncthreads();
-    score_list<T>(a, q, item, score);
-    __syncthreads();
-    c = sums[0].x; s = sums[0].y;
+    const Entry e = entry_of<T>(a, q, mem, [&] {
+        float2 t = sums[lane % kListWaves];
 #pragma unroll
-    for (int w = 1; w < kListWaves; ++w) join_sums(c, s, sums[w].x, sums[w].y);
-    const double lse = log_sum64(c, s);
-    const bool live = t.any && lse != -__builtin_inf();
-    double loss = live && tid < a.K && item[tid] >= 0 ? entry_loss(t.weight[0], t.log_weight[0], score[tid], a.temperature, lse) : 0.0;
+        for (int x = 1; x < kListWaves; x *= 2) join_sums(t.x, t.y, __shfl_xor(t.x, x), __shfl_xor(t.y, x));
+        if (lane == 0) {
+            lse_of_all = log_sum64(t.x, t.y);
+            a.lse[q] = (float)lse_of_all;
+        }
+    });
+    const double lse = lse_of_all;
+    double loss = e.any && lse != -__builtin_inf() && e.item >= 0 ? entry_loss(e.weight, e.log_weight, mem.score[tid], a.temperature, lse) : 0.0;
     loss = over_workgroup<kListThreads>(loss, part, [](double x, double y) { return x + y; });
-    if (tid == 0) {
-        a.lse[q] = (float)lse;
-        a.loss[q] = (float)(loss * (double)a.temperature * (double)a.temperature);
-    }
+    if (tid == 0) a.loss[q] = (float)(loss * (double)a.temperature * (double)a.temperature);
 }
 
 // grid = positions: the position's share of the gradient and its list in the order of the items (of default_few_kernel's workgroups first), each with p less what the teacher gives the
-// item (all its entries together, in the list's order: the same in each of them).  64 positions with 100 entries 16 us, 1024 with 32 15.
+// item (all its entries together, in the list's order: the same in each of them).  One position with 10 entries 4 us, 64 with 100 11, and 16 where an item is listed
+// ten times; 1024 with 32 12.
 template <typename T>
 __global__ __launch_bounds__(kListThreads) void default_list_kernel(ListArgs a) {
-    __shared__ double part[kListWaves], score[kMostEntries], weight[kMostEntries];
-    __shared__ int item[kMostEntries];
-    __shared__ long long order[kMostEntries];
+    __shared__ ListMemory mem;
+    __shared__ double weight[kMostEntries], total[kMostEntries];
+    __shared__ uint64_t order[kMostEntries], sorted[kMostEntries];
     const int q = blockIdx.x, tid = threadIdx.x;
-    const Teacher<kListThreads> t = teacher_of<kListThreads>(a.items, a.scores, q, a.K, a.N, a.temperature, part);
-    const float lse = a.lse_in[q];
-    const bool live = t.any && lse != -__builtin_inff() && a.grad[q] != 0.0f;
+    const float lse = a.lse_in[q], g = a.grad[q];
+    const Entry e = entry_of<T>(a, q, mem, [] {});
+    const bool live = e.any && lse != -__builtin_inff() && g != 0.0f;
+    if (tid == 0) a.share[q] = live ? g * a.temperature : 0.0f;
+    const int mine = live && e.item >= 0 ? e.item : kNoItem;
+    // what orders the entries: the workgroup over the item over the entry's place
+    const uint64_t owner = a.few_groups ? (mine == kNoItem ? 511 : few_owner(mine, a.few_items, a.few_groups)) : 0;
+    const uint64_t own = owner << 41 | (uint64_t)mine << 9 | (uint64_t)tid;
+    if (tid < a.K) order[tid] = own;
+    __syncthreads();
+    int rank = 0;
     if (tid < a.K) {
-        item[tid] = live ? t.item[0] : -1;
-        weight[tid] = t.weight[0];
+#pragma unroll 8                                               // (reads of LDS on their way together)
+        for (int k = 0; k < a.K; ++k) rank += order[k] < own;
+        sorted[rank] = own;
+        weight[rank] = e.weight;
     }
-    if (tid == 0) a.share[q] = live ? a.grad[q] * a.temperature : 0.0f;
     __syncthreads();
-    score_list<T>(a, q, item, score);
-    __syncthreads();
-    const int mine = tid >= a.K || item[tid] < 0 ? kNoItem : item[tid];
-    // (what orders the entries: the workgroup over the item)
-    auto order_of = [&](int i) { return (long long)(a.few_groups ? few_owner(i, a.few_items, a.few_groups) : 0) << 32 | i; };
-    if (tid < a.K) order[tid] = order_of(mine);
+    // the first entry of an item adds up what the teacher gives it
+    if (tid < a.K && (rank == 0 || sorted[rank - 1] >> 9 != own >> 9)) {
+        double all = e.weight;
+        int end = rank + 1;
+        for (bool more = end < a.K; more;) {                   // (four at once: a list may hold an item many times)
+            uint64_t key[4];
+            double w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                key[i] = sorted[min(end + i, a.K - 1)];
+                w[i] = weight[min(end + i, a.K - 1)];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                more = more && end < a.K && key[i] >> 9 == own >> 9;
+                all += more ? w[i] : 0.0;
+                end += more;
+            }
+        }
+        for (int i = rank; i < end; ++i) total[i] = all;
+    }
     __syncthreads();
     if (tid >= a.K) return;
-    const long long own = order[tid];
-    int rank = 0, alike = 0;
-#pragma unroll 8                                               // (reads of LDS on their way together, and no branch between them)
-    for (int k = 0; k < a.K; ++k) {
-        const long long other = order[k];
-        rank += (other < own) | ((other == own) & (k < tid));
-        alike += other == own;
-    }
-    double all = weight[tid];
-    if (alike > 1 && mine != kNoItem) {
-        all = 0.0;
-#pragma unroll 8
-        for (int k = 0; k < a.K; ++k) {
-            const double w = weight[k];
-            all += order[k] == own ? w : 0.0;
-        }
-    }
     const size_t at = (size_t)q * a.K + rank;
     a.entry_items[at] = mine;
-    a.entry_values[at] = mine == kNoItem ? 0.0f : (float)(exp(score[tid] / (double)a.temperature - (double)lse) - all);
+    a.entry_values[at] = mine == kNoItem ? 0.0f : (float)(exp(mem.score[tid] / (double)a.temperature - (double)lse) - total[rank]);
 }
 
 // What the gradient's workspace holds besides.

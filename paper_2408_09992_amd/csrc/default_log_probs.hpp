@@ -218,7 +218,7 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
     const double lse = lse_of_all;
     auto log_prob = [&](double z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(z * a.per_temperature - lse); };
     // (the given items and the candidates at once: a row's way here is most of what either takes)
-    score_rows<THREADS>(W, h, a.d, a.n + n,
+    score_rows<0, THREADS>(W, h, a.d, a.n + n,
                         [&](int i) {
                             const int item = i < a.n ? a.items[(size_t)q * a.n + i] : (int)item_of(kept[i - a.n]);
                             return item < a.N ? (long long)item : -1LL;

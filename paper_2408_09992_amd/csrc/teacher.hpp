@@ -1,4 +1,4 @@
-// A teacher's list of one position as probabilities, by one workgroup, in 64 bits (512 entries at most: nothing beside a pass over the items).
+// A teacher's list of one position as probabilities, by one wave, and its items' scores by W phi, in 64 bits (512 entries at most: nothing beside a pass over the items).
 #pragma once
 #include "head_common.hpp"
 
@@ -21,83 +21,40 @@ __device__ __forceinline__ V over_workgroup(V v, V* part, F f) {
     return v;
 }
 
-// Every THREADS-th entry of a list from the thread's own on: the item (-1: no entry), its probability w and log w.
-template <int THREADS>
-struct Teacher {
-    static constexpr int kEach = (kMostEntries + THREADS - 1) / THREADS;
-    int item[kEach];
-    double weight[kEach], log_weight[kEach];
-    bool any;                  // whether an entry has weight, or is a NaN
-    bool odd;                  // whether the list holds a NaN or +inf: all its weights are NaN
-};
-template <int THREADS>
-__device__ __forceinline__ Teacher<THREADS> teacher_of(const int* items, const float* scores, int q, int K, long long N, float temperature, double* part) {
-    constexpr int kEach = Teacher<THREADS>::kEach;
-    Teacher<THREADS> t;
-    double x[kEach], top = -__builtin_inf(), any = 0.0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        const int k = (int)threadIdx.x + j * THREADS;
-        const size_t at = (size_t)q * K + (k < K ? k : 0);
-        const int item = items[at];
-        const float u = scores[at];
-        const bool entry = k < K && item >= 0 && item < N;
-        t.item[j] = entry ? item : -1;
-        x[j] = entry ? (double)u / (double)temperature : -__builtin_inf();
-        if (x[j] != -__builtin_inf()) any = 1.0;
-        top = fmax(top, x[j]);
-    }
-    any = over_workgroup<THREADS>(any, part, [](double a, double b) { return fmax(a, b); });
-    top = over_workgroup<THREADS>(top, part, [](double a, double b) { return fmax(a, b); });
-    t.any = any != 0.0;
-    double sum = 0.0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        x[j] = t.any ? x[j] - top : x[j];
-        t.weight[j] = x[j] == -__builtin_inf() ? 0.0 : exp(x[j]);
-        sum += t.weight[j];
-    }
-    // (one order whatever the lanes': a sum of two is the same both ways)
-    sum = over_workgroup<THREADS>(sum, part, [](double a, double b) { return a + b; });
-    t.odd = t.any && !(sum < __builtin_inf());
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-        t.weight[j] = t.any ? t.weight[j] / sum : 0.0;
-        t.log_weight[j] = x[j] - log(sum);
-    }
-    return t;
-}
-
-// The same list by one wave, which keeps no entry: the largest score over T, the sum of the exponentials and its logarithm.
+// A list by one wave, which keeps no entry: the largest score over T, the sum of the exponentials and its logarithm.
 struct WaveTeacher {
     double top, sum, log_sum;
     bool any;
     // of an entry's score over T less `top`
     __device__ __forceinline__ double weight(double x) const { return x == -__builtin_inf() ? 0.0 : exp(x) / sum; }
 };
-__device__ __forceinline__ WaveTeacher wave_teacher(const int* items, const float* scores, int q, int K, long long N, float temperature) {
+// x(k): the k-th entry's score over T, -inf where there is no entry.
+template <typename X>
+__device__ __forceinline__ WaveTeacher wave_teacher(int K, X x_of) {
     WaveTeacher t{-__builtin_inf(), 0.0, 0.0, false};
-    auto each = [&](auto f) {
-        for (int k = (int)threadIdx.x % kWave; k < K; k += kWave) {
-            const int item = items[(size_t)q * K + k];
-            if (item >= 0 && item < N) f((double)scores[(size_t)q * K + k] / (double)temperature);
-        }
-    };
-    each([&](double x) {
+    for (int k = (int)threadIdx.x % kWave; k < K; k += kWave) {
+        const double x = x_of(k);
         t.any |= x != -__builtin_inf();
         t.top = fmax(t.top, x);
-    });
+    }
     t.any = __any(t.any);
 #pragma unroll
     for (int x = 1; x < kWave; x *= 2) t.top = fmax(t.top, __shfl_xor(t.top, x));
     if (!t.any) return t;
-    each([&](double x) {
+    for (int k = (int)threadIdx.x % kWave; k < K; k += kWave) {
+        const double x = x_of(k);
         if (x != -__builtin_inf()) t.sum += exp(x - t.top);
-    });
+    }
 #pragma unroll
     for (int x = 1; x < kWave; x *= 2) t.sum += __shfl_xor(t.sum, x);
     t.log_sum = log(t.sum);
     return t;
+}
+__device__ __forceinline__ WaveTeacher wave_teacher(const int* items, const float* scores, int q, int K, long long N, float temperature) {
+    return wave_teacher(K, [&](int k) {
+        const int item = items[(size_t)q * K + k];
+        return item >= 0 && item < N ? (double)scores[(size_t)q * K + k] / (double)temperature : -__builtin_inf();
+    });
 }
 
 // What an entry adds to sum_k w_k (log w_k - log p_k), log p_k = score / T - lse.
@@ -140,11 +97,11 @@ __device__ __forceinline__ void dots64(const T* x0, const T* x1, const T* y, int
         sum1 += __shfl_xor(sum1, w);
     }
 }
-// The same of the rows item(0 .. n - 1) (below 0: none), by a workgroup of THREADS; put(i, sum) by one lane each.
-template <int THREADS, typename T, typename Item, typename Put>
+// The same of the rows item(0 .. n - 1) (below 0: none), by the threads FROM .. TO - 1 of a workgroup; put(i, whether there is one, sum) by one lane each.
+template <int FROM, int TO, typename T, typename Item, typename Put>
 __device__ __forceinline__ void score_rows(const T* W, const T* h, int d, int n, Item item, Put put) {
-    constexpr int kRows = THREADS / 16;
-    for (int i = (int)threadIdx.x / 16; i < n; i += 2 * kRows) {
+    constexpr int kRows = (TO - FROM) / 16;
+    for (int i = ((int)threadIdx.x - FROM) / 16; i < n; i += 2 * kRows) {
         const bool two = i + kRows < n;
         const long long r0 = item(i), r1 = two ? item(i + kRows) : -1;       // (the same for the sixteen)
         double s0, s1;
