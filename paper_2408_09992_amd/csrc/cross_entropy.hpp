@@ -21,6 +21,8 @@ constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 // Items a lane holds at once (loss, gradient): as many as leave the registers of four waves a SIMD room.
 template <int M> constexpr int units_of() { return M >= 64 ? 1 : M >= 32 ? 2 : 4; }
 template <int M, typename CT> constexpr int units_back_of() { return M * (int)sizeof(CT) >= 32 ? 1 : 2; }
+constexpr size_t kStatBytes = (size_t)kWaves * 4 * sizeof(float4);      // the waves' sums of up to four queries
+constexpr size_t kListedBytes = 4 * sizeof(int);     // behind them, of the log-probabilities: how many keys a query's region holds
 constexpr float kHeadroom = 40.0f;                   // (log2) how far a score may rise over a lane's reference before that moves
 constexpr float kFixedBits = 30.0f;                  // probabilities are whole multiples of 2^-62: 30 bits and 32 more below them
 
@@ -252,7 +254,7 @@ __device__ __forceinline__ void sum_items(const Args& a) {
     if constexpr (PROBS) { from = a.first; end = a.end; }
     const uint32_t lo = from + blockIdx.x * a.share, hi = (uint32_t)min((long long)lo + a.share, (long long)end);
     float c[Q], s[Q], t[Q], floor[Q];
-    __shared__ int listed[PROBS ? Q : 1];
+    int* listed = reinterpret_cast<int*>(smem + (size_t)a.m * entries<CT>(a.b) * Q * sizeof(float) + kStatBytes);          // (PROBS: [Q])
     if (PROBS && (int)threadIdx.x < Q) listed[threadIdx.x] = 0;
 #pragma unroll
     for (int r = 0; r < Q; ++r) {
@@ -666,16 +668,15 @@ inline void cut_items(Plan& p, long long N, long long workgroups, long long slot
     p.shares = (int)ceil_div(N, p.share);
 }
 
-constexpr size_t kStatBytes = (size_t)kWaves * 8 * sizeof(float2);
-
-inline bool plan_loss(Plan& p, long long N, int B, int m, int b, int code_bytes) {
+// `besides`: bytes of LDS behind the tables and the waves' sums.
+inline bool plan_loss(Plan& p, long long N, int B, int m, int b, int code_bytes, size_t besides = 0) {
     const size_t entry_floats = (size_t)m * entries_of(b, code_bytes);
     p.Q = B >= 3 ? 4 : B;
-    while (p.Q > 1 && entry_floats * 4 * p.Q + kStatBytes > kMaxLds) p.Q /= 2;
+    while (p.Q > 1 && entry_floats * 4 * p.Q + kStatBytes + besides > kMaxLds) p.Q /= 2;
     p.C = 1;
     p.kept = 0;
     p.ranges = 1;
-    p.lds = entry_floats * 4 * p.Q + kStatBytes;
+    p.lds = entry_floats * 4 * p.Q + kStatBytes + besides;
     if (p.lds > kMaxLds) return false;
     p.groups = (int)ceil_div(B, p.Q);
     // Two workgroups run on a compute unit where LDS holds the tables of both and its registers (64 a lane then) the rows, which those of 16

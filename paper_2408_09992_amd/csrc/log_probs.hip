@@ -196,7 +196,7 @@ bool lay_out(Layout& l, long long N, int B, int m, int b, int K, int code_bytes)
     for (long long done = 0, now; done < N; done += now) {
         Plan p;
         now = l.passes.after(done);
-        if (!plan_loss(p, now, B, m, b, code_bytes)) return false;
+        if (!plan_loss(p, now, B, m, b, code_bytes, kListedBytes)) return false;
         l.shares += p.shares;
         l.piece(done == 0 ? now : (long long)p.shares * p.share);
     }
@@ -244,7 +244,7 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
     Plan p;
     for (long long done = 0; done < N && e == hipSuccess; done = a.end) {
         const long long now = l.passes.after(done);
-        plan_loss(p, now, B, m, b, sizeof(CT));
+        plan_loss(p, now, B, m, b, sizeof(CT), kListedBytes);
         a.first = (uint32_t)done;
         a.end = (uint32_t)(done + now);
         a.share = p.share;
