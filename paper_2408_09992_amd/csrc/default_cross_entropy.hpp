@@ -247,13 +247,14 @@ __device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
 }
 
 // The share of the gradient of a row's position: 0 where there is none, no target, no item in play or no position.
-__device__ __forceinline__ float row_weight(const DenseArgs& a, int row) {
+__device__ __forceinline__ float row_weight(const DenseArgs& a, int row, bool shares) {
     const int q = min(position_of(a, row), a.B - 1);
-    if (a.share) return row < dz_rows(a) ? a.share[q] : 0.0f;
+    if (shares) return row < dz_rows(a) ? a.share[q] : 0.0f;
     const int t = a.targets[q];
     const float g = a.grad[q], lse = a.lse_in[q];              // (all three asked for at once)
     return row < dz_rows(a) && t >= 0 && t < a.N && lse != -__builtin_inff() ? g : 0.0f;
 }
+__device__ __forceinline__ float row_weight(const DenseArgs& a, int row) { return row_weight(a, row, a.share != nullptr); }
 // The queries in pieces of 16 bytes, from piece `first` on every `stride`-th, with zeros for positions that add nothing.
 // Float16: returns the power of two above these pieces' largest product of a query's element and its position's power.
 constexpr int kNoPower = -100000;
@@ -599,12 +600,12 @@ __device__ __forceinline__ f32x4_t multiply16(s16x8 x, s16x8 y, f32x4_t c) {
 }
 
 // Rows of W or of the queries from `row0` on into LDS: LOADS 16-byte pieces a thread; past the last row the last one again
-// (from the again-th, if not 0, the first ones), past a row's end zeros.
+// (from the again-th, if not 0, the first ones), past a row's end, and past `bytes` from the first row on, zeros.
 template <typename T, int D, int LOADS>
-__device__ __forceinline__ void bring_rows(const void* base, int d, long long row0, long long rows, unsigned char* to, int again = 0) {
+__device__ __forceinline__ void bring_rows(const void* base, int d, long long row0, long long rows, unsigned char* to, int again = 0, uint32_t bytes = kBufferBytes) {
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const size_t ld = (size_t)d * sizeof(T);
-    const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + (size_t)row0 * ld, 0, kBufferBytes, 0x00020000);
+    const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + (size_t)row0 * ld, 0, bytes, 0x00020000);
     const int last = (int)min(rows - row0, 65536LL) - 1;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
@@ -647,18 +648,6 @@ __device__ __forceinline__ void few_sums(const Args& a, long long from, long lon
         if (tid < kFew) listed[tid] = 0;
         if (tid == 0) waits = 0;
     }
-    // the queries' operands: position lane % 16 of a block's sixteen, eight k of every 32
-    s16x8 h[kParts][D / 32];
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-        const int pos = min((wave * kBlocksZ + i) % 4 * 16 + lane % 16, a.B - 1);
-#pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            const int at = (4 * k + lane / 16) * 8;
-            h[i][k] = s16x8{};
-            if (at < a.d) h[i][k] = *reinterpret_cast<const s16x8*>(static_cast<const T*>(a.H) + (size_t)pos * a.d + at);
-        }
-    }
     float c[kParts], s[kParts], t[kParts], floor[kParts];
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
@@ -669,13 +658,37 @@ __device__ __forceinline__ void few_sums(const Args& a, long long from, long lon
             if (a.lists.keep && !a.store && pos < a.B) floor[i] = a.lists.floor[pos];
         }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // (only W's loads are counted from here on, also by the compiler)
+    // (behind the last tile no memory is read)
+    auto bring = [&](long long tile, unsigned char* to) { bring_rows<T, D, kLoadsW>(a.W, a.d, from + min(tile, tiles - 1) * IT, a.N, to, 0, tile < tiles ? kBufferBytes : 0u); };
+    const long long by = gridDim.x;
+    // The queries come through the third tile's place, and the fourth's, while the first two tiles are on their way.  (By loads of each wave's own from memory, before the tiles',
+    // the loss of 10,000 items of 128, 64 positions, took 10.7 us instead of 8.2: sixteen loads one after the other of sixteen rows each.)
+    const long long first = blockIdx.x;
+    constexpr int kRowsEach = kFewBytes / 2 / D < kFew ? kFewBytes / 2 / D : kFew, kLoadsH = kRowsEach * D * 2 / 16 / kFewThreads;
+    bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, w2);
+    if constexpr (kRowsEach < kFew) bring_rows<T, D, kLoadsH>(a.H, a.d, min(kRowsEach, a.B - 1), a.B, w3);
+    __builtin_amdgcn_sched_barrier(0);                         // (the waits count on this order)
+    bring(first, w0);
+    __builtin_amdgcn_sched_barrier(0);
+    bring(first + by, w1);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kLoadsW) : "memory");
+    // their operands: position lane % 16 of a block's sixteen, eight k of every 32
+    s16x8 h[kParts][D / 32];
 #pragma unroll
-    for (int i = 0; i < kParts; ++i)
+    for (int i = 0; i < kParts; ++i) {
+        const int row0 = (wave * kBlocksZ + i) % 4 * 16;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) h[i][k] = RowsD::along(row0 < kRowsEach ? w2 : w3, row0 % kRowsEach + lane % 16, 4 * k + lane / 16);
+    }
+    // (in registers before the next tile takes their place; and only W's loads are counted from here on, also by the compiler)
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        if constexpr (PROBS) asm volatile("" : "+v"(floor[i]));
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) asm volatile("" : "+v"(h[i][k]));
-    auto bring = [&](long long tile, unsigned char* to) { bring_rows<T, D, kLoadsW>(a.W, a.d, from + min(tile, tiles - 1) * IT, a.N, to); };
-    const long long by = gridDim.x;
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    bring(first + 2 * by, w2);
     auto step = [&](long long tile, const unsigned char* w, unsigned char* next) {
         // the tile has come when two later ones alone are on their way; past the barrier that holds for all waves, which are done with `next`, too
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kLoadsW) : "memory");
@@ -731,10 +744,6 @@ __device__ __forceinline__ void few_sums(const Args& a, long long from, long lon
             }
         }
     };
-    const long long first = blockIdx.x;
-    bring(first, w0);
-    bring(first + by, w1);
-    bring(first + 2 * by, w2);
     // (without a way out of the loop's middle, from which the compiler would count fewer loads under way at its start)
     long long turns = first < tiles ? (tiles - first + by - 1) / by : 0, tile = first;
     for (; turns >= 4; turns -= 4, tile += 4 * by) {
@@ -789,7 +798,74 @@ __device__ __forceinline__ void few_sums(const Args& a, long long from, long lon
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseArgs a) { few_sums<T, D, false>(a, 0, a.N); }
+__global__ __launch_bounds__(kFewThreads, 2) void default_few_long_loss_kernel(DenseArgs a) { few_sums<T, D, false>(a, 0, a.N); }
+
+// The same sums where a workgroup has few tiles: queries and two tiles in LDS, and a quarter of the code, which a launch brings in, too.  Loss, us, by this kernel and by few_sums, 64
+// positions in bfloat16: 10,000 items of 64 7.3 | 7.9, of 128 7.4 | 8.2, of 256 8.0 | 8.9, of 512 10.2 | 10.5; 20,000 of 512 11.4 | 11.2; 300,000 of 256 31.2 | 31.6, of 512 61.6 | 55.7;
+// 600,000 of 64 24.2 | 24.6, of 128 31.0 | 31.2, of 256 60.3 | 54.8; 1.27M of 64 40.4 | 39.0, of 128 62.3 | 58.2.
+inline bool few_tiles_are_many(long long tiles, int groups, int d) { return tiles > (d > 256 ? 2LL : 19LL) * groups; }
+template <typename T, int D>
+__global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseArgs a) {
+    constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
+    using RowsD = Rows<D / 8>;
+    __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2];
+    __shared__ float2 stat[kWaves][kFew];
+    constexpr int kLoadsW = kFewBytes / 16 / kFewThreads, kLoadsH = kFew * D * 2 / 16 / kFewThreads;
+    constexpr int kBlocksZ = IT / 16 * 4 / kWaves, kParts = kBlocksZ < 4 ? kBlocksZ : 4;       // as in few_sums
+    const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const long long tiles = (a.N + IT - 1) / IT;
+    bring_rows<T, D, kLoadsH>(a.H, a.d, 0, a.B, h);
+    bring_rows<T, D, kLoadsW>(a.W, a.d, (long long)blockIdx.x * IT, a.N, w0);
+    float c[kParts], s[kParts];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) { c[i] = kLowest; s[i] = 0.0f; }
+    int turn = 0;
+    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++turn) {
+        const unsigned char* w = turn % 2 ? w1 : w0;
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the tile has come, its other buffer is free
+        bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
+#pragma unroll
+        for (int i = 0; i < kBlocksZ; ++i) {
+            const int block = wave * kBlocksZ + i, item0 = block / 4 * 16, pos = block % 4 * 16 + lane % 16;
+            f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k)
+                z = multiply16<T>(RowsD::along(w, item0 + lane % 16, 4 * k + lane / 16), RowsD::along(h, pos, 4 * k + lane / 16), z);
+            const int left = left_of(a.N - tile * IT - item0, 16) - lane / 16 * 4;
+            if (left < 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e >= left) z[e] = -__builtin_inff();
+            }
+            const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) * a.scale;
+            const int part = i % kParts;
+            if (__any(top > c[part] + kHeadroom)) {
+                if (top > c[part] + kHeadroom) raise_reference(c[part], s[part], top);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[part] += exp2_fast(fmaf(z[e], a.scale, -c[part]));
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");                  // (a last load into LDS may be under way)
+    for (int q = lane; q < kFew; q += kWave) stat[wave][q] = make_float2(kLowest, 0.0f);
+    wave_reads_after_writes();
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+#pragma unroll
+        for (int x = 16; x < kWave; x *= 2) {
+            const float c2 = __shfl_xor(c[i], x), s2 = __shfl_xor(s[i], x);
+            join_sums(c[i], s[i], c2, s2);
+        }
+        if (lane < 16) stat[wave][(wave * kBlocksZ + i) % 4 * 16 + lane] = make_float2(c[i], s[i]);
+    }
+    __syncthreads();
+    if (tid < a.B) {
+        float2 t = stat[0][tid];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) join_sums(t.x, t.y, stat[w][tid].x, stat[w][tid].y);
+        a.partial[(size_t)blockIdx.x * a.B + tid] = t;
+    }
+}
 
 // D: d rounded up to 64, 128, 256 or 512.  A tile holds 16384 / D items.  Bound by memory: W in, dW out, 2.6 GB for 1.27M items
 // of 512 elements in 515 to 550 us, 4.7 to 5.1 TB/s, where a copy reaches 4.73.
@@ -838,7 +914,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     // what default_rows_kernel does for more positions: these rows are a wave's lanes
     __shared__ float factor_of_all;
     if (wave == 0) {
-        const float g = row_weight(a, lane);
+        const float g = row_weight(a, lane, DISTIL);
         const float top = wave_top(weight_size(g));
         info[lane] = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
         if (blockIdx.x == 0) a.info[lane] = info[lane];
@@ -1068,14 +1144,16 @@ hipError_t launch_dh_cols(const DensePlan& p, const DenseArgs& a, hipStream_t st
     else return p.cols == 256 ? launch_dh<T, ROWS, 256>(a, st) : p.cols == 128 ? launch_dh<T, ROWS, 128>(a, st) : launch_dh<T, ROWS, 64>(a, st);
 }
 
+template <typename T, int D>
+hipError_t launch_few_loss_of(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+    const dim3 grid(p.groups), threads(kFewThreads);
+    if (few_tiles_are_many(ceil_div(a.N, few_items(a.d)), p.groups, a.d)) hipLaunchKernelGGL((default_few_long_loss_kernel<T, D>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((default_few_loss_kernel<T, D>), grid, threads, 0, st, a);
+    return hipGetLastError();
+}
 template <typename T>
 hipError_t launch_few_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
-    const dim3 grid(p.groups), threads(kFewThreads);
-    if (a.d > 256) hipLaunchKernelGGL((default_few_loss_kernel<T, 512>), grid, threads, 0, st, a);
-    else if (a.d > 128) hipLaunchKernelGGL((default_few_loss_kernel<T, 256>), grid, threads, 0, st, a);
-    else if (a.d > 64) hipLaunchKernelGGL((default_few_loss_kernel<T, 128>), grid, threads, 0, st, a);
-    else hipLaunchKernelGGL((default_few_loss_kernel<T, 64>), grid, threads, 0, st, a);
-    return hipGetLastError();
+    return a.d > 256 ? launch_few_loss_of<T, 512>(p, a, st) : a.d > 128 ? launch_few_loss_of<T, 256>(p, a, st) : a.d > 64 ? launch_few_loss_of<T, 128>(p, a, st) : launch_few_loss_of<T, 64>(p, a, st);
 }
 template <typename T, bool PARTS, bool DISTIL>
 hipError_t launch_few_of(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
