@@ -11,8 +11,8 @@
  *
  * Conventions are those of pqtopk.h and pqtopk_train.h (device pointers, row-major, caller's stream, no allocation, no
  * synchronisation, arguments checked before anything is enqueued, results the same from run to run), and besides:
- *   - T is a finite number of 1e-4 to 1e4.  Scores over it are float32 numbers of magnitude below 5.8e6: those below count as -inf,
- *     those above as +inf.
+ *   - T is a finite number of 1e-4 to 1e4.  Scores over it are float32 numbers of magnitude below 5.8e6: those below count as -inf (also a
+ *     mask of some other large number, -1e30 say: its items have the log-probability -inf, beside other items and alone), those above as +inf.
  *   - Item ids are int32.  One outside [0, N) names no item (padding).
  *   - A position all of whose scores are -inf has lse = -inf.
  */
@@ -34,8 +34,9 @@ extern "C" {
  *   lse            out  float [B]
  *   top_items      out  int32 [B][K]       by score descending, then id ascending, as pq_score_topk() ranks them.  K may be 0 (top_items and
  *   top_log_probs  out  float [B][K]         top_log_probs may be NULL then)
- * Table entries may be -inf (a sub-id out of play; entries below -1e32 count as that): items of score -inf have the log-probability -inf and come last, by id.  Of a position
- * that meets a NaN or +inf every number is NaN, top_items are different items of the catalogue in no particular order; no other position is touched by it.
+ * Table entries may be -inf (a sub-id out of play; entries below -1e32 count as that): items of score -inf have the log-probability -inf and
+ * come last, by id; those whose scores are numbers that count as -inf come before them, by their scores.  Of a position that meets a NaN or +inf
+ * every number is NaN, top_items are different items of the catalogue in no particular order; no other position is touched by it.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, B, m, b < 1; n, K < 0; b too large; K > N; N >= 2^31; T no positive number), PQ_ERR_UNSUPPORTED
  *         (K > PQ_MAX_K, n > 65536, T out of its range, and as pq_cross_entropy()), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
  */
@@ -68,7 +69,7 @@ int pq_default_log_probs(const void* W, const void* queries, const int* items, l
  *   teacher_scores  in   float [B][K]   -inf: an entry of no weight.  A list that holds a NaN or +inf makes the position's loss and gradient NaN
  *   loss            out  float [B];  lse  out  float [B]   log sum_i exp(r_qi / T)
  * A position whose list has no entry of weight (or all of whose scores are -inf) has the loss 0 and adds nothing to any gradient, whatever
- * its query holds.  An entry of weight whose own score is -inf makes the loss +inf, and the gradient stays finite.
+ * its query holds.  An entry of weight whose own score is -inf, or counts as that, makes the loss +inf, and the gradient stays finite.
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, B, m, b, K < 1; b too large; N >= 2^31; T no positive number), PQ_ERR_UNSUPPORTED (K > PQ_MAX_K,
  *         T out of its range, and as pq_cross_entropy()), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
  */

@@ -216,7 +216,7 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
         __syncthreads();
     }
     const double lse = lse_of_all;
-    auto log_prob = [&](double z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(z * a.per_temperature - lse); };
+    auto log_prob = [&](double z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(counted(z * a.per_temperature) - lse); };
     // (the given items and the candidates at once: a row's way here is most of what either takes)
     score_rows<0, THREADS>(W, h, a.d, a.n + n,
                         [&](int i) {

@@ -33,6 +33,9 @@ __device__ __forceinline__ void wave_reads_after_writes() {
 // a half: 2^(x log2e - c) is the exact product's distance from it, so with a rounded reference far outside (a mask of -1e30) the terms
 // would be 2 to the power of that rounding, inf or 0.  Scores below the range so count as -inf, those above it as +inf.
 constexpr float kLowest = -8388608.0f, kHighest = 8388608.0f;
+// A score over T whose exponential is 0 over any reference (2^-126 and what lies below it are): as a log-probability, too, it is -inf.
+constexpr double kLeastScore = ((double)kLowest - 126.0) / kLog2eDouble;
+__device__ __forceinline__ double counted(double x) { return x < kLeastScore ? -__builtin_inf() : x; }      // (a NaN stays one)
 __device__ __forceinline__ void join_sums(float& c, float& s, float c2, float s2) {
     const float top = fmaxf(c, c2);
     s = s * exp2_fast(c - top) + s2 * exp2_fast(c2 - top);

@@ -98,7 +98,7 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
         __syncthreads();
     }
     const double lse = lse_of_all;
-    auto log_prob = [&](float z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)((double)z * a.per_temperature - lse); };
+    auto log_prob = [&](float z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(counted((double)z * a.per_temperature) - lse); };
     if (own < a.n) a.log_probs[(size_t)q * a.n + own] = item >= 0 ? log_prob(given) : 0.0f;
     for (int i = own + THREADS; i < a.n; i += THREADS) {
         const int next = a.items[(size_t)q * a.n + i];

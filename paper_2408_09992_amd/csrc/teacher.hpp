@@ -59,7 +59,7 @@ __device__ __forceinline__ WaveTeacher wave_teacher(const int* items, const floa
 
 // What an entry adds to sum_k w_k (log w_k - log p_k), log p_k = score / T - lse.
 __device__ __forceinline__ double entry_loss(double weight, double log_weight, double score, float temperature, double lse) {
-    return weight == 0.0 ? 0.0 : weight * (log_weight - (score / (double)temperature - lse));
+    return weight == 0.0 ? 0.0 : weight * (log_weight - (counted(score / (double)temperature) - lse));
 }
 
 // Rows of W by one query in 64 bits (products of 16-bit elements are exact, and nearly always their sum): sums of d products by sixteen lanes of a wave, which

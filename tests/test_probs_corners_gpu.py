@@ -1,11 +1,50 @@
-"""Corners of the log-probabilities and the distillation: tables that fill LDS."""
+"""Corners of the log-probabilities and the distillation: tables that fill LDS, masks that are numbers.
+
+Bounds are those of test_log_probs_gpu.py, but of every position by its own scores, and by those alone that do not count as -inf."""
 import numpy as np
 import pytest
 import torch
 
+import test_distillation_gpu as teaching
 import test_log_probs_gpu as probs
 
 pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+LEAST = -(2.0 ** 23 + 126) * np.log(2.0)                        # scores over T below it count as -inf
+
+
+def check_by_position(pq, first, second, items, K, T=1.0):
+    N = first.shape[0]
+    got = probs.call(pq, first, second, items, K, T)
+    log_probs, entropy, lse, _, top_log_probs = [t.double() for t in got]
+    z64, chain, _, _ = probs.scores(first, second)
+    if chain is None:
+        terms, additions = second.double().abs() @ first.double().abs().t().contiguous(), first.shape[1] + 2
+    else:
+        codes = first.to(torch.int32).long()
+        terms, additions = sum(second[:, k, :][:, codes[:, k]].double().abs() for k in range(codes.shape[1])), codes.shape[1] - 1
+    play = z64 / T >= LEAST
+    z = torch.where(play, z64 / T, -np.inf)
+    size = torch.where(play, terms, 0.0).amax(1) / T
+    off = (additions + 2) * U * size
+    tol = off + U * (N / 512 + 64 + 4 * size + 4 * np.log(max(N, 2)))
+    want_lse = torch.logsumexp(z, 1)
+    empty = want_lse == -np.inf
+    assert torch.equal(lse[empty], want_lse[empty]) and ((lse - want_lse).abs() <= tol)[~empty].all()
+    lp = torch.where(empty[:, None], -np.inf, z - want_lse[:, None])
+    p_lp = torch.where(lp > -np.inf, lp.exp() * lp, 0.0)
+    want = -p_lp.sum(1)
+    around = torch.where(lp > -np.inf, lp.exp() * (lp + want[:, None]).abs(), 0.0).sum(1)
+    assert ((entropy - want).abs() <= 2 * (off + U * (4 * size + 64)) * around + U * (N / 512 + 64) * (64 + 2 * want)).all() and not entropy[empty].any()
+    there = (items >= 0) & (items < N)
+    best = probs.ranks(chain if chain is not None else z64, K)
+    assert torch.equal(got[3], best)
+    for out, want in ((log_probs, torch.where(there, lp.gather(1, torch.where(there, items, 0).long()), 0.0)), (top_log_probs, lp.gather(1, best.long()))):
+        low = want == -np.inf
+        assert torch.equal(out == -np.inf, low)
+        assert ((out - want).abs() <= (tol + off)[:, None] + 2 * U * want.abs())[~low].all()
+    return got
 
 
 @pytest.mark.parametrize("m,b,B", [(4, 2544, 3), (8, 1272, 5), (16, 636, 3), (8, 2544, 2), (1, 20352, 3), (8, 1271, 3)])
@@ -13,3 +52,59 @@ def test_tables_as_large_as_lds(pq, m, b, B):
     # (Q queries' tables of m b floats and the sums of the waves fill 160 KB to the last 16 bytes)
     probs.check(pq, *probs.draw_codes(20_001, m, b, B, 3, seed=m + b, wide=True), 10)
     probs.check(pq, *probs.draw_codes(3_001, m, b, B, 3, seed=m + b, wide=True), 10)
+
+
+@pytest.mark.parametrize("mask", [-1e30, -1e9, -6e6])
+@pytest.mark.parametrize("N,m,b,B,wide", [(9_000, 4, 256, 5, False), (30_000, 4, 256, 5, False), (30_000, 32, 256, 40, False), (20_000, 4, 300, 3, True)])
+def test_sub_ids_masked_by_a_number(pq, N, m, b, B, wide, mask):
+    codes, S, items = probs.draw_codes(N, m, b, B, 40, seed=N + m, wide=wide)
+    S[0, 1, ::2] = mask
+    S[1, 0, 1:] = mask                                          # about a hundred items are left: fewer than asked for
+    S[2] = mask                                                 # none
+    check_by_position(pq, codes, S, items, 300)
+
+
+@pytest.mark.parametrize("type", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B", [5, 130])
+def test_items_masked_by_a_number(pq, B, type):
+    N = 20_000
+    W, H, items = probs.draw_dense(N, 64, B, 40, type, seed=B)
+    W[:, 0], H[:, 0] = 0.0, 0.0
+    W[::3, 0], H[1, 0] = (-60_000.0, 60_000.0) if type == "f16" else (-1e30, 1.0)
+    check_by_position(pq, W, H, items, 50)
+
+
+def test_scores_at_the_border_of_what_counts(pq):
+    # one split, whose entries are the scores: whether an item counts is the same for its log-probability and for the log-sum of a position that has no other
+    border = 2.0 ** 23 * np.log(2.0)
+    S = torch.tensor([[-1.0, -border + 1, -border - 1, -border - 200, -1e30, 0.5], [-border + 1] * 6, [-border - 200] * 6], dtype=torch.float32, device="cuda")[:, None, :].contiguous()
+    codes = torch.arange(6, dtype=torch.uint8, device="cuda")[:, None].contiguous()
+    items = torch.arange(6, dtype=torch.int32, device="cuda").repeat(3, 1)
+    log_probs, _, lse, _, _ = pq.pq_log_probs(codes, S, items)
+    counts = torch.tensor([[True, True, True, False, False, True], [True] * 6, [False] * 6], device="cuda")
+    assert torch.equal(log_probs > -np.inf, counts) and torch.equal(lse > -np.inf, counts.any(1))
+
+
+@pytest.mark.parametrize("T", [0.5, 2.0])
+def test_listed_items_masked_by_a_number(pq, T):
+    codes, S, items, scores, grad = teaching.draw_codes(3_000, 4, 256, 5, 8, seed=5)
+    S[1, 2] = -1e30                                             # nothing is left: no loss, no gradient
+    S[2, 0, ::2] = -1e30                                        # listed items among those out of play: the loss is infinite, the gradient is not
+    masked = torch.where(S == -1e30, -np.inf, S)
+    for step in (teaching.forward, lambda *a: (teaching.backward(*a[:5], lse, grad, T),)):
+        got, want = step(pq, codes, S, items, scores, T), step(pq, codes, masked, items, scores, T)
+        lse = got[-1]
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+    loss, lse = teaching.forward(pq, codes, S, items, scores, T)
+    dS = teaching.backward(pq, codes, S, items, scores, lse, grad, T)
+    assert loss[1] == 0 and loss[2] == np.inf and loss[[0, 3, 4]].isfinite().all() and not dS[1].any() and dS.isfinite().all()
+    for type in ("f32", "bf16"):
+        for B in (5, 90):
+            W, H, items, scores, grad = teaching.draw_dense(3_000, 64, B, 8, type, seed=6)
+            W[:, 0], H[:, 0] = 0.0, 0.0
+            W[::2, 0], H[2, 0] = -1e30, 1.0
+            items[2] = torch.tensor([0, 1, 2, 3, 4, 5, 6, 7], device="cuda")
+            loss, lse = teaching.forward(pq, W, H, items, scores, T)
+            rest = torch.arange(B, device="cuda") != 2
+            assert loss[2] == np.inf and loss[rest].isfinite().all() and lse.isfinite().all()
