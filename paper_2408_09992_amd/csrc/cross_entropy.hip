@@ -34,7 +34,7 @@ int backward(const CT* codes, const float* S, const int* targets, const float* l
         return PQ_ERR_ALIGN;
     if (ws_bytes < backward_workspace(p, B, m, b)) return PQ_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    BackArgs a{codes, S, targets, lse, grad, N, B, m, b, p.kept, p.share, static_cast<uint64_t*>(ws), dS, kLog2e};
+    BackArgs a{codes, S, targets, lse, grad, N, B, m, b, p.kept, p.share, static_cast<uint64_t*>(ws), dS, kLog2e, (double)kLog2e};
     return record_hip_error(launch_backward<CT>(p, a, st));
 }
 

@@ -180,6 +180,7 @@ struct TeacherLossArgs : LossArgs {
     const float* scores;
     int K;
     float temperature;
+    double base;               // of log_sum64()
 };
 template <typename Args>
 __device__ __forceinline__ uint32_t code_of(const Args& a, int code_bytes, int item, int k) {
@@ -190,7 +191,7 @@ __device__ __forceinline__ uint32_t code_of(const Args& a, int code_bytes, int i
 __device__ __forceinline__ void finish_position(const TeacherLossArgs& a, float c, float s, int code_bytes, int q) {
     const int lane = threadIdx.x % kWave;
     const WaveTeacher t = wave_teacher(a.items, a.scores, q, a.K, a.N, a.temperature);
-    const double lse = log_sum64(c, s);
+    const double lse = log_sum64(c, s, a.base);
     double loss = 0.0;
     if (t.any && lse != -__builtin_inf()) {
         for (int e = lane; e < a.K; e += kWave) {
@@ -424,6 +425,7 @@ struct BackArgs {
     uint64_t* partial;         // [gridDim.x][B][m][b], where the items are shared
     float* dS;
     float scale;               // log2 e over the temperature
+    double base;               // what takes lse to where scores times `scale` are: scale over 1 / T
 };
 // The same where the target is a teacher's list: its probabilities are taken from the sums, whole multiples of 2^-62 as these are.
 struct TeacherBackArgs : BackArgs {
@@ -508,7 +510,7 @@ __global__ __launch_bounds__(kThreads) void cross_entropy_backward_kernel(Args a
     for (int r = 0; r < Q; ++r) {
         const int q = min(q0 + r, a.B - 1);
         const bool live = q0 + r < a.B && has_target(a, q);
-        at[r] = live ? a.lse[q] * kLog2e - kFixedBits : __builtin_inff();
+        at[r] = live ? (float)((double)a.lse[q] * a.base) - kFixedBits : __builtin_inff();
         any |= live;
     }
     __syncthreads();

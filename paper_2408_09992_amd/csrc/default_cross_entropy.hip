@@ -188,7 +188,7 @@ int pq_default_cross_entropy_backward(const void* W, const void* queries, const 
     const DensePlan p = plan_dense(N, B, d, type);
     if (workspace_bytes < p.bytes) return PQ_ERR_WORKSPACE;
     DenseArgs a{};
-    a.W = W; a.H = queries; a.targets = targets; a.N = N; a.B = B; a.d = d; a.scale = kLog2e;
+    a.W = W; a.H = queries; a.targets = targets; a.N = N; a.B = B; a.d = d; a.scale = kLog2e; a.base = (double)kLog2e;
     a.lse_in = lse; a.grad = grad_loss; a.dH = dqueries; a.dW = dW;
     set_gradient(a, p, workspace);
     hipStream_t st = static_cast<hipStream_t>(stream);

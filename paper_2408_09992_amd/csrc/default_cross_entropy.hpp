@@ -92,6 +92,7 @@ struct DenseArgs {
     int tiles_m, tiles_n;                              // of the launch
     int h_rows, h_cols, w_blocks;                      // tiles of dH; workgroups that make dW, where one launch makes both
     float scale;                                       // what scores are multiplied with: log2 e over the temperature
+    double base;                                       // what takes lse to where scores times `scale` are: scale over 1 / T
     // distillation: a position's gradient over its dz (0: it adds nothing; NULL: grad of those that have targets), and the entries of its
     // list, by item (kNoItem after the last): what p less the teacher's probability is there
     const float* share;
@@ -238,12 +239,13 @@ __device__ __forceinline__ int weight_power(float over_top) {
 __device__ __forceinline__ float weight_size(float g) { return fabsf(g) < __builtin_inff() ? fabsf(g) : 0.0f; }
 // Of a position with gradient g (0: it adds nothing), the largest of all being top.
 template <typename T>
-__device__ __forceinline__ RowInfo row_info(float g, float top, float lse) {
+__device__ __forceinline__ RowInfo row_info(float g, float top, float lse, double base) {
     if (g == 0.0f) return RowInfo{__builtin_inff(), 0.0f, 0.0f};
+    const float at = (float)((double)lse * base) - kDzBits;
     if constexpr (kOwnPowers<T>) {
         const int power = weight_power(g / top);
-        return RowInfo{lse * kLog2e - kDzBits, ldexpf(g / top, -power), top * ldexpf(1.0f / kDzScale, power)};
-    } else return RowInfo{lse * kLog2e - kDzBits, g / top, top / kDzScale};
+        return RowInfo{at, ldexpf(g / top, -power), top * ldexpf(1.0f / kDzScale, power)};
+    } else return RowInfo{at, g / top, top / kDzScale};
 }
 
 // The share of the gradient of a row's position: 0 where there is none, no target, no item in play or no position.
@@ -316,7 +318,7 @@ __global__ __launch_bounds__(1024) void default_rows_kernel(DenseArgs a) {
         if (blockIdx.x != 0) return;
     }
     for (int q = tid; q < a.padded; q += 1024) {
-        a.info[q] = row_info<T>(row_weight(a, q), top, a.lse_in[min(position_of(a, q), a.B - 1)]);
+        a.info[q] = row_info<T>(row_weight(a, q), top, a.lse_in[min(position_of(a, q), a.B - 1)], a.base);
     }
     if (tid == 0) a.factor[kOwnPowers<T> ? 1 : 0] = kOwnPowers<T> ? top : top / kDzScale;
 }
@@ -394,7 +396,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
     if constexpr (ROWS) {                                      // (every wave: lane r has row r's)
         const float g = row_weight(a, lane);
         const float top = wave_top(weight_size(g));
-        own_row = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
+        own_row = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)], a.base);
         if (!a.more) {
             copy_live<T>(a, (size_t)tile * Tile::kThreads + threadIdx.x, (size_t)a.tiles_m * Tile::kThreads);
             if (tile == 0 && threadIdx.x < kWave) a.info[lane] = own_row;
@@ -916,7 +918,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     if (wave == 0) {
         const float g = row_weight(a, lane, DISTIL);
         const float top = wave_top(weight_size(g));
-        info[lane] = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)]);
+        info[lane] = row_info<T>(g, top, a.lse_in[min(position_of(a, lane), a.B - 1)], a.base);
         if (blockIdx.x == 0) a.info[lane] = info[lane];
         if (kOwn) over_top[lane] = g == 0.0f ? 0.0f : g / top;
         target[lane] = !DISTIL && lane < dz_rows(a) ? a.targets[position_of(a, lane)] : -1;

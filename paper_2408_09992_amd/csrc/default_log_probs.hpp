@@ -164,7 +164,7 @@ struct DenseFinishArgs {
     const int* items;
     long long N;
     int B, d, n, K;
-    double per_temperature;                            // 1 / T
+    double per_temperature, base;                      // 1 / T; of log_sum64()
     const float4* partial;     // [B][groups], of all pieces
     int groups, stored, regions;                       // groups of all pieces; of the last piece what cut_list() takes
     long long region;
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
         float4 v = sums[lane % kWaves];
         join_wave<kWaves>(v.x, v.y, v.z);
         if (lane == 0) {
-            lse_of_all = log_sum64(v.x, v.y);
+            lse_of_all = log_sum64(v.x, v.y, a.base);
             a.lse[q] = (float)lse_of_all;
             a.entropy[q] = entropy_of(v.y, v.z);
         }
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
         __syncthreads();
     }
     const double lse = lse_of_all;
-    auto log_prob = [&](double z) { return lse == -__builtin_inf() ? -__builtin_inff() : (float)(counted(z * a.per_temperature) - lse); };
+    auto log_prob = [&](double z) { return log_prob_of(z * a.per_temperature, lse); };
     // (the given items and the candidates at once: a row's way here is most of what either takes)
     score_rows<0, THREADS>(W, h, a.d, a.n + n,
                         [&](int i) {

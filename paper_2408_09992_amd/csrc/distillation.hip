@@ -37,7 +37,8 @@ int distil(const CT* codes, const float* S, const int* items, const float* score
     if ((((uintptr_t)codes | (uintptr_t)ws) & 15) || (((uintptr_t)S | (uintptr_t)items | (uintptr_t)scores | (uintptr_t)loss | (uintptr_t)lse) & 3)) return PQ_ERR_ALIGN;
     if (ws_bytes < loss_workspace(p, B)) return PQ_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const TeacherLossArgs a{{codes, S, nullptr, N, B, m, b, p.share, static_cast<float2*>(ws), loss, lse, (float)(kLog2eDouble / temperature)}, items, scores, K, temperature};
+    const float scale = (float)(kLog2eDouble / temperature);
+    const TeacherLossArgs a{{codes, S, nullptr, N, B, m, b, p.share, static_cast<float2*>(ws), loss, lse, scale}, items, scores, K, temperature, base_of(scale, temperature)};
     return record_hip_error(launch_loss<CT>(p, a, st));
 }
 
@@ -58,7 +59,8 @@ int distil_backward(const CT* codes, const float* S, const int* items, const flo
     hipStream_t st = static_cast<hipStream_t>(stream);
     uint64_t* partial = static_cast<uint64_t*>(ws);
     float* weight = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + mass_bytes);
-    const TeacherBackArgs a{{codes, S, nullptr, lse, grad, N, B, m, b, p.kept, p.share, partial, dS, (float)(kLog2eDouble / temperature)}, items, scores, K, temperature, weight};
+    const float scale = (float)(kLog2eDouble / temperature);
+    const TeacherBackArgs a{{codes, S, nullptr, lse, grad, N, B, m, b, p.kept, p.share, partial, dS, scale, base_of(scale, temperature)}, items, scores, K, temperature, weight};
     return record_hip_error(launch_backward<CT>(p, a, st));
 }
 

@@ -36,6 +36,11 @@ constexpr float kLowest = -8388608.0f, kHighest = 8388608.0f;
 // A score over T whose exponential is 0 over any reference (2^-126 and what lies below it are): as a log-probability, too, it is -inf.
 constexpr double kLeastScore = ((double)kLowest - 126.0) / kLog2eDouble;
 __device__ __forceinline__ double counted(double x) { return x < kLeastScore ? -__builtin_inf() : x; }      // (a NaN stays one)
+// Of a score over T: at most 0, also where the sums' rounding has the likeliest item over that.
+__device__ __forceinline__ float log_prob_of(double x, double lse) {
+    const double v = counted(x) - lse;
+    return lse == -__builtin_inf() ? -__builtin_inff() : v > 0.0 ? 0.0f : (float)v;
+}
 __device__ __forceinline__ void join_sums(float& c, float& s, float c2, float s2) {
     const float top = fmaxf(c, c2);
     s = s * exp2_fast(c - top) + s2 * exp2_fast(c2 - top);
@@ -78,10 +83,12 @@ __device__ __forceinline__ float log_sum(float c, float s) {
     return s == 0.0f ? -__builtin_inff() : s < __builtin_inff() ? (c + __log2f(s)) * kLn2 : __builtin_nanf("");
 }
 
-// The same in 64 bits: reference and logarithm of some 20 each lose no bits to their sum.
-__device__ __forceinline__ double log_sum64(float c, float s) {
-    return s == 0.0f ? -__builtin_inf() : s < __builtin_inff() ? ((double)c + log2((double)s)) / kLog2eDouble : __builtin_nan("");
+// The same in 64 bits: reference and logarithm of some 20 each lose no bits to their sum.  base: what scores were multiplied with, times T.  That factor is log2 e / T
+// rounded to 24 bits, so by log2 e itself the log-sum would be off by up to 2^-24 of itself, and a score over T less it by as much.
+__device__ __forceinline__ double log_sum64(float c, float s, double base) {
+    return s == 0.0f ? -__builtin_inf() : s < __builtin_inff() ? ((double)c + log2((double)s)) / base : __builtin_nan("");
 }
+inline double base_of(float scale, float temperature) { return (double)scale * (double)temperature; }
 
 template <typename F>
 inline hipError_t allow_lds(F* kernel, size_t bytes) {

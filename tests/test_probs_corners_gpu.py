@@ -108,3 +108,41 @@ def test_listed_items_masked_by_a_number(pq, T):
             loss, lse = teaching.forward(pq, W, H, items, scores, T)
             rest = torch.arange(B, device="cuda") != 2
             assert loss[2] == np.inf and loss[rest].isfinite().all() and lse.isfinite().all()
+
+
+@pytest.mark.parametrize("T", [0.01, 0.07, 0.3, 3.0])
+@pytest.mark.parametrize("kind", ["u8", "lists", "u16", "f32", "bf16", "many"])
+def test_log_probabilities_of_large_scores_at_low_temperatures(pq, kind, T):
+    # One item of the score 20, and in position 1 a second one that is half as likely, all others 0 or below.  The sums' reference c is the largest score times log2 e / T as float32
+    # numbers, and what the item's own exponent is off it is kept (fma): its exponential is 2^x, |x| <= 2^-24 c, off by a unit (2 u), of which the others, below 2^-20 of it, take at most
+    # 2^-20 N; a second one adds as much and a rounding, in joins (some 40, of which one adds them and the others add nothing).  So log p is off by some 16 u; that the log-sum and
+    # its score were made by two factors log2 e / T, one of them rounded, would be up to 2^-24 of 20 / T.
+    N, B = 30_000, 200 if kind == "many" else 40 if kind == "lists" else 3
+    second = float(np.float32(20.0) - np.float32(T) * np.float32(np.log(2.0)))
+    if kind in ("f32", "bf16", "many"):
+        W, H = torch.zeros((N, 64), device="cuda"), torch.zeros((B, 64), device="cuda")
+        W[17, 0], W[29_999, 1], H[:, 0] = 4.0, 1.0, 5.0
+        H[1, 1] = second
+        type = torch.float32 if kind == "f32" else torch.bfloat16
+        first, queries = W.to(type), H.to(type)
+        z = queries.double() @ first.double().t().contiguous()
+    else:
+        m = 32 if kind == "lists" else 4
+        first = torch.full((N, m), 3, dtype=torch.uint8 if kind != "u16" else torch.uint16, device="cuda")
+        first.view(torch.uint8 if kind != "u16" else torch.int16)[17, 1] = 5
+        first.view(torch.uint8 if kind != "u16" else torch.int16)[29_999, 2] = 7
+        queries = torch.zeros((B, m, 300 if kind == "u16" else 256), device="cuda")
+        queries[:, 1, 5] = 20.0
+        queries[1, 2, 7] = second
+        z = torch.zeros((B, N), dtype=torch.float64, device="cuda")
+        z[:, 17] = 20.0
+        z[1, 29_999] = second
+    T32 = float(np.float32(T))
+    items = torch.tensor([17, 29_999], dtype=torch.int32, device="cuda").repeat(B, 1)
+    log_probs, _, lse, top, top_log_probs = probs.call(pq, first, queries, items, 2, T)
+    want_lse = torch.logsumexp(z / T32, 1)
+    want = (z / T32 - want_lse[:, None])[:, [17, 29_999]]
+    assert (log_probs <= 0).all() and (top_log_probs <= 0).all() and (top[:, 0] == 17).all() and torch.equal(top_log_probs[:, 0], log_probs[:, 0])
+    exact = 16 * U + (0 if T < 1 else 64 * U)                    # (at T = 3 the other items have most of the mass: N / 512 additions of a lane more)
+    assert ((log_probs.double() - want).abs() <= exact + U * want.abs()).all()
+    assert ((lse.double() - want_lse).abs() <= exact + U * want_lse.abs()).all()
