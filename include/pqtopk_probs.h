@@ -6,8 +6,8 @@
  *
  *     p_qi = exp(r_qi / T - lse_q)      lse_q = log sum_i exp(r_qi / T)      entropy_q = - sum_i p_qi log p_qi
  *
- * Scores are Eq. 5's sums of m sub-item scores (pq_log_probs, pq_distillation) or the default scorer's W phi (pq_default_*).  Neither
- * a score nor a probability of the N items is kept.
+ * Scores are Eq. 5's sums of m sub-item scores (pq_log_probs, pq_distillation) or the default scorer's W phi (pq_default_*).  The
+ * distillations, and log-probabilities without likeliest items, keep neither a score nor a probability of the N items.
  *
  * Conventions are those of pqtopk.h and pqtopk_train.h (device pointers, row-major, caller's stream, no allocation, no
  * synchronisation, arguments checked before anything is enqueued, results the same from run to run), and besides:
@@ -15,6 +15,11 @@
  *     mask of some other large number, -1e30 say: its items have the log-probability -inf, beside other items and alone), those above as +inf.
  *   - Item ids are int32.  One outside [0, N) names no item (padding).
  *   - A position all of whose scores are -inf has lse = -inf.
+ *   - Workspaces of the log-probabilities with K > 0 hold lists of scored items, 8 bytes for every position and item of a piece of the
+ *     catalogue (the likeliest few come from them): up to 16,384 items are one piece, of longer catalogues the largest has most of the items,
+ *     as far as 2 GiB of lists go (of more than 32,768 positions 4.3, where K is over 496).  64 positions of 1.27M items take 614 MiB, twice
+ *     what their scores would; 16 KB a position and up to 128 MiB of sums come on top.  By sub-ids and few positions there are no lists: the ranking
+ *     follows the pass.
  */
 #ifndef PQTOPK_PROBS_H
 #define PQTOPK_PROBS_H

@@ -359,6 +359,7 @@ inline bool many_lists(int B) { return B > kCUs; }
 // times the items before them: a list gets some growth * keep new keys in each.  How many pieces: a cut and what it stops take some 25 us, a candidate 25 to 150 ps over the chip (1024
 // positions, 116 kept, 840,000 candidates beside 262,144 items of 512 bfloat16 46 us; 512 positions by sub-ids, K = 100, counted at 25 547 us, at 50, which makes a piece more, 556).
 // `most`: of the candidates of a piece, where more than that take much longer each.
+// The lists of a piece, the only one among them, take kListBytes, or what `least` items take of so many positions (8192 of 65,535: 4.3 GB).
 constexpr long long kOnePiece = 16384, kListBytes = 1LL << 31;
 struct Passes {
     long long N, first, room, growth;
@@ -374,29 +375,49 @@ inline Passes passes_of(long long N, int B, int keep, double most = 1e300) {
     Passes p{N, N, N, 1, (int)(keep < N ? keep : N)};
     if (keep == 0) return p;
     const long long least = B <= 128 ? kOnePiece : (long long)round_up(8 * (size_t)keep, 4096);
-    if (N > kOnePiece && N > 2 * least) p.first = least;
+    p.room = kListBytes / 8 / B;
+    if ((N > kOnePiece && N > 2 * least) || (N > p.room && N > least)) p.first = least;
+    if (p.room < p.first) p.room = p.first;
     double best = 1e300;
     for (int pieces = 1; pieces <= 8; ++pieces) {
         const double growth = pow((double)N / (double)p.first, 1.0 / pieces), candidates = (double)B * keep * growth, cost = pieces * (25.0 + 2.5e-5 * candidates);
         if (cost < best || (double)B * keep * (double)p.growth > most) { best = cost; p.growth = (long long)ceil(growth); }
     }
-    p.room = kListBytes / 8 / B > p.first ? kListBytes / 8 / B : p.first;
     return p;
 }
+
+// Where the sums of a piece's groups go, among a position's `slots`: behind those of the pieces before, or, where these would take more than kSumBytes (one position has some hundred
+// groups in a piece, 65,535 have a hundred pieces a million items), in their places, joined with what is there.
+constexpr size_t kSumBytes = (size_t)64 << 20;
+struct Sums {
+    int slots = 0, most = 0;
+    bool joined = false;
+    void piece(int groups) { slots += groups; most = groups > most ? groups : most; }
+    void lay_out(int B) {
+        joined = (size_t)slots * B * sizeof(float4) > kSumBytes;
+        if (joined) slots = most;
+    }
+    size_t bytes(int B) const { return (size_t)slots * B * sizeof(float4); }
+    // after a piece of so many groups: where the next one's sums go, and how many places there hold sums already
+    void advance(int groups, int& done, int& written) const {
+        if (joined) written = groups > written ? groups : written;
+        else done += groups;
+    }
+};
 
 // Where the lists lie in a workspace, behind `at` bytes.
 struct ListLayout {
     long long cap = 0;
     size_t keys_at, counts_at, kept_at, kept_count_at, floor_at, bytes;
     void piece(long long keys) { cap = keys > cap ? keys : cap; }     // a piece whose regions take so many keys
-    void lay_out(size_t at, int B, int keep) {
-        const size_t on = keep ? 1 : 0;
+    void lay_out(size_t at, int B, const Passes& p) {
+        const size_t lists = p.keep ? B : 0, on = p.first < p.N ? lists : 0;             // (one piece is cut at the end alone, from where its keys lie)
         keys_at = round_up(at, 256);
-        counts_at = keys_at + round_up(on * B * cap * sizeof(uint64_t), 256);
-        kept_at = counts_at + round_up(on * B * kMostRegions * sizeof(int), 256);
-        kept_count_at = kept_at + round_up(on * B * kMostKept * sizeof(uint64_t), 256);
-        floor_at = kept_count_at + round_up(on * B * sizeof(int), 256);
-        bytes = floor_at + round_up(on * B * sizeof(float), 256);
+        counts_at = keys_at + round_up(lists * cap * sizeof(uint64_t), 256);
+        kept_at = counts_at + round_up(on * kMostRegions * sizeof(int), 256);
+        kept_count_at = kept_at + round_up(on * kMostKept * sizeof(uint64_t), 256);
+        floor_at = kept_count_at + round_up(on * sizeof(int), 256);
+        bytes = floor_at + round_up(on * sizeof(float), 256);
     }
     Lists lists(unsigned char* ws, int keep) const {
         return Lists{reinterpret_cast<uint64_t*>(ws + keys_at), reinterpret_cast<int*>(ws + counts_at), reinterpret_cast<uint64_t*>(ws + kept_at),

@@ -226,7 +226,7 @@ struct ProbsArgs {
     uint32_t first, end;       // the piece's items
     int store;                 // whether all its scores go to the lists
     float4* partial;           // [B][partials], of all pieces: (reference, sum, weighted sum); of this one from `done` on
-    int partials, done;
+    int partials, done, written;                       // of its places the first `written` hold earlier pieces' sums
     Lists lists;
     float* finite;             // [B][m][b], or NULL: the tables as a ranking takes them, held within +-1e32, 0 for a NaN
 };
@@ -380,7 +380,9 @@ __device__ __forceinline__ void sum_items(const Args& a) {
 #pragma unroll 2                                               // (fifteen at once would be the kernel's most registers)
             for (int w = 1; w < kWaves; ++w) join_sums(sums.x, sums.y, sums.z, stat[w * Q + wave].x, stat[w * Q + wave].y, stat[w * Q + wave].z);
             if (lane == 0) {
-                a.partial[(size_t)q * a.partials + a.done + blockIdx.x] = sums;
+                float4& to = a.partial[(size_t)q * a.partials + a.done + blockIdx.x];
+                if ((int)blockIdx.x < a.written) join_sums(sums.x, sums.y, sums.z, to.x, to.y, to.z);
+                to = sums;
                 if (a.lists.keep && !a.store) a.lists.counts[(size_t)q * kMostRegions + blockIdx.x] = listed[wave];
             }
         } else {

@@ -793,7 +793,9 @@ __device__ __forceinline__ void few_sums(const Args& a, long long from, long lon
             else join_sums(v.x, v.y, stat[w][tid].x, stat[w][tid].y);
         }
         if constexpr (PROBS) {
-            a.partial[(size_t)tid * a.partials + a.done + blockIdx.x] = v;
+            float4& to = a.partial[(size_t)tid * a.partials + a.done + blockIdx.x];
+            if ((int)blockIdx.x < a.written) join_sums(v.x, v.y, v.z, to.x, to.y, to.z);
+            to = v;
             if (a.lists.keep && !a.store) a.lists.counts[(size_t)tid * kMostRegions + blockIdx.x] = listed[tid];
         } else a.partial[(size_t)blockIdx.x * a.B + tid] = v;
     }

@@ -29,6 +29,7 @@ DensePlan plan_piece(long long items, int B, int d, int type, bool listed, int& 
             }
             p.groups = (int)ceil_div(p.item_tiles, p.tiles_each);
         }
+        if (listed) p.tiles_each = (int)ceil_div(p.item_tiles, p.groups);         // (as many places as the groups have tiles, and few more)
         region = (long long)p.tiles_each * p.loss_items / shares;
     }
     regions = p.groups * shares;
@@ -37,20 +38,20 @@ DensePlan plan_piece(long long items, int B, int d, int type, bool listed, int& 
 
 struct Layout : ListLayout {
     Passes passes;
-    int groups;
+    Sums sums;
 };
 Layout lay_out(long long N, int B, int d, int type, int K) {
     Layout l;
     // (few positions' candidates wait in LDS: 64 positions of 1.28M items of 128, K = 100, one piece after the first 187 us, two 145)
     l.passes = passes_of(N, B, keep_of(K), plan_dense(N, B, d, type).few ? 0.8 * kFewWaiting * kCUs : 1e300);
-    l.groups = 0;
     for (long long done = 0, now, region; done < N; done += now) {
         int regions;
         now = l.passes.after(done);
-        l.groups += plan_piece(now, B, d, type, K != 0, regions, region).groups;
+        l.sums.piece(plan_piece(now, B, d, type, K != 0, regions, region).groups);
         l.piece(done == 0 ? now : regions * region);
     }
-    l.ListLayout::lay_out((size_t)l.groups * B * sizeof(float4), B, K);
+    l.sums.lay_out(B);
+    l.ListLayout::lay_out(l.sums.bytes(B), B, l.passes);
     return l;
 }
 
@@ -71,7 +72,7 @@ hipError_t pass(const Layout& l, DenseProbsArgs a, DenseFinishArgs f, int type, 
         a.store = f.K != 0 && done == 0;
         a.item_tiles = p.item_tiles; a.tiles_each = p.tiles_each; a.groups = p.groups; a.position_tiles = p.position_tiles;
         e = dense_probs<T>(p, a, st);
-        a.done += p.groups;
+        l.sums.advance(p.groups, a.done, a.written);
         if (e == hipSuccess && f.K && a.end < a.N) e = launch_select(a.lists, a.B, a.store ? (int)now : 0, f.regions, a.region, st);
         f.stored = a.store ? (int)now : 0;
         f.region = a.region;
@@ -108,9 +109,9 @@ int pq_default_log_probs(const void* W, const void* queries, const int* items, l
     DenseProbsArgs a{};
     a.W = W; a.H = queries; a.N = N; a.B = B; a.d = d; a.scale = (float)(kLog2eDouble / temperature);
     a.partial = reinterpret_cast<float4*>(ws);
-    a.partials = l.groups;
+    a.partials = l.sums.slots;
     a.lists = l.lists(ws, l.passes.keep);
-    const DenseFinishArgs f{W, queries, items, N, B, d, n, K, 1.0 / temperature, base_of(a.scale, temperature), a.partial, l.groups, 0, 0, 0, a.lists, log_probs, entropy, lse, top_items, top_log_probs};
+    const DenseFinishArgs f{W, queries, items, N, B, d, n, K, 1.0 / temperature, base_of(a.scale, temperature), a.partial, l.sums.slots, 0, 0, 0, a.lists, log_probs, entropy, lse, top_items, top_log_probs};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return pqk::record_hip_error(type == PQ_FLOAT32 ? pass<float>(l, a, f, type, st) : type == PQ_BFLOAT16 ? pass<__bf16>(l, a, f, type, st) : pass<_Float16>(l, a, f, type, st));
 }

@@ -21,7 +21,7 @@ struct DenseProbsArgs {
     long long item_tiles;
     int tiles_each, groups, position_tiles;
     float4* partial;                                   // [B][partials], of all pieces: (reference, sum, weighted sum); of this one from `done` on
-    int partials, done;
+    int partials, done, written;                       // of its places the first `written` hold earlier pieces' sums
     Lists lists;
     long long region;                                  // places of a region
 };
@@ -151,7 +151,9 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
         float4 v = stat[0][threadIdx.x];
 #pragma unroll
         for (int w = 1; w < kRowWaves; ++w) join_sums(v.x, v.y, v.z, stat[w][threadIdx.x].x, stat[w][threadIdx.x].y, stat[w][threadIdx.x].z);
-        a.partial[(size_t)q * a.partials + a.done + group] = v;
+        float4& to = a.partial[(size_t)q * a.partials + a.done + group];
+        if (group < a.written) join_sums(v.x, v.y, v.z, to.x, to.y, to.z);
+        to = v;
     }
 }
 

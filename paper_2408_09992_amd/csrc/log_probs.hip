@@ -176,7 +176,7 @@ hipError_t go_m(const Plan& p, const ProbsArgs& a, hipStream_t st) {
 // Where the workspace's parts lie.
 struct Layout : ListLayout {
     Passes passes;
-    int shares;
+    Sums sums;
     size_t topk_bytes, finite_at, ranked_at, topk_at;          // (topk_bytes: 0 where lists are kept)
 };
 // Whether the ranking's scan follows the pass instead of lists.  It looks the items up again, in chains that grow with m; lists take launches, more of them for a larger K, and cuts
@@ -192,15 +192,16 @@ size_t topk_bytes_of(long long N, int B, int m, int b, int K, int code_bytes) {
 bool lay_out(Layout& l, long long N, int B, int m, int b, int K, int code_bytes) {
     l.topk_bytes = topk_bytes_of(N, B, m, b, K, code_bytes);
     l.passes = passes_of(N, B, l.topk_bytes ? 0 : K);
-    l.shares = 0;
+    l.sums = Sums();
     for (long long done = 0, now; done < N; done += now) {
         Plan p;
         now = l.passes.after(done);
         if (!plan_loss(p, now, B, m, b, code_bytes, kListedBytes)) return false;
-        l.shares += p.shares;
+        l.sums.piece(p.shares);
         l.piece(done == 0 ? now : (long long)p.shares * p.share);
     }
-    l.ListLayout::lay_out((size_t)l.shares * B * sizeof(float4), B, l.passes.keep);
+    l.sums.lay_out(B);
+    l.ListLayout::lay_out(l.sums.bytes(B), B, l.passes);
     if (l.topk_bytes) {
         l.finite_at = l.bytes;
         l.ranked_at = l.finite_at + round_up((size_t)B * m * b * sizeof(float), 256);
@@ -237,7 +238,7 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
     hipStream_t st = static_cast<hipStream_t>(stream);
     unsigned char* ws = static_cast<unsigned char*>(workspace);
     const Lists lists = l.lists(ws, l.passes.keep);
-    ProbsArgs a{codes, S, N, B, m, b, 0, (float)(kLog2eDouble / temperature), 0, 0, 0, reinterpret_cast<float4*>(ws), l.shares, 0, lists,
+    ProbsArgs a{codes, S, N, B, m, b, 0, (float)(kLog2eDouble / temperature), 0, 0, 0, reinterpret_cast<float4*>(ws), l.sums.slots, 0, 0, lists,
                 l.topk_bytes ? reinterpret_cast<float*>(ws + l.finite_at) : nullptr};
     float* ranked = l.topk_bytes ? reinterpret_cast<float*>(ws + l.ranked_at) : nullptr;
     hipError_t e = hipSuccess;
@@ -250,7 +251,7 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
         a.share = p.share;
         a.store = lists.keep != 0 && done == 0;
         e = go_m<CT>(p, a, st);
-        a.done += p.shares;
+        l.sums.advance(p.shares, a.done, a.written);
         if (e == hipSuccess && lists.keep && a.end < N) e = launch_select(lists, B, a.store ? (int)now : 0, p.shares, p.share, st);
     }
     if (e == hipSuccess && ranked) {
@@ -259,7 +260,7 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
         if (rc != PQ_OK) return rc;
     }
     if (e == hipSuccess) {
-        const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), 1.0 / temperature, base_of(a.scale, temperature), reinterpret_cast<const float4*>(ws), l.shares,
+        const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), 1.0 / temperature, base_of(a.scale, temperature), reinterpret_cast<const float4*>(ws), l.sums.slots,
                            a.store ? (int)N : 0, p.shares, p.share, lists, ranked, out, entropy, lse, top_items, top_log_probs};
         if (many_lists(B) || lists.keep == 0) hipLaunchKernelGGL(log_probs_finish_kernel<256>, dim3(B), dim3(256), 0, st, f);
         else hipLaunchKernelGGL(log_probs_finish_kernel<1024>, dim3(B), dim3(1024), 0, st, f);

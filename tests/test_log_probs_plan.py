@@ -59,3 +59,25 @@ def test_nothing_lies_in_lds_that_the_plan_does_not_count(pqlib_path, tmp_path):
         if "log_probs_kernel" in name:
             found[name] = int(re.search(r"\.group_segment_fixed_size: +(\d+)", kernel).group(1))
     assert len(found) == 32 and not {k: v for k, v in found.items() if v}
+
+
+def test_no_workspace_is_larger_than_its_lists(pqlib_path):
+    # the lists' 2 GiB, or what 4096 items take (8192 where a list keeps more than 512); of positions whose items come in pieces 16 KB more, and 64 MiB of sums or a piece's
+    import ctypes
+    L = ctypes.CDLL(pqlib_path)
+    sizes = []
+    for name, rest in (("pq_log_probs", (8, 256)), ("pq_log_probs_u16", (8, 1000)), ("pq_default_log_probs", (64, 1)), ("pq_default_log_probs", (512, 0)), ("pq_default_log_probs", (512, 1))):
+        f = getattr(L, name + "_workspace_bytes")
+        f.argtypes, f.restype = [ctypes.c_longlong] + [ctypes.c_int] * 4, ctypes.c_size_t
+        sizes.append((name, lambda N, B, K, f=f, rest=rest: f(N, B, *rest, K)))
+    for N in (1, 1000, 4097, 12_000, 16_384, 16_385, 50_000, 300_000, 1_271_638, 28_457_277, 2 ** 30, 2 ** 31 - 1):
+        for B in (1, 64, 65, 128, 129, 1024, 8192, 16_384, 30_000, 60_000, 65_535):
+            for K in (1, 10, 100, 512):
+                if K > N:
+                    continue
+                for name, size in sizes:
+                    keep = K + 16 if "default" in name else K
+                    lists = max(2 ** 31, 8 * B * (4096 if keep <= 512 else 8192))
+                    assert 0 < size(N, B, K) <= lists + B * (16_384 + 64) + 2 ** 27, (name, N, B, K, size(N, B, K))
+    for name, size in sizes:                                     # in one piece nothing is kept between pieces
+        assert size(4000, 2000, 10) < 8 * 2000 * 4096 + 2 ** 23

@@ -1,4 +1,5 @@
-"""Corners of the log-probabilities and the distillation: tables that fill LDS, masks that are numbers.
+"""Corners of the log-probabilities and the distillation: tables that fill LDS, masks that are numbers, low temperatures, lists
+that are kept to their size.
 
 Bounds are those of test_log_probs_gpu.py, but of every position by its own scores, and by those alone that do not count as -inf."""
 import numpy as np
@@ -14,9 +15,11 @@ U = 2.0 ** -24
 LEAST = -(2.0 ** 23 + 126) * np.log(2.0)                        # scores over T below it count as -inf
 
 
-def check_by_position(pq, first, second, items, K, T=1.0):
+def check_by_position(pq, first, second, items, K, T=1.0, rows=None):
     N = first.shape[0]
     got = probs.call(pq, first, second, items, K, T)
+    if rows is not None:                                        # (of many positions these are looked at)
+        got, second, items = [t[rows] for t in got], second[rows], items[rows]
     log_probs, entropy, lse, _, top_log_probs = [t.double() for t in got]
     z64, chain, _, _ = probs.scores(first, second)
     if chain is None:
@@ -146,3 +149,34 @@ def test_log_probabilities_of_large_scores_at_low_temperatures(pq, kind, T):
     exact = 16 * U + (0 if T < 1 else 64 * U)                    # (at T = 3 the other items have most of the mass: N / 512 additions of a lane more)
     assert ((log_probs.double() - want).abs() <= exact + U * want.abs()).all()
     assert ((lse.double() - want_lse).abs() <= exact + U * want_lse.abs()).all()
+
+
+@pytest.mark.parametrize("N,B,K", [(16_384, 20_000, 10), (12_000, 65_535, 3), (270_001, 65_535, 5)])
+def test_lists_that_are_kept_to_their_size(pq, N, B, K):
+    # catalogues that one piece would hold, but for so many positions; and pieces whose sums take the places of those before
+    rows = torch.randint(0, B, (40,), generator=torch.Generator().manual_seed(N)).cuda()
+    rows[0], rows[1] = 0, B - 1
+    check_by_position(pq, *probs.draw_codes(N, 4, 64, B, 2, seed=N), K, rows=rows)
+    for type in ("f32", "bf16"):
+        check_by_position(pq, *probs.draw_dense(N, 8, B, 2, type, seed=B), K, rows=rows)
+    torch.cuda.empty_cache()
+
+
+def test_sums_of_many_pieces_of_few_positions(pq):
+    # 286 pieces of 2^28 / 64 items, whose sums of 256 groups share their places.  All scores but four are 0: every lane's sum is a whole number
+    N, B = 1_200_000_000, 64
+    W, H = torch.zeros((N, 8), dtype=torch.bfloat16, device="cuda"), torch.zeros((B, 8), dtype=torch.bfloat16, device="cuda")
+    H[:, 0] = 1.0
+    marked = torch.tensor([N - 1, 1_100_000_001, 17, 300_000_000], device="cuda")
+    W[marked, 0] = torch.tensor([20.0, 18.0, 16.0, 14.0], device="cuda").bfloat16()
+    assert pq.pq_default_log_probs_workspace_bytes(N, B, 8, 1, 4) < 2 ** 31 + 2 ** 25
+    log_probs, entropy, lse, top, lp = pq.pq_default_log_probs(W, H, marked.to(torch.int32).repeat(B, 1).contiguous(), 4)
+    assert torch.equal(top.long(), marked.repeat(B, 1)) and torch.equal(lp, log_probs)
+    z = torch.cat([W[marked, 0].double(), torch.zeros(1, dtype=torch.float64, device="cuda")])
+    count = torch.tensor([1.0, 1.0, 1.0, 1.0, N - 4.0], dtype=torch.float64, device="cuda")
+    want = torch.log((count * z.exp()).sum())
+    p = (z - want).exp()
+    # a join adds 4 u of a sum; a position's sums meet in some 300
+    assert ((lse.double() - want).abs() <= 1200 * U).all() and ((entropy.double() - (count * p * (want - z)).sum()).abs() <= 1200 * U * 64).all()
+    del W
+    torch.cuda.empty_cache()
