@@ -180,3 +180,64 @@ def test_sums_of_many_pieces_of_few_positions(pq):
     assert ((lse.double() - want).abs() <= 1200 * U).all() and ((entropy.double() - (count * p * (want - z)).sum()).abs() <= 1200 * U * 64).all()
     del W
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("K", [1, 40, 100, 512])
+@pytest.mark.parametrize("N,m,b,B", [(60_000, 8, 256, 330), (60_000, 4, 256, 1_300), (60_000, 32, 256, 100), (60_000, 16, 300, 400), (60_000, 4, 300, 1_300)])
+def test_lists_of_sub_ids_in_the_worst_orders(pq, N, m, b, B, K):
+    # (more lookups than the ranking is asked for, N B m^2 over 1.2e9, or over 6e9: pieces, floors, regions.)  Every third position's later items are all better, so that whatever a
+    # region has room for comes to it, every third's are worse, and every third's are alike: sums of whole numbers over 4096 are exact, ties go to the lowest id
+    assert N * B * m * m > (1.2e9 if K <= 40 or B >= 128 else 6e9)
+    rise = torch.arange(N, device="cuda")
+    digits = torch.stack([rise // 256, rise % 256], 1)
+    codes = torch.cat([digits, torch.full((N, m - 2), 9, device="cuda")], 1).to(torch.uint8 if b == 256 else torch.uint16).contiguous()
+    S = torch.zeros((B, m, b), device="cuda")
+    S[:, 0, :256], S[:, 1, :256] = torch.arange(256, device="cuda") / 16, torch.arange(256, device="cuda") / 4096
+    S[1::3] *= -1
+    S[2::3] = 0.0
+    _, _, lse, top, lp = probs.call(pq, codes, S, None, K)
+    assert (top[::3] == rise.flip(0)[:K]).all() and (top[1::3] == rise[:K]).all() and (top[2::3] == rise[:K]).all()
+    z = rise.double() / 4096
+    for q, x in ((0, z), (1, -z), (2, 0 * z)):
+        want = torch.logsumexp(x, 0)
+        tol = U * (N / 512 + 64 + 4 * 15 + 4 * np.log(N)) + 2 * U * 15
+        assert ((lse[q::3].double() - want).abs() <= tol).all()
+        assert ((lp[q::3].double() - (x[top[q].long()] - want)).abs() <= tol + 2 * U * 30).all()
+
+
+@pytest.mark.parametrize("K", [5, 100, 512])
+@pytest.mark.parametrize("type,N,d", [("bf16", 60_000, 64), ("f16", 200_000, 64), ("f16", 200_000, 136), ("bf16", 60_000, 304)])
+def test_more_candidates_of_few_positions_than_wait(pq, type, N, d, K):
+    # 64 positions whose later items are all better: every score passes its floor, thousands of them a workgroup, of which 1024 wait in LDS and the others go to memory at once
+    B = 64
+    rise = torch.arange(N, device="cuda")
+    W, H = torch.zeros((N, d), device="cuda"), torch.zeros((B, d), device="cuda")
+    W[:, 0], W[:, 1] = (rise // 256).float(), (rise % 256).float()
+    H[:, 0], H[:, 1] = 2.0 ** -4, 2.0 ** -12
+    H[1::4] *= -1
+    _, _, lse, top, lp = probs.call(pq, W.to(probs.TYPES[type]), H.to(probs.TYPES[type]), None, K)
+    up = torch.ones(B, dtype=torch.bool, device="cuda")
+    up[1::4] = False
+    assert (top[up] == rise.flip(0)[:K]).all() and (top[~up] == rise[:K]).all()
+    z = rise.double() / 4096
+    size = N / 4096
+    tol = U * (N / 512 + 64 + 4 * size + 4 * np.log(N)) + 2 * U * size
+    assert ((lse[up].double() - torch.logsumexp(z, 0)).abs() <= tol).all() and ((lse[~up].double() - torch.logsumexp(-z, 0)).abs() <= tol).all()
+    assert ((lp[up].double() - (z.flip(0)[:K] - torch.logsumexp(z, 0))).abs() <= tol + 2 * U * size).all()
+
+
+@pytest.mark.parametrize("N,m,b,B,K,wide", [(600_000, 16, 256, 110, 60, False), (1_100_000, 8, 300, 130, 60, True), (1_271_638, 8, 256, 64, 20, False), (1_271_638, 4, 256, 64, 40, False),
+                                            (90_001, 8, 256, 300, 100, False)])
+def test_lists_of_sub_ids_beside_masks(pq, N, m, b, B, K, wide):
+    assert N * B * m * m > (1.2e9 if K <= 40 or B >= 128 else 6e9)
+    codes, S, items = probs.draw_codes(N, m, b, B, 2, seed=N + m, wide=wide)
+    check_by_position(pq, codes, S, items, K)
+    S[0, 1, 5:] = -np.inf
+    S[1, 2] = -np.inf                                           # none is left
+    S[2, 0, ::2] = -np.inf
+    S[3, :2, 1:] = -np.inf                                      # a few items: fewer than asked for
+    S[4, 0, 3] = -1e30                                          # masks that are numbers
+    S[5, :2, 1:] = -1e9
+    S[6] = float(np.finfo(np.float32).min)
+    check_by_position(pq, codes, S, items, K)
+    torch.cuda.empty_cache()
