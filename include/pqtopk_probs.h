@@ -75,6 +75,9 @@ int pq_default_log_probs(const void* W, const void* queries, const int* items, l
  *   loss            out  float [B];  lse  out  float [B]   log sum_i exp(r_qi / T)
  * A position whose list has no entry of weight (or all of whose scores are -inf) has the loss 0 and adds nothing to any gradient, whatever
  * its query holds.  An entry of weight whose own score is -inf, or counts as that, makes the loss +inf, and the gradient stays finite.
+ * A list of one item has the loss -T^2 log p, so the gradient of sum_q g_q log p_{q,t_q} is that of lists of the one item t_q (of any score) with
+ * grad_loss_q = -g_q / T^2; that of several items' sum_k g_qk log p_{q,i_qk}, g_qk > 0, that of lists of these with the scores T log g_qk
+ * and grad_loss_q = -sum_k g_qk / T^2.  (The entropy's gradient has no call.)
  * Errors: PQ_ERR_NULL, PQ_ERR_SHAPE (N, B, m, b, K < 1; b too large; N >= 2^31; T no positive number), PQ_ERR_UNSUPPORTED (K > PQ_MAX_K,
  *         T out of its range, and as pq_cross_entropy()), PQ_ERR_WORKSPACE, PQ_ERR_ALIGN, PQ_ERR_HIP.
  */

@@ -241,3 +241,33 @@ def test_lists_of_sub_ids_beside_masks(pq, N, m, b, B, K, wide):
     S[6] = float(np.finfo(np.float32).min)
     check_by_position(pq, codes, S, items, K)
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("T", [0.5, 1.0, 3.0])
+def test_gradients_of_log_probabilities_are_a_distillations(pq, T):
+    # sum_qk g_qk log p_{q,i_qk} by pq_log_probs, and its gradient by the distillation from a list of these items, as the header has it, against the definition's in 64 bits
+    N, B = 3_001, 6
+    g = torch.from_numpy(np.random.default_rng(1).uniform(0.1, 2.0, (B, 3)).astype(np.float32)).cuda()
+    for n in (1, 3):
+        scores = T * g[:, :n].double().log() if n > 1 else torch.zeros((B, 1), device="cuda")
+        for first, second in (probs.draw_codes(N, 4, 256, B, 1, seed=2)[:2], probs.draw_dense(N, 64, B, 1, "f32", seed=2)[:2]):
+            items = torch.from_numpy(np.stack([np.random.default_rng(q).permutation(N)[:n] for q in range(B)]).astype(np.int32)).cuda()
+            leaf = second.double().requires_grad_()
+            if first.dtype == torch.uint8:
+                z = sum(leaf[:, k, :][:, first[:, k].long()] for k in range(4))
+                size = sum(second[:, k, :].abs().amax(1) for k in range(4)).max().item()
+            else:
+                z = leaf @ first.double().t().contiguous()
+                size = (second.double().abs() @ first.double().abs().t().contiguous()).max().item()
+            lp = torch.log_softmax(z / T, 1).gather(1, items.long())
+            objective = (g[:, :n].double() * lp).sum()
+            want, = torch.autograd.grad(objective, leaf)
+            _, lse = teaching.forward(pq, first, second, items, scores.float(), T)
+            out = teaching.backward(pq, first, second, items, scores.float(), lse, -g[:, :n].sum(1) / T ** 2, T)
+            out = out if first.dtype == torch.uint8 else out[0]
+            ours = (g[:, :n] * probs.call(pq, first, second, items, 0, T)[0]).sum()
+            # a probability is off by what its score, over T, and the log-sum are: (d + 2 + 4) u size / T and the sums' rounding; a gradient's entry adds such
+            # probabilities, g of them together at most, of either sign, times (by W phi) elements of W below 1
+            rel = U * ((2 * 66 + 8) * size / T + N / 512 + 200)
+            assert ((out.double() - want).abs() <= 4 * g.sum(1).max().item() / T * rel).all()
+            assert abs(ours.item() - objective.item()) <= g.sum().item() * 2 * rel
