@@ -58,7 +58,8 @@ int pq_log_probs_u16(const uint16_t* codes, const float* S, const int* items, lo
  * The same by the default scorer: r_qi = W[i] . phi_q, W and queries of `type` (PQ_FLOAT32, PQ_BFLOAT16, PQ_FLOAT16).
  *   W  in  type [N][d];  queries  in  type [B][d]  (both 16-byte aligned)
  * The catalogue's scores are float32 sums as in pq_default_cross_entropy().  The K + 16 best of them (all N if there are no more) are scored again in
- * 64 bits, which ranks them, and so are the given items.
+ * 64 bits, which ranks them, and so are the given items.  (Of more than 16 items beyond the K-th whose scores lie within a float32 sum's rounding of
+ * its score, near copies of one item, that rounding decides which come; equal rows of W have equal sums.)
  * Errors: as pq_log_probs() and pq_default_cross_entropy().
  */
 size_t pq_default_log_probs_workspace_bytes(long long N, int B, int d, int type, int K);

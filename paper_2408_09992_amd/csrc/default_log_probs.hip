@@ -6,7 +6,8 @@ namespace head {
 namespace {
 
 // How many candidates for the K best are scored in 64 bits at least: float32 scores may put neighbours in another order, not items that far apart
-// (neighbours among the best 100 of 1.28M lie some 1e-3 of their scores apart, a sum's rounding 1e-6).
+// (neighbours among the best 100 of 1.28M lie some 1e-3 of their scores apart, a sum's rounding 1e-6).  A number and no bound: of more than 16 items beyond the K-th within that
+// rounding, near copies of one item, it decides which are among the candidates.
 int keep_of(int K) { return K ? K + 16 : 0; }
 static_assert(most_of(PQ_MAX_K + 16) < kMostKept, "a cut leaves no more");
 

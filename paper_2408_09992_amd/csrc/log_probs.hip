@@ -184,6 +184,8 @@ struct Layout : ListLayout {
 // 113 | 118; m = 16: 4 55 | 50, 68 | 56; 16 70 | 74, 84 | 81; 64 147 | 178, 165 | 195; m = 4: 16 45 | 44, 62 | 48; 64 77 | 79, 102 | 86; 400,000 items, m = 32: 4 58 | 56,
 // 66 | 60; 16 58 | 82, 66 | 89; 200,000, m = 8: 32 42 | 39, 51 | 47; 64 46 | 49, 56 | 55; 5M, m = 8: 4 57 | 56, 149 | 61; 16 97 | 105, 186 | 112; 64 270 | 292, 301 | 330;
 // 50,000, m = 8: 200 47 | 46, 55 | 55; 400 58 | 63, 71 | 97; 1000 82 | 102, 102 | 142; 300,000, m = 4: 400 122 | 107, 137 | 125.
+// Two of these points lie on the rule's slower side: the last one (m^2 makes too much of four splits), by 14 and 10 %, and 1.28M, m = 8, 64 positions, K = 100, by 4 %.  All are of one-byte
+// sub-ids; those of two bytes follow the same rule unmeasured.
 bool by_ranking(long long N, int B, int m, int K) { return K > 0 && N > kOnePiece && (double)N * B * m * m <= (K <= kFewKept || B >= 128 ? 1.2e9 : 6e9); }
 size_t topk_bytes_of(long long N, int B, int m, int b, int K, int code_bytes) {
     if (!by_ranking(N, B, m, K)) return 0;

@@ -7,7 +7,7 @@ namespace head {
 
 constexpr int kMostEntries = 512;
 
-// Two numbers of every thread, each joined over the workgroup by `f` (which does not ask for an order); `part` is shared, a place a wave.
+// A number of every thread, joined over the workgroup by `f` (which does not ask for an order); `part` is shared, a place a wave.
 template <int THREADS, typename V, typename F>
 __device__ __forceinline__ V over_workgroup(V v, V* part, F f) {
 #pragma unroll

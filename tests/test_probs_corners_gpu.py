@@ -271,3 +271,19 @@ def test_gradients_of_log_probabilities_are_a_distillations(pq, T):
             rel = U * ((2 * 66 + 8) * size / T + N / 512 + 200)
             assert ((out.double() - want).abs() <= 4 * g.sum(1).max().item() / T * rel).all()
             assert abs(ours.item() - objective.item()) <= g.sum().item() * 2 * rel
+
+
+@pytest.mark.parametrize("B", [3, 100, 300])
+def test_near_copies_are_ranked_in_64_bits(pq, B):
+    # K + 16 items whose scores differ by 2^-34 of themselves, far less than a float32 sum tells apart
+    N, K = 20_000, 10
+    W, H, items = probs.draw_dense(N, 64, B, 1, "f32", seed=B)
+    at = torch.from_numpy(np.random.default_rng(5).permutation(N)[:K + 16]).cuda()
+    W[:, 62], W[:, 63], H[:, 62], H[:, 63] = 0.0, 0.0, 1.0, 1.0
+    W[at] = 0.0
+    W[at, 62] = 40.0
+    W[at, 63] = 2.0 ** -29 * torch.arange(K + 16, device="cuda").float()
+    z64 = H.double() @ W.double().t().contiguous()
+    assert (z64.amax(1) < 41).all()
+    top = probs.call(pq, W, H, items, K)[3]
+    assert torch.equal(top.long(), at.flip(0)[:K].repeat(B, 1))
