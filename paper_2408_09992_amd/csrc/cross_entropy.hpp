@@ -180,7 +180,7 @@ struct TeacherLossArgs : LossArgs {
     const float* scores;
     int K;
     float temperature;
-    double base;               // of log_sum64()
+    double to_nats;            // of log_sum64()
 };
 template <typename Args>
 __device__ __forceinline__ uint32_t code_of(const Args& a, int code_bytes, int item, int k) {
@@ -191,7 +191,7 @@ __device__ __forceinline__ uint32_t code_of(const Args& a, int code_bytes, int i
 __device__ __forceinline__ void finish_position(const TeacherLossArgs& a, float c, float s, int code_bytes, int q) {
     const int lane = threadIdx.x % kWave;
     const WaveTeacher t = wave_teacher(a.items, a.scores, q, a.K, a.N, a.temperature);
-    const double lse = log_sum64(c, s, a.base);
+    const double lse = log_sum64(c, s, a.to_nats);
     double loss = 0.0;
     if (t.any && lse != -__builtin_inf()) {
         for (int e = lane; e < a.K; e += kWave) {

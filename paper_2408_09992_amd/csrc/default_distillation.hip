@@ -22,7 +22,7 @@ struct ListArgs {
     long long N;
     int B, d, K;
     float temperature;
-    double base;               // of log_sum64()
+    double to_nats;            // of log_sum64()
     const float2* partial;     // loss: [groups][B]
     int groups;
     float *loss, *lse;
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kListThreads) void default_distillation_join_kernel
 #pragma unroll
         for (int x = 1; x < kListWaves; x *= 2) join_sums(t.x, t.y, __shfl_xor(t.x, x), __shfl_xor(t.y, x));
         if (lane == 0) {
-            lse_of_all = log_sum64(t.x, t.y, a.base);
+            lse_of_all = log_sum64(t.x, t.y, a.to_nats);
             a.lse[q] = (float)lse_of_all;
         }
     });
@@ -223,7 +223,7 @@ int pq_default_distillation(const void* W, const void* queries, const int* teach
     a.W = W; a.H = queries; a.N = N; a.B = B; a.d = d; a.scale = (float)(kLog2eDouble / temperature);
     a.item_tiles = p.item_tiles; a.tiles_each = p.tiles_each; a.groups = p.groups; a.position_tiles = p.position_tiles;
     a.partial = static_cast<float2*>(workspace);
-    const ListArgs l{W, queries, teacher_items, teacher_scores, N, B, d, K, temperature, base_of(a.scale, temperature), a.partial, p.groups, loss, lse, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0};
+    const ListArgs l{W, queries, teacher_items, teacher_scores, N, B, d, K, temperature, 1.0 / base_of(a.scale, temperature), a.partial, p.groups, loss, lse, nullptr, nullptr, nullptr, nullptr, nullptr, 0, 0};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return pqk::record_hip_error(type == PQ_FLOAT32 ? forward<float>(p, a, l, st) : type == PQ_BFLOAT16 ? forward<__bf16>(p, a, l, st) : forward<_Float16>(p, a, l, st));
 }
@@ -256,7 +256,7 @@ int pq_default_distillation_backward(const void* W, const void* queries, const i
     int* entry_items = reinterpret_cast<int*>(ws + at.items_at);
     float* entry_values = reinterpret_cast<float*>(ws + at.values_at);
     a.share = share; a.entry_items = entry_items; a.entry_values = entry_values; a.entries = K;
-    const ListArgs l{W, queries, teacher_items, teacher_scores, N, B, d, K, temperature, base_of(a.scale, temperature), nullptr, 0, nullptr, nullptr, lse, grad_loss, share, entry_items, entry_values, p.few ? few_items(d) : 0, p.few ? p.slices : 0};
+    const ListArgs l{W, queries, teacher_items, teacher_scores, N, B, d, K, temperature, 0.0, nullptr, 0, nullptr, nullptr, lse, grad_loss, share, entry_items, entry_values, p.few ? few_items(d) : 0, p.few ? p.slices : 0};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return pqk::record_hip_error(type == PQ_FLOAT32 ? backward<float>(p, a, l, st) : type == PQ_BFLOAT16 ? backward<__bf16>(p, a, l, st) : backward<_Float16>(p, a, l, st));
 }

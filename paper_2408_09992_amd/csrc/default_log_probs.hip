@@ -112,7 +112,7 @@ int pq_default_log_probs(const void* W, const void* queries, const int* items, l
     a.partial = reinterpret_cast<float4*>(ws);
     a.partials = l.sums.slots;
     a.lists = l.lists(ws, l.passes.keep);
-    const DenseFinishArgs f{W, queries, items, N, B, d, n, K, 1.0 / temperature, base_of(a.scale, temperature), a.partial, l.sums.slots, 0, 0, 0, a.lists, log_probs, entropy, lse, top_items, top_log_probs};
+    const DenseFinishArgs f{W, queries, items, N, B, d, n, K, 1.0 / temperature, 1.0 / base_of(a.scale, temperature), a.partial, l.sums.slots, 0, 0, 0, a.lists, log_probs, entropy, lse, top_items, top_log_probs};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return pqk::record_hip_error(type == PQ_FLOAT32 ? pass<float>(l, a, f, type, st) : type == PQ_BFLOAT16 ? pass<__bf16>(l, a, f, type, st) : pass<_Float16>(l, a, f, type, st));
 }

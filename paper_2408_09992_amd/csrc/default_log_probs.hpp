@@ -166,7 +166,7 @@ struct DenseFinishArgs {
     const int* items;
     long long N;
     int B, d, n, K;
-    double per_temperature, base;                      // 1 / T; of log_sum64()
+    double per_temperature, to_nats;                   // 1 / T; of log_sum64()
     const float4* partial;     // [B][groups], of all pieces
     int groups, stored, regions;                       // groups of all pieces; of the last piece what cut_list() takes
     long long region;
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(THREADS) void default_log_probs_finish_kernel(Dense
         float4 v = sums[lane % kWaves];
         join_wave<kWaves>(v.x, v.y, v.z);
         if (lane == 0) {
-            lse_of_all = log_sum64(v.x, v.y, a.base);
+            lse_of_all = log_sum64(v.x, v.y, a.to_nats);
             a.lse[q] = (float)lse_of_all;
             a.entropy[q] = entropy_of(v.y, v.z);
         }

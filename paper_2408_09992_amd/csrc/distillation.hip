@@ -38,7 +38,7 @@ int distil(const CT* codes, const float* S, const int* items, const float* score
     if (ws_bytes < loss_workspace(p, B)) return PQ_ERR_WORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const float scale = (float)(kLog2eDouble / temperature);
-    const TeacherLossArgs a{{codes, S, nullptr, N, B, m, b, p.share, static_cast<float2*>(ws), loss, lse, scale}, items, scores, K, temperature, base_of(scale, temperature)};
+    const TeacherLossArgs a{{codes, S, nullptr, N, B, m, b, p.share, static_cast<float2*>(ws), loss, lse, scale}, items, scores, K, temperature, 1.0 / base_of(scale, temperature)};
     return record_hip_error(launch_loss<CT>(p, a, st));
 }
 

@@ -83,10 +83,10 @@ __device__ __forceinline__ float log_sum(float c, float s) {
     return s == 0.0f ? -__builtin_inff() : s < __builtin_inff() ? (c + __log2f(s)) * kLn2 : __builtin_nanf("");
 }
 
-// The same in 64 bits: reference and logarithm of some 20 each lose no bits to their sum.  base: what scores were multiplied with, times T.  That factor is log2 e / T
-// rounded to 24 bits, so by log2 e itself the log-sum would be off by up to 2^-24 of itself, and a score over T less it by as much.
-__device__ __forceinline__ double log_sum64(float c, float s, double base) {
-    return s == 0.0f ? -__builtin_inf() : s < __builtin_inff() ? ((double)c + log2((double)s)) / base : __builtin_nan("");
+// The same in 64 bits: reference and logarithm of some 20 each lose no bits to their sum.  to_nats: 1 over what scores were multiplied with, times T.  That factor is
+// log2 e / T rounded to 24 bits, so by ln 2 itself the log-sum would be off by up to 2^-24 of itself, and a score over T less it by as much.
+__device__ __forceinline__ double log_sum64(float c, float s, double to_nats) {
+    return s == 0.0f ? -__builtin_inf() : s < __builtin_inff() ? ((double)c + log2((double)s)) * to_nats : __builtin_nan("");
 }
 inline double base_of(float scale, float temperature) { return (double)scale * (double)temperature; }
 

@@ -25,7 +25,7 @@ struct FinishArgs {
     const int* items;
     long long N;
     int B, m, b, n, K, code_bytes;
-    double per_temperature, base;                      // 1 / T; of log_sum64()
+    double per_temperature, to_nats;                   // 1 / T; of log_sum64()
     const float4* partial;     // [B][shares]
     int shares, stored, regions;                       // shares of all pieces; of the last piece what cut_list() takes
     long long region;
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(THREADS) void log_probs_finish_kernel(FinishArgs a)
         float4 v = sums[lane % kWaves];                        // (64-bit logarithms, by one wave)
         join_wave<kWaves>(v.x, v.y, v.z);
         if (lane == 0) {
-            lse_of_all = log_sum64(v.x, v.y, a.base);
+            lse_of_all = log_sum64(v.x, v.y, a.to_nats);
             a.lse[q] = (float)lse_of_all;
             a.entropy[q] = entropy_of(v.y, v.z);
         }
@@ -262,7 +262,7 @@ int log_probs(const CT* codes, const float* S, const int* items, long long N, in
         if (rc != PQ_OK) return rc;
     }
     if (e == hipSuccess) {
-        const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), 1.0 / temperature, base_of(a.scale, temperature), reinterpret_cast<const float4*>(ws), l.sums.slots,
+        const FinishArgs f{codes, S, items, N, B, m, b, n, K, (int)sizeof(CT), 1.0 / temperature, 1.0 / base_of(a.scale, temperature), reinterpret_cast<const float4*>(ws), l.sums.slots,
                            a.store ? (int)N : 0, p.shares, p.share, lists, ranked, out, entropy, lse, top_items, top_log_probs};
         if (many_lists(B) || lists.keep == 0) hipLaunchKernelGGL(log_probs_finish_kernel<256>, dim3(B), dim3(256), 0, st, f);
         else hipLaunchKernelGGL(log_probs_finish_kernel<1024>, dim3(B), dim3(1024), 0, st, f);
