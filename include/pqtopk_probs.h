@@ -105,7 +105,10 @@ int pq_distillation_u16_backward(const uint16_t* codes, const float* S, const in
 
 /*
  * Distillation of the default scorer, and its gradients with respect to queries and W (each in `type`, every element written).  Arithmetic,
- * what dz is held in and its limits are those of pq_default_cross_entropy() and its gradient, with T grad_loss for the positions' weights.
+ * what dz is held in and its limits are those of pq_default_cross_entropy() and its gradient, with T grad_loss for the positions' weights;
+ * of 33 to 64 positions of 16 bits and up to 512 elements (float16: 72 and more) listed items' dz, too, is held with what its rounding leaves.
+ * Of more positions of 16 bits it is rounded to their type: the gradients are then off by up to two roundings of it instead of one, sqrt(2) of
+ * one in the mean square.  Float32 W and queries have it in float32.
  * A list that holds a NaN or +inf makes its position's row of dqueries NaN, and the rows of dW of the items that it names.
  * Errors: as pq_distillation() and pq_default_cross_entropy().
  */

@@ -871,10 +871,16 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseA
     }
 }
 
+// Whether LDS has room for what dz's rounding leaves beside dz (float16 has two of each: over the rows' own weights and over the largest).
+template <typename T, int D> constexpr bool kKeepsRest = !kOwnPowers<T> || D > 64;
+
 // D: d rounded up to 64, 128, 256 or 512.  A tile holds 16384 / D items.  Bound by memory: W in, dW out, 2.6 GB for 1.27M items
 // of 512 elements in 515 to 550 us, 4.7 to 5.1 TB/s, where a copy reaches 4.73.
 // PARTS: two rows of dz a position (kTwoParts), in the place of the other 32 positions.
-// DISTIL: dz of a tile's items that are listed is put right in LDS.  A lane of a workgroup's first wave goes along its position's list, which is in
+// DISTIL: a listed item's dz is a teacher's whole weight in one value, and its row of dW little more than that times one row of the queries.  So tiles that hold listed items keep what dz's
+// rounding leaves here too, and add its products: 64 positions of 1.27M items of 512 bfloat16, lists of 100 (a sixth of the tiles), a step 804 to 842 us, the gradients' error 0.0024 to
+// 0.0017, which is their own rounding.  (All tiles: 900 us.)
+// dz of a tile's items that are listed is put right in LDS.  A lane of a workgroup's first wave goes along its position's list, which is in
 // the order of the workgroups and of the items of each (few_owner), with the next two entries in registers.
 template <typename T, int D, bool PARTS, bool DISTIL>
 __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a) {
@@ -887,6 +893,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
     __shared__ __align__(16) unsigned char dz_over_top[kOwn ? kFew * IT * 2 : 16];
     __shared__ float over_top[kFew];
     unsigned char* dz_w = kOwn ? dz_over_top : dz;
+    // what dz's rounding leaves in a tile that holds listed items
+    constexpr bool kRest = kKeepsRest<T, D> && DISTIL && !PARTS;
+    __shared__ __align__(16) unsigned char rest[kRest ? kFew * IT * 2 : 16], rest_over_top[kRest && kOwn ? kFew * IT * 2 : 16];
+    unsigned char* rest_w = kOwn ? rest_over_top : rest;
     __shared__ RowInfo info[kFew];
     __shared__ int target[kFew];
     const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -948,6 +958,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         bring_rows<T, D, kLoadsW>(a.W, a.d, min(tile + gridDim.x, tiles - 1) * IT, a.N, turn % 2 ? w0 : w1);
 
+        const bool exact = kRest && listed[turn % 2];          // (the same for all waves)
         // z and dz: blocks of 16 items x 16 rows
         constexpr int kBlocksZ = IT / 16 * 4 / kWaves;
 #pragma unroll
@@ -961,7 +972,7 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
             const int first = item0 + lane / 16 * 4;
             const long long hit = (long long)target[pos] - (tile * IT + first), left = a.N - (tile * IT + first);
             typedef T T4 __attribute__((ext_vector_type(4)));
-            T4 v, u;
+            T4 v, u, v_rest, u_rest;
             const float over = kOwn ? over_top[pos] : 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -970,13 +981,19 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
                 if (e >= left) p = 0.0f;
                 v[e] = (T)(p * r.scale);
                 if (PARTS && pos >= a.B) v[e] = (T)fmaf(p, r.scale, -(float)v[e]);
+                if (exact) v_rest[e] = (T)fmaf(p, r.scale, -(float)v[e]);
                 if (kOwn) {
                     u[e] = (T)(p * over);
                     if (PARTS && pos >= a.B) u[e] = (T)fmaf(p, over, -(float)u[e]);
+                    if (exact) u_rest[e] = (T)fmaf(p, over, -(float)u[e]);
                 }
             }
             *reinterpret_cast<T4*>(dz + RowsI::at(pos, first / 8) + first % 8 * 2) = v;
             if (kOwn) *reinterpret_cast<T4*>(dz_w + RowsI::at(pos, first / 8) + first % 8 * 2) = u;
+            if (exact) {
+                *reinterpret_cast<T4*>(rest + RowsI::at(pos, first / 8) + first % 8 * 2) = v_rest;
+                if (kOwn) *reinterpret_cast<T4*>(rest_w + RowsI::at(pos, first / 8) + first % 8 * 2) = u_rest;
+            }
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (DISTIL && listed[turn % 2]) {                      // (the same for all waves)
@@ -988,8 +1005,10 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
                     const T v = (T)(p * r.scale);
                     *reinterpret_cast<T*>(dz + RowsI::at(lane, at / 8) + at % 8 * 2) = v;
                     if (PARTS) *reinterpret_cast<T*>(dz + RowsI::at(lane + a.B, at / 8) + at % 8 * 2) = (T)fmaf(p, r.scale, -(float)v);
+                    if constexpr (kRest) *reinterpret_cast<T*>(rest + RowsI::at(lane, at / 8) + at % 8 * 2) = (T)fmaf(p, r.scale, -(float)v);
                     if (kOwn) {
                         const T u = (T)(p * over_top[lane]);
+                        if constexpr (kRest) *reinterpret_cast<T*>(rest_w + RowsI::at(lane, at / 8) + at % 8 * 2) = (T)fmaf(p, over_top[lane], -(float)u);
                         *reinterpret_cast<T*>(dz_w + RowsI::at(lane, at / 8) + at % 8 * 2) = u;
                         if (PARTS) *reinterpret_cast<T*>(dz_w + RowsI::at(lane + a.B, at / 8) + at % 8 * 2) = (T)fmaf(p, over_top[lane], -(float)u);
                     }
@@ -1003,25 +1022,33 @@ __global__ __launch_bounds__(kFewThreads, 2) void default_few_kernel(DenseArgs a
         }
 
         if (D / 16 >= kWaves || wave < D / 16) {
+#pragma unroll 1
+            for (int part = 0; part <= (int)exact; ++part) {
+                const unsigned char* from = part == 0 ? dz : rest;
 #pragma unroll
-            for (int k = 0; k < IT / 16; ++k) {
-                const s16x8 x = RowsI::along(dz, h_pos + lane % 32, 2 * k + lane / 32);
+                for (int k = 0; k < IT / 16; ++k) {
+                    const s16x8 x = RowsI::along(from, h_pos + lane % 32, 2 * k + lane / 32);
 #pragma unroll
-                for (int i = 0; i < kBlocksH; ++i) {
-                    const s16x8 xs[1] = {x}, ys[1] = {RowsD::across(w, 16 * k, h_col + 32 * i)};
-                    f32x16 c[1][1] = {{dh[i]}};
-                    multiply<T, 1, 1>(xs, ys, c);
-                    dh[i] = c[0][0];
+                    for (int i = 0; i < kBlocksH; ++i) {
+                        const s16x8 xs[1] = {x}, ys[1] = {RowsD::across(w, 16 * k, h_col + 32 * i)};
+                        f32x16 c[1][1] = {{dh[i]}};
+                        multiply<T, 1, 1>(xs, ys, c);
+                        dh[i] = c[0][0];
+                    }
                 }
             }
         }
         // dW: the wave's 32 items x 64 elements
         const int w_item = wave * 2 / (D / 32) * 32, w_col = wave * 2 % (D / 32) * 32;
         f32x16 dw[1][2] = {{f32x16{}, f32x16{}}};
+#pragma unroll 1
+        for (int part = 0; part <= (int)exact; ++part) {
+            const unsigned char* from = part == 0 ? dz_w : rest_w;
 #pragma unroll
-        for (int k = 0; k < kFew / 16; ++k) {
-            const s16x8 x[1] = {RowsI::across(dz_w, 16 * k, w_item)}, y[2] = {RowsD::across(h, 16 * k, w_col), RowsD::across(h, 16 * k, w_col + 32)};
-            multiply<T, 1, 2>(x, y, dw);
+            for (int k = 0; k < kFew / 16; ++k) {
+                const s16x8 x[1] = {RowsI::across(from, 16 * k, w_item)}, y[2] = {RowsD::across(h, 16 * k, w_col), RowsD::across(h, 16 * k, w_col + 32)};
+                multiply<T, 1, 2>(x, y, dw);
+            }
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");       // (nobody reads the tile any more: it is the waves' own memory now)
         unsigned char* own = w + wave * 4096;
