@@ -619,7 +619,7 @@ __device__ __forceinline__ void bring_rows(const void* base, int d, long long ro
 
 // The sums of up to 64 positions of 16-bit operands, d <= 512, over the items from..end - 1: a workgroup a compute unit, tiles of 32 KB of W by turns.
 // What a wave multiplies of the queries stays in its registers (64 of them; 32 for D = 64), so that LDS holds four tiles, three of them on their way: 24 MB
-// in flight over the chip, where the memory's rate times its latency is some 13: the loss of 64 positions, 1.3 GB of W, 222 us, 5.9 TB/s (two tiles in LDS beside the queries: 237).  Every lane's products and sums are in the order of the tiles.
+// in flight over the chip, where the memory's rate times its latency is some 13: the loss of 64 positions, 1.3 GB of W, 222 to 240 us on two cards (two tiles in LDS beside the queries: 237 to 243).  Every lane's products and sums are in the order of the tiles.
 // PROBS: the entropy's sum besides, and scores over the floors (all of a first piece: a.store) to the lists.  Candidates wait in LDS until the tiles are
 // done, as a store between the loads would have to be waited for with them.
 constexpr int kFewWaiting = 1024;

@@ -31,7 +31,7 @@ struct DenseProbsArgs {
 template <typename Tile, int ITEMS> constexpr int kShares = ITEMS / (32 * Tile::MI) * 2;
 
 // grid: groups of tiles of items x tiles of positions, one of which a chiplet takes one after the other (chiplet_order).  Bound by the matrix cores and the exponentials between the
-// products: 262,144 items of 512 bfloat16 and 1024 positions 305 to 314 us, 880 to 900 TFLOP/s with the candidates (the loss alone 920).
+// products: 262,144 items of 512 bfloat16 and 1024 positions 305 to 339 us on three cards, 811 to 900 TFLOP/s with the candidates (the loss alone 860 to 930).
 template <typename T, int BN, int ITEMS>
 __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_log_probs_kernel(DenseProbsArgs a) {
     using Tile = ScoresTile<T, BN, ITEMS>;

@@ -5,8 +5,8 @@
 //
 // The pass is the cross entropy's (cross_entropy.hpp) with one more sum.  The likeliest items come from it too, what scores pass a position's floor going to
 // its list (alternatives.hpp), or, where the lookups are few, from the ranking's own scan, whose bounds of one byte need no first piece and no cut (by_ranking()).
-// Bound by the lookups in LDS and the exponentials beside them: 512 positions of 1.28M items, m = 8, K = 100, 517 to 553 us; two launches of 6.9 and 5.9 us for one
-// position of 10,000.
+// Bound by the vector units, with the lookups in LDS close behind: 64 positions of 1.27M items, m = 8, one and a half times the loss's vector instructions, whose issue takes all of the time
+// (80 % of the loss's), LDS busy 84 % of it (89 %).  512 positions, K = 100, 517 to 553 us; two launches of 6.8 and 5.7 us for one position of 10,000.
 #include "pqtopk_probs.h"
 #include "cross_entropy.hpp"
 
