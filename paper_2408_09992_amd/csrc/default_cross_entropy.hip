@@ -160,7 +160,7 @@ int pq_default_cross_entropy(const void* W, const void* queries, const int* targ
     if ((((uintptr_t)W | (uintptr_t)queries | (uintptr_t)workspace) & 15) || (((uintptr_t)targets | (uintptr_t)loss | (uintptr_t)lse) & 3)) return PQ_ERR_ALIGN;
     const DensePlan p = plan_dense(N, B, d, type);
     if (workspace_bytes < loss_bytes(p, B)) return PQ_ERR_WORKSPACE;
-    DenseArgs a{};
+    DenseLossArgs a{};
     a.W = W; a.H = queries; a.targets = targets; a.N = N; a.B = B; a.d = d; a.scale = kLog2e;
     a.item_tiles = p.item_tiles; a.tiles_each = p.tiles_each; a.groups = p.groups; a.position_tiles = p.position_tiles;
     a.partial = static_cast<float2*>(workspace); a.loss = loss; a.lse = lse;

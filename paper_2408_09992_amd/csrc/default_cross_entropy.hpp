@@ -65,19 +65,25 @@ __device__ __forceinline__ void chiplet_order(int id, int inner_tiles, int& oute
 // How many of a wave's `rows` rows there are, given how many follow its first one.
 __device__ __forceinline__ int left_of(long long rest, int rows) { return (int)max(0LL, min(rest, (long long)rows)); }
 
-struct DenseArgs {
+// (Arguments of the loss and of the gradient apart: a kernel's arguments come from memory, and 280 bytes of them instead of 232 took the gradient of 34,742 items of 256 bfloat16 and 203
+// positions, five launches, 2 % of 44 us.)
+struct DenseInputs {
     const void *W, *H;
     const int* targets;
     long long N;
     int B, d;
-    // loss
-    long long item_tiles;
+    float scale;                                       // what scores are multiplied with: log2 e over the temperature
+};
+struct DenseLossArgs : DenseInputs {
     int tiles_each, groups, position_tiles;
+    long long item_tiles;
     float2* partial;                                   // [groups][B]
     float *loss, *lse;
-    // gradient
-    const float *lse_in, *grad;
+};
+struct DenseArgs : DenseInputs {
     int parts;                                         // rows of dz that a position has (see dz_rows)
+    const float *lse_in, *grad;
+    double base;                                       // what takes lse to where scores times `scale` are: scale over 1 / T
     RowInfo* info;                                     // [rows of dz, padded]
     void* live;                                        // [rows of dz][d]: the queries, zeros where a position adds nothing
     float* factor;                                     // what dW is multiplied with
@@ -91,25 +97,24 @@ struct DenseArgs {
     int padded, slices, slice_items, more;             // rows of dz padded; shares of a piece's items; partial_h holds earlier pieces
     int tiles_m, tiles_n;                              // of the launch
     int h_rows, h_cols, w_blocks;                      // tiles of dH; workgroups that make dW, where one launch makes both
-    float scale;                                       // what scores are multiplied with: log2 e over the temperature
-    double base;                                       // what takes lse to where scores times `scale` are: scale over 1 / T
     // distillation: a position's gradient over its dz (0: it adds nothing; NULL: grad of those that have targets), and the entries of its
     // list, by item (kNoItem after the last): what p less the teacher's probability is there
+    int entries;
     const float* share;
     const int* entry_items;                            // [B][entries]
     const float* entry_values;
-    int entries;
 };
+static_assert(sizeof(DenseArgs) <= 240, "what a launch of the gradient brings");
 constexpr int kNoItem = 0x7FFFFFFF;
 // Which of `groups` workgroups of default_few_kernel has an item, tiles of `of` items taken by turns.
 __device__ __forceinline__ int few_owner(int item, int of, int groups) { return item == kNoItem ? kNoItem : item / of % groups; }
 
 template <typename T>
-__device__ __forceinline__ Operand items_of(const DenseArgs& a, long long item) {
+__device__ __forceinline__ Operand items_of(const DenseInputs& a, long long item) {
     return Operand{a.W, (size_t)a.d * sizeof(T), item, a.N, 0, a.d};
 }
 template <typename T>
-__device__ __forceinline__ Operand positions_of(const DenseArgs& a, int position) {
+__device__ __forceinline__ Operand positions_of(const DenseInputs& a, int position) {
     return Operand{a.H, (size_t)a.d * sizeof(T), position, a.B, 0, a.d};
 }
 
@@ -127,7 +132,7 @@ __device__ __forceinline__ int position_of(const DenseArgs& a, int row) { return
 // Bound by the matrix cores: 1024 positions, 1.28M items of 512 bfloat16, 1.44 to 1.56 ms, 860 to 930 TFLOP/s with an exponential
 // per score; 2048 positions, 34,742 items of 512 float32, 404 to 439 us, 166 to 181 TFLOP/s (4.25 rounds of tiles).
 template <typename T, int BN, int ITEMS>
-__global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_cross_entropy_kernel(DenseArgs a) {
+__global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void default_cross_entropy_kernel(DenseLossArgs a) {
     using Tile = ScoresTile<T, BN, ITEMS>;
     constexpr int MI = Tile::MI, NI = Tile::NI, kRowWaves = ITEMS / (32 * MI);
     __shared__ float2 stat[kRowWaves][BN];
@@ -190,7 +195,7 @@ __global__ __launch_bounds__((ScoresTile<T, BN, ITEMS>::kThreads), 2) void defau
 
 // One wave per position joins the groups' sums and takes the target's score.
 template <typename T>
-__global__ __launch_bounds__(kWave) void default_cross_entropy_join_kernel(DenseArgs a) {
+__global__ __launch_bounds__(kWave) void default_cross_entropy_join_kernel(DenseLossArgs a) {
     const int q = blockIdx.x, lane = threadIdx.x;
     float c = kLowest, s = 0.0f;
     for (int i = lane; i < a.groups; i += kWave) {
@@ -802,14 +807,14 @@ __device__ __forceinline__ void few_sums(const Args& a, long long from, long lon
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kFewThreads, 2) void default_few_long_loss_kernel(DenseArgs a) { few_sums<T, D, false>(a, 0, a.N); }
+__global__ __launch_bounds__(kFewThreads, 2) void default_few_long_loss_kernel(DenseLossArgs a) { few_sums<T, D, false>(a, 0, a.N); }
 
 // The same sums where a workgroup has few tiles: queries and two tiles in LDS, and a quarter of the code, which a launch brings in, too.  Loss, us, by this kernel and by few_sums, 64
 // positions in bfloat16: 10,000 items of 64 7.3 | 7.9, of 128 7.4 | 8.2, of 256 8.0 | 8.9, of 512 10.2 | 10.5; 20,000 of 512 11.4 | 11.2; 300,000 of 256 31.2 | 31.6, of 512 61.6 | 55.7;
 // 600,000 of 64 24.2 | 24.6, of 128 31.0 | 31.2, of 256 60.3 | 54.8; 1.27M of 64 40.4 | 39.0, of 128 62.3 | 58.2.
 inline bool few_tiles_are_many(long long tiles, int groups, int d) { return tiles > (d > 256 ? 2LL : 19LL) * groups; }
 template <typename T, int D>
-__global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseArgs a) {
+__global__ __launch_bounds__(kFewThreads, 2) void default_few_loss_kernel(DenseLossArgs a) {
     constexpr int IT = kFewBytes / 2 / D, kWaves = kFewThreads / kWave;
     using RowsD = Rows<D / 8>;
     __shared__ __align__(16) unsigned char w0[kFewBytes], w1[kFewBytes], h[kFew * D * 2];
@@ -1132,12 +1137,12 @@ inline int grid_of(long long outer, long long inner) { return (int)(ceil_div(out
 constexpr int kSliceItems = 64;                        // a slice of dH's items is a multiple of this
 constexpr long long kMostJoinBlocks = 1LL << 20;       // (a launch has fewer than 2^32 threads)
 
-template <typename T> hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st);
+template <typename T> hipError_t dense_loss(const DensePlan& p, const DenseLossArgs& a, hipStream_t st);
 template <typename T> hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st);
 
 #ifdef PQ_DENSE_INSTANCE
 template <typename T, int POS, int ITEMS>
-hipError_t launch_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+hipError_t launch_loss(const DensePlan& p, const DenseLossArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((default_cross_entropy_kernel<T, POS, ITEMS>), dim3(grid_of(p.groups, p.position_tiles)), dim3(ScoresTile<T, POS, ITEMS>::kThreads), 0, st, a);
     return hipGetLastError();
 }
@@ -1176,14 +1181,14 @@ hipError_t launch_dh_cols(const DensePlan& p, const DenseArgs& a, hipStream_t st
 }
 
 template <typename T, int D>
-hipError_t launch_few_loss_of(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+hipError_t launch_few_loss_of(const DensePlan& p, const DenseLossArgs& a, hipStream_t st) {
     const dim3 grid(p.groups), threads(kFewThreads);
     if (few_tiles_are_many(ceil_div(a.N, few_items(a.d)), p.groups, a.d)) hipLaunchKernelGGL((default_few_long_loss_kernel<T, D>), grid, threads, 0, st, a);
     else hipLaunchKernelGGL((default_few_loss_kernel<T, D>), grid, threads, 0, st, a);
     return hipGetLastError();
 }
 template <typename T>
-hipError_t launch_few_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+hipError_t launch_few_loss(const DensePlan& p, const DenseLossArgs& a, hipStream_t st) {
     return a.d > 256 ? launch_few_loss_of<T, 512>(p, a, st) : a.d > 128 ? launch_few_loss_of<T, 256>(p, a, st) : a.d > 64 ? launch_few_loss_of<T, 128>(p, a, st) : launch_few_loss_of<T, 64>(p, a, st);
 }
 template <typename T, bool PARTS, bool DISTIL>
@@ -1202,7 +1207,7 @@ hipError_t launch_few(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
 }
 
 template <typename T>
-hipError_t dense_loss(const DensePlan& p, const DenseArgs& a, hipStream_t st) {
+hipError_t dense_loss(const DensePlan& p, const DenseLossArgs& a, hipStream_t st) {
     hipError_t e;
     if constexpr (sizeof(T) == 2) e = p.few ? launch_few_loss<T>(p, a, st) : hipSuccess;
     if (sizeof(T) != 2 || !p.few)
@@ -1269,7 +1274,7 @@ hipError_t dense_backward(const DensePlan& p, DenseArgs a, hipStream_t st) {
     return hipGetLastError();
 }
 
-template hipError_t dense_loss<PQ_DENSE_INSTANCE>(const DensePlan&, const DenseArgs&, hipStream_t);
+template hipError_t dense_loss<PQ_DENSE_INSTANCE>(const DensePlan&, const DenseLossArgs&, hipStream_t);
 template hipError_t dense_backward<PQ_DENSE_INSTANCE>(const DensePlan&, DenseArgs, hipStream_t);
 #endif
 

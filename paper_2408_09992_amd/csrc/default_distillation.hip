@@ -182,7 +182,7 @@ int check(long long N, int B, int d, int type, int K) {
 }
 
 template <typename T>
-hipError_t forward(const DensePlan& p, const DenseArgs& a, const ListArgs& l, hipStream_t st) {
+hipError_t forward(const DensePlan& p, const DenseLossArgs& a, const ListArgs& l, hipStream_t st) {
     const hipError_t e = dense_loss<T>(p, a, st);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((default_distillation_join_kernel<T>), dim3(a.B), dim3(kListThreads), 0, st, l);
@@ -219,7 +219,7 @@ int pq_default_distillation(const void* W, const void* queries, const int* teach
         return PQ_ERR_ALIGN;
     const DensePlan p = plan_dense(N, B, d, type);
     if (workspace_bytes < sums_bytes(p, B)) return PQ_ERR_WORKSPACE;
-    DenseArgs a{};
+    DenseLossArgs a{};
     a.W = W; a.H = queries; a.N = N; a.B = B; a.d = d; a.scale = (float)(kLog2eDouble / temperature);
     a.item_tiles = p.item_tiles; a.tiles_each = p.tiles_each; a.groups = p.groups; a.position_tiles = p.position_tiles;
     a.partial = static_cast<float2*>(workspace);
