@@ -16,8 +16,8 @@
  *   - Item ids are int32.  One outside [0, N) names no item (padding).
  *   - A position all of whose scores are -inf has lse = -inf.
  *   - Workspaces of the log-probabilities with K > 0 hold lists of scored items, 8 bytes for every position and item of a piece of the
- *     catalogue (the likeliest few come from them): up to 16,384 items are one piece, of longer catalogues the largest has most of the items,
- *     as far as 2 GiB of lists go (of more than 32,768 positions 4.3, where K is over 496).  64 positions of 1.27M items take 614 MiB, twice
+ *     catalogue (the likeliest few come from them): up to 16,384 items (and positions) are one piece, of longer catalogues the largest has most of
+ *     the items, as far as 2 GiB of lists go (of more than 32,768 positions 4.3, where K is over 496).  64 positions of 1.27M items take 614 MiB, twice
  *     what their scores would; 16 KB a position and up to 128 MiB of sums come on top.  By sub-ids and few positions there are no lists: the ranking
  *     follows the pass.
  */
